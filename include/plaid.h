@@ -279,6 +279,123 @@ int plaid_encode_residuals(const float *centroids, int64_t C, const float *x, co
 int plaid_build_ivf(const int32_t *codes, const int64_t *doc_offsets, int64_t P, int64_t N, int64_t C, int64_t *ivf_offsets,
                     int32_t *ivf_pids, int64_t capacity, int64_t *ivf_len, int device, void *hip_stream);
 
+/* ---- Reader: what answers from the passages a search has found.  A decoder's layer attends to its own tokens, which a paged
+ * cache in four bits a value holds, and to the states of the passages found.  None of these calls needs an index; every array
+ * is DEVICE memory of `device`, the calls are asynchronous on `hip_stream`, wait for nothing, allocate nothing and may be
+ * captured in a graph.  Offsets and lengths live on the device, so the kernels check them: a value that points outside an
+ * array is cut to it (what such a request gets is unspecified, nothing is accessed out of bounds). ---- */
+
+typedef enum { PLAID_BF16 = 0, PLAID_FP16 = 1 } plaid_dtype;
+
+/* Blocks and slots of a step's new tokens.  Request r holds lengths[r] tokens in its first ceil(lengths[r] / block_size) blocks
+ * and gets added[r] more (negative numbers count as 0; lengths[r] + added[r] < 2^31).  Blocks are handed out from free_blocks in
+ * its order, to request 0 first; a block past its end is -1, a block past max_blocks is neither handed out nor counted.
+ *   lengths, added  [n] int32, n >= 1
+ *   table           [n][max_blocks] int32, rows table_stride apart; the new entries are written, no other
+ *   free_blocks     [n_free] int32 (may be NULL when n_free = 0)
+ *   block_size      tokens of a block: 16, 32, 64, 128 or 256
+ *   offsets         [n+1] int64 (output) exclusive prefix sum of added
+ *   totals          [n] int32 (output) lengths + added
+ *   positions       [capacity] int32 (output) place of each new token in its request
+ *   slots           [capacity] int64 (output) block * block_size + position % block_size; -1 without a block
+ *                   both are -1 from offsets[n] on; tokens past capacity are left out
+ *   blocks_wanted   [1] int64 (output) blocks asked for in all: more than n_free means that some are missing
+ *   workspace       plaid_block_tables_workspace bytes, 16-byte aligned (may be NULL where that is 0)
+ * Errors: PLAID_EINVAL, PLAID_EHIP. */
+int plaid_block_tables(const int32_t *lengths, const int32_t *added, int32_t n, int32_t *table, int64_t table_stride,
+                       int32_t max_blocks, const int32_t *free_blocks, int32_t n_free, int32_t block_size, int64_t *offsets,
+                       int32_t *totals, int32_t *positions, int64_t *slots, int64_t capacity, int64_t *blocks_wanted,
+                       void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
+int plaid_block_tables_workspace(int32_t n, int64_t capacity, int64_t *bytes);
+
+/* A paged cache of keys and values in four bits a value.  Every 32 dimensions of a token's head share a power of two, stored
+ * as its biased exponent (255: the group holds a value that is not finite, all of it reads as NaN); a value is a sign and one
+ * of 0 0.5 1 1.5 2 3 4 6 (codes 0-7, the sign is bit 3) times that power.  data: [num_blocks][kv_heads] regions of
+ * block_size * head_dim * 17 / 16 bytes: the codes of the keys, the codes of the values, the scales of the keys, the scales of
+ * the values.  Key codes [token][head_dim / 2], the even dimension in the low half of a byte; value codes in cells of 16 tokens
+ * [token / 16][token / 4 % 4][dim % 16][dim / 32][token % 4], the halves of a byte being dimensions 32 i + m and
+ * 32 i + 16 + m; scales [token][head_dim / 32].  dtype is the type of what is written, and what it is read as. */
+typedef struct {
+    uint8_t *data; /* 16-byte aligned */
+    int64_t num_blocks;
+    int32_t block_size; /* 16, 32, 64, 128 or 256 */
+    int32_t kv_heads;
+    int32_t head_dim; /* 64 or 128 */
+    int32_t dtype;    /* plaid_dtype */
+} plaid_paged_cache;
+
+/* Writes keys and values of n tokens (k, v: rows token_stride apart, heads head_stride, both in elements and multiples of 8;
+ * 16-byte aligned) to their slots; a slot outside [0, num_blocks * block_size) is left out, two equal slots are a caller's
+ * mistake.  The power of two of a group is the smallest that keeps its largest magnitude within 6 (bf16: 2^-126 .. 2^126,
+ * fp16: 2^-23 .. 2^14), values round to the nearest code, ties to the even one, and stay finite in the type. */
+int plaid_cache_write(const plaid_paged_cache *cache, const void *k, const void *v, int64_t k_token_stride,
+                      int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int64_t *slots, int64_t n,
+                      int device, void *hip_stream);
+/* The keys and values that n slots hold, k and v [n][kv_heads][head_dim] contiguous (either may be NULL); zero for a slot
+ * outside the cache.  Exact: every code is a value of the type. */
+int plaid_cache_read(const plaid_paged_cache *cache, const int64_t *slots, int64_t n, void *k, void *v, int device,
+                     void *hip_stream);
+
+/* Arguments of an attention call.  Row (token i of request r, head h) attends with key head h * kv_heads / heads:
+ *   s_j = scale * q . k_j + key_bias_j,   out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j);
+ * a row that no key is left for gives zeros and -INFINITY.  lse is two numbers to be added, a score near the largest and the
+ * rest, so that it is whole where all scores are as low as the type goes.  Sums, softmax statistics and their exponentials are held in 32
+ * bits; the softmax's weights round to the type before they multiply the values.
+ *   q, k, v          [num_queries | num_keys][heads | kv_heads][head_dim] of dtype, 16-byte aligned, the strides of tokens and
+ *                    heads in elements and multiples of 8; k and v are those of plaid_cross_attention
+ *   key_bias         [num_keys] of dtype, or NULL; a key of bias -INFINITY takes no part, whatever k and v hold there
+ *   q_offsets        [n+1] int64: the tokens of request r are rows q_offsets[r] .. q_offsets[r+1]-1; rows outside every request
+ *                    are not written
+ *   k_offsets        [n+1] int64, the same for the keys (plaid_cross_attention)
+ *   out              [num_queries][heads][head_dim] contiguous, lse [num_queries][heads][2] fp32 or NULL
+ * heads is a multiple of kv_heads, head_dim 64 or 128; num_queries * (heads / kv_heads)^2 < 2^32. */
+typedef struct {
+    int32_t dtype;
+    int32_t n;
+    int32_t heads;
+    int32_t kv_heads;
+    int32_t head_dim;
+    float scale;
+    int64_t num_queries;
+    int64_t num_keys;
+    const void *q;
+    const void *k;
+    const void *v;
+    const void *key_bias;
+    int64_t q_token_stride;
+    int64_t q_head_stride;
+    int64_t k_token_stride;
+    int64_t k_head_stride;
+    int64_t v_token_stride;
+    int64_t v_head_stride;
+    const int64_t *q_offsets;
+    const int64_t *k_offsets;
+    void *out;
+    float *lse;
+} plaid_attention;
+
+/* Attention over a paged cache.  Request r's keys are the lengths[r] tokens that its row of `table` ([n][max_blocks] int32, rows
+ * table_stride apart) leads to; a block id outside the cache hides its tokens.  causal != 0: the request's queries are its last
+ * tokens, in order, and query i of m sees the first lengths[r] - m + i + 1.  k, v, key_bias, num_keys and k_offsets of *args are
+ * not looked at; kv_heads, head_dim and dtype are the cache's.
+ * workspace: plaid_cached_attention_workspace bytes, 16-byte aligned. */
+int plaid_cached_attention(const plaid_attention *args, const plaid_paged_cache *cache, const int32_t *table,
+                           int64_t table_stride, int32_t max_blocks, const int32_t *lengths, int32_t causal, void *workspace,
+                           int64_t workspace_bytes, int device, void *hip_stream);
+int plaid_cached_attention_workspace(const plaid_attention *args, int32_t max_blocks, int32_t block_size, int64_t *bytes);
+
+/* Attention to states of another length (an encoder's, or those of the passages found: plaid_decompress_passages' offsets are
+ * k_offsets, taken once a request).  workspace: plaid_cross_attention_workspace bytes (backward = 0), 16-byte aligned. */
+int plaid_cross_attention(const plaid_attention *args, void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
+/* Its gradients: with P = exp(s - lse), dP = d_out . v and dS = P (dP - d_out . out),
+ *   dv_j = sum P d_out,  dk_j = scale sum dS q,  dq_i = scale sum_j dS k,  dbias_j = sum of dS over all rows and heads.
+ * args->out and args->lse are what the forward call gave; d_out [num_queries][heads][head_dim] contiguous; dq like d_out, dk and
+ * dv [num_keys][kv_heads][head_dim] contiguous, dbias [num_keys], all of dtype; each may be NULL.  Every sum has one order: the
+ * same inputs give the same bits.  fp16: the gradient's range is the type's, so the caller scales the loss. */
+int plaid_cross_attention_backward(const plaid_attention *args, const void *d_out, void *dq, void *dk, void *dv, void *dbias,
+                                   void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
+int plaid_cross_attention_workspace(const plaid_attention *args, int32_t backward, int64_t *bytes);
+
 /* Thread-local message describing the most recent error on the calling thread ("" if none). */
 const char *plaid_last_error(void);
 

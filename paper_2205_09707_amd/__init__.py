@@ -30,3 +30,12 @@ from .plaid import (  # noqa: F401
     plaid_set_stage_timing,
     plaid_workspace_bytes,
 )
+from .reader import (  # noqa: F401
+    PagedCache,
+    plaid_block_tables,
+    plaid_cache_read,
+    plaid_cache_write,
+    plaid_cached_attention,
+    plaid_cross_attention,
+    plaid_cross_attention_backward,
+)

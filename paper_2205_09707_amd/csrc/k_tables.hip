@@ -1,0 +1,155 @@
+// Block tables and slots of a step's new tokens, from the requests' lengths.
+#include "reader.h"
+
+// Two prefix sums over the requests (tokens, blocks) and a pass over the tokens, which is all writing: 12 bytes a token.  Up to
+// TABLES_ONE requests each workgroup forms both sums in LDS for itself, so that a step needs one launch and no workspace; the
+// sums cost it 8 n bytes from L2, its tokens 12 KB of writes.  More requests take a launch that leaves the sums in the workspace.
+#define TABLES_ONE 2048
+#define TABLES_THREADS 256
+#define TABLES_TOKENS 4  // neighbouring tokens of a thread: 16-byte stores
+
+struct Growth {
+    int64_t old, added, have, want;
+};
+__device__ __forceinline__ Growth growth(const TablesArgs &t, int r)
+{
+    Growth g;
+    g.old = max(t.lengths[r], 0);
+    g.added = max(t.added[r], 0);
+    const int64_t round = (1ll << t.block_shift) - 1;
+    g.have = min((g.old + round) >> t.block_shift, (int64_t)t.max_blocks);
+    g.want = min((g.old + g.added + round) >> t.block_shift, (int64_t)t.max_blocks) - g.have;
+    return g;
+}
+
+// Exclusive prefix sums of all requests by one workgroup; out[n] is the total.
+__device__ __forceinline__ void scan_requests(const TablesArgs &t, int64_t *tokens, int64_t *blocks)
+{
+    __shared__ int64_t wave_sum[2][TABLES_THREADS / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t done[2] = {0, 0};
+    for (int r0 = 0; r0 < t.n; r0 += TABLES_THREADS) {
+        const int r = r0 + threadIdx.x;
+        int64_t mine[2] = {0, 0}, sum[2];
+        if (r < t.n) {
+            const Growth g = growth(t, r);
+            mine[0] = g.added, mine[1] = g.want;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            sum[k] = mine[k];
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int64_t y = __shfl_up(sum[k], o);
+                if (lane >= o) sum[k] += y;
+            }
+            if (lane == 63) wave_sum[k][wave] = sum[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            int64_t before = done[k];
+#pragma unroll
+            for (int w = 0; w < TABLES_THREADS / 64; ++w) {
+                if (w < wave) before += wave_sum[k][w];
+                done[k] += wave_sum[k][w];
+            }
+            if (r < t.n) (k ? blocks : tokens)[r] = before + sum[k] - mine[k];
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) tokens[t.n] = done[0], blocks[t.n] = done[1];
+}
+
+// The last request whose sum is <= x (sums ascend from 0, x < sums[n]).
+__device__ __forceinline__ int owner(const int64_t *sums, int n, int64_t x)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (sums[mid] <= x) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ void fill(const TablesArgs &t, const int64_t *tokens, const int64_t *blocks)
+{
+    const int64_t first = (int64_t)blockIdx.x * TABLES_THREADS + threadIdx.x, stride = (int64_t)gridDim.x * TABLES_THREADS;
+    if (first == 0) t.blocks_wanted[0] = blocks[t.n];
+    for (int64_t r = first; r <= t.n; r += stride) {
+        t.offsets[r] = tokens[r];
+        if (r < t.n) t.totals[r] = max(t.lengths[r], 0) + max(t.added[r], 0);
+    }
+    for (int64_t j = first; j < blocks[t.n]; j += stride) {
+        const int r = owner(blocks, t.n, j);
+        t.table[r * t.table_stride + growth(t, r).have + j - blocks[r]] = j < t.n_free ? t.free_blocks[j] : -1;
+    }
+    const int64_t all = min(tokens[t.n], t.capacity);
+    for (int64_t i = first * TABLES_TOKENS; i < t.capacity; i += stride * TABLES_TOKENS) {
+        int position[TABLES_TOKENS];
+        int64_t slot[TABLES_TOKENS];
+        int r = i < all ? owner(tokens, t.n, i) : 0;
+        Growth g = growth(t, r);
+        int64_t block = -1, id = -1;
+#pragma unroll
+        for (int k = 0; k < TABLES_TOKENS; ++k) {
+            position[k] = -1;
+            slot[k] = -1;
+            if (i + k >= all) continue;
+            if (i + k >= tokens[r + 1]) {
+                do ++r;
+                while (i + k >= tokens[r + 1]);
+                g = growth(t, r);
+                block = -1;
+            }
+            const int64_t at = g.old + i + k - tokens[r], b = at >> t.block_shift;
+            if (b != block) {
+                block = b, id = -1;
+                if (b < g.have) {
+                    id = t.table[r * t.table_stride + b];
+                } else if (b < g.have + g.want) {
+                    const int64_t j = blocks[r] + b - g.have;
+                    if (j < t.n_free) id = t.free_blocks[j];
+                }
+            }
+            position[k] = (int)at;
+            slot[k] = id < 0 ? -1 : (id << t.block_shift) + (at & ((1 << t.block_shift) - 1));
+        }
+        if (i + TABLES_TOKENS <= t.capacity) {
+            *(i32x4 *)(t.positions + i) = i32x4{position[0], position[1], position[2], position[3]};
+            typedef __attribute__((ext_vector_type(2))) long long i64x2;
+            *(i64x2 *)(t.slots + i) = i64x2{slot[0], slot[1]};
+            *(i64x2 *)(t.slots + i + 2) = i64x2{slot[2], slot[3]};
+        } else {
+#pragma unroll
+            for (int k = 0; k < TABLES_TOKENS; ++k)
+                if (i + k < t.capacity) t.positions[i + k] = position[k], t.slots[i + k] = slot[k];
+        }
+    }
+}
+
+__global__ __launch_bounds__(TABLES_THREADS) void tables_one_kernel(TablesArgs t)
+{
+    __shared__ int64_t tokens[TABLES_ONE + 1], blocks[TABLES_ONE + 1];
+    scan_requests(t, tokens, blocks);
+    __syncthreads();
+    fill(t, tokens, blocks);
+}
+__global__ __launch_bounds__(TABLES_THREADS) void tables_scan_kernel(TablesArgs t) { scan_requests(t, t.scan, t.scan + t.n + 1); }
+__global__ __launch_bounds__(TABLES_THREADS) void tables_fill_kernel(TablesArgs t) { fill(t, t.scan, t.scan + t.n + 1); }
+
+int64_t plaid_block_tables_scan_bytes(int32_t n, int64_t) { return n > TABLES_ONE ? 2 * ((int64_t)n + 1) * 8 : 0; }
+
+void plaid_launch_block_tables(hipStream_t st, const TablesArgs &t)
+{
+    const int64_t per = TABLES_THREADS * TABLES_TOKENS;
+    int64_t groups = (t.capacity + per - 1) / per;
+    groups = groups < 1 ? 1 : groups > 1024 ? 1024 : groups;
+    if (t.n <= TABLES_ONE) {
+        tables_one_kernel<<<dim3((unsigned)groups), dim3(TABLES_THREADS), 0, st>>>(t);
+    } else {
+        tables_scan_kernel<<<dim3(1), dim3(TABLES_THREADS), 0, st>>>(t);
+        tables_fill_kernel<<<dim3((unsigned)groups), dim3(TABLES_THREADS), 0, st>>>(t);
+    }
+}

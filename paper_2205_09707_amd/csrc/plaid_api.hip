@@ -28,6 +28,14 @@ static int fail(int code, const char *fmt, ...)
     return code;
 }
 extern "C" const char *plaid_last_error(void) { return g_err; }
+int plaid_fail(int code, const char *fmt, ...)  // for the other translation units
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return code;
+}
 
 #define HIP_TRY(expr)                                                                                         \
     do {                                                                                                      \

@@ -1,0 +1,251 @@
+// Declarations shared by the kernels of the reader: block tables, the cache in four bits, attention (gfx950 only).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "plaid.h"
+
+int plaid_fail(int code, const char *fmt, ...);  // sets plaid_last_error's text and returns code
+
+// ---------------------------------------------------------------------------------------------
+// Arguments of the attention kernels (by value).  Rows of a request and key head are its tokens and the group's heads, row
+// t * group + g, so that heads that share keys share the tiles of them.
+// ---------------------------------------------------------------------------------------------
+struct AttendArgs {
+    const char *q, *k, *v;             // elements of 16 bits
+    const char *bias;                  // [num_keys] of the type, or null
+    const int64_t *q_offsets, *k_offsets;
+    char *out;
+    float *lse;                        // pairs whose sum is the logarithm; may be null
+    int64_t num_queries, num_keys;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;  // strides in bytes
+    int32_t n, heads, kv_heads, group;
+    uint32_t group_magic;              // ceil(2^32 / group): row / group = umulhi(row, magic) for group > 1
+    float scale;                       // >= 0: negate_q carries the sign
+    uint32_t negate_q;                 // 0x80008000 where the caller's scale is negative, else 0
+    // paged source
+    const uint8_t *cache;
+    const int32_t *table, *lengths;
+    int64_t table_stride, num_blocks;
+    int32_t max_blocks, block_shift, causal;
+    // split over keys: partial sums
+    int32_t splits;
+    float *part_o;                     // attend_many: [splits][num_queries][heads][D]; attend_few: [workers][2][kv_heads][16][D]
+    float *part_ml;                    // the same without D, pairs (what the exponentials were taken against, their sum)
+};
+
+struct GradArgs {
+    AttendArgs a;                      // out and lse are inputs
+    const char *d_out;
+    char *dq, *dk, *dv, *dbias;        // any may be null
+    float *delta;                      // [num_queries][heads]
+    float *dbias_part;                 // [splits][kv_heads][num_keys], null without dbias
+    float *dk_part, *dv_part;          // [splits][num_keys][kv_heads][D], null with one split
+    float *dq_part;                    // [splits][num_queries][heads][D], null with one split
+};
+
+#define PLAID_SOURCE_DENSE 0
+#define PLAID_SOURCE_BIAS 1
+#define PLAID_SOURCE_PAGED 2
+
+// Keys that a step of attend_few's workgroup covers, rows of its tiles.
+#define FEW_KEYS 128
+#define FEW_ROWS 16
+// Keys of a tile of attend_many.
+#define MANY_KEYS 64
+
+// Launchers.  workers: workgroups of attend_few per key head.
+void plaid_launch_attend_few(hipStream_t st, const AttendArgs &a, int dtype, int head_dim, int source, int workers, int64_t tiles);
+void plaid_launch_attend_many(hipStream_t st, const AttendArgs &a, int dtype, int head_dim, int source, int waves, int64_t tiles);
+void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_waves, int q_splits, int k_waves,
+                              int k_splits);
+void plaid_launch_cache_write(hipStream_t st, const plaid_paged_cache &c, const char *k, const char *v, int64_t k_token, int64_t k_head,
+                              int64_t v_token, int64_t v_head, const int64_t *slots, int64_t n);
+void plaid_launch_cache_read(hipStream_t st, const plaid_paged_cache &c, const int64_t *slots, int64_t n, char *k, char *v);
+struct TablesArgs {
+    const int32_t *lengths, *added, *free_blocks;
+    int32_t *table, *totals, *positions;
+    int64_t *offsets, *slots, *blocks_wanted;
+    int64_t table_stride, capacity;
+    int32_t n, max_blocks, n_free, block_shift;
+    int64_t *scan;                     // [2][n + 1] prefix sums of tokens and blocks, null where one launch does all
+};
+void plaid_launch_block_tables(hipStream_t st, const TablesArgs &t);
+int64_t plaid_block_tables_scan_bytes(int32_t n, int64_t capacity);
+
+#ifdef __HIP__
+// ---------------------------------------------------------------------------------------------
+// Device side
+// ---------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+#define LOG2E 1.4426950408889634f
+#define LN2 0.6931471805599453f
+
+// C += A . B, 32 x 32 x 16: lane l holds row / column l % 32 of A / B at k = 8 (l / 32) .. + 7; C: column l % 32, register r is
+// row 8 (r / 4) + 4 (l / 32) + r % 4.
+template <int DT>
+__device__ __forceinline__ f32x16 mfma32(i32x4 a, i32x4 b, f32x16 c)
+{
+    if constexpr (DT == PLAID_BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// 16 x 16 x 32: lane l holds row / column l % 16 at k = 8 (l / 16) .. + 7; C: column l % 16, register r is row 4 (l / 16) + r.
+template <int DT>
+__device__ __forceinline__ f32x4 mfma16(i32x4 a, i32x4 b, f32x4 c)
+{
+    if constexpr (DT == PLAID_BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// Two values rounded (to nearest, ties to even) to the type, the first in the low half.
+template <int DT>
+__device__ __forceinline__ int pack2(float x, float y)
+{
+    if constexpr (DT == PLAID_BF16) {
+        bf16x2 p;
+        p[0] = (__bf16)x;
+        p[1] = (__bf16)y;
+        return __builtin_bit_cast(int, p);
+    } else {
+        f16x2 p;
+        p[0] = (_Float16)x;
+        p[1] = (_Float16)y;
+        return __builtin_bit_cast(int, p);
+    }
+}
+template <int DT>
+__device__ __forceinline__ float unpack(int w, int half)
+{
+    if constexpr (DT == PLAID_BF16) return __int_as_float(half ? (w & 0xffff0000) : (w << 16));
+    else return (float)__builtin_bit_cast(f16x2, w)[half];
+}
+template <int DT>
+__device__ __forceinline__ float load16(const char *p)
+{
+    return unpack<DT>(*(const uint16_t *)p, 0);
+}
+template <int DT>
+__device__ __forceinline__ void store16(char *p, float x)
+{
+    *(uint16_t *)p = (uint16_t)pack2<DT>(x, 0.0f);
+}
+// Two codes of a byte (BYTE of w) times a power of two, exact; the low half's value first.
+template <int DT, int BYTE>
+__device__ __forceinline__ int codes2(int w, float power)
+{
+    if constexpr (DT == PLAID_BF16) return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((unsigned)w, power, BYTE));
+    else return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4((unsigned)w, power, BYTE));
+}
+__device__ __forceinline__ float scale_power(int b) { return __int_as_float(b << 23); }  // 255: infinity, which makes every code NaN
+
+// The other half of the wave's value of the same lane % 32.
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// Row / group and row % group.
+__device__ __forceinline__ int row_token(const AttendArgs &a, int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_magic); }
+
+// The request that owns place p of the tiles, with the tiles of request r starting at floor(off[r] * per_token / tile) + r: a
+// request of m rows has at least ceil(m / tile) places there, so the grid needs only the totals that the host knows.
+// All lanes of a wave call it together and get the same answer; off is not trusted.
+struct TilePlace {
+    int r;       // request, -1: none
+    int tile;    // tile of the request
+    int64_t begin, end;  // its rows of the packed tensor
+};
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
+__device__ __forceinline__ TilePlace find_tile(const int64_t *off, int n, int64_t rows, int per_token, int tile_shift, int64_t p)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = n - 1;  // the last request whose first place is <= p
+    while (lo < hi) {
+        const int64_t span = (int64_t)hi - lo;  // candidates lo + 1 .. hi, 64 of them tried at a time
+        const int64_t step = (span + 63) >> 6;
+        const int64_t at = lo + step * (lane + 1);
+        bool below = false;
+        if (at <= hi) below = ((clamp64(off[at], 0, rows) * per_token) >> tile_shift) + at <= p;
+        const uint64_t votes = __ballot(below);
+        const int k = votes ? 64 - __clzll((long long)votes) : 0;  // the highest lane that said yes, plus one
+        const int64_t nlo = lo + step * k;
+        const int64_t nhi = nlo + step - 1;
+        lo = (int)nlo;
+        hi = (int)(nhi < hi ? nhi : hi);
+    }
+    TilePlace t;
+    t.begin = clamp64(off[lo], 0, rows);
+    t.end = clamp64(off[lo + 1], t.begin, rows);
+    const int64_t first = ((t.begin * per_token) >> tile_shift) + lo;
+    t.tile = (int)(p - first);
+    t.r = p >= first && ((int64_t)t.tile << tile_shift) < (t.end - t.begin) * per_token ? lo : -1;
+    return t;
+}
+
+// Linear workgroup id, re-ordered so that neighbours in the result run on one XCD (workgroups go to the eight in turn).
+__device__ __forceinline__ int64_t xcd_order(int64_t id, int64_t total)
+{
+    const int64_t even = total >> 3, rest = total & 7;
+    const int64_t xcd = id & 7, at = id >> 3;
+    return xcd * even + (xcd < rest ? xcd : rest) + at;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Tiles of 16-bit values in LDS: rows of D values, their 16-byte chunks exchanged by an exclusive-or with a number of the
+// row.  Its three bits are (row % 4) * 2 + row / 4 % 2: eight rows' chunks of one column lie in different banks (the reads
+// along a row) and so do the 32-byte pieces of four rows (the transposing reads).
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ int swizzle(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+
+template <int D>
+__device__ __forceinline__ int lds_chunk(int row, int chunk)
+{
+    return row * (D * 2) + ((chunk ^ swizzle(row)) << 4);
+}
+// Operand along the row: rows base + l % 32, values 16 s + 8 (l / 32) .. + 7.  base is a multiple of 32.
+template <int D>
+__device__ __forceinline__ i32x4 lds_rows(const char *tile, int base, int s)
+{
+    const int lane = threadIdx.x & 63;
+    return *(const i32x4 *)(tile + (base + (lane & 31)) * (D * 2) + (((2 * s + (lane >> 5)) ^ swizzle(lane & 31)) << 4));
+}
+// Transposed operand: columns 32 dt + l % 32, rows base + 4 (l / 32) .. + 3 and base + 8 + 4 (l / 32) .. + 3 (base a multiple
+// of 16): the order in which mfma32's result leaves its rows in a lane's registers 8 i .. 8 i + 7.
+template <int D>
+__device__ __forceinline__ i32x4 lds_columns(const char *tile, int base, int dt)
+{
+    const int lane = threadIdx.x & 63;
+    const int h = lane >> 5, r = (lane >> 2) & 3, c = (lane & 3) >> 1;
+    const int row = base + 4 * h + r;
+    const int chunk = (4 * dt + ((lane >> 4) & 1) * 2 + c) ^ ((r << 1) | h);
+    const char *p = tile + row * (D * 2) + (chunk << 4) + (lane & 1) * 8;
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * (D * 2)));
+    const i32x2 u = __builtin_bit_cast(i32x2, x), w = __builtin_bit_cast(i32x2, y);
+    return i32x4{u[0], u[1], w[0], w[1]};
+}
+// Rows 8 i .. of a result's registers as an operand: registers 8 i .. 8 i + 7 rounded to the type.
+template <int DT>
+__device__ __forceinline__ i32x4 round8(const f32x16 &x, int i)
+{
+    return i32x4{pack2<DT>(x[8 * i], x[8 * i + 1]), pack2<DT>(x[8 * i + 2], x[8 * i + 3]), pack2<DT>(x[8 * i + 4], x[8 * i + 5]),
+                 pack2<DT>(x[8 * i + 6], x[8 * i + 7])};
+}
+__device__ __forceinline__ f32x16 zero16()
+{
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+    return z;
+}
+#endif

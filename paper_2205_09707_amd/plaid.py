@@ -52,7 +52,9 @@ EXPORTS = ("plaid_index_load", "plaid_index_from_view", "plaid_index_free", "pla
            "plaid_get_score_kernel_clocks",
            "plaid_set_max_chunk", "plaid_get_score_kernel", "plaid_get_stage2_kernel", "plaid_assign_centroids",
            "plaid_encode_residuals", "plaid_build_ivf", "plaid_workspace_bytes", "plaid_index_set_renormalize",
-           "plaid_last_error")
+           "plaid_block_tables", "plaid_block_tables_workspace", "plaid_cache_write", "plaid_cache_read", "plaid_cached_attention",
+           "plaid_cached_attention_workspace", "plaid_cross_attention", "plaid_cross_attention_backward",
+           "plaid_cross_attention_workspace", "plaid_last_error")
 
 _lib = None
 
@@ -94,6 +96,8 @@ def load_library() -> ct.CDLL:
                                                ct.c_int32, ct.c_void_p, ct.c_int, ct.c_void_p]
         lib.plaid_build_ivf.argtypes = [ct.c_void_p, ct.c_void_p, ct.c_int64, ct.c_int64, ct.c_int64, ct.c_void_p, ct.c_void_p,
                                         ct.c_int64, ct.POINTER(ct.c_int64), ct.c_int, ct.c_void_p]
+        from . import reader
+        reader.declare(lib)
         _lib = lib
     return _lib
 

@@ -1,0 +1,298 @@
+"""Binding of the reader's operators (include/plaid.h): block tables, the paged cache in four bits, attention over it, cross
+attention and its gradients.
+
+Like `plaid.py` this only marshals: it checks tensors, allocates outputs and workspaces from torch's allocator and hands over
+torch's current stream of the tensors' device.  Nothing is kept from one call for the next.
+"""
+from __future__ import annotations
+
+import ctypes as ct
+from typing import Optional, Tuple
+
+import torch
+
+from . import plaid as _p
+
+PLAID_BF16, PLAID_FP16 = 0, 1
+_DTYPES = {torch.bfloat16: PLAID_BF16, torch.float16: PLAID_FP16}
+_BLOCK_SIZES = (16, 32, 64, 128, 256)
+
+
+class plaid_paged_cache(ct.Structure):
+    _fields_ = [("data", ct.c_void_p), ("num_blocks", ct.c_int64), ("block_size", ct.c_int32), ("kv_heads", ct.c_int32),
+                ("head_dim", ct.c_int32), ("dtype", ct.c_int32)]
+
+
+class plaid_attention(ct.Structure):
+    _fields_ = ([(n, ct.c_int32) for n in ("dtype", "n", "heads", "kv_heads", "head_dim")] + [("scale", ct.c_float)]
+                + [(n, ct.c_int64) for n in ("num_queries", "num_keys")] + [(n, ct.c_void_p) for n in ("q", "k", "v", "key_bias")]
+                + [(n, ct.c_int64) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride", "v_token_stride", "v_head_stride")]
+                + [(n, ct.c_void_p) for n in ("q_offsets", "k_offsets", "out", "lse")])
+
+
+def declare(lib: ct.CDLL) -> None:
+    """Argument types of the reader's functions."""
+    P, i32, i64 = ct.c_void_p, ct.c_int32, ct.c_int64
+    attention, cache, out64 = ct.POINTER(plaid_attention), ct.POINTER(plaid_paged_cache), ct.POINTER(i64)
+    lib.plaid_block_tables.argtypes = [P, P, i32, P, i64, i32, P, i32, i32, P, P, P, P, i64, P, P, i64, ct.c_int, P]
+    lib.plaid_block_tables_workspace.argtypes = [i32, i64, out64]
+    lib.plaid_cache_write.argtypes = [cache, P, P, i64, i64, i64, i64, P, i64, ct.c_int, P]
+    lib.plaid_cache_read.argtypes = [cache, P, i64, P, P, ct.c_int, P]
+    lib.plaid_cached_attention.argtypes = [attention, cache, P, i64, i32, P, i32, P, i64, ct.c_int, P]
+    lib.plaid_cached_attention_workspace.argtypes = [attention, i32, i32, out64]
+    lib.plaid_cross_attention.argtypes = [attention, P, i64, ct.c_int, P]
+    lib.plaid_cross_attention_backward.argtypes = [attention, P, P, P, P, P, P, i64, ct.c_int, P]
+    lib.plaid_cross_attention_workspace.argtypes = [attention, i32, out64]
+
+
+def _is(t: torch.Tensor, name: str, dtype, dim: int, device: Optional[torch.device] = None) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.dim() != dim:
+        raise ValueError(f"{name} must be a CUDA tensor of dtype {dtype} with {dim} dimension(s)")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on another device than the other tensors")
+    return t
+
+
+def _vector(t: torch.Tensor, name: str, dtype, device: torch.device, size: Optional[int] = None) -> torch.Tensor:
+    _is(t, name, dtype, 1, device)
+    if size is not None and t.shape[0] != size:
+        raise ValueError(f"{name} must hold {size} values, got {t.shape[0]}")
+    return t.contiguous()
+
+
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """The tensor itself where the kernels can read its strides, else a contiguous copy."""
+    _, heads, dim = t.shape
+    s = t.stride()
+    if t.numel() and (s[2] != 1 or t.data_ptr() % 16 or (s[0] % 8 and t.shape[0] > 1) or (s[1] % 8 and heads > 1)):
+        t = t.contiguous() if not t.is_contiguous() else t.clone(memory_format=torch.contiguous_format)
+    return t
+
+
+def _strides(t: torch.Tensor) -> Tuple[int, int]:
+    n, heads, dim = t.shape
+    return (t.stride(0) if n > 1 else heads * dim), (t.stride(1) if heads > 1 else dim)
+
+
+def _workspace(bytes_: int, device: torch.device):
+    return (None, None) if bytes_ == 0 else ((w := torch.empty(bytes_, dtype=torch.uint8, device=device)), _p._ptr(w))
+
+
+def _ordinal(device: torch.device) -> int:
+    return device.index or 0
+
+
+class PagedCache:
+    """Keys and values of a paged cache in four bits a value.
+
+    `data` is a contiguous uint8 tensor [num_blocks, kv_heads, block_size * head_dim * 17 / 16], laid out as include/plaid.h says;
+    `dtype` (torch.bfloat16 or torch.float16) is the type that is written and read.  The object holds the tensor, nothing else."""
+
+    def __init__(self, data: torch.Tensor, block_size: int, head_dim: int, dtype: torch.dtype):
+        _is(data, "data", torch.uint8, 3)
+        if dtype not in _DTYPES:
+            raise ValueError("the cache's dtype must be torch.bfloat16 or torch.float16")
+        if block_size not in _BLOCK_SIZES:
+            raise ValueError(f"block_size must be one of {_BLOCK_SIZES}")
+        if head_dim not in (64, 128) or data.shape[2] * 16 != block_size * head_dim * 17:
+            raise ValueError("head_dim must be 64 or 128 and data.shape[2] block_size * head_dim * 17 / 16")
+        if not data.is_contiguous() or data.data_ptr() % 16:
+            raise ValueError("data must be contiguous and 16-byte aligned")
+        self.data, self.block_size, self.head_dim, self.dtype = data, int(block_size), int(head_dim), dtype
+        self.num_blocks, self.kv_heads = data.shape[0], data.shape[1]
+
+    @classmethod
+    def empty(cls, num_blocks: int, block_size: int, kv_heads: int, head_dim: int, dtype: torch.dtype, device="cuda:0") -> "PagedCache":
+        """A cache of zeros."""
+        region = int(block_size) * int(head_dim) * 17 // 16
+        return cls(torch.zeros((num_blocks, kv_heads, region), dtype=torch.uint8, device=device), block_size, head_dim, dtype)
+
+    def _view(self) -> plaid_paged_cache:
+        return plaid_paged_cache(self.data.data_ptr(), self.num_blocks, self.block_size, self.kv_heads, self.head_dim, _DTYPES[self.dtype])
+
+
+def plaid_block_tables(lengths: torch.Tensor, added: torch.Tensor, table: torch.Tensor, free_blocks: torch.Tensor, block_size: int,
+                       capacity: int):
+    """Hands blocks of a paged cache to requests that hold `lengths` [n] tokens and get `added` [n] more (int32), in place in
+    `table` [n, max_blocks] int32; `capacity`: room for new tokens, normally their number.  Returns (offsets [n+1] int64, totals
+    [n] int32, positions [capacity] int32, slots [capacity] int64, blocks_wanted [1] int64).  More blocks wanted than
+    `free_blocks` holds, or a full row of the table, leaves slots of -1."""
+    dev = _is(lengths, "lengths", torch.int32, 1).device
+    n = lengths.shape[0]
+    lengths = lengths.contiguous()
+    added = _vector(added, "added", torch.int32, dev, n)
+    free_blocks = _vector(free_blocks, "free_blocks", torch.int32, dev)
+    _is(table, "table", torch.int32, 2, dev)
+    if table.shape[0] != n or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must have a row for each request and contiguous rows")
+    lib, capacity = _p.load_library(), int(capacity)
+    need = ct.c_int64(0)
+    _p._check(lib.plaid_block_tables_workspace(n, capacity, ct.byref(need)))
+    # the five outputs are one allocation; each starts at a multiple of 16 bytes
+    room = max(capacity, 0)
+    sizes = [8 * room, 8 * (n + 1), 8, 4 * room, 4 * n]
+    at, total = [], 0
+    for s in sizes:
+        at.append(total)
+        total += (s + 15) & ~15
+    buf = torch.empty(total, dtype=torch.uint8, device=dev)
+    slots, offsets, wanted, positions, totals = (
+        buf[a:a + s].view(t) for a, s, t in zip(at, sizes, (torch.int64, torch.int64, torch.int64, torch.int32, torch.int32)))
+    work, ptr = _workspace(need.value, dev)
+    _p._check(lib.plaid_block_tables(_p._ptr(lengths), _p._ptr(added), n, _p._ptr(table), table.stride(0) if n > 1 else table.shape[1],
+                                     table.shape[1], _p._ptr(free_blocks), free_blocks.shape[0], int(block_size), _p._ptr(offsets),
+                                     _p._ptr(totals), _p._ptr(positions), _p._ptr(slots), capacity, _p._ptr(wanted), ptr, need.value,
+                                     _ordinal(dev), _p._stream(dev)))
+    return offsets, totals, positions, slots, wanted
+
+
+def plaid_cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """Writes k and v [tokens, kv_heads, head_dim] of the cache's dtype to `slots` [tokens] int64 (negative: left out)."""
+    dev = cache.data.device
+    shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
+    for name, t in (("k", k), ("v", v)):
+        if tuple(_is(t, name, cache.dtype, 3, dev).shape) != shape:
+            raise ValueError(f"{name} must have the shape {shape}, got {tuple(t.shape)}")
+    slots = _vector(slots, "slots", torch.int64, dev)
+    k, v = _rows(k), _rows(v)
+    _p._check(_p.load_library().plaid_cache_write(ct.byref(cache._view()), _p._ptr(k), _p._ptr(v), *_strides(k), *_strides(v), _p._ptr(slots),
+                                                  slots.shape[0], _ordinal(dev), _p._stream(dev)))
+
+
+def plaid_cache_read(cache: PagedCache, slots: torch.Tensor):
+    """(k, v) [tokens, kv_heads, head_dim] that `slots` [tokens] int64 hold; zeros for a slot outside the cache."""
+    dev = cache.data.device
+    slots = _vector(slots, "slots", torch.int64, dev)
+    k = torch.empty((slots.shape[0], cache.kv_heads, cache.head_dim), dtype=cache.dtype, device=dev)
+    v = torch.empty_like(k)
+    _p._check(_p.load_library().plaid_cache_read(ct.byref(cache._view()), _p._ptr(slots), slots.shape[0], _p._ptr(k), _p._ptr(v), _ordinal(dev),
+                                                 _p._stream(dev)))
+    return k, v
+
+
+def _attention(q, k, v, key_bias, q_offsets, k_offsets, kv_heads, scale, out, lse) -> plaid_attention:
+    a = plaid_attention()
+    a.dtype, a.n = _DTYPES[q.dtype], q_offsets.shape[0] - 1
+    a.num_queries, a.heads, a.head_dim = q.shape
+    a.kv_heads = kv_heads
+    a.scale = a.head_dim ** -0.5 if scale is None else float(scale)
+    a.q, a.q_offsets, a.out = q.data_ptr(), q_offsets.data_ptr(), out.data_ptr()
+    a.q_token_stride, a.q_head_stride = _strides(q)
+    if lse is not None:
+        a.lse = lse.data_ptr()
+    if k is not None:
+        a.num_keys = k.shape[0]
+        a.k, a.v, a.k_offsets = k.data_ptr(), v.data_ptr(), k_offsets.data_ptr()
+        a.k_token_stride, a.k_head_stride = _strides(k)
+        a.v_token_stride, a.v_head_stride = _strides(v)
+        if key_bias is not None:
+            a.key_bias = key_bias.data_ptr()
+    return a
+
+
+def _check_heads(q: torch.Tensor, kv_heads: int, head_dim: int) -> None:
+    if q.shape[2] != head_dim or head_dim not in (64, 128):
+        raise ValueError(f"head_dim must be 64 or 128 and the same for queries and keys, got {q.shape[2]} and {head_dim}")
+    if kv_heads < 1 or q.shape[1] < 1 or q.shape[1] % kv_heads:
+        raise ValueError(f"{q.shape[1]} query heads are no multiple of {kv_heads} key heads")
+
+
+def _check_queries(q: torch.Tensor) -> None:
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dtype not in _DTYPES or q.dim() != 3:
+        raise ValueError("q must be a CUDA tensor [tokens, heads, head_dim] of dtype torch.bfloat16 or torch.float16")
+
+
+def plaid_cached_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor, lengths: torch.Tensor, q_offsets: torch.Tensor,
+                           scale: Optional[float] = None, causal: bool = True, return_lse: bool = False):
+    """Attention of q [tokens, heads, head_dim] over a paged cache: request r's queries are rows q_offsets[r] .. q_offsets[r+1]-1
+    (int64 [n+1]), its keys the lengths[r] (int32) tokens that table[r] ([n, max_blocks] int32) leads to.  causal: the queries are
+    the request's last tokens, each sees what is not after it.  scale: head_dim ** -0.5 by default.  Returns out like q, with
+    return_lse also the logarithm of the softmax's sum as two numbers to be added, [tokens, heads, 2] float32."""
+    _check_queries(q)
+    dev = q.device
+    if cache.data.device != dev or q.dtype != cache.dtype:
+        raise ValueError("q and the cache must have one device and dtype")
+    _check_heads(q, cache.kv_heads, cache.head_dim)
+    n = _is(lengths, "lengths", torch.int32, 1, dev).shape[0]
+    lengths = lengths.contiguous()
+    q_offsets = _vector(q_offsets, "q_offsets", torch.int64, dev, n + 1)
+    _is(table, "table", torch.int32, 2, dev)
+    if table.shape[0] != n:
+        raise ValueError("table must have a row for each request")
+    if table.shape[1] > 1 and table.stride(1) != 1:
+        table = table.contiguous()
+    q = _rows(q)
+    out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    lse = torch.empty(q.shape[:2] + (2,), dtype=torch.float32, device=dev) if return_lse else None
+    lib = _p.load_library()
+    a = _attention(q, None, None, None, q_offsets, None, cache.kv_heads, scale, out, lse)
+    need = ct.c_int64(0)
+    _p._check(lib.plaid_cached_attention_workspace(ct.byref(a), table.shape[1], cache.block_size, ct.byref(need)))
+    work, ptr = _workspace(need.value, dev)
+    _p._check(lib.plaid_cached_attention(ct.byref(a), ct.byref(cache._view()), _p._ptr(table), table.stride(0) if n > 1 else table.shape[1],
+                                         table.shape[1], _p._ptr(lengths), 1 if causal else 0, ptr, need.value, _ordinal(dev), _p._stream(dev)))
+    return (out, lse) if return_lse else out
+
+
+def _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias):
+    _check_queries(q)
+    dev = q.device
+    for name, t in (("k", k), ("v", v)):
+        _is(t, name, q.dtype, 3, dev)
+    if k.shape != v.shape:
+        raise ValueError("k and v must have one shape")
+    _check_heads(q, k.shape[1], k.shape[2])
+    n = _is(q_offsets, "q_offsets", torch.int64, 1, dev).shape[0] - 1
+    q_offsets = q_offsets.contiguous()
+    k_offsets = _vector(k_offsets, "k_offsets", torch.int64, dev, n + 1)
+    if key_bias is not None:
+        key_bias = _vector(key_bias, "key_bias", q.dtype, dev, k.shape[0])
+    return _rows(q), _rows(k), _rows(v), q_offsets, k_offsets, key_bias
+
+
+def plaid_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor,
+                          key_bias: Optional[torch.Tensor] = None, scale: Optional[float] = None, return_lse: bool = False):
+    """Attention of q [tokens, heads, head_dim] to states of another length, k and v [keys, kv_heads, head_dim], both packed:
+    request r owns rows q_offsets[r] .. q_offsets[r+1]-1 and keys k_offsets[r] .. k_offsets[r+1]-1 (int64 [n+1]).  key_bias [keys]
+    of q's dtype is added to the scores; -inf takes a key out.  Returns out like q (rows outside every request are not written),
+    with return_lse also the two numbers a row that plaid_cross_attention_backward wants."""
+    q, k, v, q_offsets, k_offsets, key_bias = _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias)
+    dev = q.device
+    out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    lse = torch.empty(q.shape[:2] + (2,), dtype=torch.float32, device=dev) if return_lse else None
+    lib = _p.load_library()
+    a = _attention(q, k, v, key_bias, q_offsets, k_offsets, k.shape[1], scale, out, lse)
+    need = ct.c_int64(0)
+    _p._check(lib.plaid_cross_attention_workspace(ct.byref(a), 0, ct.byref(need)))
+    work, ptr = _workspace(need.value, dev)
+    _p._check(lib.plaid_cross_attention(ct.byref(a), ptr, need.value, _ordinal(dev), _p._stream(dev)))
+    return (out, lse) if return_lse else out
+
+
+def plaid_cross_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                                   q_offsets: torch.Tensor, k_offsets: torch.Tensor, key_bias: Optional[torch.Tensor] = None,
+                                   scale: Optional[float] = None):
+    """(dq, dk, dv, dbias) of plaid_cross_attention, from its outputs out and lse and the gradient d_out; contiguous, dbias None
+    without key_bias.  Rows outside every request are not written."""
+    q, k, v, q_offsets, k_offsets, key_bias = _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias)
+    dev = q.device
+    for name, t in (("d_out", d_out), ("out", out)):
+        if _is(t, name, q.dtype, 3, dev).shape != q.shape:
+            raise ValueError(f"{name} must have q's shape")
+    _is(lse, "lse", torch.float32, 3, dev)
+    if lse.shape != q.shape[:2] + (2,):
+        raise ValueError("lse must be what plaid_cross_attention returned")
+    whole = lambda t: t if t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)  # noqa: E731
+    d_out, out, lse = whole(d_out), whole(out), whole(lse)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    dk = torch.empty(k.shape, dtype=q.dtype, device=dev)
+    dv = torch.empty(k.shape, dtype=q.dtype, device=dev)
+    dbias = torch.empty(k.shape[:1], dtype=q.dtype, device=dev) if key_bias is not None else None
+    lib = _p.load_library()
+    a = _attention(q, k, v, key_bias, q_offsets, k_offsets, k.shape[1], scale, out, lse)
+    need = ct.c_int64(0)
+    _p._check(lib.plaid_cross_attention_workspace(ct.byref(a), 1, ct.byref(need)))
+    work, ptr = _workspace(need.value, dev)
+    _p._check(lib.plaid_cross_attention_backward(ct.byref(a), _p._ptr(d_out), _p._ptr(dq), _p._ptr(dk), _p._ptr(dv), _p._ptr(dbias), ptr, need.value,
+                                                 _ordinal(dev), _p._stream(dev)))
+    return dq, dk, dv, dbias
