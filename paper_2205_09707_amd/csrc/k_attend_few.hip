@@ -26,7 +26,7 @@ struct Request {
     int64_t row0, key0, len;
     int tokens, tiles, steps;  // a request without keys has one step, which writes its zeros
 };
-template <int SRC>
+template <int SRC, int NW>
 __device__ __forceinline__ Request request(const AttendArgs &a, int r)
 {
     Request q;
@@ -34,127 +34,150 @@ __device__ __forceinline__ Request request(const AttendArgs &a, int r)
     q.tokens = (int)(clamp64(a.q_offsets[r + 1], q.row0, a.num_queries) - q.row0);
     q.tiles = (int)(((int64_t)q.tokens * a.group + FEW_ROWS - 1) / FEW_ROWS);
     q.len = key_count<SRC>(a, r, q.key0);
-    q.steps = (int)((q.len + FEW_KEYS - 1) / FEW_KEYS);
+    q.steps = (int)((q.len + NW * 32 - 1) / (NW * 32));
     if (q.steps < 1) q.steps = 1;
     return q;
 }
-__device__ __forceinline__ int64_t wave_sum(int64_t x)
+template <int SRC, int NW>
+__device__ __forceinline__ Request uniform_request(const AttendArgs &a, int r)
+{
+    Request q;
+    q.row0 = clamp64(uniform_load(a.q_offsets + r), 0, a.num_queries);
+    q.tokens = (int)(clamp64(uniform_load(a.q_offsets + r + 1), q.row0, a.num_queries) - q.row0);
+    q.tiles = (int)(((int64_t)q.tokens * a.group + FEW_ROWS - 1) / FEW_ROWS);
+    q.key0 = 0;
+    if constexpr (SRC == PLAID_SOURCE_PAGED) {
+        q.len = clamp64(uniform_load(a.lengths + r), 0, (int64_t)a.max_blocks << a.block_shift);
+    } else {
+        q.key0 = clamp64(uniform_load(a.k_offsets + r), 0, a.num_keys);
+        q.len = clamp64(uniform_load(a.k_offsets + r + 1), q.key0, a.num_keys) - q.key0;
+    }
+    q.steps = (int)((q.len + NW * 32 - 1) / (NW * 32));
+    if (q.steps < 1) q.steps = 1;
+    return q;
+}
+__device__ __forceinline__ int wave_sum(int x)
 {
 #pragma unroll
     for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
     return x;
 }
-__device__ __forceinline__ int64_t wave_prefix(int64_t x)  // sum over lower lanes and this one
+__device__ __forceinline__ int wave_prefix(int x)  // sum over lower lanes and this one
 {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int64_t y = __shfl_up(x, o);
+        const int y = __shfl_up(x, o);
         if (lane >= o) x += y;
     }
     return x;
 }
-// Steps of all requests and of those before r (r = n: of all).
-template <int SRC>
-__device__ __forceinline__ int64_t all_work(const AttendArgs &a, int r, int64_t &before)
+// Steps of all requests and of those before r.  (The host takes these kernels where all counts of steps fit 32 bits.)
+template <int SRC, int NW>
+__device__ __forceinline__ int all_work(const AttendArgs &a, int r, int &before)
 {
-    int64_t all = 0, some = 0;
+    int all = 0, some = 0;
     for (int i = threadIdx.x & 63; i < a.n; i += 64) {
-        const Request q = request<SRC>(a, i);
-        const int64_t w = (int64_t)q.tiles * q.steps;
+        const Request q = request<SRC, NW>(a, i);
+        const int w = q.tiles * q.steps;
         all += w;
         if (i < r) some += w;
     }
     before = wave_sum(some);
     return wave_sum(all);
 }
-// The request that holds place `at` of the line, and the place where it begins.
-template <int SRC>
-__device__ __forceinline__ int find_work(const AttendArgs &a, int64_t share_of, int64_t worker, int64_t &total, int64_t &at, int64_t &end, int64_t &first)
+// The worker's stretch at .. end - 1 of the line, the request that holds its beginning (-1: the stretch is empty) and the
+// place where that request begins.
+template <int SRC, int NW>
+__device__ __forceinline__ int find_work(const AttendArgs &a, int workers, int worker, int &at, int &end, int &first)
 {
     const int lane = threadIdx.x & 63, per = (a.n + 63) >> 6;
-    int64_t mine = 0;
+    int mine = 0;
     for (int i = lane * per; i < min(a.n, (lane + 1) * per); ++i) {
-        const Request q = request<SRC>(a, i);
-        mine += (int64_t)q.tiles * q.steps;
+        const Request q = request<SRC, NW>(a, i);
+        mine += q.tiles * q.steps;
     }
-    const int64_t upto = wave_prefix(mine);
-    total = __shfl(upto, 63);
-    const int64_t share = (total + share_of - 1) / share_of;
+    const int upto = wave_prefix(mine), total = uniform(__shfl(upto, 63)), share = (int)(((uint32_t)total + workers - 1) / (uint32_t)workers);
+    if ((int64_t)worker * share >= total) return -1;
     at = worker * share;
     end = min(total, at + share);
-    if (at >= end) return -1;
     const int block = __popcll(__ballot(upto <= at));  // lanes whose requests all end before
-    int64_t left = __shfl(upto - mine, block);
+    if (per == 1) {
+        first = uniform(__shfl(upto - mine, block));
+        return block;
+    }
+    int left = __shfl(upto - mine, block);
     for (int i = block * per;; i += 64) {
-        int64_t w = 0;
+        int w = 0;
         if (i + lane < a.n) {
-            const Request q = request<SRC>(a, i + lane);
-            w = (int64_t)q.tiles * q.steps;
+            const Request q = request<SRC, NW>(a, i + lane);
+            w = q.tiles * q.steps;
         }
-        const int64_t to = left + wave_prefix(w);
-        const int k = __popcll(__ballot(to <= at));
+        const int to = left + wave_prefix(w), k = __popcll(__ballot(to <= at));
         if (k < 64) {
-            first = __shfl(to - w, k);
-            return i + k;
+            first = uniform(__shfl(to - w, k));
+            return uniform(i + k);
         }
         left = __shfl(to, 63);
     }
 }
 
 template <int DT, int D, int SRC>
-struct Piece {  // 32 keys' data of a wave, as loaded
+struct Piece {  // a wave's 32 keys on their way in
     i32x4 k[2][D / 32], v[D / 16];
     int bias[4];
 };
 template <int DT, int D>
 struct Piece<DT, D, PLAID_SOURCE_PAGED> {
     i32x4 k[2], v[2], vs[2];
-    int ks[2], ok[2];
+    int ks[2];
 };
 
-template <int D, int SRC>
+template <int D, int NW, int SRC>
 struct FewLds {
     union {
-        char v[SRC == PLAID_SOURCE_PAGED ? 16 : 4 * 32 * D * 2];  // dense values, a part for each wave
-        float o[4][FEW_ROWS][D + 4];
+        char v[SRC == PLAID_SOURCE_PAGED ? 16 : NW * 32 * D * 2];  // dense values, a part for each wave
+        float o[NW][FEW_ROWS][D + 4];
     };
-    float ml[4][FEW_ROWS][2];
+    float ml[NW][FEW_ROWS][2];
 };
 
-template <int DT, int D, int SRC>
-__global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a, int workers)
+// Keys and values of a piece are loaded apart, each into the registers that its predecessor has just left: the scores of a
+// step are formed while its values are still on their way, and the next keys are asked for before the softmax.
+template <int DT, int D, int NW, int SRC>
+__global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kernel(AttendArgs a, int workers)
 {
     constexpr int KS = D / 32, OT = D / 16;  // steps of the score product, tiles of the output
-    __shared__ __align__(16) FewLds<D, SRC> lds;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = lane >> 4, m16 = lane & 15;
-    const int64_t id = xcd_order(blockIdx.x, gridDim.x);
-    const int head_kv = (int)(id / workers), worker = (int)(id % workers);
-    int64_t total, at, end, first;
-    int r = find_work<SRC>(a, workers, worker, total, at, end, first);
+    constexpr bool PAGED = SRC == PLAID_SOURCE_PAGED, BIAS = SRC == PLAID_SOURCE_BIAS;
+    __shared__ __align__(16) FewLds<D, NW, SRC> lds;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), kg = lane >> 4, m16 = lane & 15;
+    const int id = (int)xcd_order(blockIdx.x, gridDim.x);
+    const int head_kv = id / workers, worker = id % workers;
+    int at, end, first;
+    int r = find_work<SRC, NW>(a, workers, worker, at, end, first);
     if (r < 0) return;
-    const float cs = SRC == PLAID_SOURCE_BIAS ? LOG2E : a.scale * LOG2E;
+    const float cs = BIAS ? LOG2E : a.scale * LOG2E;
 
     while (at < end) {
-        Request rq = request<SRC>(a, r);
-        while (at >= first + (int64_t)rq.tiles * rq.steps) {  // to the request that owns the place
-            first += (int64_t)rq.tiles * rq.steps;
-            rq = request<SRC>(a, ++r);
+        Request rq = uniform_request<SRC, NW>(a, r);
+        while (at >= first + rq.tiles * rq.steps) {  // to the request that owns the place
+            first += rq.tiles * rq.steps;
+            rq = uniform_request<SRC, NW>(a, ++r);
         }
-        const int tile = (int)((at - first) / rq.steps), begin = (int)((at - first) % rq.steps);
-        const int stop = (int)min((int64_t)rq.steps, begin + (end - at));
+        const int tile = (int)((uint32_t)(at - first) / (uint32_t)rq.steps), begin = at - first - tile * rq.steps;
+        const int stop = min(rq.steps, begin + (end - at));
         const int rows = rq.tokens * a.group, row = tile * FEW_ROWS + m16;
         const bool there = row < rows;
         const int token = row_token(a, there ? row : 0), head = head_kv * a.group + (there ? row : 0) - token * a.group;
         const int len = (int)rq.len;
-        int limit = len;
-        if constexpr (SRC == PLAID_SOURCE_PAGED)
-            if (a.causal) limit = there ? (int)clamp64((int64_t)a.lengths[r] - rq.tokens + token + 1, 0, len) : len;
-        int least = limit;
-        if constexpr (SRC == PLAID_SOURCE_PAGED) {
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o));
-        }
+        int limit = len, least = len;
+        if constexpr (PAGED)
+            if (a.causal) {
+                const int64_t all = uniform_load(a.lengths + r);
+                limit = there ? (int)clamp64(all - rq.tokens + token + 1, 0, len) : len;
+                // the tile's first token sees the least
+                least = (int)clamp64(all - rq.tokens + row_token(a, tile * FEW_ROWS) + 1, 0, len);
+            }
 
         i32x4 q[KS];
         {
@@ -173,222 +196,254 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a, int wo
         float m = -INFINITY, l = 0.0f;
 
         // --- loads of a piece
-        int ids[2] = {-1, -1};  // paged: the blocks of the piece to be loaded next
+        Piece<DT, D, SRC> x;
+        int ids[2] = {-1, -1}, in[2] = {0, 0};  // paged: the blocks of the cells loaded last, the cells' places in them
+        bool ok[2] = {true, true};              // whether the keys' cells have a block
         auto find = [&](int step) {
-            if constexpr (SRC == PLAID_SOURCE_PAGED) {
+            if constexpr (PAGED) {
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const int key = step * FEW_KEYS + wave * 32 + 16 * c;
-                    ids[c] = step < stop && key < len ? a.table[r * a.table_stride + (key >> a.block_shift)] : -1;
+                    const int key = step * (NW * 32) + wave * 32 + 16 * c;
+                    ids[c] = -1;
+                    if (key < len) ids[c] = uniform_load(a.table + r * a.table_stride + (key >> a.block_shift));
+                    in[c] = key & ((1 << a.block_shift) - 1);
                 }
             }
         };
-        auto load = [&](int step, Piece<DT, D, SRC> &x) {
-            const int key0 = step * FEW_KEYS + wave * 32;
-            if constexpr (SRC == PLAID_SOURCE_PAGED) {
-                const int64_t bs = 1ll << a.block_shift;
+        auto cell = [&](int c) { return a.cache + ((int64_t)ids[c] * a.kv_heads + head_kv) * ((int64_t)(D * 17 / 16) << a.block_shift); };
+        auto load_k = [&](int step) {
+            const int key0 = step * (NW * 32) + wave * 32;
+            if constexpr (PAGED) {
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const int in = (key0 + 16 * c) & (int)(bs - 1);
-                    x.ok[c] = (uint32_t)ids[c] < (uint64_t)a.num_blocks;
-                    x.k[c] = x.v[c] = x.vs[c] = i32x4{0, 0, 0, 0};
+                    ok[c] = (uint32_t)ids[c] < (uint64_t)a.num_blocks;
+                    x.k[c] = i32x4{0, 0, 0, 0};
                     x.ks[c] = 0;
-                    if (x.ok[c]) {
-                        const uint8_t *p = a.cache + ((int64_t)ids[c] * a.kv_heads + head_kv) * (bs * D * 17 / 16);
-                        const uint8_t *k = p + (in + m16) * (D / 2) + kg * (D / 8), *v = p + bs * (D / 2) + in * (D / 2) + lane * (D / 8);
-                        const uint8_t *ks = p + bs * D + (in + m16) * KS + (kg * KS) / 4, *vs = p + bs * D + bs * KS + (in + 4 * kg) * KS;
+                    if (ok[c]) {
+                        const uint8_t *p = cell(c) + in[c] * (D / 2), *s = cell(c) + (D << a.block_shift) + in[c] * KS;
+                        const uint32_t off = m16 * (D / 2) + kg * (D / 8);
                         if constexpr (D == 128) {
-                            x.k[c] = *(const i32x4 *)k, x.v[c] = *(const i32x4 *)v, x.vs[c] = *(const i32x4 *)vs;
+                            x.k[c] = *(const i32x4 *)(p + off);
                         } else {
-                            const i32x2 k2 = *(const i32x2 *)k, v2 = *(const i32x2 *)v, s2 = *(const i32x2 *)vs;
-                            x.k[c] = i32x4{k2[0], k2[1], 0, 0}, x.v[c] = i32x4{v2[0], v2[1], 0, 0}, x.vs[c] = i32x4{s2[0], s2[1], 0, 0};
+                            const i32x2 y = *(const i32x2 *)(p + off);
+                            x.k[c] = i32x4{y[0], y[1], 0, 0};
                         }
-                        x.ks[c] = *ks;
+                        x.ks[c] = s[(uint32_t)(m16 * KS + (kg * KS) / 4)];
                     }
                 }
             } else {
+                const char *base = a.k + (rq.key0 + key0) * a.k_token + head_kv * a.k_head;
+                const int last = len - 1 - key0;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const int key = key0 + 16 * c + m16;
-                    const char *p = a.k + (rq.key0 + key) * a.k_token + head_kv * a.k_head + kg * (D / 2);
+                    // a key past the end is masked whatever it holds: the last one stands for it
+                    const uint32_t off = (uint32_t)(16 * c + m16 <= last ? 16 * c + m16 : last) * (uint32_t)a.k_token + kg * (D / 2);
 #pragma unroll
-                    for (int s = 0; s < KS; ++s) {
-                        x.k[c][s] = i32x4{0, 0, 0, 0};
-                        if (key < len) x.k[c][s] = *(const i32x4 *)(p + 16 * s);
+                    for (int s = 0; s < KS; ++s) x.k[c][s] = *(const i32x4 *)(base + off + 16 * s);
+                }
+            }
+        };
+        auto load_v = [&](int step) {
+            const int key0 = step * (NW * 32) + wave * 32;
+            if constexpr (PAGED) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    x.v[c] = x.vs[c] = i32x4{0, 0, 0, 0};
+                    if ((uint32_t)ids[c] < (uint64_t)a.num_blocks) {
+                        const uint8_t *p = cell(c) + ((D / 2) << a.block_shift) + in[c] * (D / 2), *s = cell(c) + ((D + KS) << a.block_shift) + in[c] * KS;
+                        const uint32_t off = lane * (D / 8), soff = 4 * kg * KS;
+                        if constexpr (D == 128) {
+                            x.v[c] = *(const i32x4 *)(p + off), x.vs[c] = *(const i32x4 *)(s + soff);
+                        } else {
+                            const i32x2 y = *(const i32x2 *)(p + off), z = *(const i32x2 *)(s + soff);
+                            x.v[c] = i32x4{y[0], y[1], 0, 0}, x.vs[c] = i32x4{z[0], z[1], 0, 0};
+                        }
                     }
                 }
+            } else {
+                const char *base = a.v + (rq.key0 + key0) * a.v_token + head_kv * a.v_head;
+                constexpr int AT_ONCE = 512 / D;  // keys that a load of the wave covers
+                const int last = len - 1 - key0;
+                if (last >= 31) {
+                    const uint32_t off = (uint32_t)(lane / (D / 8)) * (uint32_t)a.v_token + lane % (D / 8) * 16;
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const int unit = i * 64 + lane, key = key0 + unit / (D / 8);
-                    x.v[i] = i32x4{0, 0, 0, 0};
-                    if (key < len) x.v[i] = *(const i32x4 *)(a.v + (rq.key0 + key) * a.v_token + head_kv * a.v_head + unit % (D / 8) * 16);
+                    for (int i = 0; i < D / 16; ++i) x.v[i] = *(const i32x4 *)(base + (uint32_t)(i * AT_ONCE) * (uint32_t)a.v_token + off);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const int key = i * AT_ONCE + lane / (D / 8);
+                        x.v[i] = *(const i32x4 *)(base + (uint32_t)(key < last ? key : last) * (uint32_t)a.v_token + lane % (D / 8) * 16);
+                    }
                 }
-                if constexpr (SRC == PLAID_SOURCE_BIAS) {
+                if constexpr (BIAS) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const int key = key0 + 16 * c + 4 * kg;
-                        const uint16_t *p = (const uint16_t *)a.bias + rq.key0 + key;
+                        const uint16_t *p = (const uint16_t *)a.bias + rq.key0;
                         uint16_t b[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) b[e] = key + e < len ? p[e] : (DT == PLAID_BF16 ? 0xff80 : 0xfc00);
+                        for (int e = 0; e < 4; ++e) {
+                            b[e] = p[min(key + e, len - 1)];
+                            if (key + e >= len) b[e] = DT == PLAID_BF16 ? 0xff80 : 0xfc00;
+                        }
                         x.bias[2 * c] = b[0] | (b[1] << 16), x.bias[2 * c + 1] = b[2] | (b[3] << 16);
                     }
                 }
             }
         };
+        // whether the wave has keys in the step; a key past the end stands in for none only where there is one
+        auto has = [&](int step) { return step < stop && step * (NW * 32) + wave * 32 < len; };
 
-        Piece<DT, D, SRC> now, next;
-        find(begin);
-        load(begin, now);
-        find(begin + 1);
-        for (int step = begin; step < stop; ++step) {
-            if (step + 1 < stop) {
-                load(step + 1, next);
-                find(step + 2);
+        if (has(begin)) {
+            find(begin);
+            load_k(begin);
+            load_v(begin);
+        }
+        for (int step = begin; has(step); ++step) {
+            const int key0 = step * (NW * 32) + wave * 32;
+            const bool more = has(step + 1);
+            const bool held0 = ok[0], held1 = ok[1];
+            int bias[4];
+            if (more) find(step + 1);
+            char *mine = nullptr;
+            if constexpr (!PAGED) {
+                mine = lds.v + wave * (32 * D * 2);
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const int unit = i * 64 + lane;
+                    *(i32x4 *)(mine + lds_chunk<D>(unit / (D / 8), unit % (D / 8))) = x.v[i];
+                }
+                if constexpr (BIAS)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) bias[e] = x.bias[e];
+                if (more) load_v(step + 1);
             }
-            const int key0 = step * FEW_KEYS + wave * 32;
-            if (key0 < len) {
-                char *mine = nullptr;
-                if constexpr (SRC != PLAID_SOURCE_PAGED) {
-                    mine = lds.v + wave * (32 * D * 2);
+            f32x4 s[2];
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const int unit = i * 64 + lane;
-                        *(i32x4 *)(mine + lds_chunk<D>(unit / (D / 8), unit % (D / 8))) = now.v[i];
+            for (int c = 0; c < 2; ++c) {
+                s[c] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int d = 0; d < KS; ++d) {
+                    i32x4 k;
+                    if constexpr (PAGED) {
+                        const float power = scale_power(x.ks[c], 0);
+                        const int w = x.k[c][d];
+                        k = i32x4{codes2<DT, 0>(w, power), codes2<DT, 1>(w, power), codes2<DT, 2>(w, power), codes2<DT, 3>(w, power)};
+                    } else {
+                        k = x.k[c][d];
                     }
+                    s[c] = mfma16<DT>(k, q[d], s[c]);
                 }
-                f32x4 s[2];
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    s[c] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                    for (int d = 0; d < KS; ++d) {
-                        i32x4 k;
-                        if constexpr (SRC == PLAID_SOURCE_PAGED) {
-                            const float power = scale_power(now.ks[c]);
-                            const int w = now.k[c][d];
-                            k = i32x4{codes2<DT, 0>(w, power), codes2<DT, 1>(w, power), codes2<DT, 2>(w, power), codes2<DT, 3>(w, power)};
-                        } else {
-                            k = now.k[c][d];
-                        }
-                        s[c] = mfma16<DT>(k, q[d], s[c]);
-                    }
-                }
-                bool hide = false;  // whether some key of the piece may be masked for some row
-                if constexpr (SRC == PLAID_SOURCE_BIAS) {
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float b = unpack<DT>(now.bias[2 * c + (e >> 1)], e & 1);
-                            s[c][e] = b == -INFINITY ? -INFINITY : fmaf(s[c][e], a.scale, b);
-                        }
-                } else {
-                    hide = key0 + 32 > least;
-                    if constexpr (SRC == PLAID_SOURCE_PAGED) hide = hide || !(now.ok[0] & now.ok[1]);
-                    if (hide) {
-#pragma unroll
-                        for (int c = 0; c < 2; ++c)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                bool seen = key0 + 16 * c + 4 * kg + e < limit;
-                                if constexpr (SRC == PLAID_SOURCE_PAGED) seen = seen && now.ok[c];
-                                s[c][e] = seen ? s[c][e] : -INFINITY;
-                            }
-                    }
-                }
-                float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                if (__any((top - m) * cs > 8.0f)) {
-                    const float to = fmaxf(m, top);
-                    const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - to) * cs);
-                    m = to;
-                    l *= alpha;
-#pragma unroll
-                    for (int t = 0; t < OT; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[t][e] *= alpha;
-                }
-                const float ref = m == -INFINITY ? 0.0f : m, ref_cs = ref * cs;
+            }
+            if (more) load_k(step + 1);
+            if constexpr (BIAS) {
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float x = SRC == PLAID_SOURCE_BIAS ? (s[c][e] - ref) * cs : fmaf(s[c][e], cs, -ref_cs);
-                        s[c][e] = __builtin_amdgcn_exp2f(x);
-                        l += s[c][e];
+                        const float b = unpack<DT>(bias[2 * c + (e >> 1)], e & 1);
+                        s[c][e] = b == -INFINITY ? -INFINITY : fmaf(s[c][e], a.scale, b);
                     }
-                const i32x4 p{pack2<DT>(s[0][0], s[0][1]), pack2<DT>(s[0][2], s[0][3]), pack2<DT>(s[1][0], s[1][1]), pack2<DT>(s[1][2], s[1][3])};
-                if constexpr (SRC == PLAID_SOURCE_PAGED) {
+            } else if (key0 + 32 > least || !held0 || !held1) {
+                // some key of the piece is hidden from some row
 #pragma unroll
-                    for (int g = 0; g < KS; ++g) {
-                        i32x4 lo, hi;
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const int w = now.v[c][g];
-                            float power[4];
-#pragma unroll
-                            for (int t = 0; t < 4; ++t) {
-                                const int byte = t * KS + g;
-                                power[t] = scale_power((now.vs[c][byte >> 2] >> ((byte & 3) * 8)) & 255);
-                                // a token past the end may hold anything: the smallest power keeps its products with 0 zero
-                                if (hide) power[t] = key0 + 16 * c + 4 * kg + t < len ? power[t] : 0.0f;
-                            }
-                            const int t0 = codes2<DT, 0>(w, power[0]), t1 = codes2<DT, 1>(w, power[1]), t2 = codes2<DT, 2>(w, power[2]),
-                                      t3 = codes2<DT, 3>(w, power[3]);
-                            lo[2 * c] = (int)__builtin_amdgcn_perm(t1, t0, 0x05040100), lo[2 * c + 1] = (int)__builtin_amdgcn_perm(t3, t2, 0x05040100);
-                            hi[2 * c] = (int)__builtin_amdgcn_perm(t1, t0, 0x07060302), hi[2 * c + 1] = (int)__builtin_amdgcn_perm(t3, t2, 0x07060302);
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = key0 + 16 * c + 4 * kg + e;
+                        s[c][e] = key < limit && (c ? held1 : held0) ? s[c][e] : -INFINITY;
+                        if constexpr (PAGED) {
+                            // a token past the end may hold anything: with the smallest power its products with a weight of 0 are 0
+                            if constexpr (D == 128) x.vs[c][e] = key < len ? x.vs[c][e] : 0;
+                            else x.vs[c][e >> 1] &= key < len ? -1 : (e & 1 ? 0xffff : (int)0xffff0000);
                         }
-                        o[2 * g] = mfma16<DT>(lo, p, o[2 * g]);
-                        o[2 * g + 1] = mfma16<DT>(hi, p, o[2 * g + 1]);
                     }
-                } else {
-                    i32x4 keep{-1, -1, -1, -1};  // what masked keys hold must not meet their zero weights
-                    if constexpr (SRC == PLAID_SOURCE_BIAS) {
+            }
+            const float top = max_halves(max_rows(larger(larger(larger(s[0][0], s[0][1]), larger(s[0][2], s[0][3])),
+                                                         larger(larger(s[1][0], s[1][1]), larger(s[1][2], s[1][3])))));
+            if (__any((top - m) * cs > 8.0f)) {
+                const float to = fmaxf(m, top);
+                const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - to) * cs);
+                m = to;
+                l *= alpha;
 #pragma unroll
-                        for (int w = 0; w < 4; ++w)
-                            keep[w] = (unpack<DT>(now.bias[w], 0) == -INFINITY ? 0 : 0xffff) | (unpack<DT>(now.bias[w], 1) == -INFINITY ? 0 : (int)0xffff0000);
-                    }
-                    const int rr = m16 >> 2, cc = (m16 & 3) >> 1, swz = (rr << 1) | (kg & 1);
-                    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                for (int t = 0; t < OT; ++t)
 #pragma unroll
-                    for (int t = 0; t < OT; ++t) {
-                        const char *x = mine + (4 * kg + rr) * (D * 2) + (((2 * t + cc) ^ swz) << 4) + (m16 & 1) * 8;
-                        const i32x2 u = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)x));
-                        const i32x2 w = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(x + 16 * (D * 2))));
-                        o[t] = mfma16<DT>(i32x4{u[0] & keep[0], u[1] & keep[1], w[0] & keep[2], w[1] & keep[3]}, p, o[t]);
+                    for (int e = 0; e < 4; ++e) o[t][e] *= alpha;
+            }
+            const float ref = m == -INFINITY ? 0.0f : m, ref_cs = ref * cs;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float y = BIAS ? (s[c][e] - ref) * cs : fmaf(s[c][e], cs, -ref_cs);
+                    s[c][e] = __builtin_amdgcn_exp2f(y);
+                    l += s[c][e];
+                }
+            const i32x4 p{pack2<DT>(s[0][0], s[0][1]), pack2<DT>(s[0][2], s[0][3]), pack2<DT>(s[1][0], s[1][1]), pack2<DT>(s[1][2], s[1][3])};
+            if constexpr (PAGED) {
+#pragma unroll
+                for (int g = 0; g < KS; ++g) {
+                    i32x4 lo, hi;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int w = x.v[c][g];
+                        int y[4];
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            const int byte = t * KS + g;  // scale bytes [token][group]
+                            const float power = scale_power(x.vs[c][byte >> 2], byte & 3);
+                            y[t] = t == 0 ? codes2<DT, 0>(w, power) : t == 1 ? codes2<DT, 1>(w, power) : t == 2 ? codes2<DT, 2>(w, power) : codes2<DT, 3>(w, power);
+                        }
+                        lo[2 * c] = (int)__builtin_amdgcn_perm(y[1], y[0], 0x05040100), lo[2 * c + 1] = (int)__builtin_amdgcn_perm(y[3], y[2], 0x05040100);
+                        hi[2 * c] = (int)__builtin_amdgcn_perm(y[1], y[0], 0x07060302), hi[2 * c + 1] = (int)__builtin_amdgcn_perm(y[3], y[2], 0x07060302);
                     }
+                    o[2 * g] = mfma16<DT>(lo, p, o[2 * g]);
+                    o[2 * g + 1] = mfma16<DT>(hi, p, o[2 * g + 1]);
+                }
+                if (more) load_v(step + 1);
+            } else {
+                i32x4 keep{-1, -1, -1, -1};  // what masked keys hold must not meet their zero weights
+                if constexpr (BIAS) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+                        keep[w] = (unpack<DT>(bias[w], 0) == -INFINITY ? 0 : 0xffff) | (unpack<DT>(bias[w], 1) == -INFINITY ? 0 : (int)0xffff0000);
+                }
+                const int rr = m16 >> 2, cc = (m16 & 3) >> 1, swz = (rr << 1) | (kg & 1);
+                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+#pragma unroll
+                for (int t = 0; t < OT; ++t) {
+                    const char *y = mine + (4 * kg + rr) * (D * 2) + (((2 * t + cc) ^ swz) << 4) + (m16 & 1) * 8;
+                    const i32x2 u = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)y));
+                    const i32x2 w = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(y + 16 * (D * 2))));
+                    if constexpr (BIAS) o[t] = mfma16<DT>(i32x4{u[0] & keep[0], u[1] & keep[1], w[0] & keep[2], w[1] & keep[3]}, p, o[t]);
+                    else o[t] = mfma16<DT>(i32x4{u[0], u[1], w[0], w[1]}, p, o[t]);
                 }
             }
-            if (step + 1 < stop) now = next;
         }
 
         // --- the waves' sums joined
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        const float natural = SRC == PLAID_SOURCE_BIAS ? m : (m == -INFINITY ? m : m * a.scale);
+        l = sum_halves(sum_rows(l));
+        const float natural = BIAS ? m : (m == -INFINITY ? m : m * a.scale);
         __syncthreads();  // the values of all waves have been read, and a former tile's sums
 #pragma unroll
         for (int t = 0; t < OT; ++t) *(f32x4 *)&lds.o[wave][m16][16 * t + 4 * kg] = o[t];
         if (kg == 0) lds.ml[wave][m16][0] = natural, lds.ml[wave][m16][1] = l;
         __syncthreads();
-        {
-            const int y = threadIdx.x >> 4, x = threadIdx.x & 15;  // a row and D / 16 of its dimensions
-            float top = -INFINITY, w[4], sum = 0.0f, acc[D / 16];
+        for (int u = threadIdx.x; u < FEW_ROWS * (D / 4); u += NW * 64) {
+            const int y = u / (D / 4), d = u % (D / 4) * 4;  // a row and 4 of its dimensions
+            float top = -INFINITY, sum = 0.0f;
+            f32x4 acc{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(top, lds.ml[i][y][0]);
+            for (int i = 0; i < NW; ++i) top = fmaxf(top, lds.ml[i][y][0]);
             const float ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = __builtin_amdgcn_exp2f((lds.ml[i][y][0] - ref) * LOG2E);
-                sum += w[i] * lds.ml[i][y][1];
-            }
+            for (int i = 0; i < NW; ++i) {
+                const float w = __builtin_amdgcn_exp2f((lds.ml[i][y][0] - ref) * LOG2E);
+                const f32x4 z = *(const f32x4 *)&lds.o[i][y][d];
+                sum += w * lds.ml[i][y][1];
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) {
-                acc[d] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[d] += w[i] * lds.o[i][y][x * (D / 16) + d];
+                for (int e = 0; e < 4; ++e) acc[e] += w * z[e];
             }
             const int row_out = tile * FEW_ROWS + y;
             if (begin == 0 && stop == rq.steps) {
@@ -396,18 +451,13 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a, int wo
                     const int tk = row_token(a, row_out);
                     const int64_t to = (rq.row0 + tk) * a.heads + head_kv * a.group + row_out - tk * a.group;
                     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-                    for (int d = 0; d < D / 16; d += 4)
-                        *(i32x2 *)(a.out + (to * D + x * (D / 16) + d) * 2) =
-                            i32x2{pack2<DT>(acc[d] * inv, acc[d + 1] * inv), pack2<DT>(acc[d + 2] * inv, acc[d + 3] * inv)};
-                    if (a.lse && x == 0) a.lse[2 * to] = sum == 0.0f ? -INFINITY : top, a.lse[2 * to + 1] = sum == 0.0f ? 0.0f : logf(sum);
+                    *(i32x2 *)(a.out + (to * D + d) * 2) = i32x2{pack2<DT>(acc[0] * inv, acc[1] * inv), pack2<DT>(acc[2] * inv, acc[3] * inv)};
+                    if (a.lse && d == 0) a.lse[2 * to] = sum == 0.0f ? -INFINITY : top, a.lse[2 * to + 1] = sum == 0.0f ? 0.0f : logf(sum);
                 }
             } else {
                 const int64_t slot = ((int64_t)worker * 2 + (begin == 0)) * a.kv_heads + head_kv;
-#pragma unroll
-                for (int d = 0; d < D / 16; d += 4)
-                    *(f32x4 *)(a.part_o + (slot * FEW_ROWS + y) * D + x * (D / 16) + d) = f32x4{acc[d], acc[d + 1], acc[d + 2], acc[d + 3]};
-                if (x == 0) a.part_ml[(slot * FEW_ROWS + y) * 2] = top, a.part_ml[(slot * FEW_ROWS + y) * 2 + 1] = sum;
+                *(f32x4 *)(a.part_o + (slot * FEW_ROWS + y) * D + d) = acc;
+                if (d == 0) a.part_ml[(slot * FEW_ROWS + y) * 2] = top, a.part_ml[(slot * FEW_ROWS + y) * 2 + 1] = sum;
             }
         }
         __syncthreads();  // before the next tile's values and sums
@@ -416,52 +466,70 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(AttendArgs a, int wo
 }
 
 // Tiles that several workers have parts of, joined in the order of the line.
-template <int DT, int D, int SRC>
-__global__ __launch_bounds__(256) void join_workers_kernel(AttendArgs a, int workers)
+#define JOIN_THREADS 512
+#define JOIN_PARTS 16
+template <int DT, int D, int NW, int SRC>
+__global__ __launch_bounds__(JOIN_THREADS) void join_workers_kernel(AttendArgs a, int workers)
 {
+    __shared__ float s_top[JOIN_THREADS], s_sum[JOIN_THREADS];
+    __shared__ __align__(16) f32x4 s_acc[JOIN_THREADS];
     const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, 4, blockIdx.x);
     if (tp.r < 0) return;
     const int head_kv = blockIdx.y;
-    int64_t before;
-    const int64_t total = all_work<SRC>(a, tp.r, before), share = (total + workers - 1) / workers;
-    const Request rq = request<SRC>(a, tp.r);
-    const int64_t begin = before + (int64_t)tp.tile * rq.steps, end = begin + rq.steps;
-    const int64_t w0 = begin / share, w1 = (end - 1) / share;
+    int before;
+    const int total = all_work<SRC, NW>(a, tp.r, before), share = (int)(((uint32_t)total + workers - 1) / (uint32_t)workers);
+    const Request rq = request<SRC, NW>(a, tp.r);
+    const int begin = before + tp.tile * rq.steps, end = begin + rq.steps;
+    const int w0 = (int)((uint32_t)begin / (uint32_t)share), w1 = (int)((uint32_t)(end - 1) / (uint32_t)share);
     if (w0 == w1) return;
-    const int y = threadIdx.x >> 4, x = threadIdx.x & 15, row = tp.tile * FEW_ROWS + y;
-    if (row >= rq.tokens * a.group) return;
-    auto place = [&](int64_t w) { return ((w * 2 + (w == w0)) * a.kv_heads + head_kv) * FEW_ROWS + y; };
-    float top = -INFINITY, sum = 0.0f, acc[D / 16];
-    for (int64_t w = w0; w <= w1; ++w) top = fmaxf(top, a.part_ml[2 * place(w)]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) acc[d] = 0.0f;
+    // PARTS groups of threads take every PARTS-th worker's sums each, then the groups' sums are joined: the order is fixed
+    const int rows = min(FEW_ROWS, rq.tokens * a.group - tp.tile * FEW_ROWS), units = rows * (D / 4);
+    const int parts = min(min(w1 - w0 + 1, JOIN_PARTS), JOIN_THREADS / units);
+    const int part = threadIdx.x / units, u = threadIdx.x % units, y = u / (D / 4), d = u % (D / 4) * 4;
+    auto place = [&](int w) { return (((int64_t)w * 2 + (w == w0)) * a.kv_heads + head_kv) * FEW_ROWS + y; };
+    float top = -INFINITY, sum = 0.0f;
+    f32x4 acc{0, 0, 0, 0};
+    if (part < parts) {
 #pragma unroll 4
-    for (int64_t w = w0; w <= w1; ++w) {
-        const int64_t p = place(w);
-        const float f = __builtin_amdgcn_exp2f((a.part_ml[2 * p] - ref) * LOG2E);
-        sum += f * a.part_ml[2 * p + 1];
+        for (int w = w0 + part; w <= w1; w += parts) top = fmaxf(top, a.part_ml[2 * place(w)]);
+        const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
+        for (int w = w0 + part; w <= w1; w += parts) {
+            const int64_t p = place(w);
+            const float f = __builtin_amdgcn_exp2f((a.part_ml[2 * p] - ref) * LOG2E);
+            sum += f * a.part_ml[2 * p + 1];
+            const f32x4 v = *(const f32x4 *)(a.part_o + p * D + d);
 #pragma unroll
-        for (int d = 0; d < D / 16; d += 4) {
-            const f32x4 v = *(const f32x4 *)(a.part_o + p * D + x * (D / 16) + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[d + e] += f * v[e];
+            for (int e = 0; e < 4; ++e) acc[e] += f * v[e];
         }
+        s_top[threadIdx.x] = top, s_sum[threadIdx.x] = sum, s_acc[threadIdx.x] = acc;
     }
-    const int tk = row_token(a, row);
+    __syncthreads();
+    if (part) return;
+    top = s_top[u];
+    for (int i = 1; i < parts; ++i) top = fmaxf(top, s_top[i * units + u]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    sum = 0.0f;
+    acc = f32x4{0, 0, 0, 0};
+    for (int i = 0; i < parts; ++i) {
+        const float f = __builtin_amdgcn_exp2f((s_top[i * units + u] - ref) * LOG2E);
+        const f32x4 v = s_acc[i * units + u];
+        sum += f * s_sum[i * units + u];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += f * v[e];
+    }
+    const int row = tp.tile * FEW_ROWS + y, tk = row_token(a, row);
     const int64_t to = (rq.row0 + tk) * a.heads + head_kv * a.group + row - tk * a.group;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-    for (int d = 0; d < D / 16; d += 4)
-        *(i32x2 *)(a.out + (to * D + x * (D / 16) + d) * 2) = i32x2{pack2<DT>(acc[d] * inv, acc[d + 1] * inv), pack2<DT>(acc[d + 2] * inv, acc[d + 3] * inv)};
-    if (a.lse && x == 0) a.lse[2 * to] = sum == 0.0f ? -INFINITY : top, a.lse[2 * to + 1] = sum == 0.0f ? 0.0f : logf(sum);
+    *(i32x2 *)(a.out + (to * D + d) * 2) = i32x2{pack2<DT>(acc[0] * inv, acc[1] * inv), pack2<DT>(acc[2] * inv, acc[3] * inv)};
+    if (a.lse && d == 0) a.lse[2 * to] = sum == 0.0f ? -INFINITY : top, a.lse[2 * to + 1] = sum == 0.0f ? 0.0f : logf(sum);
 }
 
 template <int DT, int D, int SRC>
 static void launch(hipStream_t st, const AttendArgs &a, int workers, int64_t tiles)
 {
-    attend_few_kernel<DT, D, SRC><<<dim3((unsigned)(workers * a.kv_heads)), dim3(256), 0, st>>>(a, workers);
-    if (workers > 1) join_workers_kernel<DT, D, SRC><<<dim3((unsigned)tiles, (unsigned)a.kv_heads), dim3(256), 0, st>>>(a, workers);
+    attend_few_kernel<DT, D, 4, SRC><<<dim3((unsigned)(workers * a.kv_heads)), dim3(256), 0, st>>>(a, workers);
+    if (workers > 1) join_workers_kernel<DT, D, 4, SRC><<<dim3((unsigned)tiles, (unsigned)a.kv_heads), dim3(JOIN_THREADS), 0, st>>>(a, workers);
 }
 template <int DT, int D>
 static void launch_source(hipStream_t st, const AttendArgs &a, int source, int workers, int64_t tiles)

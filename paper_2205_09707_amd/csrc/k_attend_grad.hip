@@ -144,7 +144,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
         __syncthreads();
     }
 
-    dbias += other_half(dbias);
+    dbias = sum_halves(dbias);
     if (!there) return;
     // a masked key's column may hold anything and is zero
     const bool masked = BIAS && bias == -INFINITY;

@@ -123,7 +123,7 @@ struct Stage<DT, D, NW, PLAID_SOURCE_PAGED> {
         for (int i = 0; i < N; ++i) {
             const int u = threadIdx.x + i * THREADS, key = unit_key(u);
             if (u < KU) {
-                const float power = scale_power(scale[i][0]);
+                const float power = scale_power(scale[i][0], 0);
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
                     *(i32x4 *)(b.k[buf] + lds_chunk<D>(key, (u % G) * 4 + w)) =
@@ -138,7 +138,7 @@ struct Stage<DT, D, NW, PLAID_SOURCE_PAGED> {
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
                         const int byte = t * G + g;
-                        power[t] = t < last[i] ? scale_power((scale[i][byte >> 2] >> ((byte & 3) * 8)) & 255) : 0.0f;
+                        power[t] = t < last[i] ? scale_power(scale[i][byte >> 2], byte & 3) : 0.0f;
                     }
                     const int w = code[i][g];
                     const int t0 = codes2<DT, 0>(w, power[0]), t1 = codes2<DT, 1>(w, power[1]), t2 = codes2<DT, 2>(w, power[2]),
@@ -274,10 +274,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
                     }
             }
         }
-        float top = fmaxf(s[0][0], s[1][0]);
+        float top = larger(s[0][0], s[1][0]);
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(s[0][i], s[1][i]));
-        top = fmaxf(top, other_half(top));
+        for (int i = 1; i < 16; ++i) top = larger(larger(top, s[0][i]), s[1][i]);
+        top = max_halves(top);
         if (__any((top - m) * cs > 8.0f)) {
             const float next = fmaxf(m, top);
             const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - next) * cs);
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         __syncthreads();
     }
 
-    l += other_half(l);
+    l = sum_halves(l);
     if (!there) return;
     const int64_t out_row = (tp.begin + token) * a.heads + head;
     const float natural = SRC == PLAID_SOURCE_BIAS ? m : (m == -INFINITY ? m : m * a.scale);

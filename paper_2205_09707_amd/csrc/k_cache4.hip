@@ -33,7 +33,7 @@ __device__ __forceinline__ uint32_t encode8(i32x4 x, int &scale)
     int e = (bits >> 23) - 129 + ((bits & 0x7fffff) > 0x400000);
     e = min(max(e, Limits<DT>::LOWEST), Limits<DT>::TOP);
     scale = top >= Limits<DT>::INF ? 255 : e + 127;
-    const float power = scale_power(e + 127), most = e == Limits<DT>::TOP ? 3.0f * power : INFINITY;  // 4 2^TOP is not finite in the type
+    const float power = __int_as_float((e + 127) << 23), most = e == Limits<DT>::TOP ? 3.0f * power : INFINITY;  // 4 2^TOP is not finite in the type
     uint32_t codes = 0;
     float y[8];
 #pragma unroll
@@ -126,13 +126,13 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c)
         const uint8_t *p = c.data + ((slot >> c.block_shift) * c.kv_heads + head) * region;
         if (c.k_out) {
             const int w = *(const int *)(p + in * (D / 2) + l * 4);
-            const float power = scale_power(p[bs * D + in * G + l / 4]);
+            const float power = scale_power(p[bs * D + in * G + l / 4], 0);
             k = i32x4{codes2<DT, 0>(w, power), codes2<DT, 1>(w, power), codes2<DT, 2>(w, power), codes2<DT, 3>(w, power)};
         }
         if (c.v_out) {
             // dims 32 i + 8 (l % 4) .. + 7: m = 8 (l % 2) .. and the half that l / 2 % 2 names
             const uint8_t *q = p + bs * (D / 2) + (in >> 4) * (8 * D) + (((in >> 2) & 3) * 16 + 8 * (l & 1)) * (D / 8) + (l >> 2) * 4 + (in & 3);
-            const float power = scale_power(p[bs * D + bs * G + in * G + l / 4]);
+            const float power = scale_power(p[bs * D + bs * G + in * G + l / 4], 0);
             const int half = ((l >> 1) & 1) * 4;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

@@ -51,6 +51,8 @@ struct GradArgs {
 // Keys that a step of attend_few's workgroup covers, rows of its tiles.
 #define FEW_KEYS 128
 #define FEW_ROWS 16
+// Waves of attend_few on a SIMD: what its registers allow without spills (dense D = 128 keeps 64 of them for loads under way).
+#define FEW_PER_SIMD(D, SRC) ((D) == 64 ? 4 : (SRC) == PLAID_SOURCE_PAGED ? 3 : 2)
 // Keys of a tile of attend_many.
 #define MANY_KEYS 64
 
@@ -148,10 +150,55 @@ __device__ __forceinline__ int codes2(int w, float power)
     if constexpr (DT == PLAID_BF16) return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((unsigned)w, power, BYTE));
     else return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4((unsigned)w, power, BYTE));
 }
-__device__ __forceinline__ float scale_power(int b) { return __int_as_float(b << 23); }  // 255: infinity, which makes every code NaN
+// The power of byte `byte` of w as codes2 takes it: the conversion reads the exponent's eight bits alone (bits 23 to 30, 255: every
+// code is NaN), so what a shift leaves in the others does not matter.
+__device__ __forceinline__ float scale_power(int w, int byte) { return __int_as_float(byte == 3 ? (int)((uint32_t)w >> 1) : w << (23 - 8 * byte)); }
 
-// The other half of the wave's value of the same lane % 32.
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// A lane's value and that of the lane 32 (16) further on, exchanged between registers.
+__device__ __forceinline__ float2 both_halves(float x)
+{
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return {__uint_as_float(y[0]), __uint_as_float(y[1])};
+}
+__device__ __forceinline__ float2 both_rows(float x)
+{
+    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return {__uint_as_float(y[0]), __uint_as_float(y[1])};
+}
+__device__ __forceinline__ float max_halves(float x)
+{
+    const float2 y = both_halves(x);
+    return fmaxf(y.x, y.y);
+}
+__device__ __forceinline__ float sum_halves(float x)
+{
+    const float2 y = both_halves(x);
+    return y.x + y.y;
+}
+__device__ __forceinline__ float max_rows(float x)
+{
+    const float2 y = both_rows(x);
+    return fmaxf(y.x, y.y);
+}
+__device__ __forceinline__ float sum_rows(float x)
+{
+    const float2 y = both_rows(x);
+    return y.x + y.y;
+}
+// The larger of two products' results; fmaxf would first make each of them quiet.
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
+
+// Loads of what every lane wants alike, through the scalar cache: arguments that no kernel writes while one reads them.
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T *p)
+{
+    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)x) | ((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32));
+}
 
 // Row / group and row % group.
 __device__ __forceinline__ int row_token(const AttendArgs &a, int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_magic); }

@@ -40,7 +40,16 @@ int check_cache(const plaid_paged_cache *c)
 }
 
 // Workgroups that fill the chip: 256 compute units, and what the kernels leave room for on each.
-constexpr int FEW_TARGET = 512, MANY_TARGET = 512;
+#ifndef BIGW
+#define BIGW 8
+#endif
+#ifndef BIGK
+#define BIGK 8
+#endif
+#ifndef BIGQ
+#define BIGQ 8
+#endif
+constexpr int UNITS = 256, MANY_TARGET = 512;
 
 struct Plan {
     bool few;
@@ -49,7 +58,6 @@ struct Plan {
     int64_t o_bytes, delta_bytes, bias_bytes, k_bytes, q_bytes;
 };
 
-// keys of a request on average (dense) or at most (paged)
 int64_t split_count(int64_t groups, int64_t steps, int64_t least)
 {
     if (groups >= MANY_TARGET * 3 / 4) return 1;
@@ -58,23 +66,24 @@ int64_t split_count(int64_t groups, int64_t steps, int64_t least)
     return s < 1 ? 1 : s > 64 ? 64 : s;
 }
 
-Plan plan_forward(const plaid_attention &a, int64_t keys, int64_t longest)
+// keys: of all requests; longest: that a request can have; usual: to reckon with
+Plan plan_forward(const plaid_attention &a, int source, int64_t keys, int64_t longest, int64_t usual)
 {
     Plan p = {};
     const int64_t group = a.heads / a.kv_heads, tokens = ceil_div(a.num_queries, a.n), rows = tokens * group;
-    p.few = rows <= 2 * FEW_ROWS;
+    p.tiles = a.num_queries * group / FEW_ROWS + a.n;
+    p.few = rows <= 2 * FEW_ROWS && p.tiles * (longest / FEW_KEYS + 1) < INT32_MAX;  // its counts of steps are 32 bits wide
     if (p.few) {
-        p.tiles = a.num_queries * group / FEW_ROWS + a.n;
         const int64_t line = (ceil_div(keys, FEW_KEYS) + a.n) * ceil_div(rows < 1 ? 1 : rows, FEW_ROWS);
-        int64_t w = ceil_div(FEW_TARGET, a.kv_heads);
+        const int64_t w = ceil_div(UNITS * FEW_PER_SIMD(a.head_dim, source), a.kv_heads);
         p.workers = (int)(w < line ? w : line);
         p.o_bytes = p.workers > 1 ? (int64_t)p.workers * 2 * a.kv_heads * FEW_ROWS * a.head_dim * 4 : 0;
         p.bytes = p.o_bytes + p.o_bytes / a.head_dim * 2;
         return p;
     }
-    p.waves = rows > 128 ? 8 : 4;
+    p.waves = rows > 128 ? BIGW : 4;
     p.tiles = a.num_queries * group / (p.waves * 32) + a.n;
-    p.splits = (int)split_count(ceil_div(rows, p.waves * 32) * a.n * a.kv_heads, ceil_div(longest, MANY_KEYS), 4);
+    p.splits = (int)split_count(ceil_div(rows, p.waves * 32) * a.n * a.kv_heads, ceil_div(usual, MANY_KEYS), 4);
     p.o_bytes = p.splits > 1 ? (int64_t)p.splits * a.num_queries * a.heads * a.head_dim * 4 : 0;
     p.bytes = p.o_bytes + p.o_bytes / a.head_dim * 2;
     return p;
@@ -84,8 +93,8 @@ Plan plan_backward(const plaid_attention &a)
 {
     Plan p = {};
     const int64_t group = a.heads / a.kv_heads, rows = ceil_div(a.num_queries, a.n) * group, keys = ceil_div(a.num_keys, a.n);
-    p.q_waves = rows > 128 ? 8 : 4;
-    p.k_waves = keys > 128 ? 8 : 4;
+    p.q_waves = rows > 128 ? BIGQ : 4;
+    p.k_waves = keys > 128 ? BIGK : 4;
     p.q_splits = (int)split_count(ceil_div(rows, p.q_waves * 32) * a.n * a.kv_heads, ceil_div(keys, 64), 4);
     p.k_splits = (int)split_count(ceil_div(keys, p.k_waves * 32) * a.n * a.kv_heads, ceil_div(rows, 32), 8);
     p.delta_bytes = round16(a.num_queries * a.heads * 4);
@@ -113,6 +122,7 @@ int check_rows(const char *what, const void *p, int64_t token, int64_t head)
 {
     if (!p || misaligned(p, 16)) FAIL("%s is null or not 16-byte aligned", what);
     if (token % 8 || head % 8) FAIL("the strides of %s are no multiples of 8 elements", what);
+    if (token < 0 || token >= 1 << 25) FAIL("the token stride of %s is out of range", what);  // 32 rows lie within 32 bits
     return PLAID_OK;
 }
 // Pointers that any attention call reads; out is an input of the backward pass.
@@ -256,7 +266,7 @@ static int check_cached(const plaid_attention *args, int32_t max_blocks, int32_t
 static Plan plan_cached(const plaid_attention &a, int32_t max_blocks, int32_t block_size)
 {
     const int64_t longest = (int64_t)max_blocks * block_size;
-    return plan_forward(a, longest * a.n, longest);
+    return plan_forward(a, PLAID_SOURCE_PAGED, longest * a.n, longest, longest);
 }
 
 extern "C" int plaid_cached_attention_workspace(const plaid_attention *args, int32_t max_blocks, int32_t block_size, int64_t *bytes)
@@ -285,11 +295,16 @@ extern "C" int plaid_cached_attention(const plaid_attention *args, const plaid_p
     return run_forward(*args, x, plan_cached(*args, max_blocks, cache->block_size), PLAID_SOURCE_PAGED, workspace, workspace_bytes, device, hip_stream);
 }
 
+static Plan plan_cross(const plaid_attention &a)
+{
+    return plan_forward(a, a.key_bias ? PLAID_SOURCE_BIAS : PLAID_SOURCE_DENSE, a.num_keys, a.num_keys, ceil_div(a.num_keys, a.n));
+}
+
 extern "C" int plaid_cross_attention_workspace(const plaid_attention *args, int32_t backward, int64_t *bytes)
 {
     if (!bytes) FAIL("bytes is null");
     if (const int rc = check_shape(args)) return rc;
-    *bytes = backward ? plan_backward(*args).bytes : plan_forward(*args, args->num_keys, ceil_div(args->num_keys, args->n)).bytes;
+    *bytes = backward ? plan_backward(*args).bytes : plan_cross(*args).bytes;
     return PLAID_OK;
 }
 
@@ -299,7 +314,7 @@ extern "C" int plaid_cross_attention(const plaid_attention *args, void *workspac
     if (const int rc = check_queries(args)) return rc;
     if (const int rc = check_keys(args)) return rc;
     AttendArgs x = attend_args(*args);
-    return run_forward(*args, x, plan_forward(*args, args->num_keys, ceil_div(args->num_keys, args->n)), x.bias ? PLAID_SOURCE_BIAS : PLAID_SOURCE_DENSE,
+    return run_forward(*args, x, plan_cross(*args), x.bias ? PLAID_SOURCE_BIAS : PLAID_SOURCE_DENSE,
                        workspace, workspace_bytes, device, hip_stream);
 }
 

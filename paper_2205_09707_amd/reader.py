@@ -75,11 +75,17 @@ def _strides(t: torch.Tensor) -> Tuple[int, int]:
 
 
 def _workspace(bytes_: int, device: torch.device):
-    return (None, None) if bytes_ == 0 else ((w := torch.empty(bytes_, dtype=torch.uint8, device=device)), _p._ptr(w))
+    """(tensor that the caller holds until its launches are made, its address)"""
+    if bytes_ == 0:
+        return None, None
+    w = torch.empty(bytes_, dtype=torch.uint8, device=device)
+    return w, w.data_ptr()
 
 
-def _ordinal(device: torch.device) -> int:
-    return device.index or 0
+def _where(device: torch.device) -> Tuple[int, int]:
+    """Ordinal of a device and torch's current stream there."""
+    i = device.index or 0
+    return i, torch._C._cuda_getCurrentRawStream(i)
 
 
 class PagedCache:
@@ -128,21 +134,17 @@ def plaid_block_tables(lengths: torch.Tensor, added: torch.Tensor, table: torch.
     lib, capacity = _p.load_library(), int(capacity)
     need = ct.c_int64(0)
     _p._check(lib.plaid_block_tables_workspace(n, capacity, ct.byref(need)))
-    # the five outputs are one allocation; each starts at a multiple of 16 bytes
     room = max(capacity, 0)
-    sizes = [8 * room, 8 * (n + 1), 8, 4 * room, 4 * n]
-    at, total = [], 0
-    for s in sizes:
-        at.append(total)
-        total += (s + 15) & ~15
-    buf = torch.empty(total, dtype=torch.uint8, device=dev)
-    slots, offsets, wanted, positions, totals = (
-        buf[a:a + s].view(t) for a, s, t in zip(at, sizes, (torch.int64, torch.int64, torch.int64, torch.int32, torch.int32)))
+    offsets = torch.empty(n + 1, dtype=torch.int64, device=dev)
+    totals = torch.empty(n, dtype=torch.int32, device=dev)
+    positions = torch.empty(room, dtype=torch.int32, device=dev)
+    slots = torch.empty(room, dtype=torch.int64, device=dev)
+    wanted = torch.empty(1, dtype=torch.int64, device=dev)
     work, ptr = _workspace(need.value, dev)
-    _p._check(lib.plaid_block_tables(_p._ptr(lengths), _p._ptr(added), n, _p._ptr(table), table.stride(0) if n > 1 else table.shape[1],
-                                     table.shape[1], _p._ptr(free_blocks), free_blocks.shape[0], int(block_size), _p._ptr(offsets),
-                                     _p._ptr(totals), _p._ptr(positions), _p._ptr(slots), capacity, _p._ptr(wanted), ptr, need.value,
-                                     _ordinal(dev), _p._stream(dev)))
+    _p._check(lib.plaid_block_tables(lengths.data_ptr(), added.data_ptr(), n, table.data_ptr(), table.stride(0) if n > 1 else table.shape[1],
+                                     table.shape[1], free_blocks.data_ptr(), free_blocks.shape[0], int(block_size), offsets.data_ptr(),
+                                     totals.data_ptr(), positions.data_ptr(), slots.data_ptr(), capacity, wanted.data_ptr(), ptr, need.value,
+                                     *_where(dev)))
     return offsets, totals, positions, slots, wanted
 
 
@@ -155,8 +157,8 @@ def plaid_cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots
             raise ValueError(f"{name} must have the shape {shape}, got {tuple(t.shape)}")
     slots = _vector(slots, "slots", torch.int64, dev)
     k, v = _rows(k), _rows(v)
-    _p._check(_p.load_library().plaid_cache_write(ct.byref(cache._view()), _p._ptr(k), _p._ptr(v), *_strides(k), *_strides(v), _p._ptr(slots),
-                                                  slots.shape[0], _ordinal(dev), _p._stream(dev)))
+    _p._check(_p.load_library().plaid_cache_write(ct.byref(cache._view()), k.data_ptr(), v.data_ptr(), *_strides(k), *_strides(v), slots.data_ptr(),
+                                                  slots.shape[0], *_where(dev)))
 
 
 def plaid_cache_read(cache: PagedCache, slots: torch.Tensor):
@@ -165,29 +167,19 @@ def plaid_cache_read(cache: PagedCache, slots: torch.Tensor):
     slots = _vector(slots, "slots", torch.int64, dev)
     k = torch.empty((slots.shape[0], cache.kv_heads, cache.head_dim), dtype=cache.dtype, device=dev)
     v = torch.empty_like(k)
-    _p._check(_p.load_library().plaid_cache_read(ct.byref(cache._view()), _p._ptr(slots), slots.shape[0], _p._ptr(k), _p._ptr(v), _ordinal(dev),
-                                                 _p._stream(dev)))
+    _p._check(_p.load_library().plaid_cache_read(ct.byref(cache._view()), slots.data_ptr(), slots.shape[0], k.data_ptr(), v.data_ptr(),
+                                                 *_where(dev)))
     return k, v
 
 
 def _attention(q, k, v, key_bias, q_offsets, k_offsets, kv_heads, scale, out, lse) -> plaid_attention:
-    a = plaid_attention()
-    a.dtype, a.n = _DTYPES[q.dtype], q_offsets.shape[0] - 1
-    a.num_queries, a.heads, a.head_dim = q.shape
-    a.kv_heads = kv_heads
-    a.scale = a.head_dim ** -0.5 if scale is None else float(scale)
-    a.q, a.q_offsets, a.out = q.data_ptr(), q_offsets.data_ptr(), out.data_ptr()
-    a.q_token_stride, a.q_head_stride = _strides(q)
-    if lse is not None:
-        a.lse = lse.data_ptr()
-    if k is not None:
-        a.num_keys = k.shape[0]
-        a.k, a.v, a.k_offsets = k.data_ptr(), v.data_ptr(), k_offsets.data_ptr()
-        a.k_token_stride, a.k_head_stride = _strides(k)
-        a.v_token_stride, a.v_head_stride = _strides(v)
-        if key_bias is not None:
-            a.key_bias = key_bias.data_ptr()
-    return a
+    tokens, heads, head_dim = q.shape
+    head = (_DTYPES[q.dtype], q_offsets.shape[0] - 1, heads, kv_heads, head_dim, head_dim ** -0.5 if scale is None else float(scale), tokens)
+    tail = (out.data_ptr(), None if lse is None else lse.data_ptr())
+    if k is None:
+        return plaid_attention(*head, 0, q.data_ptr(), None, None, None, *_strides(q), 0, 0, 0, 0, q_offsets.data_ptr(), None, *tail)
+    return plaid_attention(*head, k.shape[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), None if key_bias is None else key_bias.data_ptr(),
+                           *_strides(q), *_strides(k), *_strides(v), q_offsets.data_ptr(), k_offsets.data_ptr(), *tail)
 
 
 def _check_heads(q: torch.Tensor, kv_heads: int, head_dim: int) -> None:
@@ -229,8 +221,8 @@ def plaid_cached_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tens
     need = ct.c_int64(0)
     _p._check(lib.plaid_cached_attention_workspace(ct.byref(a), table.shape[1], cache.block_size, ct.byref(need)))
     work, ptr = _workspace(need.value, dev)
-    _p._check(lib.plaid_cached_attention(ct.byref(a), ct.byref(cache._view()), _p._ptr(table), table.stride(0) if n > 1 else table.shape[1],
-                                         table.shape[1], _p._ptr(lengths), 1 if causal else 0, ptr, need.value, _ordinal(dev), _p._stream(dev)))
+    _p._check(lib.plaid_cached_attention(ct.byref(a), ct.byref(cache._view()), table.data_ptr(), table.stride(0) if n > 1 else table.shape[1],
+                                         table.shape[1], lengths.data_ptr(), 1 if causal else 0, ptr, need.value, *_where(dev)))
     return (out, lse) if return_lse else out
 
 
@@ -265,7 +257,7 @@ def plaid_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_o
     need = ct.c_int64(0)
     _p._check(lib.plaid_cross_attention_workspace(ct.byref(a), 0, ct.byref(need)))
     work, ptr = _workspace(need.value, dev)
-    _p._check(lib.plaid_cross_attention(ct.byref(a), ptr, need.value, _ordinal(dev), _p._stream(dev)))
+    _p._check(lib.plaid_cross_attention(ct.byref(a), ptr, need.value, *_where(dev)))
     return (out, lse) if return_lse else out
 
 
@@ -293,6 +285,6 @@ def plaid_cross_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torc
     need = ct.c_int64(0)
     _p._check(lib.plaid_cross_attention_workspace(ct.byref(a), 1, ct.byref(need)))
     work, ptr = _workspace(need.value, dev)
-    _p._check(lib.plaid_cross_attention_backward(ct.byref(a), _p._ptr(d_out), _p._ptr(dq), _p._ptr(dk), _p._ptr(dv), _p._ptr(dbias), ptr, need.value,
-                                                 _ordinal(dev), _p._stream(dev)))
+    _p._check(lib.plaid_cross_attention_backward(ct.byref(a), d_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), None if dbias is None else dbias.data_ptr(), ptr, need.value,
+                                                 *_where(dev)))
     return dq, dk, dv, dbias
