@@ -151,8 +151,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
     constexpr bool PAGED = SRC == PLAID_SOURCE_PAGED, BIAS = SRC == PLAID_SOURCE_BIAS;
     __shared__ __align__(16) FewLds<D, NW, SRC> lds;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), kg = lane >> 4, m16 = lane & 15;
-    const int id = (int)xcd_order(blockIdx.x, gridDim.x);
-    const int head_kv = id / workers, worker = id % workers;
+    const int head_kv = blockIdx.x % a.kv_heads, worker = blockIdx.x / a.kv_heads;
     int at, end, first;
     int r = find_work<SRC, NW>(a, workers, worker, at, end, first);
     if (r < 0) return;
@@ -409,7 +408,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
                     for (int w = 0; w < 4; ++w)
                         keep[w] = (unpack<DT>(bias[w], 0) == -INFINITY ? 0 : 0xffff) | (unpack<DT>(bias[w], 1) == -INFINITY ? 0 : (int)0xffff0000);
                 }
-                const int rr = m16 >> 2, cc = (m16 & 3) >> 1, swz = (rr << 1) | (kg & 1);
+                const int rr = m16 >> 2, cc = (m16 & 3) >> 1, swz = swizzle<D>(4 * kg + rr);  // rows 16 apart have one number
                 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 #pragma unroll
                 for (int t = 0; t < OT; ++t) {

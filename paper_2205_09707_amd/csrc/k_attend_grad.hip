@@ -39,11 +39,9 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     __shared__ __align__(16) char s_q[2][GRAD_ROWS * D * 2], s_o[2][GRAD_ROWS * D * 2];
     __shared__ __align__(16) float s_m[2][GRAD_ROWS], s_l[2][GRAD_ROWS], s_delta[2][GRAD_ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    int64_t id = xcd_order(blockIdx.x, gridDim.x);
-    const int64_t place = id % tiles;
-    id /= tiles;
-    const int head = (int)(id % a.kv_heads), split = (int)(id / a.kv_heads);
-    const TilePlace tp = find_tile(a.k_offsets, a.n, a.num_keys, 1, SHIFT, place);
+    const WorkPlace w = work_place(a, tiles);
+    const int head = w.head, split = w.split;
+    const TilePlace tp = find_tile(a.k_offsets, a.n, a.num_keys, 1, SHIFT, w.place);
     if (tp.r < 0) return;
     const int len = (int)(tp.end - tp.begin);
     const int64_t row0 = clamp64(a.q_offsets[tp.r], 0, a.num_queries);
@@ -178,11 +176,9 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
     __shared__ __align__(16) char s_k[2][GRAD_KEYS * D * 2], s_v[2][GRAD_KEYS * D * 2];
     __shared__ __align__(16) float s_bias[2][BIAS ? GRAD_KEYS : 4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    int64_t id = xcd_order(blockIdx.x, gridDim.x);
-    const int64_t place = id % tiles;
-    id /= tiles;
-    const int head_kv = (int)(id % a.kv_heads), split = (int)(id / a.kv_heads);
-    const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, place);
+    const WorkPlace w = work_place(a, tiles);
+    const int head_kv = w.head, split = w.split;
+    const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place);
     if (tp.r < 0) return;
     const int tokens = (int)(tp.end - tp.begin), rows = tokens * a.group;
     const int64_t key0 = clamp64(a.k_offsets[tp.r], 0, a.num_keys);

@@ -7,17 +7,24 @@
 // of the wave half of its keys each: the maximum and the sum need one exchange, and the result's registers, rounded, are
 // already the operand of o^T = v^T p^T (rows of v^T come from LDS by the transposing read, or lie transposed there).  q stays
 // in registers, keys and values of 64 keys at a time go through LDS twice buffered; the next tile's loads are in flight while
-// this one is multiplied.  The maximum that p is taken against lags behind the true one by up to 2^8: o is rescaled only
-// where it would fall further back.
-template <int DT, int D, int NW, int SRC>
-struct Stage;  // one tile on its way from memory to LDS
+// this one is multiplied.  m lags behind the maximum by up to 2^8: o is rescaled only where it would fall further back.
+// Tiles that lie in LDS at a time, and how many tiles ahead of the weights' one keys and values are asked for.  With two groups of
+// waves (see below) a tile of keys is read in two phases and one of values in the two after those; a buffer is filled anew from
+// the second phase of a step on.
+template <int NW, int SRC>
+struct Ahead {
+    static constexpr bool PAGED = SRC == PLAID_SOURCE_PAGED;
+    static constexpr int GROUPS = NW == 8 ? 2 : 1, TILES = PAGED || NW == 4 ? 2 : 4;
+    static constexpr int K = PAGED ? 1 : TILES - GROUPS + 1, V = PAGED ? 0 : TILES - GROUPS;
+};
 
-template <int D, int SRC>
+template <int D, int NW, int SRC>
 struct TileBuffers {
-    char k[2][MANY_KEYS * D * 2];
-    char v[2][SRC == PLAID_SOURCE_PAGED ? D * (MANY_KEYS + 4) * 2 : MANY_KEYS * D * 2];
-    float bias[2][SRC == PLAID_SOURCE_BIAS ? MANY_KEYS : 4];
-    int cell[2][4];  // paged: whether the cells of 16 keys have a block
+    static constexpr int TILES = Ahead<NW, SRC>::TILES;
+    char k[TILES][MANY_KEYS * D * 2];
+    char v[TILES][SRC == PLAID_SOURCE_PAGED ? D * (MANY_KEYS + 4) * 2 : MANY_KEYS * D * 2];
+    float bias[SRC == PLAID_SOURCE_BIAS ? NW : 1][2][SRC == PLAID_SOURCE_BIAS ? MANY_KEYS : 4];  // each wave's own
+    int cell[4][4];  // paged: whether the cells of 16 keys have a block
 };
 
 struct KeyRange {
@@ -26,136 +33,237 @@ struct KeyRange {
     int r, head;   // request, key head
 };
 
+// How a workgroup's waves bring tiles into LDS: dense keys and values go there straight from memory, each wave its share.
 template <int DT, int D, int NW, int SRC>
 struct Stage {
-    static constexpr int THREADS = NW * 64, CHUNKS = D / 8, N = (MANY_KEYS * CHUNKS + THREADS - 1) / THREADS;
-    i32x4 k[N], v[N];
-    float bias;
-    __device__ __forceinline__ void start(const AttendArgs &, const KeyRange &, int) {}
-    __device__ __forceinline__ void load(const AttendArgs &a, const KeyRange &kr, int step)
+    static constexpr int TILES = Ahead<NW, SRC>::TILES, CHUNKS = D / 8, AT_ONCE = 512 / D, N = MANY_KEYS / AT_ONCE / NW;  // loads of a wave a tile
+    static constexpr bool BIAS = SRC == PLAID_SOURCE_BIAS;
+    static constexpr uint16_t NONE = DT == PLAID_BF16 ? 0xff80 : 0xfc00;  // -infinity
+    uint16_t bias;           // of the lane's key in the tile after the one whose biases lie in LDS
+    uint64_t masked, after;  // masked keys of the tile whose biases are used, and of the next one
+
+    // Keys past the end repeat the last one.  The tiles after the last repeat that one, so that a phase's number of loads is fixed.
+    __device__ __forceinline__ void load(const KeyRange &kr, const char *rows, int64_t token, int64_t head, int tile, char *to)
     {
+        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), last = kr.len - 1 - tile * MANY_KEYS;
+        const char *base = rows + (kr.base + tile * MANY_KEYS) * token + kr.head * head;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int id = threadIdx.x + i * THREADS, key = id / CHUNKS, c = id % CHUNKS, at = step * MANY_KEYS + key;
-            k[i] = v[i] = i32x4{0, 0, 0, 0};
-            bool there = id < MANY_KEYS * CHUNKS && at < kr.len;
-            // what a masked key holds is never used: infinities there would make products with zero weights not a number
-            if constexpr (SRC == PLAID_SOURCE_BIAS) there = there && load16<DT>(a.bias + 2 * (kr.base + at)) != -INFINITY;
-            if (there) {
-                k[i] = *(const i32x4 *)(a.k + (kr.base + at) * a.k_token + kr.head * a.k_head + c * 16);
-                v[i] = *(const i32x4 *)(a.v + (kr.base + at) * a.v_token + kr.head * a.v_head + c * 16);
-            }
-        }
-        if constexpr (SRC == PLAID_SOURCE_BIAS) {
-            const int at = step * MANY_KEYS + threadIdx.x;
-            if (threadIdx.x < MANY_KEYS) bias = at < kr.len ? load16<DT>(a.bias + 2 * (kr.base + at)) : -INFINITY;
+            const int row = (wave * N + i) * AT_ONCE + lane / CHUNKS, chunk = (lane % CHUNKS) ^ swizzle<D>(row);
+            load_to_lds(base, (uint32_t)min(row, last) * (uint32_t)token + chunk * 16, to + (wave * N + i) * 1024);
         }
     }
-    __device__ __forceinline__ void store(TileBuffers<D, SRC> &b, int buf)
+    __device__ __forceinline__ void load_k(const AttendArgs &a, const KeyRange &kr, int tile, int end, TileBuffers<D, NW, SRC> &b)
     {
+        load(kr, a.k, a.k_token, a.k_head, min(tile, end - 1), b.k[tile % TILES]);
+    }
+    __device__ __forceinline__ void load_v(const AttendArgs &a, const KeyRange &kr, int tile, int end, TileBuffers<D, NW, SRC> &b)
+    {
+        load(kr, a.v, a.v_token, a.v_head, min(tile, end - 1), b.v[tile % TILES]);
+    }
+    __device__ __forceinline__ void load_bias(const AttendArgs &a, const KeyRange &kr, int tile, int end)
+    {
+        const int lane = threadIdx.x & 63, t = min(tile, end - 1), last = kr.len - 1 - t * MANY_KEYS;
+        bias = ((const uint16_t *)a.bias + kr.base + t * MANY_KEYS)[(uint32_t)min(lane, last)];
+    }
+    __device__ __forceinline__ void store_bias(const KeyRange &kr, TileBuffers<D, NW, SRC> &b, int tile)
+    {
+        const int lane = threadIdx.x & 63;
+        const uint16_t x = tile * MANY_KEYS + lane < kr.len ? bias : NONE;
+        b.bias[threadIdx.x >> 6][tile & 1][lane] = unpack<DT>(x, 0);
+        after = __ballot(x == NONE);
+    }
+    // What a masked key holds is replaced by zeros: an infinity there would make a product with a weight of zero not a number.
+    // The keys go round the first `waves` waves.
+    __device__ __forceinline__ void clear(char *tile, uint64_t keys, int waves)
+    {
+        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+        if (wave >= waves) return;
+        for (keys &= (waves == 8 ? 0x0101010101010101ull : 0x1111111111111111ull) << wave; keys; keys &= keys - 1)
+            if (lane < CHUNKS) *(i32x4 *)(tile + __builtin_ctzll(keys) * (D * 2) + lane * 16) = i32x4{0, 0, 0, 0};
+    }
+    // Before the first phase: asks for the first tiles and waits for the first one's keys.
+    __device__ __forceinline__ void start(const AttendArgs &a, const KeyRange &kr, int begin, int end, TileBuffers<D, NW, SRC> &b)
+    {
+        using A = Ahead<NW, SRC>;
+        if constexpr (BIAS) load_bias(a, kr, begin, end);
+        load_k(a, kr, begin, end, b);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int id = threadIdx.x + i * THREADS, key = id / CHUNKS, c = id % CHUNKS;
-            if (id < MANY_KEYS * CHUNKS) {
-                *(i32x4 *)(b.k[buf] + lds_chunk<D>(key, c)) = k[i];
-                *(i32x4 *)(b.v[buf] + lds_chunk<D>(key, c)) = v[i];
-            }
+        for (int i = 1; i < A::K; ++i) {
+            load_k(a, kr, begin + i, end, b);
+            load_v(a, kr, begin + i - 1, end, b);
         }
-        if constexpr (SRC == PLAID_SOURCE_BIAS)
-            if (threadIdx.x < MANY_KEYS) b.bias[buf][threadIdx.x] = bias;
+        if constexpr (BIAS) {
+            store_bias(kr, b, begin);
+            masked = after;
+            load_bias(a, kr, begin + 1, end);
+            wait_loads<0>();
+            lds_barrier();
+            clear(b.k[begin % TILES], masked, NW);
+        } else {
+            wait_loads<2 * N *(A::K - 1)>();
+        }
+        lds_barrier();
+    }
+    // In the second phase of a step, after its weights.
+    __device__ __forceinline__ void bring(const AttendArgs &a, const KeyRange &kr, int step, int end, int, TileBuffers<D, NW, SRC> &b)
+    {
+        using A = Ahead<NW, SRC>;
+        if constexpr (BIAS) {
+            store_bias(kr, b, step + 1);
+            clear(b.k[(step + 1) % TILES], after, 4);
+            clear(b.v[step % TILES], masked, 4);
+            masked = after;
+            load_bias(a, kr, step + 2, end);
+        }
+        load_k(a, kr, step + A::K, end, b);
+        load_v(a, kr, step + A::V, end, b);
+    }
+    // At the end of a phase: what the phases after the next barrier need has arrived.  A step asks for 2 N pieces (and its bias);
+    // the next step's keys and this one's values must be there after its second phase, with a bias (see clear) after its first.
+    __device__ __forceinline__ void arrive(bool second, int late)
+    {
+        constexpr int STEP = 2 * N + BIAS;
+        if constexpr (Ahead<NW, SRC>::GROUPS == 2) {
+            if constexpr (BIAS) {
+                if (second == (late == 1)) wait_loads<STEP *(TILES - 3)>();
+            } else {
+                if (second && !late) wait_loads<STEP *(TILES - 2)>();
+                if (!second && late) wait_loads<STEP *(TILES - 3)>();
+            }
+        } else if constexpr (BIAS) {
+            if (!second) wait_loads<0>();
+        } else {
+            if (second) wait_loads<STEP *(TILES - 1)>();
+        }
     }
 };
 
-// Paged: a unit is 32 dimensions of a key (one scale), or a lane's part of a cell of value codes (4 tokens, D / 16
-// dimensions), turned into 16-bit values on the way into LDS.  The block ids are read one tile ahead of the codes.
+// Paged: a unit is 32 dimensions of a key (one scale), or a lane's part of a cell of value codes (4 tokens, D / 16 dimensions),
+// turned into 16-bit values on the way into LDS.  The units of keys come first, so that a wave has one kind.  Block ids are read
+// one tile ahead of the codes.
 template <int DT, int D, int NW>
 struct Stage<DT, D, NW, PLAID_SOURCE_PAGED> {
     static constexpr int THREADS = NW * 64, G = D / 32, KU = MANY_KEYS * G, VU = MANY_KEYS / 16 * 64, N = (KU + VU + THREADS - 1) / THREADS;
-    int id_next[N], ok[N];
+    int id_next[N], ok[N], last[N];
     i32x4 code[N], scale[N];
-    int len, last[N];
 
     // first key of a unit in its tile
     static __device__ __forceinline__ int unit_key(int u) { return u < KU ? u / G : ((u - KU) >> 6) * 16 + (((u - KU) >> 4) & 3) * 4; }
 
-    __device__ __forceinline__ void find(const AttendArgs &a, const KeyRange &kr, int step)
+    // As above nothing is loaded under a condition: the last key's block stands for what is past the end, the first block for an id
+    // outside the cache (a request of a cache without blocks has no keys).
+    template <bool KEYS>
+    __device__ __forceinline__ void find(const AttendArgs &a, const KeyRange &kr, int tile)
     {
+        const int32_t *row = a.table + kr.r * a.table_stride;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int u = threadIdx.x + i * THREADS, at = step * MANY_KEYS + unit_key(u);
-            id_next[i] = u < KU + VU && at < kr.len ? a.table[kr.r * a.table_stride + (at >> a.block_shift)] : -1;
+            const int u = threadIdx.x + i * THREADS;
+            if ((u < KU) != KEYS) continue;
+            id_next[i] = row[(uint32_t)(min(tile * MANY_KEYS + unit_key(u), kr.len - 1) >> a.block_shift)];
         }
     }
-    __device__ __forceinline__ void start(const AttendArgs &a, const KeyRange &kr, int step) { find(a, kr, step); }
-    __device__ __forceinline__ void load(const AttendArgs &a, const KeyRange &kr, int step)
+    template <bool KEYS>
+    __device__ __forceinline__ void load(const AttendArgs &a, const KeyRange &kr, int tile)
     {
-        const int64_t bs = 1ll << a.block_shift, region = bs * D * 17 / 16;
+        const uint32_t bs = 1u << a.block_shift, region = bs * (D * 17 / 16);
+        const uint8_t *heads = a.cache + (int64_t)kr.head * region;
+        const int64_t block = (int64_t)a.kv_heads * region;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int u = threadIdx.x + i * THREADS, at = step * MANY_KEYS + unit_key(u);
-            const int in = at & (int)(bs - 1);
+            const int u = threadIdx.x + i * THREADS, at = tile * MANY_KEYS + unit_key(u);
+            if ((u < KU) != KEYS) continue;
+            const uint32_t in = at & (bs - 1);
             ok[i] = (uint32_t)id_next[i] < (uint64_t)a.num_blocks;
-            last[i] = kr.len - at;  // tokens of the unit that there are
-            code[i] = scale[i] = i32x4{0, 0, 0, 0};
-            if (ok[i]) {
-                const uint8_t *p = a.cache + ((int64_t)id_next[i] * a.kv_heads + kr.head) * region;
-                if (u < KU) {
-                    code[i] = *(const i32x4 *)(p + in * (D / 2) + (u % G) * 16);
-                    scale[i][0] = p[bs * D + in * G + u % G];
+            last[i] = ok[i] ? kr.len - at : 0;  // tokens of the unit that there are
+            const uint8_t *p = heads + (ok[i] ? id_next[i] : 0) * block;
+            if constexpr (KEYS) {
+                code[i] = *(const i32x4 *)(p + (in * (D / 2) + (u % G) * 16));
+                scale[i][0] = p[bs * D + in * G + u % G];
+            } else {
+                const uint32_t l = (u - KU) & 63;
+                const uint8_t *c = p + (bs * (D / 2) + (in >> 4) * (8 * D) + l * (D / 8)), *s = p + (bs * (D + G) + in * G);
+                if constexpr (D == 128) {
+                    code[i] = *(const i32x4 *)c;
+                    scale[i] = *(const i32x4 *)s;
                 } else {
-                    const int l = (u - KU) & 63;
-                    const uint8_t *c = p + bs * (D / 2) + (in >> 4) * (8 * D) + l * (D / 8), *s = p + bs * D + bs * G + in * G;
-                    if constexpr (D == 128) {
-                        code[i] = *(const i32x4 *)c;
-                        scale[i] = *(const i32x4 *)s;
-                    } else {
-                        const i32x2 x = *(const i32x2 *)c, y = *(const i32x2 *)s;
-                        code[i][0] = x[0], code[i][1] = x[1], scale[i][0] = y[0], scale[i][1] = y[1];
-                    }
+                    const i32x2 x = *(const i32x2 *)c, y = *(const i32x2 *)s;
+                    code[i][0] = x[0], code[i][1] = x[1], scale[i][0] = y[0], scale[i][1] = y[1];
                 }
             }
         }
-        find(a, kr, step + 1);
+        find<KEYS>(a, kr, tile + 1);
     }
-    __device__ __forceinline__ void store(TileBuffers<D, PLAID_SOURCE_PAGED> &b, int buf)
+    __device__ __forceinline__ void load_k(const AttendArgs &a, const KeyRange &kr, int tile) { load<true>(a, kr, tile); }
+    __device__ __forceinline__ void load_v(const AttendArgs &a, const KeyRange &kr, int tile) { load<false>(a, kr, tile); }
+    __device__ __forceinline__ void store_k(TileBuffers<D, NW, PLAID_SOURCE_PAGED> &b, int tile)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int u = threadIdx.x + i * THREADS, key = unit_key(u);
-            if (u < KU) {
-                const float power = scale_power(scale[i][0], 0);
+            if (u >= KU) continue;
+            const float power = scale_power(scale[i][0], 0);
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    *(i32x4 *)(b.k[buf] + lds_chunk<D>(key, (u % G) * 4 + w)) =
-                        i32x4{codes2<DT, 0>(code[i][w], power), codes2<DT, 1>(code[i][w], power), codes2<DT, 2>(code[i][w], power),
-                              codes2<DT, 3>(code[i][w], power)};
-            } else if (u < KU + VU) {
-                const int m = (u - KU) & 15;
+            for (int w = 0; w < 4; ++w)
+                *(i32x4 *)(b.k[tile & 1] + lds_chunk<D>(key, (u % G) * 4 + w)) =
+                    i32x4{codes2<DT, 0>(code[i][w], power), codes2<DT, 1>(code[i][w], power), codes2<DT, 2>(code[i][w], power),
+                          codes2<DT, 3>(code[i][w], power)};
+            if (u % (16 * G) == 0) b.cell[tile & 3][key >> 4] = ok[i];
+        }
+    }
+    __device__ __forceinline__ void store_v(TileBuffers<D, NW, PLAID_SOURCE_PAGED> &b, int tile)
+    {
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    // scale bytes [token][group]; a token past the end gets the smallest power: finite, and its weight is 0
-                    float power[4];
+        for (int i = 0; i < N; ++i) {
+            const int u = threadIdx.x + i * THREADS, key = unit_key(u);
+            if (u < KU || u >= KU + VU) continue;
+            const int m = (u - KU) & 15;
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const int byte = t * G + g;
-                        power[t] = t < last[i] ? scale_power(scale[i][byte >> 2], byte & 3) : 0.0f;
-                    }
-                    const int w = code[i][g];
-                    const int t0 = codes2<DT, 0>(w, power[0]), t1 = codes2<DT, 1>(w, power[1]), t2 = codes2<DT, 2>(w, power[2]),
-                              t3 = codes2<DT, 3>(w, power[3]);
-                    const i32x2 low{(int)__builtin_amdgcn_perm(t1, t0, 0x05040100), (int)__builtin_amdgcn_perm(t3, t2, 0x05040100)};
-                    const i32x2 high{(int)__builtin_amdgcn_perm(t1, t0, 0x07060302), (int)__builtin_amdgcn_perm(t3, t2, 0x07060302)};
-                    *(i32x2 *)(b.v[buf] + (32 * g + m) * ((MANY_KEYS + 4) * 2) + key * 2) = low;
-                    *(i32x2 *)(b.v[buf] + (32 * g + 16 + m) * ((MANY_KEYS + 4) * 2) + key * 2) = high;
+            for (int g = 0; g < G; ++g) {
+                // scale bytes [token][group]; a token past the end gets the smallest power: finite, and its weight is 0
+                float power[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int byte = t * G + g;
+                    power[t] = t < last[i] ? scale_power(scale[i][byte >> 2], byte & 3) : 0.0f;
                 }
-                if (((u - KU) & 63) == 0) b.cell[buf][(u - KU) >> 6] = ok[i];
+                const int w = code[i][g];
+                const int t0 = codes2<DT, 0>(w, power[0]), t1 = codes2<DT, 1>(w, power[1]), t2 = codes2<DT, 2>(w, power[2]),
+                          t3 = codes2<DT, 3>(w, power[3]);
+                const i32x2 low{(int)__builtin_amdgcn_perm(t1, t0, 0x05040100), (int)__builtin_amdgcn_perm(t3, t2, 0x05040100)};
+                const i32x2 high{(int)__builtin_amdgcn_perm(t1, t0, 0x07060302), (int)__builtin_amdgcn_perm(t3, t2, 0x07060302)};
+                *(i32x2 *)(b.v[tile & 1] + (32 * g + m) * ((MANY_KEYS + 4) * 2) + key * 2) = low;
+                *(i32x2 *)(b.v[tile & 1] + (32 * g + 16 + m) * ((MANY_KEYS + 4) * 2) + key * 2) = high;
             }
         }
     }
+    __device__ __forceinline__ void start(const AttendArgs &a, const KeyRange &kr, int begin, int end, TileBuffers<D, NW, PLAID_SOURCE_PAGED> &b)
+    {
+        find<true>(a, kr, begin);
+        find<false>(a, kr, begin);
+        load_k(a, kr, begin);
+        store_k(b, begin);
+        if (begin + 1 < end) load_k(a, kr, begin + 1);
+        load_v(a, kr, begin);
+        lds_barrier();
+        if (NW == 8 && threadIdx.x >= 256) bring(a, kr, begin - 1, end, 1, b);
+    }
+    // In its second phase of step t group g brings keys t + 1 + g and values t + g: nobody reads their buffers in that phase or the
+    // one beside it.  Then it asks for the next ones.
+    __device__ __forceinline__ void bring(const AttendArgs &a, const KeyRange &kr, int step, int end, int late, TileBuffers<D, NW, PLAID_SOURCE_PAGED> &b)
+    {
+        const int tile = step + late;
+        if (tile + 1 < end) store_k(b, tile + 1);
+        if (tile < end) store_v(b, tile);
+        if (tile + 2 < end) load_k(a, kr, tile + 2);
+        if (tile + 1 < end) load_v(a, kr, tile + 1);
+    }
+    __device__ __forceinline__ void arrive(bool, int) {}
 };
 
-template <int D, int SRC>
-__device__ __forceinline__ i32x4 value_operand(const TileBuffers<D, SRC> &b, int buf, int base, int dt)
+template <int D, int NW, int SRC>
+__device__ __forceinline__ i32x4 value_operand(const TileBuffers<D, NW, SRC> &b, int buf, int base, int dt)
 {
     if constexpr (SRC == PLAID_SOURCE_PAGED) {
         const int lane = threadIdx.x & 63;
@@ -171,15 +279,13 @@ template <int DT, int D, int NW, int SRC>
 __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, int64_t tiles)
 {
     constexpr int ROWS = NW * 32, SHIFT = NW == 8 ? 8 : 7, DT_TILES = D / 32;
-    __shared__ __align__(16) TileBuffers<D, SRC> lds;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    int64_t id = xcd_order(blockIdx.x, gridDim.x);
-    const int64_t place = id % tiles;
-    id /= tiles;
+    __shared__ __align__(16) TileBuffers<D, NW, SRC> lds;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
+    const WorkPlace w = work_place(a, tiles);
     KeyRange kr;
-    kr.head = (int)(id % a.kv_heads);
-    const int split = (int)(id / a.kv_heads);
-    const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, place);
+    kr.head = w.head;
+    const int split = w.split;
+    const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place);
     if (tp.r < 0) return;
     kr.r = tp.r;
 
@@ -192,17 +298,17 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     int limit, reach;
     if constexpr (SRC == PLAID_SOURCE_PAGED) {
         const int64_t held = (int64_t)a.max_blocks << a.block_shift;
-        const int64_t all = a.lengths[tp.r];
+        const int64_t all = uniform_load(a.lengths + tp.r);
         kr.base = 0;
-        kr.len = (int)clamp64(all, 0, held);
+        kr.len = a.num_blocks > 0 ? (int)clamp64(all, 0, held) : 0;
         const int last = tp.tile * ROWS + ROWS - 1;
         const int last_token = row_token(a, last < rows ? last : rows - 1);
         limit = a.causal && there ? (int)clamp64(all - tokens + token + 1, 0, kr.len) : kr.len;
         reach = a.causal ? (int)clamp64(all - tokens + last_token + 1, 0, kr.len) : kr.len;
         kr.len = reach;
     } else {
-        kr.base = clamp64(a.k_offsets[tp.r], 0, a.num_keys);
-        kr.len = (int)(clamp64(a.k_offsets[tp.r + 1], kr.base, a.num_keys) - kr.base);
+        kr.base = clamp64(uniform_load(a.k_offsets + tp.r), 0, a.num_keys);
+        kr.len = (int)(clamp64(uniform_load(a.k_offsets + tp.r + 1), kr.base, a.num_keys) - kr.base);
         limit = reach = kr.len;
     }
     int least = limit;  // over the wave's rows
@@ -225,6 +331,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             for (int e = 0; e < 4; ++e) q[s][e] ^= (int)a.negate_q;
         }
     }
+    // with values that are not finite in q even the zeros that stand for masked keys give scores that are not numbers
+    bool odd = false;
+    if constexpr (SRC == PLAID_SOURCE_BIAS) {
+        constexpr int INF = DT == PLAID_BF16 ? 0x7f80 : 0x7c00;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd = odd || (q[s][e] & INF) == INF || ((q[s][e] >> 16) & INF) == INF;
+        odd = __any(odd);
+    }
     f32x16 o[DT_TILES];
 #pragma unroll
     for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = zero16();
@@ -232,36 +348,62 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     const float cs = SRC == PLAID_SOURCE_BIAS ? LOG2E : a.scale * LOG2E;
     float m = -INFINITY, l = 0.0f;
 
+    // Two groups of waves, one of each on every SIMD, half a step apart: while one multiplies, the other forms exponentials.
+    // A step of a group is a phase of products (o += v^T p^T of the former tile, s of this one) and one of everything else, with
+    // barriers between them.
+    using A = Ahead<NW, SRC>;
+    const int late = A::GROUPS == 2 ? uniform((int)(threadIdx.x >> 8)) : 0;
     Stage<DT, D, NW, SRC> stage;
+    auto phase_end = [&](bool second) {
+        __builtin_amdgcn_sched_barrier(0);
+        stage.arrive(second, late);
+        lds_barrier();
+    };
     if (begin < end) {
-        stage.start(a, kr, begin);
-        stage.load(a, kr, begin);
-        stage.store(lds, 0);
+        stage.start(a, kr, begin, end, lds);
+        if (late) lds_barrier();
     }
-    __syncthreads();
-    for (int step = begin; step < end; ++step) {
-        const int buf = (step - begin) & 1;
-        if (step + 1 < end) stage.load(a, kr, step + 1);
-
-        f32x16 s[2];
+    f32x16 s[2];
+    i32x4 p[4];
+    auto scores = [&](int step) {
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
             s[mt] = zero16();
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) s[mt] = mfma32<DT>(lds_rows<D>(lds.k[buf], 32 * mt, d), q[d], s[mt]);
+            for (int d = 0; d < D / 16; ++d) s[mt] = mfma32<DT>(lds_rows<D>(lds.k[step % A::TILES], 32 * mt, d), q[d], s[mt]);
         }
+    };
+    auto add_values = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = mfma32<DT>(value_operand<D, NW, SRC>(lds, step % A::TILES, 16 * i, dt), p[i], o[dt]);
+    };
+    auto weights = [&](int step) {
+        float top;
         if constexpr (SRC == PLAID_SOURCE_BIAS) {
+            if (odd) {
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (lds.bias[wave][step & 1][32 * mt + 8 * (i >> 2) + 4 * h + (i & 3)] == -INFINITY) s[mt][i] = 0.0f;
+            }
+            top = -INFINITY;
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const f32x4 b = *(const f32x4 *)&lds.bias[buf][32 * mt + 8 * i + 4 * h];
+                    const f32x4 b = *(const f32x4 *)&lds.bias[wave][step & 1][32 * mt + 8 * i + 4 * h];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[mt][4 * i + e] = b[e] == -INFINITY ? -INFINITY : fmaf(s[mt][4 * i + e], a.scale, b[e]);
+                    for (int e = 0; e < 4; ++e) {
+                        s[mt][4 * i + e] = fmaf(s[mt][4 * i + e], a.scale, b[e]);
+                        top = fmaxf(top, s[mt][4 * i + e]);
+                    }
                 }
         } else {
             bool whole = (step + 1) * MANY_KEYS <= least;
-            if constexpr (SRC == PLAID_SOURCE_PAGED) whole = whole && (lds.cell[buf][0] & lds.cell[buf][1] & lds.cell[buf][2] & lds.cell[buf][3]);
+            if constexpr (SRC == PLAID_SOURCE_PAGED) whole = whole && (lds.cell[step & 3][0] & lds.cell[step & 3][1] & lds.cell[step & 3][2] & lds.cell[step & 3][3]);
             if (!whole) {
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
@@ -269,14 +411,14 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
                     for (int i = 0; i < 16; ++i) {
                         const int key = 32 * mt + 8 * (i >> 2) + 4 * h + (i & 3);
                         bool seen = step * MANY_KEYS + key < limit;
-                        if constexpr (SRC == PLAID_SOURCE_PAGED) seen = seen && lds.cell[buf][2 * mt + (i >> 3)];
+                        if constexpr (SRC == PLAID_SOURCE_PAGED) seen = seen && lds.cell[step & 3][2 * mt + (i >> 3)];
                         s[mt][i] = seen ? s[mt][i] : -INFINITY;
                     }
             }
-        }
-        float top = larger(s[0][0], s[1][0]);
+            top = larger(s[0][0], s[1][0]);
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = larger(larger(top, s[0][i]), s[1][i]);
+            for (int i = 1; i < 16; ++i) top = larger(larger(top, s[0][i]), s[1][i]);
+        }
         top = max_halves(top);
         if (__any((top - m) * cs > 8.0f)) {
             const float next = fmaxf(m, top);
@@ -288,27 +430,53 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
         }
-        const float ref = m == -INFINITY ? 0.0f : m, ref_cs = ref * cs;
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float ref_cs = ref * cs;
+        if constexpr (SRC == PLAID_SOURCE_BIAS) {
+            // a bias may be the type's lowest value: the difference is taken before it is scaled
+            if (__any(ref < -1e38f)) {
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[mt][i] -= ref;
+                ref_cs = 0.0f;
+            }
+        }
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                // a bias may be the type's lowest value: the difference is taken before it is scaled
-                const float e = SRC == PLAID_SOURCE_BIAS ? (s[mt][i] - ref) * cs : fmaf(s[mt][i], cs, -ref_cs);
-                const float p = __builtin_amdgcn_exp2f(e);
-                s[mt][i] = p;
-                l += p;
+                s[mt][i] = __builtin_amdgcn_exp2f(fmaf(s[mt][i], cs, -ref_cs));
+                l += s[mt][i];
             }
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        for (int i = 0; i < 4; ++i) p[i] = round8<DT>(s[i >> 1], i & 1);
+        stage.bring(a, kr, step, end, late, lds);
+    };
+    if (begin < end) {
+        scores(begin);
+        phase_end(false);
+        for (int step = begin; step + 1 < end; ++step) {
+            weights(step);
+            phase_end(true);
+            add_values(step);
+            scores(step + 1);
+            // the order of the phase: operands are asked for twelve reads ahead of the products that take them
+            constexpr int READS = D / 32 * 4 * 2 + D / 16 * 2, PRODUCTS = D / 32 * 4 + D / 16 * 2;  // 3 reads to 2 products
+            __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const i32x4 p = round8<DT>(s[mt], i);
-#pragma unroll
-                for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = mfma32<DT>(value_operand<D, SRC>(lds, buf, 32 * mt + 16 * i, dt), p, o[dt]);
+            for (int i = 0; i < (READS - 12) / 3; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
             }
-        if (step + 1 < end) stage.store(lds, buf ^ 1);
-        __syncthreads();
+            __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - 12) / 3 * 2, 0);
+            phase_end(false);
+        }
+        weights(end - 1);
+        phase_end(true);
+        add_values(end - 1);
+        if (A::GROUPS == 2 && !late) lds_barrier();
+        wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
 
     l = sum_halves(l);

@@ -226,60 +226,98 @@ __device__ __forceinline__ TilePlace find_tile(const int64_t *off, int n, int64_
         const int k = votes ? 64 - __clzll((long long)votes) : 0;  // the highest lane that said yes, plus one
         const int64_t nlo = lo + step * k;
         const int64_t nhi = nlo + step - 1;
-        lo = (int)nlo;
-        hi = (int)(nhi < hi ? nhi : hi);
+        lo = uniform((int)nlo);
+        hi = uniform((int)(nhi < hi ? nhi : hi));
     }
     TilePlace t;
-    t.begin = clamp64(off[lo], 0, rows);
-    t.end = clamp64(off[lo + 1], t.begin, rows);
+    t.begin = clamp64(uniform_load(off + lo), 0, rows);
+    t.end = clamp64(uniform_load(off + lo + 1), t.begin, rows);
     const int64_t first = ((t.begin * per_token) >> tile_shift) + lo;
     t.tile = (int)(p - first);
     t.r = p >= first && ((int64_t)t.tile << tile_shift) < (t.end - t.begin) * per_token ? lo : -1;
     return t;
 }
 
-// Linear workgroup id, re-ordered so that neighbours in the result run on one XCD (workgroups go to the eight in turn).
-__device__ __forceinline__ int64_t xcd_order(int64_t id, int64_t total)
+// What a workgroup of a grid of tiles x key heads x splits does.  Workgroups go to the eight XCDs in turn.  With an even number of
+// key heads the heads come first: the tiles of one head, which share what they read, then meet on as many XCDs as eight has more
+// factors of two than the number of heads, and every XCD gets the same mixture of long and short requests.  With an odd number
+// the tiles come first, in stretches of four that go round the XCDs.
+struct WorkPlace {
+    int64_t place;
+    int head, split;
+};
+__device__ __forceinline__ WorkPlace work_place(const AttendArgs &a, int64_t tiles)
 {
-    const int64_t even = total >> 3, rest = total & 7;
-    const int64_t xcd = id & 7, at = id >> 3;
-    return xcd * even + (xcd < rest ? xcd : rest) + at;
+    int64_t id = blockIdx.x;
+    WorkPlace w;
+    if (a.kv_heads & 1) {
+        if (id < (int64_t)gridDim.x / 32 * 32) id = ((id >> 5) * 8 + (id & 7)) * 4 + ((id >> 3) & 3);
+        w.place = id % tiles;
+        id /= tiles;
+        w.head = (int)(id % a.kv_heads), w.split = (int)(id / a.kv_heads);
+    } else {
+        w.head = (int)(id % a.kv_heads);
+        id /= a.kv_heads;
+        w.place = id % tiles, w.split = (int)(id / tiles);
+    }
+    return w;
 }
 
 // ---------------------------------------------------------------------------------------------
 // Tiles of 16-bit values in LDS: rows of D values, their 16-byte chunks exchanged by an exclusive-or with a number of the
-// row.  Its three bits are (row % 4) * 2 + row / 4 % 2: eight rows' chunks of one column lie in different banks (the reads
-// along a row) and so do the 32-byte pieces of four rows (the transposing reads).
+// row.  At D = 128 a row is as long as the 64 banks: the number's upper bits are row % 4, so that the 64-byte pieces of four
+// rows that half a wave's transposing read takes lie in different banks, the lower ones are row / 4 % 4, so that sixteen rows'
+// chunks of one column (a read along the rows) do too.  At D = 64 two rows share the banks and row / 2 % 2 does for row % 4.
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ int swizzle(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+template <int D>
+__device__ __forceinline__ int swizzle(int row)
+{
+    return D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
 
 template <int D>
 __device__ __forceinline__ int lds_chunk(int row, int chunk)
 {
-    return row * (D * 2) + ((chunk ^ swizzle(row)) << 4);
+    return row * (D * 2) + ((chunk ^ swizzle<D>(row)) << 4);
 }
 // Operand along the row: rows base + l % 32, values 16 s + 8 (l / 32) .. + 7.  base is a multiple of 32.
 template <int D>
 __device__ __forceinline__ i32x4 lds_rows(const char *tile, int base, int s)
 {
-    const int lane = threadIdx.x & 63;
-    return *(const i32x4 *)(tile + (base + (lane & 31)) * (D * 2) + (((2 * s + (lane >> 5)) ^ swizzle(lane & 31)) << 4));
+    const int lane = threadIdx.x & 63, f = swizzle<D>(lane & 31);
+    return *(const i32x4 *)(tile + base * (D * 2) + (lane & 31) * (D * 2) + (((2 * s + (lane >> 5)) ^ f) << 4));
 }
 // Transposed operand: columns 32 dt + l % 32, rows base + 4 (l / 32) .. + 3 and base + 8 + 4 (l / 32) .. + 3 (base a multiple
 // of 16): the order in which mfma32's result leaves its rows in a lane's registers 8 i .. 8 i + 7.
 template <int D>
 __device__ __forceinline__ i32x4 lds_columns(const char *tile, int base, int dt)
 {
-    const int lane = threadIdx.x & 63;
-    const int h = lane >> 5, r = (lane >> 2) & 3, c = (lane & 3) >> 1;
-    const int row = base + 4 * h + r;
-    const int chunk = (4 * dt + ((lane >> 4) & 1) * 2 + c) ^ ((r << 1) | h);
-    const char *p = tile + row * (D * 2) + (chunk << 4) + (lane & 1) * 8;
+    const int lane = threadIdx.x & 63, row = 4 * (lane >> 5) + ((lane >> 2) & 3), x = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    const char *p = tile + base * (D * 2) + row * (D * 2) + (((4 * dt + x) ^ swizzle<D>(row)) << 4) + (lane & 1) * 8;
+    const char *r = tile + base * (D * 2) + (row + 8) * (D * 2) + (((4 * dt + x) ^ swizzle<D>(row + 8)) << 4) + (lane & 1) * 8;
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
-    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * (D * 2)));
-    const i32x2 u = __builtin_bit_cast(i32x2, x), w = __builtin_bit_cast(i32x2, y);
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+    const s16x4 z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)r);
+    const i32x2 u = __builtin_bit_cast(i32x2, y), w = __builtin_bit_cast(i32x2, z);
     return i32x4{u[0], u[1], w[0], w[1]};
+}
+// Barrier of the workgroup for what its waves read and write in LDS themselves; loads from memory stay under way.
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// Waits until at most N of the wave's loads are under way: loads straight into LDS are not waited for otherwise.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// 16 bytes of every lane, one after the other, into the 1024 bytes of LDS at `to` (the same for all lanes), from base + off.
+__device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, char *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off), (__attribute__((address_space(3))) void *)to, 16, 0, 0);
 }
 // Rows 8 i .. of a result's registers as an operand: registers 8 i .. 8 i + 7 rounded to the type.
 template <int DT>
