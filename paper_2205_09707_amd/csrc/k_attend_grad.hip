@@ -1,14 +1,16 @@
 // Gradients of attention to states of another length.
+#include <stddef.h>
+
 #include "reader.h"
 
 // With P = exp(s - lse), dP = dO v^T and dS = P (dP - delta), delta_i = dO_i . out_i:
 //   dv = P^T dO,   dk = scale dS^T q,   dq = scale dS k,   dbias_j = sum_i dS_ij.
 // P is formed again from the statistics of the forward pass.  Two kernels, each with its own sums in registers and nothing
-// added up in memory, so that every sum has one order: grad_k_kernel owns keys (a wave 32 of them, the keys and values in
-// registers) and passes over the rows of all heads that share them; grad_q_kernel owns rows and passes over the keys.  Forming
-// s and dP twice costs 7 products in place of 5.  What the other side brings goes through LDS once and is read both along its
-// rows (for s and dP) and transposed (for the sums); the products s and dP leave their registers as the operands that the sums
-// need, as in the forward kernel.
+// added up in memory, so that every sum has one order: grad_k_kernel owns keys and passes over the rows of all heads that share
+// them; grad_q_kernel owns rows and passes over the keys.  Forming s and dP twice costs 7 products in place of 5; sums of dq in
+// memory, one for each tile of keys, would cost more: at 6250 keys 49 times dq in 32 bits, written and read.  What the other side
+// brings goes into LDS once and is read both along its rows (for s and dP) and transposed (for the sums); the results leave their
+// registers as the operands that the sums need, as in the forward kernel.
 
 template <int DT, int D>
 __global__ __launch_bounds__(256) void delta_kernel(GradArgs g)
@@ -23,123 +25,224 @@ __global__ __launch_bounds__(256) void delta_kernel(GradArgs g)
         for (int e = 0; e < 4; ++e) sum += unpack<DT>(x[e], 0) * unpack<DT>(y[e], 0) + unpack<DT>(x[e], 1) * unpack<DT>(y[e], 1);
 #pragma unroll
         for (int o = LANES / 2; o; o >>= 1) sum += __shfl_xor(sum, o);
-        if (c == 0) g.delta[at] = sum;
+        if (c == 0) {
+            const float2 lse = *(const float2 *)(g.a.lse + 2 * at);
+            g.delta[at] = lse.x != -INFINITY ? sum : 0.0f;
+            g.exponent[at] = lse.x != -INFINITY ? fmaf(lse.x, LOG2E, lse.y * LOG2E) : INFINITY;
+        }
     }
 }
 
-#define GRAD_ROWS 32  // rows of a step of grad_k_kernel
-#define GRAD_KEYS 64  // keys of a step of grad_q_kernel
+// Both kernels run in phases like the forward one (k_attend_many.hip): products on one side, exponentials on the other, two groups
+// of waves a phase apart, what they read on its way into LDS steps before (the first group asks for it).
+
+// --- gradients of keys and values ---------------------------------------------------------------------------------------------
+// A wave of 32 keys would hold their keys, values and both sums, 192 registers, before it multiplies anything.  So two waves of
+// one SIMD share 32 keys: the first forms P (keys and the sum dv in registers), the second, a phase behind, takes P from LDS and
+// forms dS (values and the sum dk in registers).  Each does half of the products; P, in 32 bits, costs a fifth of the traffic in LDS.
+template <int NW>
+struct GradK {
+    static constexpr int PAIRS = NW / 2, KEYS = PAIRS * 32, SHIFT = NW == 8 ? 7 : 6, ROWS = NW == 8 ? 64 : 32;  // rows of a step
+    static constexpr int AHEAD = 2, Q_TILES = AHEAD + 2, O_TILES = AHEAD + 1;  // q is read in four phases, dO in two
+};
+
+template <int D, int NW>
+struct GradKLds {
+    using K = GradK<NW>;
+    char q[K::Q_TILES][K::ROWS * D * 2], o[K::O_TILES][K::ROWS * D * 2];
+    float p[K::PAIRS][K::ROWS / 32][4][64][4];   // as the first wave's registers hold it
+    float row[NW][4][64];                        // each wave's own: the rows' exponents, or their deltas
+};
 
 template <int DT, int D, int NW, bool BIAS>
 __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t tiles, int splits)
 {
-    constexpr int THREADS = NW * 64, KEYS = NW * 32, SHIFT = NW == 8 ? 8 : 7, CHUNKS = D / 8;
-    constexpr int N = GRAD_ROWS * CHUNKS / THREADS > 0 ? GRAD_ROWS * CHUNKS / THREADS : 1;
+    using K = GradK<NW>;
+    constexpr int ROWS = K::ROWS, BLOCKS = ROWS / 32, CHUNKS = D / 8, AT_ONCE = 512 / D, N = ROWS / AT_ONCE / K::PAIRS;
     const AttendArgs &a = g.a;
-    __shared__ __align__(16) char s_q[2][GRAD_ROWS * D * 2], s_o[2][GRAD_ROWS * D * 2];
-    __shared__ __align__(16) float s_m[2][GRAD_ROWS], s_l[2][GRAD_ROWS], s_delta[2][GRAD_ROWS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    __shared__ __align__(16) GradKLds<D, NW> lds;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
+    const int second = wave >= K::PAIRS, pair = second ? wave - K::PAIRS : wave;
     const WorkPlace w = work_place(a, tiles);
     const int head = w.head, split = w.split;
-    const TilePlace tp = find_tile(a.k_offsets, a.n, a.num_keys, 1, SHIFT, w.place);
+    const TilePlace tp = find_tile(a.k_offsets, a.n, a.num_keys, 1, K::SHIFT, w.place);
     if (tp.r < 0) return;
     const int len = (int)(tp.end - tp.begin);
-    const int64_t row0 = clamp64(a.q_offsets[tp.r], 0, a.num_queries);
-    const int tokens = (int)(clamp64(a.q_offsets[tp.r + 1], row0, a.num_queries) - row0), rows = tokens * a.group;
-    const int steps = (rows + GRAD_ROWS - 1) / GRAD_ROWS, share = (steps + splits - 1) / splits;
+    const int64_t row0 = clamp64(uniform_load(a.q_offsets + tp.r), 0, a.num_queries);
+    const int tokens = (int)(clamp64(uniform_load(a.q_offsets + tp.r + 1), row0, a.num_queries) - row0), rows = tokens * a.group;
+    const int steps = (rows + ROWS - 1) / ROWS, share = (steps + splits - 1) / splits;
     const int begin = split * share, end = min(steps, begin + share);
 
-    const int key = tp.tile * KEYS + wave * 32 + (lane & 31);
+    const int key = tp.tile * K::KEYS + pair * 32 + (lane & 31);
     const bool there = key < len;
-    i32x4 k[D / 16], v[D / 16];
+    i32x4 kv[D / 16];  // the first wave's keys, the second one's values
     {
-        const char *pk = a.k + (tp.begin + key) * a.k_token + head * a.k_head + h * 16;
-        const char *pv = a.v + (tp.begin + key) * a.v_token + head * a.v_head + h * 16;
+        const char *x = second ? a.v : a.k;
+        const int64_t token = second ? a.v_token : a.k_token, hd = second ? a.v_head : a.k_head;
+        const char *at = x + (tp.begin + (there ? key : len - 1)) * token + head * hd + h * 16;
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            k[s] = v[s] = i32x4{0, 0, 0, 0};
-            if (there) k[s] = *(const i32x4 *)(pk + s * 32), v[s] = *(const i32x4 *)(pv + s * 32);
-        }
+        for (int s = 0; s < D / 16; ++s) kv[s] = *(const i32x4 *)(at + s * 32);
     }
     float bias = 0.0f;
-    if (BIAS && there) bias = load16<DT>(a.bias + 2 * (tp.begin + key));
-    f32x16 dk[D / 32], dv[D / 32];
+    if (BIAS) bias = there ? load16<DT>(a.bias + 2 * (tp.begin + key)) : 0.0f;
+    const bool is_low = BIAS && bias < -1e38f && bias != -INFINITY, low = __any(is_low);
+    const float cs = a.scale * LOG2E, bias_e = bias * LOG2E;
+    f32x16 sum[D / 32];  // the first wave's dv, the second one's dk
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) dk[t] = zero16(), dv[t] = zero16();
+    for (int t = 0; t < D / 32; ++t) sum[t] = zero16();
     float dbias = 0.0f;
 
-    i32x4 xq[N], xo[N];
-    float xm = 0.0f, xl = INFINITY, xd = 0.0f;
-    auto load = [&](int step) {
+    // Rows past the end repeat the last one; tiles past the last repeat that.  Where a step is a whole number of tokens a lane's rows
+    // lie at the same distances from the step's first token in every step.
+    const bool aligned = ROWS % a.group == 0;
+    uint32_t q_off[N], o_off[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int u = threadIdx.x + i * THREADS, row = step * GRAD_ROWS + u / CHUNKS;
-            xq[i] = xo[i] = i32x4{0, 0, 0, 0};
-            if (u < GRAD_ROWS * CHUNKS && row < rows) {
-                const int token = row_token(a, row), hd = head * a.group + row - token * a.group;
-                xq[i] = *(const i32x4 *)(a.q + (row0 + token) * a.q_token + hd * a.q_head + u % CHUNKS * 16);
-                xo[i] = *(const i32x4 *)(g.d_out + (((row0 + token) * a.heads + hd) * D + u % CHUNKS * 8) * 2);
-            }
-        }
-        if (threadIdx.x < GRAD_ROWS) {
-            const int row = step * GRAD_ROWS + threadIdx.x;
-            xm = 0.0f, xl = INFINITY, xd = 0.0f;  // no row, or one that no key was left for: its weights are 0
-            if (row < rows) {
-                const int token = row_token(a, row), hd = head * a.group + row - token * a.group;
-                const int64_t at = (row0 + token) * a.heads + hd;
-                const float m = a.lse[2 * at], l = a.lse[2 * at + 1];
-                if (m != -INFINITY) xm = m, xl = l * LOG2E, xd = g.delta[at];
-            }
-        }
-    };
-    auto store = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int u = threadIdx.x + i * THREADS;
-            if (u < GRAD_ROWS * CHUNKS) {
-                *(i32x4 *)(s_q[buf] + lds_chunk<D>(u / CHUNKS, u % CHUNKS)) = xq[i];
-                *(i32x4 *)(s_o[buf] + lds_chunk<D>(u / CHUNKS, u % CHUNKS)) = xo[i];
-            }
-        }
-        if (threadIdx.x < GRAD_ROWS) s_m[buf][threadIdx.x] = xm, s_l[buf][threadIdx.x] = xl, s_delta[buf][threadIdx.x] = xd;
-    };
-    if (begin < end) {
-        load(begin);
-        store(0);
+    for (int i = 0; i < N; ++i) {
+        const int in = (pair * N + i) * AT_ONCE + lane / CHUNKS, chunk = (lane % CHUNKS) ^ swizzle<D>(in), token = row_token(a, in), hd = in - token * a.group;
+        q_off[i] = (uint32_t)token * (uint32_t)a.q_token + (uint32_t)hd * (uint32_t)a.q_head + chunk * 16;
+        o_off[i] = ((uint32_t)token * (uint32_t)a.heads + (uint32_t)hd) * (D * 2) + chunk * 16;
     }
-    __syncthreads();
-    for (int step = begin; step < end; ++step) {
-        const int buf = (step - begin) & 1;
-        if (step + 1 < end) load(step + 1);
-        f32x16 p = zero16(), ds = zero16();
+    // the tiles' places in the rings; nothing below branches on the kind of wave but the weights
+    auto q_tile = [&](int step) { return (uint32_t)step % K::Q_TILES * (uint32_t)sizeof(lds.q[0]); };
+    auto o_tile = [&](int step) { return (uint32_t)step % K::O_TILES * (uint32_t)sizeof(lds.o[0]); };
+    constexpr uint32_t O_AT = K::Q_TILES * sizeof(lds.q[0]);
+    using Lds = GradKLds<D, NW>;
+    static_assert(offsetof(Lds, o) == O_AT, "dO's ring lies behind q's");
+    const char *ring = lds.q[0];
+    auto load = [&](int step) {
+        const int t = min(step, end - 1);
+        char *to_q = lds.q[0] + q_tile(step) + pair * N * 1024, *to_o = lds.o[0] + o_tile(step) + pair * N * 1024;
+        if (aligned && (t + 1) * ROWS <= rows) {
+            const int64_t first = row0 + row_token(a, t * ROWS);
+            const char *q = a.q + first * a.q_token + (int64_t)head * a.group * a.q_head, *o = g.d_out + (first * a.heads + head * a.group) * (D * 2);
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) p = mfma32<DT>(lds_rows<D>(s_q[buf], 0, s), k[s], p);
+            for (int i = 0; i < N; ++i) {
+                load_to_lds(q, q_off[i], to_q + i * 1024);
+                load_to_lds(o, o_off[i], to_o + i * 1024);
+            }
+        } else {
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) ds = mfma32<DT>(lds_rows<D>(s_o[buf], 0, s), v[s], ds);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 m = *(const f32x4 *)&s_m[buf][8 * i + 4 * h], l = *(const f32x4 *)&s_l[buf][8 * i + 4 * h],
-                        delta = *(const f32x4 *)&s_delta[buf][8 * i + 4 * h];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                // the difference to the maximum first: a bias may be the type's lowest value
-                const float x = (fmaf(p[4 * i + e], a.scale, bias) - m[e]) * LOG2E - l[e];
-                p[4 * i + e] = __builtin_amdgcn_exp2f(x);
-                ds[4 * i + e] = p[4 * i + e] * (ds[4 * i + e] - delta[e]);
-                dbias += ds[4 * i + e];
+            for (int i = 0; i < N; ++i) {
+                const int in = (pair * N + i) * AT_ONCE + lane / CHUNKS, row = min(t * ROWS + in, rows - 1), chunk = (lane % CHUNKS) ^ swizzle<D>(in);
+                const int token = row_token(a, row), hd = head * a.group + row - token * a.group;
+                load_to_lds(a.q + (row0 + token) * a.q_token + hd * a.q_head + chunk * 16, to_q + i * 1024);
+                load_to_lds(g.d_out + ((row0 + token) * a.heads + hd) * (D * 2) + chunk * 16, to_o + i * 1024);
             }
         }
+    };
+    auto load_row = [&](int step) {
+        const int row = min(min(step, end - 1) * ROWS + lane % ROWS, rows - 1), token = row_token(a, row);
+        load4_to_lds((second ? g.delta : g.exponent) + (row0 + token) * a.heads + head * a.group + row - token * a.group, lds.row[wave][step & 3]);
+    };
+    f32x16 s[BLOCKS];
+    i32x4 p[2 * BLOCKS];
+    auto form = [&](int step) {  // s = q k^T, or dP = dO v^T
+        const uint32_t at_q = q_tile(step), at_o = O_AT + o_tile(step);
+        const char *x = ring + (second ? at_o : at_q);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const i32x4 pr = round8<DT>(p, i), dr = round8<DT>(ds, i);
+        for (int b = 0; b < BLOCKS; ++b) {
+            s[b] = zero16();
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t) {
-                dv[t] = mfma32<DT>(lds_columns<D>(s_o[buf], 16 * i, t), pr, dv[t]);
-                dk[t] = mfma32<DT>(lds_columns<D>(s_q[buf], 16 * i, t), dr, dk[t]);
-            }
+            for (int d = 0; d < D / 16; ++d) s[b] = mfma32<DT>(lds_rows<D>(x, 32 * b, d), kv[d], s[b]);
         }
-        if (step + 1 < end) store(buf ^ 1);
-        __syncthreads();
+    };
+    auto add = [&](int step) {  // dv += dO^T P, or dk += q^T dS
+        const uint32_t at_q = q_tile(step), at_o = O_AT + o_tile(step);
+        const char *x = ring + (second ? at_q : at_o);
+#pragma unroll
+        for (int i = 0; i < 2 * BLOCKS; ++i)
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) sum[t] = mfma32<DT>(lds_columns<D>(x, 16 * i, t), p[i], sum[t]);
+    };
+    auto weights = [&](int step) {
+        load_row(step + 2);
+        if (!second) load(step + K::AHEAD);
+        else wait_loads<2>();  // this step's deltas
+        const float *of_row = lds.row[wave][step & 3];
+        if (!second) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 ex = *(const f32x4 *)(of_row + 32 * b + 8 * i + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][4 * i + e] = BIAS ? fmaf(s[b][4 * i + e], cs, bias_e) - ex[e] : fmaf(s[b][4 * i + e], cs, -ex[e]);
+                }
+            if (low || (step + 1) * ROWS > rows) {
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int row = step * ROWS + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3);
+                        if (row >= rows) {
+                            s[b][i] = -INFINITY;  // no row: its weights are 0
+                        } else if (is_low) {
+                            // a bias near the type's lowest value: a score is nothing beside it, and only where all of a row's are as low
+                            // is there a weight; the difference to the row's maximum comes before it is scaled
+                            const int token = row_token(a, row);
+                            const float2 lse = *(const float2 *)(a.lse + 2 * ((row0 + token) * a.heads + head * a.group + row - token * a.group));
+                            s[b][i] = lse.x < -1e38f ? (bias - lse.x) * LOG2E - lse.y * LOG2E : -INFINITY;
+                        }
+                    }
+            }
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x4 x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = s[b][4 * i + e] = __builtin_amdgcn_exp2f(s[b][4 * i + e]);
+                    *(f32x4 *)lds.p[pair][b][i][lane] = x;
+                }
+        } else {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 x = *(const f32x4 *)lds.p[pair][b][i][lane], dl = *(const f32x4 *)(of_row + 32 * b + 8 * i + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[b][4 * i + e] = x[e] * (s[b][4 * i + e] - dl[e]);
+                        if (BIAS) dbias += s[b][4 * i + e];
+                    }
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * BLOCKS; ++i) p[i] = round8<DT>(s[i >> 1], i & 1);
+    };
+    constexpr int STEP = 2 * N + 1;  // loads of a step: q, dO and the rows' numbers
+    if (begin < end) {
+        load_row(begin);
+        if (!second) load(begin);
+        load_row(begin + 1);
+        if (!second) load(begin + 1);
+        if (second) wait_loads<1>();
+        else wait_loads<STEP>();
+        lds_barrier();
+        if (second) lds_barrier();
+        form(begin);
+        lds_barrier();
+        for (int step = begin; step + 1 < end; ++step) {
+            weights(step);
+            if (!second) wait_loads<STEP *(K::AHEAD - 1)>();
+            lds_barrier();
+            add(step);
+            form(step + 1);
+            constexpr int READS = 2 * BLOCKS * (D / 32) * 2 + BLOCKS * (D / 16), PRODUCTS = 2 * BLOCKS * (D / 32) + BLOCKS * (D / 16);
+            __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
+#pragma unroll
+            for (int i = 0; i < (READS - 12) / 3; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - 12) / 3 * 2, 0);
+            lds_barrier();
+        }
+        weights(end - 1);
+        lds_barrier();
+        add(end - 1);
+        if (!second) lds_barrier();
+        wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
 
     dbias = sum_halves(dbias);
@@ -147,42 +250,52 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     // a masked key's column may hold anything and is zero
     const bool masked = BIAS && bias == -INFINITY;
     const int64_t at = (tp.begin + key) * a.kv_heads + head;
-    if (BIAS && h == 0 && g.dbias_part) g.dbias_part[((int64_t)split * a.kv_heads + head) * a.num_keys + tp.begin + key] = masked ? 0.0f : dbias;
+    if (BIAS && second && h == 0 && g.dbias_part) g.dbias_part[((int64_t)split * a.kv_heads + head) * a.num_keys + tp.begin + key] = masked ? 0.0f : dbias;
+    const float factor = second ? a.scale : 1.0f;
+    char *out = second ? g.dk : g.dv;
+    float *part = second ? g.dk_part : g.dv_part;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            f32x4 x, y;
+            f32x4 x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = masked ? 0.0f : dk[t][4 * i + e] * a.scale, y[e] = masked ? 0.0f : dv[t][4 * i + e];
+            for (int e = 0; e < 4; ++e) x[e] = masked ? 0.0f : sum[t][4 * i + e] * factor;
             const int d = 32 * t + 8 * i + 4 * h;
-            if (splits > 1) {
-                const int64_t to = ((int64_t)split * a.num_keys * a.kv_heads + at) * D + d;
-                *(f32x4 *)(g.dk_part + to) = x;
-                *(f32x4 *)(g.dv_part + to) = y;
-            } else {
-                if (g.dk) *(i32x2 *)(g.dk + (at * D + d) * 2) = i32x2{pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])};
-                if (g.dv) *(i32x2 *)(g.dv + (at * D + d) * 2) = i32x2{pack2<DT>(y[0], y[1]), pack2<DT>(y[2], y[3])};
-            }
+            if (splits > 1) *(f32x4 *)(part + ((int64_t)split * a.num_keys * a.kv_heads + at) * D + d) = x;
+            else if (out) *(i32x2 *)(out + (at * D + d) * 2) = i32x2{pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])};
         }
 }
+
+// --- gradients of queries -----------------------------------------------------------------------------------------------------
+// A wave owns 32 rows: q, dO and the sum dq in registers, 32 keys a step.  For a request of at most 32 keys one step sees all of a
+// row, and delta is taken as the sum of P dP: out, rounded to the type, would give it too coarsely where few keys are averaged
+// (two keys in bf16: 4 of 1000 off in dq and dk, so 2.5).
+#define GRAD_KEYS 32
+template <int D, int NW, bool BIAS>
+struct GradQLds {
+    static constexpr int AHEAD = 3, K_TILES = AHEAD + 2, V_TILES = AHEAD + 1;  // keys are read in four phases, values in two
+    char k[K_TILES][GRAD_KEYS * D * 2], v[V_TILES][GRAD_KEYS * D * 2];
+    float bias[BIAS ? NW : 1][4][BIAS ? GRAD_KEYS : 4];  // each wave's own
+    uint32_t raw[BIAS ? NW : 1][4][64];                   // as they are loaded
+};
 
 template <int DT, int D, int NW, bool BIAS>
 __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t tiles, int splits)
 {
-    constexpr int THREADS = NW * 64, ROWS = NW * 32, SHIFT = NW == 8 ? 8 : 7, CHUNKS = D / 8;
-    constexpr int N = (GRAD_KEYS * CHUNKS + THREADS - 1) / THREADS;
+    using L = GradQLds<D, NW, BIAS>;
+    constexpr int ROWS = NW * 32, SHIFT = NW == 8 ? 8 : 7, CHUNKS = D / 8, AT_ONCE = 512 / D, N = GRAD_KEYS / AT_ONCE / 4;
+    constexpr uint16_t NONE = DT == PLAID_BF16 ? 0xff80 : 0xfc00;  // -infinity
     const AttendArgs &a = g.a;
-    __shared__ __align__(16) char s_k[2][GRAD_KEYS * D * 2], s_v[2][GRAD_KEYS * D * 2];
-    __shared__ __align__(16) float s_bias[2][BIAS ? GRAD_KEYS : 4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    __shared__ __align__(16) L lds;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5, late = wave >= 4;
     const WorkPlace w = work_place(a, tiles);
     const int head_kv = w.head, split = w.split;
     const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place);
     if (tp.r < 0) return;
     const int tokens = (int)(tp.end - tp.begin), rows = tokens * a.group;
-    const int64_t key0 = clamp64(a.k_offsets[tp.r], 0, a.num_keys);
-    const int len = (int)(clamp64(a.k_offsets[tp.r + 1], key0, a.num_keys) - key0);
+    const int64_t key0 = clamp64(uniform_load(a.k_offsets + tp.r), 0, a.num_keys);
+    const int len = (int)(clamp64(uniform_load(a.k_offsets + tp.r + 1), key0, a.num_keys) - key0);
     const int steps = (len + GRAD_KEYS - 1) / GRAD_KEYS, share = (steps + splits - 1) / splits;
     const int begin = split * share, end = min(steps, begin + share);
 
@@ -194,85 +307,152 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
     {
         const char *pq = a.q + (tp.begin + token) * a.q_token + head * a.q_head + h * 16, *po = g.d_out + at * D * 2 + h * 16;
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            q[s] = d_out[s] = i32x4{0, 0, 0, 0};
-            if (there) q[s] = *(const i32x4 *)(pq + s * 32), d_out[s] = *(const i32x4 *)(po + s * 32);
-        }
+        for (int s = 0; s < D / 16; ++s) q[s] = *(const i32x4 *)(pq + s * 32), d_out[s] = *(const i32x4 *)(po + s * 32);
     }
-    float m = 0.0f, l = INFINITY, delta = 0.0f;
-    if (there && a.lse[2 * at] != -INFINITY) m = a.lse[2 * at], l = a.lse[2 * at + 1] * LOG2E, delta = g.delta[at];
+    const float2 lse = *(const float2 *)(a.lse + 2 * at);
+    const bool counts = lse.x != -INFINITY;
+    const float m = counts ? lse.x : 0.0f, l = counts ? lse.y * LOG2E : INFINITY;
+    float delta = counts ? g.delta[at] : 0.0f;
+    const float ex = fmaf(m, LOG2E, l), cs = a.scale * LOG2E;
+    const bool low = BIAS && __any(m < -1e38f);
     f32x16 dq[D / 32];
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
 
-    i32x4 xk[N], xv[N];
-    float xb = -INFINITY;
+    // keys past the end repeat the last one; tiles past the last repeat that
+    uint32_t masked = 0;  // keys of bias -infinity, and places past the end, in the tile that is asked for next
     auto load = [&](int step) {
+        const int t = min(step, end - 1), last = len - 1 - t * GRAD_KEYS;
+        const char *bk = a.k + (key0 + t * GRAD_KEYS) * a.k_token + head_kv * a.k_head, *bv = a.v + (key0 + t * GRAD_KEYS) * a.v_token + head_kv * a.v_head;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int u = threadIdx.x + i * THREADS, key = step * GRAD_KEYS + u / CHUNKS;
-            xk[i] = xv[i] = i32x4{0, 0, 0, 0};
-            bool in = u < GRAD_KEYS * CHUNKS && key < len;
-            if constexpr (BIAS) in = in && load16<DT>(a.bias + 2 * (key0 + key)) != -INFINITY;
-            if (in) {
-                xk[i] = *(const i32x4 *)(a.k + (key0 + key) * a.k_token + head_kv * a.k_head + u % CHUNKS * 16);
-                xv[i] = *(const i32x4 *)(a.v + (key0 + key) * a.v_token + head_kv * a.v_head + u % CHUNKS * 16);
+            const int in = (wave * N + i) * AT_ONCE + lane / CHUNKS, key = min(in, last), chunk = (lane % CHUNKS) ^ swizzle<D>(in);
+            const uint32_t off_k = (uint32_t)key * (uint32_t)a.k_token + chunk * 16, off_v = (uint32_t)key * (uint32_t)a.v_token + chunk * 16;
+            char *to_k = lds.k[step % L::K_TILES] + (wave * N + i) * 1024, *to_v = lds.v[step % L::V_TILES] + (wave * N + i) * 1024;
+            if constexpr (BIAS) {
+                const bool none = masked >> in & 1;
+                load_to_lds(none ? (const char *)zero_row : bk + off_k, to_k);
+                load_to_lds(none ? (const char *)zero_row : bv + off_v, to_v);
+            } else {
+                load_to_lds(bk, off_k, to_k);
+                load_to_lds(bv, off_v, to_v);
             }
+        }
+    };
+    auto load_bias = [&](int step) {
+        const int t = min(step, end - 1), last = len - 1 - t * GRAD_KEYS;
+        load2_to_lds(a.bias + 2 * (key0 + t * GRAD_KEYS), 2 * min(lane & 31, last), lds.raw[wave][step & 3]);
+    };
+    uint32_t raw = 0;  // read some time before it is used
+    auto read_bias = [&](int step) { raw = lds.raw[wave][step & 3][lane]; };
+    auto store_bias = [&](int step) {
+        const uint16_t x = min(step, end - 1) * GRAD_KEYS + (lane & 31) < len ? (uint16_t)raw : NONE;
+        lds.bias[wave][step & 3][lane & 31] = unpack<DT>(x, 0);
+        masked = (uint32_t)__ballot(x == NONE);
+    };
+    f32x16 s, ds;
+    i32x4 r[2];
+    auto form = [&](int step) {
+        s = zero16(), ds = zero16();
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) s = mfma32<DT>(lds_rows<D>(lds.k[step % L::K_TILES], 0, d), q[d], s);
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) ds = mfma32<DT>(lds_rows<D>(lds.v[step % L::V_TILES], 0, d), d_out[d], ds);
+    };
+    auto add = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) dq[t] = mfma32<DT>(lds_columns<D>(lds.k[step % L::K_TILES], 16 * i, t), r[i], dq[t]);
+    };
+    auto weights = [&](int step) {
+        if constexpr (BIAS) {
+            // the biases that the step before asked for first
+            if (late) wait_loads<0>();
+            else wait_loads<2 * N>();
+            read_bias(step + L::AHEAD);
+        } else {
+            if (!late) load(step + L::AHEAD);
         }
         if constexpr (BIAS) {
-            const int key = step * GRAD_KEYS + threadIdx.x;
-            if (threadIdx.x < GRAD_KEYS) xb = key < len ? load16<DT>(a.bias + 2 * (key0 + key)) : -INFINITY;
-        }
-    };
-    auto store = [&](int buf) {
+            f32x4 b[4];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int u = threadIdx.x + i * THREADS;
-            if (u < GRAD_KEYS * CHUNKS) {
-                *(i32x4 *)(s_k[buf] + lds_chunk<D>(u / CHUNKS, u % CHUNKS)) = xk[i];
-                *(i32x4 *)(s_v[buf] + lds_chunk<D>(u / CHUNKS, u % CHUNKS)) = xv[i];
+            for (int i = 0; i < 4; ++i) b[i] = *(const f32x4 *)&lds.bias[wave][step & 3][8 * i + 4 * h];
+            if (!low) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = fmaf(b[i >> 2][i & 3], LOG2E, fmaf(s[i], cs, -ex));
+            } else {
+                // a bias near the type's lowest value: the difference to the maximum before it is scaled
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = (fmaf(s[i], a.scale, b[i >> 2][i & 3]) - m) * LOG2E - l;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], cs, -ex);
+            if ((step + 1) * GRAD_KEYS > len) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = step * GRAD_KEYS + 8 * (i >> 2) + 4 * h + (i & 3) < len ? s[i] : -INFINITY;
             }
         }
-        if constexpr (BIAS)
-            if (threadIdx.x < GRAD_KEYS) s_bias[buf][threadIdx.x] = xb;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
+        if (steps == 1) {
+            delta = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) delta = fmaf(s[i], ds[i], delta);
+            delta = sum_halves(delta);
+            if (there && h == 0) g.delta[at] = delta;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ds[i] = s[i] * (ds[i] - delta);
+        r[0] = round8<DT>(ds, 0), r[1] = round8<DT>(ds, 1);
+        if constexpr (BIAS) {
+            store_bias(step + L::AHEAD);
+            load_bias(step + L::AHEAD + 1);
+            if (!late) load(step + L::AHEAD);
+        }
     };
+    constexpr int STEP = 2 * N + BIAS;  // loads of a step
     if (begin < end) {
-        load(begin);
-        store(0);
-    }
-    __syncthreads();
-    for (int step = begin; step < end; ++step) {
-        const int buf = (step - begin) & 1;
-        if (step + 1 < end) load(step + 1);
+        if constexpr (BIAS) {
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            f32x16 s = zero16(), ds = zero16();
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) s = mfma32<DT>(lds_rows<D>(s_k[buf], 32 * mt, d), q[d], s);
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) ds = mfma32<DT>(lds_rows<D>(s_v[buf], 32 * mt, d), d_out[d], ds);
-            const bool whole = (step + 1) * GRAD_KEYS <= len;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f32x4 b{0, 0, 0, 0};
-                if constexpr (BIAS) b = *(const f32x4 *)&s_bias[buf][32 * mt + 8 * i + 4 * h];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float p = __builtin_amdgcn_exp2f((fmaf(s[4 * i + e], a.scale, b[e]) - m) * LOG2E - l);
-                    if constexpr (BIAS) p = b[e] == -INFINITY ? 0.0f : p;
-                    else if (!whole) p = step * GRAD_KEYS + 32 * mt + 8 * i + 4 * h + e < len ? p : 0.0f;
-                    ds[4 * i + e] = p * (ds[4 * i + e] - delta);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const i32x4 dr = round8<DT>(ds, i);
-#pragma unroll
-                for (int t = 0; t < D / 32; ++t) dq[t] = mfma32<DT>(lds_columns<D>(s_k[buf], 32 * mt + 16 * i, t), dr, dq[t]);
-            }
+            for (int i = 0; i <= L::AHEAD; ++i) load_bias(begin + i);
+            wait_loads<0>();
         }
-        if (step + 1 < end) store(buf ^ 1);
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < L::AHEAD; ++i) {
+            if constexpr (BIAS) {
+                read_bias(begin + i);
+                store_bias(begin + i);
+            }
+            if (!late) load(begin + i);
+        }
+        if (!late) wait_loads<2 * N *(L::AHEAD - 1)>();
+        lds_barrier();
+        if (late) lds_barrier();
+        form(begin);
+        lds_barrier();
+        for (int step = begin; step + 1 < end; ++step) {
+            weights(step);
+            if (!late) wait_loads<STEP *(L::AHEAD - 1)>();  // the next step's keys and values
+            lds_barrier();
+            add(step);
+            form(step + 1);
+            constexpr int READS = 2 * (D / 32) * 2 + 2 * (D / 16), PRODUCTS = 2 * (D / 32) + 2 * (D / 16);  // 4 reads to 3 products
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+            for (int i = 0; i < (READS - 8) / 4; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - 8) / 4 * 3, 0);
+            lds_barrier();
+        }
+        weights(end - 1);
+        lds_barrier();
+        add(end - 1);
+        if (NW == 8 && !late) lds_barrier();
+        wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
     if (!there) return;
 #pragma unroll
@@ -321,7 +501,7 @@ static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 template <int DT, int D, int NW>
 static void launch_k(hipStream_t st, const GradArgs &g, int splits)
 {
-    const int64_t tiles = g.a.num_keys / (NW * 32) + g.a.n;
+    const int64_t tiles = g.a.num_keys / GradK<NW>::KEYS + g.a.n;
     const dim3 grid((unsigned)(tiles * g.a.kv_heads * splits)), block(NW * 64);
     if (g.a.bias) grad_k_kernel<DT, D, NW, true><<<grid, block, 0, st>>>(g, tiles, splits);
     else grad_k_kernel<DT, D, NW, false><<<grid, block, 0, st>>>(g, tiles, splits);
@@ -340,6 +520,13 @@ static void launch(hipStream_t st, const GradArgs &g, int q_waves, int q_splits,
     const AttendArgs &a = g.a;
     const int64_t q_values = a.num_queries * a.heads * D, k_values = a.num_keys * a.kv_heads * D;
     if (a.num_queries > 0) delta_kernel<DT, D><<<dim3((unsigned)ceil_div(q_values / 8, 256)), dim3(256), 0, st>>>(g);
+    if (g.dq && a.num_queries > 0) {
+        if (q_waves == 8) launch_q<DT, D, 8>(st, g, q_splits);
+        else launch_q<DT, D, 4>(st, g, q_splits);
+        if (q_splits > 1)
+            add_splits_kernel<DT><<<dim3((unsigned)ceil_div(q_values / 4, 256)), dim3(256), 0, st>>>(g.dq_part, g.dq, q_values, q_splits, a.q_offsets, a.n,
+                                                                                                    (int64_t)a.heads * D);
+    }
     if ((g.dk || g.dv || g.dbias) && a.num_keys > 0) {
         if (k_waves == 8) launch_k<DT, D, 8>(st, g, k_splits);
         else launch_k<DT, D, 4>(st, g, k_splits);
@@ -351,13 +538,6 @@ static void launch(hipStream_t st, const GradArgs &g, int q_waves, int q_splits,
         if (g.dbias)
             add_bias_kernel<DT><<<dim3((unsigned)ceil_div(a.num_keys, 256)), dim3(256), 0, st>>>(g.dbias_part, g.dbias, a.num_keys, k_splits * a.kv_heads,
                                                                                                 a.k_offsets, a.n);
-    }
-    if (g.dq && a.num_queries > 0) {
-        if (q_waves == 8) launch_q<DT, D, 8>(st, g, q_splits);
-        else launch_q<DT, D, 4>(st, g, q_splits);
-        if (q_splits > 1)
-            add_splits_kernel<DT><<<dim3((unsigned)ceil_div(q_values / 4, 256)), dim3(256), 0, st>>>(g.dq_part, g.dq, q_values, q_splits, a.q_offsets, a.n,
-                                                                                                    (int64_t)a.heads * D);
     }
 }
 void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_waves, int q_splits, int k_waves, int k_splits)

@@ -23,7 +23,8 @@ struct TileBuffers {
     static constexpr int TILES = Ahead<NW, SRC>::TILES;
     char k[TILES][MANY_KEYS * D * 2];
     char v[TILES][SRC == PLAID_SOURCE_PAGED ? D * (MANY_KEYS + 4) * 2 : MANY_KEYS * D * 2];
-    float bias[SRC == PLAID_SOURCE_BIAS ? NW : 1][2][SRC == PLAID_SOURCE_BIAS ? MANY_KEYS : 4];  // each wave's own
+    float bias[SRC == PLAID_SOURCE_BIAS ? NW : 1][4][SRC == PLAID_SOURCE_BIAS ? MANY_KEYS : 4];  // each wave's own
+    uint32_t raw[SRC == PLAID_SOURCE_BIAS ? NW : 1][4][64];  // biases as they are loaded
     int cell[4][4];  // paged: whether the cells of 16 keys have a block
 };
 
@@ -39,100 +40,98 @@ struct Stage {
     static constexpr int TILES = Ahead<NW, SRC>::TILES, CHUNKS = D / 8, AT_ONCE = 512 / D, N = MANY_KEYS / AT_ONCE / NW;  // loads of a wave a tile
     static constexpr bool BIAS = SRC == PLAID_SOURCE_BIAS;
     static constexpr uint16_t NONE = DT == PLAID_BF16 ? 0xff80 : 0xfc00;  // -infinity
-    uint16_t bias;           // of the lane's key in the tile after the one whose biases lie in LDS
-    uint64_t masked, after;  // masked keys of the tile whose biases are used, and of the next one
+    uint64_t k_masked, v_masked;  // keys of bias -infinity, and places past the end, in the tiles that are asked for next
 
     // Keys past the end repeat the last one.  The tiles after the last repeat that one, so that a phase's number of loads is fixed.
-    __device__ __forceinline__ void load(const KeyRange &kr, const char *rows, int64_t token, int64_t head, int tile, char *to)
+    __device__ __forceinline__ void load(const KeyRange &kr, const char *rows, int64_t token, int64_t head, int tile, char *to, uint64_t masked)
     {
         const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), last = kr.len - 1 - tile * MANY_KEYS;
         const char *base = rows + (kr.base + tile * MANY_KEYS) * token + kr.head * head;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int row = (wave * N + i) * AT_ONCE + lane / CHUNKS, chunk = (lane % CHUNKS) ^ swizzle<D>(row);
-            load_to_lds(base, (uint32_t)min(row, last) * (uint32_t)token + chunk * 16, to + (wave * N + i) * 1024);
+            const int first = (wave * N + i) * AT_ONCE, row = first + lane / CHUNKS, chunk = (lane % CHUNKS) ^ swizzle<D>(row);
+            const uint32_t off = (uint32_t)min(row, last) * (uint32_t)token + chunk * 16;
+            if constexpr (BIAS) {
+                const bool none = (uint32_t)(masked >> first) >> (lane / CHUNKS) & 1;
+                load_to_lds(none ? (const char *)zero_row : base + off, to + (wave * N + i) * 1024);
+            } else {
+                load_to_lds(base, off, to + (wave * N + i) * 1024);
+            }
         }
     }
     __device__ __forceinline__ void load_k(const AttendArgs &a, const KeyRange &kr, int tile, int end, TileBuffers<D, NW, SRC> &b)
     {
-        load(kr, a.k, a.k_token, a.k_head, min(tile, end - 1), b.k[tile % TILES]);
+        load(kr, a.k, a.k_token, a.k_head, min(tile, end - 1), b.k[tile % TILES], k_masked);
     }
     __device__ __forceinline__ void load_v(const AttendArgs &a, const KeyRange &kr, int tile, int end, TileBuffers<D, NW, SRC> &b)
     {
-        load(kr, a.v, a.v_token, a.v_head, min(tile, end - 1), b.v[tile % TILES]);
+        load(kr, a.v, a.v_token, a.v_head, min(tile, end - 1), b.v[tile % TILES], v_masked);
     }
-    __device__ __forceinline__ void load_bias(const AttendArgs &a, const KeyRange &kr, int tile, int end)
+    __device__ __forceinline__ void load_bias(const AttendArgs &a, const KeyRange &kr, int tile, int end, TileBuffers<D, NW, SRC> &b)
     {
-        const int lane = threadIdx.x & 63, t = min(tile, end - 1), last = kr.len - 1 - t * MANY_KEYS;
-        bias = ((const uint16_t *)a.bias + kr.base + t * MANY_KEYS)[(uint32_t)min(lane, last)];
+        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), t = min(tile, end - 1), last = kr.len - 1 - t * MANY_KEYS;
+        load2_to_lds(a.bias + 2 * (kr.base + t * MANY_KEYS), 2 * min(lane, last), b.raw[wave][tile & 3]);
     }
-    __device__ __forceinline__ void store_bias(const KeyRange &kr, TileBuffers<D, NW, SRC> &b, int tile)
+    // The biases of the tile whose keys are asked for next, in 32 bits, and which of its keys are masked.  They are read some time
+    // before they are used.
+    uint32_t raw;
+    __device__ __forceinline__ void read_bias(const TileBuffers<D, NW, SRC> &b, int tile) { raw = b.raw[threadIdx.x >> 6][tile & 3][threadIdx.x & 63]; }
+    __device__ __forceinline__ void store_bias(const KeyRange &kr, int end, TileBuffers<D, NW, SRC> &b, int tile)
     {
         const int lane = threadIdx.x & 63;
-        const uint16_t x = tile * MANY_KEYS + lane < kr.len ? bias : NONE;
-        b.bias[threadIdx.x >> 6][tile & 1][lane] = unpack<DT>(x, 0);
-        after = __ballot(x == NONE);
-    }
-    // What a masked key holds is replaced by zeros: an infinity there would make a product with a weight of zero not a number.
-    // The keys go round the first `waves` waves.
-    __device__ __forceinline__ void clear(char *tile, uint64_t keys, int waves)
-    {
-        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
-        if (wave >= waves) return;
-        for (keys &= (waves == 8 ? 0x0101010101010101ull : 0x1111111111111111ull) << wave; keys; keys &= keys - 1)
-            if (lane < CHUNKS) *(i32x4 *)(tile + __builtin_ctzll(keys) * (D * 2) + lane * 16) = i32x4{0, 0, 0, 0};
+        const uint16_t x = min(tile, end - 1) * MANY_KEYS + lane < kr.len ? (uint16_t)raw : NONE;
+        b.bias[threadIdx.x >> 6][tile & 3][lane] = unpack<DT>(x, 0);
+        v_masked = k_masked;
+        k_masked = __ballot(x == NONE);
     }
     // Before the first phase: asks for the first tiles and waits for the first one's keys.
     __device__ __forceinline__ void start(const AttendArgs &a, const KeyRange &kr, int begin, int end, TileBuffers<D, NW, SRC> &b)
     {
         using A = Ahead<NW, SRC>;
-        if constexpr (BIAS) load_bias(a, kr, begin, end);
-        load_k(a, kr, begin, end, b);
-#pragma unroll
-        for (int i = 1; i < A::K; ++i) {
-            load_k(a, kr, begin + i, end, b);
-            load_v(a, kr, begin + i - 1, end, b);
-        }
+        static_assert(A::V == A::K - 1, "values are asked for one tile behind the keys");
         if constexpr (BIAS) {
-            store_bias(kr, b, begin);
-            masked = after;
-            load_bias(a, kr, begin + 1, end);
+#pragma unroll
+            for (int i = 0; i <= A::K; ++i) load_bias(a, kr, begin + i, end, b);
             wait_loads<0>();
-            lds_barrier();
-            clear(b.k[begin % TILES], masked, NW);
-        } else {
-            wait_loads<2 * N *(A::K - 1)>();
         }
+#pragma unroll
+        for (int i = 0; i < A::K; ++i) {
+            if constexpr (BIAS) {
+                read_bias(b, begin + i);
+                store_bias(kr, end, b, begin + i);
+            }
+            load_k(a, kr, begin + i, end, b);
+            if (i > 0) load_v(a, kr, begin + i - 1, end, b);
+        }
+        wait_loads<2 * N *(A::K - 1)>();
         lds_barrier();
     }
-    // In the second phase of a step, after its weights.
+    // In the second phase of a step, before and after its weights.
+    __device__ __forceinline__ void before(int step, const TileBuffers<D, NW, SRC> &b)
+    {
+        if constexpr (BIAS) {
+            wait_loads<2 * N>();  // the biases that the step before asked for first
+            read_bias(b, step + Ahead<NW, SRC>::K);
+        }
+    }
     __device__ __forceinline__ void bring(const AttendArgs &a, const KeyRange &kr, int step, int end, int, TileBuffers<D, NW, SRC> &b)
     {
         using A = Ahead<NW, SRC>;
         if constexpr (BIAS) {
-            store_bias(kr, b, step + 1);
-            clear(b.k[(step + 1) % TILES], after, 4);
-            clear(b.v[step % TILES], masked, 4);
-            masked = after;
-            load_bias(a, kr, step + 2, end);
+            store_bias(kr, end, b, step + A::K);
+            load_bias(a, kr, step + A::K + 1, end, b);
         }
         load_k(a, kr, step + A::K, end, b);
         load_v(a, kr, step + A::V, end, b);
     }
     // At the end of a phase: what the phases after the next barrier need has arrived.  A step asks for 2 N pieces (and its bias);
-    // the next step's keys and this one's values must be there after its second phase, with a bias (see clear) after its first.
+    // the next step's keys and this one's values must be there after its second phase.
     __device__ __forceinline__ void arrive(bool second, int late)
     {
         constexpr int STEP = 2 * N + BIAS;
         if constexpr (Ahead<NW, SRC>::GROUPS == 2) {
-            if constexpr (BIAS) {
-                if (second == (late == 1)) wait_loads<STEP *(TILES - 3)>();
-            } else {
-                if (second && !late) wait_loads<STEP *(TILES - 2)>();
-                if (!second && late) wait_loads<STEP *(TILES - 3)>();
-            }
-        } else if constexpr (BIAS) {
-            if (!second) wait_loads<0>();
+            if (second && !late) wait_loads<STEP *(TILES - 2)>();
+            if (!second && late) wait_loads<STEP *(TILES - 3)>();
         } else {
             if (second) wait_loads<STEP *(TILES - 1)>();
         }
@@ -259,6 +258,7 @@ struct Stage<DT, D, NW, PLAID_SOURCE_PAGED> {
         if (tile + 2 < end) load_k(a, kr, tile + 2);
         if (tile + 1 < end) load_v(a, kr, tile + 1);
     }
+    __device__ __forceinline__ void before(int, const TileBuffers<D, NW, PLAID_SOURCE_PAGED> &) {}
     __device__ __forceinline__ void arrive(bool, int) {}
 };
 
@@ -380,6 +380,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = mfma32<DT>(value_operand<D, NW, SRC>(lds, step % A::TILES, 16 * i, dt), p[i], o[dt]);
     };
     auto weights = [&](int step) {
+        if constexpr (SRC == PLAID_SOURCE_DENSE) stage.bring(a, kr, step, end, late, lds);
+        else stage.before(step, lds);
         float top;
         if constexpr (SRC == PLAID_SOURCE_BIAS) {
             if (odd) {
@@ -387,20 +389,20 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (lds.bias[wave][step & 1][32 * mt + 8 * (i >> 2) + 4 * h + (i & 3)] == -INFINITY) s[mt][i] = 0.0f;
+                        if (lds.bias[wave][step & 3][32 * mt + 8 * (i >> 2) + 4 * h + (i & 3)] == -INFINITY) s[mt][i] = 0.0f;
             }
             top = -INFINITY;
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
+            for (int mt = 0; mt < 2; ++mt) {
+                f32x4 b[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x4 b = *(const f32x4 *)&lds.bias[wave][step & 1][32 * mt + 8 * i + 4 * h];
+                for (int i = 0; i < 4; ++i) b[i] = *(const f32x4 *)&lds.bias[wave][step & 3][32 * mt + 8 * i + 4 * h];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[mt][4 * i + e] = fmaf(s[mt][4 * i + e], a.scale, b[e]);
-                        top = fmaxf(top, s[mt][4 * i + e]);
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    s[mt][i] = fmaf(s[mt][i], a.scale, b[i >> 2][i & 3]);
+                    top = fmaxf(top, s[mt][i]);
                 }
+            }
         } else {
             bool whole = (step + 1) * MANY_KEYS <= least;
             if constexpr (SRC == PLAID_SOURCE_PAGED) whole = whole && (lds.cell[step & 3][0] & lds.cell[step & 3][1] & lds.cell[step & 3][2] & lds.cell[step & 3][3]);
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             }
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = round8<DT>(s[i >> 1], i & 1);
-        stage.bring(a, kr, step, end, late, lds);
+        if constexpr (SRC != PLAID_SOURCE_DENSE) stage.bring(a, kr, step, end, late, lds);
     };
     if (begin < end) {
         scores(begin);

@@ -39,6 +39,7 @@ struct GradArgs {
     const char *d_out;
     char *dq, *dk, *dv, *dbias;        // any may be null
     float *delta;                      // [num_queries][heads]
+    float *exponent;                   // [num_queries][heads] what the weights' exponents of 2 have subtracted, infinity without a key
     float *dbias_part;                 // [splits][kv_heads][num_keys], null without dbias
     float *dk_part, *dv_part;          // [splits][num_keys][kv_heads][D], null with one split
     float *dq_part;                    // [splits][num_queries][heads][D], null with one split
@@ -314,10 +315,28 @@ __device__ __forceinline__ void wait_loads()
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-// 16 bytes of every lane, one after the other, into the 1024 bytes of LDS at `to` (the same for all lanes), from base + off.
+// Where keys that are masked are loaded from: an infinity in what they hold would make a product with a weight of zero not a number.
+static __device__ const i32x4 zero_row[16] = {};
+
+// 16 (4) bytes of every lane, from base + off, into the 1024 (256) bytes of LDS at `to` (the same for all lanes), lane after lane.
+// There is no result in registers and the compiler does not count these loads: it would have every transposing read of LDS wait
+// for all of them.  (They go by register m0, which nothing else in these kernels uses.)  What they bring is waited for with wait_loads, before the barrier that lets it be read and before the end.
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, char *to)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off), (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_address(to)), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(const char *from, char *to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(to)), "v"(from) : "memory");
+}
+__device__ __forceinline__ void load2_to_lds(const char *base, uint32_t off, uint32_t *to)  // 2 bytes a lane, 4 in LDS
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(lds_address(to)), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load4_to_lds(const float *from, float *to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(to)), "v"(from) : "memory");
 }
 // Rows 8 i .. of a result's registers as an operand: registers 8 i .. 8 i + 7 rounded to the type.
 template <int DT>

@@ -94,10 +94,10 @@ Plan plan_backward(const plaid_attention &a)
     Plan p = {};
     const int64_t group = a.heads / a.kv_heads, rows = ceil_div(a.num_queries, a.n) * group, keys = ceil_div(a.num_keys, a.n);
     p.q_waves = rows > 128 ? BIGQ : 4;
-    p.k_waves = keys > 128 ? BIGK : 4;
+    p.k_waves = keys > 64 ? BIGK : 4;
     p.q_splits = (int)split_count(ceil_div(rows, p.q_waves * 32) * a.n * a.kv_heads, ceil_div(keys, 64), 4);
-    p.k_splits = (int)split_count(ceil_div(keys, p.k_waves * 32) * a.n * a.kv_heads, ceil_div(rows, 32), 8);
-    p.delta_bytes = round16(a.num_queries * a.heads * 4);
+    p.k_splits = (int)split_count(ceil_div(keys, p.k_waves * 16) * a.n * a.kv_heads, ceil_div(rows, 64), 4);
+    p.delta_bytes = 2 * round16(a.num_queries * a.heads * 4);  // and the rows' exponents
     p.bias_bytes = round16((int64_t)p.k_splits * a.kv_heads * a.num_keys * 4);
     p.k_bytes = p.k_splits > 1 ? (int64_t)p.k_splits * a.num_keys * a.kv_heads * a.head_dim * 4 : 0;
     p.q_bytes = p.q_splits > 1 ? (int64_t)p.q_splits * a.num_queries * a.heads * a.head_dim * 4 : 0;
@@ -122,7 +122,7 @@ int check_rows(const char *what, const void *p, int64_t token, int64_t head)
 {
     if (!p || misaligned(p, 16)) FAIL("%s is null or not 16-byte aligned", what);
     if (token % 8 || head % 8) FAIL("the strides of %s are no multiples of 8 elements", what);
-    if (token < 0 || token >= 1 << 25) FAIL("the token stride of %s is out of range", what);  // 32 rows lie within 32 bits
+    if (token < 0 || token >= 1 << 24 || head < 0 || head >= 1 << 24) FAIL("a stride of %s is out of range", what);  // 64 rows lie within 32 bits
     return PLAID_OK;
 }
 // Pointers that any attention call reads; out is an input of the backward pass.
@@ -331,7 +331,7 @@ extern "C" int plaid_cross_attention_backward(const plaid_attention *args, const
     if (const int rc = check_workspace(workspace, workspace_bytes, p.bytes)) return rc;
     const int64_t group = args->heads / args->kv_heads;
     if ((args->num_queries * group / (p.q_waves * 32) + args->n) * args->kv_heads * p.q_splits > INT32_MAX ||
-        (args->num_keys / (p.k_waves * 32) + args->n) * args->kv_heads * p.k_splits > INT32_MAX)
+        (args->num_keys / (p.k_waves * 16) + args->n) * args->kv_heads * p.k_splits > INT32_MAX)
         FAIL("too much work for one call");
     const OnDevice guard(device);
     if (!guard.ok) return plaid_fail(PLAID_EHIP, "device %d cannot be used", device);
@@ -340,7 +340,7 @@ extern "C" int plaid_cross_attention_backward(const plaid_attention *args, const
     g.d_out = (const char *)d_out;
     g.dq = (char *)dq, g.dk = (char *)dk, g.dv = (char *)dv, g.dbias = (char *)dbias;
     char *w = (char *)workspace;
-    g.delta = (float *)w, w += p.delta_bytes;
+    g.delta = (float *)w, g.exponent = (float *)(w + p.delta_bytes / 2), w += p.delta_bytes;
     g.dbias_part = dbias ? (float *)w : nullptr, w += p.bias_bytes;
     g.dk_part = p.k_bytes ? (float *)w : nullptr, w += p.k_bytes;
     g.dv_part = p.k_bytes ? (float *)w : nullptr, w += p.k_bytes;
