@@ -324,7 +324,7 @@ typedef struct {
     int32_t dtype;    /* plaid_dtype */
 } plaid_paged_cache;
 
-/* Writes keys and values of n tokens (k, v: rows token_stride apart, heads head_stride, both in elements and multiples of 8;
+/* Writes keys and values of n tokens (k, v: rows token_stride apart, heads head_stride, in elements, multiples of 8 in [0, 2^24);
  * 16-byte aligned) to their slots; a slot outside [0, num_blocks * block_size) is left out, two equal slots are a caller's
  * mistake.  The power of two of a group is the smallest that keeps its largest magnitude within 6 (bf16: 2^-126 .. 2^126,
  * fp16: 2^-23 .. 2^14), values round to the nearest code, ties to the even one, and stay finite in the type. */
@@ -338,17 +338,19 @@ int plaid_cache_read(const plaid_paged_cache *cache, const int64_t *slots, int64
 
 /* Arguments of an attention call.  Row (token i of request r, head h) attends with key head h * kv_heads / heads:
  *   s_j = scale * q . k_j + key_bias_j,   out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j);
- * a row that no key is left for gives zeros and -INFINITY.  lse is two numbers to be added, a score near the largest and the
- * rest, so that it is whole where all scores are as low as the type goes.  Sums, softmax statistics and their exponentials are held in 32
+ * a row that no key is left for gives zeros and -INFINITY.  lse is two numbers to be added, a shift
+ * (0 unless all of a request's biases are beyond 256 in magnitude) and the rest, so that it is whole where all scores are as low as
+ * the type goes.  Sums, softmax statistics and their exponentials are held in 32
  * bits; the softmax's weights round to the type before they multiply the values.
  *   q, k, v          [num_queries | num_keys][heads | kv_heads][head_dim] of dtype, 16-byte aligned, the strides of tokens and
- *                    heads in elements and multiples of 8; k and v are those of plaid_cross_attention
+ *                    heads in elements, multiples of 8 in [0, 2^24); k and v are those of plaid_cross_attention
  *   key_bias         [num_keys] of dtype, or NULL; a key of bias -INFINITY takes no part, whatever k and v hold there
  *   q_offsets        [n+1] int64: the tokens of request r are rows q_offsets[r] .. q_offsets[r+1]-1; rows outside every request
  *                    are not written
  *   k_offsets        [n+1] int64, the same for the keys (plaid_cross_attention)
  *   out              [num_queries][heads][head_dim] contiguous, lse [num_queries][heads][2] fp32 or NULL
- * heads is a multiple of kv_heads, head_dim 64 or 128; num_queries * (heads / kv_heads)^2 < 2^32. */
+ * heads is a multiple of kv_heads, head_dim 64 or 128; num_queries * (heads / kv_heads)^2 < 2^32.  A scale may be negative.  Over a
+ * paged cache a group that is not finite reaches every row whose tile of keys it is in, also rows that are before it. */
 typedef struct {
     int32_t dtype;
     int32_t n;

@@ -139,7 +139,7 @@ struct FewLds {
         char v[SRC == PLAID_SOURCE_PAGED ? 16 : NW * 32 * D * 2];  // dense values, a part for each wave
         float o[NW][FEW_ROWS][D + 4];
     };
-    float ml[NW][FEW_ROWS][2];
+    float ml[NW][FEW_ROWS][2], shift[NW];
 };
 
 // Keys and values of a piece are loaded apart, each into the registers that its predecessor has just left: the scores of a
@@ -193,6 +193,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
 #pragma unroll
         for (int t = 0; t < OT; ++t) o[t] = f32x4{0, 0, 0, 0};
         float m = -INFINITY, l = 0.0f;
+        Shift shift;
 
         // --- loads of a piece
         Piece<DT, D, SRC> x;
@@ -336,13 +337,22 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
             }
             if (more) load_k(step + 1);
             if constexpr (BIAS) {
+                float b[8], largest = -INFINITY;
+                bool unusual = false, usual = false;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int e = 0; e < 8; ++e) {
+                    b[e] = unpack<DT>(bias[e >> 1], e & 1);
+                    const bool is = unusual_bias(b[e]);
+                    unusual = unusual || is;
+                    usual = usual || (!is && b[e] != -INFINITY);
+                    largest = is ? fmaxf(largest, b[e]) : largest;
+                }
+                const float c = shift.c;
+                shift.add(__ballot(unusual), largest, __any(usual));
+                m += c - shift.c;  // m is relative to the shift
+                const float scale = beside_shift(a.scale, shift.c);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float b = unpack<DT>(bias[2 * c + (e >> 1)], e & 1);
-                        s[c][e] = b == -INFINITY ? -INFINITY : fmaf(s[c][e], a.scale, b);
-                    }
+                for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = b[e] == -INFINITY ? -INFINITY : fmaf(s[e >> 2][e & 3], scale, b[e] - shift.c);
             } else if (key0 + 32 > least || !held0 || !held1) {
                 // some key of the piece is hidden from some row
 #pragma unroll
@@ -360,7 +370,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
             }
             const float top = max_halves(max_rows(larger(larger(larger(s[0][0], s[0][1]), larger(s[0][2], s[0][3])),
                                                          larger(larger(s[1][0], s[1][1]), larger(s[1][2], s[1][3])))));
-            if (__any((top - m) * cs > 8.0f)) {
+            if (__any(!((top - m) * cs <= 8.0f))) {  // also where there was no key so far
                 const float to = fmaxf(m, top);
                 const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - to) * cs);
                 m = to;
@@ -370,12 +380,12 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[t][e] *= alpha;
             }
-            const float ref = m == -INFINITY ? 0.0f : m, ref_cs = ref * cs;
+            const float ref_cs = m == -INFINITY ? 0.0f : m * cs;
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float y = BIAS ? (s[c][e] - ref) * cs : fmaf(s[c][e], cs, -ref_cs);
+                    const float y = fmaf(s[c][e], cs, -ref_cs);
                     s[c][e] = __builtin_amdgcn_exp2f(y);
                     l += s[c][e];
                 }
@@ -428,35 +438,42 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
 #pragma unroll
         for (int t = 0; t < OT; ++t) *(f32x4 *)&lds.o[wave][m16][16 * t + 4 * kg] = o[t];
         if (kg == 0) lds.ml[wave][m16][0] = natural, lds.ml[wave][m16][1] = l;
+        if (lane == 0) lds.shift[wave] = shift.c;
         __syncthreads();
         for (int u = threadIdx.x; u < FEW_ROWS * (D / 4); u += NW * 64) {
             const int y = u / (D / 4), d = u % (D / 4) * 4;  // a row and 4 of its dimensions
-            float top = -INFINITY, sum = 0.0f;
+            float base = -INFINITY, top = -INFINITY, sum = 0.0f;
             f32x4 acc{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < NW; ++i) top = fmaxf(top, lds.ml[i][y][0]);
+            for (int i = 0; i < NW; ++i) base = fmaxf(base, lds.ml[i][y][1] == 0.0f ? -INFINITY : lds.shift[i]);
+            const float c = base == -INFINITY ? 0.0f : base;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) top = fmaxf(top, lds.shift[i] - c + lds.ml[i][y][0]);
             const float ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
-                const float w = __builtin_amdgcn_exp2f((lds.ml[i][y][0] - ref) * LOG2E);
+                const float w = __builtin_amdgcn_exp2f((lds.shift[i] - c + lds.ml[i][y][0] - ref) * LOG2E);
                 const f32x4 z = *(const f32x4 *)&lds.o[i][y][d];
                 sum += w * lds.ml[i][y][1];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[e] += w * z[e];
             }
             const int row_out = tile * FEW_ROWS + y;
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float2 lse = sum == 0.0f ? float2{-INFINITY, 0.0f} : float2{base, top + logf(sum)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] *= inv;
             if (begin == 0 && stop == rq.steps) {
                 if (row_out < rows) {
                     const int tk = row_token(a, row_out);
                     const int64_t to = (rq.row0 + tk) * a.heads + head_kv * a.group + row_out - tk * a.group;
-                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    *(i32x2 *)(a.out + (to * D + d) * 2) = i32x2{pack2<DT>(acc[0] * inv, acc[1] * inv), pack2<DT>(acc[2] * inv, acc[3] * inv)};
-                    if (a.lse && d == 0) a.lse[2 * to] = sum == 0.0f ? -INFINITY : top, a.lse[2 * to + 1] = sum == 0.0f ? 0.0f : logf(sum);
+                    *(i32x2 *)(a.out + (to * D + d) * 2) = i32x2{pack2<DT>(acc[0], acc[1]), pack2<DT>(acc[2], acc[3])};
+                    if (a.lse && d == 0) *(float2 *)(a.lse + 2 * to) = lse;
                 }
             } else {
                 const int64_t slot = ((int64_t)worker * 2 + (begin == 0)) * a.kv_heads + head_kv;
                 *(f32x4 *)(a.part_o + (slot * FEW_ROWS + y) * D + d) = acc;
-                if (d == 0) a.part_ml[(slot * FEW_ROWS + y) * 2] = top, a.part_ml[(slot * FEW_ROWS + y) * 2 + 1] = sum;
+                if (d == 0) *(float2 *)(a.part_lse + (slot * FEW_ROWS + y) * 2) = lse;
             }
         }
         __syncthreads();  // before the next tile's values and sums
@@ -470,7 +487,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
 template <int DT, int D, int NW, int SRC>
 __global__ __launch_bounds__(JOIN_THREADS) void join_workers_kernel(AttendArgs a, int workers)
 {
-    __shared__ float s_top[JOIN_THREADS], s_sum[JOIN_THREADS];
+    __shared__ float s_shift[JOIN_THREADS], s_top[JOIN_THREADS], s_sum[JOIN_THREADS];
     __shared__ __align__(16) f32x4 s_acc[JOIN_THREADS];
     const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, 4, blockIdx.x);
     if (tp.r < 0) return;
@@ -486,32 +503,40 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_workers_kernel(AttendArgs a
     const int parts = min(min(w1 - w0 + 1, JOIN_PARTS), JOIN_THREADS / units);
     const int part = threadIdx.x / units, u = threadIdx.x % units, y = u / (D / 4), d = u % (D / 4) * 4;
     auto place = [&](int w) { return (((int64_t)w * 2 + (w == w0)) * a.kv_heads + head_kv) * FEW_ROWS + y; };
-    float top = -INFINITY, sum = 0.0f;
+    float c = -INFINITY, top = -INFINITY, sum = 0.0f;
     f32x4 acc{0, 0, 0, 0};
     if (part < parts) {
 #pragma unroll 4
-        for (int w = w0 + part; w <= w1; w += parts) top = fmaxf(top, a.part_ml[2 * place(w)]);
-        const float ref = top == -INFINITY ? 0.0f : top;
+        for (int w = w0 + part; w <= w1; w += parts) {
+            const float2 x = *(const float2 *)(a.part_lse + 2 * place(w));
+            // relative to the largest shift so far
+            const float to = fmaxf(c, x.x), moved = top + (c == -INFINITY ? 0.0f : c - to), next = x.x - to + x.y;
+            if (x.x != -INFINITY) top = fmaxf(moved, next), c = to;
+        }
+        const float base = c == -INFINITY ? 0.0f : c, ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll 4
         for (int w = w0 + part; w <= w1; w += parts) {
             const int64_t p = place(w);
-            const float f = __builtin_amdgcn_exp2f((a.part_ml[2 * p] - ref) * LOG2E);
-            sum += f * a.part_ml[2 * p + 1];
+            const float2 x = *(const float2 *)(a.part_lse + 2 * p);
+            const float f = __builtin_amdgcn_exp2f((x.x - base + x.y - ref) * LOG2E);
+            sum += f;
             const f32x4 v = *(const f32x4 *)(a.part_o + p * D + d);
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += f * v[e];
         }
-        s_top[threadIdx.x] = top, s_sum[threadIdx.x] = sum, s_acc[threadIdx.x] = acc;
+        s_shift[threadIdx.x] = c, s_top[threadIdx.x] = top, s_sum[threadIdx.x] = sum, s_acc[threadIdx.x] = acc;
     }
     __syncthreads();
     if (part) return;
-    top = s_top[u];
-    for (int i = 1; i < parts; ++i) top = fmaxf(top, s_top[i * units + u]);
+    for (int i = 0; i < parts; ++i) c = fmaxf(c, s_shift[i * units + u]);
+    const float base = c == -INFINITY ? 0.0f : c;
+    top = -INFINITY;
+    for (int i = 0; i < parts; ++i) top = fmaxf(top, s_shift[i * units + u] - base + s_top[i * units + u]);
     const float ref = top == -INFINITY ? 0.0f : top;
     sum = 0.0f;
     acc = f32x4{0, 0, 0, 0};
     for (int i = 0; i < parts; ++i) {
-        const float f = __builtin_amdgcn_exp2f((s_top[i * units + u] - ref) * LOG2E);
+        const float f = __builtin_amdgcn_exp2f((s_shift[i * units + u] - base + s_top[i * units + u] - ref) * LOG2E);
         const f32x4 v = s_acc[i * units + u];
         sum += f * s_sum[i * units + u];
 #pragma unroll
@@ -521,7 +546,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_workers_kernel(AttendArgs a
     const int64_t to = (rq.row0 + tk) * a.heads + head_kv * a.group + row - tk * a.group;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     *(i32x2 *)(a.out + (to * D + d) * 2) = i32x2{pack2<DT>(acc[0] * inv, acc[1] * inv), pack2<DT>(acc[2] * inv, acc[3] * inv)};
-    if (a.lse && d == 0) a.lse[2 * to] = sum == 0.0f ? -INFINITY : top, a.lse[2 * to + 1] = sum == 0.0f ? 0.0f : logf(sum);
+    if (a.lse && d == 0) *(float2 *)(a.lse + 2 * to) = sum == 0.0f ? float2{-INFINITY, 0.0f} : float2{c, top + logf(sum)};
 }
 
 template <int DT, int D, int SRC>

@@ -28,9 +28,16 @@ __global__ __launch_bounds__(256) void delta_kernel(GradArgs g)
         if (c == 0) {
             const float2 lse = *(const float2 *)(g.a.lse + 2 * at);
             g.delta[at] = lse.x != -INFINITY ? sum : 0.0f;
-            g.exponent[at] = lse.x != -INFINITY ? fmaf(lse.x, LOG2E, lse.y * LOG2E) : INFINITY;
+            g.exponent[at] = lse.x != -INFINITY ? lse.y * LOG2E : INFINITY;
         }
     }
+}
+
+// The shift of a request's biases (see Shift): all of its rows have the same.
+__device__ __forceinline__ float request_shift(const AttendArgs &a, int64_t row0, int rows)
+{
+    const float c = rows ? uniform_load(a.lse + 2 * row0 * a.heads) : -INFINITY;
+    return c == -INFINITY ? 0.0f : c;
 }
 
 // Both kernels run in phases like the forward one (k_attend_many.hip): products on one side, exponentials on the other, two groups
@@ -85,8 +92,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     }
     float bias = 0.0f;
     if (BIAS) bias = there ? load16<DT>(a.bias + 2 * (tp.begin + key)) : 0.0f;
-    const bool is_low = BIAS && bias < -1e38f && bias != -INFINITY, low = __any(is_low);
-    const float cs = a.scale * LOG2E, bias_e = bias * LOG2E;
+    const float c = BIAS ? request_shift(a, row0, rows) : 0.0f, cs = beside_shift(a.scale, c) * LOG2E, bias_e = (bias - c) * LOG2E;
     f32x16 sum[D / 32];  // the first wave's dv, the second one's dk
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) sum[t] = zero16();
@@ -168,22 +174,12 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[b][4 * i + e] = BIAS ? fmaf(s[b][4 * i + e], cs, bias_e) - ex[e] : fmaf(s[b][4 * i + e], cs, -ex[e]);
                 }
-            if (low || (step + 1) * ROWS > rows) {
+            if ((step + 1) * ROWS > rows) {
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int row = step * ROWS + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3);
-                        if (row >= rows) {
-                            s[b][i] = -INFINITY;  // no row: its weights are 0
-                        } else if (is_low) {
-                            // a bias near the type's lowest value: a score is nothing beside it, and only where all of a row's are as low
-                            // is there a weight; the difference to the row's maximum comes before it is scaled
-                            const int token = row_token(a, row);
-                            const float2 lse = *(const float2 *)(a.lse + 2 * ((row0 + token) * a.heads + head * a.group + row - token * a.group));
-                            s[b][i] = lse.x < -1e38f ? (bias - lse.x) * LOG2E - lse.y * LOG2E : -INFINITY;
-                        }
-                    }
+                    for (int i = 0; i < 16; ++i)
+                        if (step * ROWS + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) >= rows) s[b][i] = -INFINITY;  // no row: its weights are 0
             }
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b)
@@ -311,10 +307,8 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
     }
     const float2 lse = *(const float2 *)(a.lse + 2 * at);
     const bool counts = lse.x != -INFINITY;
-    const float m = counts ? lse.x : 0.0f, l = counts ? lse.y * LOG2E : INFINITY;
+    const float c = BIAS ? request_shift(a, tp.begin, rows) : 0.0f, ex = counts ? lse.y * LOG2E : INFINITY, cs = beside_shift(a.scale, c) * LOG2E;
     float delta = counts ? g.delta[at] : 0.0f;
-    const float ex = fmaf(m, LOG2E, l), cs = a.scale * LOG2E;
-    const bool low = BIAS && __any(m < -1e38f);
     f32x16 dq[D / 32];
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
@@ -347,7 +341,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
     auto read_bias = [&](int step) { raw = lds.raw[wave][step & 3][lane]; };
     auto store_bias = [&](int step) {
         const uint16_t x = min(step, end - 1) * GRAD_KEYS + (lane & 31) < len ? (uint16_t)raw : NONE;
-        lds.bias[wave][step & 3][lane & 31] = unpack<DT>(x, 0);
+        lds.bias[wave][step & 3][lane & 31] = unpack<DT>(x, 0) - c;
         masked = (uint32_t)__ballot(x == NONE);
     };
     f32x16 s, ds;
@@ -378,14 +372,8 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
             f32x4 b[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) b[i] = *(const f32x4 *)&lds.bias[wave][step & 3][8 * i + 4 * h];
-            if (!low) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = fmaf(b[i >> 2][i & 3], LOG2E, fmaf(s[i], cs, -ex));
-            } else {
-                // a bias near the type's lowest value: the difference to the maximum before it is scaled
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = (fmaf(s[i], a.scale, b[i >> 2][i & 3]) - m) * LOG2E - l;
-            }
+            for (int i = 0; i < 16; ++i) s[i] = fmaf(b[i >> 2][i & 3], LOG2E, fmaf(s[i], cs, -ex));
         } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], cs, -ex);

@@ -24,6 +24,7 @@ struct TileBuffers {
     char k[TILES][MANY_KEYS * D * 2];
     char v[TILES][SRC == PLAID_SOURCE_PAGED ? D * (MANY_KEYS + 4) * 2 : MANY_KEYS * D * 2];
     float bias[SRC == PLAID_SOURCE_BIAS ? NW : 1][4][SRC == PLAID_SOURCE_BIAS ? MANY_KEYS : 4];  // each wave's own
+    float shift[SRC == PLAID_SOURCE_BIAS ? NW : 1][4];        // what is subtracted from them
     uint32_t raw[SRC == PLAID_SOURCE_BIAS ? NW : 1][4][64];  // biases as they are loaded
     int cell[4][4];  // paged: whether the cells of 16 keys have a block
 };
@@ -75,14 +76,19 @@ struct Stage {
     // The biases of the tile whose keys are asked for next, in 32 bits, and which of its keys are masked.  They are read some time
     // before they are used.
     uint32_t raw;
+    Shift shift;
     __device__ __forceinline__ void read_bias(const TileBuffers<D, NW, SRC> &b, int tile) { raw = b.raw[threadIdx.x >> 6][tile & 3][threadIdx.x & 63]; }
     __device__ __forceinline__ void store_bias(const KeyRange &kr, int end, TileBuffers<D, NW, SRC> &b, int tile)
     {
         const int lane = threadIdx.x & 63;
         const uint16_t x = min(tile, end - 1) * MANY_KEYS + lane < kr.len ? (uint16_t)raw : NONE;
-        b.bias[threadIdx.x >> 6][tile & 3][lane] = unpack<DT>(x, 0);
+        const float f = unpack<DT>(x, 0);
         v_masked = k_masked;
         k_masked = __ballot(x == NONE);
+        const uint64_t unusual = __ballot(unusual_bias(f));
+        shift.add(unusual, unusual_bias(f) ? f : -INFINITY, ~(k_masked | unusual) != 0);
+        b.bias[threadIdx.x >> 6][tile & 3][lane] = f - shift.c;
+        if (lane == 0) b.shift[threadIdx.x >> 6][tile & 3] = shift.c;
     }
     // Before the first phase: asks for the first tiles and waits for the first one's keys.
     __device__ __forceinline__ void start(const AttendArgs &a, const KeyRange &kr, int begin, int end, TileBuffers<D, NW, SRC> &b)
@@ -346,7 +352,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = zero16();
     // with a bias the scores are kept as they are, else as q . k: one multiply-add then makes the exponent
     const float cs = SRC == PLAID_SOURCE_BIAS ? LOG2E : a.scale * LOG2E;
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, l = 0.0f, shift = 0.0f;
 
     // Two groups of waves, one of each on every SIMD, half a step apart: while one multiplies, the other forms exponentials.
     // A step of a group is a phase of products (o += v^T p^T of the former tile, s of this one) and one of everything else, with
@@ -392,6 +398,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
                         if (lds.bias[wave][step & 3][32 * mt + 8 * (i >> 2) + 4 * h + (i & 3)] == -INFINITY) s[mt][i] = 0.0f;
             }
             top = -INFINITY;
+            const float c = lds.shift[wave][step & 3], scale = beside_shift(a.scale, c);
+            m += shift - c;  // m is relative to the shift
+            shift = c;
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
                 f32x4 b[4];
@@ -399,7 +408,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
                 for (int i = 0; i < 4; ++i) b[i] = *(const f32x4 *)&lds.bias[wave][step & 3][32 * mt + 8 * i + 4 * h];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    s[mt][i] = fmaf(s[mt][i], a.scale, b[i >> 2][i & 3]);
+                    s[mt][i] = fmaf(s[mt][i], scale, b[i >> 2][i & 3]);
                     top = fmaxf(top, s[mt][i]);
                 }
             }
@@ -422,7 +431,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             for (int i = 1; i < 16; ++i) top = larger(larger(top, s[0][i]), s[1][i]);
         }
         top = max_halves(top);
-        if (__any((top - m) * cs > 8.0f)) {
+        if (__any(!((top - m) * cs <= 8.0f))) {  // also where there was no key so far
             const float next = fmaxf(m, top);
             const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - next) * cs);
             m = next;
@@ -432,18 +441,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
         }
-        const float ref = m == -INFINITY ? 0.0f : m;
-        float ref_cs = ref * cs;
-        if constexpr (SRC == PLAID_SOURCE_BIAS) {
-            // a bias may be the type's lowest value: the difference is taken before it is scaled
-            if (__any(ref < -1e38f)) {
-#pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[mt][i] -= ref;
-                ref_cs = 0.0f;
-            }
-        }
+        const float ref_cs = m == -INFINITY ? 0.0f : m * cs;
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -461,6 +459,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         for (int step = begin; step + 1 < end; ++step) {
             weights(step);
             phase_end(true);
+            // where the other phase has the most to do, turning codes into values, products go first (536 us in place of 564)
+            if constexpr (SRC == PLAID_SOURCE_PAGED) __builtin_amdgcn_s_setprio(1);
             add_values(step);
             scores(step + 1);
             // the order of the phase: operands are asked for twelve reads ahead of the products that take them
@@ -473,6 +473,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             }
             __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - 12) / 3 * 2, 0);
             phase_end(false);
+            if constexpr (SRC == PLAID_SOURCE_PAGED) __builtin_amdgcn_s_setprio(0);
         }
         weights(end - 1);
         phase_end(true);
@@ -484,25 +485,26 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     l = sum_halves(l);
     if (!there) return;
     const int64_t out_row = (tp.begin + token) * a.heads + head;
-    const float natural = SRC == PLAID_SOURCE_BIAS ? m : (m == -INFINITY ? m : m * a.scale);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float2 lse = l == 0.0f ? float2{-INFINITY, 0.0f} : float2{shift, (SRC == PLAID_SOURCE_BIAS ? m : m * a.scale) + logf(l)};
     if (a.splits > 1) {
         const int64_t at = (int64_t)split * a.num_queries * a.heads + out_row;
 #pragma unroll
         for (int dt = 0; dt < DT_TILES; ++dt)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                *(f32x4 *)(a.part_o + at * D + 32 * dt + 8 * i + 4 * h) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-        if (h == 0) a.part_ml[2 * at] = natural, a.part_ml[2 * at + 1] = l;
+                *(f32x4 *)(a.part_o + at * D + 32 * dt + 8 * i + 4 * h) =
+                    f32x4{o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv, o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv};
+        if (h == 0) *(float2 *)(a.part_lse + 2 * at) = lse;
         return;
     }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int dt = 0; dt < DT_TILES; ++dt)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             *(i32x2 *)(a.out + (out_row * D + 32 * dt + 8 * i + 4 * h) * 2) =
                 i32x2{pack2<DT>(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv), pack2<DT>(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv)};
-    if (a.lse && h == 0) a.lse[2 * out_row] = l == 0.0f ? -INFINITY : natural, a.lse[2 * out_row + 1] = l == 0.0f ? 0.0f : logf(l);
+    if (a.lse && h == 0) *(float2 *)(a.lse + 2 * out_row) = lse;
 }
 
 // The splits of a row joined, in their order: a thread takes 4 dimensions.
@@ -515,21 +517,23 @@ __global__ __launch_bounds__(256) void join_splits_kernel(AttendArgs a)
     // a row outside every request has no sums
     const int64_t token = at / a.heads;
     if (token < a.q_offsets[0] || token >= a.q_offsets[a.n]) return;
-    float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + at)]);
-    const float ref = m == -INFINITY ? 0.0f : m;
+    float c = -INFINITY, top = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) c = fmaxf(c, a.part_lse[2 * (s * rows + at)]);
+    const float base = c == -INFINITY ? 0.0f : c;
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_lse[2 * (s * rows + at)] - base + a.part_lse[2 * (s * rows + at) + 1]);
+    const float ref = top == -INFINITY ? 0.0f : top;
     float l = 0.0f;
     f32x4 o{0, 0, 0, 0};
     for (int s = 0; s < a.splits; ++s) {
-        const float w = __builtin_amdgcn_exp2f((a.part_ml[2 * (s * rows + at)] - ref) * LOG2E);
+        const float w = __builtin_amdgcn_exp2f((a.part_lse[2 * (s * rows + at)] - base + a.part_lse[2 * (s * rows + at) + 1] - ref) * LOG2E);
         const f32x4 x = *(const f32x4 *)(a.part_o + (s * rows + at) * D + d);
-        l += w * a.part_ml[2 * (s * rows + at) + 1];
+        l += w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] += w * x[e];
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     *(i32x2 *)(a.out + (at * D + d) * 2) = i32x2{pack2<DT>(o[0] * inv, o[1] * inv), pack2<DT>(o[2] * inv, o[3] * inv)};
-    if (a.lse && d == 0) a.lse[2 * at] = l == 0.0f ? -INFINITY : m, a.lse[2 * at + 1] = l == 0.0f ? 0.0f : logf(l);
+    if (a.lse && d == 0) *(float2 *)(a.lse + 2 * at) = l == 0.0f ? float2{-INFINITY, 0.0f} : float2{c, top + logf(l)};
 }
 
 template <int DT, int D, int NW>

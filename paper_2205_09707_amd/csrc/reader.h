@@ -16,7 +16,7 @@ struct AttendArgs {
     const char *bias;                  // [num_keys] of the type, or null
     const int64_t *q_offsets, *k_offsets;
     char *out;
-    float *lse;                        // pairs whose sum is the logarithm; may be null
+    float *lse;                        // pairs whose sum is the logarithm of the sum of exponentials: a shift, and the rest; may be null
     int64_t num_queries, num_keys;
     int64_t q_token, q_head, k_token, k_head, v_token, v_head;  // strides in bytes
     int32_t n, heads, kv_heads, group;
@@ -30,8 +30,8 @@ struct AttendArgs {
     int32_t max_blocks, block_shift, causal;
     // split over keys: partial sums
     int32_t splits;
-    float *part_o;                     // attend_many: [splits][num_queries][heads][D]; attend_few: [workers][2][kv_heads][16][D]
-    float *part_ml;                    // the same without D, pairs (what the exponentials were taken against, their sum)
+    float *part_o;                     // outputs of parts of the keys. attend_many: [splits][num_queries][heads][D]; attend_few: [workers][2][kv_heads][16][D]
+    float *part_lse;                   // the same without D, pairs as in lse, (-infinity, 0) without a key
 };
 
 struct GradArgs {
@@ -315,6 +315,33 @@ __device__ __forceinline__ void wait_loads()
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// Biases.  Scores s + b are formed as s + (b - c) with a shift c, so that a mask of the type's lowest value, or any other large
+// bias that all of a row's keys have, costs the scores nothing.  c depends on the biases of the keys that are not masked alone:
+// 0 where the largest of them is within BIAS_USUAL, else the largest.  A part of the keys has its own; parts are joined under the
+// largest.  Beside a bias beyond BIAS_ALL a score vanishes, as it does in a sum in 64 bits.
+#define BIAS_USUAL 256.0f
+#define BIAS_ALL 4503599627370496.0f
+struct Shift {
+    float c = 0.0f, most = -INFINITY;  // most: the largest unusual bias
+    bool usual = false;                // whether a usual one was seen
+    // Takes in a wave's biases: lanes that have an unusual one, their largest (looked at where there are any), whether any lane has
+    // a usual one.
+    __device__ __forceinline__ void add(uint64_t unusual, float largest, bool any_usual)
+    {
+        usual = usual || any_usual;
+        if (unusual || c != 0.0f) {
+            if (unusual) {
+#pragma unroll
+                for (int o = 32; o; o >>= 1) largest = fmaxf(largest, __shfl_xor(largest, o));
+                most = fmaxf(most, largest);
+            }
+            c = most > BIAS_USUAL ? most : usual ? 0.0f : most;
+        }
+    }
+};
+__device__ __forceinline__ bool unusual_bias(float b) { return fabsf(b) > BIAS_USUAL && b != -INFINITY; }
+__device__ __forceinline__ float beside_shift(float scale, float c) { return fabsf(c) > BIAS_ALL ? 0.0f : scale; }
+
 // Where keys that are masked are loaded from: an infinity in what they hold would make a product with a weight of zero not a number.
 static __device__ const i32x4 zero_row[16] = {};
 

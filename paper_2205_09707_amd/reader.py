@@ -64,7 +64,7 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
     """The tensor itself where the kernels can read its strides, else a contiguous copy."""
     _, heads, dim = t.shape
     s = t.stride()
-    if t.numel() and (s[2] != 1 or t.data_ptr() % 16 or (s[0] % 8 and t.shape[0] > 1) or (s[1] % 8 and heads > 1)):
+    if t.numel() and (s[2] != 1 or t.data_ptr() % 16 or (t.shape[0] > 1 and (s[0] % 8 or s[0] >= 1 << 24)) or (heads > 1 and (s[1] % 8 or s[1] >= 1 << 24))):
         t = t.contiguous() if not t.is_contiguous() else t.clone(memory_format=torch.contiguous_format)
     return t
 
