@@ -212,8 +212,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
         if (!second) load(begin);
         load_row(begin + 1);
         if (!second) load(begin + 1);
-        if (second) wait_loads<1>();
-        else wait_loads<STEP>();
+        wait_all_loads();  // the keys or values too
         lds_barrier();
         if (second) lds_barrier();
         form(begin);
@@ -415,7 +414,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
             }
             if (!late) load(begin + i);
         }
-        if (!late) wait_loads<2 * N *(L::AHEAD - 1)>();
+        wait_all_loads();  // the rows too
         lds_barrier();
         if (late) lds_barrier();
         form(begin);

@@ -24,7 +24,6 @@ struct TileBuffers {
     char k[TILES][MANY_KEYS * D * 2];
     char v[TILES][SRC == PLAID_SOURCE_PAGED ? D * (MANY_KEYS + 4) * 2 : MANY_KEYS * D * 2];
     float bias[SRC == PLAID_SOURCE_BIAS ? NW : 1][4][SRC == PLAID_SOURCE_BIAS ? MANY_KEYS : 4];  // each wave's own
-    float shift[SRC == PLAID_SOURCE_BIAS ? NW : 1][4];        // what is subtracted from them
     uint32_t raw[SRC == PLAID_SOURCE_BIAS ? NW : 1][4][64];  // biases as they are loaded
     int cell[4][4];  // paged: whether the cells of 16 keys have a block
 };
@@ -77,6 +76,7 @@ struct Stage {
     // before they are used.
     uint32_t raw;
     Shift shift;
+    float shifts[Ahead<NW, SRC>::K];  // what was subtracted in the tile whose weights are next, and those after it
     __device__ __forceinline__ void read_bias(const TileBuffers<D, NW, SRC> &b, int tile) { raw = b.raw[threadIdx.x >> 6][tile & 3][threadIdx.x & 63]; }
     __device__ __forceinline__ void store_bias(const KeyRange &kr, int end, TileBuffers<D, NW, SRC> &b, int tile)
     {
@@ -88,7 +88,9 @@ struct Stage {
         const uint64_t unusual = __ballot(unusual_bias(f));
         shift.add(unusual, unusual_bias(f) ? f : -INFINITY, ~(k_masked | unusual) != 0);
         b.bias[threadIdx.x >> 6][tile & 3][lane] = f - shift.c;
-        if (lane == 0) b.shift[threadIdx.x >> 6][tile & 3] = shift.c;
+#pragma unroll
+        for (int i = 0; i + 1 < Ahead<NW, SRC>::K; ++i) shifts[i] = shifts[i + 1];
+        shifts[Ahead<NW, SRC>::K - 1] = __int_as_float(uniform(__float_as_int(shift.c)));
     }
     // Before the first phase: asks for the first tiles and waits for the first one's keys.
     __device__ __forceinline__ void start(const AttendArgs &a, const KeyRange &kr, int begin, int end, TileBuffers<D, NW, SRC> &b)
@@ -109,7 +111,7 @@ struct Stage {
             load_k(a, kr, begin + i, end, b);
             if (i > 0) load_v(a, kr, begin + i - 1, end, b);
         }
-        wait_loads<2 * N *(A::K - 1)>();
+        wait_all_loads();  // the queries too
         lds_barrier();
     }
     // In the second phase of a step, before and after its weights.
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = zero16();
     // with a bias the scores are kept as they are, else as q . k: one multiply-add then makes the exponent
     const float cs = SRC == PLAID_SOURCE_BIAS ? LOG2E : a.scale * LOG2E;
-    float m = -INFINITY, l = 0.0f, shift = 0.0f;
+    float m = -INFINITY, l = 0.0f, shift = 0.0f, scale = a.scale;
 
     // Two groups of waves, one of each on every SIMD, half a step apart: while one multiplies, the other forms exponentials.
     // A step of a group is a phase of products (o += v^T p^T of the former tile, s of this one) and one of everything else, with
@@ -398,9 +400,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
                         if (lds.bias[wave][step & 3][32 * mt + 8 * (i >> 2) + 4 * h + (i & 3)] == -INFINITY) s[mt][i] = 0.0f;
             }
             top = -INFINITY;
-            const float c = lds.shift[wave][step & 3], scale = beside_shift(a.scale, c);
-            m += shift - c;  // m is relative to the shift
-            shift = c;
+            if (stage.shifts[0] != shift) {  // m is relative to the shift
+                m += shift - stage.shifts[0];
+                shift = stage.shifts[0];
+                scale = beside_shift(a.scale, shift);
+            }
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt) {
                 f32x4 b[4];

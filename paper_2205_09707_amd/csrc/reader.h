@@ -342,6 +342,9 @@ struct Shift {
 __device__ __forceinline__ bool unusual_bias(float b) { return fabsf(b) > BIAS_USUAL && b != -INFINITY; }
 __device__ __forceinline__ float beside_shift(float scale, float c) { return fabsf(c) > BIAS_ALL ? 0.0f : scale; }
 
+// Waits for all of the wave's loads, and lets the compiler know: one that it is unsure of it would wait for in every round of a loop.
+__device__ __forceinline__ void wait_all_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 // Where keys that are masked are loaded from: an infinity in what they hold would make a product with a weight of zero not a number.
 static __device__ const i32x4 zero_row[16] = {};
 
