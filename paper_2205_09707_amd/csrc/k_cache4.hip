@@ -112,37 +112,93 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs c)
     }
 }
 
-template <int DT, int D>
+// Value codes are read four tokens at a time where neighbours in the list are neighbours in a quad of the cache (the list's
+// alignment is taken from the first token's slot): a lane gets 4 tokens x 8 dimensions and their 16 other halves from 8 words.
+// Byte by byte, the same takes eight times the loads (100 us in place of 76 for 65003 tokens of 8 heads).
+template <int DT, int D, int TOKENS>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs c)
 {
-    constexpr int LANES = D / 8, TOKENS = 256 / LANES, G = D / 32;
-    const int tok = threadIdx.x / LANES, l = threadIdx.x % LANES, head = blockIdx.y;
-    const int64_t t = (int64_t)blockIdx.x * TOKENS + tok, bs = 1ll << c.block_shift, region = bs * D * 17 / 16;
-    if (t >= c.n) return;
-    const int64_t slot = c.slots[t], to = ((t * c.kv_heads + head) * D + l * 8) * 2;
-    i32x4 k{0, 0, 0, 0}, v{0, 0, 0, 0};
-    if ((uint64_t)slot < (uint64_t)(c.num_blocks << c.block_shift)) {
-        const int in = (int)(slot & (bs - 1));
-        const uint8_t *p = c.data + ((slot >> c.block_shift) * c.kv_heads + head) * region;
-        if (c.k_out) {
-            const int w = *(const int *)(p + in * (D / 2) + l * 4);
-            const float power = scale_power(p[bs * D + in * G + l / 4], 0);
-            k = i32x4{codes2<DT, 0>(w, power), codes2<DT, 1>(w, power), codes2<DT, 2>(w, power), codes2<DT, 3>(w, power)};
-        }
-        if (c.v_out) {
-            // dims 32 i + 8 (l % 4) .. + 7: m = 8 (l % 2) .. and the half that l / 2 % 2 names
-            const uint8_t *q = p + bs * (D / 2) + (in >> 4) * (8 * D) + (((in >> 2) & 3) * 16 + 8 * (l & 1)) * (D / 8) + (l >> 2) * 4 + (in & 3);
-            const float power = scale_power(p[bs * D + bs * G + in * G + l / 4], 0);
-            const int half = ((l >> 1) & 1) * 4;
+    constexpr int LANES = D / 8, G = D / 32;
+    __shared__ int64_t s_slot[TOKENS + 8];
+    __shared__ uint8_t s_done[TOKENS];
+    const int head = blockIdx.y;
+    const int64_t t0 = (int64_t)blockIdx.x * TOKENS, bs = 1ll << c.block_shift, region = bs * D * 17 / 16;
+    const int count = (int)min((int64_t)TOKENS, c.n - t0);
+    for (int i = threadIdx.x; i < TOKENS + 8; i += 256) {
+        int64_t slot = i < count ? c.slots[t0 + i] : -1;
+        if ((uint64_t)slot >= (uint64_t)(c.num_blocks << c.block_shift)) slot = -1;
+        s_slot[i] = slot;
+        if (i < TOKENS) s_done[i] = 0;
+    }
+    __syncthreads();
+    auto cell_of = [&](int64_t slot) { return c.data + ((slot >> c.block_shift) * c.kv_heads + head) * region; };
+    auto out_of = [&](char *out, int tok) { return out + ((t0 + tok) * c.kv_heads + head) * (D * 2); };
+    if (c.v_out) {
+        const int lead = (int)(-s_slot[0] & 3);
+        for (int u = threadIdx.x; u < TOKENS / 4 * G * 2; u += 256) {
+            const int quad = u / (G * 2), l = u % (G * 2), i = l >> 1, m = (l & 1) * 8, tok = lead + 4 * quad;
+            const int64_t s = s_slot[tok];
+            if (s < 0 || (s & 3) || s_slot[tok + 1] != s + 1 || s_slot[tok + 2] != s + 2 || s_slot[tok + 3] != s + 3) continue;
+            if (l == 0) s_done[tok] = s_done[tok + 1] = s_done[tok + 2] = s_done[tok + 3] = 1;
+            const int in = (int)(s & (bs - 1));
+            const uint8_t *p = cell_of(s) + bs * (D / 2) + (in >> 4) * (8 * D) + (((in >> 2) & 3) * 16 + m) * (D / 8) + i * 4;
+            const uint8_t *scales = cell_of(s) + bs * D + bs * G + in * G + i;
+            int w[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int w = ((q[2 * j * (D / 8)] >> half) & 15) | (((q[(2 * j + 1) * (D / 8)] >> half) & 15) << 4);
-                v[j] = codes2<DT, 0>(w, power);
+            for (int j = 0; j < 8; ++j) w[j] = *(const int *)(p + j * (D / 8));
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const float power = scale_power(scales[t * G], 0);
+                i32x4 lo, hi;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int x = t == 0   ? codes2<DT, 0>(w[2 * j], power)
+                                  : t == 1 ? codes2<DT, 1>(w[2 * j], power)
+                                  : t == 2 ? codes2<DT, 2>(w[2 * j], power)
+                                           : codes2<DT, 3>(w[2 * j], power);
+                    const int y = t == 0   ? codes2<DT, 0>(w[2 * j + 1], power)
+                                  : t == 1 ? codes2<DT, 1>(w[2 * j + 1], power)
+                                  : t == 2 ? codes2<DT, 2>(w[2 * j + 1], power)
+                                           : codes2<DT, 3>(w[2 * j + 1], power);
+                    lo[j] = (int)__builtin_amdgcn_perm(y, x, 0x05040100), hi[j] = (int)__builtin_amdgcn_perm(y, x, 0x07060302);
+                }
+                char *to = out_of(c.v_out, tok + t) + (32 * i + m) * 2;
+                *(i32x4 *)to = lo;
+                *(i32x4 *)(to + 32) = hi;
             }
         }
+        __syncthreads();
     }
-    if (c.k_out) *(i32x4 *)(c.k_out + to) = k;
-    if (c.v_out) *(i32x4 *)(c.v_out + to) = v;
+    for (int u = threadIdx.x; u < count * LANES; u += 256) {
+        const int tok = u / LANES, l = u % LANES;
+        const int64_t slot = s_slot[tok];
+        const int in = (int)(slot & (bs - 1));
+        const uint8_t *p = cell_of(slot);
+        if (c.k_out) {
+            i32x4 k{0, 0, 0, 0};
+            if (slot >= 0) {
+                const int w = *(const int *)(p + in * (D / 2) + l * 4);
+                const float power = scale_power(p[bs * D + in * G + l / 4], 0);
+                k = i32x4{codes2<DT, 0>(w, power), codes2<DT, 1>(w, power), codes2<DT, 2>(w, power), codes2<DT, 3>(w, power)};
+            }
+            *(i32x4 *)(out_of(c.k_out, tok) + l * 16) = k;
+        }
+        if (c.v_out && !s_done[tok]) {
+            i32x4 v{0, 0, 0, 0};
+            if (slot >= 0) {
+                // dims 32 i + 8 (l % 4) .. + 7: m = 8 (l % 2) .. and the half that l / 2 % 2 names
+                const uint8_t *q = p + bs * (D / 2) + (in >> 4) * (8 * D) + (((in >> 2) & 3) * 16 + 8 * (l & 1)) * (D / 8) + (l >> 2) * 4 + (in & 3);
+                const float power = scale_power(p[bs * D + bs * G + in * G + l / 4], 0);
+                const int half = ((l >> 1) & 1) * 4;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int w = ((q[2 * j * (D / 8)] >> half) & 15) | (((q[(2 * j + 1) * (D / 8)] >> half) & 15) << 4);
+                    v[j] = codes2<DT, 0>(w, power);
+                }
+            }
+            *(i32x4 *)(out_of(c.v_out, tok) + l * 16) = v;
+        }
+    }
 }
 
 static CacheArgs cache_args(const plaid_paged_cache &c, const int64_t *slots, int64_t n)
@@ -171,17 +227,22 @@ void plaid_launch_cache_write(hipStream_t st, const plaid_paged_cache &c, const 
         else cache_write_kernel<PLAID_FP16, 64><<<grid, block, 0, st>>>(a);
     }
 }
+template <int DT, int D>
+static void launch_read(hipStream_t st, const CacheArgs &a)
+{
+    // 64 tokens fill a workgroup's lanes with quads; where that leaves most of the chip idle, 16 (256 tokens of 8 heads: 3.4 us in place of 6.4)
+    if (a.n * a.kv_heads >= 64 * 1024) cache_read_kernel<DT, D, 64><<<dim3((unsigned)((a.n + 63) / 64), (unsigned)a.kv_heads), dim3(256), 0, st>>>(a);
+    else cache_read_kernel<DT, D, 16><<<dim3((unsigned)((a.n + 15) / 16), (unsigned)a.kv_heads), dim3(256), 0, st>>>(a);
+}
 void plaid_launch_cache_read(hipStream_t st, const plaid_paged_cache &c, const int64_t *slots, int64_t n, char *k, char *v)
 {
     CacheArgs a = cache_args(c, slots, n);
     a.k_out = k, a.v_out = v;
-    const int tokens = c.head_dim == 128 ? 16 : 32;
-    const dim3 grid((unsigned)((n + tokens - 1) / tokens), (unsigned)c.kv_heads), block(256);
     if (c.dtype == PLAID_BF16) {
-        if (c.head_dim == 128) cache_read_kernel<PLAID_BF16, 128><<<grid, block, 0, st>>>(a);
-        else cache_read_kernel<PLAID_BF16, 64><<<grid, block, 0, st>>>(a);
+        if (c.head_dim == 128) launch_read<PLAID_BF16, 128>(st, a);
+        else launch_read<PLAID_BF16, 64>(st, a);
     } else {
-        if (c.head_dim == 128) cache_read_kernel<PLAID_FP16, 128><<<grid, block, 0, st>>>(a);
-        else cache_read_kernel<PLAID_FP16, 64><<<grid, block, 0, st>>>(a);
+        if (c.head_dim == 128) launch_read<PLAID_FP16, 128>(st, a);
+        else launch_read<PLAID_FP16, 64>(st, a);
     }
 }

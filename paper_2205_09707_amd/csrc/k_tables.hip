@@ -61,10 +61,11 @@ __device__ __forceinline__ void scan_requests(const TablesArgs &t, int64_t *toke
     if (threadIdx.x == 0) tokens[t.n] = done[0], blocks[t.n] = done[1];
 }
 
-// The last request whose sum is <= x (sums ascend from 0, x < sums[n]).
-__device__ __forceinline__ int owner(const int64_t *sums, int n, int64_t x)
+// The last request whose sum is <= x (sums ascend from 0, x < sums[n]), from request `from` on, where it usually is.
+__device__ __forceinline__ int owner(const int64_t *sums, int n, int64_t x, int from = 0)
 {
-    int lo = 0, hi = n;
+    if (x < sums[from + 1]) return from;
+    int lo = from, hi = n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (sums[mid] <= x) lo = mid;
@@ -86,10 +87,14 @@ __device__ __forceinline__ void fill(const TablesArgs &t, const int64_t *tokens,
         t.table[r * t.table_stride + growth(t, r).have + j - blocks[r]] = j < t.n_free ? t.free_blocks[j] : -1;
     }
     const int64_t all = min(tokens[t.n], t.capacity);
-    for (int64_t i = first * TABLES_TOKENS; i < t.capacity; i += stride * TABLES_TOKENS) {
+    // a workgroup's tokens are neighbours, so that a thread's request mostly stays
+    constexpr int64_t SWEEP = TABLES_THREADS * TABLES_TOKENS;
+    const int64_t per = (t.capacity + SWEEP * gridDim.x - 1) / (SWEEP * gridDim.x) * SWEEP, from = blockIdx.x * per;
+    int r = 0;
+    for (int64_t i = from + threadIdx.x * TABLES_TOKENS; i < min(t.capacity, from + per); i += SWEEP) {
         int position[TABLES_TOKENS];
         int64_t slot[TABLES_TOKENS];
-        int r = i < all ? owner(tokens, t.n, i) : 0;
+        if (i < all) r = owner(tokens, t.n, i, r);
         Growth g = growth(t, r);
         int64_t block = -1, id = -1;
 #pragma unroll
