@@ -10,7 +10,8 @@
 // lie as the operand wants them; dense values go through the wave's own LDS and the transposing read.
 //
 // All tiles' steps, request after request, form one line that the workers (workgroups of a key head) share evenly, however
-// uneven the requests are.  A worker's stretch is a tail of a tile, whole tiles and a head of one: whole tiles it finishes,
+// uneven the requests are.  (Where no request has many keys a workgroup of twice the waves takes a tile, and there is nothing to
+// join: one launch in place of two.)  A worker's stretch is a tail of a tile, whole tiles and a head of one: whole tiles it finishes,
 // the two others leave their sums in its two places, and join_workers_kernel adds them up in the order of the line.
 
 template <int SRC>
@@ -152,8 +153,14 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
     __shared__ __align__(16) FewLds<D, NW, SRC> lds;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), kg = lane >> 4, m16 = lane & 15;
     const int head_kv = blockIdx.x % a.kv_heads, worker = blockIdx.x / a.kv_heads;
-    int at, end, first;
-    int r = find_work<SRC, NW>(a, workers, worker, at, end, first);
+    int at, end, first, r;
+    if (workers) {
+        r = find_work<SRC, NW>(a, workers, worker, at, end, first);
+    } else {  // a workgroup for each tile
+        const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, 4, worker);
+        r = tp.r;
+        if (r >= 0) first = 0, at = tp.tile * uniform_request<SRC, NW>(a, r).steps, end = at + 1;
+    }
     if (r < 0) return;
     const float cs = BIAS ? LOG2E : a.scale * LOG2E;
 
@@ -164,7 +171,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
             rq = uniform_request<SRC, NW>(a, ++r);
         }
         const int tile = (int)((uint32_t)(at - first) / (uint32_t)rq.steps), begin = at - first - tile * rq.steps;
-        const int stop = min(rq.steps, begin + (end - at));
+        const int stop = workers ? min(rq.steps, begin + (end - at)) : rq.steps;
         const int rows = rq.tokens * a.group, row = tile * FEW_ROWS + m16;
         const bool there = row < rows;
         const int token = row_token(a, there ? row : 0), head = head_kv * a.group + (there ? row : 0) - token * a.group;
@@ -552,6 +559,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_workers_kernel(AttendArgs a
 template <int DT, int D, int SRC>
 static void launch(hipStream_t st, const AttendArgs &a, int workers, int64_t tiles)
 {
+    if (!workers) {
+        attend_few_kernel<DT, D, 8, SRC><<<dim3((unsigned)(tiles * a.kv_heads)), dim3(512), 0, st>>>(a, 0);
+        return;
+    }
     attend_few_kernel<DT, D, 4, SRC><<<dim3((unsigned)(workers * a.kv_heads)), dim3(256), 0, st>>>(a, workers);
     if (workers > 1) join_workers_kernel<DT, D, 4, SRC><<<dim3((unsigned)tiles, (unsigned)a.kv_heads), dim3(JOIN_THREADS), 0, st>>>(a, workers);
 }

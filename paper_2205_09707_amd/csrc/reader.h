@@ -57,7 +57,7 @@ struct GradArgs {
 // Keys of a tile of attend_many.
 #define MANY_KEYS 64
 
-// Launchers.  workers: workgroups of attend_few per key head.
+// Launchers.  workers: workgroups of attend_few per key head, 0: one for each tile.
 void plaid_launch_attend_few(hipStream_t st, const AttendArgs &a, int dtype, int head_dim, int source, int workers, int64_t tiles);
 void plaid_launch_attend_many(hipStream_t st, const AttendArgs &a, int dtype, int head_dim, int source, int waves, int64_t tiles);
 void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_waves, int q_splits, int k_waves,

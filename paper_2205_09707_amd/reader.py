@@ -74,6 +74,10 @@ def _strides(t: torch.Tensor) -> Tuple[int, int]:
     return (t.stride(0) if n > 1 else heads * dim), (t.stride(1) if heads > 1 else dim)
 
 
+def _like(t: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _workspace(bytes_: int, device: torch.device):
     """(tensor that the caller holds until its launches are made, its address)"""
     if bytes_ == 0:
@@ -214,7 +218,7 @@ def plaid_cached_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tens
     if table.shape[1] > 1 and table.stride(1) != 1:
         table = table.contiguous()
     q = _rows(q)
-    out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    out = _like(q)
     lse = torch.empty(q.shape[:2] + (2,), dtype=torch.float32, device=dev) if return_lse else None
     lib = _p.load_library()
     a = _attention(q, None, None, None, q_offsets, None, cache.kv_heads, scale, out, lse)
@@ -250,7 +254,7 @@ def plaid_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_o
     with return_lse also the two numbers a row that plaid_cross_attention_backward wants."""
     q, k, v, q_offsets, k_offsets, key_bias = _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias)
     dev = q.device
-    out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    out = _like(q)
     lse = torch.empty(q.shape[:2] + (2,), dtype=torch.float32, device=dev) if return_lse else None
     lib = _p.load_library()
     a = _attention(q, k, v, key_bias, q_offsets, k_offsets, k.shape[1], scale, out, lse)
@@ -276,9 +280,9 @@ def plaid_cross_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torc
         raise ValueError("lse must be what plaid_cross_attention returned")
     whole = lambda t: t if t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)  # noqa: E731
     d_out, out, lse = whole(d_out), whole(out), whole(lse)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    dk = torch.empty(k.shape, dtype=q.dtype, device=dev)
-    dv = torch.empty(k.shape, dtype=q.dtype, device=dev)
+    dq = _like(q)
+    dk = _like(k)
+    dv = _like(k)
     dbias = torch.empty(k.shape[:1], dtype=q.dtype, device=dev) if key_bias is not None else None
     lib = _p.load_library()
     a = _attention(q, k, v, key_bias, q_offsets, k_offsets, k.shape[1], scale, out, lse)
