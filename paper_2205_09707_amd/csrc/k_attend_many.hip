@@ -78,7 +78,7 @@ struct Stage {
     Shift shift;
     float shifts[Ahead<NW, SRC>::K];  // what was subtracted in the tile whose weights are next, and those after it
     __device__ __forceinline__ void read_bias(const TileBuffers<D, NW, SRC> &b, int tile) { raw = b.raw[threadIdx.x >> 6][tile & 3][threadIdx.x & 63]; }
-    __device__ __forceinline__ void store_bias(const KeyRange &kr, int end, TileBuffers<D, NW, SRC> &b, int tile)
+    __device__ __forceinline__ void store_bias(const AttendArgs &a, const KeyRange &kr, int end, TileBuffers<D, NW, SRC> &b, int tile)
     {
         const int lane = threadIdx.x & 63;
         const uint16_t x = min(tile, end - 1) * MANY_KEYS + lane < kr.len ? (uint16_t)raw : NONE;
@@ -87,7 +87,7 @@ struct Stage {
         k_masked = __ballot(x == NONE);
         const uint64_t unusual = __ballot(unusual_bias(f));
         shift.add(unusual, unusual_bias(f) ? f : -INFINITY, ~(k_masked | unusual) != 0);
-        b.bias[threadIdx.x >> 6][tile & 3][lane] = f - shift.c;
+        b.bias[threadIdx.x >> 6][tile & 3][lane] = (f - shift.c) * a.inv_scale;
 #pragma unroll
         for (int i = 0; i + 1 < Ahead<NW, SRC>::K; ++i) shifts[i] = shifts[i + 1];
         shifts[Ahead<NW, SRC>::K - 1] = __int_as_float(uniform(__float_as_int(shift.c)));
@@ -106,7 +106,7 @@ struct Stage {
         for (int i = 0; i < A::K; ++i) {
             if constexpr (BIAS) {
                 read_bias(b, begin + i);
-                store_bias(kr, end, b, begin + i);
+                store_bias(a, kr, end, b, begin + i);
             }
             load_k(a, kr, begin + i, end, b);
             if (i > 0) load_v(a, kr, begin + i - 1, end, b);
@@ -126,7 +126,7 @@ struct Stage {
     {
         using A = Ahead<NW, SRC>;
         if constexpr (BIAS) {
-            store_bias(kr, end, b, step + A::K);
+            store_bias(a, kr, end, b, step + A::K);
             load_bias(a, kr, step + A::K + 1, end, b);
         }
         load_k(a, kr, step + A::K, end, b);
@@ -352,9 +352,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     f32x16 o[DT_TILES];
 #pragma unroll
     for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = zero16();
-    // with a bias the scores are kept as they are, else as q . k: one multiply-add then makes the exponent
-    const float cs = SRC == PLAID_SOURCE_BIAS ? LOG2E : a.scale * LOG2E;
-    float m = -INFINITY, l = 0.0f, shift = 0.0f, scale = a.scale;
+    // scores are kept as q . k + b / scale: one multiply-add then makes the exponent
+    const float cs = a.scale * LOG2E;
+    float m = -INFINITY, l = 0.0f, shift = 0.0f;
+    bool beside = false;  // the shift leaves the scores nothing
 
     // Two groups of waves, one of each on every SIMD, half a step apart: while one multiplies, the other forms exponentials.
     // A step of a group is a phase of products (o += v^T p^T of the former tile, s of this one) and one of everything else, with
@@ -376,7 +377,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     auto scores = [&](int step) {
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
-            s[mt] = zero16();
+            if constexpr (SRC == PLAID_SOURCE_BIAS) {  // what the products are added to
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 b = *(const f32x4 *)&lds.bias[wave][step & 3][32 * mt + 8 * i + 4 * h];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[mt][4 * i + e] = b[e];
+                }
+            } else {
+                s[mt] = zero16();
+            }
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) s[mt] = mfma32<DT>(lds_rows<D>(lds.k[step % A::TILES], 32 * mt, d), q[d], s[mt]);
         }
@@ -392,29 +402,19 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         else stage.before(step, lds);
         float top;
         if constexpr (SRC == PLAID_SOURCE_BIAS) {
-            if (odd) {
+            if (stage.shifts[0] != shift) {  // m is relative to the shift
+                m += (shift - stage.shifts[0]) * a.inv_scale;
+                shift = stage.shifts[0];
+                beside = beside_shift(1.0f, shift) == 0.0f;
+            }
+            if (odd || beside) {
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (lds.bias[wave][step & 3][32 * mt + 8 * (i >> 2) + 4 * h + (i & 3)] == -INFINITY) s[mt][i] = 0.0f;
-            }
-            top = -INFINITY;
-            if (stage.shifts[0] != shift) {  // m is relative to the shift
-                m += shift - stage.shifts[0];
-                shift = stage.shifts[0];
-                scale = beside_shift(a.scale, shift);
-            }
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
-                f32x4 b[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) b[i] = *(const f32x4 *)&lds.bias[wave][step & 3][32 * mt + 8 * i + 4 * h];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[mt][i] = fmaf(s[mt][i], scale, b[i >> 2][i & 3]);
-                    top = fmaxf(top, s[mt][i]);
-                }
+                    for (int i = 0; i < 16; ++i) {
+                        const float b = lds.bias[wave][step & 3][32 * mt + 8 * (i >> 2) + 4 * h + (i & 3)];
+                        if (beside || b == -INFINITY) s[mt][i] = b;
+                    }
             }
         } else {
             bool whole = (step + 1) * MANY_KEYS <= least;
@@ -430,10 +430,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
                         s[mt][i] = seen ? s[mt][i] : -INFINITY;
                     }
             }
-            top = larger(s[0][0], s[1][0]);
-#pragma unroll
-            for (int i = 1; i < 16; ++i) top = larger(larger(top, s[0][i]), s[1][i]);
         }
+        top = larger(s[0][0], s[1][0]);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = larger(larger(top, s[0][i]), s[1][i]);
         top = max_halves(top);
         if (__any(!((top - m) * cs <= 8.0f))) {  // also where there was no key so far
             const float next = fmaxf(m, top);
@@ -468,14 +468,15 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             add_values(step);
             scores(step + 1);
             // the order of the phase: operands are asked for twelve reads ahead of the products that take them
-            constexpr int READS = D / 32 * 4 * 2 + D / 16 * 2, PRODUCTS = D / 32 * 4 + D / 16 * 2;  // 3 reads to 2 products
-            __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
+            constexpr int BIASES = SRC == PLAID_SOURCE_BIAS ? 8 : 0, FIRST = SRC == PLAID_SOURCE_BIAS ? 14 : 12;
+            constexpr int READS = D / 32 * 4 * 2 + D / 16 * 2 + BIASES, PRODUCTS = D / 32 * 4 + D / 16 * 2;  // 3 reads to 2 products
+            __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
 #pragma unroll
-            for (int i = 0; i < (READS - 12) / 3; ++i) {
+            for (int i = 0; i < (READS - FIRST) / 3; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
                 __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
             }
-            __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - 12) / 3 * 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - FIRST) / 3 * 2, 0);
             phase_end(false);
             if constexpr (SRC == PLAID_SOURCE_PAGED) __builtin_amdgcn_s_setprio(0);
         }
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     if (!there) return;
     const int64_t out_row = (tp.begin + token) * a.heads + head;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const float2 lse = l == 0.0f ? float2{-INFINITY, 0.0f} : float2{shift, (SRC == PLAID_SOURCE_BIAS ? m : m * a.scale) + logf(l)};
+    const float2 lse = l == 0.0f ? float2{-INFINITY, 0.0f} : float2{shift, m * a.scale + logf(l)};
     if (a.splits > 1) {
         const int64_t at = (int64_t)split * a.num_queries * a.heads + out_row;
 #pragma unroll

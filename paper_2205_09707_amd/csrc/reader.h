@@ -21,7 +21,7 @@ struct AttendArgs {
     int64_t q_token, q_head, k_token, k_head, v_token, v_head;  // strides in bytes
     int32_t n, heads, kv_heads, group;
     uint32_t group_magic;              // ceil(2^32 / group): row / group = umulhi(row, magic) for group > 1
-    float scale;                       // >= 0: negate_q carries the sign
+    float scale, inv_scale;            // forward: > 0 (negate_q carries the sign) and its reciprocal
     uint32_t negate_q;                 // 0x80008000 where the caller's scale is negative, else 0
     // paged source
     const uint8_t *cache;

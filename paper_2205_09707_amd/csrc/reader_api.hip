@@ -175,8 +175,9 @@ int run_forward(const plaid_attention &a, AttendArgs &x, const Plan &p, int sour
     if (!guard.ok) return plaid_fail(PLAID_EHIP, "device %d cannot be used", device);
     // the running maximum is that of q . k, so the factor is made positive and q carries its sign
     if (!(a.scale >= 0.0f)) x.negate_q = 0x80008000u, x.scale = -a.scale;
-    // a factor of 0 would meet the infinities of keys that are hidden; beside this one every finite score is nothing as well
-    if (x.scale == 0.0f && source != PLAID_SOURCE_BIAS) x.scale = 1e-30f;
+    // a factor of 0 would meet the infinities of keys that are hidden; beside this one every score that is not huge is nothing as well
+    if (x.scale < 1e-30f) x.scale = 1e-30f;
+    x.inv_scale = 1.0f / x.scale;
     x.part_o = (float *)workspace;
     x.part_lse = (float *)((char *)workspace + p.o_bytes);
     if (p.few) {
