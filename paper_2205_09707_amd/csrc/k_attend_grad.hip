@@ -70,9 +70,11 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     __shared__ __align__(16) GradKLds<D, NW> lds;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
     const int second = wave >= K::PAIRS, pair = second ? wave - K::PAIRS : wave;
-    const WorkPlace w = work_place(a, tiles);
+    const WorkPlace w = work_place(a, tiles, splits);
     const int head = w.head, split = w.split;
-    const TilePlace tp = find_tile(a.k_offsets, a.n, a.num_keys, 1, K::SHIFT, w.place);
+    const int of = min(lane, a.n - 1);
+    const TilePlace tp = a.n <= SORTED_REQUESTS ? find_sorted_tile(a.k_offsets, a.n, a.num_keys, 1, K::SHIFT, w.place, (int)(a.q_offsets[of + 1] - a.q_offsets[of]))
+                                                : find_tile(a.k_offsets, a.n, a.num_keys, 1, K::SHIFT, w.place);
     if (tp.r < 0) return;
     const int len = (int)(tp.end - tp.begin);
     const int64_t row0 = clamp64(uniform_load(a.q_offsets + tp.r), 0, a.num_queries);
@@ -284,9 +286,11 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
     const AttendArgs &a = g.a;
     __shared__ __align__(16) L lds;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5, late = wave >= 4;
-    const WorkPlace w = work_place(a, tiles);
+    const WorkPlace w = work_place(a, tiles, splits);
     const int head_kv = w.head, split = w.split;
-    const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place);
+    const int of = min(lane, a.n - 1);
+    const TilePlace tp = a.n <= SORTED_REQUESTS ? find_sorted_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place, (int)(a.k_offsets[of + 1] - a.k_offsets[of]))
+                                                : find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place);
     if (tp.r < 0) return;
     const int tokens = (int)(tp.end - tp.begin), rows = tokens * a.group;
     const int64_t key0 = clamp64(uniform_load(a.k_offsets + tp.r), 0, a.num_keys);

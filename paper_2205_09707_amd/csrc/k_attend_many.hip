@@ -289,11 +289,18 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     constexpr int ROWS = NW * 32, SHIFT = NW == 8 ? 8 : 7, DT_TILES = D / 32;
     __shared__ __align__(16) TileBuffers<D, NW, SRC> lds;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
-    const WorkPlace w = work_place(a, tiles);
+    const WorkPlace w = work_place(a, tiles, a.splits);
     KeyRange kr;
     kr.head = w.head;
     const int split = w.split;
-    const TilePlace tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place);
+    TilePlace tp;
+    if (a.n <= SORTED_REQUESTS) {
+        const int of = min(lane, a.n - 1);
+        const int keys = SRC == PLAID_SOURCE_PAGED ? a.lengths[of] : (int)(a.k_offsets[of + 1] - a.k_offsets[of]);
+        tp = find_sorted_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place, keys);
+    } else {
+        tp = find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place);
+    }
     if (tp.r < 0) return;
     kr.r = tp.r;
 

@@ -239,6 +239,31 @@ __device__ __forceinline__ TilePlace find_tile(const int64_t *off, int n, int64_
     return t;
 }
 
+// The same with the requests in the order of `work`, what a tile of request r (of lane r) takes, the largest first, and a request's
+// last tile, which sees the most of a causal mask, first: what starts last is short, so that all of the chip ends at about the same time.
+// Only for n <= 64: with more requests there are so many tiles that their order matters little.
+#define SORTED_REQUESTS 64
+__device__ __forceinline__ TilePlace find_sorted_tile(const int64_t *off, int n, int64_t rows, int per_token, int tile_shift, int64_t p, int work)
+{
+    const int lane = threadIdx.x & 63, of = min(lane, n - 1);
+    const int64_t begin = clamp64(off[of], 0, rows), end = clamp64(off[of + 1], begin, rows);
+    const int tiles = lane < n ? (int)(((end - begin) * per_token + (1ll << tile_shift) - 1) >> tile_shift) : 0;
+    int64_t first = 0;
+    for (int j = 0; j < n; ++j) {
+        const int other = __builtin_amdgcn_readlane(work, j);
+        if (other > work || (other == work && j < lane)) first += __builtin_amdgcn_readlane(tiles, j);
+    }
+    const uint64_t mine = __ballot(first <= p && p < first + tiles);
+    TilePlace t = {-1, 0, 0, 0};
+    if (mine) {
+        t.r = uniform((int)__ffsll((unsigned long long)mine) - 1);
+        t.begin = clamp64(uniform_load(off + t.r), 0, rows);
+        t.end = clamp64(uniform_load(off + t.r + 1), t.begin, rows);
+        t.tile = __builtin_amdgcn_readlane((int)(first + tiles - 1 - p), t.r);
+    }
+    return t;
+}
+
 // What a workgroup of a grid of tiles x key heads x splits does.  Workgroups go to the eight XCDs in turn.  With an even number of
 // key heads the heads come first: the tiles of one head, which share what they read, then meet on as many XCDs as eight has more
 // factors of two than the number of heads, and every XCD gets the same mixture of long and short requests.  With an odd number
@@ -247,7 +272,7 @@ struct WorkPlace {
     int64_t place;
     int head, split;
 };
-__device__ __forceinline__ WorkPlace work_place(const AttendArgs &a, int64_t tiles)
+__device__ __forceinline__ WorkPlace work_place(const AttendArgs &a, int64_t tiles, int splits)
 {
     int64_t id = blockIdx.x;
     WorkPlace w;
@@ -259,7 +284,7 @@ __device__ __forceinline__ WorkPlace work_place(const AttendArgs &a, int64_t til
     } else {
         w.head = (int)(id % a.kv_heads);
         id /= a.kv_heads;
-        w.place = id % tiles, w.split = (int)(id / tiles);
+        w.split = (int)(id % splits), w.place = id / splits;
     }
     return w;
 }
