@@ -41,42 +41,56 @@ struct Stage {
     static constexpr bool BIAS = SRC == PLAID_SOURCE_BIAS;
     static constexpr uint16_t NONE = DT == PLAID_BF16 ? 0xff80 : 0xfc00;  // -infinity
     uint64_t k_masked, v_masked;  // keys of bias -infinity, and places past the end, in the tiles that are asked for next
+    // What a load's address is made of is formed once: a tile's place is a product of 32 bits, a lane's place in a tile is kept.
+    const char *keys, *values, *biases;            // the request's first
+    uint32_t key_row[N], value_row[N], chunk[N];  // bytes of a lane's row in a tile, and within the row
+    uint32_t to_k, to_v, to_raw;                  // in LDS, of the wave
 
-    // Keys past the end repeat the last one.  The tiles after the last repeat that one, so that a phase's number of loads is fixed.
-    __device__ __forceinline__ void load(const KeyRange &kr, const char *rows, int64_t token, int64_t head, int tile, char *to, uint64_t masked)
+    __device__ __forceinline__ void init(const AttendArgs &a, const KeyRange &kr, const TileBuffers<D, NW, SRC> &b)
     {
-        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), last = kr.len - 1 - tile * MANY_KEYS;
-        const char *base = rows + (kr.base + tile * MANY_KEYS) * token + kr.head * head;
+        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+        keys = a.k + kr.base * a.k_token + kr.head * a.k_head, values = a.v + kr.base * a.v_token + kr.head * a.v_head;
+        biases = a.bias + 2 * kr.base;
+        to_k = lds_address(b.k[0]) + wave * N * 1024, to_v = lds_address(b.v[0]) + wave * N * 1024, to_raw = lds_address(b.raw[BIAS ? wave : 0]);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int first = (wave * N + i) * AT_ONCE, row = first + lane / CHUNKS, chunk = (lane % CHUNKS) ^ swizzle<D>(row);
-            const uint32_t off = (uint32_t)min(row, last) * (uint32_t)token + chunk * 16;
-            if constexpr (BIAS) {
-                const bool none = (uint32_t)(masked >> first) >> (lane / CHUNKS) & 1;
-                load_to_lds(none ? (const char *)zero_row : base + off, to + (wave * N + i) * 1024);
-            } else {
-                load_to_lds(base, off, to + (wave * N + i) * 1024);
-            }
+            const int row = (wave * N + i) * AT_ONCE + lane / CHUNKS;
+            key_row[i] = (uint32_t)row * (uint32_t)a.k_token, value_row[i] = (uint32_t)row * (uint32_t)a.v_token;
+            chunk[i] = ((lane % CHUNKS) ^ swizzle<D>(row)) * 16;
         }
     }
-    __device__ __forceinline__ void load_k(const AttendArgs &a, const KeyRange &kr, int tile, int end, TileBuffers<D, NW, SRC> &b)
+    // Keys past the end repeat the last one.  The tiles after the last repeat that one, so that a phase's number of loads is fixed.
+    __device__ __forceinline__ void load(const KeyRange &kr, const char *first, uint32_t token, const uint32_t (&rows)[N], int tile, uint32_t to, uint64_t masked)
     {
-        load(kr, a.k, a.k_token, a.k_head, min(tile, end - 1), b.k[tile % TILES], k_masked);
+        const char *base = first + (uint64_t)(uint32_t)(tile * MANY_KEYS) * token;
+        const uint32_t last = (uint32_t)min(kr.len - 1 - tile * MANY_KEYS, MANY_KEYS - 1) * token;
+        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+        const uint32_t none = (uint32_t)(masked >> (wave * N * AT_ONCE)) >> (lane / CHUNKS);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t off = min(rows[i], last) + chunk[i];
+            if constexpr (BIAS) load_to_lds(none >> (i * AT_ONCE) & 1 ? (const char *)zero_row : base + off, to + i * 1024);
+            else load_to_lds(base, off, to + i * 1024);
+        }
     }
-    __device__ __forceinline__ void load_v(const AttendArgs &a, const KeyRange &kr, int tile, int end, TileBuffers<D, NW, SRC> &b)
+    __device__ __forceinline__ void load_k(const AttendArgs &a, const KeyRange &kr, int tile, int end)
     {
-        load(kr, a.v, a.v_token, a.v_head, min(tile, end - 1), b.v[tile % TILES], v_masked);
+        load(kr, keys, (uint32_t)a.k_token, key_row, min(tile, end - 1), to_k + (uint32_t)tile % TILES * (MANY_KEYS * D * 2), k_masked);
     }
-    __device__ __forceinline__ void load_bias(const AttendArgs &a, const KeyRange &kr, int tile, int end, TileBuffers<D, NW, SRC> &b)
+    __device__ __forceinline__ void load_v(const AttendArgs &a, const KeyRange &kr, int tile, int end)
     {
-        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), t = min(tile, end - 1), last = kr.len - 1 - t * MANY_KEYS;
-        load2_to_lds(a.bias + 2 * (kr.base + t * MANY_KEYS), 2 * min(lane, last), b.raw[wave][tile & 3]);
+        load(kr, values, (uint32_t)a.v_token, value_row, min(tile, end - 1), to_v + (uint32_t)tile % TILES * (MANY_KEYS * D * 2), v_masked);
+    }
+    __device__ __forceinline__ void load_bias(const KeyRange &kr, int tile, int end)
+    {
+        const int lane = threadIdx.x & 63, t = min(tile, end - 1), last = kr.len - 1 - t * MANY_KEYS;
+        load2_to_lds(biases + (uint64_t)(uint32_t)t * (2 * MANY_KEYS), 2 * min(lane, last), to_raw + (tile & 3) * 256);
     }
     // The biases of the tile whose keys are asked for next, in 32 bits, and which of its keys are masked.  They are read some time
     // before they are used.
     uint32_t raw;
     Shift shift;
-    float shifts[Ahead<NW, SRC>::K];  // what was subtracted in the tile whose weights are next, and those after it
+    int shifts[Ahead<NW, SRC>::K];  // bits of what was subtracted in the tile whose weights are next, and those after it
     __device__ __forceinline__ void read_bias(const TileBuffers<D, NW, SRC> &b, int tile) { raw = b.raw[threadIdx.x >> 6][tile & 3][threadIdx.x & 63]; }
     __device__ __forceinline__ void store_bias(const AttendArgs &a, const KeyRange &kr, int end, TileBuffers<D, NW, SRC> &b, int tile)
     {
@@ -85,21 +99,22 @@ struct Stage {
         const float f = unpack<DT>(x, 0);
         v_masked = k_masked;
         k_masked = __ballot(x == NONE);
-        const uint64_t unusual = __ballot(unusual_bias(f));
-        shift.add(unusual, unusual_bias(f) ? f : -INFINITY, ~(k_masked | unusual) != 0);
+        const uint64_t large = __ballot(fabsf(f) > BIAS_USUAL), unusual = large & ~k_masked;
+        shift.add(unusual, unusual_bias(f) ? f : -INFINITY, ~(k_masked | large) != 0);
         b.bias[threadIdx.x >> 6][tile & 3][lane] = (f - shift.c) * a.inv_scale;
 #pragma unroll
         for (int i = 0; i + 1 < Ahead<NW, SRC>::K; ++i) shifts[i] = shifts[i + 1];
-        shifts[Ahead<NW, SRC>::K - 1] = __int_as_float(uniform(__float_as_int(shift.c)));
+        shifts[Ahead<NW, SRC>::K - 1] = __float_as_int(shift.c);
     }
     // Before the first phase: asks for the first tiles and waits for the first one's keys.
     __device__ __forceinline__ void start(const AttendArgs &a, const KeyRange &kr, int begin, int end, TileBuffers<D, NW, SRC> &b)
     {
         using A = Ahead<NW, SRC>;
         static_assert(A::V == A::K - 1, "values are asked for one tile behind the keys");
+        init(a, kr, b);
         if constexpr (BIAS) {
 #pragma unroll
-            for (int i = 0; i <= A::K; ++i) load_bias(a, kr, begin + i, end, b);
+            for (int i = 0; i <= A::K; ++i) load_bias(kr, begin + i, end);
             wait_loads<0>();
         }
 #pragma unroll
@@ -108,8 +123,8 @@ struct Stage {
                 read_bias(b, begin + i);
                 store_bias(a, kr, end, b, begin + i);
             }
-            load_k(a, kr, begin + i, end, b);
-            if (i > 0) load_v(a, kr, begin + i - 1, end, b);
+            load_k(a, kr, begin + i, end);
+            if (i > 0) load_v(a, kr, begin + i - 1, end);
         }
         wait_all_loads();  // the queries too
         lds_barrier();
@@ -127,10 +142,10 @@ struct Stage {
         using A = Ahead<NW, SRC>;
         if constexpr (BIAS) {
             store_bias(a, kr, end, b, step + A::K);
-            load_bias(a, kr, step + A::K + 1, end, b);
+            load_bias(kr, step + A::K + 1, end);
         }
-        load_k(a, kr, step + A::K, end, b);
-        load_v(a, kr, step + A::V, end, b);
+        load_k(a, kr, step + A::K, end);
+        load_v(a, kr, step + A::V, end);
     }
     // At the end of a phase: what the phases after the next barrier need has arrived.  A step asks for 2 N pieces (and its bias);
     // the next step's keys and this one's values must be there after its second phase.
@@ -347,22 +362,22 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         }
     }
     // with values that are not finite in q even the zeros that stand for masked keys give scores that are not numbers
-    bool odd = false;
+    int odd = 0;
     if constexpr (SRC == PLAID_SOURCE_BIAS) {
         constexpr int INF = DT == PLAID_BF16 ? 0x7f80 : 0x7c00;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) odd = odd || (q[s][e] & INF) == INF || ((q[s][e] >> 16) & INF) == INF;
-        odd = __any(odd);
+            for (int e = 0; e < 4; ++e) odd |= (q[s][e] & INF) == INF || ((q[s][e] >> 16) & INF) == INF;
+        odd = uniform(__any(odd) ? 1 : 0);
     }
     f32x16 o[DT_TILES];
 #pragma unroll
     for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = zero16();
     // scores are kept as q . k + b / scale: one multiply-add then makes the exponent
     const float cs = a.scale * LOG2E;
-    float m = -INFINITY, l = 0.0f, shift = 0.0f;
-    bool beside = false;  // the shift leaves the scores nothing
+    float m = -INFINITY, l = 0.0f;
+    int shift = 0, beside = 0;  // the shift's bits, and whether it leaves the scores nothing: the same for all lanes
 
     // Two groups of waves, one of each on every SIMD, half a step apart: while one multiplies, the other forms exponentials.
     // A step of a group is a phase of products (o += v^T p^T of the former tile, s of this one) and one of everything else, with
@@ -381,28 +396,38 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     }
     f32x16 s[2];
     i32x4 p[4];
-    auto scores = [&](int step) {
+    auto before_scores = [&](int step) {
+        if constexpr (SRC == PLAID_SOURCE_BIAS) {  // what the products are added to
+            typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
+            const lds_f32x4 *b = (const lds_f32x4 *)&lds.bias[wave][step & 3][4 * h];
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            if constexpr (SRC == PLAID_SOURCE_BIAS) {  // what the products are added to
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x4 b = *(const f32x4 *)&lds.bias[wave][step & 3][32 * mt + 8 * i + 4 * h];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[mt][4 * i + e] = b[e];
-                }
-            } else {
-                s[mt] = zero16();
+            for (int mt = 0; mt < 2; ++mt) {
+                const f32x4 b0 = b[8 * mt], b1 = b[8 * mt + 2], b2 = b[8 * mt + 4], b3 = b[8 * mt + 6];
+                const auto low = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7), high = __builtin_shufflevector(b2, b3, 0, 1, 2, 3, 4, 5, 6, 7);
+                s[mt] = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
             }
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) s[mt] = mfma32<DT>(lds_rows<D>(lds.k[step % A::TILES], 32 * mt, d), q[d], s[mt]);
+        } else {
+            s[0] = zero16(), s[1] = zero16();
         }
     };
-    auto add_values = [&](int step) {
+    constexpr int EARLY = 4, KEY_READS = D / 16 * 2;  // operands of keys that are read before the products with values end
+    i32x4 early[EARLY];
+    auto key_operand = [&](int step, int i) { return lds_rows<D>(lds.k[step % A::TILES], 32 * (i & 1), i >> 1); };
+    auto scores = [&](int step) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < KEY_READS; ++i) s[i & 1] = mfma32<DT>(i < EARLY ? early[i] : key_operand(step, i), q[i >> 1], s[i & 1]);
+    };
+    auto add_values = [&](int step, int from, int to) {
+#pragma unroll
+        for (int i = from; i < to; ++i)
 #pragma unroll
             for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = mfma32<DT>(value_operand<D, NW, SRC>(lds, step % A::TILES, 16 * i, dt), p[i], o[dt]);
+    };
+    auto add_weights = [&]() {
+        float sums[4] = {l, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[i & 3] += s[0][i] + s[1][i];
+        l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     };
     auto weights = [&](int step) {
         if constexpr (SRC == PLAID_SOURCE_DENSE) stage.bring(a, kr, step, end, late, lds);
@@ -410,17 +435,18 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         float top;
         if constexpr (SRC == PLAID_SOURCE_BIAS) {
             if (stage.shifts[0] != shift) {  // m is relative to the shift
-                m += (shift - stage.shifts[0]) * a.inv_scale;
+                m += (__int_as_float(shift) - __int_as_float(stage.shifts[0])) * a.inv_scale;
                 shift = stage.shifts[0];
-                beside = beside_shift(1.0f, shift) == 0.0f;
+                beside = uniform((int)(beside_shift(1.0f, __int_as_float(shift)) == 0.0f));
             }
-            if (odd || beside) {
+            if (odd | beside) {
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float b = lds.bias[wave][step & 3][32 * mt + 8 * (i >> 2) + 4 * h + (i & 3)];
-                        if (beside || b == -INFINITY) s[mt][i] = b;
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x4 b = *(const f32x4 *)&lds.bias[wave][step & 3][32 * mt + 8 * i + 4 * h];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[mt][4 * i + e] = beside || b[e] == -INFINITY ? b[e] : s[mt][4 * i + e];
                     }
             }
         } else {
@@ -458,13 +484,15 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[mt][i] = __builtin_amdgcn_exp2f(fmaf(s[mt][i], cs, -ref_cs));
-                l += s[mt][i];
             }
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = round8<DT>(s[i >> 1], i & 1);
         if constexpr (SRC != PLAID_SOURCE_DENSE) stage.bring(a, kr, step, end, late, lds);
     };
     if (begin < end) {
+        before_scores(begin);
+#pragma unroll
+        for (int i = 0; i < EARLY; ++i) early[i] = key_operand(begin, i);
         scores(begin);
         phase_end(false);
         for (int step = begin; step + 1 < end; ++step) {
@@ -472,24 +500,43 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             phase_end(true);
             // where the other phase has the most to do, turning codes into values, products go first (536 us in place of 564)
             if constexpr (SRC == PLAID_SOURCE_PAGED) __builtin_amdgcn_s_setprio(1);
-            add_values(step);
-            scores(step + 1);
-            // the order of the phase: operands are asked for twelve reads ahead of the products that take them
-            constexpr int BIASES = SRC == PLAID_SOURCE_BIAS ? 8 : 0, FIRST = SRC == PLAID_SOURCE_BIAS ? 14 : 12;
-            constexpr int READS = D / 32 * 4 * 2 + D / 16 * 2 + BIASES, PRODUCTS = D / 32 * 4 + D / 16 * 2;  // 3 reads to 2 products
-            __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
+            // the weights are added up while the first operands are on their way, and their registers then are free
+            i32x4 first[DT_TILES];
 #pragma unroll
-            for (int i = 0; i < (READS - FIRST) / 3; ++i) {
+            for (int dt = 0; dt < DT_TILES; ++dt) first[dt] = value_operand<D, NW, SRC>(lds, step % A::TILES, 0, dt);
+            __builtin_amdgcn_sched_barrier(0);
+            add_weights();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = mfma32<DT>(first[dt], p[0], o[dt]);
+            add_values(step, 1, 4);
+            before_scores(step + 1);
+#pragma unroll
+            for (int i = 0; i < EARLY; ++i) early[i] = key_operand(step + 1, i);
+            // the order of the phase: operands are asked for some reads ahead of the products that take them
+            constexpr int READS = DT_TILES * 6 + (SRC == PLAID_SOURCE_BIAS ? 8 : 0) + EARLY - 6, PAIRS = DT_TILES * 2 - 1;
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, (READS + PAIRS - 1) / PAIRS, 0);
             }
-            __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - FIRST) / 3 * 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            scores(step + 1);
+#pragma unroll
+            for (int i = 0; i < (KEY_READS - EARLY) / 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, EARLY, 0);
             phase_end(false);
             if constexpr (SRC == PLAID_SOURCE_PAGED) __builtin_amdgcn_s_setprio(0);
         }
         weights(end - 1);
         phase_end(true);
-        add_values(end - 1);
+        add_weights();
+        add_values(end - 1, 0, 4);
         if (A::GROUPS == 2 && !late) lds_barrier();
         wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
@@ -498,7 +545,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     if (!there) return;
     const int64_t out_row = (tp.begin + token) * a.heads + head;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const float2 lse = l == 0.0f ? float2{-INFINITY, 0.0f} : float2{shift, m * a.scale + logf(l)};
+    const float2 lse = l == 0.0f ? float2{-INFINITY, 0.0f} : float2{__int_as_float(shift), m * a.scale + logf(l)};
     if (a.splits > 1) {
         const int64_t at = (int64_t)split * a.num_queries * a.heads + out_row;
 #pragma unroll

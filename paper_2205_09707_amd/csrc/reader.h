@@ -348,19 +348,20 @@ __device__ __forceinline__ void wait_loads()
 #define BIAS_ALL 4503599627370496.0f
 struct Shift {
     float c = 0.0f, most = -INFINITY;  // most: the largest unusual bias
-    bool usual = false;                // whether a usual one was seen
+    bool usual = false, seen = false;  // whether a usual, an unusual one was seen
     // Takes in a wave's biases: lanes that have an unusual one, their largest (looked at where there are any), whether any lane has
     // a usual one.
     __device__ __forceinline__ void add(uint64_t unusual, float largest, bool any_usual)
     {
-        usual = usual || any_usual;
-        if (unusual || c != 0.0f) {
+        usual |= any_usual;
+        seen |= unusual != 0;
+        if (seen) {
             if (unusual) {
 #pragma unroll
                 for (int o = 32; o; o >>= 1) largest = fmaxf(largest, __shfl_xor(largest, o));
-                most = fmaxf(most, largest);
+                most = fmaxf(most, __int_as_float(uniform(__float_as_int(largest))));
             }
-            c = most > BIAS_USUAL ? most : usual ? 0.0f : most;
+            c = __int_as_float(uniform(__float_as_int(most > BIAS_USUAL ? most : usual ? 0.0f : most)));
         }
     }
 };
@@ -377,18 +378,21 @@ static __device__ const i32x4 zero_row[16] = {};
 // There is no result in registers and the compiler does not count these loads: it would have every transposing read of LDS wait
 // for all of them.  (They go by register m0, which nothing else in these kernels uses.)  What they bring is waited for with wait_loads, before the barrier that lets it be read and before the end.
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
-__device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, char *to)
+__device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_address(to)), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
 }
-__device__ __forceinline__ void load_to_lds(const char *from, char *to)
+__device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, char *to) { load_to_lds(base, off, lds_address(to)); }
+__device__ __forceinline__ void load_to_lds(const char *from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(to)), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
-__device__ __forceinline__ void load2_to_lds(const char *base, uint32_t off, uint32_t *to)  // 2 bytes a lane, 4 in LDS
+__device__ __forceinline__ void load_to_lds(const char *from, char *to) { load_to_lds(from, lds_address(to)); }
+__device__ __forceinline__ void load2_to_lds(const char *base, uint32_t off, uint32_t to)  // 2 bytes a lane, 4 in LDS
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(lds_address(to)), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
 }
+__device__ __forceinline__ void load2_to_lds(const char *base, uint32_t off, uint32_t *to) { load2_to_lds(base, off, lds_address(to)); }
 __device__ __forceinline__ void load4_to_lds(const float *from, float *to)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(to)), "v"(from) : "memory");
