@@ -27,8 +27,8 @@ __global__ __launch_bounds__(256) void delta_kernel(GradArgs g)
         for (int o = LANES / 2; o; o >>= 1) sum += __shfl_xor(sum, o);
         if (c == 0) {
             const float2 lse = *(const float2 *)(g.a.lse + 2 * at);
-            g.delta[at] = lse.x != -INFINITY ? sum : 0.0f;
-            g.exponent[at] = lse.x != -INFINITY ? lse.y * LOG2E : INFINITY;
+            g.delta[at] = lse.x != -INFINITY ? -sum : 0.0f;
+            g.exponent[at] = (lse.x != -INFINITY ? -lse.y : -INFINITY) * g.a.inv_scale;
         }
     }
 }
@@ -94,7 +94,8 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     }
     float bias = 0.0f;
     if (BIAS) bias = there ? load16<DT>(a.bias + 2 * (tp.begin + key)) : 0.0f;
-    const float c = BIAS ? request_shift(a, row0, rows) : 0.0f, cs = beside_shift(a.scale, c) * LOG2E, bias_e = (bias - c) * LOG2E;
+    const float c = BIAS ? request_shift(a, row0, rows) : 0.0f, cs = a.scale * LOG2E, bias_e = (bias - c) * LOG2E;
+    const bool beside = BIAS && beside_shift(1.0f, c) == 0.0f;
     f32x16 sum[D / 32];  // the first wave's dv, the second one's dk
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) sum[t] = zero16();
@@ -144,38 +145,54 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     };
     f32x16 s[BLOCKS];
     i32x4 p[2 * BLOCKS];
-    auto form = [&](int step) {  // s = q k^T, or dP = dO v^T
-        const uint32_t at_q = q_tile(step), at_o = O_AT + o_tile(step);
-        const char *x = ring + (second ? at_o : at_q);
+    // s = q k^T, or dP = dO v^T; the products are added to what the rows bring, -lse / scale or -delta
+    constexpr int EARLY = 4, READS = BLOCKS * D / 16;  // operands that are read before the products of add end
+    i32x4 early[EARLY];
+    auto operand = [&](int step, int i) { return lds_rows<D>(ring + (second ? O_AT + o_tile(step) : q_tile(step)), 32 * (i % BLOCKS), i / BLOCKS); };
+    auto before_form = [&](int step) {
+        typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
+        const lds_f32x4 *x = (const lds_f32x4 *)&lds.row[wave][step & 3][4 * h];
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) {
-            s[b] = zero16();
+        for (int b = 0; b < BLOCKS; ++b) s[b] = join16(x[8 * b], x[8 * b + 2], x[8 * b + 4], x[8 * b + 6]);
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) s[b] = mfma32<DT>(lds_rows<D>(x, 32 * b, d), kv[d], s[b]);
-        }
+        for (int i = 0; i < EARLY; ++i) early[i] = operand(step, i);
     };
-    auto add = [&](int step) {  // dv += dO^T P, or dk += q^T dS
-        const uint32_t at_q = q_tile(step), at_o = O_AT + o_tile(step);
-        const char *x = ring + (second ? at_q : at_o);
+    auto form = [&](int step) {
 #pragma unroll
-        for (int i = 0; i < 2 * BLOCKS; ++i)
+        for (int i = 0; i < READS; ++i) s[i % BLOCKS] = mfma32<DT>(i < EARLY ? early[i] : operand(step, i), kv[i / BLOCKS], s[i % BLOCKS]);
+    };
+    auto add_operand = [&](int step, int i, int t) { return lds_columns<D>(ring + (second ? q_tile(step) : O_AT + o_tile(step)), 16 * i, t); };
+    auto add = [&](int step, int from) {  // dv += dO^T P, or dk += q^T dS
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t) sum[t] = mfma32<DT>(lds_columns<D>(x, 16 * i, t), p[i], sum[t]);
+        for (int i = from; i < 2 * BLOCKS; ++i)
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) sum[t] = mfma32<DT>(add_operand(step, i, t), p[i], sum[t]);
+    };
+    auto add_dbias = [&]() {
+        if (!BIAS || !second) return;
+        float sums[4] = {dbias, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sums[i & 3] += s[b][i];
+        dbias = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     };
     auto weights = [&](int step) {
         load_row(step + 2);
         if (!second) load(step + K::AHEAD);
-        else wait_loads<2>();  // this step's deltas
-        const float *of_row = lds.row[wave][step & 3];
+        else wait_loads<1>();  // the next step's deltas
         if (!second) {
+            if (beside) {
+                const float *of_row = lds.row[wave][step & 3];
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = of_row[32 * b + 8 * (i >> 2) + 4 * h + (i & 3)];
+            }
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x4 ex = *(const f32x4 *)(of_row + 32 * b + 8 * i + 4 * h);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[b][4 * i + e] = BIAS ? fmaf(s[b][4 * i + e], cs, bias_e) - ex[e] : fmaf(s[b][4 * i + e], cs, -ex[e]);
-                }
+                for (int i = 0; i < 16; ++i) s[b][i] = BIAS ? fmaf(s[b][i], cs, bias_e) : s[b][i] * cs;
             if ((step + 1) * ROWS > rows) {
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
@@ -197,12 +214,9 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
             for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const f32x4 x = *(const f32x4 *)lds.p[pair][b][i][lane], dl = *(const f32x4 *)(of_row + 32 * b + 8 * i + 4 * h);
+                    const f32x4 x = *(const f32x4 *)lds.p[pair][b][i][lane];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[b][4 * i + e] = x[e] * (s[b][4 * i + e] - dl[e]);
-                        if (BIAS) dbias += s[b][4 * i + e];
-                    }
+                    for (int e = 0; e < 4; ++e) s[b][4 * i + e] *= x[e];
                 }
         }
 #pragma unroll
@@ -217,27 +231,45 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
         wait_all_loads();  // the keys or values too
         lds_barrier();
         if (second) lds_barrier();
+        before_form(begin);
         form(begin);
         lds_barrier();
         for (int step = begin; step + 1 < end; ++step) {
             weights(step);
             if (!second) wait_loads<STEP *(K::AHEAD - 1)>();
             lds_barrier();
-            add(step);
-            form(step + 1);
-            constexpr int READS = 2 * BLOCKS * (D / 32) * 2 + BLOCKS * (D / 16), PRODUCTS = 2 * BLOCKS * (D / 32) + BLOCKS * (D / 16);
-            __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
+            i32x4 first[D / 32];
 #pragma unroll
-            for (int i = 0; i < (READS - 12) / 3; ++i) {
+            for (int t = 0; t < D / 32; ++t) first[t] = add_operand(step, 0, t);
+            __builtin_amdgcn_sched_barrier(0);
+            add_dbias();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) sum[t] = mfma32<DT>(first[t], p[0], sum[t]);
+            add(step, 1);
+            before_form(step + 1);
+            constexpr int OTHERS = (2 * BLOCKS - 1) * (D / 32) * 2 + BLOCKS * 4 + EARLY - 6, PAIRS = BLOCKS * (D / 32) - 1;
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, (OTHERS + PAIRS - 1) / PAIRS, 0);
             }
-            __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - 12) / 3 * 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            form(step + 1);
+#pragma unroll
+            for (int i = 0; i < (READS - EARLY) / 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, EARLY, 0);
             lds_barrier();
         }
         weights(end - 1);
         lds_barrier();
-        add(end - 1);
+        add_dbias();
+        add(end - 1, 0);
         if (!second) lds_barrier();
         wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
@@ -248,7 +280,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     const bool masked = BIAS && bias == -INFINITY;
     const int64_t at = (tp.begin + key) * a.kv_heads + head;
     if (BIAS && second && h == 0 && g.dbias_part) g.dbias_part[((int64_t)split * a.kv_heads + head) * a.num_keys + tp.begin + key] = masked ? 0.0f : dbias;
-    const float factor = second ? a.scale : 1.0f;
+    const float factor = second ? g.factor : 1.0f;
     char *out = second ? g.dk : g.dv;
     float *part = second ? g.dk_part : g.dv_part;
 #pragma unroll
@@ -310,57 +342,86 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
     }
     const float2 lse = *(const float2 *)(a.lse + 2 * at);
     const bool counts = lse.x != -INFINITY;
-    const float c = BIAS ? request_shift(a, tp.begin, rows) : 0.0f, ex = counts ? lse.y * LOG2E : INFINITY, cs = beside_shift(a.scale, c) * LOG2E;
-    float delta = counts ? g.delta[at] : 0.0f;
+    const float c = BIAS ? request_shift(a, tp.begin, rows) : 0.0f, ex = counts ? lse.y * LOG2E : INFINITY, cs = a.scale * LOG2E;
+    const bool beside = BIAS && beside_shift(1.0f, c) == 0.0f;
+    const float minus_delta = counts && steps > 1 ? g.delta[at] : 0.0f;
     f32x16 dq[D / 32];
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
 
     // keys past the end repeat the last one; tiles past the last repeat that
     uint32_t masked = 0;  // keys of bias -infinity, and places past the end, in the tile that is asked for next
+    const char *keys = a.k + key0 * a.k_token + head_kv * a.k_head, *values = a.v + key0 * a.v_token + head_kv * a.v_head;
+    uint32_t key_row[N], value_row[N], chunk[N];  // bytes of a lane's row in a tile, and within the row
+    const uint32_t to_k = lds_address(lds.k[0]) + wave * N * 1024, to_v = lds_address(lds.v[0]) + wave * N * 1024;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int in = (wave * N + i) * AT_ONCE + lane / CHUNKS;
+        key_row[i] = (uint32_t)in * (uint32_t)a.k_token, value_row[i] = (uint32_t)in * (uint32_t)a.v_token, chunk[i] = ((lane % CHUNKS) ^ swizzle<D>(in)) * 16;
+    }
     auto load = [&](int step) {
-        const int t = min(step, end - 1), last = len - 1 - t * GRAD_KEYS;
-        const char *bk = a.k + (key0 + t * GRAD_KEYS) * a.k_token + head_kv * a.k_head, *bv = a.v + (key0 + t * GRAD_KEYS) * a.v_token + head_kv * a.v_head;
+        const int t = min(step, end - 1), last = min(len - 1 - t * GRAD_KEYS, GRAD_KEYS - 1);
+        const uint64_t first = (uint32_t)t * GRAD_KEYS;
+        const char *bk = keys + first * (uint32_t)a.k_token, *bv = values + first * (uint32_t)a.v_token;
+        const uint32_t last_k = (uint32_t)last * (uint32_t)a.k_token, last_v = (uint32_t)last * (uint32_t)a.v_token;
+        const uint32_t k_at = to_k + (uint32_t)step % L::K_TILES * (uint32_t)sizeof(lds.k[0]), v_at = to_v + (uint32_t)step % L::V_TILES * (uint32_t)sizeof(lds.v[0]);
+        const uint32_t none = masked >> (wave * N * AT_ONCE & 31) >> (lane / CHUNKS);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int in = (wave * N + i) * AT_ONCE + lane / CHUNKS, key = min(in, last), chunk = (lane % CHUNKS) ^ swizzle<D>(in);
-            const uint32_t off_k = (uint32_t)key * (uint32_t)a.k_token + chunk * 16, off_v = (uint32_t)key * (uint32_t)a.v_token + chunk * 16;
-            char *to_k = lds.k[step % L::K_TILES] + (wave * N + i) * 1024, *to_v = lds.v[step % L::V_TILES] + (wave * N + i) * 1024;
+            const uint32_t off_k = min(key_row[i], last_k) + chunk[i], off_v = min(value_row[i], last_v) + chunk[i];
             if constexpr (BIAS) {
-                const bool none = masked >> in & 1;
-                load_to_lds(none ? (const char *)zero_row : bk + off_k, to_k);
-                load_to_lds(none ? (const char *)zero_row : bv + off_v, to_v);
+                const bool hidden = none >> (i * AT_ONCE) & 1;
+                load_to_lds(hidden ? (const char *)zero_row : bk + off_k, k_at + i * 1024);
+                load_to_lds(hidden ? (const char *)zero_row : bv + off_v, v_at + i * 1024);
             } else {
-                load_to_lds(bk, off_k, to_k);
-                load_to_lds(bv, off_v, to_v);
+                load_to_lds(bk, off_k, k_at + i * 1024);
+                load_to_lds(bv, off_v, v_at + i * 1024);
             }
         }
     };
+    const char *biases = a.bias + 2 * key0;
     auto load_bias = [&](int step) {
         const int t = min(step, end - 1), last = len - 1 - t * GRAD_KEYS;
-        load2_to_lds(a.bias + 2 * (key0 + t * GRAD_KEYS), 2 * min(lane & 31, last), lds.raw[wave][step & 3]);
+        load2_to_lds(biases + (uint64_t)(uint32_t)t * (2 * GRAD_KEYS), 2 * min(lane & 31, last), lds.raw[wave][step & 3]);
     };
     uint32_t raw = 0;  // read some time before it is used
     auto read_bias = [&](int step) { raw = lds.raw[wave][step & 3][lane]; };
     auto store_bias = [&](int step) {
         const uint16_t x = min(step, end - 1) * GRAD_KEYS + (lane & 31) < len ? (uint16_t)raw : NONE;
-        lds.bias[wave][step & 3][lane & 31] = unpack<DT>(x, 0) - c;
+        lds.bias[wave][step & 3][lane & 31] = (unpack<DT>(x, 0) - c) * a.inv_scale;
         masked = (uint32_t)__ballot(x == NONE);
     };
-    f32x16 s, ds;
+    f32x16 s, ds;  // q k^T + b / scale, dO v^T - delta
     i32x4 r[2];
+    constexpr int EARLY = 4, READS = 2 * (D / 16);  // operands that are read before the products of add end
+    i32x4 early[EARLY];
+    auto operand = [&](int step, int i) { return i % 2 ? lds_rows<D>(lds.v[(uint32_t)step % L::V_TILES], 0, i / 2) : lds_rows<D>(lds.k[(uint32_t)step % L::K_TILES], 0, i / 2); };
+    auto before_form = [&](int step) {
+        if constexpr (BIAS) {
+            typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
+            const lds_f32x4 *b = (const lds_f32x4 *)&lds.bias[wave][step & 3][4 * h];
+            s = join16(b[0], b[2], b[4], b[6]);
+        } else {
+            s = zero16();
+        }
+#pragma unroll
+        for (int i = 0; i < EARLY; ++i) early[i] = operand(step, i);
+    };
     auto form = [&](int step) {
-        s = zero16(), ds = zero16();
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) s = mfma32<DT>(lds_rows<D>(lds.k[step % L::K_TILES], 0, d), q[d], s);
+        for (int i = 0; i < 16; ++i) ds[i] = minus_delta;
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) ds = mfma32<DT>(lds_rows<D>(lds.v[step % L::V_TILES], 0, d), d_out[d], ds);
+        for (int i = 0; i < READS; ++i) {
+            const i32x4 x = i < EARLY ? early[i] : operand(step, i);
+            if (i % 2) ds = mfma32<DT>(x, d_out[i / 2], ds);
+            else s = mfma32<DT>(x, q[i / 2], s);
+        }
     };
     auto add = [&](int step) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t) dq[t] = mfma32<DT>(lds_columns<D>(lds.k[step % L::K_TILES], 16 * i, t), r[i], dq[t]);
+            for (int t = 0; t < D / 32; ++t) dq[t] = mfma32<DT>(lds_columns<D>(lds.k[(uint32_t)step % L::K_TILES], 16 * i, t), r[i], dq[t]);
     };
     auto weights = [&](int step) {
         if constexpr (BIAS) {
@@ -368,34 +429,32 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
             if (late) wait_loads<0>();
             else wait_loads<2 * N>();
             read_bias(step + L::AHEAD);
+            if (beside) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = lds.bias[wave][step & 3][8 * (i >> 2) + 4 * h + (i & 3)];
+            }
         } else {
             if (!late) load(step + L::AHEAD);
         }
-        if constexpr (BIAS) {
-            f32x4 b[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) b[i] = *(const f32x4 *)&lds.bias[wave][step & 3][8 * i + 4 * h];
+        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], cs, -ex);
+        if (!BIAS && (step + 1) * GRAD_KEYS > len) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = fmaf(b[i >> 2][i & 3], LOG2E, fmaf(s[i], cs, -ex));
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], cs, -ex);
-            if ((step + 1) * GRAD_KEYS > len) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = step * GRAD_KEYS + 8 * (i >> 2) + 4 * h + (i & 3) < len ? s[i] : -INFINITY;
-            }
+            for (int i = 0; i < 16; ++i) s[i] = step * GRAD_KEYS + 8 * (i >> 2) + 4 * h + (i & 3) < len ? s[i] : -INFINITY;
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
         if (steps == 1) {
-            delta = 0.0f;
+            float delta = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) delta = fmaf(s[i], ds[i], delta);
             delta = sum_halves(delta);
-            if (there && h == 0) g.delta[at] = delta;
+            if (there && h == 0) g.delta[at] = -delta;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ds[i] -= delta;
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) ds[i] = s[i] * (ds[i] - delta);
+        for (int i = 0; i < 16; ++i) ds[i] *= s[i];
         r[0] = round8<DT>(ds, 0), r[1] = round8<DT>(ds, 1);
         if constexpr (BIAS) {
             store_bias(step + L::AHEAD);
@@ -421,6 +480,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
         wait_all_loads();  // the rows too
         lds_barrier();
         if (late) lds_barrier();
+        before_form(begin);
         form(begin);
         lds_barrier();
         for (int step = begin; step + 1 < end; ++step) {
@@ -428,15 +488,23 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
             if (!late) wait_loads<STEP *(L::AHEAD - 1)>();  // the next step's keys and values
             lds_barrier();
             add(step);
-            form(step + 1);
-            constexpr int READS = 2 * (D / 32) * 2 + 2 * (D / 16), PRODUCTS = 2 * (D / 32) + 2 * (D / 16);  // 4 reads to 3 products
-            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+            before_form(step + 1);
+            constexpr int FIRST = 12, OTHERS = 2 * (D / 32) * 2 + (BIAS ? 4 : 0) + EARLY - FIRST, PAIRS = D / 32 - 1;
+            __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
 #pragma unroll
-            for (int i = 0; i < (READS - 8) / 4; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            for (int i = 0; i < PAIRS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, (OTHERS + PAIRS - 1) / PAIRS, 0);
             }
-            __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - 8) / 4 * 3, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            form(step + 1);
+#pragma unroll
+            for (int i = 0; i < (READS - EARLY) / 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, EARLY, 0);
             lds_barrier();
         }
         weights(end - 1);
@@ -452,7 +520,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
         for (int i = 0; i < 4; ++i) {
             f32x4 x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = dq[t][4 * i + e] * a.scale;
+            for (int e = 0; e < 4; ++e) x[e] = dq[t][4 * i + e] * g.factor;
             const int d = 32 * t + 8 * i + 4 * h;
             if (splits > 1) *(f32x4 *)(g.dq_part + ((int64_t)split * a.num_queries * a.heads + at) * D + d) = x;
             else *(i32x2 *)(g.dq + (at * D + d) * 2) = i32x2{pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])};

@@ -401,11 +401,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
             const lds_f32x4 *b = (const lds_f32x4 *)&lds.bias[wave][step & 3][4 * h];
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
-                const f32x4 b0 = b[8 * mt], b1 = b[8 * mt + 2], b2 = b[8 * mt + 4], b3 = b[8 * mt + 6];
-                const auto low = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7), high = __builtin_shufflevector(b2, b3, 0, 1, 2, 3, 4, 5, 6, 7);
-                s[mt] = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
-            }
+            for (int mt = 0; mt < 2; ++mt) s[mt] = join16(b[8 * mt], b[8 * mt + 2], b[8 * mt + 4], b[8 * mt + 6]);
         } else {
             s[0] = zero16(), s[1] = zero16();
         }

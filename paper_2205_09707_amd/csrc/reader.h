@@ -21,7 +21,8 @@ struct AttendArgs {
     int64_t q_token, q_head, k_token, k_head, v_token, v_head;  // strides in bytes
     int32_t n, heads, kv_heads, group;
     uint32_t group_magic;              // ceil(2^32 / group): row / group = umulhi(row, magic) for group > 1
-    float scale, inv_scale;            // forward: > 0 (negate_q carries the sign) and its reciprocal
+    float scale;                       // forward: > 0, negate_q carries the sign
+    float inv_scale;                   // 1 / scale, or of the least scale that exponents are formed with
     uint32_t negate_q;                 // 0x80008000 where the caller's scale is negative, else 0
     // paged source
     const uint8_t *cache;
@@ -36,10 +37,11 @@ struct AttendArgs {
 
 struct GradArgs {
     AttendArgs a;                      // out and lse are inputs
+    float factor;                      // the scale as it was given, of dq and dk
     const char *d_out;
     char *dq, *dk, *dv, *dbias;        // any may be null
-    float *delta;                      // [num_queries][heads]
-    float *exponent;                   // [num_queries][heads] what the weights' exponents of 2 have subtracted, infinity without a key
+    float *delta;                      // [num_queries][heads] -dO . out
+    float *exponent;                   // [num_queries][heads] -lse / scale without the shift; without a key an infinity that makes weights 0
     float *dbias_part;                 // [splits][kv_heads][num_keys], null without dbias
     float *dk_part, *dv_part;          // [splits][num_keys][kv_heads][D], null with one split
     float *dq_part;                    // [splits][num_queries][heads][D], null with one split
@@ -185,6 +187,11 @@ __device__ __forceinline__ float sum_rows(float x)
 {
     const float2 y = both_rows(x);
     return y.x + y.y;
+}
+__device__ __forceinline__ f32x16 join16(f32x4 a, f32x4 b, f32x4 c, f32x4 d)
+{
+    const auto low = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), high = __builtin_shufflevector(c, d, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
 }
 // The larger of two products' results; fmaxf would first make each of them quiet.
 __device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }

@@ -1,5 +1,5 @@
 // C entry points of the reader (include/plaid.h): argument checks, the choice of kernel and of how the work is cut, workspaces.
-#include <math.h>
+#include <cmath>
 
 #include "reader.h"
 
@@ -41,6 +41,7 @@ int check_cache(const plaid_paged_cache *c)
 
 // Workgroups that fill the chip: 256 compute units, and what the kernels leave room for on each.
 constexpr int UNITS = 256, MANY_TARGET = 512;
+constexpr float LEAST_SCALE = 1e-30f;  // that scores are multiplied with
 
 struct Plan {
     bool few;
@@ -176,7 +177,7 @@ int run_forward(const plaid_attention &a, AttendArgs &x, const Plan &p, int sour
     // the running maximum is that of q . k, so the factor is made positive and q carries its sign
     if (!(a.scale >= 0.0f)) x.negate_q = 0x80008000u, x.scale = -a.scale;
     // a factor of 0 would meet the infinities of keys that are hidden; beside this one every score that is not huge is nothing as well
-    if (x.scale < 1e-30f) x.scale = 1e-30f;
+    if (x.scale < LEAST_SCALE) x.scale = LEAST_SCALE;
     x.inv_scale = 1.0f / x.scale;
     x.part_o = (float *)workspace;
     x.part_lse = (float *)((char *)workspace + p.o_bytes);
@@ -336,6 +337,9 @@ extern "C" int plaid_cross_attention_backward(const plaid_attention *args, const
     if (!guard.ok) return plaid_fail(PLAID_EHIP, "device %d cannot be used", device);
     GradArgs g = {};
     g.a = attend_args(*args);
+    g.factor = args->scale;
+    if (std::fabs(g.a.scale) < LEAST_SCALE) g.a.scale = std::copysign(LEAST_SCALE, g.a.scale);
+    g.a.inv_scale = 1.0f / g.a.scale;
     g.d_out = (const char *)d_out;
     g.dq = (char *)dq, g.dk = (char *)dk, g.dv = (char *)dv, g.dbias = (char *)dbias;
     char *w = (char *)workspace;
