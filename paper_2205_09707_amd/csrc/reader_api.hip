@@ -58,13 +58,27 @@ int64_t split_count(int64_t groups, int64_t steps, int64_t least)
     return s < 1 ? 1 : s > 64 ? 64 : s;
 }
 
+// Which forward kernel takes a call whose requests have `rows` rows and `keys` keys on average.  One tile of 16 rows is always the
+// few-row kernel's: the other leaves half of its 32 rows empty.  More rows it reads the same keys for once a tile, so it takes
+// them while its workgroups all find room at once and have little to read; it then cuts the keys finer.  us, few and many:
+//   16 heads on 4, D = 128, 4 requests of 64 tokens x 450 keys: 10.8 and 21.3;  x 2000: 31.6 and 29.5;  16 of 64 x 450: 37.2 and 29.0
+//   12 heads on 12, D = 64, 4 requests of 128 tokens x 450 keys: 11.4 and 15.8;  of 64 x 2000: 23.9 and 22.2;  16 of 96 x 450: 26.2 and 23.0
+//   paged, 32 heads on 8, 4 requests of 32 tokens x 2000 keys: 17.0 and 31.3;  16 of 8 x 8000: 52.4 and 93.2;  16 of 32 x 2000: 61.5 and 47.4
+bool few_rows(int64_t rows, int64_t n, int64_t kv_heads, int64_t keys, int head_dim, int source)
+{
+    if (rows <= FEW_ROWS) return true;
+    const bool paged = source == PLAID_SOURCE_PAGED;
+    const int64_t groups = ceil_div(rows, FEW_ROWS) * n * kv_heads;
+    return groups <= (paged || head_dim == 64 ? UNITS * 5 / 2 : UNITS) && groups * keys <= (paged ? 1 << 21 : 1 << 19);
+}
+
 // keys: of all requests; longest: that a request can have; usual: to reckon with
 Plan plan_forward(const plaid_attention &a, int source, int64_t keys, int64_t longest, int64_t usual)
 {
     Plan p = {};
     const int64_t group = a.heads / a.kv_heads, tokens = ceil_div(a.num_queries, a.n), rows = tokens * group;
     p.tiles = a.num_queries * group / FEW_ROWS + a.n;
-    p.few = rows <= 2 * FEW_ROWS && p.tiles * (longest / FEW_KEYS + 1) < INT32_MAX;  // its counts of steps are 32 bits wide
+    p.few = few_rows(rows, a.n, a.kv_heads, usual, a.head_dim, source) && p.tiles * (longest / FEW_KEYS + 1) < INT32_MAX;  // its counts of steps are 32 bits wide
     if (p.few) {
         // One workgroup for each tile, no workers, nothing to join: 9.4 us in place of 11.0 at 1024 keys, 14.8 in place of 11.4 at 2048
         // for one request of 8 key heads; 34.6 in place of 39.5 at 2048 for 64 of them.  Packed keys: a request may have twice the mean.
