@@ -447,7 +447,8 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
         if (kg == 0) lds.ml[wave][m16][0] = natural, lds.ml[wave][m16][1] = l;
         if (lane == 0) lds.shift[wave] = shift.c;
         __syncthreads();
-        for (int u = threadIdx.x; u < FEW_ROWS * (D / 4); u += NW * 64) {
+        const int count = min(FEW_ROWS, rows - tile * FEW_ROWS);  // rows that there are
+        for (int u = threadIdx.x; u < count * (D / 4); u += NW * 64) {
             const int y = u / (D / 4), d = u % (D / 4) * 4;  // a row and 4 of its dimensions
             float base = -INFINITY, top = -INFINITY, sum = 0.0f;
             f32x4 acc{0, 0, 0, 0};
@@ -471,12 +472,10 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] *= inv;
             if (begin == 0 && stop == rq.steps) {
-                if (row_out < rows) {
-                    const int tk = row_token(a, row_out);
-                    const int64_t to = (rq.row0 + tk) * a.heads + head_kv * a.group + row_out - tk * a.group;
-                    *(i32x2 *)(a.out + (to * D + d) * 2) = i32x2{pack2<DT>(acc[0], acc[1]), pack2<DT>(acc[2], acc[3])};
-                    if (a.lse && d == 0) *(float2 *)(a.lse + 2 * to) = lse;
-                }
+                const int tk = row_token(a, row_out);
+                const int64_t to = (rq.row0 + tk) * a.heads + head_kv * a.group + row_out - tk * a.group;
+                *(i32x2 *)(a.out + (to * D + d) * 2) = i32x2{pack2<DT>(acc[0], acc[1]), pack2<DT>(acc[2], acc[3])};
+                if (a.lse && d == 0) *(float2 *)(a.lse + 2 * to) = lse;
             } else {
                 const int64_t slot = ((int64_t)worker * 2 + (begin == 0)) * a.kv_heads + head_kv;
                 *(f32x4 *)(a.part_o + (slot * FEW_ROWS + y) * D + d) = acc;
