@@ -1,0 +1,79 @@
+"""The kernels of many rows at the sizes that reach them: sums of whole tiles, requests that are taken in the order of their work or
+(more than 64 of them) as they come, splits over long keys, masks and scales."""
+import pytest
+import torch
+
+import reader_util as ru
+from test_gpu_reader_attention import BF, HF, _bias, _check_cached, _check_cross, pl  # noqa: F401 (pl is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim,heads,kv_heads", [(64, 16, 2), (128, 16, 2), (128, 9, 1), (64, 15, 5)])
+def test_long_and_short_requests(pl, dim, heads, kv_heads, dtype, with_bias):  # noqa: F811
+    k_lengths = [64, 0, 331, 1, 130]
+    bias = _bias(sum(k_lengths), 5, dtype) if with_bias else None
+    _check_cross(pl, [300, 40, 257, 512, 1], k_lengths, heads, kv_heads, dim, dtype, bias, seed=3)
+
+
+@pytest.mark.parametrize("n", [64, 65, 130])
+def test_numbers_of_requests(pl, n):  # noqa: F811
+    lengths = [(7 * r) % 40 for r in range(n)]
+    keys = [(11 * r + 3) % 150 for r in range(n)]
+    _check_cross(pl, lengths, keys, 16, 2, 64, BF, _bias(sum(keys), 1, BF), seed=n)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_requests_of_few_and_of_many_keys(pl, dtype):  # noqa: F811
+    _check_cross(pl, [200, 333, 128], [3000, 32, 33], 8, 4, 128, dtype, _bias(3065, 2, dtype), seed=9)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.5])
+@pytest.mark.parametrize("with_bias", [False, True])
+def test_scales(pl, scale, with_bias):  # noqa: F811
+    _check_cross(pl, [300, 290], [200, 101], 16, 2, 64, BF, _bias(301, 4, BF) if with_bias else None, scale=scale, seed=6)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_masks_of_the_lowest_value(pl, dtype):  # noqa: F811
+    keys = [150, 200, 70]
+    lowest = torch.finfo(dtype).min
+    bias = _bias(sum(keys), 8, dtype, masked=0.0)
+    bias[:150] = lowest                                                  # all of the first request's
+    bias[150 + 64:150 + 128] = lowest                                    # a whole tile of the second's
+    bias[350 + 3] = -float("inf")
+    _check_cross(pl, [280, 270, 300], keys, 16, 2, 64, dtype, bias, seed=10)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,dim,bs,heads,kv_heads", [(BF, 128, 16, 16, 2), (HF, 64, 64, 16, 2), (BF, 64, 32, 9, 3), (HF, 128, 128, 12, 4)])
+def test_prompts_behind_contexts(pl, dtype, dim, bs, heads, kv_heads, causal):  # noqa: F811
+    _check_cached(pl, [400, 1, 0, 513, 257], [1200, 700, 30, 513, 100], heads, kv_heads, dim, bs, dtype, causal=causal, hide=((0, 1), (3, 0)), seed=12)
+
+
+def test_many_prompts(pl):  # noqa: F811
+    n = 70
+    q = [(13 * r) % 45 for r in range(n)]
+    _check_cached(pl, q, [x + (29 * r) % 200 for r, x in enumerate(q)], 16, 2, 64, 16, BF, seed=13)
+
+
+def test_long_keys_in_splits(pl):  # noqa: F811
+    _check_cross(pl, [330], [9000], 8, 1, 128, BF, _bias(9000, 3, BF), seed=14)
+
+
+def test_numbers_that_are_not_finite_in_masked_keys(pl):  # noqa: F811
+    bias = _bias(500, 6, BF, masked=0.4)
+
+    def change(q, k, v):
+        for t, x in ((k, float("nan")), (v, float("inf"))):
+            t[(bias == -float("inf")).nonzero().flatten()] = x
+
+    _check_cross(pl, [300, 320], [300, 200], 16, 2, 64, BF, bias, change=change, seed=15)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_scores_of_hundreds(pl, dim):  # noqa: F811
+    _check_cross(pl, [300, 270], [700, 333], 16, 2, dim, BF, gain=20.0, train=False)
+    _check_cross(pl, [300, 270], [700, 333], 16, 2, dim, HF, _bias(1033, 2, HF), gain=20.0, train=False)
