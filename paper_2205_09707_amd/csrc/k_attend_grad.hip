@@ -104,12 +104,14 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     // Rows past the end repeat the last one; tiles past the last repeat that.  Where a step is a whole number of tokens a lane's rows
     // lie at the same distances from the step's first token in every step.
     const bool aligned = ROWS % a.group == 0;
-    uint32_t q_off[N], o_off[N];
+    // The first waves bring q, the second ones dO.
+    const char *mine = second ? g.d_out : a.q;
+    const int64_t token_bytes = second ? (int64_t)a.heads * (D * 2) : a.q_token, head_bytes = second ? D * 2 : a.q_head;
+    uint32_t off[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int in = (pair * N + i) * AT_ONCE + lane / CHUNKS, chunk = (lane % CHUNKS) ^ swizzle<D>(in), token = row_token(a, in), hd = in - token * a.group;
-        q_off[i] = (uint32_t)token * (uint32_t)a.q_token + (uint32_t)hd * (uint32_t)a.q_head + chunk * 16;
-        o_off[i] = ((uint32_t)token * (uint32_t)a.heads + (uint32_t)hd) * (D * 2) + chunk * 16;
+        off[i] = (uint32_t)token * (uint32_t)token_bytes + (uint32_t)hd * (uint32_t)head_bytes + chunk * 16;
     }
     // the tiles' places in the rings; nothing below branches on the kind of wave but the weights
     auto q_tile = [&](int step) { return (uint32_t)step % K::Q_TILES * (uint32_t)sizeof(lds.q[0]); };
@@ -120,22 +122,17 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     const char *ring = lds.q[0];
     auto load = [&](int step) {
         const int t = min(step, end - 1);
-        char *to_q = lds.q[0] + q_tile(step) + pair * N * 1024, *to_o = lds.o[0] + o_tile(step) + pair * N * 1024;
+        const uint32_t to = lds_address(ring) + (second ? O_AT + o_tile(step) : q_tile(step)) + pair * N * 1024;
         if (aligned && (t + 1) * ROWS <= rows) {
-            const int64_t first = row0 + row_token(a, t * ROWS);
-            const char *q = a.q + first * a.q_token + (int64_t)head * a.group * a.q_head, *o = g.d_out + (first * a.heads + head * a.group) * (D * 2);
+            const char *base = mine + (row0 + row_token(a, t * ROWS)) * token_bytes + (int64_t)head * a.group * head_bytes;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                load_to_lds(q, q_off[i], to_q + i * 1024);
-                load_to_lds(o, o_off[i], to_o + i * 1024);
-            }
+            for (int i = 0; i < N; ++i) load_to_lds(base, off[i], to + i * 1024);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int in = (pair * N + i) * AT_ONCE + lane / CHUNKS, row = min(t * ROWS + in, rows - 1), chunk = (lane % CHUNKS) ^ swizzle<D>(in);
                 const int token = row_token(a, row), hd = head * a.group + row - token * a.group;
-                load_to_lds(a.q + (row0 + token) * a.q_token + hd * a.q_head + chunk * 16, to_q + i * 1024);
-                load_to_lds(g.d_out + ((row0 + token) * a.heads + hd) * (D * 2) + chunk * 16, to_o + i * 1024);
+                load_to_lds(mine + (row0 + token) * token_bytes + hd * head_bytes + chunk * 16, to + i * 1024);
             }
         }
     };
@@ -179,8 +176,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     };
     auto weights = [&](int step) {
         load_row(step + 2);
-        if (!second) load(step + K::AHEAD);
-        else wait_loads<1>();  // the next step's deltas
+        load(step + K::AHEAD);
         if (!second) {
             if (beside) {
                 const float *of_row = lds.row[wave][step & 3];
@@ -222,12 +218,12 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
 #pragma unroll
         for (int i = 0; i < 2 * BLOCKS; ++i) p[i] = round8<DT>(s[i >> 1], i & 1);
     };
-    constexpr int STEP = 2 * N + 1;  // loads of a step: q, dO and the rows' numbers
+    constexpr int STEP = N + 1;  // loads of a step: q or dO, and the rows' numbers
     if (begin < end) {
         load_row(begin);
-        if (!second) load(begin);
+        load(begin);
         load_row(begin + 1);
-        if (!second) load(begin + 1);
+        load(begin + 1);
         wait_all_loads();  // the keys or values too
         lds_barrier();
         if (second) lds_barrier();
@@ -236,8 +232,9 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
         lds_barrier();
         for (int step = begin; step + 1 < end; ++step) {
             weights(step);
-            if (!second) wait_loads<STEP *(K::AHEAD - 1)>();
+            wait_loads<STEP *(K::AHEAD - 1)>();  // the next step's have arrived
             lds_barrier();
+            __builtin_amdgcn_s_setprio(1);
             i32x4 first[D / 32];
 #pragma unroll
             for (int t = 0; t < D / 32; ++t) first[t] = add_operand(step, 0, t);
@@ -265,6 +262,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
             }
             __builtin_amdgcn_sched_group_barrier(0x008, EARLY, 0);
             lds_barrier();
+            __builtin_amdgcn_s_setprio(0);
         }
         weights(end - 1);
         lds_barrier();
@@ -313,6 +311,7 @@ template <int DT, int D, int NW, bool BIAS>
 __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t tiles, int splits)
 {
     using L = GradQLds<D, NW, BIAS>;
+    constexpr uint32_t TILE = GRAD_KEYS * D * 2, V_AT = offsetof(L, v);
     constexpr int ROWS = NW * 32, SHIFT = NW == 8 ? 8 : 7, CHUNKS = D / 8, AT_ONCE = 512 / D, N = GRAD_KEYS / AT_ONCE / 4;
     constexpr uint16_t NONE = DT == PLAID_BF16 ? 0xff80 : 0xfc00;  // -infinity
     const AttendArgs &a = g.a;
@@ -351,31 +350,34 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
 
     // keys past the end repeat the last one; tiles past the last repeat that
     uint32_t masked = 0;  // keys of bias -infinity, and places past the end, in the tile that is asked for next
-    const char *keys = a.k + key0 * a.k_token + head_kv * a.k_head, *values = a.v + key0 * a.v_token + head_kv * a.v_head;
-    uint32_t key_row[N], value_row[N], chunk[N];  // bytes of a lane's row in a tile, and within the row
-    const uint32_t to_k = lds_address(lds.k[0]) + wave * N * 1024, to_v = lds_address(lds.v[0]) + wave * N * 1024;
+    // of eight waves the first four bring keys, the others values; four waves bring both
+    constexpr int SIDES = NW == 8 ? 1 : 2;
+    const char *from[SIDES];
+    uint32_t token_bytes[SIDES], row_at[SIDES][N], chunk[N];  // a lane's row in a tile, and within the row
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int in = (wave * N + i) * AT_ONCE + lane / CHUNKS;
-        key_row[i] = (uint32_t)in * (uint32_t)a.k_token, value_row[i] = (uint32_t)in * (uint32_t)a.v_token, chunk[i] = ((lane % CHUNKS) ^ swizzle<D>(in)) * 16;
+    for (int i = 0; i < N; ++i) chunk[i] = ((lane % CHUNKS) ^ swizzle<D>(((wave & 3) * N + i) * AT_ONCE + lane / CHUNKS)) * 16;
+#pragma unroll
+    for (int x = 0; x < SIDES; ++x) {
+        const bool of_values = SIDES == 2 ? x == 1 : late;
+        token_bytes[x] = (uint32_t)(of_values ? a.v_token : a.k_token);
+        from[x] = (of_values ? a.v : a.k) + key0 * token_bytes[x] + head_kv * (of_values ? a.v_head : a.k_head);
+#pragma unroll
+        for (int i = 0; i < N; ++i) row_at[x][i] = (uint32_t)(((wave & 3) * N + i) * AT_ONCE + lane / CHUNKS) * token_bytes[x];
     }
     auto load = [&](int step) {
         const int t = min(step, end - 1), last = min(len - 1 - t * GRAD_KEYS, GRAD_KEYS - 1);
-        const uint64_t first = (uint32_t)t * GRAD_KEYS;
-        const char *bk = keys + first * (uint32_t)a.k_token, *bv = values + first * (uint32_t)a.v_token;
-        const uint32_t last_k = (uint32_t)last * (uint32_t)a.k_token, last_v = (uint32_t)last * (uint32_t)a.v_token;
-        const uint32_t k_at = to_k + (uint32_t)step % L::K_TILES * (uint32_t)sizeof(lds.k[0]), v_at = to_v + (uint32_t)step % L::V_TILES * (uint32_t)sizeof(lds.v[0]);
-        const uint32_t none = masked >> (wave * N * AT_ONCE & 31) >> (lane / CHUNKS);
+        const uint32_t none = masked >> ((wave & 3) * N * AT_ONCE) >> (lane / CHUNKS);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t off_k = min(key_row[i], last_k) + chunk[i], off_v = min(value_row[i], last_v) + chunk[i];
-            if constexpr (BIAS) {
-                const bool hidden = none >> (i * AT_ONCE) & 1;
-                load_to_lds(hidden ? (const char *)zero_row : bk + off_k, k_at + i * 1024);
-                load_to_lds(hidden ? (const char *)zero_row : bv + off_v, v_at + i * 1024);
-            } else {
-                load_to_lds(bk, off_k, k_at + i * 1024);
-                load_to_lds(bv, off_v, v_at + i * 1024);
+        for (int x = 0; x < SIDES; ++x) {
+            const bool of_values = SIDES == 2 ? x == 1 : late;
+            const char *base = from[x] + (uint64_t)((uint32_t)t * GRAD_KEYS) * token_bytes[x];
+            const uint32_t end_at = (uint32_t)last * token_bytes[x];
+            const uint32_t to = lds_address(&lds) + (of_values ? V_AT + (uint32_t)step % L::V_TILES * TILE : (uint32_t)step % L::K_TILES * TILE) + (wave & 3) * N * 1024;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t off = min(row_at[x][i], end_at) + chunk[i];
+                if constexpr (BIAS) load_to_lds(none >> (i * AT_ONCE) & 1 ? (const char *)zero_row : base + off, to + i * 1024);
+                else load_to_lds(base, off, to + i * 1024);
             }
         }
     };
@@ -426,15 +428,14 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
     auto weights = [&](int step) {
         if constexpr (BIAS) {
             // the biases that the step before asked for first
-            if (late) wait_loads<0>();
-            else wait_loads<2 * N>();
+            wait_loads<SIDES * N>();
             read_bias(step + L::AHEAD);
             if (beside) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = lds.bias[wave][step & 3][8 * (i >> 2) + 4 * h + (i & 3)];
             }
         } else {
-            if (!late) load(step + L::AHEAD);
+            load(step + L::AHEAD);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], cs, -ex);
@@ -459,10 +460,10 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
         if constexpr (BIAS) {
             store_bias(step + L::AHEAD);
             load_bias(step + L::AHEAD + 1);
-            if (!late) load(step + L::AHEAD);
+            load(step + L::AHEAD);
         }
     };
-    constexpr int STEP = 2 * N + BIAS;  // loads of a step
+    constexpr int STEP = SIDES * N + BIAS;  // loads of a step
     if (begin < end) {
         if constexpr (BIAS) {
 #pragma unroll
@@ -475,7 +476,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
                 read_bias(begin + i);
                 store_bias(begin + i);
             }
-            if (!late) load(begin + i);
+            load(begin + i);
         }
         wait_all_loads();  // the rows too
         lds_barrier();
@@ -485,8 +486,11 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
         lds_barrier();
         for (int step = begin; step + 1 < end; ++step) {
             weights(step);
-            if (!late) wait_loads<STEP *(L::AHEAD - 1)>();  // the next step's keys and values
+            // the next step's keys; values, which come half a step later, are needed half a step earlier
+            if (late) wait_loads<STEP *(L::AHEAD - 2)>();
+            else wait_loads<STEP *(L::AHEAD - 1)>();
             lds_barrier();
+            __builtin_amdgcn_s_setprio(1);
             add(step);
             before_form(step + 1);
             constexpr int FIRST = 12, OTHERS = 2 * (D / 32) * 2 + (BIAS ? 4 : 0) + EARLY - FIRST, PAIRS = D / 32 - 1;
@@ -506,6 +510,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
             }
             __builtin_amdgcn_sched_group_barrier(0x008, EARLY, 0);
             lds_barrier();
+            __builtin_amdgcn_s_setprio(0);
         }
         weights(end - 1);
         lds_barrier();
