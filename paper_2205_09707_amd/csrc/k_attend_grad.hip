@@ -299,24 +299,24 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
 // row, and delta is taken as the sum of P dP: out, rounded to the type, would give it too coarsely where few keys are averaged
 // (two keys in bf16: 4 of 1000 off in dq and dk, so 2.5).
 #define GRAD_KEYS 32
-template <int D, int NW, bool BIAS>
+template <int D, bool BIAS>
 struct GradQLds {
-    static constexpr int AHEAD = 3, K_TILES = AHEAD + 2, V_TILES = AHEAD + 1;  // keys are read in four phases, values in two
+    static constexpr int AHEAD = 3, K_TILES = AHEAD + 1, V_TILES = AHEAD;  // keys are read in two phases, values in one
     char k[K_TILES][GRAD_KEYS * D * 2], v[V_TILES][GRAD_KEYS * D * 2];
-    float bias[BIAS ? NW : 1][4][BIAS ? GRAD_KEYS : 4];  // each wave's own
-    uint32_t raw[BIAS ? NW : 1][4][64];                   // as they are loaded
+    float bias[BIAS ? 4 : 1][4][BIAS ? GRAD_KEYS : 4];  // each wave's own
+    uint32_t raw[BIAS ? 4 : 1][4][64];                   // as they are loaded
 };
 
-template <int DT, int D, int NW, bool BIAS>
-__global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t tiles, int splits)
+template <int DT, int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tiles, int splits)
 {
-    using L = GradQLds<D, NW, BIAS>;
-    constexpr uint32_t TILE = GRAD_KEYS * D * 2, V_AT = offsetof(L, v);
-    constexpr int ROWS = NW * 32, SHIFT = NW == 8 ? 8 : 7, CHUNKS = D / 8, AT_ONCE = 512 / D, N = GRAD_KEYS / AT_ONCE / 4;
+    using L = GradQLds<D, BIAS>;
+    constexpr uint32_t TILE = GRAD_KEYS * D * 2;
+    constexpr int ROWS = 128, SHIFT = 7, CHUNKS = D / 8, AT_ONCE = 512 / D, N = GRAD_KEYS / AT_ONCE / 4;
     constexpr uint16_t NONE = DT == PLAID_BF16 ? 0xff80 : 0xfc00;  // -infinity
     const AttendArgs &a = g.a;
     __shared__ __align__(16) L lds;
-    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5, late = wave >= 4;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
     const WorkPlace w = work_place(a, tiles, splits);
     const int head_kv = w.head, split = w.split;
     const int of = min(lane, a.n - 1);
@@ -350,34 +350,31 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
 
     // keys past the end repeat the last one; tiles past the last repeat that
     uint32_t masked = 0;  // keys of bias -infinity, and places past the end, in the tile that is asked for next
-    // of eight waves the first four bring keys, the others values; four waves bring both
-    constexpr int SIDES = NW == 8 ? 1 : 2;
-    const char *from[SIDES];
-    uint32_t token_bytes[SIDES], row_at[SIDES][N], chunk[N];  // a lane's row in a tile, and within the row
+    const char *keys = a.k + key0 * a.k_token + head_kv * a.k_head, *values = a.v + key0 * a.v_token + head_kv * a.v_head;
+    uint32_t key_row[N], value_row[N], chunk[N];  // bytes of a lane's row in a tile, and within the row
+    const uint32_t to_k = lds_address(lds.k[0]) + wave * N * 1024, to_v = lds_address(lds.v[0]) + wave * N * 1024;
 #pragma unroll
-    for (int i = 0; i < N; ++i) chunk[i] = ((lane % CHUNKS) ^ swizzle<D>(((wave & 3) * N + i) * AT_ONCE + lane / CHUNKS)) * 16;
-#pragma unroll
-    for (int x = 0; x < SIDES; ++x) {
-        const bool of_values = SIDES == 2 ? x == 1 : late;
-        token_bytes[x] = (uint32_t)(of_values ? a.v_token : a.k_token);
-        from[x] = (of_values ? a.v : a.k) + key0 * token_bytes[x] + head_kv * (of_values ? a.v_head : a.k_head);
-#pragma unroll
-        for (int i = 0; i < N; ++i) row_at[x][i] = (uint32_t)(((wave & 3) * N + i) * AT_ONCE + lane / CHUNKS) * token_bytes[x];
+    for (int i = 0; i < N; ++i) {
+        const int in = (wave * N + i) * AT_ONCE + lane / CHUNKS;
+        key_row[i] = (uint32_t)in * (uint32_t)a.k_token, value_row[i] = (uint32_t)in * (uint32_t)a.v_token, chunk[i] = ((lane % CHUNKS) ^ swizzle<D>(in)) * 16;
     }
     auto load = [&](int step) {
         const int t = min(step, end - 1), last = min(len - 1 - t * GRAD_KEYS, GRAD_KEYS - 1);
-        const uint32_t none = masked >> ((wave & 3) * N * AT_ONCE) >> (lane / CHUNKS);
+        const uint64_t first = (uint32_t)t * GRAD_KEYS;
+        const char *bk = keys + first * (uint32_t)a.k_token, *bv = values + first * (uint32_t)a.v_token;
+        const uint32_t last_k = (uint32_t)last * (uint32_t)a.k_token, last_v = (uint32_t)last * (uint32_t)a.v_token;
+        const uint32_t k_at = to_k + (uint32_t)step % L::K_TILES * TILE, v_at = to_v + (uint32_t)step % L::V_TILES * TILE;
+        const uint32_t none = masked >> (wave * N * AT_ONCE) >> (lane / CHUNKS);
 #pragma unroll
-        for (int x = 0; x < SIDES; ++x) {
-            const bool of_values = SIDES == 2 ? x == 1 : late;
-            const char *base = from[x] + (uint64_t)((uint32_t)t * GRAD_KEYS) * token_bytes[x];
-            const uint32_t end_at = (uint32_t)last * token_bytes[x];
-            const uint32_t to = lds_address(&lds) + (of_values ? V_AT + (uint32_t)step % L::V_TILES * TILE : (uint32_t)step % L::K_TILES * TILE) + (wave & 3) * N * 1024;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const uint32_t off = min(row_at[x][i], end_at) + chunk[i];
-                if constexpr (BIAS) load_to_lds(none >> (i * AT_ONCE) & 1 ? (const char *)zero_row : base + off, to + i * 1024);
-                else load_to_lds(base, off, to + i * 1024);
+        for (int i = 0; i < N; ++i) {
+            const uint32_t off_k = min(key_row[i], last_k) + chunk[i], off_v = min(value_row[i], last_v) + chunk[i];
+            if constexpr (BIAS) {
+                const bool hidden = none >> (i * AT_ONCE) & 1;
+                load_to_lds(hidden ? (const char *)zero_row : bk + off_k, k_at + i * 1024);
+                load_to_lds(hidden ? (const char *)zero_row : bv + off_v, v_at + i * 1024);
+            } else {
+                load_to_lds(bk, off_k, k_at + i * 1024);
+                load_to_lds(bv, off_v, v_at + i * 1024);
             }
         }
     };
@@ -428,7 +425,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
     auto weights = [&](int step) {
         if constexpr (BIAS) {
             // the biases that the step before asked for first
-            wait_loads<SIDES * N>();
+            wait_loads<2 * N>();
             read_bias(step + L::AHEAD);
             if (beside) {
 #pragma unroll
@@ -463,7 +460,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
             load(step + L::AHEAD);
         }
     };
-    constexpr int STEP = SIDES * N + BIAS;  // loads of a step
+    constexpr int STEP = 2 * N + BIAS;  // loads of a step
     if (begin < end) {
         if constexpr (BIAS) {
 #pragma unroll
@@ -480,15 +477,12 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
         }
         wait_all_loads();  // the rows too
         lds_barrier();
-        if (late) lds_barrier();
         before_form(begin);
         form(begin);
         lds_barrier();
         for (int step = begin; step + 1 < end; ++step) {
             weights(step);
-            // the next step's keys; values, which come half a step later, are needed half a step earlier
-            if (late) wait_loads<STEP *(L::AHEAD - 2)>();
-            else wait_loads<STEP *(L::AHEAD - 1)>();
+            wait_loads<STEP *(L::AHEAD - 1)>();  // the next step's keys and values
             lds_barrier();
             __builtin_amdgcn_s_setprio(1);
             add(step);
@@ -515,7 +509,6 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_q_kernel(GradArgs g, int64_t 
         weights(end - 1);
         lds_barrier();
         add(end - 1);
-        if (NW == 8 && !late) lds_barrier();
         wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
     if (!there) return;
@@ -570,30 +563,33 @@ static void launch_k(hipStream_t st, const GradArgs &g, int splits)
     if (g.a.bias) grad_k_kernel<DT, D, NW, true><<<grid, block, 0, st>>>(g, tiles, splits);
     else grad_k_kernel<DT, D, NW, false><<<grid, block, 0, st>>>(g, tiles, splits);
 }
-template <int DT, int D, int NW>
+template <int DT, int D>
 static void launch_q(hipStream_t st, const GradArgs &g, int splits)
 {
-    const int64_t tiles = g.a.num_queries * g.a.group / (NW * 32) + g.a.n;
-    const dim3 grid((unsigned)(tiles * g.a.kv_heads * splits)), block(NW * 64);
-    if (g.a.bias) grad_q_kernel<DT, D, NW, true><<<grid, block, 0, st>>>(g, tiles, splits);
-    else grad_q_kernel<DT, D, NW, false><<<grid, block, 0, st>>>(g, tiles, splits);
+    const int64_t tiles = g.a.num_queries * g.a.group / 128 + g.a.n;
+    const dim3 grid((unsigned)(tiles * g.a.kv_heads * splits)), block(256);
+    if (g.a.bias) grad_q_kernel<DT, D, true><<<grid, block, 0, st>>>(g, tiles, splits);
+    else grad_q_kernel<DT, D, false><<<grid, block, 0, st>>>(g, tiles, splits);
 }
 template <int DT, int D>
-static void launch(hipStream_t st, const GradArgs &g, int q_waves, int q_splits, int k_waves, int k_splits)
+static void launch(hipStream_t st, const GradArgs &g, int q_splits, int k_waves, int k_splits)
 {
     const AttendArgs &a = g.a;
     const int64_t q_values = a.num_queries * a.heads * D, k_values = a.num_keys * a.kv_heads * D;
     if (a.num_queries > 0) delta_kernel<DT, D><<<dim3((unsigned)ceil_div(q_values / 8, 256)), dim3(256), 0, st>>>(g);
     if (g.dq && a.num_queries > 0) {
-        if (q_waves == 8) launch_q<DT, D, 8>(st, g, q_splits);
-        else launch_q<DT, D, 4>(st, g, q_splits);
+        launch_q<DT, D>(st, g, q_splits);
         if (q_splits > 1)
             add_splits_kernel<DT><<<dim3((unsigned)ceil_div(q_values / 4, 256)), dim3(256), 0, st>>>(g.dq_part, g.dq, q_values, q_splits, a.q_offsets, a.n,
                                                                                                     (int64_t)a.heads * D);
     }
     if ((g.dk || g.dv || g.dbias) && a.num_keys > 0) {
-        if (k_waves == 8) launch_k<DT, D, 8>(st, g, k_splits);
-        else launch_k<DT, D, 4>(st, g, k_splits);
+        if constexpr (D == 128) {
+            if (k_waves == 8) launch_k<DT, D, 8>(st, g, k_splits);
+            else launch_k<DT, D, 4>(st, g, k_splits);
+        } else {
+            launch_k<DT, D, 4>(st, g, k_splits);
+        }
         if (k_splits > 1) {
             const dim3 grid((unsigned)ceil_div(k_values / 4, 256));
             if (g.dk) add_splits_kernel<DT><<<grid, dim3(256), 0, st>>>(g.dk_part, g.dk, k_values, k_splits, a.k_offsets, a.n, (int64_t)a.kv_heads * D);
@@ -604,8 +600,8 @@ static void launch(hipStream_t st, const GradArgs &g, int q_waves, int q_splits,
                                                                                                 a.k_offsets, a.n);
     }
 }
-void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_waves, int q_splits, int k_waves, int k_splits)
+void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_splits, int k_waves, int k_splits)
 {
-    if (dtype == PLAID_BF16) head_dim == 64 ? launch<PLAID_BF16, 64>(st, g, q_waves, q_splits, k_waves, k_splits) : launch<PLAID_BF16, 128>(st, g, q_waves, q_splits, k_waves, k_splits);
-    else head_dim == 64 ? launch<PLAID_FP16, 64>(st, g, q_waves, q_splits, k_waves, k_splits) : launch<PLAID_FP16, 128>(st, g, q_waves, q_splits, k_waves, k_splits);
+    if (dtype == PLAID_BF16) head_dim == 64 ? launch<PLAID_BF16, 64>(st, g, q_splits, k_waves, k_splits) : launch<PLAID_BF16, 128>(st, g, q_splits, k_waves, k_splits);
+    else head_dim == 64 ? launch<PLAID_FP16, 64>(st, g, q_splits, k_waves, k_splits) : launch<PLAID_FP16, 128>(st, g, q_splits, k_waves, k_splits);
 }

@@ -62,8 +62,7 @@ struct GradArgs {
 // Launchers.  workers: workgroups of attend_few per key head, 0: one for each tile.
 void plaid_launch_attend_few(hipStream_t st, const AttendArgs &a, int dtype, int head_dim, int source, int workers, int64_t tiles);
 void plaid_launch_attend_many(hipStream_t st, const AttendArgs &a, int dtype, int head_dim, int source, int waves, int64_t tiles);
-void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_waves, int q_splits, int k_waves,
-                              int k_splits);
+void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_splits, int k_waves, int k_splits);
 void plaid_launch_cache_write(hipStream_t st, const plaid_paged_cache &c, const char *k, const char *v, int64_t k_token, int64_t k_head,
                               int64_t v_token, int64_t v_head, const int64_t *slots, int64_t n);
 void plaid_launch_cache_read(hipStream_t st, const plaid_paged_cache &c, const int64_t *slots, int64_t n, char *k, char *v);

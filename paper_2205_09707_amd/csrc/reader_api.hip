@@ -9,11 +9,15 @@ namespace {
 
 struct OnDevice {  // the calling thread's device for the length of a call
     int before = -1;
-    bool ok = false;
-    explicit OnDevice(int device) { ok = hipGetDevice(&before) == hipSuccess && (before == device || hipSetDevice(device) == hipSuccess); }
+    bool ok = false, moved = false;
+    explicit OnDevice(int device)
+    {
+        ok = hipGetDevice(&before) == hipSuccess;
+        if (ok && before != device) ok = moved = hipSetDevice(device) == hipSuccess;
+    }
     ~OnDevice()
     {
-        if (before >= 0) (void)hipSetDevice(before);
+        if (moved) (void)hipSetDevice(before);
     }
 };
 
@@ -39,21 +43,21 @@ int check_cache(const plaid_paged_cache *c)
     return PLAID_OK;
 }
 
-// Workgroups that fill the chip: 256 compute units, and what the kernels leave room for on each.
-constexpr int UNITS = 256, MANY_TARGET = 512;
+constexpr int UNITS = 256;             // compute units
 constexpr float LEAST_SCALE = 1e-30f;  // that scores are multiplied with
 
 struct Plan {
     bool few;
-    int workers, waves, splits, q_waves, q_splits, k_waves, k_splits;
+    int workers, waves, splits, q_splits, k_waves, k_splits;
     int64_t tiles, bytes;
     int64_t o_bytes, delta_bytes, bias_bytes, k_bytes, q_bytes;
 };
 
-int64_t split_count(int64_t groups, int64_t steps, int64_t least)
+// Parts that an axis of `steps` steps is cut into, at least `least` of them a part, where `groups` workgroups of so many waves leave
+// compute units empty: one of eight waves has room on each, two of four.  One part too many would start a second round.
+int64_t split_count(int64_t groups, int waves, int64_t steps, int64_t least)
 {
-    if (groups >= MANY_TARGET * 3 / 4) return 1;
-    int64_t s = ceil_div(MANY_TARGET, groups < 1 ? 1 : groups);
+    int64_t s = UNITS * 8 / waves / (groups < 1 ? 1 : groups);
     if (s > steps / least) s = steps / least;
     return s < 1 ? 1 : s > 64 ? 64 : s;
 }
@@ -91,9 +95,11 @@ Plan plan_forward(const plaid_attention &a, int source, int64_t keys, int64_t lo
         p.bytes = p.o_bytes + p.o_bytes / a.head_dim * 2;
         return p;
     }
+    // 8 waves share a tile of keys among 256 rows: 488 us in place of 498 with 4 for 16 x 456 tokens of 16 heads on 6250 keys, 435 in place of
+    // 507 where the tile comes out of the cache (6 x 850 tokens of 32 heads behind 4750)
     p.waves = rows > 128 ? 8 : 4;
     p.tiles = a.num_queries * group / (p.waves * 32) + a.n;
-    p.splits = (int)split_count(ceil_div(rows, p.waves * 32) * a.n * a.kv_heads, ceil_div(usual, MANY_KEYS), 4);
+    p.splits = (int)split_count(ceil_div(rows, p.waves * 32) * a.n * a.kv_heads, p.waves, ceil_div(usual, MANY_KEYS), 4);
     p.o_bytes = p.splits > 1 ? (int64_t)p.splits * a.num_queries * a.heads * a.head_dim * 4 : 0;
     p.bytes = p.o_bytes + p.o_bytes / a.head_dim * 2;
     return p;
@@ -103,11 +109,11 @@ Plan plan_backward(const plaid_attention &a)
 {
     Plan p = {};
     const int64_t group = a.heads / a.kv_heads, rows = ceil_div(a.num_queries, a.n) * group, keys = ceil_div(a.num_keys, a.n);
-    p.q_waves = rows > 128 ? 8 : 4;
-    // a step of 8 waves takes 64 rows and most of a compute unit's LDS; 4 waves leave room for others where there are few steps
-    p.k_waves = keys > 64 && rows > 128 ? 8 : 4;
-    p.q_splits = (int)split_count(ceil_div(rows, p.q_waves * 32) * a.n * a.kv_heads, ceil_div(keys, 64), 4);
-    p.k_splits = (int)split_count(ceil_div(keys, p.k_waves * 16) * a.n * a.kv_heads, ceil_div(rows, 64), 4);
+    // Workgroups of dk and dv, us with 8 and with 4 waves.  D = 128, 16 heads on 4: 16 x 456 rows on 6250 keys 1504 and 1552, 16 x 100 on 1000
+    // 110 and 106.  D = 64, 12 heads on 12: 16 x 200 on 900 134 and 100, 8 x 500 on 3000 282 and 240: two workgroups of 4 on a unit do more.
+    p.k_waves = a.head_dim == 128 && keys > 64 && rows > 128 ? 8 : 4;
+    p.q_splits = (int)split_count(ceil_div(rows, 128) * a.n * a.kv_heads, 4, ceil_div(keys, 64), 4);
+    p.k_splits = (int)split_count(ceil_div(keys, p.k_waves * 16) * a.n * a.kv_heads, p.k_waves, ceil_div(rows, 64), 4);
     p.delta_bytes = 2 * round16(a.num_queries * a.heads * 4);  // and the rows' exponents
     p.bias_bytes = round16((int64_t)p.k_splits * a.kv_heads * a.num_keys * 4);
     p.k_bytes = p.k_splits > 1 ? (int64_t)p.k_splits * a.num_keys * a.kv_heads * a.head_dim * 4 : 0;
@@ -344,7 +350,7 @@ extern "C" int plaid_cross_attention_backward(const plaid_attention *args, const
     const Plan p = plan_backward(*args);
     if (const int rc = check_workspace(workspace, workspace_bytes, p.bytes)) return rc;
     const int64_t group = args->heads / args->kv_heads;
-    if ((args->num_queries * group / (p.q_waves * 32) + args->n) * args->kv_heads * p.q_splits > INT32_MAX ||
+    if ((args->num_queries * group / 128 + args->n) * args->kv_heads * p.q_splits > INT32_MAX ||
         (args->num_keys / (p.k_waves * 16) + args->n) * args->kv_heads * p.k_splits > INT32_MAX)
         FAIL("too much work for one call");
     const OnDevice guard(device);
@@ -362,6 +368,6 @@ extern "C" int plaid_cross_attention_backward(const plaid_attention *args, const
     g.dk_part = p.k_bytes ? (float *)w : nullptr, w += p.k_bytes;
     g.dv_part = p.k_bytes ? (float *)w : nullptr, w += p.k_bytes;
     g.dq_part = p.q_bytes ? (float *)w : nullptr;
-    plaid_launch_attend_grad((hipStream_t)hip_stream, g, args->dtype, args->head_dim, p.q_waves, p.q_splits, p.k_waves, p.k_splits);
+    plaid_launch_attend_grad((hipStream_t)hip_stream, g, args->dtype, args->head_dim, p.q_splits, p.k_waves, p.k_splits);
     return launched();
 }
