@@ -349,8 +349,8 @@ int plaid_cache_read(const plaid_paged_cache *cache, const int64_t *slots, int64
  *                    are not written
  *   k_offsets        [n+1] int64, the same for the keys (plaid_cross_attention)
  *   out              [num_queries][heads][head_dim] contiguous, lse [num_queries][heads][2] fp32 or NULL
- * heads is a multiple of kv_heads, head_dim 64 or 128; num_queries * (heads / kv_heads)^2 < 2^32.  A scale may be negative.  Over a
- * paged cache a group that is not finite reaches every row whose tile of keys it is in, also rows that are before it. */
+ * heads is a multiple of kv_heads, head_dim 64 or 128; num_queries * (heads / kv_heads)^2 < 2^32.  A scale may be negative.
+ * What a key holds reaches the rows that see it, and no other, also where it is not finite. */
 typedef struct {
     int32_t dtype;
     int32_t n;

@@ -201,6 +201,9 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
         for (int t = 0; t < OT; ++t) o[t] = f32x4{0, 0, 0, 0};
         float m = -INFINITY, l = 0.0f;
         Shift shift;
+        int bad[KS];  // paged: the first key of those that are hidden from some row whose values of 32 dimensions are not finite
+#pragma unroll
+        for (int g = 0; g < KS; ++g) bad[g] = INT32_MAX;
 
         // --- loads of a piece
         Piece<DT, D, SRC> x;
@@ -372,6 +375,14 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
                             // a token past the end may hold anything: with the smallest power its products with a weight of 0 are 0
                             if constexpr (D == 128) x.vs[c][e] = key < len ? x.vs[c][e] : 0;
                             else x.vs[c][e >> 1] &= key < len ? -1 : (e & 1 ? 0xffff : (int)0xffff0000);
+                            // so may one that only some of the rows see: those get what it holds at the end
+                            if (least < len && key >= least) {
+#pragma unroll
+                                for (int g = 0; g < KS; ++g) {
+                                    const int byte = e * KS + g, mask = 255 << 8 * (byte & 3);
+                                    if ((x.vs[c][byte >> 2] & mask) == mask) bad[g] = min(bad[g], key), x.vs[c][byte >> 2] &= ~mask;
+                                }
+                            }
                         }
                     }
             }
@@ -435,6 +446,16 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
                     if constexpr (BIAS) o[t] = mfma16<DT>(i32x4{u[0] & keep[0], u[1] & keep[1], w[0] & keep[2], w[1] & keep[3]}, p, o[t]);
                     else o[t] = mfma16<DT>(i32x4{u[0], u[1], w[0], w[1]}, p, o[t]);
                 }
+            }
+        }
+
+        if (PAGED && least < len) {
+#pragma unroll
+            for (int g = 0; g < KS; ++g) {
+                if (!__any(bad[g] != INT32_MAX)) continue;
+                bad[g] = min(bad[g], __shfl_xor(bad[g], 16));
+                bad[g] = min(bad[g], __shfl_xor(bad[g], 32));
+                if (bad[g] < limit) o[2 * g] = o[2 * g + 1] = f32x4{NAN, NAN, NAN, NAN};
             }
         }
 

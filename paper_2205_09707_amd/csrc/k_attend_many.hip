@@ -1,4 +1,6 @@
 // Attention where a request has many rows (tokens x heads that share keys): tiles of rows x 64 keys on the matrix units.
+#include <type_traits>
+
 #include "reader.h"
 
 // out = softmax(scale q k^T + b) v in one pass over the keys, with the running maximum m and sum l of each row:
@@ -26,12 +28,14 @@ struct TileBuffers {
     float bias[SRC == PLAID_SOURCE_BIAS ? NW : 1][4][SRC == PLAID_SOURCE_BIAS ? MANY_KEYS : 4];  // each wave's own
     uint32_t raw[SRC == PLAID_SOURCE_BIAS ? NW : 1][4][64];  // biases as they are loaded
     int cell[4][4];  // paged: whether the cells of 16 keys have a block
+    int bad[D / 32]; // paged: the first key of those that are hidden from some row whose values of 32 dimensions are not finite
 };
 
 struct KeyRange {
     int64_t base;  // dense: the request's first key
     int len;       // keys of the request that there are
     int r, head;   // request, key head
+    int least;     // keys that every row of the tile sees
 };
 
 // How a workgroup's waves bring tiles into LDS: dense keys and values go there straight from memory, each wave its share.
@@ -137,6 +141,7 @@ struct Stage {
             read_bias(b, step + Ahead<NW, SRC>::K);
         }
     }
+    template <bool>
     __device__ __forceinline__ void bring(const AttendArgs &a, const KeyRange &kr, int step, int end, int, TileBuffers<D, NW, SRC> &b)
     {
         using A = Ahead<NW, SRC>;
@@ -234,8 +239,25 @@ struct Stage<DT, D, NW, PLAID_SOURCE_PAGED> {
             if (u % (16 * G) == 0) b.cell[tile & 3][key >> 4] = ok[i];
         }
     }
-    __device__ __forceinline__ void store_v(TileBuffers<D, NW, PLAID_SOURCE_PAGED> &b, int tile)
+    template <bool CAREFUL>
+    __device__ __forceinline__ void store_v(const KeyRange &kr, TileBuffers<D, NW, PLAID_SOURCE_PAGED> &b, int tile)
     {
+        // A key that only some of the rows see may hold what is not finite, which would meet the zero weights of the others: it goes in
+        // as zero, and those that see it get it at the end.
+        if (CAREFUL && (tile + 1) * MANY_KEYS > kr.least) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int u = threadIdx.x + i * THREADS, at = tile * MANY_KEYS + unit_key(u);
+                if (u < KU || u >= KU + VU) continue;
+#pragma unroll
+                for (int byte = 0; byte < 4 * G; ++byte) {
+                    const int mask = 255 << 8 * (byte & 3), t = byte / G;
+                    if (at + t < kr.least || t >= last[i] || (scale[i][byte >> 2] & mask) != mask) continue;
+                    atomicMin(&b.bad[byte % G], at + t);
+                    scale[i][byte >> 2] &= ~mask;
+                }
+            }
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int u = threadIdx.x + i * THREADS, key = unit_key(u);
@@ -266,18 +288,20 @@ struct Stage<DT, D, NW, PLAID_SOURCE_PAGED> {
         find<false>(a, kr, begin);
         load_k(a, kr, begin);
         store_k(b, begin);
+        if (threadIdx.x < G) b.bad[threadIdx.x] = INT32_MAX;
         if (begin + 1 < end) load_k(a, kr, begin + 1);
         load_v(a, kr, begin);
         lds_barrier();
-        if (NW == 8 && threadIdx.x >= 256) bring(a, kr, begin - 1, end, 1, b);
+        if (NW == 8 && threadIdx.x >= 256) bring<true>(a, kr, begin - 1, end, 1, b);
     }
     // In its second phase of step t group g brings keys t + 1 + g and values t + g: nobody reads their buffers in that phase or the
     // one beside it.  Then it asks for the next ones.
+    template <bool CAREFUL>
     __device__ __forceinline__ void bring(const AttendArgs &a, const KeyRange &kr, int step, int end, int late, TileBuffers<D, NW, PLAID_SOURCE_PAGED> &b)
     {
         const int tile = step + late;
         if (tile + 1 < end) store_k(b, tile + 1);
-        if (tile < end) store_v(b, tile);
+        if (tile < end) store_v<CAREFUL>(kr, b, tile);
         if (tile + 2 < end) load_k(a, kr, tile + 2);
         if (tile + 1 < end) load_v(a, kr, tile + 1);
     }
@@ -336,6 +360,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         limit = a.causal && there ? (int)clamp64(all - tokens + token + 1, 0, kr.len) : kr.len;
         reach = a.causal ? (int)clamp64(all - tokens + last_token + 1, 0, kr.len) : kr.len;
         kr.len = reach;
+        kr.least = a.causal ? (int)clamp64(all - tokens + row_token(a, tp.tile * ROWS) + 1, 0, reach) : reach;
     } else {
         kr.base = clamp64(uniform_load(a.k_offsets + tp.r), 0, a.num_keys);
         kr.len = (int)(clamp64(uniform_load(a.k_offsets + tp.r + 1), kr.base, a.num_keys) - kr.base);
@@ -425,8 +450,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         for (int i = 0; i < 16; ++i) sums[i & 3] += s[0][i] + s[1][i];
         l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     };
-    auto weights = [&](int step) {
-        if constexpr (SRC == PLAID_SOURCE_DENSE) stage.bring(a, kr, step, end, late, lds);
+    auto weights = [&](int step, auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        if constexpr (SRC == PLAID_SOURCE_DENSE) stage.template bring<CAREFUL>(a, kr, step, end, late, lds);
         else stage.before(step, lds);
         float top;
         if constexpr (SRC == PLAID_SOURCE_BIAS) {
@@ -483,7 +509,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             }
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = round8<DT>(s[i >> 1], i & 1);
-        if constexpr (SRC != PLAID_SOURCE_DENSE) stage.bring(a, kr, step, end, late, lds);
+        if constexpr (SRC != PLAID_SOURCE_DENSE) stage.template bring<CAREFUL>(a, kr, step, end, late, lds);
     };
     if (begin < end) {
         before_scores(begin);
@@ -491,8 +517,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         for (int i = 0; i < EARLY; ++i) early[i] = key_operand(begin, i);
         scores(begin);
         phase_end(false);
-        for (int step = begin; step + 1 < end; ++step) {
-            weights(step);
+        auto both_phases = [&](int step, auto careful) {
+            weights(step, careful);
             phase_end(true);
             // products go before the other group's instructions (382 us in place of 391; paged 536 in place of 564)
             __builtin_amdgcn_s_setprio(1);
@@ -528,8 +554,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             __builtin_amdgcn_sched_group_barrier(0x008, EARLY, 0);
             phase_end(false);
             __builtin_amdgcn_s_setprio(0);
-        }
-        weights(end - 1);
+        };
+        int step = begin;
+        if constexpr (SRC == PLAID_SOURCE_PAGED)  // the tiles of values that a step stores: its own and the next one
+            for (; step + 1 < end && (step + 2) * MANY_KEYS <= kr.least; ++step) both_phases(step, std::false_type());
+        for (; step + 1 < end; ++step) both_phases(step, std::true_type());
+        weights(end - 1, std::true_type());
         phase_end(true);
         add_weights();
         add_values(end - 1, 0, 4);
@@ -537,6 +567,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
 
+    if constexpr (SRC == PLAID_SOURCE_PAGED) {
+        if (begin < end) {
+#pragma unroll
+            for (int dt = 0; dt < DT_TILES; ++dt)
+                if (lds.bad[dt] < limit) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[dt][i] = NAN;
+                }
+        }
+    }
     l = sum_halves(l);
     if (!there) return;
     const int64_t out_row = (tp.begin + token) * a.heads + head;

@@ -77,3 +77,32 @@ def test_numbers_that_are_not_finite_in_masked_keys(pl):  # noqa: F811
 def test_scores_of_hundreds(pl, dim):  # noqa: F811
     _check_cross(pl, [300, 270], [700, 333], 16, 2, dim, BF, gain=20.0, train=False)
     _check_cross(pl, [300, 270], [700, 333], 16, 2, dim, HF, _bias(1033, 2, HF), gain=20.0, train=False)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads,m", [(2, 5), (2, 40), (16, 600)])
+def test_what_is_not_finite_reaches_later_tokens_only(pl, dim, heads, m):  # noqa: F811
+    """A key or a value of a prompt's token that is not finite: earlier tokens do not see it, later ones do, where it is."""
+    kv, bs, n = 2, 16, m + 70
+    g = torch.Generator().manual_seed(m)
+    q, k, v = (torch.randn(x, h, dim, generator=g).to(BF).to("cuda:0") for x, h in ((m, heads), (n, kv), (n, kv)))
+    at_k, at_v = n - m + m // 2, n - m + 2 * m // 3
+    k[at_k, 0, 3] = float("nan")
+    v[at_v, 1, dim - 1] = float("inf")
+    blocks = -(-n // bs)
+    cache = pl.PagedCache.empty(blocks, bs, kv, dim, BF)
+    slots = torch.arange(n, device="cuda:0")
+    table, lengths = torch.arange(blocks, device="cuda:0", dtype=torch.int32)[None], torch.tensor([n], device="cuda:0", dtype=torch.int32)
+    offsets = torch.tensor([0, m], device="cuda:0")
+    pl.plaid_cache_write(cache, k, v, slots)
+    out = pl.plaid_cached_attention(q, cache, table, lengths, offsets).float()
+    clean = k.clone(), v.clone()
+    clean[0][at_k, 0, 3] = 0.0
+    clean[1][at_v, 1, dim - 1] = 0.0
+    pl.plaid_cache_write(cache, *clean, slots)
+    want = pl.plaid_cached_attention(q, cache, table, lengths, offsets).float()
+    first, second = heads // kv, slice(heads // kv, heads)
+    assert torch.equal(out[:m // 2, :first], want[:m // 2, :first]) and torch.isnan(out[m // 2:, :first]).all()
+    seen = 2 * m // 3
+    assert torch.equal(out[:seen, second], want[:seen, second])
+    assert torch.isnan(out[seen:, second, dim - 32:]).all() and torch.equal(out[:, second, :dim - 32], want[:, second, :dim - 32])
