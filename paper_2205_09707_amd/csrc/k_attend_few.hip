@@ -13,6 +13,10 @@
 // uneven the requests are.  (Where no request has many keys a workgroup of twice the waves takes a tile, and there is nothing to
 // join: one launch in place of two.)  A worker's stretch is a tail of a tile, whole tiles and a head of one: whole tiles it finishes,
 // the two others leave their sums in its two places, and join_workers_kernel adds them up in the order of the line.
+//
+// Bound by reading: 64 contexts of 1 to 8192 tokens in the cache, 8 key heads of 128 (279 MB): 59 us = 4.7 TB/s and 7.5 of joining, which is
+// a chain of loads by 64 x 8 workgroups; 4 of 115 000 (523 MB): 99 = 5.3 TB/s and 10; 4 x 65 000 dense keys with biases (1.07 GB): 195 = 5.5
+// TB/s and 9.5.  Twice the workers: 65.5 in place of 63.4, and 29 in place of 21 for one context of 20 000.
 
 template <int SRC>
 __device__ __forceinline__ int64_t key_count(const AttendArgs &a, int r, int64_t &base)
@@ -420,7 +424,10 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
                         for (int t = 0; t < 4; ++t) {
                             const int byte = t * KS + g;  // scale bytes [token][group]
                             const float power = scale_power(x.vs[c][byte >> 2], byte & 3);
-                            y[t] = t == 0 ? codes2<DT, 0>(w, power) : t == 1 ? codes2<DT, 1>(w, power) : t == 2 ? codes2<DT, 2>(w, power) : codes2<DT, 3>(w, power);
+                            y[t] = t == 0   ? codes2<DT, 0>(w, power)
+                                   : t == 1 ? codes2<DT, 1>(w, power)
+                                   : t == 2 ? codes2<DT, 2>(w, power)
+                                            : codes2<DT, 3>(w, power);
                         }
                         lo[2 * c] = (int)__builtin_amdgcn_perm(y[1], y[0], 0x05040100), lo[2 * c + 1] = (int)__builtin_amdgcn_perm(y[3], y[2], 0x05040100);
                         hi[2 * c] = (int)__builtin_amdgcn_perm(y[1], y[0], 0x07060302), hi[2 * c + 1] = (int)__builtin_amdgcn_perm(y[3], y[2], 0x07060302);
@@ -595,6 +602,7 @@ static void launch_source(hipStream_t st, const AttendArgs &a, int source, int w
 }
 void plaid_launch_attend_few(hipStream_t st, const AttendArgs &a, int dtype, int head_dim, int source, int workers, int64_t tiles)
 {
-    if (dtype == PLAID_BF16) head_dim == 64 ? launch_source<PLAID_BF16, 64>(st, a, source, workers, tiles) : launch_source<PLAID_BF16, 128>(st, a, source, workers, tiles);
+    if (dtype == PLAID_BF16)
+        head_dim == 64 ? launch_source<PLAID_BF16, 64>(st, a, source, workers, tiles) : launch_source<PLAID_BF16, 128>(st, a, source, workers, tiles);
     else head_dim == 64 ? launch_source<PLAID_FP16, 64>(st, a, source, workers, tiles) : launch_source<PLAID_FP16, 128>(st, a, source, workers, tiles);
 }

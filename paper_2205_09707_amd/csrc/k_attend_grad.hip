@@ -40,13 +40,19 @@ __device__ __forceinline__ float request_shift(const AttendArgs &a, int64_t row0
     return c == -INFINITY ? 0.0f : c;
 }
 
-// Both kernels run in phases like the forward one (k_attend_many.hip): products on one side, exponentials on the other, two groups
-// of waves a phase apart, what they read on its way into LDS steps before (the first group asks for it).
+// What the rows bring (-lse / scale, -delta) and the keys' biases over the scale are what the matrix instruction adds the products to;
+// a weight then takes one multiply-add and an exponential.  P and dS round to the type before they are multiplied again.
+// Measured on 16 requests of 456 tokens x 16 heads, 6250 keys of 4 heads, D = 128, biases: grad_k 830 us (746 GFLOP, 0.90 PFLOP/s),
+// grad_q 545 (560 GFLOP, 1.03 PFLOP/s), delta 12 (180 MB, 4.6 TB/s with the statistics).  Bound by products and what feeds them: without
+// exponentials both together took 1454 in place of 1522, without loads 1298.  Both in one launch are no faster (the same for short
+// answers, 1684 in place of 1565 for these).
 
 // --- gradients of keys and values ---------------------------------------------------------------------------------------------
 // A wave of 32 keys would hold their keys, values and both sums, 192 registers, before it multiplies anything.  So two waves of
 // one SIMD share 32 keys: the first forms P (keys and the sum dv in registers), the second, a phase behind, takes P from LDS and
 // forms dS (values and the sum dk in registers).  Each does half of the products; P, in 32 bits, costs a fifth of the traffic in LDS.
+// The two kinds run in phases like the forward kernel's groups (k_attend_many.hip), products on one side, exponentials on the other;
+// the first kind asks for q, the second for dO, two steps ahead.
 template <int NW>
 struct GradK {
     static constexpr int PAIRS = NW / 2, KEYS = PAIRS * 32, SHIFT = NW == 8 ? 7 : 6, ROWS = NW == 8 ? 64 : 32;  // rows of a step
@@ -73,7 +79,8 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     const WorkPlace w = work_place(a, tiles, splits);
     const int head = w.head, split = w.split;
     const int of = min(lane, a.n - 1);
-    const TilePlace tp = a.n <= SORTED_REQUESTS ? find_sorted_tile(a.k_offsets, a.n, a.num_keys, 1, K::SHIFT, w.place, (int)(a.q_offsets[of + 1] - a.q_offsets[of]))
+    const int work = (int)(a.q_offsets[of + 1] - a.q_offsets[of]);
+    const TilePlace tp = a.n <= SORTED_REQUESTS ? find_sorted_tile(a.k_offsets, a.n, a.num_keys, 1, K::SHIFT, w.place, work)
                                                 : find_tile(a.k_offsets, a.n, a.num_keys, 1, K::SHIFT, w.place);
     if (tp.r < 0) return;
     const int len = (int)(tp.end - tp.begin);
@@ -295,7 +302,9 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
 }
 
 // --- gradients of queries -----------------------------------------------------------------------------------------------------
-// A wave owns 32 rows: q, dO and the sum dq in registers, 32 keys a step.  For a request of at most 32 keys one step sees all of a
+// A wave owns 32 rows: q, dO and the sum dq in registers, 32 keys a step.  Workgroups of four waves, two on a compute unit, so that one
+// multiplies while the other forms exponentials: 545 us in place of 650 for eight waves in phases at D = 128, 934 in place of 1010 for
+// both gradients at 64.  For a request of at most 32 keys one step sees all of a
 // row, and delta is taken as the sum of P dP: out, rounded to the type, would give it too coarsely where few keys are averaged
 // (two keys in bf16: 4 of 1000 off in dq and dk, so 2.5).
 #define GRAD_KEYS 32
@@ -320,7 +329,8 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
     const WorkPlace w = work_place(a, tiles, splits);
     const int head_kv = w.head, split = w.split;
     const int of = min(lane, a.n - 1);
-    const TilePlace tp = a.n <= SORTED_REQUESTS ? find_sorted_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place, (int)(a.k_offsets[of + 1] - a.k_offsets[of]))
+    const int work = (int)(a.k_offsets[of + 1] - a.k_offsets[of]);
+    const TilePlace tp = a.n <= SORTED_REQUESTS ? find_sorted_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place, work)
                                                 : find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place);
     if (tp.r < 0) return;
     const int tokens = (int)(tp.end - tp.begin), rows = tokens * a.group;
@@ -394,7 +404,9 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
     i32x4 r[2];
     constexpr int EARLY = 4, READS = 2 * (D / 16);  // operands that are read before the products of add end
     i32x4 early[EARLY];
-    auto operand = [&](int step, int i) { return i % 2 ? lds_rows<D>(lds.v[(uint32_t)step % L::V_TILES], 0, i / 2) : lds_rows<D>(lds.k[(uint32_t)step % L::K_TILES], 0, i / 2); };
+    auto operand = [&](int step, int i) {
+        return lds_rows<D>(i % 2 ? lds.v[(uint32_t)step % L::V_TILES] : lds.k[(uint32_t)step % L::K_TILES], 0, i / 2);
+    };
     auto before_form = [&](int step) {
         if constexpr (BIAS) {
             typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
@@ -602,6 +614,7 @@ static void launch(hipStream_t st, const GradArgs &g, int q_splits, int k_waves,
 }
 void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_splits, int k_waves, int k_splits)
 {
-    if (dtype == PLAID_BF16) head_dim == 64 ? launch<PLAID_BF16, 64>(st, g, q_splits, k_waves, k_splits) : launch<PLAID_BF16, 128>(st, g, q_splits, k_waves, k_splits);
+    if (dtype == PLAID_BF16)
+        head_dim == 64 ? launch<PLAID_BF16, 64>(st, g, q_splits, k_waves, k_splits) : launch<PLAID_BF16, 128>(st, g, q_splits, k_waves, k_splits);
     else head_dim == 64 ? launch<PLAID_FP16, 64>(st, g, q_splits, k_waves, k_splits) : launch<PLAID_FP16, 128>(st, g, q_splits, k_waves, k_splits);
 }

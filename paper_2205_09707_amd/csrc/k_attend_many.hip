@@ -8,8 +8,18 @@
 // A wave owns 32 rows.  It computes s^T = k q^T, so that a lane holds one row (column l % 32 of the result) and the two halves
 // of the wave half of its keys each: the maximum and the sum need one exchange, and the result's registers, rounded, are
 // already the operand of o^T = v^T p^T (rows of v^T come from LDS by the transposing read, or lie transposed there).  q stays
-// in registers, keys and values of 64 keys at a time go through LDS twice buffered; the next tile's loads are in flight while
-// this one is multiplied.  m lags behind the maximum by up to 2^8: o is rescaled only where it would fall further back.
+// in registers; keys and values of 64 keys at a time go through LDS, dense ones straight from memory up to three tiles ahead, those of
+// the cache as codes in registers that are turned into values on the way.  m lags behind the maximum by up to 2^8: o is rescaled
+// only where it would fall further back.  Biases, divided by the scale, are what the matrix instruction adds the products to, so
+// that a biased score costs no instruction of its own (565 us in place of 614, below).
+// The weights round to the type before they multiply the values (half of the matrix rate is lost with more bits); their sum does not.
+//
+// What bounds it: one group's vector instructions (exponential 16 cycles, multiply-add, half a maximum, half a rounding and one addition a
+// score) against the other's products.  Measured: 16 requests of 456 tokens x 16 heads on 6250 keys of 4 heads, D = 128 (373 GFLOP):
+// 373 us without biases, 433 with = 1.00 and 0.86 PFLOP/s; 381 without products first, 395 before addresses of loads were kept in
+// registers.  6 prompts of 850 tokens x 32 heads behind 4750 in the cache (419 GFLOP): 475 us = 0.88 PFLOP/s; what is left there is the
+// codes' way into values, which every 256 rows pay.
+//
 // Tiles that lie in LDS at a time, and how many tiles ahead of the weights' one keys and values are asked for.  With two groups of
 // waves (see below) a tile of keys is read in two phases and one of values in the two after those; a buffer is filled anew from
 // the second phase of a step on.
@@ -64,7 +74,8 @@ struct Stage {
         }
     }
     // Keys past the end repeat the last one.  The tiles after the last repeat that one, so that a phase's number of loads is fixed.
-    __device__ __forceinline__ void load(const KeyRange &kr, const char *first, uint32_t token, const uint32_t (&rows)[N], int tile, uint32_t to, uint64_t masked)
+    __device__ __forceinline__ void load(const KeyRange &kr, const char *first, uint32_t token, const uint32_t (&rows)[N], int tile, uint32_t to,
+                                         uint64_t masked)
     {
         const char *base = first + (uint64_t)(uint32_t)(tile * MANY_KEYS) * token;
         const uint32_t last = (uint32_t)min(kr.len - 1 - tile * MANY_KEYS, MANY_KEYS - 1) * token;
@@ -473,7 +484,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             }
         } else {
             bool whole = (step + 1) * MANY_KEYS <= least;
-            if constexpr (SRC == PLAID_SOURCE_PAGED) whole = whole && (lds.cell[step & 3][0] & lds.cell[step & 3][1] & lds.cell[step & 3][2] & lds.cell[step & 3][3]);
+            if constexpr (SRC == PLAID_SOURCE_PAGED) {
+                const int *held = lds.cell[step & 3];
+                whole = whole && (held[0] & held[1] & held[2] & held[3]);
+            }
             if (!whole) {
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
@@ -653,6 +667,7 @@ static void launch_type(hipStream_t st, const AttendArgs &a, int source, int wav
 
 void plaid_launch_attend_many(hipStream_t st, const AttendArgs &a, int dtype, int head_dim, int source, int waves, int64_t tiles)
 {
-    if (dtype == PLAID_BF16) head_dim == 64 ? launch_type<PLAID_BF16, 64>(st, a, source, waves, tiles) : launch_type<PLAID_BF16, 128>(st, a, source, waves, tiles);
+    if (dtype == PLAID_BF16)
+        head_dim == 64 ? launch_type<PLAID_BF16, 64>(st, a, source, waves, tiles) : launch_type<PLAID_BF16, 128>(st, a, source, waves, tiles);
     else head_dim == 64 ? launch_type<PLAID_FP16, 64>(st, a, source, waves, tiles) : launch_type<PLAID_FP16, 128>(st, a, source, waves, tiles);
 }

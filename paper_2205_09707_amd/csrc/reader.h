@@ -247,7 +247,8 @@ __device__ __forceinline__ TilePlace find_tile(const int64_t *off, int n, int64_
 
 // The same with the requests in the order of `work`, what a tile of request r (of lane r) takes, the largest first, and a request's
 // last tile, which sees the most of a causal mask, first: what starts last is short, so that all of the chip ends at about the same time.
-// Only for n <= 64: with more requests there are so many tiles that their order matters little.
+// 6 prompts behind contexts: 498 us in place of 531; a training step of 16 long answers: 1981 in place of 2050.  Only for n <= 64, a lane for
+// each request: with more of them there are many rounds of tiles, whose order matters less.
 #define SORTED_REQUESTS 64
 __device__ __forceinline__ TilePlace find_sorted_tile(const int64_t *off, int n, int64_t rows, int per_token, int tile_shift, int64_t p, int work)
 {
@@ -382,7 +383,8 @@ static __device__ const i32x4 zero_row[16] = {};
 
 // 16 (4) bytes of every lane, from base + off, into the 1024 (256) bytes of LDS at `to` (the same for all lanes), lane after lane.
 // There is no result in registers and the compiler does not count these loads: it would have every transposing read of LDS wait
-// for all of them.  (They go by register m0, which nothing else in these kernels uses.)  What they bring is waited for with wait_loads, before the barrier that lets it be read and before the end.
+// for all of them.  (They go by register m0, which nothing else in these kernels uses.)  What they bring is waited for with
+// wait_loads, before the barrier that lets it be read and before the end.
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t to)
 {

@@ -82,12 +82,14 @@ Plan plan_forward(const plaid_attention &a, int source, int64_t keys, int64_t lo
     Plan p = {};
     const int64_t group = a.heads / a.kv_heads, tokens = ceil_div(a.num_queries, a.n), rows = tokens * group;
     p.tiles = a.num_queries * group / FEW_ROWS + a.n;
-    p.few = few_rows(rows, a.n, a.kv_heads, usual, a.head_dim, source) && p.tiles * (longest / FEW_KEYS + 1) < INT32_MAX;  // its counts of steps are 32 bits wide
+    // its counts of steps are 32 bits wide
+    p.few = few_rows(rows, a.n, a.kv_heads, usual, a.head_dim, source) && p.tiles * (longest / FEW_KEYS + 1) < INT32_MAX;
     if (p.few) {
         // One workgroup for each tile, no workers, nothing to join: 9.4 us in place of 11.0 at 1024 keys, 14.8 in place of 11.4 at 2048
-        // for one request of 8 key heads; 34.6 in place of 39.5 at 2048 for 64 of them.  Packed keys: a request may have twice the mean.
+        // for one request of 8 key heads; 34.6 in place of 39.5 at 2048 for 64 of them.  Packed keys: a request is taken to have at most
+        // twice the mean, unless that could make it wait for eight times as many (75 us at 8192).
         const int64_t most = p.tiles * a.kv_heads >= 128 ? 2048 : 1024;
-        if (longest <= most || 2 * usual <= most) return p;
+        if (longest <= most || (2 * usual <= most && longest <= 8 * most)) return p;
         const int64_t line = (ceil_div(keys, FEW_KEYS) + a.n) * ceil_div(rows < 1 ? 1 : rows, FEW_ROWS);
         const int64_t w = ceil_div(UNITS * FEW_PER_SIMD(a.head_dim, source), a.kv_heads);
         p.workers = (int)(w < line ? w : line);
@@ -165,7 +167,8 @@ int check_keys(const plaid_attention *a)
 }
 int check_workspace(const void *p, int64_t have, int64_t need)
 {
-    if (need > 0 && (!p || misaligned(p, 16) || have < need)) FAIL("workspace: %lld bytes, 16-byte aligned, are needed, %lld given", (long long)need, (long long)have);
+    if (need > 0 && (!p || misaligned(p, 16) || have < need))
+        FAIL("workspace: %lld bytes, 16-byte aligned, are needed, %lld given", (long long)need, (long long)have);
     return PLAID_OK;
 }
 

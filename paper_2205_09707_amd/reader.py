@@ -289,6 +289,6 @@ def plaid_cross_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torc
     need = ct.c_int64(0)
     _p._check(lib.plaid_cross_attention_workspace(ct.byref(a), 1, ct.byref(need)))
     work, ptr = _workspace(need.value, dev)
-    _p._check(lib.plaid_cross_attention_backward(ct.byref(a), d_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), None if dbias is None else dbias.data_ptr(), ptr, need.value,
-                                                 *_where(dev)))
+    _p._check(lib.plaid_cross_attention_backward(ct.byref(a), d_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                                 None if dbias is None else dbias.data_ptr(), ptr, need.value, *_where(dev)))
     return dq, dk, dv, dbias
