@@ -537,32 +537,45 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
         }
 }
 
-// out[i] = sum over the splits of part[s][i], in their order, for the rows that a request owns.
+// What the kernels above left in parts, in one launch: out[i] = sum over the parts of part[s][i], in their order, for the rows that a
+// request owns.  dbias is a sum over splits and key heads.
+struct Sums {
+    const float *part;
+    char *out;
+    int64_t count, per_row;  // values, values of a row: 1 a thread or a multiple of 4
+    const int64_t *offsets;
+    int32_t parts, n;
+    uint32_t groups;         // workgroups up to this sum's last one
+};
+struct AllSums {
+    Sums of[4];
+};
 template <int DT>
-__global__ __launch_bounds__(256) void add_splits_kernel(const float *part, char *out, int64_t count, int splits, const int64_t *offsets, int n,
-                                                         int64_t per_row)
+__global__ __launch_bounds__(256) void add_parts_kernel(AllSums all)
 {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= count) return;
-    const int64_t row = i / per_row;
-    if (row < offsets[0] || row >= offsets[n]) return;
-    f32x4 sum{0, 0, 0, 0};
-    for (int s = 0; s < splits; ++s) {
-        const f32x4 x = *(const f32x4 *)(part + s * count + i);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += x[e];
+    int which = 0;
+    while (blockIdx.x >= all.of[which].groups) ++which;
+    const Sums &x = all.of[which];
+    const int64_t at = (int64_t)(blockIdx.x - (which ? all.of[which - 1].groups : 0)) * 256 + threadIdx.x;
+    if (x.per_row == 1) {
+        if (at >= x.count || at < x.offsets[0] || at >= x.offsets[x.n]) return;
+        float sum = 0.0f;
+#pragma unroll 4
+        for (int s = 0; s < x.parts; ++s) sum += x.part[s * x.count + at];
+        store16<DT>(x.out + 2 * at, sum);
+        return;
     }
-    *(i32x2 *)(out + 2 * i) = i32x2{pack2<DT>(sum[0], sum[1]), pack2<DT>(sum[2], sum[3])};
-}
-// dbias[j] = sum over splits and key heads.
-template <int DT>
-__global__ __launch_bounds__(256) void add_bias_kernel(const float *part, char *out, int64_t keys, int parts, const int64_t *offsets, int n)
-{
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= keys || i < offsets[0] || i >= offsets[n]) return;
-    float sum = 0.0f;
-    for (int s = 0; s < parts; ++s) sum += part[s * keys + i];
-    store16<DT>(out + 2 * i, sum);
+    const int64_t i = at * 4;
+    if (i >= x.count) return;
+    const int64_t row = i / x.per_row;
+    if (row < x.offsets[0] || row >= x.offsets[x.n]) return;
+    f32x4 sum{0, 0, 0, 0};
+    for (int s = 0; s < x.parts; ++s) {
+        const f32x4 y = *(const f32x4 *)(x.part + s * x.count + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += y[e];
+    }
+    *(i32x2 *)(x.out + 2 * i) = i32x2{pack2<DT>(sum[0], sum[1]), pack2<DT>(sum[2], sum[3])};
 }
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -588,12 +601,18 @@ static void launch(hipStream_t st, const GradArgs &g, int q_splits, int k_waves,
 {
     const AttendArgs &a = g.a;
     const int64_t q_values = a.num_queries * a.heads * D, k_values = a.num_keys * a.kv_heads * D;
+    AllSums all = {};
+    uint32_t groups = 0;
+    int sums = 0;
+    auto add = [&](const float *part, char *out, int64_t count, int64_t per_row, int parts, const int64_t *offsets) {
+        if (!out) return;
+        groups += (uint32_t)ceil_div(count, per_row == 1 ? 256 : 1024);
+        all.of[sums++] = {part, out, count, per_row, offsets, parts, a.n, groups};
+    };
     if (a.num_queries > 0) delta_kernel<DT, D><<<dim3((unsigned)ceil_div(q_values / 8, 256)), dim3(256), 0, st>>>(g);
     if (g.dq && a.num_queries > 0) {
         launch_q<DT, D>(st, g, q_splits);
-        if (q_splits > 1)
-            add_splits_kernel<DT><<<dim3((unsigned)ceil_div(q_values / 4, 256)), dim3(256), 0, st>>>(g.dq_part, g.dq, q_values, q_splits, a.q_offsets, a.n,
-                                                                                                    (int64_t)a.heads * D);
+        if (q_splits > 1) add(g.dq_part, g.dq, q_values, (int64_t)a.heads * D, q_splits, a.q_offsets);
     }
     if ((g.dk || g.dv || g.dbias) && a.num_keys > 0) {
         if constexpr (D == 128) {
@@ -603,14 +622,12 @@ static void launch(hipStream_t st, const GradArgs &g, int q_splits, int k_waves,
             launch_k<DT, D, 4>(st, g, k_splits);
         }
         if (k_splits > 1) {
-            const dim3 grid((unsigned)ceil_div(k_values / 4, 256));
-            if (g.dk) add_splits_kernel<DT><<<grid, dim3(256), 0, st>>>(g.dk_part, g.dk, k_values, k_splits, a.k_offsets, a.n, (int64_t)a.kv_heads * D);
-            if (g.dv) add_splits_kernel<DT><<<grid, dim3(256), 0, st>>>(g.dv_part, g.dv, k_values, k_splits, a.k_offsets, a.n, (int64_t)a.kv_heads * D);
+            add(g.dk_part, g.dk, k_values, (int64_t)a.kv_heads * D, k_splits, a.k_offsets);
+            add(g.dv_part, g.dv, k_values, (int64_t)a.kv_heads * D, k_splits, a.k_offsets);
         }
-        if (g.dbias)
-            add_bias_kernel<DT><<<dim3((unsigned)ceil_div(a.num_keys, 256)), dim3(256), 0, st>>>(g.dbias_part, g.dbias, a.num_keys, k_splits * a.kv_heads,
-                                                                                                a.k_offsets, a.n);
+        add(g.dbias_part, g.dbias, a.num_keys, 1, k_splits * a.kv_heads, a.k_offsets);
     }
+    if (groups > 0) add_parts_kernel<DT><<<dim3(groups), dim3(256), 0, st>>>(all);
 }
 void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_splits, int k_waves, int k_splits)
 {
