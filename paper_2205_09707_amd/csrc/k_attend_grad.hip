@@ -530,7 +530,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
         for (int i = 0; i < 4; ++i) {
             f32x4 x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = dq[t][4 * i + e] * g.factor;
+            for (int e = 0; e < 4; ++e) x[e] = counts ? dq[t][4 * i + e] * g.factor : 0.0f;  // without a key: whatever q holds
             const int d = 32 * t + 8 * i + 4 * h;
             if (splits > 1) *(f32x4 *)(g.dq_part + ((int64_t)split * a.num_queries * a.heads + at) * D + d) = x;
             else *(i32x2 *)(g.dq + (at * D + d) * 2) = i32x2{pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])};

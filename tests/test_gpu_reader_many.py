@@ -106,3 +106,23 @@ def test_what_is_not_finite_reaches_later_tokens_only(pl, dim, heads, m):  # noq
     seen = 2 * m // 3
     assert torch.equal(out[:seen, second], want[:seen, second])
     assert torch.isnan(out[seen:, second, dim - 32:]).all() and torch.equal(out[:, second, :dim - 32], want[:, second, :dim - 32])
+
+
+@pytest.mark.parametrize("m", [3, 300])
+def test_a_row_without_keys_has_no_gradient(pl, m):  # noqa: F811
+    """Every key of the first request is masked and its queries are not finite: zeros, and nothing of it reaches the second request."""
+    g = torch.Generator().manual_seed(m)
+    q, k, v = (torch.randn(n, 4, 64, generator=g).to(BF).to("cuda:0") for n in (2 * m, 130, 130))
+    d_out = torch.randn(2 * m, 4, 64, generator=g).to(BF).to("cuda:0")
+    bias = torch.zeros(130, dtype=BF, device="cuda:0")
+    bias[:50] = -float("inf")
+    offsets = torch.tensor([0, m, 2 * m], device="cuda:0"), torch.tensor([0, 50, 130], device="cuda:0")
+    results = []
+    for value in (0.0, float("nan"), float("inf")):
+        q[:m] = value
+        out, lse = pl.plaid_cross_attention(q, k, v, *offsets, key_bias=bias, return_lse=True)
+        results.append((out, *pl.plaid_cross_attention_backward(d_out, q, k, v, out, lse, *offsets, key_bias=bias)))
+    for got in results:
+        for x, y in zip(got, results[0]):
+            assert torch.equal(x, y) and torch.isfinite(x).all()
+        assert (got[0][:m] == 0).all() and (got[1][:m] == 0).all() and all((x[:50] == 0).all() for x in got[2:])
