@@ -7,6 +7,7 @@ torch's current stream of the tensors' device.  Nothing is kept from one call fo
 from __future__ import annotations
 
 import ctypes as ct
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -60,22 +61,23 @@ def _vector(t: torch.Tensor, name: str, dtype, device: torch.device, size: Optio
     return t.contiguous()
 
 
-def _rows(t: torch.Tensor) -> torch.Tensor:
-    """The tensor itself where the kernels can read its strides, else a contiguous copy."""
-    _, heads, dim = t.shape
-    s = t.stride()
-    if t.numel() and (s[2] != 1 or t.data_ptr() % 16 or (t.shape[0] > 1 and (s[0] % 8 or s[0] >= 1 << 24)) or (heads > 1 and (s[1] % 8 or s[1] >= 1 << 24))):
-        t = t.contiguous() if not t.is_contiguous() else t.clone(memory_format=torch.contiguous_format)
-    return t
-
-
-def _strides(t: torch.Tensor) -> Tuple[int, int]:
+def _rows(t: torch.Tensor) -> Tuple[torch.Tensor, int, int]:
+    """The tensor itself where the kernels can read its strides, else a contiguous copy, and its strides of tokens and heads."""
     n, heads, dim = t.shape
-    return (t.stride(0) if n > 1 else heads * dim), (t.stride(1) if heads > 1 else dim)
+    token, head, one = t.stride()
+    if n < 2:
+        token = heads * dim
+    if heads < 2:
+        head = dim
+    if one != 1 or token % 8 or head % 8 or token >= 1 << 24 or head >= 1 << 24 or t.data_ptr() % 16:
+        if t.numel():
+            t = t.contiguous() if not t.is_contiguous() else t.clone(memory_format=torch.contiguous_format)
+        token, head = heads * dim, dim
+    return t, token, head
 
 
 def _like(t: torch.Tensor) -> torch.Tensor:
-    return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _workspace(bytes_: int, device: torch.device):
@@ -140,7 +142,7 @@ def plaid_block_tables(lengths: torch.Tensor, added: torch.Tensor, table: torch.
     _p._check(lib.plaid_block_tables_workspace(n, capacity, ct.byref(need)))
     room = max(capacity, 0)
     offsets = torch.empty(n + 1, dtype=torch.int64, device=dev)
-    totals = torch.empty(n, dtype=torch.int32, device=dev)
+    totals = torch.empty_like(lengths)
     positions = torch.empty(room, dtype=torch.int32, device=dev)
     slots = torch.empty(room, dtype=torch.int64, device=dev)
     wanted = torch.empty(1, dtype=torch.int64, device=dev)
@@ -160,9 +162,10 @@ def plaid_cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots
         if tuple(_is(t, name, cache.dtype, 3, dev).shape) != shape:
             raise ValueError(f"{name} must have the shape {shape}, got {tuple(t.shape)}")
     slots = _vector(slots, "slots", torch.int64, dev)
-    k, v = _rows(k), _rows(v)
-    _p._check(_p.load_library().plaid_cache_write(ct.byref(cache._view()), k.data_ptr(), v.data_ptr(), *_strides(k), *_strides(v), slots.data_ptr(),
-                                                  slots.shape[0], *_where(dev)))
+    k, k_token, k_head = _rows(k)
+    v, v_token, v_head = _rows(v)
+    _p._check(_p.load_library().plaid_cache_write(ct.byref(cache._view()), k.data_ptr(), v.data_ptr(), k_token, k_head, v_token, v_head,
+                                                  slots.data_ptr(), slots.shape[0], *_where(dev)))
 
 
 def plaid_cache_read(cache: PagedCache, slots: torch.Tensor):
@@ -176,14 +179,21 @@ def plaid_cache_read(cache: PagedCache, slots: torch.Tensor):
     return k, v
 
 
+_PACKED = struct.Struct("5if2q4P6q4P")  # plaid_attention's fields: half the time of the structure's own constructor
+
+
 def _attention(q, k, v, key_bias, q_offsets, k_offsets, kv_heads, scale, out, lse) -> plaid_attention:
+    """q, k and v: what _rows gave (k and v None over a cache)."""
+    q, q_token, q_head = q
     tokens, heads, head_dim = q.shape
-    head = (_DTYPES[q.dtype], q_offsets.shape[0] - 1, heads, kv_heads, head_dim, head_dim ** -0.5 if scale is None else float(scale), tokens)
-    tail = (out.data_ptr(), None if lse is None else lse.data_ptr())
-    if k is None:
-        return plaid_attention(*head, 0, q.data_ptr(), None, None, None, *_strides(q), 0, 0, 0, 0, q_offsets.data_ptr(), None, *tail)
-    return plaid_attention(*head, k.shape[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), None if key_bias is None else key_bias.data_ptr(),
-                           *_strides(q), *_strides(k), *_strides(v), q_offsets.data_ptr(), k_offsets.data_ptr(), *tail)
+    keys = k_ptr = v_ptr = k_token = k_head = v_token = v_head = k_off = 0
+    if k is not None:
+        (k, k_token, k_head), (v, v_token, v_head) = k, v
+        keys, k_ptr, v_ptr, k_off = k.shape[0], k.data_ptr(), v.data_ptr(), k_offsets.data_ptr()
+    return plaid_attention.from_buffer_copy(_PACKED.pack(
+        _DTYPES[q.dtype], q_offsets.shape[0] - 1, heads, kv_heads, head_dim, head_dim ** -0.5 if scale is None else float(scale), tokens, keys,
+        q.data_ptr(), k_ptr, v_ptr, 0 if key_bias is None else key_bias.data_ptr(), q_token, q_head, k_token, k_head, v_token, v_head,
+        q_offsets.data_ptr(), k_off, out.data_ptr(), 0 if lse is None else lse.data_ptr()))
 
 
 def _check_heads(q: torch.Tensor, kv_heads: int, head_dim: int) -> None:
@@ -217,11 +227,11 @@ def plaid_cached_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tens
         raise ValueError("table must have a row for each request")
     if table.shape[1] > 1 and table.stride(1) != 1:
         table = table.contiguous()
-    q = _rows(q)
+    rows = _rows(q)
     out = _like(q)
     lse = torch.empty(q.shape[:2] + (2,), dtype=torch.float32, device=dev) if return_lse else None
     lib = _p.load_library()
-    a = _attention(q, None, None, None, q_offsets, None, cache.kv_heads, scale, out, lse)
+    a = _attention(rows, None, None, None, q_offsets, None, cache.kv_heads, scale, out, lse)
     need = ct.c_int64(0)
     _p._check(lib.plaid_cached_attention_workspace(ct.byref(a), table.shape[1], cache.block_size, ct.byref(need)))
     work, ptr = _workspace(need.value, dev)
@@ -252,12 +262,12 @@ def plaid_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_o
     request r owns rows q_offsets[r] .. q_offsets[r+1]-1 and keys k_offsets[r] .. k_offsets[r+1]-1 (int64 [n+1]).  key_bias [keys]
     of q's dtype is added to the scores; -inf takes a key out.  Returns out like q (rows outside every request are not written),
     with return_lse also the two numbers a row that plaid_cross_attention_backward wants."""
-    q, k, v, q_offsets, k_offsets, key_bias = _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias)
+    rows, keys, values, q_offsets, k_offsets, key_bias = _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias)
     dev = q.device
     out = _like(q)
     lse = torch.empty(q.shape[:2] + (2,), dtype=torch.float32, device=dev) if return_lse else None
     lib = _p.load_library()
-    a = _attention(q, k, v, key_bias, q_offsets, k_offsets, k.shape[1], scale, out, lse)
+    a = _attention(rows, keys, values, key_bias, q_offsets, k_offsets, k.shape[1], scale, out, lse)
     need = ct.c_int64(0)
     _p._check(lib.plaid_cross_attention_workspace(ct.byref(a), 0, ct.byref(need)))
     work, ptr = _workspace(need.value, dev)
@@ -270,7 +280,7 @@ def plaid_cross_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torc
                                    scale: Optional[float] = None):
     """(dq, dk, dv, dbias) of plaid_cross_attention, from its outputs out and lse and the gradient d_out; contiguous, dbias None
     without key_bias.  Rows outside every request are not written."""
-    q, k, v, q_offsets, k_offsets, key_bias = _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias)
+    rows, keys, values, q_offsets, k_offsets, key_bias = _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias)
     dev = q.device
     for name, t in (("d_out", d_out), ("out", out)):
         if _is(t, name, q.dtype, 3, dev).shape != q.shape:
@@ -285,7 +295,7 @@ def plaid_cross_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torc
     dv = _like(k)
     dbias = torch.empty(k.shape[:1], dtype=q.dtype, device=dev) if key_bias is not None else None
     lib = _p.load_library()
-    a = _attention(q, k, v, key_bias, q_offsets, k_offsets, k.shape[1], scale, out, lse)
+    a = _attention(rows, keys, values, key_bias, q_offsets, k_offsets, k.shape[1], scale, out, lse)
     need = ct.c_int64(0)
     _p._check(lib.plaid_cross_attention_workspace(ct.byref(a), 1, ct.byref(need)))
     work, ptr = _workspace(need.value, dev)
