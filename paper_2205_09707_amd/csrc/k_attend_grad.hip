@@ -533,7 +533,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
             for (int e = 0; e < 4; ++e) x[e] = counts ? dq[t][4 * i + e] * g.factor : 0.0f;  // without a key: whatever q holds
             const int d = 32 * t + 8 * i + 4 * h;
             if (splits > 1) *(f32x4 *)(g.dq_part + ((int64_t)split * a.num_queries * a.heads + at) * D + d) = x;
-            else *(i32x2 *)(g.dq + (at * D + d) * 2) = i32x2{pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])};
+            else if (g.dq) *(i32x2 *)(g.dq + (at * D + d) * 2) = i32x2{pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])};
         }
 }
 
@@ -610,7 +610,8 @@ static void launch(hipStream_t st, const GradArgs &g, int q_splits, int k_waves,
         all.of[sums++] = {part, out, count, per_row, offsets, parts, a.n, groups};
     };
     if (a.num_queries > 0) delta_kernel<DT, D><<<dim3((unsigned)ceil_div(q_values / 8, 256)), dim3(256), 0, st>>>(g);
-    if (g.dq && a.num_queries > 0) {
+    // also without dq: what it finds out about delta is dk's and dbias's as well, which are the same whatever is asked for
+    if ((g.dq || g.dk || g.dbias) && a.num_queries > 0) {
         launch_q<DT, D>(st, g, q_splits);
         if (q_splits > 1) add(g.dq_part, g.dq, q_values, (int64_t)a.heads * D, q_splits, a.q_offsets);
     }
