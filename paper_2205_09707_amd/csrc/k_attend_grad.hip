@@ -76,7 +76,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     __shared__ __align__(16) GradKLds<D, NW> lds;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
     const int second = wave >= K::PAIRS, pair = second ? wave - K::PAIRS : wave;
-    const WorkPlace w = work_place(a, tiles, splits);
+    const WorkPlace w = work_place(a, tiles, splits, blockIdx.x);
     const int head = w.head, split = w.split;
     const int of = min(lane, a.n - 1);
     const int work = (int)(a.q_offsets[of + 1] - a.q_offsets[of]);
@@ -305,28 +305,41 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
 // A wave owns 32 rows: q, dO and the sum dq in registers, 32 keys a step.  Workgroups of four waves, two on a compute unit, so that one
 // multiplies while the other forms exponentials: 545 us in place of 650 for eight waves in phases at D = 128, 934 in place of 1010 for
 // both gradients at 64.  For a request of at most 32 keys one step sees all of a
-// row, and delta is taken as the sum of P dP: out, rounded to the type, would give it too coarsely where few keys are averaged
-// (two keys in bf16: 4 of 1000 off in dq and dk, so 2.5).
+// row, and delta is the sum of P dP over that of P.
+//
+// Other requests begin with delta = dO . out, whose error, that of an out rounded to the type, grows with |dO| |out| and not with dS: 4 of 1000
+// off in dq and dk where two keys of bf16 share the weight, 11 of 100 where one has 0.99 of it.  But the sum of dS over a row's keys is zero, so what
+// it comes to is that error.  It is added to delta, for grad_k_kernel as well, and where it is more than DELTA_OFF of the sum of |dS|, half of
+// what rounding dS costs, finish_kernel makes the rows' pass over the keys again.  Weights spread over tens of keys do not come near that.
 #define GRAD_KEYS 32
+#define DELTA_OFF(DT) ((DT) == PLAID_BF16 ? 0x1p-9f : 0x1p-12f)
 template <int D, bool BIAS>
 struct GradQLds {
     static constexpr int AHEAD = 3, K_TILES = AHEAD + 1, V_TILES = AHEAD;  // keys are read in two phases, values in one
     char k[K_TILES][GRAD_KEYS * D * 2], v[V_TILES][GRAD_KEYS * D * 2];
     float bias[BIAS ? 4 : 1][4][BIAS ? GRAD_KEYS : 4];  // each wave's own
     uint32_t raw[BIAS ? 4 : 1][4][64];                   // as they are loaded
+    float2 sums[256];                                    // of dS and |dS| over a lane's keys: there are no registers for them
+    int far[4];                                          // whether a wave has a row whose delta was too far off
 };
 
-template <int DT, int D, bool BIAS>
-__global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tiles, int splits)
+// Workgroup id of a launch's first or second pass.
+template <int DT, int D, bool BIAS, bool AGAIN>
+__device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, int splits, int id, GradQLds<D, BIAS> &lds)
 {
     using L = GradQLds<D, BIAS>;
     constexpr uint32_t TILE = GRAD_KEYS * D * 2;
     constexpr int ROWS = 128, SHIFT = 7, CHUNKS = D / 8, AT_ONCE = 512 / D, N = GRAD_KEYS / AT_ONCE / 4;
     constexpr uint16_t NONE = DT == PLAID_BF16 ? 0xff80 : 0xfc00;  // -infinity
     const AttendArgs &a = g.a;
-    __shared__ __align__(16) L lds;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
-    const WorkPlace w = work_place(a, tiles, splits);
+    if constexpr (AGAIN) {
+        if (splits == 1) {
+            const i32x4 far = uniform_load((const i32x4 *)g.far + id);
+            if (!(far[0] | far[1] | far[2] | far[3])) return;
+        }
+    }
+    const WorkPlace w = work_place(a, tiles, splits, id);
     const int head_kv = w.head, split = w.split;
     const int of = min(lane, a.n - 1);
     const int work = (int)(a.k_offsets[of + 1] - a.k_offsets[of]);
@@ -334,15 +347,32 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
                                                 : find_tile(a.q_offsets, a.n, a.num_queries, a.group, SHIFT, w.place);
     if (tp.r < 0) return;
     const int tokens = (int)(tp.end - tp.begin), rows = tokens * a.group;
-    const int64_t key0 = clamp64(uniform_load(a.k_offsets + tp.r), 0, a.num_keys);
-    const int len = (int)(clamp64(uniform_load(a.k_offsets + tp.r + 1), key0, a.num_keys) - key0);
-    const int steps = (len + GRAD_KEYS - 1) / GRAD_KEYS, share = (steps + splits - 1) / splits;
-    const int begin = split * share, end = min(steps, begin + share);
-
     const int row = tp.tile * ROWS + wave * 32 + (lane & 31);
     const bool there = row < rows;
     const int token = row_token(a, there ? row : 0), head = head_kv * a.group + (there ? row : 0) - token * a.group;
     const int64_t at = (tp.begin + token) * a.heads + head;
+    float minus_delta;
+    if constexpr (AGAIN) {
+        minus_delta = g.delta[at];
+        if (splits > 1) {  // the parts' sums
+            float off = 0.0f, size = 0.0f;
+#pragma unroll 4
+            for (int i = 0; i < splits; ++i) {
+                const float2 x = *(const float2 *)(g.row_part + 2 * ((int64_t)i * a.num_queries * a.heads + at));
+                off += x.x, size += x.y;
+            }
+            minus_delta -= off;
+            if (split == 0 && there && h == 0) g.delta_sum[at] = minus_delta;
+            const int far = uniform(__any(there && fabsf(off) > DELTA_OFF(DT) * size) ? 1 : 0);
+            if (lane == 0) lds.far[wave] = far;
+            lds_barrier();
+            if (!g.dq || !(lds.far[0] | lds.far[1] | lds.far[2] | lds.far[3])) return;
+        }
+    }
+    const int64_t key0 = clamp64(uniform_load(a.k_offsets + tp.r), 0, a.num_keys);
+    const int len = (int)(clamp64(uniform_load(a.k_offsets + tp.r + 1), key0, a.num_keys) - key0);
+    const int steps = (len + GRAD_KEYS - 1) / GRAD_KEYS, share = (steps + splits - 1) / splits;
+    const int begin = split * share, end = min(steps, begin + share);
     i32x4 q[D / 16], d_out[D / 16];
     {
         const char *pq = a.q + (tp.begin + token) * a.q_token + head * a.q_head + h * 16, *po = g.d_out + at * D * 2 + h * 16;
@@ -353,7 +383,10 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
     const bool counts = lse.x != -INFINITY;
     const float c = BIAS ? request_shift(a, tp.begin, rows) : 0.0f, ex = counts ? lse.y * LOG2E : INFINITY, cs = a.scale * LOG2E;
     const bool beside = BIAS && beside_shift(1.0f, c) == 0.0f;
-    const float minus_delta = counts && steps > 1 ? g.delta[at] : 0.0f;
+    if constexpr (!AGAIN) {
+        minus_delta = counts && steps > 1 ? g.delta[at] : 0.0f;
+        lds.sums[threadIdx.x] = float2{0.0f, 0.0f};
+    }
     f32x16 dq[D / 32];
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) dq[t] = zero16();
@@ -454,17 +487,26 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]);
-        if (steps == 1) {
-            float delta = 0.0f;
+        if (!AGAIN && steps == 1) {
+            float delta = 0.0f, total = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) delta = fmaf(s[i], ds[i], delta);
-            delta = sum_halves(delta);
+            for (int i = 0; i < 16; ++i) delta = fmaf(s[i], ds[i], delta), total += s[i];
+            delta = sum_halves(delta), total = sum_halves(total);
+            delta = total == 0.0f ? 0.0f : delta / total;
             if (there && h == 0) g.delta[at] = -delta;
 #pragma unroll
             for (int i = 0; i < 16; ++i) ds[i] -= delta;
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) ds[i] *= s[i];
+        if constexpr (!AGAIN) {
+            float2 &sums = lds.sums[threadIdx.x];
+            const float2 former = sums;
+            float off[2] = {0.0f, 0.0f}, size[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 16; ++i) off[i & 1] += ds[i], size[i & 1] += fabsf(ds[i]);
+            sums = float2{former.x + (off[0] + off[1]), former.y + (size[0] + size[1])};
+        }
         r[0] = round8<DT>(ds, 0), r[1] = round8<DT>(ds, 1);
         if constexpr (BIAS) {
             store_bias(step + L::AHEAD);
@@ -523,6 +565,18 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
         add(end - 1);
         wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
+    if constexpr (!AGAIN) {
+        float off = 0.0f, size = 0.0f;
+        if (steps > 1 && counts) off = lds.sums[threadIdx.x].x, size = lds.sums[threadIdx.x].y;
+        off = sum_halves(off), size = sum_halves(size);
+        if (splits > 1) {
+            if (there && h == 0) *(float2 *)(g.row_part + 2 * ((int64_t)split * a.num_queries * a.heads + at)) = float2{off, size};
+        } else {
+            if (steps > 1 && there && h == 0) g.delta[at] = minus_delta - off;
+            const int far = uniform(__any(there && fabsf(off) > DELTA_OFF(DT) * size) ? 1 : 0);
+            if (lane == 0) g.far[4 * (int64_t)id + wave] = far;
+        }
+    }
     if (!there) return;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
@@ -535,6 +589,12 @@ __global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tile
             if (splits > 1) *(f32x4 *)(g.dq_part + ((int64_t)split * a.num_queries * a.heads + at) * D + d) = x;
             else if (g.dq) *(i32x2 *)(g.dq + (at * D + d) * 2) = i32x2{pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])};
         }
+}
+template <int DT, int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void grad_q_kernel(GradArgs g, int64_t tiles, int splits)
+{
+    __shared__ __align__(16) GradQLds<D, BIAS> lds;
+    grad_q_pass<DT, D, BIAS, false>(g, tiles, splits, blockIdx.x, lds);
 }
 
 // What the kernels above left in parts, in one launch: out[i] = sum over the parts of part[s][i], in their order, for the rows that a
@@ -551,12 +611,12 @@ struct AllSums {
     Sums of[4];
 };
 template <int DT>
-__global__ __launch_bounds__(256) void add_parts_kernel(AllSums all)
+__device__ __forceinline__ void add_parts(const AllSums &all, uint32_t id)
 {
     int which = 0;
-    while (blockIdx.x >= all.of[which].groups) ++which;
+    while (id >= all.of[which].groups) ++which;
     const Sums &x = all.of[which];
-    const int64_t at = (int64_t)(blockIdx.x - (which ? all.of[which - 1].groups : 0)) * 256 + threadIdx.x;
+    const int64_t at = (int64_t)(id - (which ? all.of[which - 1].groups : 0)) * 256 + threadIdx.x;
     if (x.per_row == 1) {
         if (at >= x.count || at < x.offsets[0] || at >= x.offsets[x.n]) return;
         float sum = 0.0f;
@@ -578,6 +638,21 @@ __global__ __launch_bounds__(256) void add_parts_kernel(AllSums all)
     *(i32x2 *)(x.out + 2 * i) = i32x2{pack2<DT>(sum[0], sum[1]), pack2<DT>(sum[2], sum[3])};
 }
 
+template <int DT>
+__global__ __launch_bounds__(256) void add_parts_kernel(AllSums all)
+{
+    add_parts<DT>(all, blockIdx.x);
+}
+// The second pass of the rows that need one, by `again` workgroups, and sums.  With q's keys in one part it is the last launch, in which
+// the sums are those of dbias alone; else it comes before grad_k_kernel and joins the parts' sums of dS.
+template <int DT, int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void finish_kernel(GradArgs g, int64_t tiles, int splits, uint32_t again, AllSums all)
+{
+    __shared__ __align__(16) GradQLds<D, BIAS> lds;
+    if (blockIdx.x < again) grad_q_pass<DT, D, BIAS, true>(g, tiles, splits, blockIdx.x, lds);
+    else add_parts<DT>(all, blockIdx.x - again);
+}
+
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 template <int DT, int D, int NW>
@@ -597,7 +672,16 @@ static void launch_q(hipStream_t st, const GradArgs &g, int splits)
     else grad_q_kernel<DT, D, false><<<grid, block, 0, st>>>(g, tiles, splits);
 }
 template <int DT, int D>
-static void launch(hipStream_t st, const GradArgs &g, int q_splits, int k_waves, int k_splits)
+static void launch_finish(hipStream_t st, const GradArgs &g, int splits, const AllSums &all, uint32_t groups)
+{
+    const int64_t tiles = g.a.num_queries * g.a.group / 128 + g.a.n;
+    const uint32_t again = (uint32_t)(tiles * g.a.kv_heads * splits);
+    const dim3 grid(again + groups), block(256);
+    if (g.a.bias) finish_kernel<DT, D, true><<<grid, block, 0, st>>>(g, tiles, splits, again, all);
+    else finish_kernel<DT, D, false><<<grid, block, 0, st>>>(g, tiles, splits, again, all);
+}
+template <int DT, int D>
+static void launch(hipStream_t st, GradArgs g, int q_splits, int k_waves, int k_splits)
 {
     const AttendArgs &a = g.a;
     const int64_t q_values = a.num_queries * a.heads * D, k_values = a.num_keys * a.kv_heads * D;
@@ -611,9 +695,16 @@ static void launch(hipStream_t st, const GradArgs &g, int q_splits, int k_waves,
     };
     if (a.num_queries > 0) delta_kernel<DT, D><<<dim3((unsigned)ceil_div(q_values / 8, 256)), dim3(256), 0, st>>>(g);
     // also without dq: what it finds out about delta is dk's and dbias's as well, which are the same whatever is asked for
-    if ((g.dq || g.dk || g.dbias) && a.num_queries > 0) {
+    const bool rows = (g.dq || g.dk || g.dbias) && a.num_queries > 0;
+    if (rows) {
         launch_q<DT, D>(st, g, q_splits);
-        if (q_splits > 1) add(g.dq_part, g.dq, q_values, (int64_t)a.heads * D, q_splits, a.q_offsets);
+        if (q_splits > 1) {
+            launch_finish<DT, D>(st, g, q_splits, all, 0);
+            g.delta = g.delta_sum;  // for dk and dbias
+            add(g.dq_part, g.dq, q_values, (int64_t)a.heads * D, q_splits, a.q_offsets);
+        } else if (g.dq && k_splits > 1) {
+            launch_finish<DT, D>(st, g, 1, all, 0);
+        }
     }
     if ((g.dk || g.dv || g.dbias) && a.num_keys > 0) {
         if constexpr (D == 128) {
@@ -628,7 +719,8 @@ static void launch(hipStream_t st, const GradArgs &g, int q_splits, int k_waves,
         }
         add(g.dbias_part, g.dbias, a.num_keys, 1, k_splits * a.kv_heads, a.k_offsets);
     }
-    if (groups > 0) add_parts_kernel<DT><<<dim3(groups), dim3(256), 0, st>>>(all);
+    if (rows && g.dq && q_splits == 1 && k_splits == 1) launch_finish<DT, D>(st, g, 1, all, groups);
+    else if (groups > 0) add_parts_kernel<DT><<<dim3(groups), dim3(256), 0, st>>>(all);
 }
 void plaid_launch_attend_grad(hipStream_t st, const GradArgs &g, int dtype, int head_dim, int q_splits, int k_waves, int k_splits)
 {

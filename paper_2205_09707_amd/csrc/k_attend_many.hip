@@ -339,7 +339,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     constexpr int ROWS = NW * 32, SHIFT = NW == 8 ? 8 : 7, DT_TILES = D / 32;
     __shared__ __align__(16) TileBuffers<D, NW, SRC> lds;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 5;
-    const WorkPlace w = work_place(a, tiles, a.splits);
+    const WorkPlace w = work_place(a, tiles, a.splits, blockIdx.x);
     KeyRange kr;
     kr.head = w.head;
     const int split = w.split;

@@ -40,7 +40,9 @@ struct GradArgs {
     float factor;                      // the scale as it was given, of dq and dk
     const char *d_out;
     char *dq, *dk, *dv, *dbias;        // any may be null
-    float *delta;                      // [num_queries][heads] -dO . out
+    float *delta, *delta_sum;          // [num_queries][heads] -dO . out, corrected in place; corrected, where the keys are cut into parts
+    float *row_part;                   // [q_splits][num_queries][heads][2] sums of dS and |dS| over parts of the keys, null with one part
+    int32_t *far;                      // [workgroups of dq][4] whether a wave's rows need a second pass, with one part
     float *exponent;                   // [num_queries][heads] -lse / scale without the shift; without a key an infinity that makes weights 0
     float *dbias_part;                 // [splits][kv_heads][num_keys], null without dbias
     float *dk_part, *dv_part;          // [splits][num_keys][kv_heads][D], null with one split
@@ -279,12 +281,11 @@ struct WorkPlace {
     int64_t place;
     int head, split;
 };
-__device__ __forceinline__ WorkPlace work_place(const AttendArgs &a, int64_t tiles, int splits)
+__device__ __forceinline__ WorkPlace work_place(const AttendArgs &a, int64_t tiles, int splits, int64_t id)
 {
-    int64_t id = blockIdx.x;
     WorkPlace w;
     if (a.kv_heads & 1) {
-        if (id < (int64_t)gridDim.x / 32 * 32) id = ((id >> 5) * 8 + (id & 7)) * 4 + ((id >> 3) & 3);
+        if (id < tiles * a.kv_heads * splits / 32 * 32) id = ((id >> 5) * 8 + (id & 7)) * 4 + ((id >> 3) & 3);
         w.place = id % tiles;
         id /= tiles;
         w.head = (int)(id % a.kv_heads), w.split = (int)(id / a.kv_heads);

@@ -50,7 +50,7 @@ struct Plan {
     bool few;
     int workers, waves, splits, q_splits, k_waves, k_splits;
     int64_t tiles, bytes;
-    int64_t o_bytes, delta_bytes, bias_bytes, k_bytes, q_bytes;
+    int64_t o_bytes, row_bytes, part_bytes, bias_bytes, k_bytes, q_bytes;
 };
 
 // Parts that an axis of `steps` steps is cut into, at least `least` of them a part, where `groups` workgroups of so many waves leave
@@ -116,11 +116,13 @@ Plan plan_backward(const plaid_attention &a)
     p.k_waves = a.head_dim == 128 && keys > 64 && rows > 128 ? 8 : 4;
     p.q_splits = (int)split_count(ceil_div(rows, 128) * a.n * a.kv_heads, 4, ceil_div(keys, 64), 4);
     p.k_splits = (int)split_count(ceil_div(keys, p.k_waves * 16) * a.n * a.kv_heads, p.k_waves, ceil_div(rows, 64), 4);
-    p.delta_bytes = 2 * round16(a.num_queries * a.heads * 4);  // and the rows' exponents
+    p.row_bytes = round16(a.num_queries * a.heads * 4);  // delta, the rows' exponents
+    // what delta was off by: of parts, with the corrected delta, or whether a workgroup's waves need a second pass
+    p.part_bytes = p.q_splits > 1 ? round16(a.num_queries * a.heads * 8 * p.q_splits) + p.row_bytes : (a.num_queries * group / 128 + a.n) * a.kv_heads * 16;
     p.bias_bytes = round16((int64_t)p.k_splits * a.kv_heads * a.num_keys * 4);
     p.k_bytes = p.k_splits > 1 ? (int64_t)p.k_splits * a.num_keys * a.kv_heads * a.head_dim * 4 : 0;
     p.q_bytes = p.q_splits > 1 ? (int64_t)p.q_splits * a.num_queries * a.heads * a.head_dim * 4 : 0;
-    p.bytes = p.delta_bytes + p.bias_bytes + 2 * p.k_bytes + p.q_bytes;
+    p.bytes = 2 * p.row_bytes + p.part_bytes + p.bias_bytes + 2 * p.k_bytes + p.q_bytes;
     return p;
 }
 
@@ -366,7 +368,10 @@ extern "C" int plaid_cross_attention_backward(const plaid_attention *args, const
     g.d_out = (const char *)d_out;
     g.dq = (char *)dq, g.dk = (char *)dk, g.dv = (char *)dv, g.dbias = (char *)dbias;
     char *w = (char *)workspace;
-    g.delta = (float *)w, g.exponent = (float *)(w + p.delta_bytes / 2), w += p.delta_bytes;
+    g.delta = (float *)w, g.exponent = (float *)(w + p.row_bytes), w += 2 * p.row_bytes;
+    if (p.q_splits > 1) g.delta_sum = (float *)w, g.row_part = (float *)(w + p.row_bytes);
+    else g.far = (int32_t *)w;
+    w += p.part_bytes;
     g.dbias_part = dbias ? (float *)w : nullptr, w += p.bias_bytes;
     g.dk_part = p.k_bytes ? (float *)w : nullptr, w += p.k_bytes;
     g.dv_part = p.k_bytes ? (float *)w : nullptr, w += p.k_bytes;

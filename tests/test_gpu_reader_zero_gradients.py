@@ -25,6 +25,59 @@ def _gradients(pl, q, k, v, d_out, bias, q_lengths, k_lengths):  # noqa: F811
     return out, pl.plaid_cross_attention_backward(d(d_out), d(q), d(k), d(v), out, lse, _off(q_lengths), _off(k_lengths), key_bias=d(bias))
 
 
+def _close_in_scores(pl, q, k, v, d_out, bias, m, n, dtype):  # noqa: F811
+    """Bounds that grow with the scores' gradient dS and not with d_out . out: dS rounds to the type (u), delta is known to u / 2 of the sum
+    of |dS| over a row, and the arithmetic in 32 bits is allowed E32 of what is subtracted."""
+    u, (_, heads, dim), kv_heads = ru.U[dtype], q.shape, k.shape[1]
+    _, (dq, dk, _, dbias) = _gradients(pl, q, k, v, d_out, bias, [m], [n])
+    want = {x: torch.zeros(y.shape, dtype=torch.float64) for x, y in (("dq", q), ("dk", k), ("db", k[:, 0, 0]))}
+    off = {x: torch.zeros_like(y) for x, y in want.items()}
+    scale = dim ** -0.5
+    for h in range(heads):
+        g = h * kv_heads // heads
+        x, y, z, o = q[:, h].double(), k[:, g].double(), v[:, g].double(), d_out[:, h].double()
+        p = torch.softmax(x @ y.T * scale + (0.0 if bias is None else bias.double()), -1)
+        dp = o @ z.T
+        ds = p * (dp - (p * dp).sum(-1, keepdim=True))
+        rough = (o.abs() @ z.abs().T).amax(-1, keepdim=True)
+        err = (u + ru.E32) * ds.abs() + p * (u / 2 * ds.abs().sum(-1, keepdim=True) + ru.E32 * rough) + (2.0 ** -25 if dtype == HF else 0.0)
+        want["dq"][:, h], off["dq"][:, h] = ds @ y * scale, err @ y.abs() * scale
+        want["dk"][:, g] += ds.T @ x * scale
+        off["dk"][:, g] += err.T @ x.abs() * scale
+        want["db"] += ds.sum(0)
+        off["db"] += err.sum(0)
+    for name, got in (("dq", dq), ("dk", dk), ("db", dbias)):
+        if got is not None:
+            ru.close(got, want[name], off[name] + u * want[name].abs() + ru.TINY[dtype], name)
+
+
+# queries: rows that one workgroup has, and rows that are shared among several keys' parts
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("m,n,live", [(40, 40, 2), (300, 40, 2), (5, 40, 3), (64, 1000, 2), (3, 4000, 2), (200, 3000, 4), (33, 20, 2)])
+def test_few_keys_that_count(pl, m, n, live, dtype):  # noqa: F811
+    for dim, heads, kv_heads in ((64, 4, 4), (128, 4, 1)):
+        q, k, v, d_out = _inputs([m], [n], heads, kv_heads, dim, dtype, m * n)
+        bias = torch.full((n,), -math.inf, dtype=dtype)
+        bias[torch.randperm(n, generator=torch.Generator().manual_seed(n))[:live]] = 0.25
+        _close_in_scores(pl, q, k, v, d_out, bias, m, n, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("m,n", [(40, 50), (300, 333), (3, 4000), (200, 3000), (20, 31)])
+def test_weight_on_one_key(pl, m, n, with_bias, dtype):  # noqa: F811
+    """One key's score is far above the others: its weight is about 0.99, and dS a hundredth of what it is a difference of."""
+    for dim, heads, kv_heads in ((64, 2, 2), (128, 4, 1)):
+        q, k, v, d_out = _inputs([m], [n], heads, kv_heads, dim, dtype, m + n)
+        bias = _bias(n, 5, dtype, 0.1) if with_bias else None
+        if with_bias:
+            bias[n // 2] = 2.0
+        lift = math.log(99 * n * math.e ** 0.5) * dim ** 0.5 / 16       # q's first dimension is 16: the score of that key rises by log(99 n e^1/2)
+        q[..., 0], k[..., 0] = 16.0, 0.0
+        k[n // 2, :, 0] = lift
+        _close_in_scores(pl, q, k, v, d_out, bias, m, n, dtype)
+
+
 @pytest.mark.parametrize("with_bias", [False, True])
 @pytest.mark.parametrize("q_lengths,k_lengths", [([5, 40], [2, 31]), ([300, 7], [40, 90]), ([3], [3000]), ([700], [20])])
 def test_gradients_do_not_depend_on_which_are_asked_for(pl, q_lengths, k_lengths, with_bias):  # noqa: F811
