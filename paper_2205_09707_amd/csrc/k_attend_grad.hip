@@ -40,6 +40,22 @@ __device__ __forceinline__ float request_shift(const AttendArgs &a, int64_t row0
     return c == -INFINITY ? 0.0f : c;
 }
 
+// Whether a request has one key that is not masked.  Then P = 1 and dP = delta by definition, and dq, dk and dbias are zero: what is left of
+// dP - delta in 32 bits is rounding.  The loop ends where a second one is found, mostly in its first round.
+template <int DT, bool BIAS>
+__device__ __forceinline__ bool one_key(const AttendArgs &a, int64_t key0, int len)
+{
+    constexpr uint16_t NONE = DT == PLAID_BF16 ? 0xff80 : 0xfc00;  // -infinity
+    if (!BIAS) return len == 1;
+    int live = 0;
+    for (int at = threadIdx.x & 63; live < 2; at += 256) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) live += __popcll(__ballot(at + 64 * i < len && ((const uint16_t *)a.bias)[key0 + min(at + 64 * i, len - 1)] != NONE));
+        if (uniform(at) + 256 >= len) break;
+    }
+    return live == 1;
+}
+
 // What the rows bring (-lse / scale, -delta) and the keys' biases over the scale are what the matrix instruction adds the products to;
 // a weight then takes one multiply-add and an exponential.  P and dS round to the type before they are multiplied again.
 // Measured on 16 requests of 456 tokens x 16 heads, 6250 keys of 4 heads, D = 128, biases: grad_k 830 us (746 GFLOP, 0.90 PFLOP/s),
@@ -280,11 +296,13 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     }
 
     dbias = sum_halves(dbias);
+    const int own = __popc((uint32_t)__ballot(there && !(BIAS && bias == -INFINITY)));  // of the wave's keys
+    const bool one = second && own == 1 && one_key<DT, BIAS>(a, tp.begin, len);
     if (!there) return;
     // a masked key's column may hold anything and is zero
     const bool masked = BIAS && bias == -INFINITY;
     const int64_t at = (tp.begin + key) * a.kv_heads + head;
-    if (BIAS && second && h == 0 && g.dbias_part) g.dbias_part[((int64_t)split * a.kv_heads + head) * a.num_keys + tp.begin + key] = masked ? 0.0f : dbias;
+    if (BIAS && second && h == 0 && g.dbias_part) g.dbias_part[((int64_t)split * a.kv_heads + head) * a.num_keys + tp.begin + key] = masked || one ? 0.0f : dbias;
     const float factor = second ? g.factor : 1.0f;
     char *out = second ? g.dk : g.dv;
     float *part = second ? g.dk_part : g.dv_part;
@@ -294,7 +312,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
         for (int i = 0; i < 4; ++i) {
             f32x4 x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = masked ? 0.0f : sum[t][4 * i + e] * factor;
+            for (int e = 0; e < 4; ++e) x[e] = masked || one ? 0.0f : sum[t][4 * i + e] * factor;
             const int d = 32 * t + 8 * i + 4 * h;
             if (splits > 1) *(f32x4 *)(part + ((int64_t)split * a.num_keys * a.kv_heads + at) * D + d) = x;
             else if (out) *(i32x2 *)(out + (at * D + d) * 2) = i32x2{pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])};
@@ -393,6 +411,7 @@ __device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, in
 
     // keys past the end repeat the last one; tiles past the last repeat that
     uint32_t masked = 0;  // keys of bias -infinity, and places past the end, in the tile that is asked for next
+    int live = 0;         // keys that are not masked
     const char *keys = a.k + key0 * a.k_token + head_kv * a.k_head, *values = a.v + key0 * a.v_token + head_kv * a.v_head;
     uint32_t key_row[N], value_row[N], chunk[N];  // bytes of a lane's row in a tile, and within the row
     const uint32_t to_k = lds_address(lds.k[0]) + wave * N * 1024, to_v = lds_address(lds.v[0]) + wave * N * 1024;
@@ -432,6 +451,7 @@ __device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, in
         const uint16_t x = min(step, end - 1) * GRAD_KEYS + (lane & 31) < len ? (uint16_t)raw : NONE;
         lds.bias[wave][step & 3][lane & 31] = (unpack<DT>(x, 0) - c) * a.inv_scale;
         masked = (uint32_t)__ballot(x == NONE);
+        if (step < end) live += __popc(~masked);
     };
     f32x16 s, ds;  // q k^T + b / scale, dO v^T - delta
     i32x4 r[2];
@@ -565,9 +585,10 @@ __device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, in
         add(end - 1);
         wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
+    const bool one = BIAS ? live == 1 && (splits == 1 || one_key<DT, true>(a, key0, len)) : len == 1;
     if constexpr (!AGAIN) {
         float off = 0.0f, size = 0.0f;
-        if (steps > 1 && counts) off = lds.sums[threadIdx.x].x, size = lds.sums[threadIdx.x].y;
+        if (steps > 1 && counts && !one) off = lds.sums[threadIdx.x].x, size = lds.sums[threadIdx.x].y;
         off = sum_halves(off), size = sum_halves(size);
         if (splits > 1) {
             if (there && h == 0) *(float2 *)(g.row_part + 2 * ((int64_t)split * a.num_queries * a.heads + at)) = float2{off, size};
@@ -584,7 +605,7 @@ __device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, in
         for (int i = 0; i < 4; ++i) {
             f32x4 x;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = counts ? dq[t][4 * i + e] * g.factor : 0.0f;  // without a key: whatever q holds
+            for (int e = 0; e < 4; ++e) x[e] = counts && !one ? dq[t][4 * i + e] * g.factor : 0.0f;  // without a key: whatever q holds
             const int d = 32 * t + 8 * i + 4 * h;
             if (splits > 1) *(f32x4 *)(g.dq_part + ((int64_t)split * a.num_queries * a.heads + at) * D + d) = x;
             else if (g.dq) *(i32x2 *)(g.dq + (at * D + d) * 2) = i32x2{pack2<DT>(x[0], x[1]), pack2<DT>(x[2], x[3])};

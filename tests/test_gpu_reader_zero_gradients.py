@@ -25,6 +25,49 @@ def _gradients(pl, q, k, v, d_out, bias, q_lengths, k_lengths):  # noqa: F811
     return out, pl.plaid_cross_attention_backward(d(d_out), d(q), d(k), d(v), out, lse, _off(q_lengths), _off(k_lengths), key_bias=d(bias))
 
 
+# keys of the request, the place of the one that is not masked (None: no bias), queries: every kernel and both ways to cut its work
+ONE = [(1, None, 1), (1, None, 40), (1, None, 700), (1, 0, 5), (2, 1, 33), (32, 31, 300), (33, 0, 7), (40, 39, 64), (100, 50, 300), (700, 333, 3),
+       (3000, 2999, 1), (3000, 64, 200)]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim,heads,kv_heads", [(64, 3, 3), (128, 8, 2)])
+@pytest.mark.parametrize("n,at,m", ONE)
+def test_one_key_that_counts(pl, n, at, m, dim, heads, kv_heads, dtype):  # noqa: F811
+    """P is 1 and dP = delta: dq, dk and dbias are zero, not nearly so.  dv is the sum of d_out."""
+    q, k, v, d_out = _inputs([m], [n], heads, kv_heads, dim, dtype, n + m)
+    bias = None
+    if at is not None:
+        bias = torch.full((n,), -math.inf, dtype=dtype)
+        bias[at] = -1.25
+    out, (dq, dk, dv, dbias) = _gradients(pl, q, k, v, d_out, bias, [m], [n])
+    assert torch.equal(out.cpu(), v[at or 0].repeat_interleave(heads // kv_heads, 0).expand(m, heads, dim))
+    assert not dq.any() and not dk.any() and (dbias is None or not dbias.any())
+    want = ru.cross(q, k, v, [m], [n], dim ** -0.5, bias, d_out)
+    ru.close(dv, want["dv"], want["dv_bound"], "dv")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_one_key_beside_other_requests(pl, dtype):  # noqa: F811
+    """A request with one key that counts among others, in both orders of requests (up to 64 of them and more)."""
+    for times in (1, 20):
+        q_lengths, k_lengths = [5, 40, 0, 70] * times, [1, 70, 3, 45] * times
+        nq, nk = sum(q_lengths), sum(k_lengths)
+        q, k, v, d_out = _inputs(q_lengths, k_lengths, 4, 2, 64, dtype, times)
+        bias = _bias(nk, 3, dtype)
+        for r in range(times):
+            bias[r * 119] = 0.5
+            bias[r * 119 + 74:r * 119 + 119] = -math.inf
+            bias[r * 119 + 74 + 37] = 2.0
+        _, (dq, dk, dv, dbias) = _gradients(pl, q, k, v, d_out, bias, q_lengths, k_lengths)
+        want = ru.cross(q, k, v, q_lengths, k_lengths, 0.125, bias, d_out)
+        for name, x in zip(("dq", "dk", "dv", "dbias"), (dq, dk, dv, dbias)):
+            ru.close(x, want[name], want[name + "_bound"], name)
+        dq, dk, dbias = dq.view(times, nq // times, -1), dk.view(times, nk // times, -1), dbias.view(times, -1)
+        assert not dq[:, :5].any() and not dq[:, 45:].any() and dq[:, 5:45].any()
+        assert not dk[:, 0].any() and not dk[:, 74:].any() and not dbias[:, 0].any() and not dbias[:, 74:].any() and dk[:, 1:71].any()
+
+
 def _close_in_scores(pl, q, k, v, d_out, bias, m, n, dtype):  # noqa: F811
     """Bounds that grow with the scores' gradient dS and not with d_out . out: dS rounds to the type (u), delta is known to u / 2 of the sum
     of |dS| over a row, and the arithmetic in 32 bits is allowed E32 of what is subtracted."""
