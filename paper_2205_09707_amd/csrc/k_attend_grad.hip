@@ -57,7 +57,8 @@ __device__ __forceinline__ bool one_key(const AttendArgs &a, int64_t key0, int l
 }
 
 // What the rows bring (-lse / scale, -delta) and the keys' biases over the scale are what the matrix instruction adds the products to;
-// a weight then takes one multiply-add and an exponential.  P and dS round to the type before they are multiplied again.
+// a weight then takes one multiply-add and an exponential.  P and dS round to the type before they are multiplied again; P, which is at most 1
+// and with many keys far below what fp16 holds in full (2^-14), times 2^WEIGHT there, which dv is freed of in the end.
 // Measured on 16 requests of 456 tokens x 16 heads, 6250 keys of 4 heads, D = 128, biases: grad_k 830 us (746 GFLOP, 0.90 PFLOP/s),
 // grad_q 545 (560 GFLOP, 1.03 PFLOP/s), delta 12 (180 MB, 4.6 TB/s with the statistics).  Bound by products and what feeds them: without
 // exponentials both together took 1454 in place of 1522, without loads 1298.  Both in one launch are no faster (the same for short
@@ -69,6 +70,8 @@ __device__ __forceinline__ bool one_key(const AttendArgs &a, int64_t key0, int l
 // forms dS (values and the sum dk in registers).  Each does half of the products; P, in 32 bits, costs a fifth of the traffic in LDS.
 // The two kinds run in phases like the forward kernel's groups (k_attend_many.hip), products on one side, exponentials on the other;
 // the first kind asks for q, the second for dO, two steps ahead.
+#define WEIGHT 15
+constexpr __device__ float powf2(int e) { return __builtin_bit_cast(float, (e + 127) << 23); }
 template <int NW>
 struct GradK {
     static constexpr int PAIRS = NW / 2, KEYS = PAIRS * 32, SHIFT = NW == 8 ? 7 : 6, ROWS = NW == 8 ? 64 : 32;  // rows of a step
@@ -117,7 +120,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     }
     float bias = 0.0f;
     if (BIAS) bias = there ? load16<DT>(a.bias + 2 * (tp.begin + key)) : 0.0f;
-    const float c = BIAS ? request_shift(a, row0, rows) : 0.0f, cs = a.scale * LOG2E, bias_e = (bias - c) * LOG2E;
+    const float c = BIAS ? request_shift(a, row0, rows) : 0.0f, cs = a.scale * LOG2E, bias_e = (bias - c) * LOG2E + (DT == PLAID_FP16 ? WEIGHT : 0);
     const bool beside = BIAS && beside_shift(1.0f, c) == 0.0f;
     f32x16 sum[D / 32];  // the first wave's dv, the second one's dk
 #pragma unroll
@@ -211,7 +214,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[b][i] = BIAS ? fmaf(s[b][i], cs, bias_e) : s[b][i] * cs;
+                for (int i = 0; i < 16; ++i) s[b][i] = BIAS || DT == PLAID_FP16 ? fmaf(s[b][i], cs, bias_e) : s[b][i] * cs;
             if ((step + 1) * ROWS > rows) {
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
                 for (int i = 0; i < 4; ++i) {
                     const f32x4 x = *(const f32x4 *)lds.p[pair][b][i][lane];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[b][4 * i + e] *= x[e];
+                    for (int e = 0; e < 4; ++e) s[b][4 * i + e] *= DT == PLAID_FP16 ? x[e] * powf2(-WEIGHT) : x[e];
                 }
         }
 #pragma unroll
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     const bool masked = BIAS && bias == -INFINITY;
     const int64_t at = (tp.begin + key) * a.kv_heads + head;
     if (BIAS && second && h == 0 && g.dbias_part) g.dbias_part[((int64_t)split * a.kv_heads + head) * a.num_keys + tp.begin + key] = masked || one ? 0.0f : dbias;
-    const float factor = second ? g.factor : 1.0f;
+    const float factor = second ? g.factor : DT == PLAID_FP16 ? powf2(-WEIGHT) : 1.0f;
     char *out = second ? g.dk : g.dv;
     float *part = second ? g.dk_part : g.dv_part;
 #pragma unroll

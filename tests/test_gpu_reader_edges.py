@@ -1,0 +1,26 @@
+"""Values that are not finite at a request's end, rows whose scores overflow, weights below the type's normal range, and offsets that do not ascend."""
+import math
+
+import pytest
+import torch
+
+import reader_util as ru
+from test_gpu_reader_attention import BF, DEV, HF, _off, _randn, pl  # noqa: F401 (pl is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_small_weights_of_half_precision(pl, dtype):  # noqa: F811
+    """A hundred thousand keys: a weight is 1e-5, which fp16 holds as a multiple of 2^-24.  dv keeps the type's relative precision."""
+    n, m, dim = 100_000, 3, 64
+    q, k, v = (_randn((x, 1, dim), i, dtype, g) for i, (x, g) in enumerate(((m, 0.25), (n, 1.0), (n, 1.0))))
+    d_out = _randn((m, 1, dim), 9, dtype, 256.0)
+    d = lambda t: t.to(DEV)  # noqa: E731
+    out, lse = pl.plaid_cross_attention(d(q), d(k), d(v), _off([m]), _off([n]), return_lse=True)
+    _, _, dv, _ = pl.plaid_cross_attention_backward(d(d_out), d(q), d(k), d(v), out, lse, _off([m]), _off([n]))
+    s = q[:, 0].double() @ k[:, 0].double().T * dim ** -0.5
+    p = torch.softmax(s, -1)
+    want = p.T @ d_out[:, 0].double()
+    u, e = ru.U[dtype], ru.E32 * (1 + float((q[:, 0].double().abs() @ k[:, 0].double().abs().T).max()) * dim ** -0.5 / 16)
+    ru.close(dv[:, 0], want, u * want.abs() + (u + e) * (p.T @ d_out[:, 0].double().abs()) + ru.TINY[dtype], "dv")
