@@ -285,8 +285,9 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
                 } else {
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) {
+                        // a value past the end meets a weight of zero
                         const int key = i * AT_ONCE + lane / (D / 8);
-                        x.v[i] = *(const i32x4 *)(base + (uint32_t)(key < last ? key : last) * (uint32_t)a.v_token + lane % (D / 8) * 16);
+                        x.v[i] = *(const i32x4 *)(key <= last ? base + ((uint32_t)key * (uint32_t)a.v_token + lane % (D / 8) * 16) : (const char *)zero_row);
                     }
                 }
                 if constexpr (BIAS) {

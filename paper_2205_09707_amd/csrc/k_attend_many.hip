@@ -73,7 +73,7 @@ struct Stage {
             chunk[i] = ((lane % CHUNKS) ^ swizzle<D>(row)) * 16;
         }
     }
-    // Keys past the end repeat the last one.  The tiles after the last repeat that one, so that a phase's number of loads is fixed.
+    // Keys past the end repeat the last one (with biases they are zeros, else the last step leaves them out).  The tiles after the last repeat that one, so that a phase's number of loads is fixed.
     __device__ __forceinline__ void load(const KeyRange &kr, const char *first, uint32_t token, const uint32_t (&rows)[N], int tile, uint32_t to,
                                          uint64_t masked)
     {
@@ -576,7 +576,22 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         weights(end - 1, std::true_type());
         phase_end(true);
         add_weights();
-        add_values(end - 1, 0, 4);
+        if (SRC == PLAID_SOURCE_DENSE && end * MANY_KEYS > kr.len) {
+            // what stands in for values past the end may not be finite and must not meet its weights of zero
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                i32x4 keep;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int left = kr.len - ((end - 1) * MANY_KEYS + 16 * i + 8 * (x >> 1) + 4 * h + 2 * (x & 1));
+                    keep[x] = left >= 2 ? -1 : left == 1 ? 0xffff : 0;
+                }
+#pragma unroll
+                for (int dt = 0; dt < DT_TILES; ++dt) o[dt] = mfma32<DT>(value_operand<D, NW, SRC>(lds, (end - 1) % A::TILES, 16 * i, dt) & keep, p[i], o[dt]);
+            }
+        } else {
+            add_values(end - 1, 0, 4);
+        }
         if (A::GROUPS == 2 && !late) lds_barrier();
         wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }

@@ -24,3 +24,20 @@ def test_small_weights_of_half_precision(pl, dtype):  # noqa: F811
     want = p.T @ d_out[:, 0].double()
     u, e = ru.U[dtype], ru.E32 * (1 + float((q[:, 0].double().abs() @ k[:, 0].double().abs().T).max()) * dim ** -0.5 / 16)
     ru.close(dv[:, 0], want, u * want.abs() + (u + e) * (p.T @ d_out[:, 0].double().abs()) + ru.TINY[dtype], "dv")
+
+
+# lengths that no tile divides; the key that is not finite is the last one, which has nothing behind it
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads", [2, 16])
+@pytest.mark.parametrize("m,n", [(1, 83), (40, 83), (300, 83), (1, 3001), (300, 3001), (64, 1), (300, 1)])
+def test_a_last_key_that_is_not_finite(pl, m, n, heads, dim, dtype):  # noqa: F811
+    """An infinite value of the last key gives what one of the first key gives."""
+    q, k, v = _randn((2 * m, heads, dim), 1, dtype).to(DEV), _randn((2 * n, 2, dim), 2, dtype).to(DEV), _randn((2 * n, 2, dim), 3, dtype).to(DEV)
+    half, qo, ko = heads // 2, _off([m, m]), _off([n, n])
+    for at in (0, n - 1):
+        w = v.clone()
+        w[at, 1, 7] = math.inf
+        out = pl.plaid_cross_attention(q, k, w, qo, ko)
+        assert torch.isinf(out[:m, half:, 7]).all() and torch.isfinite(out[m:]).all() and torch.isfinite(out[:, :half]).all()
+        assert torch.isfinite(out[..., :7]).all() and torch.isfinite(out[..., 8:]).all()
