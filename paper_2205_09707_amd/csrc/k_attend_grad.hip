@@ -127,7 +127,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     for (int t = 0; t < D / 32; ++t) sum[t] = zero16();
     float dbias = 0.0f;
 
-    // Rows past the end repeat the last one; tiles past the last repeat that.  Where a step is a whole number of tokens a lane's rows
+    // Rows past the end repeat the last one, which the last step leaves out; tiles past the last repeat that.  Where a step is a whole number of tokens a lane's rows
     // lie at the same distances from the step's first token in every step.
     const bool aligned = ROWS % a.group == 0;
     // The first waves bring q, the second ones dO.
@@ -293,7 +293,22 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
         weights(end - 1);
         lds_barrier();
         add_dbias();
-        add(end - 1, 0);
+        if (end * ROWS > rows) {
+            // what stands in for rows past the end may not be finite and must not meet their weights of zero
+#pragma unroll
+            for (int i = 0; i < 2 * BLOCKS; ++i) {
+                i32x4 keep;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int left = rows - ((end - 1) * ROWS + 16 * i + 8 * (x >> 1) + 4 * h + 2 * (x & 1));
+                    keep[x] = left >= 2 ? -1 : left == 1 ? 0xffff : 0;
+                }
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) sum[t] = mfma32<DT>(add_operand(end - 1, i, t) & keep, p[i], sum[t]);
+            }
+        } else {
+            add(end - 1, 0);
+        }
         if (!second) lds_barrier();
         wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }

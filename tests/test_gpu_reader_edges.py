@@ -41,3 +41,18 @@ def test_a_last_key_that_is_not_finite(pl, m, n, heads, dim, dtype):  # noqa: F8
         out = pl.plaid_cross_attention(q, k, w, qo, ko)
         assert torch.isinf(out[:m, half:, 7]).all() and torch.isfinite(out[m:]).all() and torch.isfinite(out[:, :half]).all()
         assert torch.isfinite(out[..., :7]).all() and torch.isfinite(out[..., 8:]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("m,n,heads", [(1, 40, 2), (41, 90, 2), (5, 700, 6), (301, 90, 8), (301, 20, 10)])
+def test_a_last_row_that_is_not_finite(pl, m, n, heads, dtype):  # noqa: F811
+    """An infinite d_out of the last row makes its dimension of dv infinite, as one of the first row does, and no other."""
+    for dim in (64, 128):
+        q, k, v, d_out = (_randn((x, h, dim), i, dtype).to(DEV) for i, (x, h) in enumerate(((2 * m, heads), (2 * n, 2), (2 * n, 2), (2 * m, heads))))
+        out, lse = pl.plaid_cross_attention(q, k, v, _off([m, m]), _off([n, n]), return_lse=True)
+        for token, head in ((0, 0), (m - 1, heads // 2 - 1)):
+            o = d_out.clone()
+            o[token, head, 9] = math.inf
+            _, dk, dv, _ = pl.plaid_cross_attention_backward(o, q, k, v, out, lse, _off([m, m]), _off([n, n]))
+            assert torch.isinf(dv[:n, 0, 9]).all() and torch.isfinite(dv[:, 1]).all() and torch.isfinite(dv[n:]).all() and torch.isfinite(dk[n:]).all()
+            assert torch.isfinite(dv[..., :9]).all() and torch.isfinite(dv[..., 10:]).all()
