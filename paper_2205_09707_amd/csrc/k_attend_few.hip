@@ -145,6 +145,7 @@ struct FewLds {
         float o[NW][FEW_ROWS][D + 4];
     };
     float ml[NW][FEW_ROWS][2], shift[NW];
+    int any[NW];  // whether a wave has seen a key that is not masked
 };
 
 // Keys and values of a piece are loaded apart, each into the registers that its predecessor has just left: the scores of a
@@ -285,9 +286,10 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
                 } else {
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) {
-                        // a value past the end meets a weight of zero
+                        // a value past the end meets a weight of zero; with biases it is left out below
                         const int key = i * AT_ONCE + lane / (D / 8);
-                        x.v[i] = *(const i32x4 *)(key <= last ? base + ((uint32_t)key * (uint32_t)a.v_token + lane % (D / 8) * 16) : (const char *)zero_row);
+                        const char *from = base + (uint32_t)(key < last ? key : last) * (uint32_t)a.v_token + lane % (D / 8) * 16;
+                        x.v[i] = *(const i32x4 *)(BIAS || key <= last ? from : (const char *)zero_row);
                     }
                 }
                 if constexpr (BIAS) {
@@ -365,7 +367,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
                 const float c = shift.c;
                 shift.add(__ballot(unusual), largest, __any(usual));
                 m += c - shift.c;  // m is relative to the shift
-                const float scale = beside_shift(a.scale, shift.c);
+                const float scale = beside(shift.c) ? __int_as_float(1) : a.scale;  // what is finite vanishes, an infinity stays one
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = b[e] == -INFINITY ? -INFINITY : fmaf(s[e >> 2][e & 3], scale, b[e] - shift.c);
             } else if (key0 + 32 > least || !held0 || !held1) {
@@ -474,7 +476,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
 #pragma unroll
         for (int t = 0; t < OT; ++t) *(f32x4 *)&lds.o[wave][m16][16 * t + 4 * kg] = o[t];
         if (kg == 0) lds.ml[wave][m16][0] = natural, lds.ml[wave][m16][1] = l;
-        if (lane == 0) lds.shift[wave] = shift.c;
+        if (lane == 0) lds.shift[wave] = shift.c, lds.any[wave] = shift.any();
         __syncthreads();
         const int count = min(FEW_ROWS, rows - tile * FEW_ROWS);  // rows that there are
         for (int u = threadIdx.x; u < count * (D / 4); u += NW * 64) {
@@ -482,7 +484,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
             float base = -INFINITY, top = -INFINITY, sum = 0.0f;
             f32x4 acc{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < NW; ++i) base = fmaxf(base, lds.ml[i][y][1] == 0.0f ? -INFINITY : lds.shift[i]);
+            for (int i = 0; i < NW; ++i) base = fmaxf(base, lds.ml[i][y][1] == 0.0f && !(BIAS && lds.any[i]) ? -INFINITY : lds.shift[i]);
             const float c = base == -INFINITY ? 0.0f : base;
 #pragma unroll
             for (int i = 0; i < NW; ++i) top = fmaxf(top, lds.shift[i] - c + lds.ml[i][y][0]);
@@ -497,7 +499,7 @@ __global__ __launch_bounds__(NW * 64, FEW_PER_SIMD(D, SRC)) void attend_few_kern
             }
             const int row_out = tile * FEW_ROWS + y;
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            const float2 lse = sum == 0.0f ? float2{-INFINITY, 0.0f} : float2{base, top + logf(sum)};
+            const float2 lse = base == -INFINITY ? float2{-INFINITY, 0.0f} : float2{base, top + logf(sum)};
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] *= inv;
             if (begin == 0 && stop == rq.steps) {
@@ -581,7 +583,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_workers_kernel(AttendArgs a
     const int64_t to = (rq.row0 + tk) * a.heads + head_kv * a.group + row - tk * a.group;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     *(i32x2 *)(a.out + (to * D + d) * 2) = i32x2{pack2<DT>(acc[0] * inv, acc[1] * inv), pack2<DT>(acc[2] * inv, acc[3] * inv)};
-    if (a.lse && d == 0) *(float2 *)(a.lse + 2 * to) = sum == 0.0f ? float2{-INFINITY, 0.0f} : float2{c, top + logf(sum)};
+    if (a.lse && d == 0) *(float2 *)(a.lse + 2 * to) = c == -INFINITY ? float2{-INFINITY, 0.0f} : float2{c, top + logf(sum)};
 }
 
 template <int DT, int D, int SRC>

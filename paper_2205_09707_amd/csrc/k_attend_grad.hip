@@ -12,6 +12,9 @@
 // brings goes into LDS once and is read both along its rows (for s and dP) and transposed (for the sums); the results leave their
 // registers as the operands that the sums need, as in the forward kernel.
 
+// Whether any weight is left in a row.
+__device__ __forceinline__ bool row_counts(float2 lse) { return lse.x != -INFINITY && lse.y != -INFINITY; }
+
 template <int DT, int D>
 __global__ __launch_bounds__(256) void delta_kernel(GradArgs g)
 {
@@ -27,13 +30,13 @@ __global__ __launch_bounds__(256) void delta_kernel(GradArgs g)
         for (int o = LANES / 2; o; o >>= 1) sum += __shfl_xor(sum, o);
         if (c == 0) {
             const float2 lse = *(const float2 *)(g.a.lse + 2 * at);
-            g.delta[at] = lse.x != -INFINITY ? -sum : 0.0f;
-            g.exponent[at] = (lse.x != -INFINITY ? -lse.y : -INFINITY) * g.a.inv_scale;
+            g.delta[at] = row_counts(lse) ? -sum : 0.0f;
+            g.exponent[at] = (row_counts(lse) ? -lse.y : -INFINITY) * g.a.inv_scale;
         }
     }
 }
 
-// The shift of a request's biases (see Shift): all of its rows have the same.
+// The shift of a request's biases (see Shift): all of its rows have the same, -infinity where every key is masked.
 __device__ __forceinline__ float request_shift(const AttendArgs &a, int64_t row0, int rows)
 {
     const float c = rows ? uniform_load(a.lse + 2 * row0 * a.heads) : -INFINITY;
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     float bias = 0.0f;
     if (BIAS) bias = there ? load16<DT>(a.bias + 2 * (tp.begin + key)) : 0.0f;
     const float c = BIAS ? request_shift(a, row0, rows) : 0.0f, cs = a.scale * LOG2E, bias_e = (bias - c) * LOG2E + (DT == PLAID_FP16 ? WEIGHT : 0);
-    const bool beside = BIAS && beside_shift(1.0f, c) == 0.0f;
+    const bool alone = BIAS && beside(c);
     f32x16 sum[D / 32];  // the first wave's dv, the second one's dk
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) sum[t] = zero16();
@@ -204,12 +207,12 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
         load_row(step + 2);
         load(step + K::AHEAD);
         if (!second) {
-            if (beside) {
+            if (alone) {
                 const float *of_row = lds.row[wave][step & 3];
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = of_row[32 * b + 8 * (i >> 2) + 4 * h + (i & 3)];
+                    for (int i = 0; i < 16; ++i) s[b][i] = vanish(s[b][i], of_row[32 * b + 8 * (i >> 2) + 4 * h + (i & 3)]);
             }
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b)
@@ -416,9 +419,9 @@ __device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, in
         for (int s = 0; s < D / 16; ++s) q[s] = *(const i32x4 *)(pq + s * 32), d_out[s] = *(const i32x4 *)(po + s * 32);
     }
     const float2 lse = *(const float2 *)(a.lse + 2 * at);
-    const bool counts = lse.x != -INFINITY;
+    const bool counts = row_counts(lse);
     const float c = BIAS ? request_shift(a, tp.begin, rows) : 0.0f, ex = counts ? lse.y * LOG2E : INFINITY, cs = a.scale * LOG2E;
-    const bool beside = BIAS && beside_shift(1.0f, c) == 0.0f;
+    const bool alone = BIAS && beside(c);
     if constexpr (!AGAIN) {
         minus_delta = counts && steps > 1 ? g.delta[at] : 0.0f;
         lds.sums[threadIdx.x] = float2{0.0f, 0.0f};
@@ -510,9 +513,12 @@ __device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, in
             // the biases that the step before asked for first
             wait_loads<2 * N>();
             read_bias(step + L::AHEAD);
-            if (beside) {
+            if (alone) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = lds.bias[wave][step & 3][8 * (i >> 2) + 4 * h + (i & 3)];
+                for (int i = 0; i < 16; ++i) {
+                    const float b = lds.bias[wave][step & 3][8 * (i >> 2) + 4 * h + (i & 3)];
+                    s[i] = b == -INFINITY ? b : vanish(s[i], b);
+                }
             }
         } else {
             load(step + L::AHEAD);

@@ -413,7 +413,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     // scores are kept as q . k + b / scale: one multiply-add then makes the exponent
     const float cs = a.scale * LOG2E;
     float m = -INFINITY, l = 0.0f;
-    int shift = 0, beside = 0;  // the shift's bits, and whether it leaves the scores nothing: the same for all lanes
+    int shift = 0, alone = 0;  // the shift's bits, and whether it leaves the scores nothing: the same for all lanes
 
     // Two groups of waves, one of each on every SIMD, half a step apart: while one multiplies, the other forms exponentials.
     // A step of a group is a phase of products (o += v^T p^T of the former tile, s of this one) and one of everything else, with
@@ -470,16 +470,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
             if (stage.shifts[0] != shift) {  // m is relative to the shift
                 m += (__int_as_float(shift) - __int_as_float(stage.shifts[0])) * a.inv_scale;
                 shift = stage.shifts[0];
-                beside = uniform((int)(beside_shift(1.0f, __int_as_float(shift)) == 0.0f));
+                alone = uniform((int)beside(__int_as_float(shift)));
             }
-            if (odd | beside) {
+            if (odd | alone) {
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const f32x4 b = *(const f32x4 *)&lds.bias[wave][step & 3][32 * mt + 8 * i + 4 * h];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[mt][4 * i + e] = beside || b[e] == -INFINITY ? b[e] : s[mt][4 * i + e];
+                        for (int e = 0; e < 4; ++e) s[mt][4 * i + e] = b[e] == -INFINITY ? b[e] : alone ? vanish(s[mt][4 * i + e], b[e]) : s[mt][4 * i + e];
                     }
             }
         } else {
@@ -610,7 +610,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
     if (!there) return;
     const int64_t out_row = (tp.begin + token) * a.heads + head;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const float2 lse = l == 0.0f ? float2{-INFINITY, 0.0f} : float2{__int_as_float(shift), m * a.scale + logf(l)};
+    bool any = l != 0.0f;
+    if constexpr (SRC == PLAID_SOURCE_BIAS) any = stage.shift.any();
+    const float2 lse = any ? float2{__int_as_float(shift), m * a.scale + logf(l)} : float2{-INFINITY, 0.0f};
     if (a.splits > 1) {
         const int64_t at = (int64_t)split * a.num_queries * a.heads + out_row;
 #pragma unroll
@@ -657,7 +659,7 @@ __global__ __launch_bounds__(256) void join_splits_kernel(AttendArgs a)
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     *(i32x2 *)(a.out + (at * D + d) * 2) = i32x2{pack2<DT>(o[0] * inv, o[1] * inv), pack2<DT>(o[2] * inv, o[3] * inv)};
-    if (a.lse && d == 0) *(float2 *)(a.lse + 2 * at) = l == 0.0f ? float2{-INFINITY, 0.0f} : float2{c, top + logf(l)};
+    if (a.lse && d == 0) *(float2 *)(a.lse + 2 * at) = c == -INFINITY ? float2{-INFINITY, 0.0f} : float2{c, top + logf(l)};
 }
 
 template <int DT, int D, int NW>

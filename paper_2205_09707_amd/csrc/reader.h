@@ -16,7 +16,8 @@ struct AttendArgs {
     const char *bias;                  // [num_keys] of the type, or null
     const int64_t *q_offsets, *k_offsets;
     char *out;
-    float *lse;                        // pairs whose sum is the logarithm of the sum of exponentials: a shift, and the rest; may be null
+    float *lse;                        // pairs whose sum is the logarithm of the sum of exponentials: a shift, and the rest; may be null.
+                                       // (-infinity, 0): no key; (the biases' shift, -infinity): keys whose scores are all -infinity
     int64_t num_queries, num_keys;
     int64_t q_token, q_head, k_token, k_head, v_token, v_head;  // strides in bytes
     int32_t n, heads, kv_heads, group;
@@ -351,12 +352,13 @@ __device__ __forceinline__ void wait_loads()
 // Biases.  Scores s + b are formed as s + (b - c) with a shift c, so that a mask of the type's lowest value, or any other large
 // bias that all of a row's keys have, costs the scores nothing.  c depends on the biases of the keys that are not masked alone:
 // 0 where the largest of them is within BIAS_USUAL, else the largest.  A part of the keys has its own; parts are joined under the
-// largest.  Beside a bias beyond BIAS_ALL a score vanishes, as it does in a sum in 64 bits.
+// largest.  So all rows of a request have one, also a row whose scores are -infinity throughout.  Beside a bias beyond BIAS_ALL a score vanishes, as it does in a sum in 64 bits.
 #define BIAS_USUAL 256.0f
 #define BIAS_ALL 4503599627370496.0f
 struct Shift {
     float c = 0.0f, most = -INFINITY;  // most: the largest unusual bias
     bool usual = false, seen = false;  // whether a usual, an unusual one was seen
+    __device__ __forceinline__ bool any() const { return usual || seen; }
     // Takes in a wave's biases: lanes that have an unusual one, their largest (looked at where there are any), whether any lane has
     // a usual one.
     __device__ __forceinline__ void add(uint64_t unusual, float largest, bool any_usual)
@@ -374,7 +376,9 @@ struct Shift {
     }
 };
 __device__ __forceinline__ bool unusual_bias(float b) { return fabsf(b) > BIAS_USUAL && b != -INFINITY; }
-__device__ __forceinline__ float beside_shift(float scale, float c) { return fabsf(c) > BIAS_ALL ? 0.0f : scale; }
+__device__ __forceinline__ bool beside(float c) { return fabsf(c) > BIAS_ALL; }
+// A score that vanishes beside b, unless it is not finite.
+__device__ __forceinline__ float vanish(float s, float b) { return fabsf(s) < INFINITY ? b : s; }
 
 // Waits for all of the wave's loads, and lets the compiler know: one that it is unsure of it would wait for in every round of a loop.
 __device__ __forceinline__ void wait_all_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }

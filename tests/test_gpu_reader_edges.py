@@ -56,3 +56,44 @@ def test_a_last_row_that_is_not_finite(pl, m, n, heads, dtype):  # noqa: F811
             _, dk, dv, _ = pl.plaid_cross_attention_backward(o, q, k, v, out, lse, _off([m, m]), _off([n, n]))
             assert torch.isinf(dv[:n, 0, 9]).all() and torch.isfinite(dv[:, 1]).all() and torch.isfinite(dv[n:]).all() and torch.isfinite(dk[n:]).all()
             assert torch.isfinite(dv[..., :9]).all() and torch.isfinite(dv[..., 10:]).all()
+
+
+@pytest.mark.parametrize("low", [-1000.0, 3000.0, -3e38])
+@pytest.mark.parametrize("m,n,heads", [(3, 40, 2), (3, 3000, 2), (40, 90, 4), (300, 200, 8), (300, 2000, 8)])
+def test_a_row_whose_scores_overflow(pl, m, n, heads, low):  # noqa: F811
+    """The first row's products are -infinity throughout, so no weight is left there.  The other rows of its request, whose biases are all
+    far from zero, have their gradients all the same."""
+    dim = 64
+    q, k, v, d_out = (_randn((x, h, dim), i, BF) for i, (x, h) in enumerate(((m, heads), (n, 2), (n, 2), (m, heads))))
+    q[..., 0], k[..., 0] = 0.0, 1e10
+    q[0, 0, 0] = -1e32
+    d_out[0, 0] = 0.0
+    bias = (torch.randn(n, generator=torch.Generator().manual_seed(4)) * 8 + low).to(BF)
+    d = lambda t: t.to(DEV)  # noqa: E731
+    out, lse = pl.plaid_cross_attention(d(q), d(k), d(v), _off([m]), _off([n]), key_bias=d(bias), return_lse=True)
+    assert not out[0, 0].any() and float(lse[0, 0].sum()) == -math.inf
+    got = pl.plaid_cross_attention_backward(d(d_out), d(q), d(k), d(v), out, lse, _off([m]), _off([n]), key_bias=d(bias))
+    assert not got[0][0, 0].any()
+    want = ru.cross(q, k, v, [m], [n], dim ** -0.5, bias, d_out)
+    keep = torch.ones(m, heads, dtype=torch.bool)
+    keep[0, 0] = False
+    for name, x in zip(("out", "dq"), (out, got[0])):
+        ru.close(x.cpu()[keep], want[name][keep], want[name + "_bound"][keep], name)
+    for name, x in zip(("dk", "dv", "dbias"), got[1:]):
+        ru.close(x[..., 1:] if x.dim() == 3 else x, *(want[name + e][..., 1:] if x.dim() == 3 else want[name + e] for e in ("", "_bound")), name)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("m,n,heads", [(1, 40, 2), (3, 3000, 2), (40, 90, 4), (300, 200, 8), (300, 2000, 8)])
+def test_a_key_that_is_not_finite_beside_the_lowest_biases(pl, m, n, heads, dtype):  # noqa: F811
+    """Scores vanish beside biases of the type's lowest value; a key that is not a number makes its rows so all the same."""
+    q, k, v, d_out = (_randn((x, h, 64), i, dtype).to(DEV) for i, (x, h) in enumerate(((2 * m, heads), (2 * n, 2), (2 * n, 2), (2 * m, heads))))
+    k[n // 2, 1, 3] = math.nan
+    bias = torch.full((2 * n,), torch.finfo(dtype).min, dtype=dtype, device=DEV)
+    out, lse = pl.plaid_cross_attention(q, k, v, _off([m, m]), _off([n, n]), key_bias=bias, return_lse=True)
+    half = heads // 2
+    assert torch.isnan(out[:m, half:]).all() and torch.isfinite(out[:m, :half]).all() and torch.isfinite(out[m:]).all()
+    dq, dk, dv, _ = pl.plaid_cross_attention_backward(d_out, q, k, v, out, lse, _off([m, m]), _off([n, n]), key_bias=bias)
+    for x, at in ((dq, m), (dk, n), (dv, n)):
+        first = x.shape[1] // 2
+        assert torch.isnan(x[:at, first:]).all() and torch.isfinite(x[:at, :first]).all() and torch.isfinite(x[at:]).all()
