@@ -61,35 +61,40 @@ __device__ __forceinline__ Request uniform_request(const AttendArgs &a, int r)
     if (q.steps < 1) q.steps = 1;
     return q;
 }
-__device__ __forceinline__ int wave_sum(int x)
+template <typename T>
+__device__ __forceinline__ T wave_sum(T x)
 {
 #pragma unroll
     for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
     return x;
 }
-__device__ __forceinline__ int wave_prefix(int x)  // sum over lower lanes and this one
+template <typename T>
+__device__ __forceinline__ T wave_prefix(T x)  // sum over lower lanes and this one
 {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
+        const T y = __shfl_up(x, o);
         if (lane >= o) x += y;
     }
     return x;
 }
-// Steps of all requests and of those before r.  (The host takes these kernels where all counts of steps fit 32 bits.)
+// Steps of all requests and of those before r.  The host takes these kernels where the counts of steps fit 32 bits, a request's whatever the
+// offsets hold, all requests' if the offsets ascend.  Others may claim a row many times over: the sum is formed in 64 bits, and where it
+// does not fit, 0 is returned and nothing is done.
 template <int SRC, int NW>
 __device__ __forceinline__ int all_work(const AttendArgs &a, int r, int &before)
 {
-    int all = 0, some = 0;
+    int64_t all = 0, some = 0;
     for (int i = threadIdx.x & 63; i < a.n; i += 64) {
         const Request q = request<SRC, NW>(a, i);
         const int w = q.tiles * q.steps;
         all += w;
         if (i < r) some += w;
     }
-    before = wave_sum(some);
-    return wave_sum(all);
+    before = (int)wave_sum(some);
+    all = wave_sum(all);
+    return all > INT32_MAX ? 0 : (int)all;
 }
 // The worker's stretch at .. end - 1 of the line, the request that holds its beginning (-1: the stretch is empty) and the
 // place where that request begins.
@@ -97,12 +102,14 @@ template <int SRC, int NW>
 __device__ __forceinline__ int find_work(const AttendArgs &a, int workers, int worker, int &at, int &end, int &first)
 {
     const int lane = threadIdx.x & 63, per = (a.n + 63) >> 6;
-    int mine = 0;
+    int64_t sum = 0;
     for (int i = lane * per; i < min(a.n, (lane + 1) * per); ++i) {
         const Request q = request<SRC, NW>(a, i);
-        mine += q.tiles * q.steps;
+        sum += q.tiles * q.steps;
     }
-    const int upto = wave_prefix(mine), total = uniform(__shfl(upto, 63)), share = (int)(((uint32_t)total + workers - 1) / (uint32_t)workers);
+    const int64_t sums = wave_prefix(sum), all = uniform(__shfl(sums, 63));
+    if (all > INT32_MAX) return -1;
+    const int mine = (int)sum, upto = (int)sums, total = (int)all, share = (int)(((uint32_t)total + workers - 1) / (uint32_t)workers);
     if ((int64_t)worker * share >= total) return -1;
     at = worker * share;
     end = min(total, at + share);
@@ -112,7 +119,7 @@ __device__ __forceinline__ int find_work(const AttendArgs &a, int workers, int w
         return block;
     }
     int left = __shfl(upto - mine, block);
-    for (int i = block * per;; i += 64) {
+    for (int i = block * per; i < a.n; i += 64) {
         int w = 0;
         if (i + lane < a.n) {
             const Request q = request<SRC, NW>(a, i + lane);
@@ -125,6 +132,7 @@ __device__ __forceinline__ int find_work(const AttendArgs &a, int workers, int w
         }
         left = __shfl(to, 63);
     }
+    return -1;
 }
 
 template <int DT, int D, int SRC>
@@ -531,6 +539,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_workers_kernel(AttendArgs a
     const int head_kv = blockIdx.y;
     int before;
     const int total = all_work<SRC, NW>(a, tp.r, before), share = (int)(((uint32_t)total + workers - 1) / (uint32_t)workers);
+    if (total == 0) return;
     const Request rq = request<SRC, NW>(a, tp.r);
     const int begin = before + tp.tile * rq.steps, end = begin + rq.steps;
     const int w0 = (int)((uint32_t)begin / (uint32_t)share), w1 = (int)((uint32_t)(end - 1) / (uint32_t)share);

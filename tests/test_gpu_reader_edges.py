@@ -97,3 +97,17 @@ def test_a_key_that_is_not_finite_beside_the_lowest_biases(pl, m, n, heads, dtyp
     for x, at in ((dq, m), (dk, n), (dv, n)):
         first = x.shape[1] // 2
         assert torch.isnan(x[:at, first:]).all() and torch.isfinite(x[:at, :first]).all() and torch.isfinite(x[at:]).all()
+
+
+def test_offsets_that_claim_rows_many_times(pl):  # noqa: F811
+    """Offsets that do not ascend: half of 3000 requests claim all of 40 000 tokens and 131 072 keys, 3.8e9 steps of work, which 32 bits do
+    not hold.  What they get is unspecified; the call ends, touches nothing else, and the next one is right."""
+    n, nq, nk = 3000, 40_000, 131_072
+    q, k = _randn((nq, 1, 64), 1, BF).to(DEV), _randn((nk, 1, 64), 2, BF).to(DEV)
+    off = lambda x: torch.tensor([0, x], device=DEV).repeat(n // 2 + 1)[:n + 1].contiguous()  # noqa: E731
+    want = pl.plaid_cross_attention(q[:3], k, k, _off([1, 1, 1]), _off([nk, 0, 0]))
+    for _ in range(2):
+        pl.plaid_cross_attention(q, k, k, off(nq), off(nk))
+        torch.cuda.synchronize()
+    assert torch.equal(q.cpu(), _randn((nq, 1, 64), 1, BF)) and torch.equal(k.cpu(), _randn((nk, 1, 64), 2, BF))
+    assert torch.equal(pl.plaid_cross_attention(q[:3], k, k, _off([1, 1, 1]), _off([nk, 0, 0])), want)
