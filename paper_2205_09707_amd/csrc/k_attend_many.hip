@@ -468,7 +468,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_many_kernel(AttendArgs a, i
         float top;
         if constexpr (SRC == PLAID_SOURCE_BIAS) {
             if (stage.shifts[0] != shift) {  // m is relative to the shift
-                m += (__int_as_float(shift) - __int_as_float(stage.shifts[0])) * a.inv_scale;
+                // in one operation: the product alone may overflow, and m may be -infinity
+                m = fmaf(__int_as_float(shift) - __int_as_float(stage.shifts[0]), a.inv_scale, m);
                 shift = stage.shifts[0];
                 alone = uniform((int)beside(__int_as_float(shift)));
             }
