@@ -19,7 +19,7 @@
 // ------------------------------------------------------------------ errors
 static thread_local char g_err[512] = "";
 
-static int fail(int code, const char *fmt, ...)
+int plaid_fail(int code, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -27,15 +27,8 @@ static int fail(int code, const char *fmt, ...)
     va_end(ap);
     return code;
 }
+static int (*const fail)(int, const char *, ...) = plaid_fail;
 extern "C" const char *plaid_last_error(void) { return g_err; }
-int plaid_fail(int code, const char *fmt, ...)  // for the other translation units
-{
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_err, sizeof(g_err), fmt, ap);
-    va_end(ap);
-    return code;
-}
 
 #define HIP_TRY(expr)                                                                                         \
     do {                                                                                                      \

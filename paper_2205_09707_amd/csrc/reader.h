@@ -388,7 +388,8 @@ static __device__ const i32x4 zero_row[16] = {};
 
 // 16 (4) bytes of every lane, from base + off, into the 1024 (256) bytes of LDS at `to` (the same for all lanes), lane after lane.
 // There is no result in registers and the compiler does not count these loads: it would have every transposing read of LDS wait
-// for all of them.  (They go by register m0, which nothing else in these kernels uses.)  What they bring is waited for with
+// for all of them.  (They go by register m0, which is reserved: the compiler keeps nothing there and sets it itself before what
+// needs it, so it cannot be named as overwritten.)  What they bring is waited for with
 // wait_loads, before the barrier that lets it be read and before the end.
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p; }
 __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t to)
