@@ -27,8 +27,8 @@ int launched()
     return e == hipSuccess ? PLAID_OK : plaid_fail(PLAID_EHIP, "kernel launch: %s", hipGetErrorString(e));
 }
 bool misaligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-int64_t round16(int64_t x) { return (x + 15) & ~(int64_t)15; }
+constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t round16(int64_t x) { return (x + 15) & ~(int64_t)15; }
 bool block_size_ok(int32_t b) { return b == 16 || b == 32 || b == 64 || b == 128 || b == 256; }
 
 int check_cache(const plaid_paged_cache *c)
@@ -55,7 +55,7 @@ struct Plan {
 
 // Parts that an axis of `steps` steps is cut into, at least `least` of them a part, where `groups` workgroups of so many waves leave
 // compute units empty: one of eight waves has room on each, two of four.  One part too many would start a second round.
-int64_t split_count(int64_t groups, int waves, int64_t steps, int64_t least)
+constexpr int64_t split_count(int64_t groups, int waves, int64_t steps, int64_t least)
 {
     int64_t s = UNITS * 8 / waves / (groups < 1 ? 1 : groups);
     if (s > steps / least) s = steps / least;
@@ -68,7 +68,7 @@ int64_t split_count(int64_t groups, int waves, int64_t steps, int64_t least)
 //   16 heads on 4, D = 128, 4 requests of 64 tokens x 450 keys: 10.8 and 21.3;  x 2000: 31.6 and 29.5;  16 of 64 x 450: 37.2 and 29.0
 //   12 heads on 12, D = 64, 4 requests of 128 tokens x 450 keys: 11.4 and 15.8;  of 64 x 2000: 23.9 and 22.2;  16 of 96 x 450: 26.2 and 23.0
 //   paged, 32 heads on 8, 4 requests of 32 tokens x 2000 keys: 17.0 and 31.3;  16 of 8 x 8000: 52.4 and 93.2;  16 of 32 x 2000: 61.5 and 47.4
-bool few_rows(int64_t rows, int64_t n, int64_t kv_heads, int64_t keys, int head_dim, int source)
+constexpr bool few_rows(int64_t rows, int64_t n, int64_t kv_heads, int64_t keys, int head_dim, int source)
 {
     if (rows <= FEW_ROWS) return true;
     const bool paged = source == PLAID_SOURCE_PAGED;
@@ -77,7 +77,7 @@ bool few_rows(int64_t rows, int64_t n, int64_t kv_heads, int64_t keys, int head_
 }
 
 // keys: of all requests; longest: that a request can have; usual: to reckon with
-Plan plan_forward(const plaid_attention &a, int source, int64_t keys, int64_t longest, int64_t usual)
+constexpr Plan plan_forward(const plaid_attention &a, int source, int64_t keys, int64_t longest, int64_t usual)
 {
     Plan p = {};
     const int64_t group = a.heads / a.kv_heads, tokens = ceil_div(a.num_queries, a.n), rows = tokens * group;
@@ -107,7 +107,7 @@ Plan plan_forward(const plaid_attention &a, int source, int64_t keys, int64_t lo
     return p;
 }
 
-Plan plan_backward(const plaid_attention &a)
+constexpr Plan plan_backward(const plaid_attention &a)
 {
     Plan p = {};
     const int64_t group = a.heads / a.kv_heads, rows = ceil_div(a.num_queries, a.n) * group, keys = ceil_div(a.num_keys, a.n);
@@ -288,7 +288,7 @@ static int check_cached(const plaid_attention *args, int32_t max_blocks, int32_t
     if (max_blocks < 1 || (int64_t)max_blocks * block_size > (1 << 30)) FAIL("max_blocks %d out of range", max_blocks);
     return PLAID_OK;
 }
-static Plan plan_cached(const plaid_attention &a, int32_t max_blocks, int32_t block_size)
+static constexpr Plan plan_cached(const plaid_attention &a, int32_t max_blocks, int32_t block_size)
 {
     const int64_t longest = (int64_t)max_blocks * block_size;
     return plan_forward(a, PLAID_SOURCE_PAGED, longest * a.n, longest, longest);
@@ -320,7 +320,7 @@ extern "C" int plaid_cached_attention(const plaid_attention *args, const plaid_p
     return run_forward(*args, x, plan_cached(*args, max_blocks, cache->block_size), PLAID_SOURCE_PAGED, workspace, workspace_bytes, device, hip_stream);
 }
 
-static Plan plan_cross(const plaid_attention &a)
+static constexpr Plan plan_cross(const plaid_attention &a)
 {
     return plan_forward(a, a.key_bias ? PLAID_SOURCE_BIAS : PLAID_SOURCE_DENSE, a.num_keys, a.num_keys, ceil_div(a.num_keys, a.n));
 }
