@@ -213,7 +213,8 @@ def plaid_cached_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tens
     """Attention of q [tokens, heads, head_dim] over a paged cache: request r's queries are rows q_offsets[r] .. q_offsets[r+1]-1
     (int64 [n+1]), its keys the lengths[r] (int32) tokens that table[r] ([n, max_blocks] int32) leads to.  causal: the queries are
     the request's last tokens, each sees what is not after it.  scale: head_dim ** -0.5 by default.  Returns out like q, with
-    return_lse also the logarithm of the softmax's sum as two numbers to be added, [tokens, heads, 2] float32."""
+    return_lse also the logarithm of the softmax's sum as two numbers to be added, [tokens, heads, 2] float32.  It has no gradient:
+    what the cache holds is rounded."""
     _check_queries(q)
     dev = q.device
     if cache.data.device != dev or q.dtype != cache.dtype:
@@ -256,13 +257,24 @@ def _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias):
     return _rows(q), _rows(k), _rows(v), q_offsets, k_offsets, key_bias
 
 
+def _no_autograd(**tensors) -> None:
+    """The calls are not recorded: where one would be differentiated through, its result would be cut off without a word."""
+    if torch.is_grad_enabled():
+        for name, t in tensors.items():
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{name} requires a gradient, which this call does not record: call it in torch.no_grad(), or in a "
+                                 "torch.autograd.Function whose backward calls plaid_cross_attention_backward")
+
+
 def plaid_cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor,
                           key_bias: Optional[torch.Tensor] = None, scale: Optional[float] = None, return_lse: bool = False):
     """Attention of q [tokens, heads, head_dim] to states of another length, k and v [keys, kv_heads, head_dim], both packed:
     request r owns rows q_offsets[r] .. q_offsets[r+1]-1 and keys k_offsets[r] .. k_offsets[r+1]-1 (int64 [n+1]).  key_bias [keys]
     of q's dtype is added to the scores; -inf takes a key out.  Returns out like q (rows outside every request are not written),
-    with return_lse also the two numbers a row that plaid_cross_attention_backward wants."""
+    with return_lse also the two numbers a row that plaid_cross_attention_backward wants.  Not recorded by autograd: inputs that
+    require a gradient are refused where it is enabled (examples/reader.py has the torch.autograd.Function of both calls)."""
     rows, keys, values, q_offsets, k_offsets, key_bias = _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias)
+    _no_autograd(q=q, k=k, v=v, key_bias=key_bias)
     dev = q.device
     out = _like(q)
     lse = torch.empty(q.shape[:2] + (2,), dtype=torch.float32, device=dev) if return_lse else None
