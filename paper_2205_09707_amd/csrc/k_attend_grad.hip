@@ -43,17 +43,19 @@ __device__ __forceinline__ float request_shift(const AttendArgs &a, int64_t row0
     return c == -INFINITY ? 0.0f : c;
 }
 
-// Whether a request has one key that is not masked.  Then P = 1 and dP = delta by definition, and dq, dk and dbias are zero: what is left of
-// dP - delta in 32 bits is rounding.  The loop ends where a second one is found, mostly in its first round.
+// Whether a key can have a weight beside the shift c: not with a bias of -infinity, nor with one so low that no score makes up for it.
+__device__ __forceinline__ bool weighs(float bias, float c) { return !(bias - c <= -0x1p100f); }
+
+// Whether a request has one such key.  Then P = 1 and dP = delta by definition, and dq, dk and dbias are zero: what is left of dP - delta in
+// 32 bits is rounding.  The loop ends where a second one is found, mostly in its first round.
 template <int DT, bool BIAS>
-__device__ __forceinline__ bool one_key(const AttendArgs &a, int64_t key0, int len)
+__device__ __forceinline__ bool one_key(const AttendArgs &a, int64_t key0, int len, float c)
 {
-    constexpr uint16_t NONE = DT == PLAID_BF16 ? 0xff80 : 0xfc00;  // -infinity
     if (!BIAS) return len == 1;
     int live = 0;
     for (int at = threadIdx.x & 63; live < 2; at += 256) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) live += __popcll(__ballot(at + 64 * i < len && ((const uint16_t *)a.bias)[key0 + min(at + 64 * i, len - 1)] != NONE));
+        for (int i = 0; i < 4; ++i) live += __popcll(__ballot(at + 64 * i < len && weighs(load16<DT>(a.bias + 2 * (key0 + min(at + 64 * i, len - 1))), c)));
         if (uniform(at) + 256 >= len) break;
     }
     return live == 1;
@@ -317,8 +319,8 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
     }
 
     dbias = sum_halves(dbias);
-    const int own = __popc((uint32_t)__ballot(there && !(BIAS && bias == -INFINITY)));  // of the wave's keys
-    const bool one = second && own == 1 && one_key<DT, BIAS>(a, tp.begin, len);
+    const int own = __popc((uint32_t)__ballot(there && (!BIAS || weighs(bias, c))));  // of the wave's keys
+    const bool one = second && own == 1 && one_key<DT, BIAS>(a, tp.begin, len, c);
     if (!there) return;
     // a masked key's column may hold anything and is zero
     const bool masked = BIAS && bias == -INFINITY;
@@ -432,7 +434,6 @@ __device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, in
 
     // keys past the end repeat the last one; tiles past the last repeat that
     uint32_t masked = 0;  // keys of bias -infinity, and places past the end, in the tile that is asked for next
-    int live = 0;         // keys that are not masked
     const char *keys = a.k + key0 * a.k_token + head_kv * a.k_head, *values = a.v + key0 * a.v_token + head_kv * a.v_head;
     uint32_t key_row[N], value_row[N], chunk[N];  // bytes of a lane's row in a tile, and within the row
     const uint32_t to_k = lds_address(lds.k[0]) + wave * N * 1024, to_v = lds_address(lds.v[0]) + wave * N * 1024;
@@ -472,7 +473,6 @@ __device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, in
         const uint16_t x = min(step, end - 1) * GRAD_KEYS + (lane & 31) < len ? (uint16_t)raw : NONE;
         lds.bias[wave][step & 3][lane & 31] = (unpack<DT>(x, 0) - c) * a.inv_scale;
         masked = (uint32_t)__ballot(x == NONE);
-        if (step < end) live += __popc(~masked);
     };
     f32x16 s, ds;  // q k^T + b / scale, dO v^T - delta
     i32x4 r[2];
@@ -609,10 +609,12 @@ __device__ __forceinline__ void grad_q_pass(const GradArgs &g, int64_t tiles, in
         add(end - 1);
         wait_loads<0>();  // nothing may arrive in LDS that is no longer the workgroup's
     }
-    const bool one = BIAS ? live == 1 && (splits == 1 || one_key<DT, true>(a, key0, len)) : len == 1;
+    bool one = AGAIN && one_key<DT, BIAS>(a, key0, len, c);
     if constexpr (!AGAIN) {
-        float off = 0.0f, size = 0.0f;
-        if (steps > 1 && counts && !one) off = lds.sums[threadIdx.x].x, size = lds.sums[threadIdx.x].y;
+        float off = lds.sums[threadIdx.x].x, size = lds.sums[threadIdx.x].y;
+        // with one key the two are one number: otherwise there is nothing to look for
+        one = !__any(there && fabsf(off) != size) && one_key<DT, BIAS>(a, key0, len, c);
+        if (steps <= 1 || !counts || one) off = size = 0.0f;
         off = sum_halves(off), size = sum_halves(size);
         if (splits > 1) {
             if (there && h == 0) *(float2 *)(g.row_part + 2 * ((int64_t)split * a.num_queries * a.heads + at)) = float2{off, size};

@@ -47,6 +47,18 @@ def test_one_key_that_counts(pl, n, at, m, dim, heads, kv_heads, dtype):  # noqa
     ru.close(dv, want["dv"], want["dv_bound"], "dv")
 
 
+@pytest.mark.parametrize("dim,heads,kv_heads", [(64, 3, 3), (128, 8, 2)])
+@pytest.mark.parametrize("n,at,m", [c for c in ONE if c[1] is not None])
+def test_one_key_beside_masks_of_the_lowest_value(pl, n, at, m, dim, heads, kv_heads):  # noqa: F811
+    """Beside a key of an ordinary bias those of bfloat16's lowest value have weights of zero: the gradients are zero as well."""
+    q, k, v, d_out = _inputs([m], [n], heads, kv_heads, dim, BF, n + m)
+    bias = torch.full((n,), torch.finfo(BF).min, dtype=BF)
+    bias[at] = 0.75
+    out, (dq, dk, dv, dbias) = _gradients(pl, q, k, v, d_out, bias, [m], [n])
+    assert torch.equal(out.cpu(), v[at].repeat_interleave(heads // kv_heads, 0).expand(m, heads, dim))
+    assert not dq.any() and not dk.any() and not dbias.any()
+
+
 @pytest.mark.parametrize("dtype", [BF, HF])
 def test_one_key_beside_other_requests(pl, dtype):  # noqa: F811
     """A request with one key that counts among others, in both orders of requests (up to 64 of them and more)."""
