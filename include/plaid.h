@@ -339,7 +339,7 @@ int plaid_cache_read(const plaid_paged_cache *cache, const int64_t *slots, int64
 /* Arguments of an attention call.  Row (token i of request r, head h) attends with key head h * kv_heads / heads:
  *   s_j = scale * q . k_j + key_bias_j,   out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j);
  * a row that no key is left for gives zeros and -INFINITY.  lse is two numbers to be added, a shift
- * (0 unless all of a request's biases are beyond 256 in magnitude) and the rest, so that it is whole where all scores are as low as
+ * (0 unless the largest of a request's biases is above 256, or below -256) and the rest, so that it is whole where all scores are as low as
  * the type goes.  Sums, softmax statistics and their exponentials are held in 32
  * bits; the softmax's weights round to the type before they multiply the values.
  *   q, k, v          [num_queries | num_keys][heads | kv_heads][head_dim] of dtype, 16-byte aligned, the strides of tokens and
@@ -392,8 +392,9 @@ int plaid_cross_attention(const plaid_attention *args, void *workspace, int64_t 
 /* Its gradients: with P = exp(s - lse), dP = d_out . v and dS = P (dP - d_out . out),
  *   dv_j = sum P d_out,  dk_j = scale sum dS q,  dq_i = scale sum_j dS k,  dbias_j = sum of dS over all rows and heads.
  * args->out and args->lse are what the forward call gave; d_out [num_queries][heads][head_dim] contiguous; dq like d_out, dk and
- * dv [num_keys][kv_heads][head_dim] contiguous, dbias [num_keys], all of dtype; each may be NULL.  Every sum has one order: the
- * same inputs give the same bits.  fp16: the gradient's range is the type's, so the caller scales the loss. */
+ * dv [num_keys][kv_heads][head_dim] contiguous, dbias [num_keys], all of dtype; each may be NULL, which changes nothing of the others.  Every
+ * sum has one order: the same inputs give the same bits.  dq, dk and dbias are zero where one key of a request can have a weight.  fp16: the
+ * gradient's range is the type's, so the caller scales the loss. */
 int plaid_cross_attention_backward(const plaid_attention *args, const void *d_out, void *dq, void *dk, void *dv, void *dbias,
                                    void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
 int plaid_cross_attention_workspace(const plaid_attention *args, int32_t backward, int64_t *bytes);

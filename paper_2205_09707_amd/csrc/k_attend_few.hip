@@ -14,8 +14,8 @@
 // join: one launch in place of two.)  A worker's stretch is a tail of a tile, whole tiles and a head of one: whole tiles it finishes,
 // the two others leave their sums in its two places, and join_workers_kernel adds them up in the order of the line.
 //
-// Bound by reading: 64 contexts of 1 to 8192 tokens in the cache, 8 key heads of 128 (279 MB): 59 us = 4.7 TB/s and 7.5 of joining, which is
-// a chain of loads by 64 x 8 workgroups; 4 of 115 000 (523 MB): 99 = 5.3 TB/s and 10; 4 x 65 000 dense keys with biases (1.07 GB): 195 = 5.5
+// Bound by reading: 64 contexts of 1 to 8192 tokens in the cache, 8 key heads of 128 (279 MB): 58 us = 4.8 TB/s and 8 of joining, which is
+// a chain of loads by 64 x 8 workgroups; 4 of 115 000 (523 MB): 101 = 5.2 TB/s and 11; 4 x 65 000 dense keys with biases (1.07 GB): 195 = 5.5
 // TB/s and 9.5.  Twice the workers: 65.5 in place of 63.4, and 29 in place of 21 for one context of 20 000.
 
 template <int SRC>

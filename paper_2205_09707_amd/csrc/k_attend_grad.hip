@@ -64,10 +64,10 @@ __device__ __forceinline__ bool one_key(const AttendArgs &a, int64_t key0, int l
 // What the rows bring (-lse / scale, -delta) and the keys' biases over the scale are what the matrix instruction adds the products to;
 // a weight then takes one multiply-add and an exponential.  P and dS round to the type before they are multiplied again; P, which is at most 1
 // and with many keys far below what fp16 holds in full (2^-14), times 2^WEIGHT there, which dv is freed of in the end.
-// Measured on 16 requests of 456 tokens x 16 heads, 6250 keys of 4 heads, D = 128, biases: grad_k 830 us (746 GFLOP, 0.90 PFLOP/s),
-// grad_q 545 (560 GFLOP, 1.03 PFLOP/s), delta 12 (180 MB, 4.6 TB/s with the statistics).  Bound by products and what feeds them: without
-// exponentials both together took 1454 in place of 1522, without loads 1298.  Both in one launch are no faster (the same for short
-// answers, 1684 in place of 1565 for these).
+// Measured on 16 requests of 456 tokens x 16 heads, 6250 keys of 4 heads, D = 128, biases: grad_k 843 us (746 GFLOP, 0.89 PFLOP/s),
+// grad_q 598 (560 GFLOP, 0.94 PFLOP/s; its sums of dS and |dS| take 50 of them), delta 12 (180 MB, 4.6 TB/s with the statistics), the last
+// launch 6.  Bound by products and what feeds them: before those sums, without exponentials both together took 1454 in place of 1522, without
+// loads 1298.  Both in one launch are no faster (the same for short answers, 1684 in place of 1565 for these).
 
 // --- gradients of keys and values ---------------------------------------------------------------------------------------------
 // A wave of 32 keys would hold their keys, values and both sums, 192 registers, before it multiplies anything.  So two waves of
@@ -344,14 +344,14 @@ __global__ __launch_bounds__(NW * 64, 2) void grad_k_kernel(GradArgs g, int64_t 
 
 // --- gradients of queries -----------------------------------------------------------------------------------------------------
 // A wave owns 32 rows: q, dO and the sum dq in registers, 32 keys a step.  Workgroups of four waves, two on a compute unit, so that one
-// multiplies while the other forms exponentials: 545 us in place of 650 for eight waves in phases at D = 128, 934 in place of 1010 for
-// both gradients at 64.  For a request of at most 32 keys one step sees all of a
-// row, and delta is the sum of P dP over that of P.
+// multiplies while the other forms exponentials: a sixth less time than eight waves in phases at D = 128 (545 in place of 650 us), 934 in place
+// of 1010 for both gradients at 64.  For a request of at most 32 keys one step sees all of a row, and delta is the sum of P dP over that of P.
 //
-// Other requests begin with delta = dO . out, whose error, that of an out rounded to the type, grows with |dO| |out| and not with dS: 4 of 1000
-// off in dq and dk where two keys of bf16 share the weight, 11 of 100 where one has 0.99 of it.  But the sum of dS over a row's keys is zero, so what
+// Other requests begin with delta = dO . out, whose error, that of an out rounded to the type, grows with |dO| |out| and not with dS: in bf16
+// 3.6 of 1000 off in dq where two keys share the weight, 85 where one has 0.99 of it.  But the sum of dS over a row's keys is zero, so what
 // it comes to is that error.  It is added to delta, for grad_k_kernel as well, and where it is more than DELTA_OFF of the sum of |dS|, half of
-// what rounding dS costs, finish_kernel makes the rows' pass over the keys again.  Weights spread over tens of keys do not come near that.
+// what rounding dS costs, finish_kernel makes the rows' pass over the keys again: 2.3 of 1000 then, as everywhere.  Weights spread over some
+// hundred keys do not come near that; 16 short answers on up to 900 keys, the shortest on 70, pay 5 us for second passes and 5 for joining the sums.
 #define GRAD_KEYS 32
 #define DELTA_OFF(DT) ((DT) == PLAID_BF16 ? 0x1p-9f : 0x1p-12f)
 template <int D, bool BIAS>

@@ -16,8 +16,8 @@
 //
 // What bounds it: one group's vector instructions (exponential 16 cycles, multiply-add, half a maximum, half a rounding and one addition a
 // score) against the other's products.  Measured: 16 requests of 456 tokens x 16 heads on 6250 keys of 4 heads, D = 128 (373 GFLOP):
-// 373 us without biases, 433 with = 1.00 and 0.86 PFLOP/s; 381 without products first, 395 before addresses of loads were kept in
-// registers.  6 prompts of 850 tokens x 32 heads behind 4750 in the cache (419 GFLOP): 475 us = 0.88 PFLOP/s; what is left there is the
+// 378 us without biases, 462 with = 0.99 and 0.81 PFLOP/s, many calls in a row; products first and addresses of loads kept in registers took
+// 2 % each off.  6 prompts of 850 tokens x 32 heads behind 4750 in the cache (419 GFLOP): 482 us = 0.87 PFLOP/s; what is left there is the
 // codes' way into values, which every 256 rows pay.
 //
 // Tiles that lie in LDS at a time, and how many tiles ahead of the weights' one keys and values are asked for.  With two groups of

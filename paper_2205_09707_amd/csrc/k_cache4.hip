@@ -4,7 +4,7 @@
 // 8 values of a lane are 16 bytes; four lanes share a scale.  The codes of 16-bit values leave at a quarter of what came in, so
 // both directions are bound by the 16-bit side.  Value codes interleave four tokens: a thread that finds four tokens in a row
 // of slots stores their bytes as one piece (16 bytes at D = 128), others byte by byte.  65003 tokens of 8 heads of 128, keys and values
-// (266 MB of 16 bits, 71 of codes and scales): written in 76 us (4.4 TB/s), read back in 77; a decode step's 64 tokens 3.5 each.
+// (266 MB of 16 bits, 71 of codes and scales): written in 75 us (4.5 TB/s), 87 between other calls, read back in 78; a decode step's 64 tokens 3.6 each.
 template <int DT>
 struct Limits {
     static constexpr int TOP = DT == PLAID_BF16 ? 126 : 14, LOWEST = DT == PLAID_BF16 ? -126 : -23, INF = DT == PLAID_BF16 ? 0x7f80 : 0x7c00;

@@ -4,7 +4,7 @@
 // Two prefix sums over the requests (tokens, blocks) and a pass over the tokens, which is all writing: 12 bytes a token.  Up to
 // TABLES_ONE requests each workgroup forms both sums in LDS for itself, so that a step needs one launch and no workspace; the
 // sums cost it 8 n bytes from L2, its tokens 12 KB of writes.  More requests take a launch that leaves the sums in the workspace.
-// 1000 prompts of 6500 tokens: 21 us, 3.8 TB/s of writes, of which about 5 go before a workgroup's first token; a step of 16 requests 4.6.
+// 1000 prompts of 6500 tokens: 22 us, 3.6 TB/s of writes, of which about 5 go before a workgroup's first token; a step of 16 requests 4.6.
 #define TABLES_ONE 2048
 #define TABLES_THREADS 256
 #define TABLES_TOKENS 4  // neighbouring tokens of a thread: 16-byte stores
