@@ -51,7 +51,7 @@ __device__ __forceinline__ bool weighs(float bias, float c) { return !(bias - c 
 template <int DT, bool BIAS>
 __device__ __forceinline__ bool one_key(const AttendArgs &a, int64_t key0, int len, float c)
 {
-    if (!BIAS) return len == 1;
+    if (!BIAS || len < 2) return len == 1;
     int live = 0;
     for (int at = threadIdx.x & 63; live < 2; at += 256) {
 #pragma unroll
