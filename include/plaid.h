@@ -399,6 +399,83 @@ int plaid_cross_attention_backward(const plaid_attention *args, const void *d_ou
                                    void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
 int plaid_cross_attention_workspace(const plaid_attention *args, int32_t backward, int64_t *bytes);
 
+/* ---- Training a reader: what a training step does around its attention -- tokens in, states between the layers, states into a loss.
+ * The rules of the reader's calls hold: no index, arrays of `device`, asynchronous on `hip_stream`, nothing waited for or allocated, and a
+ * call may be captured in a graph.  dtype is a plaid_dtype, that of all states, parameters and their gradients; results are formed in
+ * 32 bits and rounded once.  Every sum has one order: the same inputs give the same bits.  Strides are in elements, from one row to
+ * the next; outputs are contiguous.  Outputs overlap no input, but where it says so. ---- */
+
+/* Rows of a table for n tokens: out[t] = scale * table[ids[t]]; zeros for an id outside [0, vocabulary).
+ *   table  [vocabulary][width], table_stride apart     ids  [n] int64     out  [n][width], 16-byte aligned
+ * width 1 .. 2^20, n and vocabulary up to 2^30. */
+int plaid_embedding(const void *table, int64_t table_stride, int64_t vocabulary, int32_t width, const int64_t *ids, int64_t n,
+                    float scale, void *out, int32_t dtype, int device, void *hip_stream);
+/* The table's gradient: d_table[v] = scale * the sum of d_out[t] over the tokens t of id v, zeros where there is none; with add != 0 the
+ * sum is added to what d_table holds, and rows without a token stay as they are (a table that is used twice, or that is the loss's
+ * vocabulary too).  A token of an id outside [0, vocabulary) is not read.
+ *   d_out  [n][width], d_out_stride apart     d_table  [vocabulary][width]
+ * workspace: plaid_embedding_backward_workspace bytes, 16-byte aligned. */
+int plaid_embedding_backward(const void *d_out, int64_t d_out_stride, int64_t vocabulary, int32_t width, const int64_t *ids, int64_t n,
+                             float scale, int32_t add, void *d_table, int32_t dtype, void *workspace, int64_t workspace_bytes,
+                             int device, void *hip_stream);
+int plaid_embedding_backward_workspace(int64_t n, int64_t vocabulary, int32_t width, int64_t *bytes);
+
+/* Dropout, with a residual added: out[e] = residual[e] + (kept ? x[e] / (1 - T / 65536) : 0), T = p * 65536 rounded to a whole number
+ * (halves up), for elements e = 0 .. n-1 in memory's order.  The mask is never stored: element e is kept where 16 bits of
+ * Philox4x32-10 are at least T -- key: rng[0], counter: e / 8 (low half first) and rng[1]; of its four words, element e takes word
+ * e / 2 % 4, the low half where e is even.  The gradient of x is the same call on d_out without a residual, that of the residual is d_out.
+ *   x, residual  [n] (residual may be NULL)     rng  [2] int64 on the device: a seed, and a number that each call of a program's has for
+ *   itself     out  [n]; may be x or residual
+ * p in [0, 1] (1: nothing is kept), n up to 2^40. */
+int plaid_dropout(const void *x, const void *residual, int64_t n, float p, const int64_t *rng, void *out, int32_t dtype, int device,
+                  void *hip_stream);
+
+/* Layer norm of rows: with m a row's mean and r = 1 / sqrt(its variance + eps), out = (x - m) r weight + bias.
+ *   x  [rows][width], x_stride apart     weight, bias  [width], each may be NULL     out  [rows][width]
+ *   statistics  [rows][2] fp32 (output, may be NULL) m and r, for the backward pass
+ * width 1 .. 16384, eps not negative. */
+int plaid_layer_norm(const void *x, int64_t x_stride, const void *weight, const void *bias, int64_t rows, int32_t width, float eps,
+                     void *out, float *statistics, int32_t dtype, int device, void *hip_stream);
+/* Its gradients: with x^ = (x - m) r and g = d_out weight, dx = r (g - mean g - x^ mean (g x^)), dweight = sum over rows of d_out x^,
+ * dbias = sum over rows of d_out.  dx, dweight and dbias may each be NULL; dweight takes a weight.
+ * workspace: plaid_layer_norm_backward_workspace bytes, 16-byte aligned (not looked at without dweight and dbias). */
+int plaid_layer_norm_backward(const void *d_out, int64_t d_out_stride, const void *x, int64_t x_stride, const void *weight,
+                              const float *statistics, int64_t rows, int32_t width, void *dx, void *dweight, void *dbias, int32_t dtype,
+                              void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
+int plaid_layer_norm_backward_workspace(int64_t rows, int32_t width, int64_t *bytes);
+
+/* Softmax cross entropy of states over a vocabulary, without the scores in memory: with s_tv = scale * hidden[t] . weight[v],
+ *   lse[t] = log sum_v exp(s_tv),   loss[t] = lse[t] - s_t,targets[t].
+ * A row whose target is outside [0, vocabulary) takes no part: its loss is 0, its gradient zero, and what it holds reaches nothing.
+ *   hidden   [rows][width], weight  [vocabulary][width]: 16-byte aligned, strides multiples of 8 in [0, 2^24)
+ *   targets  [rows] int64
+ *   loss     [rows] fp32     lse  [rows][2] fp32 or NULL: two numbers to be added, the largest score and the rest
+ * width a multiple of 8 up to 16384, rows up to 2^24, vocabulary up to 2^27. */
+typedef struct {
+    int32_t dtype;
+    int32_t width;
+    int64_t rows;
+    int64_t vocabulary;
+    float scale;
+    const void *hidden;
+    const void *weight;
+    int64_t hidden_stride;
+    int64_t weight_stride;
+    const int64_t *targets;
+    float *loss;
+    float *lse;
+} plaid_token_loss;
+
+/* workspace: plaid_cross_entropy_workspace bytes (backward = 0 or 1), 16-byte aligned. */
+int plaid_cross_entropy(const plaid_token_loss *args, void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
+/* Its gradients, the scores formed again over a piece of the vocabulary at a time: with G_tv = d_loss[t] (exp(s_tv - lse[t]) - [v = target]),
+ *   d_hidden[t] = scale sum_v G_tv weight[v],   d_weight[v] = scale sum_t G_tv hidden[t]   (contiguous, either may be NULL).
+ * args->lse is what the forward call gave, args->loss is not looked at.  d_loss [rows] fp32, d_loss_stride 1, or 0: one number for all rows.
+ * G rounds to the type before it is multiplied; the power of two of d_loss is kept apart, so that it costs fp16 no digits. */
+int plaid_cross_entropy_backward(const plaid_token_loss *args, const float *d_loss, int64_t d_loss_stride, void *d_hidden, void *d_weight,
+                                 void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
+int plaid_cross_entropy_workspace(const plaid_token_loss *args, int32_t backward, int64_t *bytes);
+
 /* Thread-local message describing the most recent error on the calling thread ("" if none). */
 const char *plaid_last_error(void);
 

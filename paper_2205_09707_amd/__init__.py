@@ -39,3 +39,12 @@ from .reader import (  # noqa: F401
     plaid_cross_attention,
     plaid_cross_attention_backward,
 )
+from .training import (  # noqa: F401
+    plaid_cross_entropy,
+    plaid_cross_entropy_backward,
+    plaid_dropout,
+    plaid_embedding,
+    plaid_embedding_backward,
+    plaid_layer_norm,
+    plaid_layer_norm_backward,
+)

@@ -1,0 +1,282 @@
+// Cross entropy over a vocabulary: the products.
+#include "train.h"
+
+// Three products, each of tiles of 256 x 256 over an axis k taken 64 at a time:
+//   scores   s[t][v]  = sum over the width of h[t] W[v];      the tile ends as statistics of its rows, or as G, rounded to the type
+//   d_hidden dh[t][j] = sum over the vocabulary of G[t][v] W[v][j]
+//   d_weight dW[v][j] = sum over rows of G[t][v] h[t][j]
+// An operand lies in memory with k along its rows, or across them; the latter goes into LDS as it is and is read transposed.  Eight waves
+// have 128 x 64 of a tile each.  The axis that is to lie together in memory is the one of the result's registers (M): four neighbours a lane.
+#define BK LOSS_STEP
+#define TILE_BYTES (LOSS_TILE * BK * 2)
+
+// How a wave brings its eighth of an operand's tile into LDS, four loads of 1 KB.  Along: [256 rows][64], a load has 8 rows.  Across: two
+// halves [64 k][128], a load has 4 rows of k.  The chunks of 16 bytes of a row change places as lds_chunk says; a load's lanes write
+// LDS one after another, so it is the lanes' addresses that do.
+template <bool ACROSS>
+struct Operand {
+    const char *at[4];
+    int k[4];  // across: the load's row of k
+    __device__ __forceinline__ void set(const char *base, int64_t stride, int64_t rows, int64_t first, int64_t columns)
+    {
+        const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int load = wave * 4 + i;
+            if constexpr (!ACROSS) {
+                const int row = load * 8 + (lane >> 3), chunk = (lane & 7) ^ swizzle<64>(row);
+                k[i] = chunk * 8;
+                at[i] = base + min(first + row, rows - 1) * stride + chunk * 16;
+            } else {
+                const int half = load >> 4, row = (load & 15) * 4 + (lane >> 4), chunk = (lane & 15) ^ swizzle<128>(row);
+                const int64_t column = first + half * 128 + chunk * 8;
+                k[i] = row;
+                at[i] = base + row * stride + (column < columns ? column : 0) * 2;  // what lies past the end is not kept
+            }
+        }
+    }
+    __device__ __forceinline__ void load(char *tile) const
+    {
+        const int wave = uniform((int)(threadIdx.x >> 6));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_to_lds(at[i], tile + (wave * 4 + i) * 1024);
+    }
+    // The last step of an axis that ends inside it: `left` of the 64 are there.  Along: zeros for the others.  Across: the last one again
+    // (the other operand has zeros there).
+    __device__ __forceinline__ void load_end(char *tile, int left, int64_t stride) const
+    {
+        const int wave = uniform((int)(threadIdx.x >> 6));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const char *p = at[i];
+            if constexpr (!ACROSS) p = k[i] < left ? p : (const char *)zero_row;
+            else p = k[i] < left ? p : p - (k[i] - (left - 1)) * stride;
+            load_to_lds(p, tile + (wave * 4 + i) * 1024);
+        }
+    }
+    __device__ __forceinline__ void step(int64_t bytes)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] += bytes;
+    }
+};
+// The operand of 32 rows (columns, across) from `base` on at k = 16 s + 8 (l / 32) .. + 7.
+template <bool ACROSS>
+__device__ __forceinline__ i32x4 operand(const char *tile, int base, int s)
+{
+    if constexpr (!ACROSS) return lds_rows<64>(tile, base, s);
+    else {
+        const int lane = threadIdx.x & 63, row = 16 * s + 8 * (lane >> 5) + ((lane >> 2) & 3), x = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+        const char *half = tile + (base >> 7) * (TILE_BYTES / 2);
+        const int dt = (base >> 5) & 3;
+        const char *p = half + row * 256 + (((4 * dt + x) ^ swizzle<128>(row)) << 4) + (lane & 1) * 8;
+        const char *r = half + (row + 4) * 256 + (((4 * dt + x) ^ swizzle<128>(row + 4)) << 4) + (lane & 1) * 8;
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const i32x2 u = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
+        const i32x2 w = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)r));
+        return i32x4{u[0], u[1], w[0], w[1]};
+    }
+}
+
+struct Tile {
+    int m, n;
+};
+// Tile of workgroup `id`: workgroups go to the eight XCDs in turn, and each XCD gets a stretch of panels of four tiles of n, so that what its
+// workgroups read together is in its cache.
+__device__ __forceinline__ bool find_tile(int id, int ms, int ns, Tile &t)
+{
+    const int all = ms * ns, each = (all + 7) / 8, o = (id & 7) * each + (id >> 3);
+    if ((id >> 3) >= each || o >= all) return false;
+    const int panels = ns / 4, whole = panels * 4 * ms;
+    if (o < whole) t.n = o / (4 * ms) * 4 + o % 4, t.m = o % (4 * ms) / 4;
+    else t.n = panels * 4 + (o - whole) % (ns % 4), t.m = (o - whole) / (ns % 4);
+    return true;
+}
+
+#define KIND_STATISTICS 0
+#define KIND_GRADIENT 1
+#define KIND_D_HIDDEN 2
+#define KIND_D_WEIGHT 3
+
+template <int DT, int KIND>
+__global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
+{
+    constexpr bool SCORES = KIND <= KIND_GRADIENT, A_ACROSS = !SCORES, B_ACROSS = KIND == KIND_D_WEIGHT;
+    __shared__ __align__(16) char lds[2][2][TILE_BYTES];
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wm = wave >> 2, wn = wave & 3;
+    const int live = uniform_load(a.state), row_tiles = (live + LOSS_TILE - 1) / LOSS_TILE;
+    const int pieces = (a.piece + LOSS_TILE - 1) / LOSS_TILE, widths = a.columns / LOSS_TILE;
+    Tile t;
+    const int split = KIND == KIND_D_HIDDEN ? blockIdx.y : 0;
+    if (!find_tile(blockIdx.x, SCORES ? pieces : widths, KIND == KIND_D_WEIGHT ? pieces : row_tiles, t)) return;
+
+    const int64_t gradient_stride = (int64_t)pieces * LOSS_TILE * 2;
+    Operand<A_ACROSS> A;
+    Operand<B_ACROSS> B;
+    int64_t a_step = 2 * BK, b_step = 2 * BK;
+    int begin = 0, steps, end_left = BK;  // steps of k, what there is of the last
+    if constexpr (SCORES) {
+        steps = a.pitch / BK, end_left = a.width - (steps - 1) * BK;
+        A.set(a.weight, a.weight_stride, a.vocabulary, a.first + t.m * LOSS_TILE, 0);
+        B.set(a.packed, (int64_t)a.pitch * 2, a.padded_rows, t.n * LOSS_TILE, 0);
+    } else if constexpr (KIND == KIND_D_HIDDEN) {
+        const int all = (a.piece + BK - 1) / BK, share = (all + a.splits - 1) / a.splits;
+        begin = min(all, split * share), steps = min(all, begin + share) - begin;
+        if (begin + steps == all) end_left = a.piece - (all - 1) * BK;
+        a_step = BK * a.weight_stride;
+        A.set(a.weight + (a.first + (int64_t)begin * BK) * a.weight_stride, a.weight_stride, 0, t.m * LOSS_TILE, a.width);
+        B.set(a.gradient + begin * BK * 2, gradient_stride, a.padded_rows, t.n * LOSS_TILE, 0);
+    } else {
+        steps = (live + BK - 1) / BK;
+        a_step = (int64_t)BK * a.pitch * 2, b_step = BK * gradient_stride;
+        A.set(a.scaled, (int64_t)a.pitch * 2, 0, t.m * LOSS_TILE, a.pitch);
+        B.set(a.gradient, gradient_stride, 0, t.n * LOSS_TILE, (int64_t)pieces * LOSS_TILE);
+    }
+
+    f32x16 acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = zero16();
+
+    const auto bring = [&](int s) {
+        char *x = lds[s & 1][0], *y = lds[s & 1][1];
+        if (KIND != KIND_D_WEIGHT && s == steps - 1 && end_left < BK) A.load_end(x, end_left, a.weight_stride);
+        else A.load(x);
+        B.load(y);
+        A.step(a_step), B.step(b_step);
+    };
+    if (steps > 0) bring(0);
+    for (int s = 0; s < steps; ++s) {
+        wait_loads<0>();
+        lds_barrier();
+        if (s + 1 < steps) bring(s + 1);
+        const char *x = lds[s & 1][0], *y = lds[s & 1][1];
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k) {
+            i32x4 p[4], q[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = operand<A_ACROSS>(x, wm * 128 + 32 * i, k);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) q[j] = operand<B_ACROSS>(y, wn * 64 + 32 * j, k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = mfma32<DT>(p[i], q[j], acc[i][j]);
+        }
+    }
+
+    // a lane's results: column n = 64 wn + 32 j + lane % 32, rows m = 128 wm + 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4
+    const int m0 = t.m * LOSS_TILE + wm * 128 + 4 * (lane >> 5), n0 = t.n * LOSS_TILE + wn * 64 + (lane & 31);
+    if constexpr (KIND == KIND_STATISTICS) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int row = n0 + 32 * j;
+            const bool there = row < live;
+            const int target = there ? a.row[row].target - (int)a.first - m0 : -1;  // place in the piece, from the lane's first
+            float most = -INFINITY, own = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int m = 32 * i + 8 * (r / 4) + r % 4;
+                    const float s = acc[i][j][r] * a.scale;
+                    own = m == target ? s : own;
+                    acc[i][j][r] = m0 + m < a.piece ? s : -INFINITY;
+                    most = fmaxf(most, acc[i][j][r]);
+                }
+            if (target >= 0 && target < 128 && !(target & 4) && m0 + target < a.piece) a.own[row] = own;
+            most = max_halves(most);
+            const float base = most == -INFINITY ? 0.0f : most;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E);
+            sum = sum_halves(sum);
+            if (lane < 32) a.part[(int64_t)(t.m * 2 + wm) * a.padded_rows + row] = {most, sum};
+        }
+    } else if constexpr (KIND == KIND_GRADIENT) {
+        constexpr float GAIN = DT == PLAID_FP16 ? 0x1p15f : 1.0f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int row = n0 + 32 * j;
+            const bool there = row < live;
+            const LossRow x = there ? a.row[row] : LossRow{-1, 0, 0.0f, 0.0f, 0.0f};
+            const int target = there ? x.target - (int)a.first - m0 : -1;
+            const float rest = x.log_total * LOG2E, factor = x.fraction * GAIN;
+            float own = 0.0f;  // of the target: the probability less one, which keeps its digits where the probability is almost one
+            if (__any(target >= 0 && target < 128)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) own = 32 * i + 8 * (r / 4) + r % 4 == target ? acc[i][j][r] : own;
+                own = expm1f(own * a.scale - x.top - x.log_total);
+            }
+            char *out = a.gradient + row * gradient_stride + m0 * 2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float g[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int m = 32 * i + 8 * c + r;
+                        const float d = acc[i][j][4 * c + r] * a.scale - x.top;
+                        const float p = m == target ? own : __builtin_amdgcn_exp2f(d * LOG2E - rest);
+                        g[r] = there && m0 + m < a.piece ? p * factor : 0.0f;
+                    }
+                    *(i32x2 *)(out + (32 * i + 8 * c) * 2) = i32x2{pack2<DT>(g[0], g[1]), pack2<DT>(g[2], g[3])};
+                }
+        }
+    } else if constexpr (KIND == KIND_D_HIDDEN) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float *out = a.d_part + ((int64_t)split * a.padded_rows + n0 + 32 * j) * a.columns + m0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    f32x4 *p = (f32x4 *)(out + 32 * i + 8 * c);
+                    f32x4 v = {acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+                    if (a.first > 0) v += *p;
+                    *p = v;
+                }
+        }
+    } else {
+        const float factor = a.scale * (DT == PLAID_FP16 ? 0x1p-15f : 1.0f);
+        const int exponent = uniform_load(a.state + 1);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int v = n0 + 32 * j;
+            if (v >= a.piece) continue;
+            char *out = a.d_weight + ((a.first + v) * (int64_t)a.width + m0) * 2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (m0 + 32 * i + 8 * c >= a.width) continue;  // the width is a multiple of 8
+                    float g[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) g[r] = ldexpf(acc[i][j][4 * c + r] * factor, exponent);
+                    *(i32x2 *)(out + (32 * i + 8 * c) * 2) = i32x2{pack2<DT>(g[0], g[1]), pack2<DT>(g[2], g[3])};
+                }
+        }
+    }
+}
+
+template <int KIND>
+static void launch(hipStream_t st, const LossArgs &a, int dtype)
+{
+    const int64_t pieces = (a.piece + LOSS_TILE - 1) / LOSS_TILE, widths = a.columns / LOSS_TILE, rows = a.padded_rows / LOSS_TILE;
+    const int64_t tiles = KIND <= KIND_GRADIENT ? pieces * rows : KIND == KIND_D_HIDDEN ? widths * rows : widths * pieces;
+    const dim3 grid((unsigned)((tiles + 7) / 8 * 8), KIND == KIND_D_HIDDEN ? a.splits : 1);
+    if (dtype == PLAID_BF16) loss_mm_kernel<PLAID_BF16, KIND><<<grid, 512, 0, st>>>(a);
+    else loss_mm_kernel<PLAID_FP16, KIND><<<grid, 512, 0, st>>>(a);
+}
+void plaid_launch_loss_scores(hipStream_t st, const LossArgs &a, int dtype, bool backward)
+{
+    backward ? launch<KIND_GRADIENT>(st, a, dtype) : launch<KIND_STATISTICS>(st, a, dtype);
+}
+void plaid_launch_loss_d_weight(hipStream_t st, const LossArgs &a, int dtype) { launch<KIND_D_WEIGHT>(st, a, dtype); }
+void plaid_launch_loss_d_hidden(hipStream_t st, const LossArgs &a, int dtype) { launch<KIND_D_HIDDEN>(st, a, dtype); }

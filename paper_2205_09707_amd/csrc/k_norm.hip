@@ -1,0 +1,204 @@
+// Layer norm and its gradients.
+#include "train.h"
+
+// With m the mean of a row, r = 1 / sqrt(variance + eps) and x^ = (x - m) r:  y = x^ w + b, and with g = dy w
+//   dx = r (g - mean(g) - x^ mean(g x^)),   dw = sum over rows of dy x^,   db = sum over rows of dy.
+// A row's threads keep it in registers, so that the variance is that of x - m (no difference of large numbers) and the row is read once.
+// LANES threads have a row, each up to C pieces of eight neighbouring elements, LANES * 8 elements apart.
+
+// Sums of a row's threads; all of them get both.
+template <int LANES>
+__device__ __forceinline__ float2 row_sum(float2 s, float2 *lds)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) s.x += __shfl_xor(s.x, o), s.y += __shfl_xor(s.y, o);
+    if constexpr (LANES > 64) {
+        __syncthreads();  // the sums before have been read
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+        __syncthreads();
+        s = {0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < LANES / 64; ++w) s.x += lds[w].x, s.y += lds[w].y;
+    }
+    return s;
+}
+
+template <int DT, int LANES, int C>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArgs a)
+{
+    constexpr int THREADS = LANES < 256 ? 256 : LANES;
+    __shared__ float2 lds[THREADS / 64];
+    const int lane = threadIdx.x % LANES;
+    const int64_t row = (int64_t)blockIdx.x * (THREADS / LANES) + threadIdx.x / LANES;
+    if (row >= a.rows) return;  // whole waves, or the whole workgroup
+    const char *x = a.x + row * a.x_stride;
+    Eight v[C];
+    float sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * LANES + lane) * 8;
+        v[c] = unpack8<DT>(load_piece(x, at, a.width));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[c].x[i];
+    }
+    const float mean = row_sum<LANES>({sum, 0.0f}, lds).x / (float)a.width;
+    float square = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[c].x[i] -= mean;
+            if ((c * LANES + lane) * 8 + i < a.width) square += v[c].x[i] * v[c].x[i];
+        }
+    const float inverse = 1.0f / sqrtf(row_sum<LANES>({square, 0.0f}, lds).x / (float)a.width + a.eps);
+    if (a.statistics && lane == 0) *(float2 *)(a.statistics + 2 * row) = {mean, inverse};
+    char *out = a.out + row * a.width * 2;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * LANES + lane) * 8;
+        if (at >= a.width) break;
+        const Eight w = unpack8<DT>(a.weight ? load_piece(a.weight, at, a.width) : i32x4{}), b = unpack8<DT>(a.bias ? load_piece(a.bias, at, a.width) : i32x4{});
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c].x[i] = v[c].x[i] * inverse * (a.weight ? w.x[i] : 1.0f) + b.x[i];
+        store_piece(out, at, a.width, pack8<DT>(v[c]));
+    }
+}
+
+// Workers go over the rows in turn and keep the sums of dw and db of their columns in registers; the last launch adds up the workers', in order.
+template <int DT, int LANES, int C>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_grad_kernel(NormArgs a)
+{
+    constexpr int THREADS = LANES < 256 ? 256 : LANES, TEAMS = THREADS / LANES;
+    __shared__ float2 lds[THREADS / 64];
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+    i32x4 w[C];
+    Eight dw[C] = {}, db[C] = {};
+#pragma unroll
+    for (int c = 0; c < C; ++c) w[c] = a.weight ? load_piece(a.weight, (c * LANES + lane) * 8, a.width) : i32x4{};
+    const float per = 1.0f / (float)a.width;
+    for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < a.rows; row += (int64_t)gridDim.x * TEAMS) {
+        const char *x = a.x + row * a.x_stride, *d = a.d_out + row * a.d_out_stride;
+        i32x4 xr[C], dr[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            xr[c] = load_piece(x, (c * LANES + lane) * 8, a.width);
+            dr[c] = load_piece(d, (c * LANES + lane) * 8, a.width);
+        }
+        const float2 st = {uniform_load(a.statistics + 2 * row), uniform_load(a.statistics + 2 * row + 1)};
+        float2 sum = {0.0f, 0.0f};
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const Eight xv = unpack8<DT>(xr[c]), dv = unpack8<DT>(dr[c]), wv = unpack8<DT>(w[c]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float n = (xv.x[i] - st.x) * st.y, g = a.weight ? dv.x[i] * wv.x[i] : dv.x[i];
+                sum.x += g, sum.y += g * n;  // past the end d_out is zero
+                dw[c].x[i] += dv.x[i] * n, db[c].x[i] += dv.x[i];
+            }
+        }
+        sum = row_sum<LANES>(sum, lds);
+        const float m0 = sum.x * per, m1 = sum.y * per;
+        if (a.dx) {
+            char *dx = a.dx + row * a.width * 2;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int at = (c * LANES + lane) * 8;
+                if (at >= a.width) break;
+                const Eight xv = unpack8<DT>(xr[c]), dv = unpack8<DT>(dr[c]), wv = unpack8<DT>(w[c]);
+                Eight r;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float n = (xv.x[i] - st.x) * st.y, g = a.weight ? dv.x[i] * wv.x[i] : dv.x[i];
+                    r.x[i] = st.y * (g - m0 - n * m1);
+                }
+                store_piece(dx, at, a.width, pack8<DT>(r));
+            }
+        }
+    }
+    if (!a.part) return;
+    // the teams of a workgroup, in order
+    constexpr int COLUMNS = LANES * 8;
+    __shared__ float both[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? COLUMNS : 1];
+    float *part = a.part + (int64_t)blockIdx.x * 2 * a.width;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const Eight &s = k ? db[c] : dw[c];
+            if constexpr (TEAMS > 1) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) both[team][i * LANES + lane] = s.x[i];
+                __syncthreads();
+                for (int at = threadIdx.x; at < COLUMNS; at += THREADS) {
+                    const int column = c * COLUMNS + at % LANES * 8 + at / LANES;
+                    float t = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < TEAMS; ++j) t += both[j][at];
+                    if (column < a.width) part[k * a.width + column] = t;
+                }
+            } else {
+                const int at = (c * LANES + lane) * 8;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (at + i < a.width) part[k * a.width + at + i] = s.x[i];
+            }
+        }
+}
+
+// A workgroup has 64 columns of dw or of db; its sixteen waves take the workers in turn.
+template <int DT>
+__global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a)
+{
+    __shared__ float lds[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, column = blockIdx.x * 64 + lane, k = blockIdx.y;
+    char *out = k ? a.dbias : a.dweight;
+    if (!out) return;
+    float sum = 0.0f;
+    if (column < a.width) {
+        const float *p = a.part + k * a.width + column;
+#pragma unroll 8
+        for (int i = wave; i < a.workers; i += 16) sum += p[(int64_t)i * 2 * a.width];
+    }
+    lds[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && column < a.width) {
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += lds[i][lane];
+        store16<DT>(out + 2 * column, sum);
+    }
+}
+
+template <int DT>
+static void launch_norm(hipStream_t st, const NormArgs &a)
+{
+    const int pieces = (a.width + 7) / 8;
+#define GO(LANES, C) norm_kernel<DT, LANES, C><<<(unsigned)((a.rows * LANES + 255) / (LANES < 256 ? 256 : LANES)), LANES < 256 ? 256 : LANES, 0, st>>>(a)
+    if (pieces <= 64) GO(64, 1);
+    else if (pieces <= 128) GO(64, 2);
+    else if (pieces <= 256) GO(256, 1);
+    else if (pieces <= 512) GO(256, 2);
+    else if (pieces <= 1024) GO(256, 4);
+    else GO(1024, 2);
+#undef GO
+}
+template <int DT>
+static void launch_norm_backward(hipStream_t st, const NormArgs &a)
+{
+    const int pieces = (a.width + 7) / 8;
+#define GO(LANES, C) norm_grad_kernel<DT, LANES, C><<<a.workers, LANES < 256 ? 256 : LANES, 0, st>>>(a)
+    if (pieces <= 64) GO(64, 1);
+    else if (pieces <= 128) GO(64, 2);
+    else if (pieces <= 256) GO(256, 1);
+    else if (pieces <= 512) GO(256, 2);
+    else if (pieces <= 1024) GO(256, 4);
+    else GO(1024, 2);
+#undef GO
+    if (a.part) norm_join_kernel<DT><<<dim3((a.width + 63) / 64, 2), 1024, 0, st>>>(a);
+}
+void plaid_launch_layer_norm(hipStream_t st, const NormArgs &a, int dtype) { dtype == PLAID_BF16 ? launch_norm<PLAID_BF16>(st, a) : launch_norm<PLAID_FP16>(st, a); }
+void plaid_launch_layer_norm_backward(hipStream_t st, const NormArgs &a, int dtype)
+{
+    dtype == PLAID_BF16 ? launch_norm_backward<PLAID_BF16>(st, a) : launch_norm_backward<PLAID_FP16>(st, a);
+}

@@ -1,34 +1,11 @@
 // C entry points of the reader (include/plaid.h): argument checks, the choice of kernel and of how the work is cut, workspaces.
 #include <cmath>
 
+#include "api_common.h"
 #include "reader.h"
-
-#define FAIL(...) return plaid_fail(PLAID_EINVAL, __VA_ARGS__)
 
 namespace {
 
-struct OnDevice {  // the calling thread's device for the length of a call
-    int before = -1;
-    bool ok = false, moved = false;
-    explicit OnDevice(int device)
-    {
-        ok = hipGetDevice(&before) == hipSuccess;
-        if (ok && before != device) ok = moved = hipSetDevice(device) == hipSuccess;
-    }
-    ~OnDevice()
-    {
-        if (moved) (void)hipSetDevice(before);
-    }
-};
-
-int launched()
-{
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? PLAID_OK : plaid_fail(PLAID_EHIP, "kernel launch: %s", hipGetErrorString(e));
-}
-bool misaligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
-constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr int64_t round16(int64_t x) { return (x + 15) & ~(int64_t)15; }
 bool block_size_ok(int32_t b) { return b == 16 || b == 32 || b == 64 || b == 128 || b == 256; }
 
 int check_cache(const plaid_paged_cache *c)
@@ -167,13 +144,6 @@ int check_keys(const plaid_attention *a)
     if (misaligned(a->key_bias, 2)) FAIL("key_bias is misaligned");
     return PLAID_OK;
 }
-int check_workspace(const void *p, int64_t have, int64_t need)
-{
-    if (need > 0 && (!p || misaligned(p, 16) || have < need))
-        FAIL("workspace: %lld bytes, 16-byte aligned, are needed, %lld given", (long long)need, (long long)have);
-    return PLAID_OK;
-}
-
 AttendArgs attend_args(const plaid_attention &a)
 {
     AttendArgs x = {};

@@ -1,0 +1,125 @@
+// Declarations shared by the kernels of a reader's training step around its attention: embedding, dropout, layer norm, cross entropy
+// over a vocabulary (gfx950 only).
+#pragma once
+#include "reader.h"
+
+struct EmbedArgs {
+    const char *table, *d_out;
+    char *out, *d_table;
+    const int64_t *ids;
+    int64_t n, vocabulary, table_stride, d_out_stride;  // strides in bytes
+    int32_t width, add;
+    float scale;
+    // gradient's workspace
+    int32_t *keys[2], *places[2];      // tokens in ascending order, and where each stood; two of each where several launches sort
+    int32_t *counts, *totals;          // [bins][blocks] of a pass, [bins]
+    int32_t sorted;                    // which of the two holds the result
+    int32_t bits, passes, digit;       // bits of a key, passes, bits a pass
+    int32_t chunk;                     // sorted places that a team of threads adds up
+    float *part;                       // [chunks][2][columns()] sums of tokens that several chunks share
+    __host__ __device__ int columns() const { return (width + 7) & ~7; }
+};
+// Up to this many tokens are sorted by one workgroup in one launch.
+#define SORT_ONE 4096
+#define SORT_TILE 2048
+void plaid_launch_embedding(hipStream_t st, const EmbedArgs &e, int dtype);
+void plaid_launch_embedding_backward(hipStream_t st, const EmbedArgs &e, int dtype);
+
+void plaid_launch_dropout(hipStream_t st, const char *x, const char *residual, int64_t n, uint32_t threshold, const int64_t *rng, char *out, int dtype);
+
+struct NormArgs {
+    const char *x, *weight, *bias, *d_out;
+    char *out, *dx, *dweight, *dbias;
+    float *statistics;                 // [rows][2] mean, 1 / sqrt(variance + eps)
+    int64_t rows, x_stride, d_out_stride;  // strides in bytes
+    int32_t width, workers;
+    float eps;
+    float *part;                       // [workers][2][width] sums of dweight and dbias
+};
+#define NORM_WIDEST 16384
+void plaid_launch_layer_norm(hipStream_t st, const NormArgs &a, int dtype);
+void plaid_launch_layer_norm_backward(hipStream_t st, const NormArgs &a, int dtype);
+
+// Cross entropy.  Rows that have a target are packed first; what follows sees only those.
+struct LossRow {
+    int32_t target, exponent;          // d_loss = fraction 2^exponent
+    float fraction, top, log_total;    // lse = top + log_total
+};
+struct LossArgs {
+    const char *hidden, *weight;
+    const int64_t *targets;
+    const float *d_loss;
+    float *loss, *lse;
+    char *d_hidden, *d_weight;
+    int64_t rows, vocabulary, hidden_stride, weight_stride, d_loss_stride;  // strides in bytes
+    int32_t width;
+    float scale;
+    // workspace
+    int32_t padded_rows, pitch;        // rows rounded up to LOSS_TILE, width to LOSS_STEP
+    int32_t *state;                    // [0] rows that have a target, [1] the largest exponent among them
+    int32_t *list;                     // [rows] which these are
+    LossRow *row;                      // [padded_rows]
+    char *packed, *scaled;             // [padded_rows][pitch] states, and those times 2^(exponent - largest)
+    float2 *part;                      // [parts][padded_rows] maximum and sum of exponentials over parts of the vocabulary
+    float2 *running;                   // [padded_rows] over all parts before
+    float *own;                        // [padded_rows] score of the target
+    char *gradient;                    // [padded_rows][piece] of the scores, over a piece of the vocabulary
+    float *d_part;                     // [splits][padded_rows][columns] sums of d_hidden
+    int32_t columns;                   // width rounded up to LOSS_TILE
+    int32_t splits;
+    int64_t first;                     // the piece's first entry, and how many there are
+    int32_t piece, last;               // last: no piece comes after this one
+};
+#define LOSS_TILE 256
+#define LOSS_STEP 64
+#define LOSS_PART 128
+#define LOSS_FEW 64
+void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool backward);
+void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int blocks);
+void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool packed);
+void plaid_launch_loss_scores(hipStream_t st, const LossArgs &a, int dtype, bool backward);
+void plaid_launch_loss_d_weight(hipStream_t st, const LossArgs &a, int dtype);
+void plaid_launch_loss_d_hidden(hipStream_t st, const LossArgs &a, int dtype);
+void plaid_launch_loss_d_hidden_join(hipStream_t st, const LossArgs &a, int dtype);
+
+#ifdef __HIP__
+// Sixteen bytes of a row that starts at any element: the memory system takes such addresses.
+typedef i32x4 __attribute__((aligned(2))) i32x4_any;
+
+struct Eight {
+    float x[8];
+};
+template <int DT>
+__device__ __forceinline__ Eight unpack8(i32x4 w)
+{
+    Eight r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.x[2 * i] = unpack<DT>(w[i], 0), r.x[2 * i + 1] = unpack<DT>(w[i], 1);
+    return r;
+}
+template <int DT>
+__device__ __forceinline__ i32x4 pack8(const Eight &r)
+{
+    return i32x4{pack2<DT>(r.x[0], r.x[1]), pack2<DT>(r.x[2], r.x[3]), pack2<DT>(r.x[4], r.x[5]), pack2<DT>(r.x[6], r.x[7])};
+}
+// Elements at .. at + 7 of a row of `width`; those past its end are zero, and not read.
+__device__ __forceinline__ i32x4 load_piece(const char *row, int at, int width)
+{
+    if (at + 8 <= width) return *(const i32x4_any *)(row + 2 * at);
+    i32x4 w = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (at + i < width) w[i / 2] |= (int)((uint32_t) * (const uint16_t *)(row + 2 * (at + i)) << (16 * (i & 1)));
+    return w;
+}
+__device__ __forceinline__ void store_piece(char *row, int at, int width, i32x4 w)
+{
+    if (at + 8 <= width) {
+        *(i32x4_any *)(row + 2 * at) = w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (at + i < width) *(uint16_t *)(row + 2 * (at + i)) = (uint16_t)((uint32_t)w[i / 2] >> (16 * (i & 1)));
+}
+#endif

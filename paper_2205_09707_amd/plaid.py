@@ -54,7 +54,9 @@ EXPORTS = ("plaid_index_load", "plaid_index_from_view", "plaid_index_free", "pla
            "plaid_encode_residuals", "plaid_build_ivf", "plaid_workspace_bytes", "plaid_index_set_renormalize",
            "plaid_block_tables", "plaid_block_tables_workspace", "plaid_cache_write", "plaid_cache_read", "plaid_cached_attention",
            "plaid_cached_attention_workspace", "plaid_cross_attention", "plaid_cross_attention_backward",
-           "plaid_cross_attention_workspace", "plaid_last_error")
+           "plaid_cross_attention_workspace", "plaid_embedding", "plaid_embedding_backward", "plaid_embedding_backward_workspace",
+           "plaid_dropout", "plaid_layer_norm", "plaid_layer_norm_backward", "plaid_layer_norm_backward_workspace", "plaid_cross_entropy",
+           "plaid_cross_entropy_backward", "plaid_cross_entropy_workspace", "plaid_last_error")
 
 _lib = None
 
@@ -96,8 +98,9 @@ def load_library() -> ct.CDLL:
                                                ct.c_int32, ct.c_void_p, ct.c_int, ct.c_void_p]
         lib.plaid_build_ivf.argtypes = [ct.c_void_p, ct.c_void_p, ct.c_int64, ct.c_int64, ct.c_int64, ct.c_void_p, ct.c_void_p,
                                         ct.c_int64, ct.POINTER(ct.c_int64), ct.c_int, ct.c_void_p]
-        from . import reader
+        from . import reader, training
         reader.declare(lib)
+        training.declare(lib)
         _lib = lib
     return _lib
 

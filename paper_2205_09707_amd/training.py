@@ -1,0 +1,237 @@
+"""Binding of what a reader's training step does around its attention (include/plaid.h): embedding, dropout, layer norm, cross entropy
+over a vocabulary, with their gradients.
+
+Like `reader.py` this only marshals, and keeps nothing from one call for the next.  Autograd records none of the calls: each gradient
+is a call of its own, and inputs that require a gradient are refused where it is enabled (examples/reader.py has the Functions).
+"""
+from __future__ import annotations
+
+import ctypes as ct
+from typing import Optional, Tuple
+
+import torch
+
+from . import plaid as _p
+from .reader import _DTYPES, _is, _vector, _where, _workspace
+
+
+class plaid_token_loss(ct.Structure):
+    _fields_ = [("dtype", ct.c_int32), ("width", ct.c_int32), ("rows", ct.c_int64), ("vocabulary", ct.c_int64), ("scale", ct.c_float),
+                ("hidden", ct.c_void_p), ("weight", ct.c_void_p), ("hidden_stride", ct.c_int64), ("weight_stride", ct.c_int64),
+                ("targets", ct.c_void_p), ("loss", ct.c_void_p), ("lse", ct.c_void_p)]
+
+
+def declare(lib: ct.CDLL) -> None:
+    """Argument types of these functions."""
+    P, i32, i64, f32, out64 = ct.c_void_p, ct.c_int32, ct.c_int64, ct.c_float, ct.POINTER(ct.c_int64)
+    loss = ct.POINTER(plaid_token_loss)
+    lib.plaid_embedding.argtypes = [P, i64, i64, i32, P, i64, f32, P, i32, ct.c_int, P]
+    lib.plaid_embedding_backward.argtypes = [P, i64, i64, i32, P, i64, f32, i32, P, i32, P, i64, ct.c_int, P]
+    lib.plaid_embedding_backward_workspace.argtypes = [i64, i64, i32, out64]
+    lib.plaid_dropout.argtypes = [P, P, i64, f32, P, P, i32, ct.c_int, P]
+    lib.plaid_layer_norm.argtypes = [P, i64, P, P, i64, i32, f32, P, P, i32, ct.c_int, P]
+    lib.plaid_layer_norm_backward.argtypes = [P, i64, P, i64, P, P, i64, i32, P, P, P, i32, P, i64, ct.c_int, P]
+    lib.plaid_layer_norm_backward_workspace.argtypes = [i64, i32, out64]
+    lib.plaid_cross_entropy.argtypes = [loss, P, i64, ct.c_int, P]
+    lib.plaid_cross_entropy_backward.argtypes = [loss, P, i64, P, P, P, i64, ct.c_int, P]
+    lib.plaid_cross_entropy_workspace.argtypes = [loss, i32, out64]
+
+
+def _states(t: torch.Tensor, name: str, dim: Optional[int] = 2) -> torch.device:
+    """Checks a tensor of states; its device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _DTYPES or (dim is not None and t.dim() != dim):
+        raise ValueError(f"{name} must be a CUDA tensor of dtype torch.bfloat16 or torch.float16" + ("" if dim is None else f" with {dim} dimensions"))
+    return t.device
+
+
+def _no_autograd(backward: str, **tensors) -> None:
+    if torch.is_grad_enabled():
+        for name, t in tensors.items():
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{name} requires a gradient, which this call does not record: call it in torch.no_grad(), or in a "
+                                 f"torch.autograd.Function whose backward calls {backward}")
+
+
+def _rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
+    """A matrix whose rows are contiguous, and from one row to the next."""
+    n, width = t.shape
+    if (width > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < 0):
+        t = t.contiguous()
+    return t, t.stride(0) if n > 1 else width
+
+
+def _aligned_rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
+    """The same where the kernels want rows of whole 16-byte pieces."""
+    n, width = t.shape
+    stride = t.stride(0) if n > 1 else width
+    if (width > 1 and t.stride(1) != 1) or stride % 8 or not 0 <= stride < 1 << 24 or t.data_ptr() % 16:
+        if t.numel():
+            t = t.clone(memory_format=torch.contiguous_format)
+        stride = width
+    return t, stride
+
+
+def plaid_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
+    """scale * table[ids] for a table [vocabulary, width] and ids [n] int64; zeros for an id outside the vocabulary."""
+    dev = _states(table, "table")
+    _no_autograd("plaid_embedding_backward", table=table)
+    ids = _vector(ids, "ids", torch.int64, dev)
+    table, stride = _rows(table)
+    out = torch.empty((ids.shape[0], table.shape[1]), dtype=table.dtype, device=dev)
+    _p._check(_p.load_library().plaid_embedding(table.data_ptr(), stride, table.shape[0], table.shape[1], ids.data_ptr(), ids.shape[0], float(scale),
+                                                out.data_ptr(), _DTYPES[table.dtype], *_where(dev)))
+    return out
+
+
+def plaid_embedding_backward(d_out: torch.Tensor, ids: torch.Tensor, vocabulary: int, scale: float = 1.0,
+                             add_to: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient [vocabulary, width] of plaid_embedding's table from that of its result, d_out [n, width]: dense, or added in place to
+    `add_to`, which it then returns (a contiguous gradient of the same table from another use)."""
+    dev = _states(d_out, "d_out")
+    ids = _vector(ids, "ids", torch.int64, dev, d_out.shape[0])
+    d_out, stride = _rows(d_out)
+    n, width = d_out.shape
+    if add_to is None:
+        d_table = torch.empty((vocabulary, width), dtype=d_out.dtype, device=dev)
+    else:
+        d_table = _is(add_to, "add_to", d_out.dtype, 2, dev)
+        if tuple(d_table.shape) != (vocabulary, width) or not d_table.is_contiguous():
+            raise ValueError(f"add_to must be contiguous and have the shape {(vocabulary, width)}")
+    lib = _p.load_library()
+    need = ct.c_int64(0)
+    _p._check(lib.plaid_embedding_backward_workspace(n, vocabulary, width, ct.byref(need)))
+    work, ptr = _workspace(need.value, dev)
+    _p._check(lib.plaid_embedding_backward(d_out.data_ptr(), stride, vocabulary, width, ids.data_ptr(), n, float(scale), 0 if add_to is None else 1,
+                                           d_table.data_ptr(), _DTYPES[d_out.dtype], ptr, need.value, *_where(dev)))
+    return d_table
+
+
+def plaid_dropout(x: torch.Tensor, p: float, rng: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """residual + dropout of x, any shape: an element is zero with the probability p (a multiple of 2^-16), else x / (1 - p).  rng [2] int64
+    on x's device: a seed, and a number that no other call of the program has.  The gradient of x is the same call on the result's
+    gradient, without a residual; the residual's is the result's."""
+    dev = _states(x, "x", None)
+    _no_autograd("plaid_dropout", x=x, residual=residual)
+    rng = _vector(rng, "rng", torch.int64, dev, 2)
+    x = x.contiguous()
+    if residual is not None:
+        _is(residual, "residual", x.dtype, x.dim(), dev)
+        if residual.shape != x.shape:
+            raise ValueError("residual must have x's shape")
+        residual = residual.contiguous()
+    out = torch.empty_like(x)
+    _p._check(_p.load_library().plaid_dropout(x.data_ptr(), None if residual is None else residual.data_ptr(), x.numel(), float(p), rng.data_ptr(),
+                                              out.data_ptr(), _DTYPES[x.dtype], *_where(dev)))
+    return out
+
+
+def _parameters(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor]):
+    dev, width = x.device, x.shape[1]
+    if weight is not None:
+        weight = _vector(weight, "weight", x.dtype, dev, width)
+    if bias is not None:
+        bias = _vector(bias, "bias", x.dtype, dev, width)
+    return weight, bias
+
+
+def plaid_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                     return_statistics: bool = False):
+    """Layer norm of the rows of x [rows, width], times weight [width], plus bias [width].  With return_statistics also what
+    plaid_layer_norm_backward wants, each row's mean and 1 / sqrt(variance + eps), [rows, 2] float32."""
+    dev = _states(x, "x")
+    _no_autograd("plaid_layer_norm_backward", x=x, weight=weight, bias=bias)
+    weight, bias = _parameters(x, weight, bias)
+    x, stride = _rows(x)
+    rows, width = x.shape
+    out = torch.empty((rows, width), dtype=x.dtype, device=dev)
+    statistics = torch.empty((rows, 2), dtype=torch.float32, device=dev) if return_statistics else None
+    _p._check(_p.load_library().plaid_layer_norm(x.data_ptr(), stride, None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(),
+                                                 rows, width, float(eps), out.data_ptr(), None if statistics is None else statistics.data_ptr(),
+                                                 _DTYPES[x.dtype], *_where(dev)))
+    return (out, statistics) if return_statistics else out
+
+
+def plaid_layer_norm_backward(d_out: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor],
+                              statistics: torch.Tensor):
+    """(dx, dweight, dbias) of plaid_layer_norm from its statistics and the gradient d_out; None for a weight or bias that there is not."""
+    dev = _states(x, "x")
+    if _is(d_out, "d_out", x.dtype, 2, dev).shape != x.shape:
+        raise ValueError("d_out must have x's shape")
+    weight, bias = _parameters(x, weight, bias)
+    rows, width = x.shape
+    if _is(statistics, "statistics", torch.float32, 2, dev).shape != (rows, 2):
+        raise ValueError("statistics must be what plaid_layer_norm returned")
+    statistics = statistics.contiguous()
+    x, stride = _rows(x)
+    d_out, d_stride = _rows(d_out)
+    dx = torch.empty((rows, width), dtype=x.dtype, device=dev)
+    dweight = None if weight is None else torch.empty_like(weight)
+    dbias = None if bias is None else torch.empty_like(bias)
+    lib = _p.load_library()
+    need = ct.c_int64(0)
+    if weight is not None or bias is not None:
+        _p._check(lib.plaid_layer_norm_backward_workspace(rows, width, ct.byref(need)))
+    work, ptr = _workspace(need.value, dev)
+    address = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    _p._check(lib.plaid_layer_norm_backward(d_out.data_ptr(), d_stride, x.data_ptr(), stride, address(weight), statistics.data_ptr(), rows, width,
+                                            dx.data_ptr(), address(dweight), address(dbias), _DTYPES[x.dtype], ptr, need.value, *_where(dev)))
+    return dx, dweight, dbias
+
+
+def _loss_args(hidden, weight, targets, scale, loss, lse) -> plaid_token_loss:
+    """hidden, weight: what _aligned_rows gave."""
+    (h, h_stride), (w, w_stride) = hidden, weight
+    return plaid_token_loss(_DTYPES[h.dtype], h.shape[1], h.shape[0], w.shape[0], float(scale), h.data_ptr(), w.data_ptr(), h_stride, w_stride,
+                            targets.data_ptr(), None if loss is None else loss.data_ptr(), None if lse is None else lse.data_ptr())
+
+
+def _loss_inputs(hidden, weight, targets):
+    dev = _states(hidden, "hidden")
+    if _is(weight, "weight", hidden.dtype, 2, dev).shape[1] != hidden.shape[1]:
+        raise ValueError("hidden and weight must have rows of one width")
+    targets = _vector(targets, "targets", torch.int64, dev, hidden.shape[0])
+    return _aligned_rows(hidden), _aligned_rows(weight), targets
+
+
+def plaid_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, return_lse: bool = False):
+    """The negative logarithm of each target's probability under softmax(scale * hidden @ weight.T): hidden [rows, width], weight
+    [vocabulary, width], targets [rows] int64 -> [rows] float32, zero for a target outside the vocabulary.  With return_lse also what
+    plaid_cross_entropy_backward wants, the logarithm of the softmax's sum as two numbers to be added, [rows, 2] float32."""
+    rows, table, targets = _loss_inputs(hidden, weight, targets)
+    _no_autograd("plaid_cross_entropy_backward", hidden=hidden, weight=weight)
+    dev = hidden.device
+    loss = torch.empty(hidden.shape[0], dtype=torch.float32, device=dev)
+    lse = torch.empty((hidden.shape[0], 2), dtype=torch.float32, device=dev) if return_lse else None
+    lib = _p.load_library()
+    a = _loss_args(rows, table, targets, scale, loss, lse)
+    need = ct.c_int64(0)
+    _p._check(lib.plaid_cross_entropy_workspace(ct.byref(a), 0, ct.byref(need)))
+    work, ptr = _workspace(need.value, dev)
+    _p._check(lib.plaid_cross_entropy(ct.byref(a), ptr, need.value, *_where(dev)))
+    return (loss, lse) if return_lse else loss
+
+
+def plaid_cross_entropy_backward(d_loss: torch.Tensor, hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
+                                 scale: float = 1.0) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(d_hidden, d_weight) of plaid_cross_entropy from its lse and the gradient of its result, d_loss [rows] float32 (an expanded single
+    number is taken as it is)."""
+    rows, table, targets = _loss_inputs(hidden, weight, targets)
+    dev = hidden.device
+    n = hidden.shape[0]
+    if _is(d_loss, "d_loss", torch.float32, 1, dev).shape[0] != n:
+        raise ValueError(f"d_loss must hold {n} values, got {d_loss.shape[0]}")
+    if d_loss.stride(0) not in (0, 1):
+        d_loss = d_loss.contiguous()
+    if _is(lse, "lse", torch.float32, 2, dev).shape != (n, 2):
+        raise ValueError("lse must be what plaid_cross_entropy returned")
+    lse = lse.contiguous()
+    d_hidden = torch.empty((n, hidden.shape[1]), dtype=hidden.dtype, device=dev)
+    d_weight = torch.empty(tuple(weight.shape), dtype=hidden.dtype, device=dev)
+    lib = _p.load_library()
+    a = _loss_args(rows, table, targets, scale, None, lse)
+    need = ct.c_int64(0)
+    _p._check(lib.plaid_cross_entropy_workspace(ct.byref(a), 1, ct.byref(need)))
+    work, ptr = _workspace(need.value, dev)
+    _p._check(lib.plaid_cross_entropy_backward(ct.byref(a), d_loss.data_ptr(), d_loss.stride(0) if n > 1 else 1, d_hidden.data_ptr(), d_weight.data_ptr(), ptr, need.value,
+                                               *_where(dev)))
+    return d_hidden, d_weight

@@ -1,0 +1,279 @@
+"""Cross entropy over a vocabulary and its gradients against the definitions in 64 bits."""
+import pytest
+import torch
+
+from training_util import close, cross_entropy
+
+pytestmark = pytest.mark.gpu
+DEV, BF, HALF = torch.device("cuda", 0), torch.bfloat16, torch.float16
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def pl():
+    import paper_2205_09707_amd as pl
+    pl.load_library()
+    return pl
+
+
+def _inputs(rows, vocabulary, width, dtype, seed=0, without=0.15, lean=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    weight = torch.randn(vocabulary, width, generator=g, device=DEV).to(dtype)
+    targets = torch.randint(0, vocabulary, (rows,), generator=g, device=DEV)
+    h = torch.randn(rows, width, generator=g, device=DEV) + lean * torch.rand(rows, 1, generator=g, device=DEV) * weight[targets].float()
+    none = torch.tensor([-1, -100, vocabulary, 2 ** 40], device=DEV)[torch.arange(rows, device=DEV) % 4]
+    targets = torch.where(torch.rand(rows, generator=g, device=DEV) < without, none, targets)
+    d = torch.randn(rows, generator=g, device=DEV)
+    return h.to(dtype), weight, targets, d
+
+
+def _check(pl, h, w, t, d, scale, what="", forward_only=False):
+    want = cross_entropy(h, w, t, scale, None if forward_only else d)
+    loss, lse = pl.plaid_cross_entropy(h, w, t, scale=scale, return_lse=True)
+    close(loss, want["loss"], want["loss_bound"], what + " loss")
+    live = (t >= 0) & (t < w.shape[0])
+    close(lse.double().sum(1), want["lse"], want["loss_bound"], what + " lse")
+    assert not loss[~live].any()
+    assert torch.equal(pl.plaid_cross_entropy(h, w, t, scale=scale), loss)
+    if forward_only:
+        return loss
+    dh, dw = pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=scale)
+    close(dh, want["d_hidden"], want["d_hidden_bound"], what + " d_hidden")
+    close(dw, want["d_weight"], want["d_weight_bound"], what + " d_weight")
+    assert not dh[~live].any()
+    again = pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=scale)
+    assert torch.equal(dh, again[0]) and torch.equal(dw, again[1])
+    return loss, dh, dw
+
+
+SIZES = [(1, 1, 8), (1, 2, 64), (5, 17, 72), (16, 256, 128), (17, 1000, 512), (33, 257, 200), (48, 3001, 264), (64, 255, 96), (65, 300, 64), (100, 128, 8),
+         (255, 1000, 256), (256, 256, 256), (257, 513, 320), (300, 5000, 768), (700, 3001, 520), (3, 20_000, 136)]
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("rows,vocabulary,width", SIZES)
+def test_sizes(pl, rows, vocabulary, width, dtype):
+    h, w, t, d = _inputs(rows, vocabulary, width, dtype, seed=rows + vocabulary, without=0.15 if rows > 1 else 0.0)
+    _check(pl, h, w, t, d, width ** -0.5)
+
+
+@pytest.mark.parametrize("rows", [16, 300])
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1.0, 4.0])
+def test_scales(pl, rows, scale):
+    """Up to probabilities of one and of nothing."""
+    h, w, t, d = _inputs(rows, 700, 128, BF, lean=3.0)
+    _check(pl, h, w, t, d, scale)
+
+
+@pytest.mark.parametrize("rows", [7, 500])
+def test_probabilities_near_one_keep_their_distance(pl, rows):
+    """One score above the others, all of them above a thousand: loss and gradient are as far off as the sum of exponentials beside the
+    largest, not as lse, whose spacing is 2^-13 there.  The sum is between 1 and 2 and has at most 64 additions of a lane and 16 joins after
+    the largest, each off by 2^-24.  The scores themselves are exact: 1024 and a number of 8 digits."""
+    w = torch.zeros(300, 64, device=DEV, dtype=BF)
+    w[:, 0], w[:, 1] = -1.0, 16.0
+    w[11, 0] = 1.0
+    h = torch.zeros(rows, 64, device=DEV, dtype=BF)
+    h[:, 0], h[:, 1] = torch.linspace(3.5, 12, rows, device=DEV), 64.0
+    t = torch.full((rows,), 11, device=DEV)
+    loss, lse = pl.plaid_cross_entropy(h, w, t, return_lse=True)
+    want = torch.log1p(299 * torch.exp(-2 * h[:, 0].double()))
+    off = 80 * 2.0 ** -24
+    close(loss, want, want * 2.0 ** -20 + off, "loss")
+    dh, _ = pl.plaid_cross_entropy_backward(torch.ones(rows, device=DEV), h, w, t, lse)
+    others = 1 - torch.exp(-want)
+    # G of the target and of the others: each rounds to bf16, and so does the sum of both
+    close(dh[:, 0], -2 * others, 2 * others * 2.0 ** -7 + 2.1 * off, "d_hidden")
+
+
+@pytest.mark.parametrize("rows", [20, 400])
+def test_no_row_has_a_target(pl, rows):
+    h, w, t, d = _inputs(rows, 300, 64, BF)
+    t.fill_(-100)
+    h.fill_(NAN)
+    d.fill_(NAN)
+    loss, lse = pl.plaid_cross_entropy(h, w, t, return_lse=True)
+    dh, dw = pl.plaid_cross_entropy_backward(d, h, w, t, lse)
+    assert not loss.any() and not lse.any() and not dh.any() and not dw.any()
+
+
+@pytest.mark.parametrize("rows", [20, 400])
+@pytest.mark.parametrize("dtype", [BF, HALF])
+def test_rows_without_a_target_reach_nothing(pl, rows, dtype):
+    h, w, t, d = _inputs(rows, 500, 96, dtype, without=0.4)
+    want = _check(pl, h, w, t, d, 0.1)
+    out = (t < 0) | (t >= 500)
+    h[out], d[out] = NAN, INF
+    h[out.nonzero()[0]] = INF
+    loss, lse = pl.plaid_cross_entropy(h, w, t, scale=0.1, return_lse=True)
+    dh, dw = pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=0.1)
+    assert torch.equal(loss, want[0]) and torch.equal(dh, want[1]) and torch.equal(dw, want[2])
+
+
+def test_no_rows(pl):
+    h, w, t, d = _inputs(4, 30, 64, BF)
+    loss, lse = pl.plaid_cross_entropy(h[:0], w, t[:0], return_lse=True)
+    assert loss.shape == (0,) and lse.shape == (0, 2)
+    dh, dw = pl.plaid_cross_entropy_backward(d[:0], h[:0], w, t[:0], lse)
+    assert dh.shape == (0, 64) and dw.shape == (30, 64) and not dw.any()
+
+
+@pytest.mark.parametrize("rows", [9, 300])
+def test_what_is_not_finite_is_seen(pl, rows):
+    h, w, t, d = _inputs(rows, 400, 64, BF, without=0.0)
+    clean, _ = pl.plaid_cross_entropy(h, w, t, scale=0.1, return_lse=True)
+    h[2, 5] = NAN
+    loss, lse = pl.plaid_cross_entropy(h, w, t, scale=0.1, return_lse=True)
+    keep = [i for i in range(rows) if i != 2]
+    assert torch.isnan(loss[2]) and torch.equal(loss[keep], clean[keep])
+    dh, dw = pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=0.1)
+    assert torch.isnan(dh[2]).all() and torch.isfinite(dh[keep]).all() and torch.isnan(dw).all()
+    d[4] = INF
+    h[2, 5] = 0.0
+    _, lse = pl.plaid_cross_entropy(h, w, t, scale=0.1, return_lse=True)
+    dh, _ = pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=0.1)
+    keep = [i for i in range(rows) if i != 4]
+    assert not torch.isfinite(dh[4]).any() and torch.isfinite(dh[keep]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("kind", ["tiny", "spread", "zeros", "one", "huge"])
+def test_gradients_of_the_loss(pl, dtype, kind):
+    """In fp16 the results' range is the type's; G's is not."""
+    h, w, t, d = _inputs(200, 900, 64, dtype)
+    if kind == "tiny":
+        d = d * 1e-3 if dtype == HALF else d * 1e-30
+    elif kind == "spread":
+        d = d * torch.exp2(-torch.arange(200, device=DEV) % 20.0)
+    elif kind == "zeros":
+        d[::3] = 0.0
+    elif kind == "one":
+        d = d[:1].expand(200)
+    else:
+        d = d * (100 if dtype == HALF else 1e30)
+    _check(pl, h, w, t, d, 0.125, kind)
+    _check(pl, h, w, t, torch.zeros_like(d), 0.125, "nothing")
+
+
+def test_views_and_misaligned_rows(pl):
+    h, w, t, d = _inputs(270, 600, 64, BF)
+    want = _check(pl, h, w, t, d, 0.2)
+    wide, tall = torch.full((270, 200), NAN, device=DEV, dtype=BF), torch.full((600, 72), NAN, device=DEV, dtype=BF)
+    for first in (8, 3):  # read in place, copied
+        wide[:, first:first + 64], tall[:, :64] = h, w
+        got = _check(pl, wide[:, first:first + 64], tall[:, :64], t, d, 0.2, "views")
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(torch.equal(a, b) for a, b in zip(_check(pl, h, w.T.contiguous().T, t.repeat_interleave(2)[::2], d.repeat_interleave(2)[::2], 0.2, "transposed"), want))
+    _check(pl, h[:1].expand(270, 64), w, t, d, 0.2, "one state for all rows")
+
+
+def test_pieces_of_the_vocabulary(pl):
+    """More entries than the workspace's pieces have; the last is not whole."""
+    h, w, t, d = _inputs(130, 700_001, 16, BF)
+    _check(pl, h, w, t, d, 0.25)
+    h, w, t, d = _inputs(5000, 131_073, 8, HALF)
+    want = None
+    for rows in (slice(0, 64), slice(64, 128)):  # the same rows by the kernel of few rows
+        part = _check(pl, h[rows], w, t[rows], d[rows], 0.25, "few", forward_only=True)
+        want = part if want is None else torch.cat([want, part])
+    loss, lse = pl.plaid_cross_entropy(h, w, t, scale=0.25, return_lse=True)
+    # each is off by the sum of exponentials' 2 (131073 / 128 + 150) 2^-24 = 1.4e-4 at most
+    close(loss[:128], want.double(), 3e-4, "the same rows")
+    dh, dw = pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=0.25)
+    some = torch.cat([torch.arange(40, device=DEV), torch.arange(4900, 5000, device=DEV)])
+    few = cross_entropy(h[some], w, t[some], 0.25, d[some])
+    close(loss[some], few["loss"], few["loss_bound"], "some rows")
+    close(dh[some], few["d_hidden"], few["d_hidden_bound"], "some rows' gradients")
+    # a row of G adds up to nothing, so the columns of dW do, but for roundings: of G (its magnitudes add up to 2 |d| at most), and of dW
+    live = (t >= 0) & (t < 131_073)
+    total, size = dw.double().sum(0), dw.double().abs().sum(0)
+    roundings = 0.25 * 2 * d[live].double().abs() @ h[live].double().abs() * (2.0 ** -11 + 2.0 ** -12) + 2.0 ** -11 * size + 131_073 * 2.0 ** -25
+    assert (total.abs() <= roundings).all()
+
+
+def test_weights_beyond_four_gigabytes(pl):
+    vocabulary, width = 300_000, 8192
+    w = torch.empty(vocabulary, width, dtype=BF, device=DEV)
+    for a in range(0, vocabulary, 50_000):
+        w[a:a + 50_000] = torch.randn(50_000, width, device=DEV).to(BF)
+    for rows in (3, 70):
+        h = torch.randn(rows, width, device=DEV).to(BF)
+        t = torch.randint(vocabulary - 1000, vocabulary, (rows,), device=DEV)
+        loss, lse = pl.plaid_cross_entropy(h, w, t, scale=0.02, return_lse=True)
+        s = torch.cat([h.double() @ w[a:a + 50_000].double().T * 0.02 for a in range(0, vocabulary, 50_000)], 1)
+        want = torch.logsumexp(s, 1) - s[torch.arange(rows), t]
+        # scores of a few units, sums of 8192 products of either sign: partial sums stay below 32, each rounds by at most 2^-20, in either
+        # direction: 8 sqrt(8192) of them
+        close(loss, want, 1e-3, f"{rows} rows")
+        if rows == 70:
+            d = torch.randn(rows, device=DEV)
+            dh, dw = pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=0.02)
+            p = torch.exp(s - torch.logsumexp(s, 1, keepdim=True))
+            p[torch.arange(rows), t] -= 1
+            g = p * d.double()[:, None] * 0.02
+            last = slice(vocabulary - 1000, vocabulary)
+            close(dw[last], g[:, last].T @ h.double(), 1.1 * 2.0 ** -7 * (g[:, last].abs().T @ h.double().abs()) + 1e-30, "the last rows' gradients")
+            want = sum(g[:, a:a + 50_000] @ w[a:a + 50_000].double() for a in range(0, vocabulary, 50_000))
+            size = sum(g[:, a:a + 50_000].abs() @ w[a:a + 50_000].double().abs() for a in range(0, vocabulary, 50_000))
+            close(dh, want, 1.1 * 2.0 ** -7 * size, "d_hidden")
+        del s
+
+
+@pytest.mark.parametrize("rows", [9, 400])
+def test_captured_and_replayed(pl, rows):
+    h, w, t, d = _inputs(rows, 2000, 128, BF)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        lse = pl.plaid_cross_entropy(h, w, t, return_lse=True)[1]
+        pl.plaid_cross_entropy_backward(d, h, w, t, lse)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, lse = pl.plaid_cross_entropy(h, w, t, scale=0.1, return_lse=True)
+        dh, dw = pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=0.1)
+    for seed in (1, 2, 3):
+        for to, new in zip((h, w, t, d), _inputs(rows, 2000, 128, BF, seed=seed, without=0.1 * seed)):
+            to.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, want_lse = pl.plaid_cross_entropy(h, w, t, scale=0.1, return_lse=True)
+        assert torch.equal(loss, want) and torch.equal(lse, want_lse)
+        assert all(torch.equal(a, b) for a, b in zip((dh, dw), pl.plaid_cross_entropy_backward(d, h, w, t, want_lse, scale=0.1)))
+
+
+def test_two_streams_at_once(pl):
+    sets = [_inputs(300, 3000, 128, BF, seed=s) for s in (1, 2)]
+    want = []
+    for h, w, t, d in sets:
+        loss, lse = pl.plaid_cross_entropy(h, w, t, scale=0.1, return_lse=True)
+        want.append((loss,) + pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=0.1))
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for _ in range(3):
+        for i, (h, w, t, d) in enumerate(sets):
+            with torch.cuda.stream(streams[i]):
+                loss, lse = pl.plaid_cross_entropy(h, w, t, scale=0.1, return_lse=True)
+                got[i] = (loss,) + pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=0.1)
+    torch.cuda.synchronize()
+    for g, x in zip(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(g, x))
+
+
+def test_refusals(pl):
+    h, w, t, d = _inputs(10, 40, 64, BF)
+    _, lse = pl.plaid_cross_entropy(h, w, t, return_lse=True)
+    for f in (lambda: pl.plaid_cross_entropy(h.float(), w, t), lambda: pl.plaid_cross_entropy(h, w.half(), t), lambda: pl.plaid_cross_entropy(h, w[:, :32], t),
+              lambda: pl.plaid_cross_entropy(h, w, t[:5]), lambda: pl.plaid_cross_entropy(h, w, t.int()), lambda: pl.plaid_cross_entropy_backward(d[:5], h, w, t, lse),
+              lambda: pl.plaid_cross_entropy_backward(d.double(), h, w, t, lse), lambda: pl.plaid_cross_entropy_backward(d, h, w, t, lse[:, :1])):
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(pl.PlaidError):
+        pl.plaid_cross_entropy(torch.zeros(2, 60, device=DEV, dtype=BF), torch.zeros(9, 60, device=DEV, dtype=BF), t[:2])
+    with pytest.raises(pl.PlaidError):
+        pl.plaid_cross_entropy(h, w[:0], t)
+    for which in (h, w):
+        which.requires_grad_()
+        with pytest.raises(ValueError, match="requires a gradient"):
+            pl.plaid_cross_entropy(h, w, t)
+        which.requires_grad_(False)
