@@ -58,28 +58,31 @@ __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a, int backwar
     }
 }
 
-// Their states, packed; zeros up to a whole tile of rows and a whole step of columns.  A workgroup has a row.
+// Their states, packed in the order in which the products' tiles take them; zeros up to a whole tile of rows and a whole step of columns.
+// A workgroup has a row.
 template <int DT, bool BACKWARD>
 __global__ __launch_bounds__(128) void loss_pack_kernel(LossArgs a)
 {
+    constexpr int BLOCK = LOSS_TILE * LOSS_STEP * 2;
     const int live = uniform_load(a.state), top = uniform_load(a.state + 1), i = blockIdx.x;
     if (i >= (live + LOSS_TILE - 1) / LOSS_TILE * LOSS_TILE) return;
     const bool there = i < live;
     const char *from = a.hidden + (there ? (int64_t)uniform_load(a.list + i) : 0) * a.hidden_stride;
-    char *to = a.packed + (int64_t)i * a.pitch * 2, *scaled = BACKWARD ? a.scaled + (int64_t)i * a.pitch * 2 : nullptr;
+    char *to = a.packed + (int64_t)(i / LOSS_TILE) * (a.pitch / LOSS_STEP) * BLOCK + i % LOSS_TILE * (2 * LOSS_STEP);
+    char *scaled = BACKWARD ? a.scaled + (int64_t)(i / LOSS_STEP) * (a.columns / LOSS_TILE) * BLOCK + i % LOSS_STEP * (2 * LOSS_TILE) : nullptr;
     float power = 1.0f;
     if (BACKWARD && there) {
         const int e = uniform_load(&a.row[i].exponent);
         if (e != NO_EXPONENT) power = ldexpf(1.0f, e - top);
     }
-    for (int at = threadIdx.x * 8; at < a.pitch; at += 1024) {
+    for (int at = threadIdx.x * 8; at < (BACKWARD ? a.columns : a.pitch); at += 1024) {
         const i32x4 w = there && at < a.width ? *(const i32x4 *)(from + 2 * at) : i32x4{0, 0, 0, 0};
-        *(i32x4 *)(to + 2 * at) = w;
+        if (at < a.pitch) *(i32x4 *)(to + (int64_t)(at / LOSS_STEP) * BLOCK + at % LOSS_STEP * 2) = w;
         if (BACKWARD) {
             Eight v = unpack8<DT>(w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v.x[j] *= power;
-            *(i32x4 *)(scaled + 2 * at) = pack8<DT>(v);
+            *(i32x4 *)(scaled + (int64_t)(at / LOSS_TILE) * BLOCK + at % LOSS_TILE * 2) = pack8<DT>(v);
         }
     }
 }
@@ -102,65 +105,93 @@ void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool b
     if (backward && a.d_hidden) loss_zero_kernel<<<(unsigned)a.rows, 128, 0, st>>>(a);
 }
 
-// --- few rows -------------------------------------------------------------------------------------------------------------------
-// The vocabulary's rows go straight from memory into registers, the operand of the matrix instruction, and are read once; the states come
-// out of the caches.  A wave has 16 BLOCKS entries and up to 16 GROUPS rows.
-template <int DT, int BLOCKS, int GROUPS>
-__global__ __launch_bounds__(256) void loss_few_kernel(LossArgs a)
+// Maxima and sums of exponentials beside them, of two parts.
+__device__ __forceinline__ float2 join_parts(float2 x, float2 y)
 {
-    constexpr int STEP = 32;
-    const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4;
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), v0 = wave * (16 * BLOCKS);
-    if (v0 >= a.vocabulary) return;
-    const char *w[BLOCKS], *h[GROUPS];
+    const float m = fmaxf(x.x, y.x), base = m == -INFINITY ? 0.0f : m;
+    return {m, x.y * __builtin_amdgcn_exp2f((x.x - base) * LOG2E) + y.y * __builtin_amdgcn_exp2f((y.x - base) * LOG2E)};
+}
+
+// --- few rows -------------------------------------------------------------------------------------------------------------------
+// The vocabulary is read once, at the rate of memory if enough of it is under way: a workgroup has 64 BLOCKS entries, a quarter for each of its
+// four waves, and up to 16 GROUPS rows; 64 columns of both go straight into LDS, two steps ahead of the products.
+#define FEW_STAGES 3
+template <int DT, int BLOCKS, int GROUPS>
+__global__ __launch_bounds__(LOSS_FEW_THREADS) void loss_few_kernel(LossArgs a)
+{
+    constexpr int ENTRIES = 64 * BLOCKS, W_LOADS = 2 * BLOCKS, H_PIECES = 2 * GROUPS, H_LOADS = (H_PIECES + 3) / 4, LOADS = W_LOADS + H_LOADS;
+    __shared__ __align__(16) char lds_w[FEW_STAGES][ENTRIES * 128], lds_h[FEW_STAGES][GROUPS * 16 * 128];
+    __shared__ float2 joined[4][16 * GROUPS];
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), l = lane & 15, q = lane >> 4;
+    const int64_t v0 = (int64_t)blockIdx.x * ENTRIES;
+    // a load has eight rows of 128 bytes, whose chunks change places as lds_chunk says; with fewer pieces of states than waves some are brought twice
+    const char *from[LOADS];
+    int to[LOADS];
+    int chunk[LOADS];
 #pragma unroll
-    for (int i = 0; i < BLOCKS; ++i) w[i] = a.weight + min(v0 + 16 * i + l, a.vocabulary - 1) * a.weight_stride + 16 * q;
+    for (int i = 0; i < LOADS; ++i) {
+        const bool w = i < W_LOADS;
+        const int piece = w ? wave * W_LOADS + i : (wave + 4 * (i - W_LOADS)) % H_PIECES, row = piece * 8 + (lane >> 3);
+        chunk[i] = (lane & 7) ^ swizzle<64>(row);
+        to[i] = piece * 1024;
+        from[i] = w ? a.weight + min(v0 + row, a.vocabulary - 1) * a.weight_stride : a.hidden + min((int64_t)row, a.rows - 1) * a.hidden_stride;
+        from[i] += chunk[i] * 16;
+    }
+    const int steps = (a.width + 63) / 64, left = a.width - (steps - 1) * 64;
+    const auto bring = [&](int s, int stage) {
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) h[i] = a.hidden + min((int64_t)16 * i + l, a.rows - 1) * a.hidden_stride + 16 * q;
+        for (int i = 0; i < LOADS; ++i) {
+            const char *p = from[i] + s * 128;
+            if (s == steps - 1 && chunk[i] * 8 >= left) p = (const char *)zero_row;  // zeros past the end of the rows
+            load_to_lds(p, (i < W_LOADS ? lds_w[stage] : lds_h[stage]) + to[i]);
+        }
+    };
     f32x4 acc[BLOCKS][GROUPS];
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
         for (int j = 0; j < GROUPS; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-    const int whole = a.width / STEP;
-#pragma unroll 4
-    for (int s = 0; s < whole; ++s) {
-        i32x4 x[BLOCKS], y[GROUPS];
+    int place[2];
 #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) x[i] = *(const i32x4 *)(w[i] + s * (2 * STEP));
+    for (int k = 0; k < 2; ++k) place[k] = l * 128 + (((4 * k + q) ^ swizzle<64>(l)) << 4);  // rows 16 on: 2048 bytes
 #pragma unroll
-        for (int j = 0; j < GROUPS; ++j) y[j] = *(const i32x4 *)(h[j] + s * (2 * STEP));
+    for (int s = 0; s < FEW_STAGES - 1; ++s)
+        if (s < steps) bring(s, s);
+    int stage = 0;
+    for (int s = 0; s < steps; ++s) {
+        if (s + 1 < steps) wait_loads<LOADS * (FEW_STAGES - 2)>();
+        else wait_loads<0>();
+        lds_barrier();  // this step's tiles have come, and all waves are done with those of the step before
+        if (s + FEW_STAGES - 1 < steps) bring(s + FEW_STAGES - 1, stage == 0 ? FEW_STAGES - 1 : stage - 1);
+        const char *w = lds_w[stage] + wave * (BLOCKS * 2048), *h = lds_h[stage];
 #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i)
+        for (int k = 0; k < 2; ++k) {
+            i32x4 x[BLOCKS], y[GROUPS];
 #pragma unroll
-            for (int j = 0; j < GROUPS; ++j) acc[i][j] = mfma16<DT>(x[i], y[j], acc[i][j]);
+            for (int i = 0; i < BLOCKS; ++i) x[i] = *(const i32x4 *)(w + i * 2048 + place[k]);
+#pragma unroll
+            for (int j = 0; j < GROUPS; ++j) y[j] = *(const i32x4 *)(h + j * 2048 + place[k]);
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                for (int j = 0; j < GROUPS; ++j) acc[i][j] = mfma16<DT>(x[i], y[j], acc[i][j]);
+        }
+        stage = stage == FEW_STAGES - 1 ? 0 : stage + 1;
     }
-    if (whole * STEP < a.width) {
-        const bool there = whole * STEP + 8 * q < a.width;
-        const i32x4 zero = {0, 0, 0, 0};
-        i32x4 x[BLOCKS], y[GROUPS];
-#pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) x[i] = there ? *(const i32x4 *)(w[i] + whole * (2 * STEP)) : zero;
-#pragma unroll
-        for (int j = 0; j < GROUPS; ++j) y[j] = there ? *(const i32x4 *)(h[j] + whole * (2 * STEP)) : zero;
-#pragma unroll
-        for (int i = 0; i < BLOCKS; ++i)
-#pragma unroll
-            for (int j = 0; j < GROUPS; ++j) acc[i][j] = mfma16<DT>(x[i], y[j], acc[i][j]);
-    }
+    const int64_t mine = v0 + wave * (16 * BLOCKS);
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
         const int64_t t = 16 * j + l;
-        const int64_t target = t < a.rows ? a.targets[t] - v0 : -1;
+        const int64_t target = t < a.rows ? a.targets[t] : -1;
         float most = -INFINITY;
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int v = 16 * i + 4 * q + r;
+                const int64_t v = mine + 16 * i + 4 * q + r;
                 float s = acc[i][j][r] * a.scale;
-                if (v0 + v >= a.vocabulary) s = -INFINITY;
-                else if (v == target) a.own[t] = s;
+                if (v == target && v < a.vocabulary) a.own[t] = s;
+                if (v == target || v >= a.vocabulary) s = -INFINITY;
                 acc[i][j][r] = s;
                 most = fmaxf(most, s);
             }
@@ -172,7 +203,12 @@ __global__ __launch_bounds__(256) void loss_few_kernel(LossArgs a)
 #pragma unroll
             for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E);
         sum = sum_halves(sum_rows(sum));
-        if (lane < 16 && t < a.rows) a.part[wave * a.padded_rows + t] = {most, sum};
+        if (lane < 16) joined[wave][16 * j + l] = {most, sum};
+    }
+    __syncthreads();
+    if (threadIdx.x < 16 * GROUPS && threadIdx.x < a.rows) {
+        const int t = threadIdx.x;
+        a.part[(int64_t)blockIdx.x * a.padded_rows + t] = join_parts(join_parts(joined[0][t], joined[1][t]), join_parts(joined[2][t], joined[3][t]));
     }
 }
 
@@ -180,26 +216,22 @@ void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int blo
 {
     const int groups = (int)((a.rows + 15) / 16);
     const unsigned grid = (unsigned)((a.vocabulary + 64 * blocks - 1) / (64 * blocks));
-#define GO(DT, B, G) loss_few_kernel<DT, B, G><<<grid, 256, 0, st>>>(a)
+#define GO(DT, B, G) loss_few_kernel<DT, B, G><<<grid, LOSS_FEW_THREADS, 0, st>>>(a)
 #define GROUPS(DT, B) (groups == 1 ? GO(DT, B, 1) : groups == 2 ? GO(DT, B, 2) : groups == 3 ? GO(DT, B, 3) : GO(DT, B, 4))
-    if (dtype == PLAID_BF16) blocks == 1 ? GROUPS(PLAID_BF16, 1) : GROUPS(PLAID_BF16, 4);
-    else blocks == 1 ? GROUPS(PLAID_FP16, 1) : GROUPS(PLAID_FP16, 4);
+    if (dtype == PLAID_BF16) blocks == 1 ? GROUPS(PLAID_BF16, 1) : GROUPS(PLAID_BF16, 2);
+    else blocks == 1 ? GROUPS(PLAID_FP16, 1) : GROUPS(PLAID_FP16, 2);
 #undef GROUPS
 #undef GO
 }
 
 // --- parts joined ---------------------------------------------------------------------------------------------------------------
-// ROWS rows a workgroup; its threads of one row take the parts in turn.  With the last piece come the loss and lse.
-__device__ __forceinline__ float2 join_parts(float2 x, float2 y)
-{
-    const float m = fmaxf(x.x, y.x), base = m == -INFINITY ? 0.0f : m;
-    return {m, x.y * __builtin_amdgcn_exp2f((x.x - base) * LOG2E) + y.y * __builtin_amdgcn_exp2f((y.x - base) * LOG2E)};
-}
+// ROWS rows a workgroup; its threads of one row take the parts in turn.  With the last piece come the loss and lse: the target's score is
+// not among the parts, so that where it is the largest the sum beside it is what the others have, and a loss near nothing keeps its digits.
 template <int ROWS>
 __global__ __launch_bounds__(256) void loss_join_kernel(LossArgs a, int parts, int packed)
 {
     constexpr int SHARES = 256 / ROWS;
-    __shared__ float2 lds[SHARES][ROWS];
+    __shared__ float2 lds[4][ROWS];
     const int r = threadIdx.x % ROWS, share = threadIdx.x / ROWS, live = packed ? uniform_load(a.state) : (int)a.rows;
     const int i = blockIdx.x * ROWS + r;
     float2 x = {-INFINITY, 0.0f};
@@ -207,10 +239,12 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossArgs a, int parts, i
 #pragma unroll 4
         for (int p = share; p < parts; p += SHARES) x = join_parts(x, a.part[(int64_t)p * a.padded_rows + i]);
     }
-    lds[share][r] = x;
+#pragma unroll
+    for (int o = ROWS; o < 64; o <<= 1) x = join_parts(x, {__shfl_xor(x.x, o), __shfl_xor(x.y, o)});
+    if ((threadIdx.x & 63) < ROWS) lds[threadIdx.x >> 6][r] = x;
     __syncthreads();
     if (share != 0 || i >= live) return;
-    for (int s = 1; s < SHARES; ++s) x = join_parts(x, lds[s][r]);
+    x = join_parts(join_parts(lds[0][r], lds[1][r]), join_parts(lds[2][r], lds[3][r]));
     if (a.first > 0) x = join_parts(a.running[i], x);
     if (!a.last) {
         a.running[i] = x;
@@ -218,15 +252,18 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossArgs a, int parts, i
     }
     const int64_t t = packed ? (int64_t)a.list[i] : i;
     const bool there = packed || (a.targets[t] >= 0 && a.targets[t] < a.vocabulary);
-    const float rest = logf(x.y);
-    a.loss[t] = there ? (x.x - a.own[i]) + rest : 0.0f;
-    if (a.lse) *(float2 *)(a.lse + 2 * t) = there ? float2{x.x, rest} : float2{0.0f, 0.0f};
+    const float own = there ? a.own[i] : 0.0f;
+    // log(exp(own) + sum), beside the larger of the two; where both are infinite or not a number, so is the result
+    const float top = x.x > own ? x.x : own;
+    const float rest = x.x > own ? logf(x.y + __builtin_amdgcn_exp2f((own - top) * LOG2E)) : x.x == -INFINITY && x.y == 0.0f ? 0.0f : log1pf(x.y * __builtin_amdgcn_exp2f((x.x - top) * LOG2E));
+    a.loss[t] = there ? (top - own) + rest : 0.0f;
+    if (a.lse) *(float2 *)(a.lse + 2 * t) = there ? float2{top, rest} : float2{0.0f, 0.0f};
 }
 
 void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool packed)
 {
     if (a.rows >= 4096) loss_join_kernel<32><<<(unsigned)((a.rows + 31) / 32), 256, 0, st>>>(a, parts, packed);
-    else if (a.rows >= 512) loss_join_kernel<8><<<(unsigned)((a.rows + 7) / 8), 256, 0, st>>>(a, parts, packed);
+    else if (a.rows > LOSS_FEW) loss_join_kernel<8><<<(unsigned)((a.rows + 7) / 8), 256, 0, st>>>(a, parts, packed);
     else loss_join_kernel<1><<<(unsigned)a.rows, 256, 0, st>>>(a, parts, packed);
 }
 
@@ -238,11 +275,12 @@ __global__ __launch_bounds__(128) void loss_d_hidden_join_kernel(LossArgs a)
     if (i >= uniform_load(a.state)) return;
     const int64_t t = uniform_load(a.list + i);
     const int e = uniform_load(&a.row[i].exponent);
+    const int splits = hidden_splits((uniform_load(a.state) + LOSS_TILE - 1) / LOSS_TILE * (a.columns / LOSS_TILE), a.hidden_steps, a.splits);
     // the power of two last, where the result may leave the normal range
     const float factor = a.scale * (DT == PLAID_FP16 ? 0x1p-15f : 1.0f);
     for (int at = threadIdx.x * 8; at < a.width; at += 1024) {
         Eight v = {};
-        for (int s = 0; s < a.splits; ++s) {
+        for (int s = 0; s < splits; ++s) {
             const float *p = a.d_part + ((int64_t)s * a.padded_rows + i) * a.columns + at;
             const f32x4 x = *(const f32x4 *)p, y = *(const f32x4 *)(p + 4);
 #pragma unroll

@@ -16,8 +16,10 @@
 template <bool ACROSS>
 struct Operand {
     const char *at[4];
-    int k[4];  // across: the load's row of k
-    __device__ __forceinline__ void set(const char *base, int64_t stride, int64_t rows, int64_t first, int64_t columns)
+    int k[4];  // of the lane's chunk
+    // along: rows first .. first + 255 of `rows`, later ones are the last again.  across: columns first .. first + 255 of `columns`; what lies
+    // past the end is column 0, and its results are not kept.
+    __device__ __forceinline__ void set(const char *base, int64_t stride, int64_t first, int64_t rows, int64_t columns)
     {
         const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
 #pragma unroll
@@ -31,7 +33,7 @@ struct Operand {
                 const int half = load >> 4, row = (load & 15) * 4 + (lane >> 4), chunk = (lane & 15) ^ swizzle<128>(row);
                 const int64_t column = first + half * 128 + chunk * 8;
                 k[i] = row;
-                at[i] = base + row * stride + (column < columns ? column : 0) * 2;  // what lies past the end is not kept
+                at[i] = base + row * stride + (column < columns ? column : 0) * 2;
             }
         }
     }
@@ -60,23 +62,37 @@ struct Operand {
         for (int i = 0; i < 4; ++i) at[i] += bytes;
     }
 };
-// The operand of 32 rows (columns, across) from `base` on at k = 16 s + 8 (l / 32) .. + 7.
-template <bool ACROSS>
-__device__ __forceinline__ i32x4 operand(const char *tile, int base, int s)
-{
-    if constexpr (!ACROSS) return lds_rows<64>(tile, base, s);
-    else {
-        const int lane = threadIdx.x & 63, row = 16 * s + 8 * (lane >> 5) + ((lane >> 2) & 3), x = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-        const char *half = tile + (base >> 7) * (TILE_BYTES / 2);
-        const int dt = (base >> 5) & 3;
-        const char *p = half + row * 256 + (((4 * dt + x) ^ swizzle<128>(row)) << 4) + (lane & 1) * 8;
-        const char *r = half + (row + 4) * 256 + (((4 * dt + x) ^ swizzle<128>(row + 4)) << 4) + (lane & 1) * 8;
-        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const i32x2 u = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p));
-        const i32x2 w = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)r));
-        return i32x4{u[0], u[1], w[0], w[1]};
+// Where a lane reads its part of the operand of 32 rows (columns, across) at k = 16 s + 8 (l / 32) .. + 7, for N such blocks.  Along, blocks are
+// at a constant distance and s = 0 .. 3 have a place each; across, steps of s are, and blocks have two places each, four rows of k apart.
+template <bool ACROSS, int N>
+struct Places {
+    int at[ACROSS ? 2 * N : 4];
+    __device__ __forceinline__ void set(int base)
+    {
+        const int lane = threadIdx.x & 63;
+        if constexpr (!ACROSS) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) at[s] = (base + (lane & 31)) * 128 + (((2 * s + (lane >> 5)) ^ swizzle<64>(lane & 31)) << 4);
+        } else {
+            const int row = 8 * (lane >> 5) + ((lane >> 2) & 3), x = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+#pragma unroll
+            for (int i = 0; i < 2 * N; ++i) {
+                const int r = row + 4 * (i & 1), block = (base >> 5) + i / 2;
+                at[i] = (block >> 2) * (TILE_BYTES / 2) + r * 256 + ((((block & 3) * 4 + x) ^ swizzle<128>(r)) << 4) + (lane & 1) * 8;
+            }
+        }
     }
-}
+    __device__ __forceinline__ i32x4 read(const char *tile, int i, int s) const
+    {
+        if constexpr (!ACROSS) return *(const i32x4 *)(tile + at[s] + i * 4096);
+        else {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const i32x2 u = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + at[2 * i] + s * 4096)));
+            const i32x2 w = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + at[2 * i + 1] + s * 4096)));
+            return i32x4{u[0], u[1], w[0], w[1]};
+        }
+    }
+};
 
 struct Tile {
     int m, n;
@@ -110,28 +126,33 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
     const int split = KIND == KIND_D_HIDDEN ? blockIdx.y : 0;
     if (!find_tile(blockIdx.x, SCORES ? pieces : widths, KIND == KIND_D_WEIGHT ? pieces : row_tiles, t)) return;
 
-    const int64_t gradient_stride = (int64_t)pieces * LOSS_TILE * 2;
+    // a piece's gradients lie tile by tile, rows by pieces, 128 KB each; packed states too, of 64 columns, 32 KB each
+    constexpr int64_t G_TILE = LOSS_TILE * LOSS_TILE * 2;
     Operand<A_ACROSS> A;
     Operand<B_ACROSS> B;
-    int64_t a_step = 2 * BK, b_step = 2 * BK;
+    int64_t a_step = 2 * BK, b_step = TILE_BYTES;
     int begin = 0, steps, end_left = BK;  // steps of k, what there is of the last
     if constexpr (SCORES) {
         steps = a.pitch / BK, end_left = a.width - (steps - 1) * BK;
-        A.set(a.weight, a.weight_stride, a.vocabulary, a.first + t.m * LOSS_TILE, 0);
-        B.set(a.packed, (int64_t)a.pitch * 2, a.padded_rows, t.n * LOSS_TILE, 0);
+        A.set(a.weight, a.weight_stride, a.first + t.m * LOSS_TILE, a.vocabulary, 0);
+        B.set(a.packed + (int64_t)t.n * steps * TILE_BYTES, 2 * BK, 0, LOSS_TILE, 0);
     } else if constexpr (KIND == KIND_D_HIDDEN) {
-        const int all = (a.piece + BK - 1) / BK, share = (all + a.splits - 1) / a.splits;
+        const int all = (a.piece + BK - 1) / BK, splits = hidden_splits(row_tiles * widths, a.hidden_steps, a.splits), share = (all + splits - 1) / splits;
+        if (split >= splits) return;
         begin = min(all, split * share), steps = min(all, begin + share) - begin;
         if (begin + steps == all) end_left = a.piece - (all - 1) * BK;
-        a_step = BK * a.weight_stride;
-        A.set(a.weight + (a.first + (int64_t)begin * BK) * a.weight_stride, a.weight_stride, 0, t.m * LOSS_TILE, a.width);
-        B.set(a.gradient + begin * BK * 2, gradient_stride, a.padded_rows, t.n * LOSS_TILE, 0);
+        a_step = BK * a.weight_stride, b_step = 2 * BK;
+        A.set(a.weight + (a.first + (int64_t)begin * BK) * a.weight_stride, a.weight_stride, t.m * LOSS_TILE, 0, a.width);
+        B.set(a.gradient + ((int64_t)t.n * pieces + begin / 4) * G_TILE + begin % 4 * (2 * BK), 2 * LOSS_TILE, 0, LOSS_TILE, 0);
     } else {
         steps = (live + BK - 1) / BK;
-        a_step = (int64_t)BK * a.pitch * 2, b_step = BK * gradient_stride;
-        A.set(a.scaled, (int64_t)a.pitch * 2, 0, t.m * LOSS_TILE, a.pitch);
-        B.set(a.gradient, gradient_stride, 0, t.n * LOSS_TILE, (int64_t)pieces * LOSS_TILE);
+        a_step = (int64_t)widths * TILE_BYTES;
+        A.set(a.scaled + (int64_t)t.m * TILE_BYTES, 2 * LOSS_TILE, 0, 0, LOSS_TILE);
+        B.set(a.gradient + t.n * G_TILE, 2 * LOSS_TILE, 0, 0, LOSS_TILE);
     }
+    Places<A_ACROSS, 4> pa;
+    Places<B_ACROSS, 2> pb;
+    pa.set(wm * 128), pb.set(wn * 64);
 
     f32x16 acc[4][2];
 #pragma unroll
@@ -144,26 +165,51 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
         if (KIND != KIND_D_WEIGHT && s == steps - 1 && end_left < BK) A.load_end(x, end_left, a.weight_stride);
         else A.load(x);
         B.load(y);
-        A.step(a_step), B.step(b_step);
+        A.step(a_step);
+        // four steps are a tile of gradients
+        if constexpr (SCORES) B.step(b_step);
+        else if constexpr (KIND == KIND_D_HIDDEN) B.step(((begin + s) & 3) == 3 ? G_TILE - 6 * BK : 2 * BK);
+        else B.step((s & 3) == 3 ? pieces * G_TILE - 3 * TILE_BYTES : TILE_BYTES);
     };
-    if (steps > 0) bring(0);
-    for (int s = 0; s < steps; ++s) {
-        wait_loads<0>();
-        lds_barrier();
-        if (s + 1 < steps) bring(s + 1);
+    i32x4 p[2][4], q[2][2];
+    const auto read = [&](int s, int k) {
         const char *x = lds[s & 1][0], *y = lds[s & 1][1];
 #pragma unroll
-        for (int k = 0; k < BK / 16; ++k) {
-            i32x4 p[4], q[2];
+        for (int i = 0; i < 4; ++i) p[k & 1][i] = pa.read(x, i, k);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = operand<A_ACROSS>(x, wm * 128 + 32 * i, k);
+        for (int j = 0; j < 2; ++j) q[k & 1][j] = pb.read(y, j, k);
+    };
+    const auto multiply = [&](int k) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) q[j] = operand<B_ACROSS>(y, wn * 64 + 32 * j, k);
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = mfma32<DT>(p[i], q[j], acc[i][j]);
+            for (int j = 0; j < 2; ++j) acc[i][j] = mfma32<DT>(p[k & 1][i], q[k & 1][j], acc[i][j]);
+    };
+    // Operands are read a quarter of a step before they are multiplied, those of the next step's first quarter too: its tiles have come when
+    // the last quarter's operands are in registers, and the tiles of the step after may then take this one's place.
+    if (steps > 0) {
+        bring(0);
+        if (steps > 1) {
+            bring(1);
+            wait_loads<8>();
+        } else wait_loads<0>();
+        lds_barrier();
+        read(0, 0);
+    }
+    for (int s = 0; s < steps; ++s) {
+        read(s, 1);
+        multiply(0);
+        read(s, 2);
+        multiply(1);
+        read(s, 3);
+        multiply(2);
+        if (s + 1 < steps) {
+            wait_loads<0>();
+            lds_barrier();
+            if (s + 2 < steps) bring(s + 2);
+            read(s + 1, 0);
         }
+        multiply(3);
     }
 
     // a lane's results: column n = 64 wn + 32 j + lane % 32, rows m = 128 wm + 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4
@@ -174,18 +220,30 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
             const int row = n0 + 32 * j;
             const bool there = row < live;
             const int target = there ? a.row[row].target - (int)a.first - m0 : -1;  // place in the piece, from the lane's first
-            float most = -INFINITY, own = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i][j] *= a.scale;
+            if (__any(target >= 0 && target < 128)) {  // the target's score is kept apart
+                float own = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const bool is = 32 * i + 8 * (r / 4) + r % 4 == target;
+                        own = is ? acc[i][j][r] : own;
+                        acc[i][j][r] = is ? -INFINITY : acc[i][j][r];
+                    }
+                if (target >= 0 && target < 128 && !(target & 4) && m0 + target < a.piece) a.own[row] = own;
+            }
+            if (t.m == pieces - 1)  // entries past the end
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] = m0 + 32 * i + 8 * (r / 4) + r % 4 < a.piece ? acc[i][j][r] : -INFINITY;
+            float most = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int m = 32 * i + 8 * (r / 4) + r % 4;
-                    const float s = acc[i][j][r] * a.scale;
-                    own = m == target ? s : own;
-                    acc[i][j][r] = m0 + m < a.piece ? s : -INFINITY;
-                    most = fmaxf(most, acc[i][j][r]);
-                }
-            if (target >= 0 && target < 128 && !(target & 4) && m0 + target < a.piece) a.own[row] = own;
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[i][j][r]);
             most = max_halves(most);
             const float base = most == -INFINITY ? 0.0f : most;
             float sum = 0.0f;
@@ -213,7 +271,7 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
                     for (int r = 0; r < 16; ++r) own = 32 * i + 8 * (r / 4) + r % 4 == target ? acc[i][j][r] : own;
                 own = expm1f(own * a.scale - x.top - x.log_total);
             }
-            char *out = a.gradient + row * gradient_stride + m0 * 2;
+            char *out = a.gradient + ((int64_t)t.n * pieces + t.m) * G_TILE + ((row & 255) * LOSS_TILE + (m0 & 255)) * 2;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll

@@ -59,21 +59,24 @@ struct LossArgs {
     int32_t *state;                    // [0] rows that have a target, [1] the largest exponent among them
     int32_t *list;                     // [rows] which these are
     LossRow *row;                      // [padded_rows]
-    char *packed, *scaled;             // [padded_rows][pitch] states, and those times 2^(exponent - largest)
-    float2 *part;                      // [parts][padded_rows] maximum and sum of exponentials over parts of the vocabulary
+    char *packed;                      // [rows / 256][pitch / 64][256][64] states
+    char *scaled;                      // [rows / 64][columns / 256][64][256] the same times 2^(exponent - largest)
+    float2 *part;                      // [parts][padded_rows] maximum and sum of exponentials over parts of the vocabulary, without the target
     float2 *running;                   // [padded_rows] over all parts before
     float *own;                        // [padded_rows] score of the target
-    char *gradient;                    // [padded_rows][piece] of the scores, over a piece of the vocabulary
+    char *gradient;                    // [rows / 256][piece / 256][256][256] of the scores, over a piece of the vocabulary
     float *d_part;                     // [splits][padded_rows][columns] sums of d_hidden
     int32_t columns;                   // width rounded up to LOSS_TILE
-    int32_t splits;
+    int32_t splits, hidden_steps;      // most parts of d_hidden's axis, steps of a whole piece
     int64_t first;                     // the piece's first entry, and how many there are
     int32_t piece, last;               // last: no piece comes after this one
 };
 #define LOSS_TILE 256
 #define LOSS_STEP 64
 #define LOSS_PART 128
+#define LOSS_PART_STEPS 24
 #define LOSS_FEW 64
+#define LOSS_FEW_THREADS 256
 void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool backward);
 void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int blocks);
 void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool packed);
@@ -83,6 +86,19 @@ void plaid_launch_loss_d_hidden(hipStream_t st, const LossArgs &a, int dtype);
 void plaid_launch_loss_d_hidden_join(hipStream_t st, const LossArgs &a, int dtype);
 
 #ifdef __HIP__
+// Parts that the vocabulary's axis of d_hidden is cut into, of at most `most`: as few as leave least of the chip idle in the last round of
+// `tiles` times as many workgroups; a part costs what LOSS_PART_STEPS steps of it cost, as its sums are read and written.
+__device__ __forceinline__ int hidden_splits(int tiles, int steps, int most)
+{
+    int best = 1;
+    float least = 0.0f;
+    for (int s = 1; s <= most; ++s) {
+        const float cost = (float)((tiles * s + 255) / 256) * ((float)steps / (float)s + LOSS_PART_STEPS);
+        if (s == 1 || cost < 0.98f * least) best = s, least = cost;
+    }
+    return best;
+}
+
 // Sixteen bytes of a row that starts at any element: the memory system takes such addresses.
 typedef i32x4 __attribute__((aligned(2))) i32x4_any;
 

@@ -69,7 +69,7 @@ struct LossPlan {
     bool few;
     int blocks, splits;
     int64_t padded_rows, pitch, columns, piece;
-    int64_t list_bytes, row_bytes, packed_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, d_part_bytes, bytes;
+    int64_t list_bytes, row_bytes, packed_bytes, scaled_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, d_part_bytes, bytes;
 };
 LossPlan plan_loss(const plaid_token_loss &a, bool backward)
 {
@@ -77,8 +77,8 @@ LossPlan plan_loss(const plaid_token_loss &a, bool backward)
     p.few = !backward && a.rows <= LOSS_FEW;
     if (p.few) {
         p.padded_rows = a.rows;
-        p.blocks = a.vocabulary >= 64 * 4 * 2048 ? 4 : 1;
-        p.part_bytes = round16(ceil_div(a.vocabulary, 16 * p.blocks) * p.padded_rows * 8);
+        p.blocks = a.vocabulary >= 128 * 512 ? 2 : 1;
+        p.part_bytes = round16(ceil_div(a.vocabulary, 64 * p.blocks) * p.padded_rows * 8);
         p.own_bytes = round16(p.padded_rows * 4);
         p.bytes = p.part_bytes + p.own_bytes;
         return p;
@@ -97,10 +97,13 @@ LossPlan plan_loss(const plaid_token_loss &a, bool backward)
     p.piece = ceil_div(ceil_div(a.vocabulary, pieces), LOSS_TILE) * LOSS_TILE;
     if (backward) {
         p.gradient_bytes = p.padded_rows * p.piece * 2;
-        const int64_t tiles = p.columns / LOSS_TILE * (p.padded_rows / LOSS_TILE), most = ceil_div(p.piece, 4 * LOSS_STEP);
-        p.splits = (int)(256 / tiles < 1 ? 1 : 256 / tiles < most ? 256 / tiles : most);
+        // at most so many parts of d_hidden's axis (the kernel knows how many rows have a target, and takes fewer where they are better)
+        const int64_t tiles = p.columns / LOSS_TILE * (p.padded_rows / LOSS_TILE), steps = ceil_div(p.piece, LOSS_STEP), want = ceil_div(4 * 256, tiles);
+        p.splits = (int)(want > 32 ? 32 : want);
+        if (p.splits > ceil_div(steps, 4)) p.splits = (int)ceil_div(steps, 4);
+        p.scaled_bytes = p.padded_rows * p.columns * 2;
         p.d_part_bytes = p.splits * p.padded_rows * p.columns * 4;
-        p.bytes = p.list_bytes + p.row_bytes + 2 * p.packed_bytes + p.gradient_bytes + p.d_part_bytes;
+        p.bytes = p.list_bytes + p.row_bytes + p.packed_bytes + p.scaled_bytes + p.gradient_bytes + p.d_part_bytes;
     } else {
         p.part_bytes = p.piece / LOSS_PART * p.padded_rows * 8;
         p.running_bytes = p.padded_rows * 8;
@@ -144,14 +147,14 @@ LossArgs loss_args(const plaid_token_loss &a, const LossPlan &p, void *workspace
     x.loss = a.loss, x.lse = a.lse;
     x.rows = a.rows, x.vocabulary = a.vocabulary, x.hidden_stride = 2 * a.hidden_stride, x.weight_stride = 2 * a.weight_stride;
     x.width = a.width, x.scale = a.scale;
-    x.padded_rows = (int32_t)p.padded_rows, x.pitch = (int32_t)p.pitch, x.columns = (int32_t)p.columns, x.splits = p.splits;
+    x.padded_rows = (int32_t)p.padded_rows, x.pitch = (int32_t)p.pitch, x.columns = (int32_t)p.columns, x.splits = p.splits, x.hidden_steps = (int32_t)ceil_div(p.piece, LOSS_STEP);
     char *w = (char *)workspace;
     if (!p.few) {
         x.state = (int32_t *)w, x.list = (int32_t *)(w + 16), w += p.list_bytes;
         x.row = (LossRow *)w, w += p.row_bytes;
         x.packed = w, w += p.packed_bytes;
         if (backward) {
-            x.scaled = w, w += p.packed_bytes;
+            x.scaled = w, w += p.scaled_bytes;
             x.gradient = w, w += p.gradient_bytes;
             x.d_part = (float *)w;
         }
@@ -307,7 +310,7 @@ extern "C" int plaid_cross_entropy(const plaid_token_loss *args, void *workspace
     if (p.few) {
         x.last = 1;
         plaid_launch_loss_few(st, x, args->dtype, p.blocks);
-        plaid_launch_loss_join(st, x, (int)ceil_div(x.vocabulary, 16 * p.blocks), false);
+        plaid_launch_loss_join(st, x, (int)ceil_div(x.vocabulary, 64 * p.blocks), false);
         return launched();
     }
     plaid_launch_loss_pack(st, x, args->dtype, false);
