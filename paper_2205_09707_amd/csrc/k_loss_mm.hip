@@ -1,4 +1,6 @@
 // Cross entropy over a vocabulary: the products.
+#include <type_traits>
+
 #include "train.h"
 
 // Three products, each of tiles of 256 x 256 over an axis k taken 64 at a time:
@@ -37,24 +39,15 @@ struct Operand {
             }
         }
     }
-    __device__ __forceinline__ void load(char *tile) const
-    {
-        const int wave = uniform((int)(threadIdx.x >> 6));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load_to_lds(at[i], tile + (wave * 4 + i) * 1024);
-    }
+    __device__ __forceinline__ void load(int i, uint32_t tile) const { load_to_lds(at[i], tile + i * 1024); }
     // The last step of an axis that ends inside it: `left` of the 64 are there.  Along: zeros for the others.  Across: the last one again
     // (the other operand has zeros there).
-    __device__ __forceinline__ void load_end(char *tile, int left, int64_t stride) const
+    __device__ __forceinline__ void load_end(int i, uint32_t tile, int left, int64_t stride) const
     {
-        const int wave = uniform((int)(threadIdx.x >> 6));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const char *p = at[i];
-            if constexpr (!ACROSS) p = k[i] < left ? p : (const char *)zero_row;
-            else p = k[i] < left ? p : p - (k[i] - (left - 1)) * stride;
-            load_to_lds(p, tile + (wave * 4 + i) * 1024);
-        }
+        const char *p = at[i];
+        if constexpr (!ACROSS) p = k[i] < left ? p : (const char *)zero_row;
+        else p = k[i] < left ? p : p - (k[i] - (left - 1)) * stride;
+        load_to_lds(p, tile + i * 1024);
     }
     __device__ __forceinline__ void step(int64_t bytes)
     {
@@ -160,11 +153,15 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
 #pragma unroll
         for (int j = 0; j < 2; ++j) acc[i][j] = zero16();
 
-    const auto bring = [&](int s) {
-        char *x = lds[s & 1][0], *y = lds[s & 1][1];
-        if (KIND != KIND_D_WEIGHT && s == steps - 1 && end_left < BK) A.load_end(x, end_left, a.weight_stride);
-        else A.load(x);
-        B.load(y);
+    // A step's loads, of which the first four are A's; a wave's go to its own 4 KB of both tiles.
+    const uint32_t mine = lds_address(lds) + wave * 4096;
+    const auto bring = [&](int s, int i, bool last) {
+        const uint32_t x = mine + (s & 1) * (2 * TILE_BYTES);
+        if (i >= 4) B.load(i - 4, x + TILE_BYTES);
+        else if (KIND != KIND_D_WEIGHT && last && end_left < BK) A.load_end(i, x, end_left, a.weight_stride);
+        else A.load(i, x);
+    };
+    const auto advance = [&](int s) {
         A.step(a_step);
         // four steps are a tile of gradients
         if constexpr (SCORES) B.step(b_step);
@@ -175,41 +172,62 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
     const auto read = [&](int s, int k) {
         const char *x = lds[s & 1][0], *y = lds[s & 1][1];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[k & 1][i] = pa.read(x, i, k);
-#pragma unroll
         for (int j = 0; j < 2; ++j) q[k & 1][j] = pb.read(y, j, k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[k & 1][i] = pa.read(x, i, k);
     };
-    const auto multiply = [&](int k) {
+    const auto multiply = [&](int k, int i, int j) { acc[i][j] = mfma32<DT>(p[k & 1][i], q[k & 1][j], acc[i][j]); };
+    // A quarter's products, with the next quarter's operands read among them.
+    const auto quarter = [&](int s, int k) {
+        constexpr int READS = (A_ACROSS ? 8 : 4) + (B_ACROSS ? 4 : 2);
+        read(s, k + 1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = mfma32<DT>(p[k & 1][i], q[k & 1][j], acc[i][j]);
+        for (int i = 0; i < 8; ++i) multiply(k, i >> 1, i & 1);
+        // the order: one or two reads before each of the first six products
+#define PAIR(I) __builtin_amdgcn_sched_group_barrier(0x100, READS / 6 + (I < READS % 6), 0), __builtin_amdgcn_sched_group_barrier(0x008, 1, 0)
+        PAIR(0), PAIR(1), PAIR(2), PAIR(3), PAIR(4), PAIR(5);
+#undef PAIR
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        __builtin_amdgcn_sched_barrier(0);
     };
     // Operands are read a quarter of a step before they are multiplied, those of the next step's first quarter too: its tiles have come when
-    // the last quarter's operands are in registers, and the tiles of the step after may then take this one's place.
+    // the last quarter's operands are in registers, and the tiles of the step after may then take this one's place.  The last steps stand apart,
+    // so that the others have no branches.
+    const auto step = [&](int s, auto stands) {
+        constexpr int AFTER = decltype(stands)::value;  // steps that come after this one, 3: more than two
+        quarter(s, 0);
+        quarter(s, 1);
+        quarter(s, 2);
+        if constexpr (AFTER > 0) {
+            wait_loads<0>();
+            lds_barrier();
+            read(s + 1, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            multiply(3, i >> 1, i & 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (AFTER > 1) bring(s + 2, i, AFTER == 2);
+        }
+        if constexpr (AFTER > 2) advance(s + 2);
+    };
     if (steps > 0) {
-        bring(0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bring(0, i, steps == 1);
+        advance(0);
         if (steps > 1) {
-            bring(1);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) bring(1, i, steps == 2);
+            advance(1);
             wait_loads<8>();
         } else wait_loads<0>();
         lds_barrier();
         read(0, 0);
-    }
-    for (int s = 0; s < steps; ++s) {
-        read(s, 1);
-        multiply(0);
-        read(s, 2);
-        multiply(1);
-        read(s, 3);
-        multiply(2);
-        if (s + 1 < steps) {
-            wait_loads<0>();
-            lds_barrier();
-            if (s + 2 < steps) bring(s + 2);
-            read(s + 1, 0);
-        }
-        multiply(3);
+        for (int s = 0; s < steps - 3; ++s) step(s, std::integral_constant<int, 3>());
+        if (steps > 2) step(steps - 3, std::integral_constant<int, 2>());
+        if (steps > 1) step(steps - 2, std::integral_constant<int, 1>());
+        step(steps - 1, std::integral_constant<int, 0>());
     }
 
     // a lane's results: column n = 64 wn + 32 j + lane % 32, rows m = 128 wm + 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4
