@@ -268,31 +268,36 @@ void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool p
 }
 
 // --- gradient of the states: the splits' sums added up, in order ------------------------------------------------------------------
+// The sums lie in tiles of 256 rows and columns, in the order in which the products' registers hold them: for a wave of 128 columns and 64 rows
+// [32 rows' half][32 columns' quarter][8 columns' quarter][lane][4 columns], a lane being a row and a half of the 8 columns.  A workgroup has
+// 32 rows of a tile, each of its waves 8 columns.
 template <int DT>
-__global__ __launch_bounds__(128) void loss_d_hidden_join_kernel(LossArgs a)
+__global__ __launch_bounds__(256) void loss_d_hidden_join_kernel(LossArgs a)
 {
-    const int i = blockIdx.x;
-    if (i >= uniform_load(a.state)) return;
-    const int64_t t = uniform_load(a.list + i);
-    const int e = uniform_load(&a.row[i].exponent);
-    const int splits = hidden_splits((uniform_load(a.state) + LOSS_TILE - 1) / LOSS_TILE * (a.columns / LOSS_TILE), a.hidden_steps, a.splits);
+    const int live = uniform_load(a.state), row_tiles = (live + LOSS_TILE - 1) / LOSS_TILE, widths = a.columns / LOSS_TILE;
+    const int block = blockIdx.x & 7, k = blockIdx.x >> 3 & 7, tile = blockIdx.x >> 6, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row = tile / widths * LOSS_TILE + block * 32 + (lane & 31);
+    if (tile / widths * LOSS_TILE + block * 32 >= live) return;
+    const int splits = hidden_splits(row_tiles * widths, a.hidden_steps, a.splits);
+    const int64_t part = (int64_t)(a.padded_rows / LOSS_TILE) * widths * (LOSS_TILE * LOSS_TILE);
+    const bool there = row < live;
+    const int64_t t = there ? a.list[row] : 0;
+    const int e = there ? a.row[row].exponent : 0;
     // the power of two last, where the result may leave the normal range
     const float factor = a.scale * (DT == PLAID_FP16 ? 0x1p-15f : 1.0f);
-    for (int at = threadIdx.x * 8; at < a.width; at += 1024) {
-        Eight v = {};
-        for (int s = 0; s < splits; ++s) {
-            const float *p = a.d_part + ((int64_t)s * a.padded_rows + i) * a.columns + at;
-            const f32x4 x = *(const f32x4 *)p, y = *(const f32x4 *)(p + 4);
+    // wave w of these four: eight of columns 64 w .. 64 w + 63, two quarters of 32
+    const int i = (wave & 1) * 2 + k / 4, c = k % 4, column = tile % widths * LOSS_TILE + wave * 64 + k * 8 + 4 * (lane >> 5);
+    const float *p = a.d_part + (int64_t)tile * (LOSS_TILE * LOSS_TILE) + ((wave >> 1) * 4 + block / 2) * 8192 + (((block & 1) * 4 + i) * 4 + c) * 256 + lane * 4;
+    f32x4 v = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) v += *(const f32x4 *)(p + s * part);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v.x[j] += x[j], v.x[4 + j] += y[j];
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v.x[j] = ldexpf(v.x[j] * factor, e == NO_EXPONENT ? 0 : e);
-        *(i32x4 *)(a.d_hidden + (t * a.width + at) * 2) = pack8<DT>(v);
-    }
+    for (int j = 0; j < 4; ++j) v[j] = ldexpf(v[j] * factor, e == NO_EXPONENT ? 0 : e);
+    if (there && column < a.width) *(i32x2 *)(a.d_hidden + (t * a.width + column) * 2) = i32x2{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
 }
 void plaid_launch_loss_d_hidden_join(hipStream_t st, const LossArgs &a, int dtype)
 {
-    if (dtype == PLAID_BF16) loss_d_hidden_join_kernel<PLAID_BF16><<<(unsigned)a.rows, 128, 0, st>>>(a);
-    else loss_d_hidden_join_kernel<PLAID_FP16><<<(unsigned)a.rows, 128, 0, st>>>(a);
+    const unsigned grid = (unsigned)(a.padded_rows / LOSS_TILE * (a.columns / LOSS_TILE) * 64);
+    if (dtype == PLAID_BF16) loss_d_hidden_join_kernel<PLAID_BF16><<<grid, 256, 0, st>>>(a);
+    else loss_d_hidden_join_kernel<PLAID_FP16><<<grid, 256, 0, st>>>(a);
 }

@@ -65,7 +65,7 @@ struct LossArgs {
     float2 *running;                   // [padded_rows] over all parts before
     float *own;                        // [padded_rows] score of the target
     char *gradient;                    // [rows / 256][piece / 256][256][256] of the scores, over a piece of the vocabulary
-    float *d_part;                     // [splits][padded_rows][columns] sums of d_hidden
+    float *d_part;                     // [splits][rows / 256][columns / 256][256 x 256] sums of d_hidden, in the order of the products' registers
     int32_t columns;                   // width rounded up to LOSS_TILE
     int32_t splits, hidden_steps;      // most parts of d_hidden's axis, steps of a whole piece
     int64_t first;                     // the piece's first entry, and how many there are
@@ -74,7 +74,7 @@ struct LossArgs {
 #define LOSS_TILE 256
 #define LOSS_STEP 64
 #define LOSS_PART 128
-#define LOSS_PART_STEPS 24
+#define LOSS_PART_STEPS 12
 #define LOSS_FEW 64
 #define LOSS_FEW_THREADS 256
 void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool backward);

@@ -90,7 +90,7 @@ LossPlan plan_loss(const plaid_token_loss &a, bool backward)
     p.row_bytes = round16(p.padded_rows * (int64_t)sizeof(LossRow));
     p.packed_bytes = p.padded_rows * p.pitch * 2;
     // pieces of the vocabulary whose statistics (forward) or gradients of the scores (backward) take so much of the workspace, all of a size
-    const int64_t room = backward ? (256ll << 20) / (p.padded_rows * 2) : (64ll << 20) / (p.padded_rows * 8) * LOSS_PART;
+    const int64_t room = backward ? (512ll << 20) / (p.padded_rows * 2) : (64ll << 20) / (p.padded_rows * 8) * LOSS_PART;
     int64_t piece = room / LOSS_TILE * LOSS_TILE;
     if (piece < LOSS_TILE) piece = LOSS_TILE;
     const int64_t pieces = ceil_div(a.vocabulary, piece);
