@@ -30,6 +30,7 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs e, int team_shift)
     }
 }
 
+#define FILL_EACH 4  // pieces of 16 bytes that a thread fills
 // --- the tokens in ascending order, equal ones in the order in which they stood -------------------------------------------------
 // A radix sort from the lowest digit on.  Each wave has a stretch of places and goes through it 64 at a time: lanes with the same digit find
 // each other by votes, so that every place's rank is counted in order and none depends on which atomic came first.
@@ -55,10 +56,23 @@ __device__ __forceinline__ int rank_digit(int digit, bool there, int bits, volat
     return base + before;
 }
 
-// Up to SORT_ONE tokens: one workgroup, everything in LDS.
-__global__ __launch_bounds__(1024) void sort_one_kernel(EmbedArgs e)
+// Up to SORT_ONE tokens: one workgroup, everything in LDS.  The others fill the gradient with zeros meanwhile, rows with a token too: there
+// are few of them.
+__global__ __launch_bounds__(1024) void sort_one_kernel(EmbedArgs e, int64_t pieces)
 {
     constexpr int WAVES = 16, EACH = SORT_ONE / 1024;
+    if (blockIdx.x > 0) {
+        const i32x4 zero = {0, 0, 0, 0};
+        const int64_t first = (int64_t)(blockIdx.x - 1) * (1024 * FILL_EACH) + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < FILL_EACH; ++i)
+            if (first + i * 1024 < pieces) *(i32x4_any *)(e.d_table + (first + i * 1024) * 16) = zero;
+        // what is left of a whole number of pieces
+        const int64_t rest = pieces * 8 + threadIdx.x;
+        if (blockIdx.x == 1 && rest < e.vocabulary * e.width) *(uint16_t *)(e.d_table + 2 * rest) = 0;
+        return;
+    }
+    if (threadIdx.x == 0) *e.shared = 0;
     __shared__ int keys[SORT_ONE], counts[WAVES][256], totals[256];
     __shared__ uint16_t places[SORT_ONE];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)e.n;
@@ -138,6 +152,7 @@ __global__ __launch_bounds__(256) void sort_scan_kernel(EmbedArgs e, int tiles)
 {
     __shared__ int wave_sum[4];
     int *c = e.counts + (int64_t)blockIdx.x * tiles;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *e.shared = 0;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int before = 0;
     for (int first = 0; first < tiles; first += 256) {
@@ -212,8 +227,8 @@ __global__ __launch_bounds__(256) void sort_place_kernel(EmbedArgs e, int pass, 
 // --- sums -----------------------------------------------------------------------------------------------------------------------
 // dE[v] = scale times the sum of d_out over the places of token v, in order, held in 32 bits.  The sorted places are cut into chunks, a
 // team of threads each, so that a token that stands everywhere is no one's burden.  What a chunk has of a token that it shares with its
-// neighbours goes to the workspace: [0] of a token that the chunk before has too, [1] of one that begins here and goes on; the second
-// launch adds these up, in order, where the token begins.
+// neighbours goes to the workspace: [0] of a token that the chunk before has too, [1] of one that begins here and goes on.  Such beginnings are
+// put on a list, in whatever order, and the second launch adds up each one's parts, in theirs.
 template <int DT>
 __device__ __forceinline__ void write_row(const EmbedArgs &e, int key, int at, const Eight &sum)
 {
@@ -231,33 +246,51 @@ __device__ __forceinline__ void write_part(const EmbedArgs &e, int64_t chunk, in
     *(f32x4 *)(p + 4) = f32x4{sum.x[4], sum.x[5], sum.x[6], sum.x[7]};
 }
 
-template <int DT>
-__global__ __launch_bounds__(256) void embed_grad_kernel(EmbedArgs e, int team_shift)
+// WIDE: a team is whole waves, whose lanes bring 64 tokens and places at a time; a place is then the same for all lanes.
+template <int DT, bool WIDE>
+__device__ __forceinline__ void add_chunk(const EmbedArgs &e, int team_shift, int64_t block, int slice)
 {
     constexpr int AHEAD = 8;
     const int lane = threadIdx.x & ((1 << team_shift) - 1), teams = 256 >> team_shift;
-    const int at = (blockIdx.y * 256 + lane) * 8;
-    const int64_t chunk = (int64_t)blockIdx.x * teams + (threadIdx.x >> team_shift), begin = chunk * e.chunk, end = min(begin + e.chunk, e.n);
-    if (begin >= e.n || at >= e.width) return;
+    const int at = (slice * 256 + lane) * 8, wave_lane = threadIdx.x & 63;
+    int64_t chunk = block * teams + (threadIdx.x >> team_shift);
+    if (WIDE) chunk = uniform(chunk);
+    const int64_t begin = chunk * e.chunk, end = min(begin + e.chunk, e.n);
+    if (begin >= e.n || (!WIDE && at >= e.width)) return;
+    const bool there = at < e.width;
     const int *keys = e.keys[e.sorted], *places = e.places[e.sorted];
     int key = keys[begin];
     bool shared = begin > 0 && keys[begin - 1] == key;  // with the chunk before
+    if (WIDE) key = uniform(key), shared = uniform((int)shared);
     Eight sum = {};
+    int many_keys = 0, many_places = 0;
     for (int64_t i = begin; i < end; i += AHEAD) {
         i32x4 w[AHEAD];
         int next[AHEAD];
+        if (WIDE && ((i - begin) & 63) == 0) {
+            const int64_t p = min(i + wave_lane, end - 1);
+            many_keys = keys[p], many_places = places[p];
+        }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            const int64_t p = min(i + k, end - 1);
-            next[k] = keys[p];
-            w[k] = next[k] < e.vocabulary ? load_piece(e.d_out + places[p] * e.d_out_stride, at, e.width) : i32x4{0, 0, 0, 0};
+            int place;
+            if (WIDE) {
+                const int from = (int)((i - begin) & 63) + k;
+                next[k] = __builtin_amdgcn_readlane(many_keys, from), place = __builtin_amdgcn_readlane(many_places, from);
+            } else {
+                const int64_t p = min(i + k, end - 1);
+                next[k] = keys[p], place = places[p];
+            }
+            w[k] = next[k] < e.vocabulary ? load_piece(e.d_out + place * e.d_out_stride, at, e.width) : i32x4{0, 0, 0, 0};
         }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
             if (i + k < end) {
                 if (next[k] != key) {
-                    if (shared) write_part(e, chunk, 0, at, sum);
-                    else write_row<DT>(e, key, at, sum);
+                    if (there) {
+                        if (shared) write_part(e, chunk, 0, at, sum);
+                        else write_row<DT>(e, key, at, sum);
+                    }
                     key = next[k], shared = false;
                     sum = Eight{};
                 }
@@ -266,53 +299,19 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedArgs e, int team_s
                 for (int j = 0; j < 8; ++j) sum.x[j] += v.x[j];
             }
     }
-    if (key >= e.vocabulary) return;  // what has no token is last
+    if (key >= e.vocabulary || !there) return;  // what has no token is last
     if (shared) write_part(e, chunk, 0, at, sum);
-    else if (end < e.n && keys[end] == key) write_part(e, chunk, 1, at, sum);
-    else write_row<DT>(e, key, at, sum);
-}
-
-template <int DT>
-__global__ __launch_bounds__(256) void embed_grad_join_kernel(EmbedArgs e, int team_shift)
-{
-    constexpr int AHEAD = 8;
-    const int lane = threadIdx.x & ((1 << team_shift) - 1), teams = 256 >> team_shift;
-    const int at = (blockIdx.y * 256 + lane) * 8;
-    const int64_t chunk = (int64_t)blockIdx.x * teams + (threadIdx.x >> team_shift), begin = chunk * e.chunk, end = begin + e.chunk;
-    if (end >= e.n || at >= e.width) return;
-    const int *keys = e.keys[e.sorted];
-    const int key = keys[end - 1];
-    if (key >= e.vocabulary || keys[end] != key) return;                              // nothing goes on
-    if (keys[begin] == key && begin > 0 && keys[begin - 1] == key) return;            // it began before
-    const float *p = e.part + (chunk * 2 + 1) * (int64_t)e.columns() + at;
-    Eight sum;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum.x[j] = p[j];
-    for (int64_t c = chunk + 1;; c += AHEAD) {
-        bool same[AHEAD];
-        f32x4 w[AHEAD][2];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            same[k] = (c + k) * e.chunk < e.n && keys[min((c + k) * e.chunk, e.n - 1)] == key;
-            const float *q = e.part + (c + k) * 2 * (int64_t)e.columns() + at;
-            w[k][0] = w[k][1] = f32x4{0, 0, 0, 0};
-            if (same[k]) w[k][0] = *(const f32x4 *)q, w[k][1] = *(const f32x4 *)(q + 4);
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (same[k])
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sum.x[j] += w[k][j / 4][j % 4];
-        if (!same[AHEAD - 1]) break;
-    }
-    write_row<DT>(e, key, at, sum);
+    else if (end < e.n && keys[end] == key) {
+        write_part(e, chunk, 1, at, sum);
+        if (lane == 0 && slice == 0) e.begins[atomicAdd(e.shared, 1)] = (int32_t)chunk;
+    } else write_row<DT>(e, key, at, sum);
 }
 
 // Zeros for the rows of tokens that are not there: a wave looks 64 of them up in the sorted list, a lane each.
-__global__ __launch_bounds__(256) void embed_zero_kernel(EmbedArgs e)
+__device__ __forceinline__ void fill_absent(const EmbedArgs &e, int64_t block)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t first = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64, mine = first + lane;
+    const int64_t first = (block * 4 + (threadIdx.x >> 6)) * 64, mine = first + lane;
     if (first >= e.vocabulary) return;
     const int *keys = e.keys[e.sorted];
     int64_t lo = 0, hi = e.n;  // the first place whose token is not below mine
@@ -327,6 +326,52 @@ __global__ __launch_bounds__(256) void embed_zero_kernel(EmbedArgs e)
         absent &= absent - 1;
         char *row = e.d_table + (first + r) * e.width * 2;
         for (int at = lane * 8; at < e.width; at += 512) store_piece(row, at, e.width, i32x4{0, 0, 0, 0});
+    }
+}
+
+// Chunks first, then rows without a token.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void embed_grad_kernel(EmbedArgs e, int team_shift, unsigned chunk_blocks, unsigned slices)
+{
+    if (blockIdx.x < chunk_blocks) add_chunk<DT, WIDE>(e, team_shift, blockIdx.x / slices, blockIdx.x % slices);
+    else fill_absent(e, blockIdx.x - chunk_blocks);
+}
+
+// 256 columns of a token that several chunks share: each of the four waves has a quarter of its parts.
+template <int DT>
+__global__ __launch_bounds__(256) void embed_grad_join_kernel(EmbedArgs e)
+{
+    __shared__ f32x4 lds[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = (blockIdx.y * 64 + lane) * 4, many = *e.shared;
+    const int *keys = e.keys[e.sorted];
+    const int64_t columns = e.columns();
+    for (int i = blockIdx.x; i < many; i += gridDim.x) {
+        const int64_t chunk = e.begins[i];
+        const int key = keys[chunk * e.chunk + e.chunk - 1];
+        int parts = 1;  // this chunk's, and of as many chunks as begin with the token
+        for (int more = 64; more == 64; parts += more) {
+            const int64_t p = (chunk + parts + lane) * e.chunk;
+            const uint64_t same = __ballot(p < e.n && keys[min(p, e.n - 1)] == key);
+            more = same == ~0ull ? 64 : __ffsll((unsigned long long)~same) - 1;
+        }
+        const int each = (parts + 3) / 4, first = wave * each, last = min(parts, first + each);
+        f32x4 sum = {0, 0, 0, 0};
+        if (at < columns) {
+            const float *p = e.part + chunk * 2 * columns + at;  // part 0 has place 1 of its chunk, the others place 0
+#pragma unroll 8
+            for (int k = first; k < last; ++k) sum += *(const f32x4 *)(p + (k == 0 ? 1 : 2 * k) * columns);
+        }
+        lds[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && at < e.width) {
+#pragma unroll
+            for (int w = 1; w < 4; ++w) sum += lds[w][lane];
+            char *row = e.d_table + ((int64_t)key * e.width + at) * 2;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (at + j < e.width) store16<DT>(row + 2 * j, e.add ? load16<DT>(row + 2 * j) + sum[j] * e.scale : sum[j] * e.scale);
+        }
+        __syncthreads();
     }
 }
 
@@ -352,23 +397,26 @@ void plaid_launch_embedding(hipStream_t st, const EmbedArgs &e, int dtype)
 template <int DT>
 static void launch_backward(hipStream_t st, const EmbedArgs &e)
 {
-    if (e.n > 0) {
-        if (e.n <= SORT_ONE) sort_one_kernel<<<1, 1024, 0, st>>>(e);
-        else
-            for (int pass = 0; pass < e.passes; ++pass) {
-                const int tiles = (int)((e.n + SORT_TILE - 1) / SORT_TILE);
-                sort_count_kernel<<<tiles, 256, 0, st>>>(e, pass, tiles);
-                sort_scan_kernel<<<1 << e.digit, 256, 0, st>>>(e, tiles);
-                sort_place_kernel<<<tiles, 256, 0, st>>>(e, pass, tiles);
-            }
-    }
-    if (!e.add) embed_zero_kernel<<<(unsigned)((e.vocabulary + 255) / 256), 256, 0, st>>>(e);
+    const bool one = e.n <= SORT_ONE, fill = one && !e.add;
+    if (one) {
+        const int64_t pieces = fill ? e.vocabulary * e.width / 8 : 0;
+        const int64_t blocks = fill ? (pieces + 1024 * FILL_EACH - 1) / (1024 * FILL_EACH) : 0;
+        sort_one_kernel<<<(unsigned)(1 + (fill && blocks == 0 ? 1 : blocks)), 1024, 0, st>>>(e, pieces);
+    } else
+        for (int pass = 0; pass < e.passes; ++pass) {
+            const int tiles = (int)((e.n + SORT_TILE - 1) / SORT_TILE);
+            sort_count_kernel<<<tiles, 256, 0, st>>>(e, pass, tiles);
+            sort_scan_kernel<<<1 << e.digit, 256, 0, st>>>(e, tiles);
+            sort_place_kernel<<<tiles, 256, 0, st>>>(e, pass, tiles);
+        }
     if (e.n == 0) return;
     const int shift = team_shift_of(e.width);
-    const int64_t teams = 256 >> shift, chunks = (e.n + e.chunk - 1) / e.chunk;
-    const dim3 grid((unsigned)((chunks + teams - 1) / teams), (unsigned)((e.width + 2047) / 2048));
-    embed_grad_kernel<DT><<<grid, 256, 0, st>>>(e, shift);
-    if (chunks > 1) embed_grad_join_kernel<DT><<<grid, 256, 0, st>>>(e, shift);
+    const int64_t teams = 256 >> shift, chunks = (e.n + e.chunk - 1) / e.chunk, slices = (e.width + 2047) / 2048;
+    const unsigned chunk_blocks = (unsigned)((chunks + teams - 1) / teams * slices);
+    const unsigned fill_blocks = !one && !e.add ? (unsigned)((e.vocabulary + 255) / 256) : 0;
+    if (shift >= 6) embed_grad_kernel<DT, true><<<chunk_blocks + fill_blocks, 256, 0, st>>>(e, shift, chunk_blocks, (unsigned)slices);
+    else embed_grad_kernel<DT, false><<<chunk_blocks + fill_blocks, 256, 0, st>>>(e, shift, chunk_blocks, (unsigned)slices);
+    if (chunks > 1) embed_grad_join_kernel<DT><<<dim3((unsigned)(chunks < 1024 ? chunks : 1024), (unsigned)((e.width + 255) / 256)), 256, 0, st>>>(e);
 }
 void plaid_launch_embedding_backward(hipStream_t st, const EmbedArgs &e, int dtype)
 {

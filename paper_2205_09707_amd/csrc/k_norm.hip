@@ -174,11 +174,12 @@ template <int DT>
 static void launch_norm(hipStream_t st, const NormArgs &a)
 {
     const int pieces = (a.width + 7) / 8;
+    const bool many = a.rows >= NORM_MANY;
 #define GO(LANES, C) norm_kernel<DT, LANES, C><<<(unsigned)((a.rows * LANES + 255) / (LANES < 256 ? 256 : LANES)), LANES < 256 ? 256 : LANES, 0, st>>>(a)
     if (pieces <= 64) GO(64, 1);
     else if (pieces <= 128) GO(64, 2);
-    else if (pieces <= 256) GO(256, 1);
-    else if (pieces <= 512) GO(256, 2);
+    else if (pieces <= 256) many ? GO(64, 4) : GO(256, 1);
+    else if (pieces <= 512) many ? GO(64, 8) : GO(256, 2);
     else if (pieces <= 1024) GO(256, 4);
     else GO(1024, 2);
 #undef GO

@@ -13,6 +13,7 @@ struct EmbedArgs {
     // gradient's workspace
     int32_t *keys[2], *places[2];      // tokens in ascending order, and where each stood; two of each where several launches sort
     int32_t *counts, *totals;          // [bins][blocks] of a pass, [bins]
+    int32_t *shared, *begins;          // how many tokens several chunks share, and the chunks in which they begin
     int32_t sorted;                    // which of the two holds the result
     int32_t bits, passes, digit;       // bits of a key, passes, bits a pass
     int32_t chunk;                     // sorted places that a team of threads adds up
@@ -21,7 +22,7 @@ struct EmbedArgs {
 };
 // Up to this many tokens are sorted by one workgroup in one launch.
 #define SORT_ONE 4096
-#define SORT_TILE 2048
+#define SORT_TILE 1024
 void plaid_launch_embedding(hipStream_t st, const EmbedArgs &e, int dtype);
 void plaid_launch_embedding_backward(hipStream_t st, const EmbedArgs &e, int dtype);
 
@@ -37,6 +38,7 @@ struct NormArgs {
     float *part;                       // [workers][2][width] sums of dweight and dbias
 };
 #define NORM_WIDEST 16384
+#define NORM_MANY 2048
 void plaid_launch_layer_norm(hipStream_t st, const NormArgs &a, int dtype);
 void plaid_launch_layer_norm_backward(hipStream_t st, const NormArgs &a, int dtype);
 

@@ -25,24 +25,28 @@ int check_table(int64_t n, int64_t vocabulary, int32_t width, const int64_t *ids
 
 struct EmbedPlan {
     int32_t bits, passes, digit, chunk;
-    int64_t tiles, key_bytes, count_bytes, part_bytes, bytes;
+    int64_t tiles, key_bytes, count_bytes, begin_bytes, part_bytes, bytes;
 };
 EmbedPlan plan_embedding(int64_t n, int64_t vocabulary, int32_t width)
 {
     EmbedPlan p = {};
-    if (n == 0) return p;
+    if (n == 0) {  // the gradient is filled with zeros
+        p.bytes = p.begin_bytes = 16;
+        return p;
+    }
     p.bits = 64 - __builtin_clzll((unsigned long long)vocabulary);  // keys are 0 .. vocabulary
     p.passes = (int32_t)ceil_div(p.bits, 9);
     p.digit = (int32_t)ceil_div(p.bits, p.passes);
     p.tiles = ceil_div(n, SORT_TILE);
     // at most 2048 chunks, whose partial sums are added up one after another where one token has them all
     p.chunk = (int32_t)ceil_div(n, 2048);
-    if (p.chunk < 32) p.chunk = 32;
+    if (p.chunk < 8) p.chunk = 8;
     p.key_bytes = round16(n * 4);
     p.count_bytes = n > SORT_ONE ? round16(((p.tiles + 1) << p.digit) * 4) : 0;
     const int64_t chunks = ceil_div(n, p.chunk);
+    p.begin_bytes = 16 + round16(chunks * 4);
     p.part_bytes = chunks > 1 ? chunks * 2 * ((width + 7) / 8 * 8) * 4 : 0;
-    p.bytes = (n > SORT_ONE ? 4 : 2) * p.key_bytes + p.count_bytes + p.part_bytes;
+    p.bytes = (n > SORT_ONE ? 4 : 2) * p.key_bytes + p.count_bytes + p.begin_bytes + p.part_bytes;
     return p;
 }
 
@@ -60,7 +64,7 @@ int check_stride(const char *what, int64_t stride)
 }
 int norm_workers(int64_t rows, int32_t width)
 {
-    const int64_t teams = width <= 1024 ? 4 : 1, per = 4;  // at least `per` rows a team
+    const int64_t teams = width <= 1024 ? 4 : 1, per = 2;  // at least `per` rows a team
     const int64_t most = width <= 2048 ? 1024 : width <= 8192 ? 512 : 256, want = ceil_div(rows, teams * per);
     return (int)(want < 1 ? 1 : want < most ? want : most);
 }
@@ -215,6 +219,7 @@ extern "C" int plaid_embedding_backward(const void *d_out, int64_t d_out_stride,
         e.sorted = (p.passes - 1) & 1;
         e.counts = (int32_t *)w, e.totals = e.counts + (p.tiles << p.digit), w += p.count_bytes;
     }
+    e.shared = (int32_t *)w, e.begins = (int32_t *)(w + 16), w += p.begin_bytes;
     e.part = (float *)w;
     plaid_launch_embedding_backward((hipStream_t)hip_stream, e, dtype);
     return launched();

@@ -58,7 +58,7 @@ def test_embedding_workspace(lib):
         assert lib.plaid_embedding_backward_workspace(n, vocabulary, width, ct.byref(need)) == OK
         return need.value
 
-    assert of(0, 100, 64) == 0 and 0 < of(32, 100, 64) < of(33, 100, 64) < of(5000, 100, 64)
+    assert 0 < of(0, 100, 64) < of(8, 100, 64) < of(9, 100, 64) < of(5000, 100, 64)
     for bad in ((-1, 100, 64), (1, 0, 64), (1, 100, 0), (1 << 31, 100, 64)):
         assert lib.plaid_embedding_backward_workspace(*bad, ct.byref(need)) == E
     assert lib.plaid_embedding_backward_workspace(1, 1, 1, None) == E
