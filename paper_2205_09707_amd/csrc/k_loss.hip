@@ -1,6 +1,8 @@
 // Cross entropy over a vocabulary: what goes before and after its products, and the scores of a few rows.
 #include "train.h"
 
+#define NO_EXPONENT (-100000)  // of a d_loss of zero
+
 // With s_tv = scale h_t . W_v:  lse_t = log sum_v exp s_tv, loss_t = lse_t - s_t,target, and for gradients
 //   G_tv = d_loss_t (exp(s_tv - lse_t) - [v = target_t]),  dh_t = scale sum_v G_tv W_v,  dW_v = scale sum_t G_tv h_t.
 // Scores are never kept: the products' kernels (k_loss_mm.hip) leave a maximum and a sum of exponentials for each part of the vocabulary,
@@ -8,10 +10,98 @@
 // distance from one.
 
 // --- rows that have a target ----------------------------------------------------------------------------------------------------
-// One workgroup numbers them; the others have a loss of zero.  A row's place goes by those before it, so the order is the caller's.
-// Backward, d_loss = fraction 2^exponent: the fraction goes into G, which rounds to the type before it is multiplied, the power of two
-// into what G is multiplied with, where it is exact, so that G in fp16 stays in its range however small the gradient of a mean is.
-#define NO_EXPONENT (-100000)
+// They are numbered in the caller's order, and their states packed in the order in which the products' tiles take them, with zeros up to a whole
+// tile of rows and a whole step of columns; a row without a target has a loss of zero and no gradient.  Backward, d_loss = fraction 2^exponent:
+// the fraction goes into G, which rounds to the type before it is multiplied, the power of two into what G is multiplied with, where it is
+// exact, so that G in fp16 stays in its range however small the gradient of a mean is.
+__device__ __forceinline__ bool has_target(const LossArgs &a, int64_t t, int &target)
+{
+    const int64_t v = a.targets[t];
+    target = (int)v;
+    return v >= 0 && v < a.vocabulary;
+}
+__device__ __forceinline__ LossRow loss_row(const LossArgs &a, int64_t t, int target, bool backward)
+{
+    LossRow r = {target, 0, 0.0f, 0.0f, 0.0f};
+    if (backward) {
+        const float d = *(const float *)((const char *)a.d_loss + t * a.d_loss_stride);
+        if (fabsf(d) < INFINITY) r.fraction = frexpf(d, &r.exponent);
+        else r.fraction = d;
+        if (d == 0.0f) r.exponent = NO_EXPONENT;
+        r.top = a.lse[2 * t], r.log_total = a.lse[2 * t + 1];
+    }
+    return r;
+}
+// 128 threads; t < 0: zeros.
+template <int DT, bool BACKWARD>
+__device__ __forceinline__ void pack_row(const LossArgs &a, int place, int64_t t, int shift)
+{
+    constexpr int BLOCK = LOSS_TILE * LOSS_STEP * 2;
+    const char *from = a.hidden + (t < 0 ? 0 : t) * a.hidden_stride;
+    char *to = a.packed + (int64_t)(place / LOSS_TILE) * (a.pitch / LOSS_STEP) * BLOCK + place % LOSS_TILE * (2 * LOSS_STEP);
+    char *scaled = BACKWARD ? a.scaled + (int64_t)(place / LOSS_STEP) * (a.columns / LOSS_TILE) * BLOCK + place % LOSS_STEP * (2 * LOSS_TILE) : nullptr;
+    const float power = ldexpf(1.0f, shift);
+    for (int at = threadIdx.x * 8; at < (BACKWARD ? a.columns : a.pitch); at += 1024) {
+        const i32x4 w = t >= 0 && at < a.width ? *(const i32x4 *)(from + 2 * at) : i32x4{0, 0, 0, 0};
+        if (at < a.pitch) *(i32x4 *)(to + (int64_t)(at / LOSS_STEP) * BLOCK + at % LOSS_STEP * 2) = w;
+        if (BACKWARD) {
+            Eight v = unpack8<DT>(w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v.x[j] *= power;
+            *(i32x4 *)(scaled + (int64_t)(at / LOSS_TILE) * BLOCK + at % LOSS_TILE * 2) = pack8<DT>(v);
+        }
+    }
+}
+template <bool BACKWARD>
+__device__ __forceinline__ void no_target(const LossArgs &a, int64_t t)
+{
+    if (!BACKWARD) {
+        if (threadIdx.x == 0) {
+            a.loss[t] = 0.0f;
+            if (a.lse) *(float2 *)(a.lse + 2 * t) = {0.0f, 0.0f};
+        }
+    } else if (a.d_hidden)
+        for (int at = threadIdx.x * 8; at < a.width; at += 1024) *(i32x4 *)(a.d_hidden + (t * a.width + at) * 2) = i32x4{0, 0, 0, 0};
+}
+
+// Up to LOSS_PREPARE_ONE rows: one launch, in which each row's workgroup looks at all targets itself.  (509 rows of 768: 6 us in place of 14 for the
+// three below.)
+template <int DT, bool BACKWARD>
+__global__ __launch_bounds__(128) void loss_prepare_kernel(LossArgs a)
+{
+    __shared__ int found[2][3];
+    const int rows = (int)a.rows, t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int live = 0, before = 0, top = NO_EXPONENT;
+    for (int first = 0; first < rows; first += 128) {
+        const int i = first + threadIdx.x;
+        int target = 0;
+        const bool mine = i < rows && has_target(a, i, target);
+        live += __popcll(__ballot(mine)), before += __popcll(__ballot(mine && i < t));
+        if (BACKWARD && mine) top = max(top, loss_row(a, i, target, true).exponent);
+    }
+    if (BACKWARD)
+#pragma unroll
+        for (int o = 32; o; o >>= 1) top = max(top, __shfl_xor(top, o));
+    if (lane == 0) found[wave][0] = live, found[wave][1] = before, found[wave][2] = top;
+    __syncthreads();
+    live = found[0][0] + found[1][0], before = found[0][1] + found[1][1], top = max(found[0][2], found[1][2]);
+    if (top == NO_EXPONENT) top = 0;
+    if (t == 0 && threadIdx.x == 0) a.state[0] = live, a.state[1] = top;
+    int target = 0;
+    const bool mine = t < rows && has_target(a, t, target);
+    if (mine) {
+        const LossRow r = loss_row(a, t, target, BACKWARD);
+        if (threadIdx.x == 0) a.list[before] = t, a.row[before] = r;
+        pack_row<DT, BACKWARD>(a, before, t, r.exponent == NO_EXPONENT ? 0 : r.exponent - top);
+        return;
+    }
+    // the others, and those past the end, are as many as there are places up to the last tile's end
+    const int place = live + (t < rows ? t - before : t - live);
+    if (place < (live + LOSS_TILE - 1) / LOSS_TILE * LOSS_TILE) pack_row<DT, BACKWARD>(a, place, -1, 0);
+    if (t < rows) no_target<BACKWARD>(a, t);
+}
+
+// More rows: one workgroup numbers them.
 __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a, int backward)
 {
     __shared__ int wave_sum[16], wave_top[16];
@@ -19,8 +109,8 @@ __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a, int backwar
     int before = 0, top = NO_EXPONENT;
     for (int64_t first = 0; first < a.rows; first += 1024) {
         const int64_t t = first + threadIdx.x;
-        const int64_t target = t < a.rows ? a.targets[t] : -1;
-        const bool live = target >= 0 && target < a.vocabulary;
+        int target = 0;
+        const bool live = t < a.rows && has_target(a, t, target);
         const uint64_t votes = __ballot(live);
         if (lane == 0) wave_sum[wave] = __popcll(votes);
         __syncthreads();
@@ -31,20 +121,10 @@ __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a, int backwar
         }
         before += all;
         if (live) {
+            const LossRow r = loss_row(a, t, target, backward);
+            top = max(top, backward ? r.exponent : 0);
             a.list[at] = (int)t;
-            LossRow r = {(int)target, 0, 0.0f, 0.0f, 0.0f};
-            if (backward) {
-                const float d = *(const float *)((const char *)a.d_loss + t * a.d_loss_stride);
-                if (fabsf(d) < INFINITY) r.fraction = frexpf(d, &r.exponent);
-                else r.fraction = d;
-                if (d == 0.0f) r.exponent = NO_EXPONENT;
-                top = max(top, r.exponent);
-                r.top = a.lse[2 * t], r.log_total = a.lse[2 * t + 1];
-            }
             a.row[at] = r;
-        } else if (!backward && t < a.rows) {
-            a.loss[t] = 0.0f;
-            if (a.lse) *(float2 *)(a.lse + 2 * t) = {0.0f, 0.0f};
         }
         __syncthreads();
     }
@@ -57,52 +137,31 @@ __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a, int backwar
         a.state[0] = before, a.state[1] = top == NO_EXPONENT ? 0 : top;
     }
 }
-
-// Their states, packed in the order in which the products' tiles take them; zeros up to a whole tile of rows and a whole step of columns.
-// A workgroup has a row.
+// Workgroup i has place i, and row i if that has no target.
 template <int DT, bool BACKWARD>
 __global__ __launch_bounds__(128) void loss_pack_kernel(LossArgs a)
 {
-    constexpr int BLOCK = LOSS_TILE * LOSS_STEP * 2;
     const int live = uniform_load(a.state), top = uniform_load(a.state + 1), i = blockIdx.x;
+    int target = 0;
+    if (i < a.rows && !has_target(a, i, target)) no_target<BACKWARD>(a, i);
     if (i >= (live + LOSS_TILE - 1) / LOSS_TILE * LOSS_TILE) return;
-    const bool there = i < live;
-    const char *from = a.hidden + (there ? (int64_t)uniform_load(a.list + i) : 0) * a.hidden_stride;
-    char *to = a.packed + (int64_t)(i / LOSS_TILE) * (a.pitch / LOSS_STEP) * BLOCK + i % LOSS_TILE * (2 * LOSS_STEP);
-    char *scaled = BACKWARD ? a.scaled + (int64_t)(i / LOSS_STEP) * (a.columns / LOSS_TILE) * BLOCK + i % LOSS_STEP * (2 * LOSS_TILE) : nullptr;
-    float power = 1.0f;
-    if (BACKWARD && there) {
-        const int e = uniform_load(&a.row[i].exponent);
-        if (e != NO_EXPONENT) power = ldexpf(1.0f, e - top);
-    }
-    for (int at = threadIdx.x * 8; at < (BACKWARD ? a.columns : a.pitch); at += 1024) {
-        const i32x4 w = there && at < a.width ? *(const i32x4 *)(from + 2 * at) : i32x4{0, 0, 0, 0};
-        if (at < a.pitch) *(i32x4 *)(to + (int64_t)(at / LOSS_STEP) * BLOCK + at % LOSS_STEP * 2) = w;
-        if (BACKWARD) {
-            Eight v = unpack8<DT>(w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v.x[j] *= power;
-            *(i32x4 *)(scaled + (int64_t)(at / LOSS_TILE) * BLOCK + at % LOSS_TILE * 2) = pack8<DT>(v);
-        }
-    }
-}
-
-// A row without a target has no gradient.
-__global__ __launch_bounds__(128) void loss_zero_kernel(LossArgs a)
-{
-    const int64_t t = blockIdx.x, target = uniform_load(a.targets + t);
-    if (target >= 0 && target < a.vocabulary) return;
-    for (int at = threadIdx.x * 8; at < a.width; at += 1024) *(i32x4 *)(a.d_hidden + (t * a.width + at) * 2) = i32x4{0, 0, 0, 0};
+    const int e = BACKWARD && i < live ? uniform_load(&a.row[i].exponent) : NO_EXPONENT;
+    pack_row<DT, BACKWARD>(a, i, i < live ? uniform_load(a.list + i) : -1, e == NO_EXPONENT ? 0 : e - top);
 }
 
 void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool backward)
 {
-    loss_list_kernel<<<1, 1024, 0, st>>>(a, backward);
     const unsigned grid = (unsigned)a.padded_rows;
+    if (a.rows <= LOSS_PREPARE_ONE) {
+        if (!backward) loss_prepare_kernel<PLAID_BF16, false><<<grid, 128, 0, st>>>(a);
+        else if (dtype == PLAID_BF16) loss_prepare_kernel<PLAID_BF16, true><<<grid, 128, 0, st>>>(a);
+        else loss_prepare_kernel<PLAID_FP16, true><<<grid, 128, 0, st>>>(a);
+        return;
+    }
+    loss_list_kernel<<<1, 1024, 0, st>>>(a, backward);
     if (!backward) loss_pack_kernel<PLAID_BF16, false><<<grid, 128, 0, st>>>(a);
     else if (dtype == PLAID_BF16) loss_pack_kernel<PLAID_BF16, true><<<grid, 128, 0, st>>>(a);
     else loss_pack_kernel<PLAID_FP16, true><<<grid, 128, 0, st>>>(a);
-    if (backward && a.d_hidden) loss_zero_kernel<<<(unsigned)a.rows, 128, 0, st>>>(a);
 }
 
 // Maxima and sums of exponentials beside them, of two parts.
@@ -278,8 +337,8 @@ __global__ __launch_bounds__(256) void loss_d_hidden_join_kernel(LossArgs a)
     const int block = blockIdx.x & 7, k = blockIdx.x >> 3 & 7, tile = blockIdx.x >> 6, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int row = tile / widths * LOSS_TILE + block * 32 + (lane & 31);
     if (tile / widths * LOSS_TILE + block * 32 >= live) return;
-    const int splits = hidden_splits(row_tiles * widths, a.hidden_steps, a.splits);
-    const int64_t part = (int64_t)(a.padded_rows / LOSS_TILE) * widths * (LOSS_TILE * LOSS_TILE);
+    const int splits = hidden_splits(a, live);
+    const int64_t part = (int64_t)row_tiles * widths * (LOSS_TILE * LOSS_TILE);
     const bool there = row < live;
     const int64_t t = there ? a.list[row] : 0;
     const int e = there ? a.row[row].exponent : 0;

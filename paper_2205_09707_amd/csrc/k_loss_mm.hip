@@ -92,10 +92,12 @@ struct Tile {
 };
 // Tile of workgroup `id`: workgroups go to the eight XCDs in turn, and each XCD gets a stretch of panels of four tiles of n, so that what its
 // workgroups read together is in its cache.
-__device__ __forceinline__ bool find_tile(int id, int ms, int ns, Tile &t)
+__device__ __forceinline__ bool find_tile(int id, int ms, int ns, int splits, Tile &t, int &split)
 {
-    const int all = ms * ns, each = (all + 7) / 8, o = (id & 7) * each + (id >> 3);
+    const int tiles = ms * ns, all = tiles * splits, each = (all + 7) / 8;
+    int o = (id & 7) * each + (id >> 3);
     if ((id >> 3) >= each || o >= all) return false;
+    split = o / tiles, o -= split * tiles;
     const int panels = ns / 4, whole = panels * 4 * ms;
     if (o < whole) t.n = o / (4 * ms) * 4 + o % 4, t.m = o % (4 * ms) / 4;
     else t.n = panels * 4 + (o - whole) % (ns % 4), t.m = (o - whole) / (ns % 4);
@@ -112,17 +114,22 @@ __device__ __forceinline__ int result_place(int n, int m) { return n * (LOSS_TIL
 #define KIND_D_HIDDEN 2
 #define KIND_D_WEIGHT 3
 
+struct TileLds {
+    char operand[2][2][TILE_BYTES];
+};
 template <int DT, int KIND>
-__global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
+__device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int id)
 {
     constexpr bool SCORES = KIND <= KIND_GRADIENT, A_ACROSS = !SCORES, B_ACROSS = KIND == KIND_D_WEIGHT;
-    __shared__ __align__(16) char lds[2][2][TILE_BYTES];
+    auto &lds = tiles.operand;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wm = wave >> 2, wn = wave & 3;
     const int live = uniform_load(a.state), row_tiles = (live + LOSS_TILE - 1) / LOSS_TILE;
     const int pieces = (a.piece + LOSS_TILE - 1) / LOSS_TILE, widths = a.columns / LOSS_TILE;
+    // d_hidden's tiles come once for each part of its axis, those of one part together
+    const int splits = KIND == KIND_D_HIDDEN ? hidden_splits(a, live) : 1;
     Tile t;
-    const int split = KIND == KIND_D_HIDDEN ? blockIdx.y : 0;
-    if (!find_tile(blockIdx.x, SCORES ? pieces : widths, KIND == KIND_D_WEIGHT ? pieces : row_tiles, t)) return;
+    int split = 0;
+    if (!find_tile(id, SCORES ? pieces : widths, KIND == KIND_D_WEIGHT ? pieces : row_tiles, splits, t, split)) return;
 
     // a piece's gradients lie tile by tile, rows by pieces, 128 KB each; packed states too, of 64 columns, 32 KB each
     constexpr int64_t G_TILE = LOSS_TILE * LOSS_TILE * 2;
@@ -135,8 +142,7 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
         A.set(a.weight, a.weight_stride, a.first + t.m * LOSS_TILE, a.vocabulary, 0);
         B.set(a.packed + (int64_t)t.n * steps * TILE_BYTES, 2 * BK, 0, LOSS_TILE, 0);
     } else if constexpr (KIND == KIND_D_HIDDEN) {
-        const int all = (a.piece + BK - 1) / BK, splits = hidden_splits(row_tiles * widths, a.hidden_steps, a.splits), share = (all + splits - 1) / splits;
-        if (split >= splits) return;
+        const int all = (a.piece + BK - 1) / BK, share = (all + splits - 1) / splits;
         begin = min(all, split * share), steps = min(all, begin + share) - begin;
         if (begin + steps == all) end_left = a.piece - (all - 1) * BK;
         a_step = BK * a.weight_stride, b_step = 2 * BK;
@@ -258,7 +264,9 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
             const bool there = row < live;
             const int target = there ? a.row[row].target - (int)a.first - m0 : -1;  // place in the piece, from the lane's first
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i][j] *= a.scale;
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = acc[i][j][r] * a.scale;
             if (__any(target >= 0 && target < 128)) {  // the target's score is kept apart
                 float own = 0.0f;
 #pragma unroll
@@ -326,7 +334,7 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
         send(a.gradient + ((int64_t)t.n * pieces + t.m) * G_TILE, LOSS_TILE * 2, LOSS_TILE, LOSS_TILE);
     } else if constexpr (KIND == KIND_D_HIDDEN) {
         // sums over parts stay in the order of the registers: 1 KB of a wave at a time
-        float *out = a.d_part + (((int64_t)split * (a.padded_rows / LOSS_TILE) + t.n) * widths + t.m) * (LOSS_TILE * LOSS_TILE) + wave * 8192 + lane * 4;
+        float *out = a.d_part + (((int64_t)split * row_tiles + t.n) * widths + t.m) * (LOSS_TILE * LOSS_TILE) + wave * 8192 + lane * 4;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -356,18 +364,36 @@ __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
     }
 }
 
-template <int KIND>
-static void launch(hipStream_t st, const LossArgs &a, int dtype)
+template <int DT, int KIND>
+__global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
 {
-    const int64_t pieces = (a.piece + LOSS_TILE - 1) / LOSS_TILE, widths = a.columns / LOSS_TILE, rows = a.padded_rows / LOSS_TILE;
-    const int64_t tiles = KIND <= KIND_GRADIENT ? pieces * rows : KIND == KIND_D_HIDDEN ? widths * rows : widths * pieces;
-    const dim3 grid((unsigned)((tiles + 7) / 8 * 8), KIND == KIND_D_HIDDEN ? a.splits : 1);
-    if (dtype == PLAID_BF16) loss_mm_kernel<PLAID_BF16, KIND><<<grid, 512, 0, st>>>(a);
-    else loss_mm_kernel<PLAID_FP16, KIND><<<grid, 512, 0, st>>>(a);
+    __shared__ __align__(16) TileLds lds;
+    product<DT, KIND>(a, lds, blockIdx.x);
 }
+// Both gradients: d_hidden's tiles, which take longer, then d_weight's.
+template <int DT>
+__global__ __launch_bounds__(512, 2) void loss_gradients_kernel(LossArgs a, int hidden)
+{
+    __shared__ __align__(16) TileLds lds;
+    if ((int)blockIdx.x < hidden) product<DT, KIND_D_HIDDEN>(a, lds, blockIdx.x);
+    else product<DT, KIND_D_WEIGHT>(a, lds, blockIdx.x - hidden);
+}
+
+static int rounded_up(int64_t tiles) { return (int)((tiles + 7) / 8 * 8); }
+
 void plaid_launch_loss_scores(hipStream_t st, const LossArgs &a, int dtype, bool backward)
 {
-    backward ? launch<KIND_GRADIENT>(st, a, dtype) : launch<KIND_STATISTICS>(st, a, dtype);
+    const int grid = rounded_up((int64_t)((a.piece + LOSS_TILE - 1) / LOSS_TILE) * (a.padded_rows / LOSS_TILE));
+#define GO(DT) backward ? loss_mm_kernel<DT, KIND_GRADIENT><<<grid, 512, 0, st>>>(a) : loss_mm_kernel<DT, KIND_STATISTICS><<<grid, 512, 0, st>>>(a)
+    if (dtype == PLAID_BF16) GO(PLAID_BF16);
+    else GO(PLAID_FP16);
+#undef GO
 }
-void plaid_launch_loss_d_weight(hipStream_t st, const LossArgs &a, int dtype) { launch<KIND_D_WEIGHT>(st, a, dtype); }
-void plaid_launch_loss_d_hidden(hipStream_t st, const LossArgs &a, int dtype) { launch<KIND_D_HIDDEN>(st, a, dtype); }
+void plaid_launch_loss_gradients(hipStream_t st, const LossArgs &a, int dtype)
+{
+    const int64_t widths = a.columns / LOSS_TILE;
+    const int hidden = a.d_hidden ? rounded_up(loss_part_tiles(a.padded_rows, a.columns, a.hidden_steps)) : 0;
+    const int weight = a.d_weight ? rounded_up(widths * ((a.piece + LOSS_TILE - 1) / LOSS_TILE)) : 0;
+    if (dtype == PLAID_BF16) loss_gradients_kernel<PLAID_BF16><<<hidden + weight, 512, 0, st>>>(a, hidden);
+    else loss_gradients_kernel<PLAID_FP16><<<hidden + weight, 512, 0, st>>>(a, hidden);
+}

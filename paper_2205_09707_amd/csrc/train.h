@@ -67,9 +67,9 @@ struct LossArgs {
     float2 *running;                   // [padded_rows] over all parts before
     float *own;                        // [padded_rows] score of the target
     char *gradient;                    // [rows / 256][piece / 256][256][256] of the scores, over a piece of the vocabulary
-    float *d_part;                     // [splits][rows / 256][columns / 256][256 x 256] sums of d_hidden, in the order of the products' registers
+    float *d_part;                     // [parts][tiles of rows that have a target][columns / 256][256 x 256] sums of d_hidden, in the order of the products' registers
     int32_t columns;                   // width rounded up to LOSS_TILE
-    int32_t splits, hidden_steps;      // most parts of d_hidden's axis, steps of a whole piece
+    int32_t hidden_steps;              // steps of a whole piece along d_hidden's axis
     int64_t first;                     // the piece's first entry, and how many there are
     int32_t piece, last;               // last: no piece comes after this one
 };
@@ -77,24 +77,40 @@ struct LossArgs {
 #define LOSS_STEP 64
 #define LOSS_PART 128
 #define LOSS_PART_STEPS 12
+#define LOSS_PARTS 512  // tiles of all parts of d_hidden, where there are several
 #define LOSS_FEW 64
+#define LOSS_PREPARE_ONE 2048
 #define LOSS_FEW_THREADS 256
+// Tiles that the parts of d_hidden have at most.
+constexpr int64_t loss_part_tiles(int64_t padded_rows, int64_t columns, int64_t steps)
+{
+    const int64_t tiles = padded_rows / LOSS_TILE * (columns / LOSS_TILE), most = steps < 4 ? 1 : steps / 4;
+    return tiles > LOSS_PARTS ? tiles : tiles * most < LOSS_PARTS ? tiles * most : LOSS_PARTS;
+}
 void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool backward);
 void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int blocks);
 void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool packed);
 void plaid_launch_loss_scores(hipStream_t st, const LossArgs &a, int dtype, bool backward);
-void plaid_launch_loss_d_weight(hipStream_t st, const LossArgs &a, int dtype);
-void plaid_launch_loss_d_hidden(hipStream_t st, const LossArgs &a, int dtype);
+void plaid_launch_loss_gradients(hipStream_t st, const LossArgs &a, int dtype);
 void plaid_launch_loss_d_hidden_join(hipStream_t st, const LossArgs &a, int dtype);
 
 #ifdef __HIP__
-// Parts that the vocabulary's axis of d_hidden is cut into, of at most `most`: as few as leave least of the chip idle in the last round of
-// `tiles` times as many workgroups; a part costs what LOSS_PART_STEPS steps of it cost, as its sums are read and written.
-__device__ __forceinline__ int hidden_splits(int tiles, int steps, int most)
+// Parts that the vocabulary's axis of d_hidden is cut into, from the number of rows that have a target.  Beside d_weight's tiles, which fill up what
+// is left of the chip: so many that none takes longer than all together take on average (7296 rows of 2048 on 128000 entries, 160 tiles:
+// one part, 4820 us for both gradients in place of 4960 with three).  Alone: as few as leave least of the chip idle in the last round; a part costs
+// what LOSS_PART_STEPS steps of it cost, as its sums are written and read.
+__device__ __forceinline__ int hidden_splits(const LossArgs &a, int live)
 {
+    const int widths = a.columns / LOSS_TILE, tiles = (live + LOSS_TILE - 1) / LOSS_TILE * widths, steps = a.hidden_steps;
+    if (tiles == 0) return 1;
+    if (a.d_weight) {
+        const int64_t others = (int64_t)((steps + 3) / 4) * widths * ((live + LOSS_STEP - 1) / LOSS_STEP);
+        const int share = max((int)(((int64_t)tiles * steps + others) / 256), LOSS_PART_STEPS);
+        return max(1, min(min((steps + share - 1) / share, LOSS_PARTS / tiles), steps / 4));
+    }
     int best = 1;
     float least = 0.0f;
-    for (int s = 1; s <= most; ++s) {
+    for (int s = 1; s == 1 || (s * tiles <= LOSS_PARTS && 4 * s <= steps); ++s) {
         const float cost = (float)((tiles * s + 255) / 256) * ((float)steps / (float)s + LOSS_PART_STEPS);
         if (s == 1 || cost < 0.98f * least) best = s, least = cost;
     }

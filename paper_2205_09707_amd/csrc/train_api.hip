@@ -71,7 +71,7 @@ int norm_workers(int64_t rows, int32_t width)
 
 struct LossPlan {
     bool few;
-    int blocks, splits;
+    int blocks;
     int64_t padded_rows, pitch, columns, piece;
     int64_t list_bytes, row_bytes, packed_bytes, scaled_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, d_part_bytes, bytes;
 };
@@ -101,12 +101,8 @@ LossPlan plan_loss(const plaid_token_loss &a, bool backward)
     p.piece = ceil_div(ceil_div(a.vocabulary, pieces), LOSS_TILE) * LOSS_TILE;
     if (backward) {
         p.gradient_bytes = p.padded_rows * p.piece * 2;
-        // at most so many parts of d_hidden's axis (the kernel knows how many rows have a target, and takes fewer where they are better)
-        const int64_t tiles = p.columns / LOSS_TILE * (p.padded_rows / LOSS_TILE), steps = ceil_div(p.piece, LOSS_STEP), want = ceil_div(4 * 256, tiles);
-        p.splits = (int)(want > 32 ? 32 : want);
-        if (p.splits > ceil_div(steps, 4)) p.splits = (int)ceil_div(steps, 4);
         p.scaled_bytes = p.padded_rows * p.columns * 2;
-        p.d_part_bytes = p.splits * p.padded_rows * p.columns * 4;
+        p.d_part_bytes = loss_part_tiles(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
         p.bytes = p.list_bytes + p.row_bytes + p.packed_bytes + p.scaled_bytes + p.gradient_bytes + p.d_part_bytes;
     } else {
         p.part_bytes = p.piece / LOSS_PART * p.padded_rows * 8;
@@ -151,7 +147,7 @@ LossArgs loss_args(const plaid_token_loss &a, const LossPlan &p, void *workspace
     x.loss = a.loss, x.lse = a.lse;
     x.rows = a.rows, x.vocabulary = a.vocabulary, x.hidden_stride = 2 * a.hidden_stride, x.weight_stride = 2 * a.weight_stride;
     x.width = a.width, x.scale = a.scale;
-    x.padded_rows = (int32_t)p.padded_rows, x.pitch = (int32_t)p.pitch, x.columns = (int32_t)p.columns, x.splits = p.splits, x.hidden_steps = (int32_t)ceil_div(p.piece, LOSS_STEP);
+    x.padded_rows = (int32_t)p.padded_rows, x.pitch = (int32_t)p.pitch, x.columns = (int32_t)p.columns, x.hidden_steps = (int32_t)ceil_div(p.piece, LOSS_STEP);
     char *w = (char *)workspace;
     if (!p.few) {
         x.state = (int32_t *)w, x.list = (int32_t *)(w + 16), w += p.list_bytes;
@@ -348,8 +344,7 @@ extern "C" int plaid_cross_entropy_backward(const plaid_token_loss *args, const 
     for (x.first = 0; x.first < x.vocabulary; x.first += p.piece) {
         x.piece = (int32_t)(x.vocabulary - x.first < p.piece ? x.vocabulary - x.first : p.piece);
         plaid_launch_loss_scores(st, x, args->dtype, true);
-        if (d_weight) plaid_launch_loss_d_weight(st, x, args->dtype);
-        if (x.d_hidden) plaid_launch_loss_d_hidden(st, x, args->dtype);
+        plaid_launch_loss_gradients(st, x, args->dtype);
     }
     if (x.d_hidden) plaid_launch_loss_d_hidden_join(st, x, args->dtype);
     return launched();
