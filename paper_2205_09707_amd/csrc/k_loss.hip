@@ -172,36 +172,40 @@ __device__ __forceinline__ float2 join_parts(float2 x, float2 y)
 }
 
 // --- few rows -------------------------------------------------------------------------------------------------------------------
-// The vocabulary is read once, at the rate of memory if enough of it is under way: a workgroup has 64 BLOCKS entries, a quarter for each of its
-// four waves, and up to 16 GROUPS rows; 64 columns of both go straight into LDS, two steps ahead of the products.
-#define FEW_STAGES 3
-template <int DT, int BLOCKS, int GROUPS>
-__global__ __launch_bounds__(LOSS_FEW_THREADS) void loss_few_kernel(LossArgs a)
+// The vocabulary is read at the rate of memory if enough of it is under way: a workgroup has 64 BLOCKS entries, a quarter for each of its four
+// waves, and up to 16 GROUPS rows; 64 columns of both go straight into LDS, some steps ahead of the products.  Forward it takes the caller's
+// rows, all of them (a row without a target has its own column of the result, and is left out when parts are joined); backward (GRADIENT) the
+// packed ones, and leaves G over the piece as the products take it, with zeros up to whole steps of 64 rows and entries.
+template <int DT, int WAVES, int BLOCKS, int GROUPS, bool GRADIENT>
+__global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
 {
-    constexpr int ENTRIES = 64 * BLOCKS, W_LOADS = 2 * BLOCKS, H_PIECES = 2 * GROUPS, H_LOADS = (H_PIECES + 3) / 4, LOADS = W_LOADS + H_LOADS;
-    __shared__ __align__(16) char lds_w[FEW_STAGES][ENTRIES * 128], lds_h[FEW_STAGES][GROUPS * 16 * 128];
-    __shared__ float2 joined[4][16 * GROUPS];
+    constexpr int ENTRIES = 16 * WAVES * BLOCKS, W_LOADS = 2 * BLOCKS, H_PIECES = 2 * GROUPS, H_LOADS = (H_PIECES + WAVES - 1) / WAVES, LOADS = W_LOADS + H_LOADS;
+    constexpr int STAGES = 3;
+    __shared__ __align__(16) char lds_w[STAGES][ENTRIES * 128], lds_h[STAGES][GROUPS * 16 * 128];
+    __shared__ float2 joined[WAVES][16 * GROUPS];
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), l = lane & 15, q = lane >> 4;
-    const int64_t v0 = (int64_t)blockIdx.x * ENTRIES;
+    const int rows = GRADIENT ? uniform_load(a.state) : (int)a.rows;
+    const int64_t first = GRADIENT ? a.first : 0, end = GRADIENT ? a.first + a.piece : a.vocabulary, v0 = first + (int64_t)blockIdx.x * ENTRIES;
     // a load has eight rows of 128 bytes, whose chunks change places as lds_chunk says; with fewer pieces of states than waves some are brought twice
     const char *from[LOADS];
-    int to[LOADS];
-    int chunk[LOADS];
+    int to[LOADS], chunk[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
         const bool w = i < W_LOADS;
-        const int piece = w ? wave * W_LOADS + i : (wave + 4 * (i - W_LOADS)) % H_PIECES, row = piece * 8 + (lane >> 3);
+        const int piece = w ? wave * W_LOADS + i : (wave + WAVES * (i - W_LOADS)) % H_PIECES, row = piece * 8 + (lane >> 3);
         chunk[i] = (lane & 7) ^ swizzle<64>(row);
         to[i] = piece * 1024;
-        from[i] = w ? a.weight + min(v0 + row, a.vocabulary - 1) * a.weight_stride : a.hidden + min((int64_t)row, a.rows - 1) * a.hidden_stride;
+        if (w) from[i] = a.weight + min(v0 + row, a.vocabulary - 1) * a.weight_stride;
+        else from[i] = GRADIENT ? a.packed + row * 128 : a.hidden + min((int64_t)row, a.rows - 1) * a.hidden_stride;
         from[i] += chunk[i] * 16;
     }
     const int steps = (a.width + 63) / 64, left = a.width - (steps - 1) * 64;
     const auto bring = [&](int s, int stage) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const char *p = from[i] + s * 128;
-            if (s == steps - 1 && chunk[i] * 8 >= left) p = (const char *)zero_row;  // zeros past the end of the rows
+            const bool packed = GRADIENT && i >= W_LOADS;
+            const char *p = from[i] + (int64_t)s * (packed ? LOSS_TILE * 128 : 128);
+            if (!packed && s == steps - 1 && chunk[i] * 8 >= left) p = (const char *)zero_row;  // zeros past the end of the rows
             load_to_lds(p, (i < W_LOADS ? lds_w[stage] : lds_h[stage]) + to[i]);
         }
     };
@@ -214,14 +218,14 @@ __global__ __launch_bounds__(LOSS_FEW_THREADS) void loss_few_kernel(LossArgs a)
 #pragma unroll
     for (int k = 0; k < 2; ++k) place[k] = l * 128 + (((4 * k + q) ^ swizzle<64>(l)) << 4);  // rows 16 on: 2048 bytes
 #pragma unroll
-    for (int s = 0; s < FEW_STAGES - 1; ++s)
+    for (int s = 0; s < STAGES - 1; ++s)
         if (s < steps) bring(s, s);
     int stage = 0;
     for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) wait_loads<LOADS * (FEW_STAGES - 2)>();
+        if (s + STAGES - 1 <= steps) wait_loads<LOADS * (STAGES - 2)>();
         else wait_loads<0>();
         lds_barrier();  // this step's tiles have come, and all waves are done with those of the step before
-        if (s + FEW_STAGES - 1 < steps) bring(s + FEW_STAGES - 1, stage == 0 ? FEW_STAGES - 1 : stage - 1);
+        if (s + STAGES - 1 < steps) bring(s + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
         const char *w = lds_w[stage] + wave * (BLOCKS * 2048), *h = lds_h[stage];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -235,22 +239,48 @@ __global__ __launch_bounds__(LOSS_FEW_THREADS) void loss_few_kernel(LossArgs a)
 #pragma unroll
                 for (int j = 0; j < GROUPS; ++j) acc[i][j] = mfma16<DT>(x[i], y[j], acc[i][j]);
         }
-        stage = stage == FEW_STAGES - 1 ? 0 : stage + 1;
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
-    const int64_t mine = v0 + wave * (16 * BLOCKS);
+    // a lane's results: row 16 j + l, entries 16 i + 4 q .. + 3 from the wave's first
+    const int64_t mine = v0 + wave * (16 * BLOCKS) + 4 * q;
+    if constexpr (GRADIENT) {
+        const int pieces = (a.piece + LOSS_TILE - 1) / LOSS_TILE;
+#pragma unroll
+        for (int j = 0; j < GROUPS; ++j) {
+            const int t = 16 * j + l;
+            const bool there = t < rows;
+            const LossRow x = there ? a.row[t] : LossRow{-1, 0, 0.0f, 0.0f, 0.0f};
+            const ScoreGradient gradient(x, a.scale, DT);
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+                float g[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t v = mine + 16 * i + r;
+                    g[r] = gradient.other(acc[i][j][r]);
+                    if (v == x.target) g[r] = gradient.target(acc[i][j][r]);
+                    if (!there || v >= end) g[r] = 0.0f;
+                }
+                const int at = (int)(mine - first) + 16 * i;
+                char *out = a.gradient + ((int64_t)(t / LOSS_TILE) * pieces + at / LOSS_TILE) * (LOSS_TILE * LOSS_TILE * 2) + (t % LOSS_TILE * LOSS_TILE + at % LOSS_TILE) * 2;
+                *(i32x2 *)out = i32x2{pack2<DT>(g[0], g[1]), pack2<DT>(g[2], g[3])};
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
         const int64_t t = 16 * j + l;
-        const int64_t target = t < a.rows ? a.targets[t] : -1;
+        const int64_t target = t < rows ? a.targets[t] : -1;
         float most = -INFINITY;
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int64_t v = mine + 16 * i + 4 * q + r;
+                const int64_t v = mine + 16 * i + r;
                 float s = acc[i][j][r] * a.scale;
-                if (v == target && v < a.vocabulary) a.own[t] = s;
-                if (v == target || v >= a.vocabulary) s = -INFINITY;
+                if (v == target && v < end) a.own[t] = s;
+                if (v == target || v >= end) s = -INFINITY;
                 acc[i][j][r] = s;
                 most = fmaxf(most, s);
             }
@@ -267,19 +297,46 @@ __global__ __launch_bounds__(LOSS_FEW_THREADS) void loss_few_kernel(LossArgs a)
     __syncthreads();
     if (threadIdx.x < 16 * GROUPS && threadIdx.x < a.rows) {
         const int t = threadIdx.x;
-        a.part[(int64_t)blockIdx.x * a.padded_rows + t] = join_parts(join_parts(joined[0][t], joined[1][t]), join_parts(joined[2][t], joined[3][t]));
+        float2 x = join_parts(join_parts(joined[0][t], joined[1][t]), join_parts(joined[2][t], joined[3][t]));
+        if constexpr (WAVES == 8) x = join_parts(x, join_parts(join_parts(joined[4][t], joined[5][t]), join_parts(joined[6][t], joined[7][t])));
+        a.part[(int64_t)blockIdx.x * a.padded_rows + t] = x;
     }
 }
 
-void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int blocks)
+template <int DT, int WAVES, int BLOCKS>
+static void launch_few(hipStream_t st, const LossArgs &a, bool gradient)
 {
     const int groups = (int)((a.rows + 15) / 16);
-    const unsigned grid = (unsigned)((a.vocabulary + 64 * blocks - 1) / (64 * blocks));
-#define GO(DT, B, G) loss_few_kernel<DT, B, G><<<grid, LOSS_FEW_THREADS, 0, st>>>(a)
-#define GROUPS(DT, B) (groups == 1 ? GO(DT, B, 1) : groups == 2 ? GO(DT, B, 2) : groups == 3 ? GO(DT, B, 3) : GO(DT, B, 4))
-    if (dtype == PLAID_BF16) blocks == 1 ? GROUPS(PLAID_BF16, 1) : GROUPS(PLAID_BF16, 2);
-    else blocks == 1 ? GROUPS(PLAID_FP16, 1) : GROUPS(PLAID_FP16, 2);
-#undef GROUPS
+    const int64_t entries = gradient ? a.piece : a.vocabulary;
+    const unsigned grid = (unsigned)((entries + 16 * WAVES * BLOCKS - 1) / (16 * WAVES * BLOCKS));
+#define GO(G, GRADIENT) loss_few_kernel<DT, WAVES, BLOCKS, G, GRADIENT><<<grid, WAVES * 64, 0, st>>>(a)
+    if constexpr (WAVES == 8) {
+        if (gradient) GO(8, true);
+        else if (groups <= 6) GO(6, false);
+        else GO(8, false);
+    } else if constexpr (BLOCKS == 2) {
+        if (gradient) GO(4, true);
+        else if (groups == 1) GO(1, false);
+        else if (groups == 2) GO(2, false);
+        else if (groups == 3) GO(3, false);
+        else GO(4, false);
+    } else {
+        if (gradient) groups <= 4 ? GO(4, true) : GO(8, true);
+        else if (groups == 1) GO(1, false);
+        else if (groups == 2) GO(2, false);
+        else if (groups == 3) GO(3, false);
+        else if (groups == 4) GO(4, false);
+        else if (groups <= 6) GO(6, false);
+        else GO(8, false);
+    }
+#undef GO
+}
+// entries: of a workgroup, 64, 128 (up to 64 rows) or 256 (more rows)
+void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int entries, bool gradient)
+{
+#define GO(DT) entries == 64 ? launch_few<DT, 4, 1>(st, a, gradient) : entries == 128 ? launch_few<DT, 4, 2>(st, a, gradient) : launch_few<DT, 8, 2>(st, a, gradient)
+    if (dtype == PLAID_BF16) GO(PLAID_BF16);
+    else GO(PLAID_FP16);
 #undef GO
 }
 
@@ -322,7 +379,7 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossArgs a, int parts, i
 void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool packed)
 {
     if (a.rows >= 4096) loss_join_kernel<32><<<(unsigned)((a.rows + 31) / 32), 256, 0, st>>>(a, parts, packed);
-    else if (a.rows > LOSS_FEW) loss_join_kernel<8><<<(unsigned)((a.rows + 7) / 8), 256, 0, st>>>(a, parts, packed);
+    else if (a.rows > 64) loss_join_kernel<8><<<(unsigned)((a.rows + 7) / 8), 256, 0, st>>>(a, parts, packed);
     else loss_join_kernel<1><<<(unsigned)a.rows, 256, 0, st>>>(a, parts, packed);
 }
 

@@ -300,21 +300,20 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
             if (lane < 32) a.part[(int64_t)(t.m * 2 + wm) * a.padded_rows + row] = {most, sum};
         }
     } else if constexpr (KIND == KIND_GRADIENT) {
-        constexpr float GAIN = DT == PLAID_FP16 ? 0x1p15f : 1.0f;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int row = n0 + 32 * j;
             const bool there = row < live;
             const LossRow x = there ? a.row[row] : LossRow{-1, 0, 0.0f, 0.0f, 0.0f};
             const int target = there ? x.target - (int)a.first - m0 : -1;
-            const float rest = x.log_total * LOG2E, factor = x.fraction * GAIN;
-            float own = 0.0f;  // of the target: the probability less one, which keeps its digits where the probability is almost one
+            const ScoreGradient gradient(x, a.scale, DT);
+            float own = 0.0f;
             if (__any(target >= 0 && target < 128)) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) own = 32 * i + 8 * (r / 4) + r % 4 == target ? acc[i][j][r] : own;
-                own = expm1f(own * a.scale - x.top - x.log_total);
+                own = gradient.target(own);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -324,9 +323,8 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int m = 32 * i + 8 * c + r;
-                        const float d = acc[i][j][4 * c + r] * a.scale - x.top;
-                        const float p = m == target ? own : __builtin_amdgcn_exp2f(d * LOG2E - rest);
-                        g[r] = there && m0 + m < a.piece ? p * factor : 0.0f;
+                        g[r] = m == target ? own : gradient.other(acc[i][j][4 * c + r]);
+                        if (!there || m0 + m >= a.piece) g[r] = 0.0f;
                     }
                     keep(i, j, c, g[0], g[1], g[2], g[3]);
                 }

@@ -78,9 +78,8 @@ struct LossArgs {
 #define LOSS_PART 128
 #define LOSS_PART_STEPS 12
 #define LOSS_PARTS 512  // tiles of all parts of d_hidden, where there are several
-#define LOSS_FEW 64
-#define LOSS_PREPARE_ONE 2048
-#define LOSS_FEW_THREADS 256
+#define LOSS_FEW 128
+#define LOSS_PREPARE_ONE 1024
 // Tiles that the parts of d_hidden have at most.
 constexpr int64_t loss_part_tiles(int64_t padded_rows, int64_t columns, int64_t steps)
 {
@@ -88,7 +87,7 @@ constexpr int64_t loss_part_tiles(int64_t padded_rows, int64_t columns, int64_t 
     return tiles > LOSS_PARTS ? tiles : tiles * most < LOSS_PARTS ? tiles * most : LOSS_PARTS;
 }
 void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool backward);
-void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int blocks);
+void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int entries, bool gradient);
 void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool packed);
 void plaid_launch_loss_scores(hipStream_t st, const LossArgs &a, int dtype, bool backward);
 void plaid_launch_loss_gradients(hipStream_t st, const LossArgs &a, int dtype);
@@ -116,6 +115,18 @@ __device__ __forceinline__ int hidden_splits(const LossArgs &a, int live)
     }
     return best;
 }
+
+// G of a row, in units of its d_loss's power of two, times 2^15 in fp16: of a product, by the score it is.  The target's is the probability less
+// one, formed so that it keeps its digits where the probability is almost one.
+struct ScoreGradient {
+    float scale, top, rest, log_total, factor;
+    __device__ __forceinline__ ScoreGradient(const LossRow &x, float scale_, int dtype)
+        : scale(scale_), top(x.top), rest(x.log_total * LOG2E), log_total(x.log_total), factor(x.fraction * (dtype == PLAID_FP16 ? 0x1p15f : 1.0f))
+    {
+    }
+    __device__ __forceinline__ float other(float product) const { return __builtin_amdgcn_exp2f((product * scale - top) * LOG2E - rest) * factor; }
+    __device__ __forceinline__ float target(float product) const { return expm1f(product * scale - top - log_total) * factor; }
+};
 
 // Sixteen bytes of a row that starts at any element: the memory system takes such addresses.
 typedef i32x4 __attribute__((aligned(2))) i32x4_any;

@@ -71,18 +71,18 @@ int norm_workers(int64_t rows, int32_t width)
 
 struct LossPlan {
     bool few;
-    int blocks;
+    int entries;
     int64_t padded_rows, pitch, columns, piece;
     int64_t list_bytes, row_bytes, packed_bytes, scaled_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, d_part_bytes, bytes;
 };
 LossPlan plan_loss(const plaid_token_loss &a, bool backward)
 {
     LossPlan p = {};
-    p.few = !backward && a.rows <= LOSS_FEW;
-    if (p.few) {
+    p.few = a.rows <= LOSS_FEW;
+    p.entries = a.rows <= 64 ? (a.vocabulary >= 65536 ? 128 : 64) : (a.vocabulary >= 32768 ? 256 : 64);
+    if (p.few && !backward) {
         p.padded_rows = a.rows;
-        p.blocks = a.vocabulary >= 128 * 512 ? 2 : 1;
-        p.part_bytes = round16(ceil_div(a.vocabulary, 64 * p.blocks) * p.padded_rows * 8);
+        p.part_bytes = round16(ceil_div(a.vocabulary, p.entries) * p.padded_rows * 8);
         p.own_bytes = round16(p.padded_rows * 4);
         p.bytes = p.part_bytes + p.own_bytes;
         return p;
@@ -149,7 +149,7 @@ LossArgs loss_args(const plaid_token_loss &a, const LossPlan &p, void *workspace
     x.width = a.width, x.scale = a.scale;
     x.padded_rows = (int32_t)p.padded_rows, x.pitch = (int32_t)p.pitch, x.columns = (int32_t)p.columns, x.hidden_steps = (int32_t)ceil_div(p.piece, LOSS_STEP);
     char *w = (char *)workspace;
-    if (!p.few) {
+    if (backward || !p.few) {
         x.state = (int32_t *)w, x.list = (int32_t *)(w + 16), w += p.list_bytes;
         x.row = (LossRow *)w, w += p.row_bytes;
         x.packed = w, w += p.packed_bytes;
@@ -310,8 +310,8 @@ extern "C" int plaid_cross_entropy(const plaid_token_loss *args, void *workspace
     LossArgs x = loss_args(*args, p, workspace, false);
     if (p.few) {
         x.last = 1;
-        plaid_launch_loss_few(st, x, args->dtype, p.blocks);
-        plaid_launch_loss_join(st, x, (int)ceil_div(x.vocabulary, 64 * p.blocks), false);
+        plaid_launch_loss_few(st, x, args->dtype, p.entries, false);
+        plaid_launch_loss_join(st, x, (int)ceil_div(x.vocabulary, p.entries), false);
         return launched();
     }
     plaid_launch_loss_pack(st, x, args->dtype, false);
@@ -343,7 +343,8 @@ extern "C" int plaid_cross_entropy_backward(const plaid_token_loss *args, const 
     plaid_launch_loss_pack(st, x, args->dtype, true);
     for (x.first = 0; x.first < x.vocabulary; x.first += p.piece) {
         x.piece = (int32_t)(x.vocabulary - x.first < p.piece ? x.vocabulary - x.first : p.piece);
-        plaid_launch_loss_scores(st, x, args->dtype, true);
+        if (p.few) plaid_launch_loss_few(st, x, args->dtype, p.entries, true);
+        else plaid_launch_loss_scores(st, x, args->dtype, true);
         plaid_launch_loss_gradients(st, x, args->dtype);
     }
     if (x.d_hidden) plaid_launch_loss_d_hidden_join(st, x, args->dtype);
