@@ -7,12 +7,13 @@ is a call of its own, and inputs that require a gradient are refused where it is
 from __future__ import annotations
 
 import ctypes as ct
+import struct
 from typing import Optional, Tuple
 
 import torch
 
 from . import plaid as _p
-from .reader import _DTYPES, _is, _vector, _where, _workspace
+from .reader import _DTYPES, _is, _where, _workspace
 
 
 class plaid_token_loss(ct.Structure):
@@ -44,42 +45,71 @@ def _states(t: torch.Tensor, name: str, dim: Optional[int] = 2) -> torch.device:
     return t.device
 
 
-def _no_autograd(backward: str, **tensors) -> None:
-    if torch.is_grad_enabled():
-        for name, t in tensors.items():
-            if t is not None and t.requires_grad:
-                raise ValueError(f"{name} requires a gradient, which this call does not record: call it in torch.no_grad(), or in a "
-                                 f"torch.autograd.Function whose backward calls {backward}")
+def _not_recorded(backward: str, **tensors) -> None:
+    """Called where autograd is enabled and one of the tensors may require a gradient."""
+    for name, t in tensors.items():
+        if t is not None and t.requires_grad:
+            raise ValueError(f"{name} requires a gradient, which this call does not record: call it in torch.no_grad(), or in a "
+                             f"torch.autograd.Function whose backward calls {backward}")
+
+
+_recording = torch.is_grad_enabled
 
 
 def _rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
     """A matrix whose rows are contiguous, and from one row to the next."""
-    n, width = t.shape
-    if (width > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < 0):
+    row, one = t.stride()
+    if one != 1 and t.shape[1] > 1:
         t = t.contiguous()
-    return t, t.stride(0) if n > 1 else width
+        return t, t.shape[1]
+    return t, row if t.shape[0] > 1 else t.shape[1]
 
 
 def _aligned_rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
     """The same where the kernels want rows of whole 16-byte pieces."""
     n, width = t.shape
-    stride = t.stride(0) if n > 1 else width
-    if (width > 1 and t.stride(1) != 1) or stride % 8 or not 0 <= stride < 1 << 24 or t.data_ptr() % 16:
+    stride, one = t.stride()
+    if n < 2:
+        stride = width
+    if (one != 1 and width > 1) or stride % 8 or stride >= 1 << 24 or t.data_ptr() % 16:
         if t.numel():
             t = t.clone(memory_format=torch.contiguous_format)
         stride = width
     return t, stride
 
 
+def _parameter(t: Optional[torch.Tensor], name: str, x: torch.Tensor, width: int) -> Tuple[Optional[torch.Tensor], Optional[int]]:
+    """A weight or bias of x's rows, and its address."""
+    if t is None:
+        return None, None
+    if t.dtype is not x.dtype or t.dim() != 1 or t.shape[0] != width or t.device != x.device:
+        raise ValueError(f"{name} must hold {width} values of x's dtype on its device")
+    if t.stride(0) != 1:
+        t = t.contiguous()
+    return t, t.data_ptr()
+
+
+def _numbers(t: torch.Tensor, name: str, device: torch.device, size: Optional[int] = None) -> torch.Tensor:
+    """A vector of 64-bit integers."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int64 or t.dim() != 1 or t.device != device:
+        raise ValueError(f"{name} must be a tensor of dtype torch.int64 with 1 dimension on {device}")
+    if size is not None and t.shape[0] != size:
+        raise ValueError(f"{name} must hold {size} values, got {t.shape[0]}")
+    return t if t.is_contiguous() else t.contiguous()
+
+
 def plaid_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
     """scale * table[ids] for a table [vocabulary, width] and ids [n] int64; zeros for an id outside the vocabulary."""
     dev = _states(table, "table")
-    _no_autograd("plaid_embedding_backward", table=table)
-    ids = _vector(ids, "ids", torch.int64, dev)
+    if _recording() and table.requires_grad:
+        _not_recorded("plaid_embedding_backward", table=table)
+    ids = _numbers(ids, "ids", dev)
     table, stride = _rows(table)
-    out = torch.empty((ids.shape[0], table.shape[1]), dtype=table.dtype, device=dev)
-    _p._check(_p.load_library().plaid_embedding(table.data_ptr(), stride, table.shape[0], table.shape[1], ids.data_ptr(), ids.shape[0], float(scale),
-                                                out.data_ptr(), _DTYPES[table.dtype], *_where(dev)))
+    vocabulary, width = table.shape
+    n = ids.shape[0]
+    out = table.new_empty((n, width))
+    _p._check(_p.load_library().plaid_embedding(table.data_ptr(), stride, vocabulary, width, ids.data_ptr(), n, scale, out.data_ptr(), _DTYPES[table.dtype],
+                                                *_where(dev)))
     return out
 
 
@@ -88,11 +118,11 @@ def plaid_embedding_backward(d_out: torch.Tensor, ids: torch.Tensor, vocabulary:
     """The gradient [vocabulary, width] of plaid_embedding's table from that of its result, d_out [n, width]: dense, or added in place to
     `add_to`, which it then returns (a contiguous gradient of the same table from another use)."""
     dev = _states(d_out, "d_out")
-    ids = _vector(ids, "ids", torch.int64, dev, d_out.shape[0])
+    ids = _numbers(ids, "ids", dev, d_out.shape[0])
     d_out, stride = _rows(d_out)
     n, width = d_out.shape
     if add_to is None:
-        d_table = torch.empty((vocabulary, width), dtype=d_out.dtype, device=dev)
+        d_table = d_out.new_empty((vocabulary, width))
     else:
         d_table = _is(add_to, "add_to", d_out.dtype, 2, dev)
         if tuple(d_table.shape) != (vocabulary, width) or not d_table.is_contiguous():
@@ -101,7 +131,7 @@ def plaid_embedding_backward(d_out: torch.Tensor, ids: torch.Tensor, vocabulary:
     need = ct.c_int64(0)
     _p._check(lib.plaid_embedding_backward_workspace(n, vocabulary, width, ct.byref(need)))
     work, ptr = _workspace(need.value, dev)
-    _p._check(lib.plaid_embedding_backward(d_out.data_ptr(), stride, vocabulary, width, ids.data_ptr(), n, float(scale), 0 if add_to is None else 1,
+    _p._check(lib.plaid_embedding_backward(d_out.data_ptr(), stride, vocabulary, width, ids.data_ptr(), n, scale, 0 if add_to is None else 1,
                                            d_table.data_ptr(), _DTYPES[d_out.dtype], ptr, need.value, *_where(dev)))
     return d_table
 
@@ -111,27 +141,20 @@ def plaid_dropout(x: torch.Tensor, p: float, rng: torch.Tensor, residual: Option
     on x's device: a seed, and a number that no other call of the program has.  The gradient of x is the same call on the result's
     gradient, without a residual; the residual's is the result's."""
     dev = _states(x, "x", None)
-    _no_autograd("plaid_dropout", x=x, residual=residual)
-    rng = _vector(rng, "rng", torch.int64, dev, 2)
-    x = x.contiguous()
+    if _recording() and (x.requires_grad or residual is not None):
+        _not_recorded("plaid_dropout", x=x, residual=residual)
+    rng = _numbers(rng, "rng", dev, 2)
+    if not x.is_contiguous():
+        x = x.contiguous()
+    other = None
     if residual is not None:
-        _is(residual, "residual", x.dtype, x.dim(), dev)
-        if residual.shape != x.shape:
-            raise ValueError("residual must have x's shape")
+        if not isinstance(residual, torch.Tensor) or residual.dtype is not x.dtype or residual.shape != x.shape or residual.device != dev:
+            raise ValueError("residual must have x's shape and dtype on its device")
         residual = residual.contiguous()
+        other = residual.data_ptr()
     out = torch.empty_like(x)
-    _p._check(_p.load_library().plaid_dropout(x.data_ptr(), None if residual is None else residual.data_ptr(), x.numel(), float(p), rng.data_ptr(),
-                                              out.data_ptr(), _DTYPES[x.dtype], *_where(dev)))
+    _p._check(_p.load_library().plaid_dropout(x.data_ptr(), other, x.numel(), p, rng.data_ptr(), out.data_ptr(), _DTYPES[x.dtype], *_where(dev)))
     return out
-
-
-def _parameters(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor]):
-    dev, width = x.device, x.shape[1]
-    if weight is not None:
-        weight = _vector(weight, "weight", x.dtype, dev, width)
-    if bias is not None:
-        bias = _vector(bias, "bias", x.dtype, dev, width)
-    return weight, bias
 
 
 def plaid_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
@@ -139,14 +162,15 @@ def plaid_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bia
     """Layer norm of the rows of x [rows, width], times weight [width], plus bias [width].  With return_statistics also what
     plaid_layer_norm_backward wants, each row's mean and 1 / sqrt(variance + eps), [rows, 2] float32."""
     dev = _states(x, "x")
-    _no_autograd("plaid_layer_norm_backward", x=x, weight=weight, bias=bias)
-    weight, bias = _parameters(x, weight, bias)
+    if _recording():
+        _not_recorded("plaid_layer_norm_backward", x=x, weight=weight, bias=bias)
     x, stride = _rows(x)
     rows, width = x.shape
-    out = torch.empty((rows, width), dtype=x.dtype, device=dev)
-    statistics = torch.empty((rows, 2), dtype=torch.float32, device=dev) if return_statistics else None
-    _p._check(_p.load_library().plaid_layer_norm(x.data_ptr(), stride, None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(),
-                                                 rows, width, float(eps), out.data_ptr(), None if statistics is None else statistics.data_ptr(),
+    weight, w = _parameter(weight, "weight", x, width)
+    bias, b = _parameter(bias, "bias", x, width)
+    out = torch.empty_like(x) if stride == width else x.new_empty((rows, width))
+    statistics = x.new_empty((rows, 2), dtype=torch.float32) if return_statistics else None
+    _p._check(_p.load_library().plaid_layer_norm(x.data_ptr(), stride, w, b, rows, width, eps, out.data_ptr(), None if statistics is None else statistics.data_ptr(),
                                                  _DTYPES[x.dtype], *_where(dev)))
     return (out, statistics) if return_statistics else out
 
@@ -157,14 +181,15 @@ def plaid_layer_norm_backward(d_out: torch.Tensor, x: torch.Tensor, weight: Opti
     dev = _states(x, "x")
     if _is(d_out, "d_out", x.dtype, 2, dev).shape != x.shape:
         raise ValueError("d_out must have x's shape")
-    weight, bias = _parameters(x, weight, bias)
     rows, width = x.shape
+    weight, w = _parameter(weight, "weight", x, width)
+    bias, _ = _parameter(bias, "bias", x, width)
     if _is(statistics, "statistics", torch.float32, 2, dev).shape != (rows, 2):
         raise ValueError("statistics must be what plaid_layer_norm returned")
     statistics = statistics.contiguous()
     x, stride = _rows(x)
     d_out, d_stride = _rows(d_out)
-    dx = torch.empty((rows, width), dtype=x.dtype, device=dev)
+    dx = torch.empty_like(x) if stride == width else x.new_empty((rows, width))
     dweight = None if weight is None else torch.empty_like(weight)
     dbias = None if bias is None else torch.empty_like(bias)
     lib = _p.load_library()
@@ -172,24 +197,27 @@ def plaid_layer_norm_backward(d_out: torch.Tensor, x: torch.Tensor, weight: Opti
     if weight is not None or bias is not None:
         _p._check(lib.plaid_layer_norm_backward_workspace(rows, width, ct.byref(need)))
     work, ptr = _workspace(need.value, dev)
-    address = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    _p._check(lib.plaid_layer_norm_backward(d_out.data_ptr(), d_stride, x.data_ptr(), stride, address(weight), statistics.data_ptr(), rows, width,
-                                            dx.data_ptr(), address(dweight), address(dbias), _DTYPES[x.dtype], ptr, need.value, *_where(dev)))
+    _p._check(lib.plaid_layer_norm_backward(d_out.data_ptr(), d_stride, x.data_ptr(), stride, w, statistics.data_ptr(), rows, width, dx.data_ptr(),
+                                            None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(), _DTYPES[x.dtype], ptr,
+                                            need.value, *_where(dev)))
     return dx, dweight, dbias
+
+
+_PACKED = struct.Struct("2i2qf2P2q3P")  # plaid_token_loss's fields, as the C compiler lays them out
 
 
 def _loss_args(hidden, weight, targets, scale, loss, lse) -> plaid_token_loss:
     """hidden, weight: what _aligned_rows gave."""
     (h, h_stride), (w, w_stride) = hidden, weight
-    return plaid_token_loss(_DTYPES[h.dtype], h.shape[1], h.shape[0], w.shape[0], float(scale), h.data_ptr(), w.data_ptr(), h_stride, w_stride,
-                            targets.data_ptr(), None if loss is None else loss.data_ptr(), None if lse is None else lse.data_ptr())
+    return plaid_token_loss.from_buffer_copy(_PACKED.pack(_DTYPES[h.dtype], h.shape[1], h.shape[0], w.shape[0], scale, h.data_ptr(), w.data_ptr(), h_stride, w_stride,
+                                                          targets.data_ptr(), 0 if loss is None else loss.data_ptr(), 0 if lse is None else lse.data_ptr()))
 
 
 def _loss_inputs(hidden, weight, targets):
     dev = _states(hidden, "hidden")
     if _is(weight, "weight", hidden.dtype, 2, dev).shape[1] != hidden.shape[1]:
         raise ValueError("hidden and weight must have rows of one width")
-    targets = _vector(targets, "targets", torch.int64, dev, hidden.shape[0])
+    targets = _numbers(targets, "targets", dev, hidden.shape[0])
     return _aligned_rows(hidden), _aligned_rows(weight), targets
 
 
@@ -198,10 +226,12 @@ def plaid_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: tor
     [vocabulary, width], targets [rows] int64 -> [rows] float32, zero for a target outside the vocabulary.  With return_lse also what
     plaid_cross_entropy_backward wants, the logarithm of the softmax's sum as two numbers to be added, [rows, 2] float32."""
     rows, table, targets = _loss_inputs(hidden, weight, targets)
-    _no_autograd("plaid_cross_entropy_backward", hidden=hidden, weight=weight)
+    if _recording():
+        _not_recorded("plaid_cross_entropy_backward", hidden=hidden, weight=weight)
     dev = hidden.device
-    loss = torch.empty(hidden.shape[0], dtype=torch.float32, device=dev)
-    lse = torch.empty((hidden.shape[0], 2), dtype=torch.float32, device=dev) if return_lse else None
+    n = hidden.shape[0]
+    loss = hidden.new_empty(n, dtype=torch.float32)
+    lse = hidden.new_empty((n, 2), dtype=torch.float32) if return_lse else None
     lib = _p.load_library()
     a = _loss_args(rows, table, targets, scale, loss, lse)
     need = ct.c_int64(0)
@@ -225,8 +255,8 @@ def plaid_cross_entropy_backward(d_loss: torch.Tensor, hidden: torch.Tensor, wei
     if _is(lse, "lse", torch.float32, 2, dev).shape != (n, 2):
         raise ValueError("lse must be what plaid_cross_entropy returned")
     lse = lse.contiguous()
-    d_hidden = torch.empty((n, hidden.shape[1]), dtype=hidden.dtype, device=dev)
-    d_weight = torch.empty(tuple(weight.shape), dtype=hidden.dtype, device=dev)
+    d_hidden = hidden.new_empty(hidden.shape)
+    d_weight = hidden.new_empty(weight.shape)
     lib = _p.load_library()
     a = _loss_args(rows, table, targets, scale, None, lse)
     need = ct.c_int64(0)
