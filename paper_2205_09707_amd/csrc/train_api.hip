@@ -11,6 +11,7 @@ int check_dtype(int32_t dtype)
     if (dtype != PLAID_BF16 && dtype != PLAID_FP16) FAIL("dtype %d is neither PLAID_BF16 nor PLAID_FP16", dtype);
     return PLAID_OK;
 }
+constexpr int UNITS = 256;  // compute units
 constexpr int64_t MOST_ROWS = 1ll << 30, MOST_STRIDE = 1ll << 32;
 
 int check_table(int64_t n, int64_t vocabulary, int32_t width, const int64_t *ids, int32_t dtype)
@@ -79,7 +80,11 @@ LossPlan plan_loss(const plaid_token_loss &a, bool backward)
 {
     LossPlan p = {};
     p.few = a.rows <= LOSS_FEW;
-    p.entries = a.rows <= 64 ? (a.vocabulary >= 65536 ? 128 : 64) : (a.vocabulary >= 32768 ? 256 : 64);
+    // Entries of a few rows' workgroup: 64 where all workgroups then find room on the chip at once, else more, so that fewer of them read the
+    // rows.  us with 64 and 128, width 1024: 16 rows on 40000 entries 16.3 and 17.1, 48 on 40000 18.2 and 19.3, on 50021 23.9 and 20.9; with 64 and
+    // 256, 90 rows on 50000 49 and 23
+    const int64_t stage = 3 * (64 + 16 * ceil_div(a.rows, 16)) * 128, resident = UNITS * (160 * 1024 / (stage + 2048));
+    p.entries = ceil_div(a.vocabulary, 64) <= resident ? 64 : a.rows <= 64 ? 128 : 256;
     if (p.few && !backward) {
         p.padded_rows = a.rows;
         p.part_bytes = round16(ceil_div(a.vocabulary, p.entries) * p.padded_rows * 8);
