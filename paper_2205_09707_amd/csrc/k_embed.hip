@@ -76,17 +76,19 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedArgs e, int64_t pie
     __shared__ int keys[SORT_ONE], counts[WAVES][256], totals[256];
     __shared__ uint16_t places[SORT_ONE];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)e.n;
+    const int each = (n + 1023) / 1024, base = wave * (each * 64) + lane;  // a wave's places: each times 64
     int key[EACH], place[EACH], rank[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        place[i] = wave * (EACH * 64) + i * 64 + lane;
-        key[i] = place[i] < n ? token_key(e, place[i]) : 0;
+        place[i] = base + i * 64;
+        key[i] = i < each && place[i] < n ? token_key(e, place[i]) : 0;
     }
     for (int shift = 0; shift < e.bits; shift += 8) {
         for (int i = threadIdx.x; i < WAVES * 256; i += 1024) (&counts[0][0])[i] = 0;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) rank[i] = rank_digit((key[i] >> shift) & 255, wave * (EACH * 64) + i * 64 + lane < n, 8, counts[wave]);
+        for (int i = 0; i < EACH; ++i)
+            if (i < each) rank[i] = rank_digit((key[i] >> shift) & 255, base + i * 64 < n, 8, counts[wave]);
         __syncthreads();
         int sum = 0;
         if (threadIdx.x < 256)
@@ -108,7 +110,7 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedArgs e, int64_t pie
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-            if (wave * (EACH * 64) + i * 64 + lane < n) {
+            if (i < each && base + i * 64 < n) {
                 const int d = (key[i] >> shift) & 255;
                 int to = rank[i] + counts[wave][d] + (d & 63 ? totals[d - 1] : 0);
                 for (int w = 0; w < d >> 6; ++w) to += totals[64 * w + 63];
@@ -117,14 +119,14 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedArgs e, int64_t pie
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int at = wave * (EACH * 64) + i * 64 + lane;
-            if (at < n) key[i] = keys[at], place[i] = places[at];
+            const int at = base + i * 64;
+            if (i < each && at < n) key[i] = keys[at], place[i] = places[at];
         }
     }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        const int at = wave * (EACH * 64) + i * 64 + lane;
-        if (at < n) e.keys[0][at] = key[i], e.places[0][at] = place[i];
+        const int at = base + i * 64;
+        if (i < each && at < n) e.keys[0][at] = key[i], e.places[0][at] = place[i];
     }
 }
 

@@ -11,7 +11,7 @@ template <int LANES>
 __device__ __forceinline__ float2 row_sum(float2 s, float2 *lds)
 {
 #pragma unroll
-    for (int o = 32; o; o >>= 1) s.x += __shfl_xor(s.x, o), s.y += __shfl_xor(s.y, o);
+    for (int o = (LANES < 64 ? LANES : 64) / 2; o; o >>= 1) s.x += __shfl_xor(s.x, o), s.y += __shfl_xor(s.y, o);
     if constexpr (LANES > 64) {
         __syncthreads();  // the sums before have been read
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
@@ -30,7 +30,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
     __shared__ float2 lds[THREADS / 64];
     const int lane = threadIdx.x % LANES;
     const int64_t row = (int64_t)blockIdx.x * (THREADS / LANES) + threadIdx.x / LANES;
-    if (row >= a.rows) return;  // whole waves, or the whole workgroup
+    if (row >= a.rows) return;  // whole teams
     const char *x = a.x + row * a.x_stride;
     Eight v[C];
     float sum = 0.0f;
@@ -176,8 +176,13 @@ static void launch_norm(hipStream_t st, const NormArgs &a)
     const int pieces = (a.width + 7) / 8;
     const bool many = a.rows >= NORM_MANY;
 #define GO(LANES, C) norm_kernel<DT, LANES, C><<<(unsigned)((a.rows * LANES + 255) / (LANES < 256 ? 256 : LANES)), LANES < 256 ? 256 : LANES, 0, st>>>(a)
-    if (pieces <= 64) GO(64, 1);
+    if (pieces == 1) GO(1, 1);
+    else if (pieces <= 8) GO(8, 1);
+    else if (pieces <= 16) GO(16, 1);
+    else if (pieces <= 32) GO(32, 1);
+    else if (pieces <= 64) GO(64, 1);
     else if (pieces <= 128) GO(64, 2);
+    else if (pieces <= 192 && many) GO(64, 3);
     else if (pieces <= 256) many ? GO(64, 4) : GO(256, 1);
     else if (pieces <= 512) many ? GO(64, 8) : GO(256, 2);
     else if (pieces <= 1024) GO(256, 4);
@@ -189,8 +194,13 @@ static void launch_norm_backward(hipStream_t st, const NormArgs &a)
 {
     const int pieces = (a.width + 7) / 8;
 #define GO(LANES, C) norm_grad_kernel<DT, LANES, C><<<a.workers, LANES < 256 ? 256 : LANES, 0, st>>>(a)
-    if (pieces <= 64) GO(64, 1);
+    if (pieces == 1) GO(1, 1);
+    else if (pieces <= 8) GO(8, 1);
+    else if (pieces <= 16) GO(16, 1);
+    else if (pieces <= 32) GO(32, 1);
+    else if (pieces <= 64) GO(64, 1);
     else if (pieces <= 128) GO(64, 2);
+    else if (pieces <= 192) GO(64, 3);
     else if (pieces <= 256) GO(256, 1);
     else if (pieces <= 512) GO(256, 2);
     else if (pieces <= 1024) GO(256, 4);

@@ -21,7 +21,7 @@ struct EmbedArgs {
     __host__ __device__ int columns() const { return (width + 7) & ~7; }
 };
 // Up to this many tokens are sorted by one workgroup in one launch.
-#define SORT_ONE 4096
+#define SORT_ONE 8192
 #define SORT_TILE 1024
 void plaid_launch_embedding(hipStream_t st, const EmbedArgs &e, int dtype);
 void plaid_launch_embedding_backward(hipStream_t st, const EmbedArgs &e, int dtype);

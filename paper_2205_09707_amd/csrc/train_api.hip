@@ -63,10 +63,12 @@ int check_stride(const char *what, int64_t stride)
     if (stride < 0 || stride >= MOST_STRIDE) FAIL("the stride of %s is out of range", what);
     return PLAID_OK;
 }
+// Workgroups that go over the rows: teams of as many threads as a row has pieces of eight elements (as the launch has them), and at least two
+// rows a team.
 int norm_workers(int64_t rows, int32_t width)
 {
-    const int64_t teams = width <= 1024 ? 4 : 1, per = 2;  // at least `per` rows a team
-    const int64_t most = width <= 2048 ? 1024 : width <= 8192 ? 512 : 256, want = ceil_div(rows, teams * per);
+    const int pieces = (width + 7) / 8, lanes = pieces == 1 ? 1 : pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : pieces <= 192 ? 64 : 256;
+    const int64_t teams = 256 / lanes, most = width <= 2048 ? 1024 : width <= 8192 ? 512 : 256, want = ceil_div(rows, teams * 2);
     return (int)(want < 1 ? 1 : want < most ? want : most);
 }
 

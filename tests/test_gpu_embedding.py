@@ -24,7 +24,7 @@ def _inputs(n, vocabulary, width, dtype, seed=0, frequent=0.0, outside=0.1):
     return torch.randn(vocabulary, width, generator=g, device=DEV).to(dtype), ids, torch.randn(n, width, generator=g, device=DEV).to(dtype)
 
 
-SIZES = [(1, 1, 1), (1, 5, 8), (2, 1, 64), (33, 10, 7), (64, 300, 765), (70, 1000, 2048), (200, 50, 2056), (257, 100_000, 16), (5000, 3, 40), (4096, 700, 128),
+SIZES = [(1, 1, 1), (1, 5, 8), (2, 1, 64), (33, 10, 7), (64, 300, 765), (70, 1000, 2048), (200, 50, 2056), (257, 100_000, 16), (5000, 3, 40), (4096, 700, 128), (8192, 5000, 40), (8193, 70_000, 40), (1025, 300, 64),
          (4097, 700, 128), (20_011, 1000, 64), (30_000, 300_000, 24), (3, 70, 5000)]
 
 

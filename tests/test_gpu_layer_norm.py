@@ -38,7 +38,7 @@ def _check(pl, x, weight, bias, d, eps, what):
     return out
 
 
-WIDTHS = [1, 2, 7, 8, 9, 64, 511, 512, 520, 765, 1024, 1025, 2048, 2056, 4096, 4100, 8192, 8193, 16384]
+WIDTHS = [1, 2, 7, 8, 9, 64, 65, 128, 130, 200, 256, 257, 511, 512, 520, 765, 1024, 1025, 1500, 1537, 2048, 2056, 4096, 4100, 8192, 8193, 16384]
 
 
 @pytest.mark.parametrize("dtype", [BF, HALF])
@@ -49,7 +49,7 @@ def test_widths(pl, rows, width, dtype):
     _check(pl, x, w, b, d, 1e-5, "all")
 
 
-@pytest.mark.parametrize("rows,width", [(4001, 765), (9000, 64), (5000, 1024), (3000, 2048), (2100, 4096), (1300, 9000)])
+@pytest.mark.parametrize("rows,width", [(4001, 765), (9000, 64), (70_000, 7), (40_000, 120), (20_000, 250), (6000, 1500), (5000, 1024), (3000, 2048), (2100, 4096), (1300, 9000)])
 def test_more_rows_than_workers(pl, rows, width):
     x, w, b, d = _inputs(rows, width, BF, seed=rows)
     _check(pl, x, w, b, d, 1e-5, "all")
