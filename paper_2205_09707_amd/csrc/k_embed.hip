@@ -339,12 +339,13 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedArgs e, int team_s
     else fill_absent(e, blockIdx.x - chunk_blocks);
 }
 
-// 256 columns of a token that several chunks share: each of the four waves has a quarter of its parts.
+// Up to 256 columns of a token that several chunks share: the threads that have the same four columns have a stretch of its parts each.
 template <int DT>
-__global__ __launch_bounds__(256) void embed_grad_join_kernel(EmbedArgs e)
+__global__ __launch_bounds__(256) void embed_grad_join_kernel(EmbedArgs e, int lane_shift)
 {
-    __shared__ f32x4 lds[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = (blockIdx.y * 64 + lane) * 4, many = *e.shared;
+    __shared__ f32x4 lds[256];
+    const int lane = threadIdx.x & 63, column = threadIdx.x & ((1 << lane_shift) - 1), share = threadIdx.x >> lane_shift, shares = 256 >> lane_shift;
+    const int at = (blockIdx.y * 64 + column) * 4, many = *e.shared;
     const int *keys = e.keys[e.sorted];
     const int64_t columns = e.columns();
     for (int i = blockIdx.x; i < many; i += gridDim.x) {
@@ -356,18 +357,17 @@ __global__ __launch_bounds__(256) void embed_grad_join_kernel(EmbedArgs e)
             const uint64_t same = __ballot(p < e.n && keys[min(p, e.n - 1)] == key);
             more = same == ~0ull ? 64 : __ffsll((unsigned long long)~same) - 1;
         }
-        const int each = (parts + 3) / 4, first = wave * each, last = min(parts, first + each);
+        const int each = (parts + shares - 1) / shares, first = share * each, last = min(parts, first + each);
         f32x4 sum = {0, 0, 0, 0};
         if (at < columns) {
             const float *p = e.part + chunk * 2 * columns + at;  // part 0 has place 1 of its chunk, the others place 0
 #pragma unroll 8
             for (int k = first; k < last; ++k) sum += *(const f32x4 *)(p + (k == 0 ? 1 : 2 * k) * columns);
         }
-        lds[wave][lane] = sum;
+        lds[threadIdx.x] = sum;
         __syncthreads();
-        if (wave == 0 && at < e.width) {
-#pragma unroll
-            for (int w = 1; w < 4; ++w) sum += lds[w][lane];
+        if (share == 0 && at < e.width) {
+            for (int w = 1; w < min(shares, parts); ++w) sum += lds[(w << lane_shift) + column];
             char *row = e.d_table + ((int64_t)key * e.width + at) * 2;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -418,7 +418,10 @@ static void launch_backward(hipStream_t st, const EmbedArgs &e)
     const unsigned fill_blocks = !one && !e.add ? (unsigned)((e.vocabulary + 255) / 256) : 0;
     if (shift >= 6) embed_grad_kernel<DT, true><<<chunk_blocks + fill_blocks, 256, 0, st>>>(e, shift, chunk_blocks, (unsigned)slices);
     else embed_grad_kernel<DT, false><<<chunk_blocks + fill_blocks, 256, 0, st>>>(e, shift, chunk_blocks, (unsigned)slices);
-    if (chunks > 1) embed_grad_join_kernel<DT><<<dim3((unsigned)(chunks < 1024 ? chunks : 1024), (unsigned)((e.width + 255) / 256)), 256, 0, st>>>(e);
+    if (chunks > 1) {
+        const int lane_shift = shift + 1 < 6 ? shift + 1 : 6;  // a team's thread has eight columns, one of these four
+        embed_grad_join_kernel<DT><<<dim3((unsigned)(chunks < 1024 ? chunks : 1024), (unsigned)((e.width + 255) / 256)), 256, 0, st>>>(e, lane_shift);
+    }
 }
 void plaid_launch_embedding_backward(hipStream_t st, const EmbedArgs &e, int dtype)
 {
