@@ -407,7 +407,7 @@ int plaid_cross_attention_workspace(const plaid_attention *args, int32_t backwar
 
 /* Rows of a table for n tokens: out[t] = scale * table[ids[t]]; zeros for an id outside [0, vocabulary).
  *   table  [vocabulary][width], table_stride apart     ids  [n] int64     out  [n][width], 16-byte aligned
- * width 1 .. 2^20, n and vocabulary up to 2^30. */
+ * width 1 .. 2^20, n and vocabulary up to 2^30, n * width and vocabulary * width up to 2^40. */
 int plaid_embedding(const void *table, int64_t table_stride, int64_t vocabulary, int32_t width, const int64_t *ids, int64_t n,
                     float scale, void *out, int32_t dtype, int device, void *hip_stream);
 /* The table's gradient: d_table[v] = scale * the sum of d_out[t] over the tokens t of id v, zeros where there is none; with add != 0 the

@@ -173,7 +173,7 @@ __device__ __forceinline__ float2 join_parts(float2 x, float2 y)
 
 // --- few rows -------------------------------------------------------------------------------------------------------------------
 // The vocabulary is read at the rate of memory if enough of it is under way: a workgroup has 64 BLOCKS entries, a quarter for each of its four
-// waves, and up to 16 GROUPS rows; 64 columns of both go straight into LDS, some steps ahead of the products.  Forward it takes the caller's
+// waves, and up to 16 GROUPS rows (more than 128: those of 128 after those); 64 columns of both go straight into LDS, some steps ahead of the products.  Forward it takes the caller's
 // rows, all of them (a row without a target has its own column of the result, and is left out when parts are joined); backward (GRADIENT) the
 // packed ones, and leaves G over the piece as the products take it, with zeros up to whole steps of 64 rows and entries.
 template <int DT, int WAVES, int BLOCKS, int GROUPS, bool GRADIENT>
@@ -184,7 +184,8 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
     __shared__ __align__(16) char lds_w[STAGES][ENTRIES * 128], lds_h[STAGES][GROUPS * 16 * 128];
     __shared__ float2 joined[WAVES][16 * GROUPS];
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), l = lane & 15, q = lane >> 4;
-    const int rows = GRADIENT ? uniform_load(a.state) : (int)a.rows;
+    const int rows = GRADIENT ? uniform_load(a.state) : (int)a.rows, row0 = blockIdx.y * (16 * GROUPS);
+    if (GRADIENT && row0 >= (rows + LOSS_STEP - 1) / LOSS_STEP * LOSS_STEP && row0 > 0) return;  // no one reads what would be here
     const int64_t first = GRADIENT ? a.first : 0, end = GRADIENT ? a.first + a.piece : a.vocabulary, v0 = first + (int64_t)blockIdx.x * ENTRIES;
     // a load has eight rows of 128 bytes, whose chunks change places as lds_chunk says; with fewer pieces of states than waves some are brought twice
     const char *from[LOADS];
@@ -196,7 +197,8 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
         chunk[i] = (lane & 7) ^ swizzle<64>(row);
         to[i] = piece * 1024;
         if (w) from[i] = a.weight + min(v0 + row, a.vocabulary - 1) * a.weight_stride;
-        else from[i] = GRADIENT ? a.packed + row * 128 : a.hidden + min((int64_t)row, a.rows - 1) * a.hidden_stride;
+        else if (GRADIENT) from[i] = a.packed + (int64_t)(row0 / LOSS_TILE) * (a.pitch / LOSS_STEP) * (LOSS_TILE * 128) + (row0 % LOSS_TILE + row) * 128;
+        else from[i] = a.hidden + min((int64_t)row0 + row, a.rows - 1) * a.hidden_stride;
         from[i] += chunk[i] * 16;
     }
     const int steps = (a.width + 63) / 64, left = a.width - (steps - 1) * 64;
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
         const int pieces = (a.piece + LOSS_TILE - 1) / LOSS_TILE;
 #pragma unroll
         for (int j = 0; j < GROUPS; ++j) {
-            const int t = 16 * j + l;
+            const int t = row0 + 16 * j + l;
             const bool there = t < rows;
             const LossRow x = there ? a.row[t] : LossRow{-1, 0, 0.0f, 0.0f, 0.0f};
             const ScoreGradient gradient(x, a.scale, DT);
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
     }
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
-        const int64_t t = 16 * j + l;
+        const int64_t t = row0 + 16 * j + l;
         const int64_t target = t < rows ? a.targets[t] : -1;
         float most = -INFINITY;
 #pragma unroll
@@ -299,11 +301,11 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
         if (lane < 16) joined[wave][16 * j + l] = {most, sum};
     }
     __syncthreads();
-    if (threadIdx.x < 16 * GROUPS && threadIdx.x < a.rows) {
+    if (threadIdx.x < 16 * GROUPS && row0 + (int)threadIdx.x < rows) {
         const int t = threadIdx.x;
         float2 x = join_parts(join_parts(joined[0][t], joined[1][t]), join_parts(joined[2][t], joined[3][t]));
         if constexpr (WAVES == 8) x = join_parts(x, join_parts(join_parts(joined[4][t], joined[5][t]), join_parts(joined[6][t], joined[7][t])));
-        a.part[(int64_t)blockIdx.x * a.padded_rows + t] = x;
+        a.part[(int64_t)blockIdx.x * a.padded_rows + row0 + t] = x;
     }
 }
 
@@ -312,7 +314,7 @@ static void launch_few(hipStream_t st, const LossArgs &a, bool gradient)
 {
     const int groups = (int)((a.rows + 15) / 16);
     const int64_t entries = gradient ? a.piece : a.vocabulary;
-    const unsigned grid = (unsigned)((entries + 16 * WAVES * BLOCKS - 1) / (16 * WAVES * BLOCKS));
+    const dim3 grid((unsigned)((entries + 16 * WAVES * BLOCKS - 1) / (16 * WAVES * BLOCKS)), (unsigned)((a.rows + 127) / 128 < 1 ? 1 : (a.rows + 127) / 128));
 #define GO(G, GRADIENT) loss_few_kernel<DT, WAVES, BLOCKS, G, GRADIENT><<<grid, WAVES * 64, 0, st>>>(a)
     if constexpr (WAVES == 8) {
         if (gradient) GO(8, true);

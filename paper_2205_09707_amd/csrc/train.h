@@ -76,7 +76,7 @@ struct LossArgs {
 #define LOSS_TILE 256
 #define LOSS_STEP 64
 #define LOSS_PART 128
-#define LOSS_PART_STEPS 12
+#define LOSS_PART_STEPS 6
 #define LOSS_PARTS 512  // tiles of all parts of d_hidden, where there are several
 #define LOSS_FEW 128
 #define LOSS_PREPARE_ONE 1024

@@ -12,7 +12,7 @@ int check_dtype(int32_t dtype)
     return PLAID_OK;
 }
 constexpr int UNITS = 256;  // compute units
-constexpr int64_t MOST_ROWS = 1ll << 30, MOST_STRIDE = 1ll << 32;
+constexpr int64_t MOST_ROWS = 1ll << 30, MOST_STRIDE = 1ll << 32, MOST_VALUES = 1ll << 40;
 
 int check_table(int64_t n, int64_t vocabulary, int32_t width, const int64_t *ids, int32_t dtype)
 {
@@ -20,6 +20,7 @@ int check_table(int64_t n, int64_t vocabulary, int32_t width, const int64_t *ids
     if (n < 0 || n > MOST_ROWS) FAIL("n %lld out of range", (long long)n);
     if (vocabulary < 1 || vocabulary > MOST_ROWS) FAIL("vocabulary %lld out of range", (long long)vocabulary);
     if (width < 1 || width > (1 << 20)) FAIL("width %d out of range", width);
+    if (vocabulary * width > MOST_VALUES || n * width > MOST_VALUES) FAIL("a table or result of more than 2^40 values");
     if (n > 0 && (!ids || misaligned(ids, 8))) FAIL("ids is null or misaligned");
     return PLAID_OK;
 }
@@ -85,12 +86,15 @@ struct LossPlan {
 LossPlan plan_loss(const plaid_token_loss &a, bool backward)
 {
     LossPlan p = {};
-    p.few = a.rows <= LOSS_FEW;
+    // Tiles of 64 entries and 128 rows in place of 256 and 256 where the larger ones would leave much of the chip idle.  us of a forward call with the
+    // small and the large ones (and so many small ones), width 512: 300 rows on 2600 entries 19 and 30 (123), 1000 on 2600 20 and 30 (328), 500 on
+    // 11000 28 and 32 (688); width 1024: 2000 on 2000 28 and 46 (512), 200 on 30000 45 and 43 (938)
+    p.few = a.rows <= LOSS_FEW || ceil_div(a.vocabulary, 64) * ceil_div(a.rows, LOSS_FEW) <= 3 * UNITS;
     // Entries of a few rows' workgroup: 64 where all workgroups then find room on the chip at once, else more, so that fewer of them read the
     // rows.  us with 64 and 128, width 1024: 16 rows on 40000 entries 16.3 and 17.1, 48 on 40000 18.2 and 19.3, on 50021 23.9 and 20.9; with 64 and
     // 256, 90 rows on 50000 49 and 23
     const int64_t stage = 3 * (64 + 16 * ceil_div(a.rows, 16)) * 128, resident = UNITS * (160 * 1024 / (stage + 2048));
-    p.entries = ceil_div(a.vocabulary, 64) <= resident ? 64 : a.rows <= 64 ? 128 : 256;
+    p.entries = ceil_div(a.vocabulary, 64) <= resident || a.rows > LOSS_FEW ? 64 : a.rows <= 64 ? 128 : 256;
     if (p.few && !backward) {
         p.padded_rows = a.rows;
         p.part_bytes = round16(ceil_div(a.vocabulary, p.entries) * p.padded_rows * 8);
@@ -199,7 +203,8 @@ extern "C" int plaid_embedding(const void *table, int64_t table_stride, int64_t 
 extern "C" int plaid_embedding_backward_workspace(int64_t n, int64_t vocabulary, int32_t width, int64_t *bytes)
 {
     if (!bytes) FAIL("bytes is null");
-    if (n < 0 || n > MOST_ROWS || vocabulary < 1 || vocabulary > MOST_ROWS || width < 1 || width > (1 << 20)) FAIL("n, vocabulary or width out of range");
+    if (n < 0 || n > MOST_ROWS || vocabulary < 1 || vocabulary > MOST_ROWS || width < 1 || width > (1 << 20) || vocabulary * width > MOST_VALUES || n * width > MOST_VALUES)
+        FAIL("n, vocabulary or width out of range");
     *bytes = plan_embedding(n, vocabulary, width).bytes;
     return PLAID_OK;
 }

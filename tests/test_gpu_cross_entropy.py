@@ -47,7 +47,8 @@ def _check(pl, h, w, t, d, scale, what="", forward_only=False):
 
 
 SIZES = [(1, 1, 8), (1, 2, 64), (5, 17, 72), (16, 256, 128), (17, 1000, 512), (33, 257, 200), (48, 3001, 264), (64, 255, 96), (65, 300, 64), (100, 128, 8),
-         (255, 1000, 256), (256, 256, 256), (257, 513, 320), (300, 5000, 768), (700, 3001, 520), (3, 20_000, 136)]
+         (255, 1000, 256), (256, 256, 256), (257, 513, 320), (300, 5000, 768), (700, 3001, 520), (3, 20_000, 136),
+         (129, 64, 64), (128, 40_000, 64), (1000, 9000, 72), (2050, 3000, 264), (1100, 30_000, 8)]
 
 
 @pytest.mark.parametrize("dtype", [BF, HALF])

@@ -37,7 +37,7 @@ def _call(f, defaults, over):
 EMBED = dict(table=A, table_stride=64, vocabulary=100, width=64, ids=A, n=5, scale=1.0, out=A, dtype=0, device=0, stream=None)
 EMBED_BACK = dict(d_out=A, d_out_stride=64, vocabulary=100, width=64, ids=A, n=5, scale=1.0, add=0, d_table=A, dtype=0, work=A, bytes=1 << 30, device=0, stream=None)
 TABLES = [dict(dtype=2), dict(dtype=-1), dict(n=-1), dict(n=(1 << 30) + 1), dict(vocabulary=0), dict(vocabulary=(1 << 30) + 1), dict(width=0), dict(width=(1 << 20) + 1),
-          dict(ids=None), dict(ids=4100)]
+          dict(ids=None), dict(ids=4100), dict(vocabulary=1 << 30, width=1 << 11), dict(n=1 << 30, width=1 << 11)]
 
 
 @pytest.mark.parametrize("over", TABLES + [dict(table=None), dict(table=ODD), dict(table_stride=-1), dict(table_stride=1 << 32), dict(out=None), dict(out=4098)])
@@ -59,7 +59,7 @@ def test_embedding_workspace(lib):
         return need.value
 
     assert 0 < of(0, 100, 64) < of(8, 100, 64) < of(9, 100, 64) < of(5000, 100, 64)
-    for bad in ((-1, 100, 64), (1, 0, 64), (1, 100, 0), (1 << 31, 100, 64)):
+    for bad in ((-1, 100, 64), (1, 0, 64), (1, 100, 0), (1 << 31, 100, 64), (1, 1 << 30, 1 << 11)):
         assert lib.plaid_embedding_backward_workspace(*bad, ct.byref(need)) == E
     assert lib.plaid_embedding_backward_workspace(1, 1, 1, None) == E
     assert _call(lib.plaid_embedding, EMBED, dict(n=0, ids=None, table=None, out=None)) == OK  # nothing is launched
