@@ -41,8 +41,10 @@ __device__ __forceinline__ void pack_row(const LossArgs &a, int place, int64_t t
     char *to = a.packed + (int64_t)(place / LOSS_TILE) * (a.pitch / LOSS_STEP) * BLOCK + place % LOSS_TILE * (2 * LOSS_STEP);
     char *scaled = BACKWARD ? a.scaled + (int64_t)(place / LOSS_STEP) * (a.columns / LOSS_TILE) * BLOCK + place % LOSS_STEP * (2 * LOSS_TILE) : nullptr;
     const float power = ldexpf(1.0f, shift);
+    const int sign = a.scale < 0.0f ? (int)0x80008000u : 0;
     for (int at = threadIdx.x * 8; at < (BACKWARD ? a.columns : a.pitch); at += 1024) {
-        const i32x4 w = t >= 0 && at < a.width ? *(const i32x4 *)(from + 2 * at) : i32x4{0, 0, 0, 0};
+        i32x4 w = t >= 0 && at < a.width ? *(const i32x4 *)(from + 2 * at) : i32x4{0, 0, 0, 0};
+        w ^= i32x4{sign, sign, sign, sign};
         if (at < a.pitch) *(i32x4 *)(to + (int64_t)(at / LOSS_STEP) * BLOCK + at % LOSS_STEP * 2) = w;
         if (BACKWARD) {
             Eight v = unpack8<DT>(w);
@@ -164,11 +166,11 @@ void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool b
     else loss_pack_kernel<PLAID_FP16, true><<<grid, 128, 0, st>>>(a);
 }
 
-// Maxima and sums of exponentials beside them, of two parts.
-__device__ __forceinline__ float2 join_parts(float2 x, float2 y)
+// Largest products and sums of exponentials beside them, of two parts; f: exponent_factor.
+__device__ __forceinline__ float2 join_parts(float2 x, float2 y, float f)
 {
     const float m = fmaxf(x.x, y.x), base = m == -INFINITY ? 0.0f : m;
-    return {m, x.y * __builtin_amdgcn_exp2f((x.x - base) * LOG2E) + y.y * __builtin_amdgcn_exp2f((y.x - base) * LOG2E)};
+    return {m, x.y * __builtin_amdgcn_exp2f((x.x - base) * f) + y.y * __builtin_amdgcn_exp2f((y.x - base) * f)};
 }
 
 // --- few rows -------------------------------------------------------------------------------------------------------------------
@@ -256,7 +258,7 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
             const int t = row0 + 16 * j + l;
             const bool there = t < rows;
             const LossRow x = there ? a.row[t] : LossRow{-1, 0, 0.0f, 0.0f, 0.0f};
-            const ScoreGradient gradient(x, a.scale, DT);
+            const ScoreGradient gradient(x, a, DT);
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) {
                 float g[4];
@@ -274,6 +276,7 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
         }
         return;
     }
+    const float sign = a.scale < 0.0f ? -1.0f : 1.0f, f = exponent_factor(a);
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
         const int64_t t = row0 + 16 * j + l;
@@ -284,7 +287,7 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int64_t v = mine + 16 * i + r;
-                float s = acc[i][j][r] * a.scale;
+                float s = acc[i][j][r] * sign;
                 if (v == target && v < end) a.own[t] = s;
                 if (v == target || v >= end) s = -INFINITY;
                 acc[i][j][r] = s;
@@ -296,15 +299,15 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E);
+            for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * f);
         sum = sum_halves(sum_rows(sum));
         if (lane < 16) joined[wave][16 * j + l] = {most, sum};
     }
     __syncthreads();
     if (threadIdx.x < 16 * GROUPS && row0 + (int)threadIdx.x < rows) {
         const int t = threadIdx.x;
-        float2 x = join_parts(join_parts(joined[0][t], joined[1][t]), join_parts(joined[2][t], joined[3][t]));
-        if constexpr (WAVES == 8) x = join_parts(x, join_parts(join_parts(joined[4][t], joined[5][t]), join_parts(joined[6][t], joined[7][t])));
+        float2 x = join_parts(join_parts(joined[0][t], joined[1][t], f), join_parts(joined[2][t], joined[3][t], f), f);
+        if constexpr (WAVES == 8) x = join_parts(x, join_parts(join_parts(joined[4][t], joined[5][t], f), join_parts(joined[6][t], joined[7][t], f), f), f);
         a.part[(int64_t)blockIdx.x * a.padded_rows + row0 + t] = x;
     }
 }
@@ -356,18 +359,19 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossArgs a, int parts, i
     __shared__ float2 lds[4][ROWS];
     const int r = threadIdx.x % ROWS, share = threadIdx.x / ROWS, live = packed ? uniform_load(a.state) : (int)a.rows;
     const int i = blockIdx.x * ROWS + r;
+    const float f = exponent_factor(a);
     float2 x = {-INFINITY, 0.0f};
     if (i < live) {
 #pragma unroll 4
-        for (int p = share; p < parts; p += SHARES) x = join_parts(x, a.part[(int64_t)p * a.padded_rows + i]);
+        for (int p = share; p < parts; p += SHARES) x = join_parts(x, a.part[(int64_t)p * a.padded_rows + i], f);
     }
 #pragma unroll
-    for (int o = ROWS; o < 64; o <<= 1) x = join_parts(x, {__shfl_xor(x.x, o), __shfl_xor(x.y, o)});
+    for (int o = ROWS; o < 64; o <<= 1) x = join_parts(x, {__shfl_xor(x.x, o), __shfl_xor(x.y, o)}, f);
     if ((threadIdx.x & 63) < ROWS) lds[threadIdx.x >> 6][r] = x;
     __syncthreads();
     if (share != 0 || i >= live) return;
-    x = join_parts(join_parts(lds[0][r], lds[1][r]), join_parts(lds[2][r], lds[3][r]));
-    if (a.first > 0) x = join_parts(a.running[i], x);
+    x = join_parts(join_parts(lds[0][r], lds[1][r], f), join_parts(lds[2][r], lds[3][r], f), f);
+    if (a.first > 0) x = join_parts(a.running[i], x, f);
     if (!a.last) {
         a.running[i] = x;
         return;
@@ -377,9 +381,10 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossArgs a, int parts, i
     const float own = there ? a.own[i] : 0.0f;
     // log(exp(own) + sum), beside the larger of the two; where both are infinite or not a number, so is the result
     const float top = x.x > own ? x.x : own;
-    const float rest = x.x > own ? logf(x.y + __builtin_amdgcn_exp2f((own - top) * LOG2E)) : x.x == -INFINITY && x.y == 0.0f ? 0.0f : log1pf(x.y * __builtin_amdgcn_exp2f((x.x - top) * LOG2E));
-    a.loss[t] = there ? (top - own) + rest : 0.0f;
-    if (a.lse) *(float2 *)(a.lse + 2 * t) = there ? float2{top, rest} : float2{0.0f, 0.0f};
+    const float rest = x.x > own ? logf(x.y + __builtin_amdgcn_exp2f((own - top) * f))
+                                 : x.x == -INFINITY && x.y == 0.0f ? 0.0f : log1pf(x.y * __builtin_amdgcn_exp2f((x.x - top) * f));
+    a.loss[t] = there ? (top - own) * score_factor(a) + rest : 0.0f;
+    if (a.lse) *(float2 *)(a.lse + 2 * t) = there ? float2{top * score_factor(a), rest} : float2{0.0f, 0.0f};
 }
 
 void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool packed)

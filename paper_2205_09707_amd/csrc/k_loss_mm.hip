@@ -258,16 +258,13 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
     };
     if constexpr (KIND != KIND_STATISTICS && KIND != KIND_D_HIDDEN) __syncthreads();  // all waves are done with the operands
     if constexpr (KIND == KIND_STATISTICS) {
+        const float f = exponent_factor(a);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int row = n0 + 32 * j;
             const bool there = row < live;
             const int target = there ? a.row[row].target - (int)a.first - m0 : -1;  // place in the piece, from the lane's first
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = acc[i][j][r] * a.scale;
-            if (__any(target >= 0 && target < 128)) {  // the target's score is kept apart
+            if (__any(target >= 0 && target < 128)) {  // the target is kept apart
                 float own = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -295,7 +292,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * LOG2E);
+                for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * f);
             sum = sum_halves(sum);
             if (lane < 32) a.part[(int64_t)(t.m * 2 + wm) * a.padded_rows + row] = {most, sum};
         }
@@ -306,28 +303,31 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
             const bool there = row < live;
             const LossRow x = there ? a.row[row] : LossRow{-1, 0, 0.0f, 0.0f, 0.0f};
             const int target = there ? x.target - (int)a.first - m0 : -1;
-            const ScoreGradient gradient(x, a.scale, DT);
-            float own = 0.0f;
+            const ScoreGradient gradient(x, a, DT);
+            if (t.n == row_tiles - 1)  // rows past the end, packed as zeros: whatever the vocabulary holds
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] = there ? acc[i][j][r] : 0.0f;
+            if (t.m == pieces - 1)  // entries past the end
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][j][r] = m0 + 32 * i + 8 * (r / 4) + r % 4 < a.piece ? acc[i][j][r] : -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    keep(i, j, c, gradient.other(acc[i][j][4 * c]), gradient.other(acc[i][j][4 * c + 1]), gradient.other(acc[i][j][4 * c + 2]), gradient.other(acc[i][j][4 * c + 3]));
             if (__any(target >= 0 && target < 128)) {
+                float own = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) own = 32 * i + 8 * (r / 4) + r % 4 == target ? acc[i][j][r] : own;
-                own = gradient.target(own);
+                const int n = (n0 & 255) + 32 * j, m = (m0 & 255) + target;
+                if (target >= 0 && target < 128 && !(target & 4) && m0 + target < a.piece) store16<DT>(results + result_place(n, m) + (m & 3) * 2, gradient.target(own));
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    float g[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int m = 32 * i + 8 * c + r;
-                        g[r] = m == target ? own : gradient.other(acc[i][j][4 * c + r]);
-                        if (!there || m0 + m >= a.piece) g[r] = 0.0f;
-                    }
-                    keep(i, j, c, g[0], g[1], g[2], g[3]);
-                }
         }
         send(a.gradient + ((int64_t)t.n * pieces + t.m) * G_TILE, LOSS_TILE * 2, LOSS_TILE, LOSS_TILE);
     } else if constexpr (KIND == KIND_D_HIDDEN) {
@@ -345,7 +345,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
                     *p = v;
                 }
     } else {
-        const float factor = a.scale * (DT == PLAID_FP16 ? 0x1p-15f : 1.0f);
+        const float factor = score_factor(a) * (DT == PLAID_FP16 ? 0x1p-15f : 1.0f);
         const int exponent = uniform_load(a.state + 1);
 #pragma unroll
         for (int j = 0; j < 2; ++j)

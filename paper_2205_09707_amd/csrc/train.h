@@ -61,11 +61,11 @@ struct LossArgs {
     int32_t *state;                    // [0] rows that have a target, [1] the largest exponent among them
     int32_t *list;                     // [rows] which these are
     LossRow *row;                      // [padded_rows]
-    char *packed;                      // [rows / 256][pitch / 64][256][64] states
+    char *packed;                      // [rows / 256][pitch / 64][256][64] states, with the sign of the scale
     char *scaled;                      // [rows / 64][columns / 256][64][256] the same times 2^(exponent - largest)
-    float2 *part;                      // [parts][padded_rows] maximum and sum of exponentials over parts of the vocabulary, without the target
+    float2 *part;                      // [parts][padded_rows] largest product and sum of exponentials beside it over parts of the vocabulary, without the target
     float2 *running;                   // [padded_rows] over all parts before
-    float *own;                        // [padded_rows] score of the target
+    float *own;                        // [padded_rows] product of the target
     char *gradient;                    // [rows / 256][piece / 256][256][256] of the scores, over a piece of the vocabulary
     float *d_part;                     // [parts][tiles of rows that have a target][columns / 256][256 x 256] sums of d_hidden, in the order of the products' registers
     int32_t columns;                   // width rounded up to LOSS_TILE
@@ -116,15 +116,24 @@ __device__ __forceinline__ int hidden_splits(const LossArgs &a, int live)
     return best;
 }
 
+// Scores s = scale h . W are formed from products u = h . W whose sign is that of the scale (the packed states carry it), so that the largest product
+// has the largest score: statistics are those of products, and a score costs one multiply-add on its way into an exponential.
+__device__ __forceinline__ float score_factor(const LossArgs &a) { return fabsf(a.scale); }
+// The same for exponentials of base two.  A factor of zero would meet the infinities of entries that are left out; beside this one every
+// product that is not huge is nothing as well.
+__device__ __forceinline__ float exponent_factor(const LossArgs &a) { return fmaxf(fabsf(a.scale), 1e-30f) * LOG2E; }
+
 // G of a row, in units of its d_loss's power of two, times 2^15 in fp16: of a product, by the score it is.  The target's is the probability less
 // one, formed so that it keeps its digits where the probability is almost one.
 struct ScoreGradient {
-    float scale, top, rest, log_total, factor;
-    __device__ __forceinline__ ScoreGradient(const LossRow &x, float scale_, int dtype)
-        : scale(scale_), top(x.top), rest(x.log_total * LOG2E), log_total(x.log_total), factor(x.fraction * (dtype == PLAID_FP16 ? 0x1p15f : 1.0f))
+    float scale, k, top, log_total, shift, factor;
+    __device__ __forceinline__ ScoreGradient(const LossRow &x, const LossArgs &a, int dtype)
+        : scale(score_factor(a)), k(exponent_factor(a)), top(x.top), log_total(x.log_total), shift((x.top + x.log_total) * LOG2E),
+          factor(x.fraction * (dtype == PLAID_FP16 ? 0x1p15f : 1.0f))
     {
     }
-    __device__ __forceinline__ float other(float product) const { return __builtin_amdgcn_exp2f((product * scale - top) * LOG2E - rest) * factor; }
+    // (the shift's rounding, 2^-24 of a score, costs a probability less than its own rounding to the type while scores stay below 2^12)
+    __device__ __forceinline__ float other(float product) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(product, k, -shift)) * factor; }
     __device__ __forceinline__ float target(float product) const { return expm1f(product * scale - top - log_total) * factor; }
 };
 

@@ -136,6 +136,23 @@ def test_what_is_not_finite_is_seen(pl, rows):
     assert not torch.isfinite(dh[4]).any() and torch.isfinite(dh[keep]).all()
 
 
+@pytest.mark.parametrize("rows", [9, 70, 300, 1100])
+def test_an_entry_that_no_score_reaches(pl, rows):
+    """Its scores are -infinity: it has no probability and no gradient, and the other entries have what they have without it."""
+    h, w, t, d = _inputs(rows, 700, 72, BF, without=0.1)
+    h[:, 0] = 1.0
+    t[t == 7] = 8
+    w[7] = 0.0
+    w[7, 0] = -INF
+    rest = torch.cat([w[:7], w[8:]])
+    want = cross_entropy(h, rest, torch.where(t > 7, torch.where(t < 700, t - 1, 699), t), 0.25, d)
+    loss, lse = pl.plaid_cross_entropy(h, w, t, scale=0.25, return_lse=True)
+    close(loss, want["loss"], want["loss_bound"], "loss")
+    _, dw = pl.plaid_cross_entropy_backward(d, h, w, t, lse, scale=0.25)
+    assert not dw[7].any()
+    close(torch.cat([dw[:7], dw[8:]]), want["d_weight"], want["d_weight_bound"], "d_weight")
+
+
 @pytest.mark.parametrize("dtype", [BF, HALF])
 @pytest.mark.parametrize("kind", ["tiny", "spread", "zeros", "one", "huge"])
 def test_gradients_of_the_loss(pl, dtype, kind):
