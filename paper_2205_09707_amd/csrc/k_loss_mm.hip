@@ -114,14 +114,15 @@ __device__ __forceinline__ int result_place(int n, int m) { return n * (LOSS_TIL
 #define KIND_D_HIDDEN 2
 #define KIND_D_WEIGHT 3
 
+// Tiles that lie in LDS at a time: two of A, two or three of B, the results' place afterwards.
+template <int NB>
 struct TileLds {
-    char operand[2][2][TILE_BYTES];
+    char a[2][TILE_BYTES], b[NB][TILE_BYTES];
 };
-template <int DT, int KIND>
-__device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int id)
+template <int DT, int KIND, int NB>
+__device__ __forceinline__ void product(const LossArgs &a, TileLds<NB> &lds, int id)
 {
     constexpr bool SCORES = KIND <= KIND_GRADIENT, A_ACROSS = !SCORES, B_ACROSS = KIND == KIND_D_WEIGHT;
-    auto &lds = tiles.operand;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wm = wave >> 2, wn = wave & 3;
     const int live = uniform_load(a.state), row_tiles = (live + LOSS_TILE - 1) / LOSS_TILE;
     const int pieces = (a.piece + LOSS_TILE - 1) / LOSS_TILE, widths = a.columns / LOSS_TILE;
@@ -164,24 +165,23 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
 #pragma unroll
         for (int j = 0; j < 2; ++j) acc[i][j] = zero16();
 
-    // A step's loads, of which the first four are A's; a wave's go to its own 4 KB of both tiles.
-    const uint32_t mine = lds_address(lds) + wave * 4096;
-    const auto bring = [&](int s, int i, bool last) {
-        const uint32_t x = mine + (s & 1) * (2 * TILE_BYTES);
-        if (i >= 4) B.load(i - 4, x + TILE_BYTES);
-        else if (KIND != KIND_D_WEIGHT && last && end_left < BK) A.load_end(i, x, end_left, a.weight_stride);
+    // A wave's loads of a step go to its own 4 KB of both tiles.  B's tile of step s is in place `slot`, s modulo NB.
+    const uint32_t a_mine = lds_address(lds.a) + wave * 4096, b_mine = lds_address(lds.b) + wave * 4096;
+    int slot = 0;
+    const auto bring_a = [&](int s, int i, bool last) {
+        const uint32_t x = a_mine + (s & 1) * TILE_BYTES;
+        if (KIND != KIND_D_WEIGHT && last && end_left < BK) A.load_end(i, x, end_left, a.weight_stride);
         else A.load(i, x);
     };
-    const auto advance = [&](int s) {
-        A.step(a_step);
-        // four steps are a tile of gradients
+    const auto bring_b = [&](int place, int i) { B.load(i, b_mine + place * TILE_BYTES); };
+    const auto advance_b = [&](int s) {  // from step s to the next; four steps are a tile of gradients
         if constexpr (SCORES) B.step(b_step);
         else if constexpr (KIND == KIND_D_HIDDEN) B.step(((begin + s) & 3) == 3 ? G_TILE - 6 * BK : 2 * BK);
         else B.step((s & 3) == 3 ? pieces * G_TILE - 3 * TILE_BYTES : TILE_BYTES);
     };
     i32x4 p[2][4], q[2][2];
-    const auto read = [&](int s, int k) {
-        const char *x = lds[s & 1][0], *y = lds[s & 1][1];
+    const auto read = [&](int s, int place, int k) {
+        const char *x = lds.a[s & 1], *y = lds.b[place];
 #pragma unroll
         for (int j = 0; j < 2; ++j) q[k & 1][j] = pb.read(y, j, k);
 #pragma unroll
@@ -191,7 +191,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
     // A quarter's products, with the next quarter's operands read among them.
     const auto quarter = [&](int s, int k) {
         constexpr int READS = (A_ACROSS ? 8 : 4) + (B_ACROSS ? 4 : 2);
-        read(s, k + 1);
+        read(s, slot, k + 1);
 #pragma unroll
         for (int i = 0; i < 8; ++i) multiply(k, i >> 1, i & 1);
         // the order: one or two reads before each of the first six products
@@ -202,40 +202,57 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
         __builtin_amdgcn_sched_barrier(0);
     };
     // Operands are read a quarter of a step before they are multiplied, those of the next step's first quarter too: its tiles have come when
-    // the last quarter's operands are in registers, and the tiles of the step after may then take this one's place.  The last steps stand apart,
-    // so that the others have no branches.
+    // the last quarter's operands are in registers, and the tiles of the steps after may then take this one's places.  The last steps stand
+    // apart, so that the others have no branches.  (Three tiles of B: gradients of scores come from memory, 512 MB of them, and a step is not
+    // long enough for that.)
     const auto step = [&](int s, auto stands) {
-        constexpr int AFTER = decltype(stands)::value;  // steps that come after this one, 3: more than two
+        constexpr int AFTER = decltype(stands)::value;  // steps that come after this one, NB + 1: more than NB
+        const int next = slot == NB - 1 ? 0 : slot + 1;
         quarter(s, 0);
         quarter(s, 1);
         quarter(s, 2);
         if constexpr (AFTER > 0) {
-            wait_loads<0>();
+            wait_loads<NB == 3 && AFTER >= 2 ? 4 : 0>();
             lds_barrier();
-            read(s + 1, 0);
+            read(s + 1, next, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             multiply(3, i >> 1, i & 1);
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (AFTER > 1) bring(s + 2, i, AFTER == 2);
+            if constexpr (AFTER >= 2)
+                if (i < 4) bring_a(s + 2, i, AFTER == 2);
+            if constexpr (AFTER >= NB)
+                if (i >= 4) bring_b(slot, i - 4);
         }
-        if constexpr (AFTER > 2) advance(s + 2);
+        if constexpr (AFTER > 2) A.step(a_step);
+        if constexpr (AFTER > NB) advance_b(s + NB);
+        slot = next;
     };
     if (steps > 0) {
+        const auto first = [&](int s, bool with_a) {
+            if (s >= steps) return;
+            if (with_a) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bring(0, i, steps == 1);
-        advance(0);
-        if (steps > 1) {
+                for (int i = 0; i < 4; ++i) bring_a(s, i, s == steps - 1);
+                A.step(a_step);
+            }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) bring(1, i, steps == 2);
-            advance(1);
-            wait_loads<8>();
-        } else wait_loads<0>();
+            for (int i = 0; i < 4; ++i) bring_b(s, i);
+            advance_b(s);
+        };
+        first(0, true);
+        first(1, true);
+        if constexpr (NB == 3) first(2, false);
+        if (steps == 1) wait_loads<0>();
+        else if (steps == 2 || NB == 2) wait_loads<8>();
+        else wait_loads<12>();
         lds_barrier();
-        read(0, 0);
-        for (int s = 0; s < steps - 3; ++s) step(s, std::integral_constant<int, 3>());
+        read(0, 0, 0);
+        for (int s = 0; s < steps - NB - 1; ++s) step(s, std::integral_constant<int, NB + 1>());
+        if constexpr (NB == 3)
+            if (steps > 3) step(steps - 4, std::integral_constant<int, 3>());
         if (steps > 2) step(steps - 3, std::integral_constant<int, 2>());
         if (steps > 1) step(steps - 2, std::integral_constant<int, 1>());
         step(steps - 1, std::integral_constant<int, 0>());
@@ -243,7 +260,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
 
     // a lane's results: column n = 64 wn + 32 j + lane % 32, rows m = 128 wm + 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4
     const int m0 = t.m * LOSS_TILE + wm * 128 + 4 * (lane >> 5), n0 = t.n * LOSS_TILE + wn * 64 + (lane & 31);
-    char *const results = &lds[0][0][0];
+    char *const results = lds.a[0];
     const auto keep = [&](int i, int j, int c, float x0, float x1, float x2, float x3) {
         *(i32x2 *)(results + result_place((n0 & 255) + 32 * j, (m0 & 255) + 32 * i + 8 * c)) = i32x2{pack2<DT>(x0, x1), pack2<DT>(x2, x3)};
     };
@@ -365,14 +382,14 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &tiles, int i
 template <int DT, int KIND>
 __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
 {
-    __shared__ __align__(16) TileLds lds;
+    __shared__ __align__(16) TileLds<2> lds;
     product<DT, KIND>(a, lds, blockIdx.x);
 }
 // Both gradients: d_hidden's tiles, which take longer, then d_weight's.
 template <int DT>
 __global__ __launch_bounds__(512, 2) void loss_gradients_kernel(LossArgs a, int hidden)
 {
-    __shared__ __align__(16) TileLds lds;
+    __shared__ __align__(16) TileLds<3> lds;
     if ((int)blockIdx.x < hidden) product<DT, KIND_D_HIDDEN>(a, lds, blockIdx.x);
     else product<DT, KIND_D_WEIGHT>(a, lds, blockIdx.x - hidden);
 }
