@@ -114,13 +114,13 @@ __device__ __forceinline__ int result_place(int n, int m) { return n * (LOSS_TIL
 #define KIND_D_HIDDEN 2
 #define KIND_D_WEIGHT 3
 
-// Tiles that lie in LDS at a time: two of A, two or three of B, the results' place afterwards.
-template <int NB>
+// Tiles that lie in LDS at a time: three of the operand that comes from memory (the vocabulary for scores, the scores' gradients for the others), for
+// which a step is not long enough, two of the other; the results' place afterwards.
 struct TileLds {
-    char a[2][TILE_BYTES], b[NB][TILE_BYTES];
+    char near[2][TILE_BYTES], far[3][TILE_BYTES];
 };
-template <int DT, int KIND, int NB>
-__device__ __forceinline__ void product(const LossArgs &a, TileLds<NB> &lds, int id)
+template <int DT, int KIND>
+__device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
 {
     constexpr bool SCORES = KIND <= KIND_GRADIENT, A_ACROSS = !SCORES, B_ACROSS = KIND == KIND_D_WEIGHT;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wm = wave >> 2, wn = wave & 3;
@@ -165,23 +165,35 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds<NB> &lds, int
 #pragma unroll
         for (int j = 0; j < 2; ++j) acc[i][j] = zero16();
 
-    // A wave's loads of a step go to its own 4 KB of both tiles.  B's tile of step s is in place `slot`, s modulo NB.
-    const uint32_t a_mine = lds_address(lds.a) + wave * 4096, b_mine = lds_address(lds.b) + wave * 4096;
+    // A wave's loads of a step go to its own 4 KB of both tiles.  The far operand's tile of step s is in place `slot`, s modulo 3.
+    const uint32_t near_mine = lds_address(lds.near) + wave * 4096, far_mine = lds_address(lds.far) + wave * 4096;
     int slot = 0;
-    const auto bring_a = [&](int s, int i, bool last) {
-        const uint32_t x = a_mine + (s & 1) * TILE_BYTES;
-        if (KIND != KIND_D_WEIGHT && last && end_left < BK) A.load_end(i, x, end_left, a.weight_stride);
-        else A.load(i, x);
+    const auto bring_a = [&](uint32_t to, int i, bool last) {
+        if (KIND != KIND_D_WEIGHT && last && end_left < BK) A.load_end(i, to, end_left, a.weight_stride);
+        else A.load(i, to);
     };
-    const auto bring_b = [&](int place, int i) { B.load(i, b_mine + place * TILE_BYTES); };
-    const auto advance_b = [&](int s) {  // from step s to the next; four steps are a tile of gradients
+    const auto bring_near = [&](int s, int i, bool last) {
+        const uint32_t to = near_mine + (s & 1) * TILE_BYTES;
+        if constexpr (SCORES) B.load(i, to);
+        else bring_a(to, i, last);
+    };
+    const auto bring_far = [&](int place, int i, bool last) {
+        const uint32_t to = far_mine + place * TILE_BYTES;
+        if constexpr (SCORES) bring_a(to, i, last);
+        else B.load(i, to);
+    };
+    const auto advance_near = [&]() {
         if constexpr (SCORES) B.step(b_step);
+        else A.step(a_step);
+    };
+    const auto advance_far = [&](int s) {  // from step s to the next; four steps are a tile of gradients
+        if constexpr (SCORES) A.step(a_step);
         else if constexpr (KIND == KIND_D_HIDDEN) B.step(((begin + s) & 3) == 3 ? G_TILE - 6 * BK : 2 * BK);
         else B.step((s & 3) == 3 ? pieces * G_TILE - 3 * TILE_BYTES : TILE_BYTES);
     };
     i32x4 p[2][4], q[2][2];
     const auto read = [&](int s, int place, int k) {
-        const char *x = lds.a[s & 1], *y = lds.b[place];
+        const char *x = SCORES ? lds.far[place] : lds.near[s & 1], *y = SCORES ? lds.near[s & 1] : lds.far[place];
 #pragma unroll
         for (int j = 0; j < 2; ++j) q[k & 1][j] = pb.read(y, j, k);
 #pragma unroll
@@ -203,16 +215,15 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds<NB> &lds, int
     };
     // Operands are read a quarter of a step before they are multiplied, those of the next step's first quarter too: its tiles have come when
     // the last quarter's operands are in registers, and the tiles of the steps after may then take this one's places.  The last steps stand
-    // apart, so that the others have no branches.  (Three tiles of B: gradients of scores come from memory, 512 MB of them, and a step is not
-    // long enough for that.)
+    // apart, so that the others have no branches.
     const auto step = [&](int s, auto stands) {
-        constexpr int AFTER = decltype(stands)::value;  // steps that come after this one, NB + 1: more than NB
-        const int next = slot == NB - 1 ? 0 : slot + 1;
+        constexpr int AFTER = decltype(stands)::value;  // steps that come after this one, 4: more than three
+        const int next = slot == 2 ? 0 : slot + 1;
         quarter(s, 0);
         quarter(s, 1);
         quarter(s, 2);
         if constexpr (AFTER > 0) {
-            wait_loads<NB == 3 && AFTER >= 2 ? 4 : 0>();
+            wait_loads<AFTER >= 2 ? 4 : 0>();  // the far operand's of the step after next
             lds_barrier();
             read(s + 1, next, 0);
             __builtin_amdgcn_sched_barrier(0);
@@ -222,37 +233,36 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds<NB> &lds, int
             multiply(3, i >> 1, i & 1);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (AFTER >= 2)
-                if (i < 4) bring_a(s + 2, i, AFTER == 2);
-            if constexpr (AFTER >= NB)
-                if (i >= 4) bring_b(slot, i - 4);
+                if (i < 4) bring_near(s + 2, i, AFTER == 2);
+            if constexpr (AFTER >= 3)
+                if (i >= 4) bring_far(slot, i - 4, AFTER == 3);
         }
-        if constexpr (AFTER > 2) A.step(a_step);
-        if constexpr (AFTER > NB) advance_b(s + NB);
+        if constexpr (AFTER > 2) advance_near();
+        if constexpr (AFTER > 3) advance_far(s + 3);
         slot = next;
     };
     if (steps > 0) {
-        const auto first = [&](int s, bool with_a) {
+        const auto first = [&](int s, bool with_near) {
             if (s >= steps) return;
-            if (with_a) {
+            if (with_near) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) bring_a(s, i, s == steps - 1);
-                A.step(a_step);
+                for (int i = 0; i < 4; ++i) bring_near(s, i, s == steps - 1);
+                advance_near();
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) bring_b(s, i);
-            advance_b(s);
+            for (int i = 0; i < 4; ++i) bring_far(s, i, s == steps - 1);
+            advance_far(s);
         };
         first(0, true);
         first(1, true);
-        if constexpr (NB == 3) first(2, false);
+        first(2, false);
         if (steps == 1) wait_loads<0>();
-        else if (steps == 2 || NB == 2) wait_loads<8>();
+        else if (steps == 2) wait_loads<8>();
         else wait_loads<12>();
         lds_barrier();
         read(0, 0, 0);
-        for (int s = 0; s < steps - NB - 1; ++s) step(s, std::integral_constant<int, NB + 1>());
-        if constexpr (NB == 3)
-            if (steps > 3) step(steps - 4, std::integral_constant<int, 3>());
+        for (int s = 0; s < steps - 4; ++s) step(s, std::integral_constant<int, 4>());
+        if (steps > 3) step(steps - 4, std::integral_constant<int, 3>());
         if (steps > 2) step(steps - 3, std::integral_constant<int, 2>());
         if (steps > 1) step(steps - 2, std::integral_constant<int, 1>());
         step(steps - 1, std::integral_constant<int, 0>());
@@ -260,7 +270,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds<NB> &lds, int
 
     // a lane's results: column n = 64 wn + 32 j + lane % 32, rows m = 128 wm + 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4
     const int m0 = t.m * LOSS_TILE + wm * 128 + 4 * (lane >> 5), n0 = t.n * LOSS_TILE + wn * 64 + (lane & 31);
-    char *const results = lds.a[0];
+    char *const results = lds.near[0];
     const auto keep = [&](int i, int j, int c, float x0, float x1, float x2, float x3) {
         *(i32x2 *)(results + result_place((n0 & 255) + 32 * j, (m0 & 255) + 32 * i + 8 * c)) = i32x2{pack2<DT>(x0, x1), pack2<DT>(x2, x3)};
     };
@@ -382,14 +392,14 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds<NB> &lds, int
 template <int DT, int KIND>
 __global__ __launch_bounds__(512, 2) void loss_mm_kernel(LossArgs a)
 {
-    __shared__ __align__(16) TileLds<2> lds;
+    __shared__ __align__(16) TileLds lds;
     product<DT, KIND>(a, lds, blockIdx.x);
 }
 // Both gradients: d_hidden's tiles, which take longer, then d_weight's.
 template <int DT>
 __global__ __launch_bounds__(512, 2) void loss_gradients_kernel(LossArgs a, int hidden)
 {
-    __shared__ __align__(16) TileLds<3> lds;
+    __shared__ __align__(16) TileLds lds;
     if ((int)blockIdx.x < hidden) product<DT, KIND_D_HIDDEN>(a, lds, blockIdx.x);
     else product<DT, KIND_D_WEIGHT>(a, lds, blockIdx.x - hidden);
 }
