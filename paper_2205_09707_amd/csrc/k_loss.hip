@@ -394,37 +394,51 @@ void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool p
     else loss_join_kernel<1><<<(unsigned)a.rows, 256, 0, st>>>(a, parts, packed);
 }
 
-// --- gradient of the states: the splits' sums added up, in order ------------------------------------------------------------------
-// The sums lie in tiles of 256 rows and columns, in the order in which the products' registers hold them: for a wave of 128 columns and 64 rows
-// [32 rows' half][32 columns' quarter][8 columns' quarter][lane][4 columns], a lane being a row and a half of the 8 columns.  A workgroup has
-// 32 rows of a tile, each of its waves 8 columns.
-template <int DT>
-__global__ __launch_bounds__(256) void loss_d_hidden_join_kernel(LossArgs a)
+// --- gradients: the parts' sums added up, in order -----------------------------------------------------------------------------------
+// The sums lie in tiles of 256 rows (of states, or entries) and columns, in the order in which the products' registers hold them: for a wave of 128
+// columns and 64 rows [32 rows' half][32 columns' quarter][8 columns' quarter][lane][4 columns], a lane being a row and a half of the 8
+// columns.  A workgroup has 32 rows of a tile, each of its waves 8 columns.
+template <int DT, bool WEIGHT>
+__device__ __forceinline__ void join_gradients(const LossArgs &a, int id)
 {
-    const int live = uniform_load(a.state), row_tiles = (live + LOSS_TILE - 1) / LOSS_TILE, widths = a.columns / LOSS_TILE;
-    const int block = blockIdx.x & 7, k = blockIdx.x >> 3 & 7, tile = blockIdx.x >> 6, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row = tile / widths * LOSS_TILE + block * 32 + (lane & 31);
-    if (tile / widths * LOSS_TILE + block * 32 >= live) return;
-    const int splits = hidden_splits(a, live);
+    const int live = uniform_load(a.state), widths = a.columns / LOSS_TILE, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int rows = WEIGHT ? a.piece : live, row_tiles = (rows + LOSS_TILE - 1) / LOSS_TILE;
+    const int block = id & 7, k = id >> 3 & 7, tile = id >> 6, row = tile / widths * LOSS_TILE + block * 32 + (lane & 31);
+    if (tile / widths * LOSS_TILE + block * 32 >= rows) return;
+    const LossParts parts = loss_parts(a, live);
+    const int splits = WEIGHT ? parts.weight : parts.hidden;
+    if (WEIGHT && splits == 1) return;  // written by the products
     const int64_t part = (int64_t)row_tiles * widths * (LOSS_TILE * LOSS_TILE);
-    const bool there = row < live;
-    const int64_t t = there ? a.list[row] : 0;
-    const int e = there ? a.row[row].exponent : 0;
+    const bool there = row < rows;
+    int64_t to = 0;
+    int e = 0;
+    if constexpr (WEIGHT) to = a.first + row, e = uniform_load(a.state + 1);
+    else if (there) to = a.list[row], e = a.row[row].exponent;
     // the power of two last, where the result may leave the normal range
-    const float factor = a.scale * (DT == PLAID_FP16 ? 0x1p-15f : 1.0f);
+    const float factor = (WEIGHT ? score_factor(a) : a.scale) * (DT == PLAID_FP16 ? 0x1p-15f : 1.0f);
     // wave w of these four: eight of columns 64 w .. 64 w + 63, two quarters of 32
     const int i = (wave & 1) * 2 + k / 4, c = k % 4, column = tile % widths * LOSS_TILE + wave * 64 + k * 8 + 4 * (lane >> 5);
-    const float *p = a.d_part + (int64_t)tile * (LOSS_TILE * LOSS_TILE) + ((wave >> 1) * 4 + block / 2) * 8192 + (((block & 1) * 4 + i) * 4 + c) * 256 + lane * 4;
+    const float *p = (WEIGHT ? a.w_part : a.d_part) + (int64_t)tile * (LOSS_TILE * LOSS_TILE) + ((wave >> 1) * 4 + block / 2) * 8192 + (((block & 1) * 4 + i) * 4 + c) * 256 + lane * 4;
     f32x4 v = {0, 0, 0, 0};
 #pragma unroll 4
     for (int s = 0; s < splits; ++s) v += *(const f32x4 *)(p + s * part);
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = ldexpf(v[j] * factor, e == NO_EXPONENT ? 0 : e);
-    if (there && column < a.width) *(i32x2 *)(a.d_hidden + (t * a.width + column) * 2) = i32x2{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+    char *out = WEIGHT ? a.d_weight : a.d_hidden;
+    if (there && column < a.width) *(i32x2 *)(out + (to * a.width + column) * 2) = i32x2{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
 }
-void plaid_launch_loss_d_hidden_join(hipStream_t st, const LossArgs &a, int dtype)
+template <int DT>
+__global__ __launch_bounds__(256) void loss_gradients_join_kernel(LossArgs a, int hidden)
 {
-    const unsigned grid = (unsigned)(a.padded_rows / LOSS_TILE * (a.columns / LOSS_TILE) * 64);
-    if (dtype == PLAID_BF16) loss_d_hidden_join_kernel<PLAID_BF16><<<grid, 256, 0, st>>>(a);
-    else loss_d_hidden_join_kernel<PLAID_FP16><<<grid, 256, 0, st>>>(a);
+    if ((int)blockIdx.x < hidden) join_gradients<DT, false>(a, blockIdx.x);
+    else join_gradients<DT, true>(a, blockIdx.x - hidden);
+}
+// After each piece for d_weight, if its axis may be cut, after the last one for d_hidden.
+void plaid_launch_loss_gradients_join(hipStream_t st, const LossArgs &a, int dtype)
+{
+    const int widths = a.columns / LOSS_TILE, hidden = a.d_hidden && a.last ? a.padded_rows / LOSS_TILE * widths * 64 : 0;
+    const int weight = a.d_weight && a.w_part ? (a.piece + LOSS_TILE - 1) / LOSS_TILE * widths * 64 : 0;
+    if (hidden + weight == 0) return;
+    if (dtype == PLAID_BF16) loss_gradients_join_kernel<PLAID_BF16><<<hidden + weight, 256, 0, st>>>(a, hidden);
+    else loss_gradients_join_kernel<PLAID_FP16><<<hidden + weight, 256, 0, st>>>(a, hidden);
 }

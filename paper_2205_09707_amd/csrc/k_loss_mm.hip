@@ -126,8 +126,9 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wm = wave >> 2, wn = wave & 3;
     const int live = uniform_load(a.state), row_tiles = (live + LOSS_TILE - 1) / LOSS_TILE;
     const int pieces = (a.piece + LOSS_TILE - 1) / LOSS_TILE, widths = a.columns / LOSS_TILE;
-    // d_hidden's tiles come once for each part of its axis, those of one part together
-    const int splits = KIND == KIND_D_HIDDEN ? hidden_splits(a, live) : 1;
+    // a gradient's tiles come once for each part of its axis, those of one part together
+    const LossParts parts = SCORES ? LossParts{1, 1} : loss_parts(a, live);
+    const int splits = KIND == KIND_D_HIDDEN ? parts.hidden : parts.weight;
     Tile t;
     int split = 0;
     if (!find_tile(id, SCORES ? pieces : widths, KIND == KIND_D_WEIGHT ? pieces : row_tiles, splits, t, split)) return;
@@ -150,10 +151,11 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
         A.set(a.weight + (a.first + (int64_t)begin * BK) * a.weight_stride, a.weight_stride, t.m * LOSS_TILE, 0, a.width);
         B.set(a.gradient + ((int64_t)t.n * pieces + begin / 4) * G_TILE + begin % 4 * (2 * BK), 2 * LOSS_TILE, 0, LOSS_TILE, 0);
     } else {
-        steps = (live + BK - 1) / BK;
+        const int all = (live + BK - 1) / BK, share = (all + splits - 1) / splits;
+        begin = min(all, split * share), steps = min(all, begin + share) - begin;
         a_step = (int64_t)widths * TILE_BYTES;
-        A.set(a.scaled + (int64_t)t.m * TILE_BYTES, 2 * LOSS_TILE, 0, 0, LOSS_TILE);
-        B.set(a.gradient + t.n * G_TILE, 2 * LOSS_TILE, 0, 0, LOSS_TILE);
+        A.set(a.scaled + ((int64_t)begin * widths + t.m) * TILE_BYTES, 2 * LOSS_TILE, 0, 0, LOSS_TILE);
+        B.set(a.gradient + ((int64_t)(begin / 4) * pieces + t.n) * G_TILE + begin % 4 * TILE_BYTES, 2 * LOSS_TILE, 0, 0, LOSS_TILE);
     }
     Places<A_ACROSS, 4> pa;
     Places<B_ACROSS, 2> pb;
@@ -189,7 +191,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
     const auto advance_far = [&](int s) {  // from step s to the next; four steps are a tile of gradients
         if constexpr (SCORES) A.step(a_step);
         else if constexpr (KIND == KIND_D_HIDDEN) B.step(((begin + s) & 3) == 3 ? G_TILE - 6 * BK : 2 * BK);
-        else B.step((s & 3) == 3 ? pieces * G_TILE - 3 * TILE_BYTES : TILE_BYTES);
+        else B.step(((begin + s) & 3) == 3 ? pieces * G_TILE - 3 * TILE_BYTES : TILE_BYTES);
     };
     i32x4 p[2][4], q[2][2];
     const auto read = [&](int s, int place, int k) {
@@ -283,7 +285,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
             if (n < rows && m < columns) *(i32x4 *)(out + n * stride + m * 2) = *(const i32x4 *)(results + result_place(n, m));
         }
     };
-    if constexpr (KIND != KIND_STATISTICS && KIND != KIND_D_HIDDEN) __syncthreads();  // all waves are done with the operands
+    if (KIND == KIND_GRADIENT || (KIND == KIND_D_WEIGHT && splits == 1)) __syncthreads();  // all waves are done with the operands
     if constexpr (KIND == KIND_STATISTICS) {
         const float f = exponent_factor(a);
 #pragma unroll
@@ -357,9 +359,11 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
             }
         }
         send(a.gradient + ((int64_t)t.n * pieces + t.m) * G_TILE, LOSS_TILE * 2, LOSS_TILE, LOSS_TILE);
-    } else if constexpr (KIND == KIND_D_HIDDEN) {
-        // sums over parts stay in the order of the registers: 1 KB of a wave at a time
-        float *out = a.d_part + (((int64_t)split * row_tiles + t.n) * widths + t.m) * (LOSS_TILE * LOSS_TILE) + wave * 8192 + lane * 4;
+    } else if (KIND == KIND_D_HIDDEN || splits > 1) {
+        // sums over parts stay in the order of the registers: 1 KB of a wave at a time; those of d_hidden go on from piece to piece
+        float *out = KIND == KIND_D_HIDDEN ? a.d_part + (((int64_t)split * row_tiles + t.n) * widths + t.m) * (LOSS_TILE * LOSS_TILE)
+                                           : a.w_part + (((int64_t)split * pieces + t.n) * widths + t.m) * (LOSS_TILE * LOSS_TILE);
+        out += wave * 8192 + lane * 4;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -368,7 +372,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
                 for (int c = 0; c < 4; ++c) {
                     f32x4 *p = (f32x4 *)(out + ((j * 4 + i) * 4 + c) * 256);
                     f32x4 v = {acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
-                    if (a.first > 0) v += *p;
+                    if (KIND == KIND_D_HIDDEN && a.first > 0) v += *p;
                     *p = v;
                 }
     } else {
@@ -417,8 +421,8 @@ void plaid_launch_loss_scores(hipStream_t st, const LossArgs &a, int dtype, bool
 void plaid_launch_loss_gradients(hipStream_t st, const LossArgs &a, int dtype)
 {
     const int64_t widths = a.columns / LOSS_TILE;
-    const int hidden = a.d_hidden ? rounded_up(loss_part_tiles(a.padded_rows, a.columns, a.hidden_steps)) : 0;
-    const int weight = a.d_weight ? rounded_up(widths * ((a.piece + LOSS_TILE - 1) / LOSS_TILE)) : 0;
+    const int hidden = a.d_hidden ? rounded_up(loss_hidden_parts(a.padded_rows, a.columns, a.hidden_steps)) : 0;
+    const int weight = !a.d_weight ? 0 : rounded_up(a.w_part ? loss_weight_parts(a.padded_rows, a.columns, a.hidden_steps) : widths * ((a.piece + LOSS_TILE - 1) / LOSS_TILE));
     if (dtype == PLAID_BF16) loss_gradients_kernel<PLAID_BF16><<<hidden + weight, 512, 0, st>>>(a, hidden);
     else loss_gradients_kernel<PLAID_FP16><<<hidden + weight, 512, 0, st>>>(a, hidden);
 }

@@ -68,6 +68,7 @@ struct LossArgs {
     float *own;                        // [padded_rows] product of the target
     char *gradient;                    // [rows / 256][piece / 256][256][256] of the scores, over a piece of the vocabulary
     float *d_part;                     // [parts][tiles of rows that have a target][columns / 256][256 x 256] sums of d_hidden, in the order of the products' registers
+    float *w_part;                     // [parts][piece / 256][columns / 256][256 x 256] the same of d_weight, null where its axis is never cut
     int32_t columns;                   // width rounded up to LOSS_TILE
     int32_t hidden_steps;              // steps of a whole piece along d_hidden's axis
     int64_t first;                     // the piece's first entry, and how many there are
@@ -80,40 +81,53 @@ struct LossArgs {
 #define LOSS_PARTS 512  // tiles of all parts of d_hidden, where there are several
 #define LOSS_FEW 128
 #define LOSS_PREPARE_ONE 1024
-// Tiles that the parts of d_hidden have at most.
-constexpr int64_t loss_part_tiles(int64_t padded_rows, int64_t columns, int64_t steps)
+// Tiles that the parts of d_hidden have at most, and those of d_weight where its axis may be cut, else 0.
+constexpr int64_t loss_most_parts(int64_t tiles, int64_t steps)
 {
-    const int64_t tiles = padded_rows / LOSS_TILE * (columns / LOSS_TILE), most = steps < 4 ? 1 : steps / 4;
+    const int64_t most = steps < 4 ? 1 : steps / 4;
     return tiles > LOSS_PARTS ? tiles : tiles * most < LOSS_PARTS ? tiles * most : LOSS_PARTS;
+}
+constexpr int64_t loss_hidden_parts(int64_t padded_rows, int64_t columns, int64_t steps) { return loss_most_parts(padded_rows / LOSS_TILE * (columns / LOSS_TILE), steps); }
+constexpr int64_t loss_weight_parts(int64_t padded_rows, int64_t columns, int64_t steps)
+{
+    const int64_t tiles = (steps + 3) / 4 * (columns / LOSS_TILE);
+    return tiles < 256 ? loss_most_parts(tiles, padded_rows / LOSS_STEP) : 0;
 }
 void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool backward);
 void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int entries, bool gradient);
 void plaid_launch_loss_join(hipStream_t st, const LossArgs &a, int parts, bool packed);
 void plaid_launch_loss_scores(hipStream_t st, const LossArgs &a, int dtype, bool backward);
 void plaid_launch_loss_gradients(hipStream_t st, const LossArgs &a, int dtype);
-void plaid_launch_loss_d_hidden_join(hipStream_t st, const LossArgs &a, int dtype);
+void plaid_launch_loss_gradients_join(hipStream_t st, const LossArgs &a, int dtype);
 
 #ifdef __HIP__
-// Parts that the vocabulary's axis of d_hidden is cut into, from the number of rows that have a target.  Beside d_weight's tiles, which fill up what
-// is left of the chip: so many that none takes longer than all together take on average (7296 rows of 2048 on 128000 entries, 160 tiles:
-// one part, 4820 us for both gradients in place of 4960 with three).  Alone: as few as leave least of the chip idle in the last round; a part costs
-// what LOSS_PART_STEPS steps of it cost, as its sums are written and read.
-__device__ __forceinline__ int hidden_splits(const LossArgs &a, int live)
+// Parts that the gradients' axes are cut into: the vocabulary's for d_hidden, the rows' for d_weight (where it has fewer tiles than the chip units).
+// Both share a launch and fill up what the other leaves: so many that none takes longer than all together take on average (7296 rows of
+// 2048 on 128000 entries, 160 tiles of d_hidden: one part, 4820 us for both gradients in place of 4960 with three; 8000 rows of 256 on 5000
+// entries, 20 tiles of d_weight: 64 us in place of 164 with one).  d_hidden alone: as few as leave least of the chip idle in the last round.  A
+// part costs what LOSS_PART_STEPS steps of it cost, as its sums are written and read.
+struct LossParts {
+    int hidden, weight;
+};
+__device__ __forceinline__ LossParts loss_parts(const LossArgs &a, int live)
 {
     const int widths = a.columns / LOSS_TILE, tiles = (live + LOSS_TILE - 1) / LOSS_TILE * widths, steps = a.hidden_steps;
-    if (tiles == 0) return 1;
+    LossParts p = {1, 1};
+    if (tiles == 0) return p;
     if (a.d_weight) {
-        const int64_t others = (int64_t)((steps + 3) / 4) * widths * ((live + LOSS_STEP - 1) / LOSS_STEP);
-        const int share = max((int)(((int64_t)tiles * steps + others) / 256), LOSS_PART_STEPS);
-        return max(1, min(min((steps + share - 1) / share, LOSS_PARTS / tiles), steps / 4));
+        const int w_tiles = (steps + 3) / 4 * widths, w_steps = (live + LOSS_STEP - 1) / LOSS_STEP;
+        const int64_t all = (a.d_hidden ? (int64_t)tiles * steps : 0) + (int64_t)w_tiles * w_steps;
+        const int share = max((int)(all / 256), LOSS_PART_STEPS);
+        p.hidden = max(1, min(min((steps + share - 1) / share, LOSS_PARTS / tiles), steps / 4));
+        if (a.w_part) p.weight = max(1, min(min(w_steps / share, LOSS_PARTS / w_tiles), w_steps / 4));  // not for less than twice as long
+        return p;
     }
-    int best = 1;
     float least = 0.0f;
     for (int s = 1; s == 1 || (s * tiles <= LOSS_PARTS && 4 * s <= steps); ++s) {
         const float cost = (float)((tiles * s + 255) / 256) * ((float)steps / (float)s + LOSS_PART_STEPS);
-        if (s == 1 || cost < 0.98f * least) best = s, least = cost;
+        if (s == 1 || cost < 0.98f * least) p.hidden = s, least = cost;
     }
-    return best;
+    return p;
 }
 
 // Scores s = scale h . W are formed from products u = h . W whose sign is that of the scale (the packed states carry it), so that the largest product

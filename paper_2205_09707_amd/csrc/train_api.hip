@@ -81,7 +81,7 @@ struct LossPlan {
     bool few;
     int entries;
     int64_t padded_rows, pitch, columns, piece;
-    int64_t list_bytes, row_bytes, packed_bytes, scaled_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, d_part_bytes, bytes;
+    int64_t list_bytes, row_bytes, packed_bytes, scaled_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, d_part_bytes, w_part_bytes, bytes;
 };
 LossPlan plan_loss(const plaid_token_loss &a, bool backward)
 {
@@ -117,8 +117,9 @@ LossPlan plan_loss(const plaid_token_loss &a, bool backward)
     if (backward) {
         p.gradient_bytes = p.padded_rows * p.piece * 2;
         p.scaled_bytes = p.padded_rows * p.columns * 2;
-        p.d_part_bytes = loss_part_tiles(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
-        p.bytes = p.list_bytes + p.row_bytes + p.packed_bytes + p.scaled_bytes + p.gradient_bytes + p.d_part_bytes;
+        p.d_part_bytes = loss_hidden_parts(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
+        p.w_part_bytes = loss_weight_parts(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
+        p.bytes = p.list_bytes + p.row_bytes + p.packed_bytes + p.scaled_bytes + p.gradient_bytes + p.d_part_bytes + p.w_part_bytes;
     } else {
         p.part_bytes = p.piece / LOSS_PART * p.padded_rows * 8;
         p.running_bytes = p.padded_rows * 8;
@@ -171,7 +172,8 @@ LossArgs loss_args(const plaid_token_loss &a, const LossPlan &p, void *workspace
         if (backward) {
             x.scaled = w, w += p.scaled_bytes;
             x.gradient = w, w += p.gradient_bytes;
-            x.d_part = (float *)w;
+            x.d_part = (float *)w, w += p.d_part_bytes;
+            x.w_part = p.w_part_bytes ? (float *)w : nullptr;
         }
     }
     if (!backward) {
@@ -359,10 +361,11 @@ extern "C" int plaid_cross_entropy_backward(const plaid_token_loss *args, const 
     plaid_launch_loss_pack(st, x, args->dtype, true);
     for (x.first = 0; x.first < x.vocabulary; x.first += p.piece) {
         x.piece = (int32_t)(x.vocabulary - x.first < p.piece ? x.vocabulary - x.first : p.piece);
+        x.last = x.first + p.piece >= x.vocabulary;
         if (p.few) plaid_launch_loss_few(st, x, args->dtype, p.entries, true);
         else plaid_launch_loss_scores(st, x, args->dtype, true);
         plaid_launch_loss_gradients(st, x, args->dtype);
+        plaid_launch_loss_gradients_join(st, x, args->dtype);
     }
-    if (x.d_hidden) plaid_launch_loss_d_hidden_join(st, x, args->dtype);
     return launched();
 }

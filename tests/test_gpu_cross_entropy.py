@@ -236,6 +236,26 @@ def test_weights_beyond_four_gigabytes(pl):
         del s
 
 
+@pytest.mark.parametrize("rows,vocabulary,width", [(30, 900, 64), (300, 5000, 264), (3000, 700, 256)])
+def test_one_gradient_alone(pl, rows, vocabulary, width):
+    """Sums of d_hidden may be cut otherwise without d_weight, so both are held to their bounds."""
+    import ctypes as ct
+    from paper_2205_09707_amd import plaid, training
+    h, w, t, d = _inputs(rows, vocabulary, width, BF)
+    want = cross_entropy(h, w, t, 0.1, d)
+    _, lse = pl.plaid_cross_entropy(h, w, t, scale=0.1, return_lse=True)
+    lib, need = pl.load_library(), ct.c_int64(0)
+    a = training.plaid_token_loss(0, width, rows, vocabulary, 0.1, h.data_ptr(), w.data_ptr(), width, width, t.data_ptr(), None, lse.data_ptr())
+    plaid._check(lib.plaid_cross_entropy_workspace(ct.byref(a), 1, ct.byref(need)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+    for name, like in (("d_hidden", h), ("d_weight", w)):
+        got = torch.full_like(like, NAN)
+        outs = (got.data_ptr(), None) if name == "d_hidden" else (None, got.data_ptr())
+        plaid._check(lib.plaid_cross_entropy_backward(ct.byref(a), d.data_ptr(), 1, *outs, work.data_ptr(), need.value, 0, stream))
+        close(got, want[name], want[name + "_bound"], name + " alone")
+
+
 @pytest.mark.parametrize("rows", [9, 400])
 def test_captured_and_replayed(pl, rows):
     h, w, t, d = _inputs(rows, 2000, 128, BF)
