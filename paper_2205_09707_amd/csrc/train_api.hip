@@ -86,15 +86,15 @@ struct LossPlan {
 LossPlan plan_loss(const plaid_token_loss &a, bool backward)
 {
     LossPlan p = {};
-    // Tiles of 64 entries and 128 rows in place of 256 and 256 where the larger ones would leave much of the chip idle.  us of a forward call with the
-    // small and the large ones (and so many small ones), width 512: 300 rows on 2600 entries 19 and 30 (123), 1000 on 2600 20 and 30 (328), 500 on
-    // 11000 28 and 32 (688); width 1024: 2000 on 2000 28 and 46 (512), 200 on 30000 45 and 43 (938)
-    p.few = a.rows <= LOSS_FEW || ceil_div(a.vocabulary, 64) * ceil_div(a.rows, LOSS_FEW) <= 3 * UNITS;
-    // Entries of a few rows' workgroup: 64 where all workgroups then find room on the chip at once, else more, so that fewer of them read the
-    // rows.  us with 64 and 128, width 1024: 16 rows on 40000 entries 16.3 and 17.1, 48 on 40000 18.2 and 19.3, on 50021 23.9 and 20.9; with 64 and
-    // 256, 90 rows on 50000 49 and 23
-    const int64_t stage = 3 * (64 + 16 * ceil_div(a.rows, 16)) * 128, resident = UNITS * (160 * 1024 / (stage + 2048));
-    p.entries = ceil_div(a.vocabulary, 64) <= resident || a.rows > LOSS_FEW ? 64 : a.rows <= 64 ? 128 : 256;
+    // Tiles of few rows: up to 128 rows, and where all of them then find room on the chip at once, in place of 256 entries and 256 rows.  Of 64 entries
+    // where that is so, else of more, so that fewer workgroups read the rows.  us of a forward call by entries of a tile (64, 128 or 256, large):
+    //   16 rows on 40000 entries, width 1024: 16.3, 17.1;  48 on 40000: 18.2, 19.3;  48 on 50021: 23.9, 20.9;  90 on 50000: 49, 23, 31
+    //   1000 on 2600, width 512: 19, 22, 30;  500 on 11000: 29, 25, 32;  400 on 16000: 32, 27, 31;  250 on 40000: 42, 38, 33
+    //   2000 on 2000, width 1024: 27, 32, 46;  200 on 30000: 46, 36, 44;  200 on 50000: 73, 57, 46
+    const int64_t row_tiles = ceil_div(a.rows, LOSS_FEW), tiles = ceil_div(a.vocabulary, 64) * row_tiles;
+    const int64_t stage = 3 * (64 + 16 * ceil_div(a.rows < LOSS_FEW ? a.rows : LOSS_FEW, 16)) * 128, resident = UNITS * (160 * 1024 / (stage + 2048));
+    p.few = row_tiles <= 1 || tiles <= resident || ceil_div(a.vocabulary, 256) * row_tiles <= UNITS;
+    p.entries = tiles <= resident ? 64 : a.rows <= 64 ? 128 : 256;
     if (p.few && !backward) {
         p.padded_rows = a.rows;
         p.part_bytes = round16(ceil_div(a.vocabulary, p.entries) * p.padded_rows * 8);
