@@ -4,7 +4,14 @@
 // With m the mean of a row, r = 1 / sqrt(variance + eps) and x^ = (x - m) r:  y = x^ w + b, and with g = dy w
 //   dx = r (g - mean(g) - x^ mean(g x^)),   dw = sum over rows of dy x^,   db = sum over rows of dy.
 // A row's threads keep it in registers, so that the variance is that of x - m (no difference of large numbers) and the row is read once.
-// LANES threads have a row, each up to C pieces of eight neighbouring elements, LANES * 8 elements apart.
+// LANES threads have a row, each up to C pieces of eight neighbouring elements, LANES * 8 elements apart.  Rows may start at any element.
+//
+// Memory bounds them: 100000 rows of 2048 in bf16 take 157 us forward (819 MB, 5.2 TB/s) and 241 backward (1.23 GB, 5.1 TB/s), and 8 to add up the
+// workers' sums.  4001 rows of 765 out of rows of 784, in the caches, 8, 12 and 5 us: a chain of loads, sums across lanes and stores.
+// How many threads have a row: as few as hold it in registers, so that no barrier is needed and narrow rows leave no lanes idle (200000 x 64,
+// forward and backward: 38 us with eight lanes, 147 with 64).  Forward, us with a wave and with 256 threads: 100000 x 2048 146 and 171, 100000 x 1500
+// 130 and 241, 3000 x 2048 7.7 and 8.4, but 512 x 2048 5.4 and 4.8, 64 x 4096 9.1 and 4.9, 50000 x 4096 160 and 147.  Backward, where a thread also holds
+// two sums for each of its columns: 60000 x 1500 240 and 323 in all, 100000 x 2048 234 and 240.
 
 // Sums of a row's threads; all of them get both.
 template <int LANES>
@@ -184,7 +191,9 @@ static void launch_norm(hipStream_t st, const NormArgs &a)
     else if (pieces <= 128) GO(64, 2);
     else if (pieces <= 192 && many) GO(64, 3);
     else if (pieces <= 256) many ? GO(64, 4) : GO(256, 1);
-    else if (pieces <= 512) many ? GO(64, 8) : GO(256, 2);
+    else if (pieces <= 320 && many) GO(64, 5);
+    else if (pieces <= 384 && many) GO(64, 6);
+    else if (pieces <= 512) GO(256, 2);
     else if (pieces <= 1024) GO(256, 4);
     else GO(1024, 2);
 #undef GO

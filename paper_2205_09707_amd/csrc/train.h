@@ -80,7 +80,7 @@ struct LossArgs {
 #define LOSS_PART_STEPS 6
 #define LOSS_PARTS 512  // tiles of all parts of d_hidden, where there are several
 #define LOSS_FEW 128
-#define LOSS_PREPARE_ONE 1024
+#define LOSS_PREPARE_ONE 1536
 // Tiles that the parts of d_hidden have at most, and those of d_weight where its axis may be cut, else 0.
 constexpr int64_t loss_most_parts(int64_t tiles, int64_t steps)
 {
@@ -103,7 +103,7 @@ void plaid_launch_loss_gradients_join(hipStream_t st, const LossArgs &a, int dty
 #ifdef __HIP__
 // Parts that the gradients' axes are cut into: the vocabulary's for d_hidden, the rows' for d_weight (where it has fewer tiles than the chip units).
 // Both share a launch and fill up what the other leaves: so many that none takes longer than all together take on average (7296 rows of
-// 2048 on 128000 entries, 160 tiles of d_hidden: one part, 4820 us for both gradients in place of 4960 with three; 8000 rows of 256 on 5000
+// 2048 on 128000 entries, 160 tiles of d_hidden: one part, 4820 us for both gradients in place of 4960 with three at the time; 8000 rows of 256 on 5000
 // entries, 20 tiles of d_weight: 64 us in place of 164 with one).  d_hidden alone: as few as leave least of the chip idle in the last round.  A
 // part costs what LOSS_PART_STEPS steps of it cost, as its sums are written and read.
 struct LossParts {
