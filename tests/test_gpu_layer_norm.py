@@ -146,3 +146,20 @@ def test_refusals(pl):
     w.requires_grad_()
     with pytest.raises(ValueError, match="weight requires a gradient"):
         pl.plaid_layer_norm(x, w, b)
+
+
+def test_rows_beyond_four_gigabytes(pl):
+    """The same thousand rows again and again: every thousand of the result is the first, bit for bit, and the first is right."""
+    rows, width = 1_100_000, 2048
+    few, w, b, d = _inputs(1000, width, BF)
+    x = torch.empty(rows, width, dtype=BF, device=DEV)
+    x.view(1100, 1000, width)[:] = few
+    out, statistics = pl.plaid_layer_norm(x, w, b, return_statistics=True)
+    want = norm(few, w, b, 1e-5, d)
+    close(out[:1000], want["out"], want["out_bound"], "out")
+    d = d.expand(1100, 1000, width).reshape(rows, width)
+    dx, _, _ = pl.plaid_layer_norm_backward(d, x, w, b, statistics)
+    close(dx[:1000], want["dx"], want["dx_bound"], "dx")
+    for t in (out, statistics, dx):
+        for block in t.view(1100, 1000, -1).split(100):
+            assert (block == t[:1000]).all()
