@@ -13,7 +13,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import plaid as _p
-from .reader import _DTYPES, _is, _where, _workspace
+from .reader import _DTYPES, _workspace
 
 
 class plaid_token_loss(ct.Structure):
@@ -38,11 +38,18 @@ def declare(lib: ct.CDLL) -> None:
     lib.plaid_cross_entropy_workspace.argtypes = [loss, i32, out64]
 
 
-def _states(t: torch.Tensor, name: str, dim: Optional[int] = 2) -> torch.device:
-    """Checks a tensor of states; its device."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _DTYPES or (dim is not None and t.dim() != dim):
+def _states(t: torch.Tensor, name: str, dim: Optional[int] = 2) -> int:
+    """Checks a tensor of states; its device's ordinal."""
+    device = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if device < 0 or t.dtype not in _DTYPES or (dim is not None and t.dim() != dim):
         raise ValueError(f"{name} must be a CUDA tensor of dtype torch.bfloat16 or torch.float16" + ("" if dim is None else f" with {dim} dimensions"))
-    return t.device
+    return device
+
+
+def _same(t: torch.Tensor, name: str, dtype: torch.dtype, shape, device: int) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name} must be a tensor of dtype {dtype} and shape {tuple(shape)} on the device of the states")
+    return t
 
 
 def _not_recorded(backward: str, **tensors) -> None:
@@ -58,6 +65,8 @@ _recording = torch.is_grad_enabled
 
 def _rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
     """A matrix whose rows are contiguous, and from one row to the next."""
+    if t.is_contiguous():
+        return t, t.shape[1]
     row, one = t.stride()
     if one != 1 and t.shape[1] > 1:
         t = t.contiguous()
@@ -78,24 +87,28 @@ def _aligned_rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
     return t, stride
 
 
-def _parameter(t: Optional[torch.Tensor], name: str, x: torch.Tensor, width: int) -> Tuple[Optional[torch.Tensor], Optional[int]]:
+def _parameter(t: Optional[torch.Tensor], name: str, x: torch.Tensor, width: int, device: int) -> Tuple[Optional[torch.Tensor], Optional[int]]:
     """A weight or bias of x's rows, and its address."""
     if t is None:
         return None, None
-    if t.dtype is not x.dtype or t.dim() != 1 or t.shape[0] != width or t.device != x.device:
+    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.dtype is not x.dtype or t.dim() != 1 or t.shape[0] != width:
         raise ValueError(f"{name} must hold {width} values of x's dtype on its device")
-    if t.stride(0) != 1:
+    if not t.is_contiguous():
         t = t.contiguous()
     return t, t.data_ptr()
 
 
-def _numbers(t: torch.Tensor, name: str, device: torch.device, size: Optional[int] = None) -> torch.Tensor:
+def _numbers(t: torch.Tensor, name: str, device: int, size: Optional[int] = None) -> torch.Tensor:
     """A vector of 64-bit integers."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int64 or t.dim() != 1 or t.device != device:
-        raise ValueError(f"{name} must be a tensor of dtype torch.int64 with 1 dimension on {device}")
+    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.dtype is not torch.int64 or t.dim() != 1:
+        raise ValueError(f"{name} must be a tensor of dtype torch.int64 with 1 dimension on the device of the states")
     if size is not None and t.shape[0] != size:
         raise ValueError(f"{name} must hold {size} values, got {t.shape[0]}")
     return t if t.is_contiguous() else t.contiguous()
+
+
+def _stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def plaid_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
@@ -109,7 +122,7 @@ def plaid_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) 
     n = ids.shape[0]
     out = table.new_empty((n, width))
     _p._check(_p.load_library().plaid_embedding(table.data_ptr(), stride, vocabulary, width, ids.data_ptr(), n, scale, out.data_ptr(), _DTYPES[table.dtype],
-                                                *_where(dev)))
+                                                dev, _stream(dev)))
     return out
 
 
@@ -124,15 +137,15 @@ def plaid_embedding_backward(d_out: torch.Tensor, ids: torch.Tensor, vocabulary:
     if add_to is None:
         d_table = d_out.new_empty((vocabulary, width))
     else:
-        d_table = _is(add_to, "add_to", d_out.dtype, 2, dev)
-        if tuple(d_table.shape) != (vocabulary, width) or not d_table.is_contiguous():
-            raise ValueError(f"add_to must be contiguous and have the shape {(vocabulary, width)}")
+        d_table = _same(add_to, "add_to", d_out.dtype, (vocabulary, width), dev)
+        if not d_table.is_contiguous():
+            raise ValueError("add_to must be contiguous")
     lib = _p.load_library()
     need = ct.c_int64(0)
     _p._check(lib.plaid_embedding_backward_workspace(n, vocabulary, width, ct.byref(need)))
-    work, ptr = _workspace(need.value, dev)
+    work, ptr = _workspace(need.value, d_out.device)
     _p._check(lib.plaid_embedding_backward(d_out.data_ptr(), stride, vocabulary, width, ids.data_ptr(), n, scale, 0 if add_to is None else 1,
-                                           d_table.data_ptr(), _DTYPES[d_out.dtype], ptr, need.value, *_where(dev)))
+                                           d_table.data_ptr(), _DTYPES[d_out.dtype], ptr, need.value, dev, _stream(dev)))
     return d_table
 
 
@@ -148,12 +161,10 @@ def plaid_dropout(x: torch.Tensor, p: float, rng: torch.Tensor, residual: Option
         x = x.contiguous()
     other = None
     if residual is not None:
-        if not isinstance(residual, torch.Tensor) or residual.dtype is not x.dtype or residual.shape != x.shape or residual.device != dev:
-            raise ValueError("residual must have x's shape and dtype on its device")
-        residual = residual.contiguous()
+        residual = _same(residual, "residual", x.dtype, x.shape, dev).contiguous()
         other = residual.data_ptr()
     out = torch.empty_like(x)
-    _p._check(_p.load_library().plaid_dropout(x.data_ptr(), other, x.numel(), p, rng.data_ptr(), out.data_ptr(), _DTYPES[x.dtype], *_where(dev)))
+    _p._check(_p.load_library().plaid_dropout(x.data_ptr(), other, x.numel(), p, rng.data_ptr(), out.data_ptr(), _DTYPES[x.dtype], dev, _stream(dev)))
     return out
 
 
@@ -162,16 +173,16 @@ def plaid_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bia
     """Layer norm of the rows of x [rows, width], times weight [width], plus bias [width].  With return_statistics also what
     plaid_layer_norm_backward wants, each row's mean and 1 / sqrt(variance + eps), [rows, 2] float32."""
     dev = _states(x, "x")
-    if _recording():
+    if _recording() and (x.requires_grad or weight is not None or bias is not None):
         _not_recorded("plaid_layer_norm_backward", x=x, weight=weight, bias=bias)
     x, stride = _rows(x)
     rows, width = x.shape
-    weight, w = _parameter(weight, "weight", x, width)
-    bias, b = _parameter(bias, "bias", x, width)
+    weight, w = _parameter(weight, "weight", x, width, dev)
+    bias, b = _parameter(bias, "bias", x, width, dev)
     out = torch.empty_like(x) if stride == width else x.new_empty((rows, width))
     statistics = x.new_empty((rows, 2), dtype=torch.float32) if return_statistics else None
     _p._check(_p.load_library().plaid_layer_norm(x.data_ptr(), stride, w, b, rows, width, eps, out.data_ptr(), None if statistics is None else statistics.data_ptr(),
-                                                 _DTYPES[x.dtype], *_where(dev)))
+                                                 _DTYPES[x.dtype], dev, _stream(dev)))
     return (out, statistics) if return_statistics else out
 
 
@@ -179,14 +190,11 @@ def plaid_layer_norm_backward(d_out: torch.Tensor, x: torch.Tensor, weight: Opti
                               statistics: torch.Tensor):
     """(dx, dweight, dbias) of plaid_layer_norm from its statistics and the gradient d_out; None for a weight or bias that there is not."""
     dev = _states(x, "x")
-    if _is(d_out, "d_out", x.dtype, 2, dev).shape != x.shape:
-        raise ValueError("d_out must have x's shape")
+    _same(d_out, "d_out", x.dtype, x.shape, dev)
     rows, width = x.shape
-    weight, w = _parameter(weight, "weight", x, width)
-    bias, _ = _parameter(bias, "bias", x, width)
-    if _is(statistics, "statistics", torch.float32, 2, dev).shape != (rows, 2):
-        raise ValueError("statistics must be what plaid_layer_norm returned")
-    statistics = statistics.contiguous()
+    weight, w = _parameter(weight, "weight", x, width, dev)
+    bias, _ = _parameter(bias, "bias", x, width, dev)
+    statistics = _same(statistics, "statistics", torch.float32, (rows, 2), dev).contiguous()
     x, stride = _rows(x)
     d_out, d_stride = _rows(d_out)
     dx = torch.empty_like(x) if stride == width else x.new_empty((rows, width))
@@ -196,10 +204,10 @@ def plaid_layer_norm_backward(d_out: torch.Tensor, x: torch.Tensor, weight: Opti
     need = ct.c_int64(0)
     if weight is not None or bias is not None:
         _p._check(lib.plaid_layer_norm_backward_workspace(rows, width, ct.byref(need)))
-    work, ptr = _workspace(need.value, dev)
+    work, ptr = _workspace(need.value, x.device)
     _p._check(lib.plaid_layer_norm_backward(d_out.data_ptr(), d_stride, x.data_ptr(), stride, w, statistics.data_ptr(), rows, width, dx.data_ptr(),
                                             None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(), _DTYPES[x.dtype], ptr,
-                                            need.value, *_where(dev)))
+                                            need.value, dev, _stream(dev)))
     return dx, dweight, dbias
 
 
@@ -215,8 +223,8 @@ def _loss_args(hidden, weight, targets, scale, loss, lse) -> plaid_token_loss:
 
 def _loss_inputs(hidden, weight, targets):
     dev = _states(hidden, "hidden")
-    if _is(weight, "weight", hidden.dtype, 2, dev).shape[1] != hidden.shape[1]:
-        raise ValueError("hidden and weight must have rows of one width")
+    if _states(weight, "weight") != dev or weight.dtype is not hidden.dtype or weight.shape[1] != hidden.shape[1]:
+        raise ValueError("hidden and weight must have rows of one width, one dtype and one device")
     targets = _numbers(targets, "targets", dev, hidden.shape[0])
     return _aligned_rows(hidden), _aligned_rows(weight), targets
 
@@ -226,9 +234,9 @@ def plaid_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: tor
     [vocabulary, width], targets [rows] int64 -> [rows] float32, zero for a target outside the vocabulary.  With return_lse also what
     plaid_cross_entropy_backward wants, the logarithm of the softmax's sum as two numbers to be added, [rows, 2] float32."""
     rows, table, targets = _loss_inputs(hidden, weight, targets)
-    if _recording():
+    if _recording() and (hidden.requires_grad or weight.requires_grad):
         _not_recorded("plaid_cross_entropy_backward", hidden=hidden, weight=weight)
-    dev = hidden.device
+    dev = hidden.get_device()
     n = hidden.shape[0]
     loss = hidden.new_empty(n, dtype=torch.float32)
     lse = hidden.new_empty((n, 2), dtype=torch.float32) if return_lse else None
@@ -236,8 +244,8 @@ def plaid_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: tor
     a = _loss_args(rows, table, targets, scale, loss, lse)
     need = ct.c_int64(0)
     _p._check(lib.plaid_cross_entropy_workspace(ct.byref(a), 0, ct.byref(need)))
-    work, ptr = _workspace(need.value, dev)
-    _p._check(lib.plaid_cross_entropy(ct.byref(a), ptr, need.value, *_where(dev)))
+    work, ptr = _workspace(need.value, hidden.device)
+    _p._check(lib.plaid_cross_entropy(ct.byref(a), ptr, need.value, dev, _stream(dev)))
     return (loss, lse) if return_lse else loss
 
 
@@ -246,22 +254,17 @@ def plaid_cross_entropy_backward(d_loss: torch.Tensor, hidden: torch.Tensor, wei
     """(d_hidden, d_weight) of plaid_cross_entropy from its lse and the gradient of its result, d_loss [rows] float32 (an expanded single
     number is taken as it is)."""
     rows, table, targets = _loss_inputs(hidden, weight, targets)
-    dev = hidden.device
-    n = hidden.shape[0]
-    if _is(d_loss, "d_loss", torch.float32, 1, dev).shape[0] != n:
-        raise ValueError(f"d_loss must hold {n} values, got {d_loss.shape[0]}")
-    if d_loss.stride(0) not in (0, 1):
+    dev, n = hidden.get_device(), hidden.shape[0]
+    if _same(d_loss, "d_loss", torch.float32, (n,), dev).stride(0) not in (0, 1):
         d_loss = d_loss.contiguous()
-    if _is(lse, "lse", torch.float32, 2, dev).shape != (n, 2):
-        raise ValueError("lse must be what plaid_cross_entropy returned")
-    lse = lse.contiguous()
+    lse = _same(lse, "lse", torch.float32, (n, 2), dev).contiguous()
     d_hidden = hidden.new_empty(hidden.shape)
     d_weight = hidden.new_empty(weight.shape)
     lib = _p.load_library()
     a = _loss_args(rows, table, targets, scale, None, lse)
     need = ct.c_int64(0)
     _p._check(lib.plaid_cross_entropy_workspace(ct.byref(a), 1, ct.byref(need)))
-    work, ptr = _workspace(need.value, dev)
+    work, ptr = _workspace(need.value, hidden.device)
     _p._check(lib.plaid_cross_entropy_backward(ct.byref(a), d_loss.data_ptr(), d_loss.stride(0) if n > 1 else 1, d_hidden.data_ptr(), d_weight.data_ptr(), ptr, need.value,
-                                               *_where(dev)))
+                                               dev, _stream(dev)))
     return d_hidden, d_weight
