@@ -24,7 +24,7 @@ template <int DT, bool RESIDUAL>
 __global__ __launch_bounds__(256) void dropout_kernel(const char *x, const char *residual, int64_t n, uint32_t threshold, float factor, const int64_t *rng, char *out)
 {
     const uint64_t seed = (uint64_t)uniform_load(rng), call = (uint64_t)uniform_load(rng + 1);
-    const int64_t group = (int64_t)blockIdx.x * 256 + threadIdx.x, at = group * 8;
+    const int64_t group = wide_block() * 256 + threadIdx.x, at = group * 8;
     if (at >= n) return;
     const int here = (int)min(n - at, (int64_t)8);
     const i32x4 raw = load_piece(x + 2 * at, 0, here);
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const char *x, const char 
 void plaid_launch_dropout(hipStream_t st, const char *x, const char *residual, int64_t n, uint32_t threshold, const int64_t *rng, char *out, int dtype)
 {
     const float factor = threshold < 65536 ? 65536.0f / (float)(65536 - threshold) : 0.0f;
-    const dim3 grid((unsigned)((n + 2047) / 2048));
+    const dim3 grid = wide_grid((n + 2047) / 2048);
 #define GO(DT, R) dropout_kernel<DT, R><<<grid, 256, 0, st>>>(x, residual, n, threshold, factor, rng, out)
     if (dtype == PLAID_BF16) residual ? GO(PLAID_BF16, true) : GO(PLAID_BF16, false);
     else residual ? GO(PLAID_FP16, true) : GO(PLAID_FP16, false);

@@ -7,7 +7,7 @@ template <int DT, int ROWS>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs e, int team_shift)
 {
     const int lane = threadIdx.x & ((1 << team_shift) - 1), teams = 256 >> team_shift;
-    const int64_t t0 = ((int64_t)blockIdx.x * teams + (threadIdx.x >> team_shift)) * ROWS;
+    const int64_t t0 = (wide_block() * teams + (threadIdx.x >> team_shift)) * ROWS;
     if (t0 >= e.n) return;
     const char *row[ROWS];
     bool there[ROWS];
@@ -34,8 +34,8 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs e, int team_shift)
 #define FILL_EACH 4  // pieces of 16 bytes that a thread fills
 // --- the tokens in ascending order, equal ones in the order in which they stood -------------------------------------------------
 // A radix sort from the lowest digit on; up to SORT_ONE tokens by one workgroup and in one launch (with the gradient of 50000 x 768: 100 tokens 26 us
-// in place of 41 with three launches a pass, 4000 34 and 53, 8000 46 and 59).  Each wave has a stretch of places and goes through it 64 at a time: lanes with the same digit find
-// each other by votes, so that every place's rank is counted in order and none depends on which atomic came first.
+// in place of 41 with three launches a pass, 4000 34 and 53, 8000 46 and 59).  Each wave has a stretch of places and goes through it 64 at a time:
+// lanes with the same digit find each other by votes, so that every place's rank is counted in order and none depends on which atomic came first.
 __device__ __forceinline__ int token_key(const EmbedArgs &e, int64_t t)
 {
     const int64_t id = e.ids[t];
@@ -63,15 +63,16 @@ __device__ __forceinline__ int rank_digit(int digit, bool there, int bits, volat
 __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedArgs e, int64_t pieces)
 {
     constexpr int WAVES = 16, EACH = SORT_ONE / 1024;
-    if (blockIdx.x > 0) {
+    const int64_t block = wide_block();
+    if (block > 0) {
         const i32x4 zero = {0, 0, 0, 0};
-        const int64_t first = (int64_t)(blockIdx.x - 1) * (1024 * FILL_EACH) + threadIdx.x;
+        const int64_t first = (block - 1) * (1024 * FILL_EACH) + threadIdx.x;
 #pragma unroll
         for (int i = 0; i < FILL_EACH; ++i)
             if (first + i * 1024 < pieces) *(i32x4_any *)(e.d_table + (first + i * 1024) * 16) = zero;
         // what is left of a whole number of pieces
         const int64_t rest = pieces * 8 + threadIdx.x;
-        if (blockIdx.x == 1 && rest < e.vocabulary * e.width) *(uint16_t *)(e.d_table + 2 * rest) = 0;
+        if (block == 1 && rest < e.vocabulary * e.width) *(uint16_t *)(e.d_table + 2 * rest) = 0;
         return;
     }
     if (threadIdx.x == 0) *e.shared = 0;
@@ -394,7 +395,7 @@ void plaid_launch_embedding(hipStream_t st, const EmbedArgs &e, int dtype)
     const int shift = team_shift_of(e.width);
     const int64_t teams = 256 >> shift;
     const bool four = e.n >= 4096 * teams;
-    const dim3 grid((unsigned)((e.n + teams * (four ? 4 : 1) - 1) / (teams * (four ? 4 : 1))));
+    const dim3 grid = wide_grid((e.n + teams * (four ? 4 : 1) - 1) / (teams * (four ? 4 : 1)));
 #define GO(DT, R) embed_kernel<DT, R><<<grid, 256, 0, st>>>(e, shift)
     if (dtype == PLAID_BF16) four ? GO(PLAID_BF16, 4) : GO(PLAID_BF16, 1);
     else four ? GO(PLAID_FP16, 4) : GO(PLAID_FP16, 1);
@@ -408,7 +409,7 @@ static void launch_backward(hipStream_t st, const EmbedArgs &e)
     if (one) {
         const int64_t pieces = fill ? e.vocabulary * e.width / 8 : 0;
         const int64_t blocks = fill ? (pieces + 1024 * FILL_EACH - 1) / (1024 * FILL_EACH) : 0;
-        sort_one_kernel<<<(unsigned)(1 + (fill && blocks == 0 ? 1 : blocks)), 1024, 0, st>>>(e, pieces);
+        sort_one_kernel<<<wide_grid(1 + (fill && blocks == 0 ? 1 : blocks)), 1024, 0, st>>>(e, pieces);
     } else
         for (int pass = 0; pass < e.passes; ++pass) {
             const int tiles = (int)((e.n + SORT_TILE - 1) / SORT_TILE);

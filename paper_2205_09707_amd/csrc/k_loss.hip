@@ -175,8 +175,8 @@ __device__ __forceinline__ float2 join_parts(float2 x, float2 y, float f)
 
 // --- few rows -------------------------------------------------------------------------------------------------------------------
 // The vocabulary is read at the rate of memory if enough of it is under way: a workgroup has 64 BLOCKS entries, a quarter for each of its four
-// waves, and up to 16 GROUPS rows (more than 128: those of 128 after those); 64 columns of both go straight into LDS, some steps ahead of the products.  Forward it takes the caller's
-// rows, all of them (a row without a target has its own column of the result, and is left out when parts are joined); backward (GRADIENT) the
+// waves, and up to 16 GROUPS rows (more than 128: those of 128 after those); 64 columns of both go straight into LDS, some steps ahead of the
+// products.  Forward it takes the caller's rows, all of them (a row without a target has its own column of the result, and is left out when parts are joined); backward (GRADIENT) the
 // packed ones, and leaves G over the piece as the products take it, with zeros up to whole steps of 64 rows and entries.
 template <int DT, int WAVES, int BLOCKS, int GROUPS, bool GRADIENT>
 __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
@@ -352,8 +352,7 @@ void plaid_launch_loss_few(hipStream_t st, const LossArgs &a, int dtype, int ent
 // --- parts joined ---------------------------------------------------------------------------------------------------------------
 // ROWS rows a workgroup, so that lanes read neighbours where there are many rows, and all threads have work where there are few (a forward call on
 // 32000 entries of 512 with 1, 8 and 32 rows: 16 rows 10.2, 11.4, 15.6 us; 500 30.9, 30.7, 32.5; 8000 296, 285, 281); its threads of one row take the
-// parts in turn.  With the last piece come the loss and lse: the target's score is
-// not among the parts, so that where it is the largest the sum beside it is what the others have, and a loss near nothing keeps its digits.
+// parts in turn.  With the last piece come the loss and lse: the target's score is not among the parts, so that where it is the largest the sum beside it is what the others have, and a loss near nothing keeps its digits.
 template <int ROWS>
 __global__ __launch_bounds__(256) void loss_join_kernel(LossArgs a, int parts, int packed)
 {
@@ -432,8 +431,9 @@ __device__ __forceinline__ void join_gradients(const LossArgs &a, int id)
 template <int DT>
 __global__ __launch_bounds__(256) void loss_gradients_join_kernel(LossArgs a, int hidden)
 {
-    if ((int)blockIdx.x < hidden) join_gradients<DT, false>(a, blockIdx.x);
-    else join_gradients<DT, true>(a, blockIdx.x - hidden);
+    const int id = (int)wide_block();
+    if (id < hidden) join_gradients<DT, false>(a, id);
+    else join_gradients<DT, true>(a, id - hidden);
 }
 // After each piece for d_weight, if its axis may be cut, after the last one for d_hidden.
 void plaid_launch_loss_gradients_join(hipStream_t st, const LossArgs &a, int dtype)
@@ -441,6 +441,6 @@ void plaid_launch_loss_gradients_join(hipStream_t st, const LossArgs &a, int dty
     const int widths = a.columns / LOSS_TILE, hidden = a.d_hidden && a.last ? a.padded_rows / LOSS_TILE * widths * 64 : 0;
     const int weight = a.d_weight && a.w_part ? (a.piece + LOSS_TILE - 1) / LOSS_TILE * widths * 64 : 0;
     if (hidden + weight == 0) return;
-    if (dtype == PLAID_BF16) loss_gradients_join_kernel<PLAID_BF16><<<hidden + weight, 256, 0, st>>>(a, hidden);
-    else loss_gradients_join_kernel<PLAID_FP16><<<hidden + weight, 256, 0, st>>>(a, hidden);
+    if (dtype == PLAID_BF16) loss_gradients_join_kernel<PLAID_BF16><<<wide_grid(hidden + weight), 256, 0, st>>>(a, hidden);
+    else loss_gradients_join_kernel<PLAID_FP16><<<wide_grid(hidden + weight), 256, 0, st>>>(a, hidden);
 }

@@ -10,8 +10,8 @@
 // An operand lies in memory with k along its rows, or across them; the latter goes into LDS as it is and is read transposed.  Eight waves
 // have 128 x 64 of a tile each.  The axis that is to lie together in memory is the one of the result's registers (M): four neighbours a lane.
 //
-// Measured, 7296 rows of 2048, 5107 of them with a target, on 128000 entries in bf16 (2.7 TFLOP a product): statistics of the scores 2220 us = 1.21 PFLOP/s,
-// G 2350 = 1.14, both gradients 4520 = 1.18.  A step of 64 takes 1.6 us (1.34 PFLOP/s), a tile's first loads and its way out 5 (statistics) to 7 (G).
+// Measured, 7296 rows of 2048, 5107 of them with a target, on 128000 entries in bf16 (2.7 TFLOP a product): statistics of the scores 2160 us = 1.24 PFLOP/s,
+// G 2260 = 1.18, both gradients 4370 = 1.23 (another card: 2220, 2350 and 4520).  A step of 64 takes 1.6 us (1.34 PFLOP/s), a tile's first loads and its way out 5 (statistics) to 7 (G).
 // The matrix units are busy for 63 % of the time at 1.73 GHz, and for 52 % at 1.9 GHz before the reads of operands lay among the products: what is
 // left is power and the loads (statistics without loads 1855 in place of 2276, without reads of LDS 2064, without waiting for loads 2243).
 // Kept out: lines of later steps touched in advance (2515), a wave's priority raised for its products (no change), four waves with 128 x 128 each, which

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
     constexpr int THREADS = LANES < 256 ? 256 : LANES;
     __shared__ float2 lds[THREADS / 64];
     const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)blockIdx.x * (THREADS / LANES) + threadIdx.x / LANES;
+    const int64_t row = wide_block() * (THREADS / LANES) + threadIdx.x / LANES;
     if (row >= a.rows) return;  // whole teams
     const char *x = a.x + row * a.x_stride;
     Eight v[C];
@@ -182,7 +182,7 @@ static void launch_norm(hipStream_t st, const NormArgs &a)
 {
     const int pieces = (a.width + 7) / 8;
     const bool many = a.rows >= NORM_MANY;
-#define GO(LANES, C) norm_kernel<DT, LANES, C><<<(unsigned)((a.rows * LANES + 255) / (LANES < 256 ? 256 : LANES)), LANES < 256 ? 256 : LANES, 0, st>>>(a)
+#define GO(LANES, C) norm_kernel<DT, LANES, C><<<wide_grid((a.rows * LANES + 255) / (LANES < 256 ? 256 : LANES)), LANES < 256 ? 256 : LANES, 0, st>>>(a)
     if (pieces == 1) GO(1, 1);
     else if (pieces <= 8) GO(8, 1);
     else if (pieces <= 16) GO(16, 1);

@@ -63,11 +63,13 @@ struct LossArgs {
     LossRow *row;                      // [padded_rows]
     char *packed;                      // [rows / 256][pitch / 64][256][64] states, with the sign of the scale
     char *scaled;                      // [rows / 64][columns / 256][64][256] the same times 2^(exponent - largest)
-    float2 *part;                      // [parts][padded_rows] largest product and sum of exponentials beside it over parts of the vocabulary, without the target
+    float2 *part;                      // [parts][padded_rows] largest product and sum of exponentials beside it over parts of the
+                                       // vocabulary, without the target
     float2 *running;                   // [padded_rows] over all parts before
     float *own;                        // [padded_rows] product of the target
     char *gradient;                    // [rows / 256][piece / 256][256][256] of the scores, over a piece of the vocabulary
-    float *d_part;                     // [parts][tiles of rows that have a target][columns / 256][256 x 256] sums of d_hidden, in the order of the products' registers
+    float *d_part;                     // [parts][tiles of rows that have a target][columns / 256][256 x 256] sums of d_hidden, in the
+                                       // order of the products' registers
     float *w_part;                     // [parts][piece / 256][columns / 256][256 x 256] the same of d_weight, null where its axis is never cut
     int32_t columns;                   // width rounded up to LOSS_TILE
     int32_t hidden_steps;              // steps of a whole piece along d_hidden's axis
@@ -101,6 +103,11 @@ void plaid_launch_loss_gradients(hipStream_t st, const LossArgs &a, int dtype);
 void plaid_launch_loss_gradients_join(hipStream_t st, const LossArgs &a, int dtype);
 
 #ifdef __HIP__
+// An axis of a grid has fewer than 2^32 threads: more workgroups than WIDE_GRID, of up to 1024, take a second one, whose last row goes past the end.
+#define WIDE_GRID (1 << 21)
+inline dim3 wide_grid(int64_t blocks) { return blocks <= WIDE_GRID ? dim3((unsigned)blocks) : dim3(WIDE_GRID, (unsigned)((blocks + WIDE_GRID - 1) / WIDE_GRID)); }
+__device__ __forceinline__ int64_t wide_block() { return (int64_t)blockIdx.y * WIDE_GRID + blockIdx.x; }
+
 // Parts that the gradients' axes are cut into: the vocabulary's for d_hidden, the rows' for d_weight (where it has fewer tiles than the chip units).
 // Both share a launch and fill up what the other leaves: so many that none takes longer than all together take on average (7296 rows of
 // 2048 on 128000 entries, 160 tiles of d_hidden: one part, 4820 us for both gradients in place of 4960 with three at the time; 8000 rows of 256 on 5000

@@ -122,3 +122,18 @@ def test_refusals(pl):
     x.requires_grad_()
     with pytest.raises(ValueError, match="x requires a gradient"):
         pl.plaid_dropout(x, 0.1, _rng(1, 2))
+
+
+def test_more_threads_than_one_axis_of_a_grid_has(pl):
+    """2^32 groups of eight elements and some more: the counter's second word is used too."""
+    n = 2 ** 35 + 2048 + 5
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 5 * n:
+        pytest.skip("the arrays do not fit beside what else the card holds")
+    x = torch.ones(n, device=DEV, dtype=BF)
+    out = pl.plaid_dropout(x, 0.5, _rng(5, 6))
+    del x
+    for first in (0, 2 ** 34, 2 ** 35 - 2048 - 16, 2 ** 35 - 16, n - 37):
+        first = first // 8 * 8
+        mask, factor = kept(first, 29, 0.5, 5, 6)
+        assert torch.equal(out[first:first + 29].double().cpu(), mask * factor), first
