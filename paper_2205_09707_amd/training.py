@@ -2,7 +2,8 @@
 over a vocabulary, with their gradients.
 
 Like `reader.py` this only marshals, and keeps nothing from one call for the next.  Autograd records none of the calls: each gradient
-is a call of its own, and inputs that require a gradient are refused where it is enabled (examples/reader.py has the Functions).
+is a call of its own, and inputs that require a gradient are refused where it is enabled, those of the gradients' calls too (examples/reader.py
+has the Functions).
 """
 from __future__ import annotations
 
@@ -52,12 +53,12 @@ def _same(t: torch.Tensor, name: str, dtype: torch.dtype, shape, device: int) ->
     return t
 
 
-def _not_recorded(backward: str, **tensors) -> None:
-    """Called where autograd is enabled and one of the tensors may require a gradient."""
+def _not_recorded(backward: Optional[str], **tensors) -> None:
+    """Called where autograd is enabled and one of the tensors may require a gradient; backward: the call that forms it, if there is one."""
     for name, t in tensors.items():
         if t is not None and t.requires_grad:
-            raise ValueError(f"{name} requires a gradient, which this call does not record: call it in torch.no_grad(), or in a "
-                             f"torch.autograd.Function whose backward calls {backward}")
+            raise ValueError(f"{name} requires a gradient, which this call does not record: call it in torch.no_grad()" +
+                             (f", or in a torch.autograd.Function whose backward calls {backward}" if backward else " (gradients of gradients are not formed)"))
 
 
 _recording = torch.is_grad_enabled
@@ -131,6 +132,8 @@ def plaid_embedding_backward(d_out: torch.Tensor, ids: torch.Tensor, vocabulary:
     """The gradient [vocabulary, width] of plaid_embedding's table from that of its result, d_out [n, width]: dense, or added in place to
     `add_to`, which it then returns (a contiguous gradient of the same table from another use)."""
     dev = _states(d_out, "d_out")
+    if _recording() and (d_out.requires_grad or add_to is not None):
+        _not_recorded(None, d_out=d_out, add_to=add_to)
     ids = _numbers(ids, "ids", dev, d_out.shape[0])
     d_out, stride = _rows(d_out)
     n, width = d_out.shape
@@ -191,6 +194,8 @@ def plaid_layer_norm_backward(d_out: torch.Tensor, x: torch.Tensor, weight: Opti
     """(dx, dweight, dbias) of plaid_layer_norm from its statistics and the gradient d_out; None for a weight or bias that there is not."""
     dev = _states(x, "x")
     _same(d_out, "d_out", x.dtype, x.shape, dev)
+    if _recording():
+        _not_recorded(None, d_out=d_out, x=x, weight=weight, bias=bias)
     rows, width = x.shape
     weight, w = _parameter(weight, "weight", x, width, dev)
     bias, _ = _parameter(bias, "bias", x, width, dev)
@@ -255,6 +260,8 @@ def plaid_cross_entropy_backward(d_loss: torch.Tensor, hidden: torch.Tensor, wei
     number is taken as it is)."""
     rows, table, targets = _loss_inputs(hidden, weight, targets)
     dev, n = hidden.get_device(), hidden.shape[0]
+    if _recording():
+        _not_recorded(None, d_loss=d_loss, hidden=hidden, weight=weight)
     if _same(d_loss, "d_loss", torch.float32, (n,), dev).stride(0) not in (0, 1):
         d_loss = d_loss.contiguous()
     lse = _same(lse, "lse", torch.float32, (n, 2), dev).contiguous()

@@ -314,3 +314,16 @@ def test_refusals(pl):
         with pytest.raises(ValueError, match="requires a gradient"):
             pl.plaid_cross_entropy(h, w, t)
         which.requires_grad_(False)
+
+
+def test_gradients_of_gradients_are_refused(pl):
+    h, w = torch.randn(6, 16, device=DEV).to(BF), torch.randn(40, 16, device=DEV).to(BF)
+    t, d = torch.arange(6, device=DEV), torch.ones(6, device=DEV)
+    _, lse = pl.plaid_cross_entropy(h, w, t, return_lse=True)
+    for x, name in ((d, "d_loss"), (h, "hidden"), (w, "weight")):
+        x.requires_grad_()
+        with pytest.raises(ValueError, match=f"{name} requires a gradient"):
+            pl.plaid_cross_entropy_backward(d, h, w, t, lse)
+        with torch.no_grad():
+            pl.plaid_cross_entropy_backward(d, h, w, t, lse)
+        x.requires_grad_(False)

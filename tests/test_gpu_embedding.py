@@ -132,3 +132,14 @@ def test_refusals(pl):
         pl.plaid_embedding(table, ids)
     with torch.no_grad():
         pl.plaid_embedding(table, ids)
+
+
+def test_gradients_of_gradients_are_refused(pl):
+    d, ids, held = torch.randn(6, 16, device=DEV).to(BF), torch.arange(6, device=DEV), torch.zeros(9, 16, device=DEV, dtype=BF)
+    for x, name in ((d, "d_out"), (held, "add_to")):
+        x.requires_grad_()
+        with pytest.raises(ValueError, match=f"{name} requires a gradient"):
+            pl.plaid_embedding_backward(d, ids, 9, add_to=held)
+        with torch.no_grad():
+            pl.plaid_embedding_backward(d, ids, 9, add_to=held)
+        x.requires_grad_(False)

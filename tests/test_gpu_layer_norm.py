@@ -163,3 +163,26 @@ def test_rows_beyond_four_gigabytes(pl):
     for t in (out, statistics, dx):
         for block in t.view(1100, 1000, -1).split(100):
             assert (block == t[:1000]).all()
+
+
+def test_more_threads_than_one_axis_of_a_grid_has(pl):
+    """One row, expanded: each row of the result is the first, and the first is right."""
+    rows, width = 2 ** 29 + 3, 16
+    few, w, b, d = _inputs(1, width, BF)
+    out = pl.plaid_layer_norm(few.expand(rows, width), w, b)
+    want = norm(few, w, b, 1e-5, d)
+    close(out[:1], want["out"], want["out_bound"], "out")
+    for block in out.split(2 ** 26):
+        assert (block == out[:1]).all()
+
+
+def test_gradients_of_gradients_are_refused(pl):
+    x, w, b, d = _inputs(10, 24, BF)
+    _, statistics = pl.plaid_layer_norm(x, w, b, return_statistics=True)
+    for t, name in ((d, "d_out"), (x, "x"), (w, "weight"), (b, "bias")):
+        t.requires_grad_()
+        with pytest.raises(ValueError, match=f"{name} requires a gradient"):
+            pl.plaid_layer_norm_backward(d, x, w, b, statistics)
+        with torch.no_grad():
+            pl.plaid_layer_norm_backward(d, x, w, b, statistics)
+        t.requires_grad_(False)
