@@ -266,7 +266,10 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
                 for (int r = 0; r < 4; ++r) {
                     const int64_t v = mine + 16 * i + r;
                     g[r] = gradient.other(acc[i][j][r]);
-                    if (v == x.target) g[r] = gradient.target(acc[i][j][r]);
+                    if (v == x.target) {
+                        g[r] = gradient.target(acc[i][j][r]);
+                        if (there && v < end) a.rest[t] = left_out<DT>(g[r]);
+                    }
                     if (!there || v >= end) g[r] = 0.0f;
                 }
                 const int at = (int)(mine - first) + 16 * i;
@@ -423,6 +426,15 @@ __device__ __forceinline__ void join_gradients(const LossArgs &a, int id)
     f32x4 v = {0, 0, 0, 0};
 #pragma unroll 4
     for (int s = 0; s < splits; ++s) v += *(const f32x4 *)(p + s * part);
+    if (!WEIGHT && there && column < a.width) {
+        const float rest = a.rest[row];
+        const char *w = a.weight + a.row[row].target * a.weight_stride + column * 2;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float more = rest * load16<DT>(w + 2 * j);
+            if (fabsf(more) < INFINITY) v[j] += more;
+        }
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = ldexpf(v[j] * factor, e == NO_EXPONENT ? 0 : e);
     char *out = WEIGHT ? a.d_weight : a.d_hidden;

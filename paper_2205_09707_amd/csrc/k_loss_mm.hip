@@ -277,6 +277,62 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
         step(steps - 1, std::integral_constant<int, 0>());
     }
 
+    if constexpr (KIND == KIND_D_WEIGHT) {
+        // What the targets' entries left out: the rows whose target is one of the tile's are multiplied again, 64 of them at a time, with a tile that has a
+        // single entry in each.  They are looked for among all of the axis, up to 8192 at a time, in order.  (7296 rows, 5107 with a target, of 2048 on
+        // 128000 entries: FIGURE.)
+        const int end = min(live, (begin + steps) * BK), first_entry = (int)a.first + t.n * LOSS_TILE;
+        int *const list = (int *)lds.far[2], *const counts = (int *)lds.far[1];
+        for (int r0 = begin * BK; r0 < end; r0 += TILE_BYTES / 4) {
+            const int mine0 = r0 + wave * 1024 + lane;  // the lane's rows are 64 apart, a bit each
+            int bits = 0, mine = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                bits |= (int)(mine0 + i * 64 < end && (unsigned)(a.row[min(mine0 + i * 64, end - 1)].target - first_entry) < LOSS_TILE) << i;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mine += __popcll(__ballot(bits >> i & 1));
+            __syncthreads();  // the tiles have been read
+            if (lane == 0) counts[wave] = mine;
+            __syncthreads();
+            int at = 0, all = 0;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                if (w < wave) at += counts[w];
+                all += counts[w];
+            }
+            for (int i = 0; i < 16; ++i) {
+                const uint64_t votes = __ballot(bits >> i & 1);
+                if (bits >> i & 1) list[at + __popcll(votes & ((1ull << lane) - 1))] = mine0 + i * 64;
+                at += __popcll(votes);
+            }
+            for (int b = 0; b < all; b += BK) {
+                __syncthreads();  // the list is there; the tiles have been read
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int load = wave * 4 + i, k = (load & 15) * 4 + (lane >> 4), column = (load >> 4) * 128 + (((lane & 15) ^ swizzle<128>(k)) * 8);
+                    const int row = b + k < all ? list[b + k] : -1;
+                    const char *p = a.scaled + ((int64_t)(row / BK) * widths + t.m) * TILE_BYTES + row % BK * (2 * LOSS_TILE) + column * 2;
+                    load_to_lds(row < 0 ? (const char *)zero_row : p, near_mine + i * 1024);
+                    *(i32x4 *)(lds.far[0] + (i * 512 + threadIdx.x) * 16) = i32x4{0, 0, 0, 0};
+                }
+                __syncthreads();
+                const int k = threadIdx.x;
+                if (k < BK && b + k < all) {
+                    const int row = list[b + k], v = a.row[row].target - first_entry;
+                    store16<DT>(lds.far[0] + (v >> 7) * (TILE_BYTES / 2) + k * 256 + ((((v & 127) >> 3) ^ swizzle<128>(k)) << 4) + (v & 7) * 2, a.rest[row]);
+                }
+                wait_loads<0>();
+                lds_barrier();
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    read(0, 0, s);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) multiply(s, i >> 1, i & 1);
+                }
+            }
+        }
+    }
+
     // a lane's results: column n = 64 wn + 32 j + lane % 32, rows m = 128 wm + 32 i + 8 (r / 4) + 4 (lane / 32) + r % 4
     const int m0 = t.m * LOSS_TILE + wm * 128 + 4 * (lane >> 5), n0 = t.n * LOSS_TILE + wn * 64 + (lane & 31);
     char *const results = lds.near[0];
@@ -362,7 +418,11 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) own = 32 * i + 8 * (r / 4) + r % 4 == target ? acc[i][j][r] : own;
                 const int n = (n0 & 255) + 32 * j, m = (m0 & 255) + target;
-                if (target >= 0 && target < 128 && !(target & 4) && m0 + target < a.piece) store16<DT>(results + result_place(n, m) + (m & 3) * 2, gradient.target(own));
+                if (target >= 0 && target < 128 && !(target & 4) && m0 + target < a.piece) {
+                    const float g = gradient.target(own);
+                    store16<DT>(results + result_place(n, m) + (m & 3) * 2, g);
+                    a.rest[row] = left_out<DT>(g);
+                }
             }
         }
         send(a.gradient + ((int64_t)t.n * pieces + t.m) * G_TILE, LOSS_TILE * 2, LOSS_TILE, LOSS_TILE);

@@ -71,6 +71,7 @@ struct LossArgs {
     float *d_part;                     // [parts][tiles of rows that have a target][columns / 256][256 x 256] sums of d_hidden, in the
                                        // order of the products' registers
     float *w_part;                     // [parts][piece / 256][columns / 256][256 x 256] the same of d_weight, null where its axis is never cut
+    float *rest;                       // [padded_rows] what the rounding of the target's entry of `gradient` left out
     int32_t columns;                   // width rounded up to LOSS_TILE
     int32_t hidden_steps;              // steps of a whole piece along d_hidden's axis
     int64_t first;                     // the piece's first entry, and how many there are
@@ -157,6 +158,14 @@ struct ScoreGradient {
     __device__ __forceinline__ float other(float product) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(product, k, -shift)) * factor; }
     __device__ __forceinline__ float target(float product) const { return expm1f(product * scale - top - log_total) * factor; }
 };
+// The target's entry of G rounds like the others, but a row has nothing larger, so that its rounding alone would be as much of a gradient's error as the
+// result's own: what it left out is kept in 32 bits, and both gradients add its product.  (Where it is no number, they need no digits.)
+template <int DT>
+__device__ __forceinline__ float left_out(float g)
+{
+    const float rest = g - unpack<DT>(pack2<DT>(g, 0.0f), 0);
+    return fabsf(rest) < INFINITY ? rest : 0.0f;
+}
 
 // Sixteen bytes of a row that starts at any element: the memory system takes such addresses.
 typedef i32x4 __attribute__((aligned(2))) i32x4_any;

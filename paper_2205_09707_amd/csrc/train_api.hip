@@ -81,7 +81,7 @@ struct LossPlan {
     bool few;
     int entries;
     int64_t padded_rows, pitch, columns, piece;
-    int64_t list_bytes, row_bytes, packed_bytes, scaled_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, d_part_bytes, w_part_bytes, bytes;
+    int64_t list_bytes, row_bytes, packed_bytes, scaled_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, rest_bytes, d_part_bytes, w_part_bytes, bytes;
 };
 LossPlan plan_loss(const plaid_token_loss &a, bool backward)
 {
@@ -117,9 +117,10 @@ LossPlan plan_loss(const plaid_token_loss &a, bool backward)
     if (backward) {
         p.gradient_bytes = p.padded_rows * p.piece * 2;
         p.scaled_bytes = p.padded_rows * p.columns * 2;
+        p.rest_bytes = p.padded_rows * 4;
         p.d_part_bytes = loss_hidden_parts(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
         p.w_part_bytes = loss_weight_parts(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
-        p.bytes = p.list_bytes + p.row_bytes + p.packed_bytes + p.scaled_bytes + p.gradient_bytes + p.d_part_bytes + p.w_part_bytes;
+        p.bytes = p.list_bytes + p.row_bytes + p.packed_bytes + p.scaled_bytes + p.gradient_bytes + p.rest_bytes + p.d_part_bytes + p.w_part_bytes;
     } else {
         p.part_bytes = p.piece / LOSS_PART * p.padded_rows * 8;
         p.running_bytes = p.padded_rows * 8;
@@ -172,6 +173,7 @@ LossArgs loss_args(const plaid_token_loss &a, const LossPlan &p, void *workspace
         if (backward) {
             x.scaled = w, w += p.scaled_bytes;
             x.gradient = w, w += p.gradient_bytes;
+            x.rest = (float *)w, w += p.rest_bytes;
             x.d_part = (float *)w, w += p.d_part_bytes;
             x.w_part = p.w_part_bytes ? (float *)w : nullptr;
         }

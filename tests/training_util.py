@@ -114,8 +114,8 @@ def norm(x, weight, bias, eps, d_out=None):
 def cross_entropy(hidden, weight, targets, scale, d_loss=None):
     """A dict of loss, lse and, with d_loss, d_hidden and d_weight, and of their bounds.
 
-    A score is a sum of `width` products in 32 bits; a probability is off by twice a score's error, relative; G rounds to the type once, in
-    fp16 in steps of 2^-24 of 2^15 d_loss's power of two; the states that G is multiplied with carry that power, in fp16 in steps of 2^-24 of
+    A score is a sum of `width` products in 32 bits; a probability is off by twice a score's error, relative; G rounds to the type once, its
+    targets' entries twice as finely, in fp16 in steps of 2^-24 of 2^15 d_loss's power of two; the states that G is multiplied with carry that power, in fp16 in steps of 2^-24 of
     the largest one's.  What is below 2^-126, the least normal number of 32 bits and of bf16, may become zero, as the exponential's instruction
     and the matrix unit make it: a probability, and its product with the fraction of d_loss (in units of the power: 2^-125 for both), and a state."""
     dtype, u, (rows, width), vocabulary, dev = hidden.dtype, half_step(hidden.dtype), hidden.shape, weight.shape[0], hidden.device
@@ -139,6 +139,8 @@ def cross_entropy(hidden, weight, targets, scale, d_loss=None):
     g = p.clone()
     g[at, t] = torch.expm1(-loss)
     g_off = p * (2 * off + sum_off + 4 * E * (1 + s.abs())) + u * g.abs() * (1 + 2 ** -6)
+    # what the target's entry loses in rounding is multiplied too, itself rounded: u of u
+    g_off[at, t] = p[at, t] * (2 * off + sum_off + 4 * E * (1 + s.abs()))[at, t] + u * u * g[at, t].abs() * (1 + 2 ** -6)
     power = torch.exp2(torch.where(c == 0, -math.inf, torch.floor(torch.log2(c.abs())) + 1))
     top = power.amax() if len(live) else torch.tensor(0.0, dtype=torch.float64, device=dev)
     if not top > 0:
