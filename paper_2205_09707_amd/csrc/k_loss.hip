@@ -217,11 +217,11 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
             load_to_lds(p, (i < W_LOADS ? lds_w[stage] : lds_h[stage]) + to[i]);
         }
     };
-    f32x4 acc[BLOCKS][GROUPS];
+    f32x4 acc[BLOCKS][GROUPS], odd[BLOCKS][GROUPS];  // two sums, of every other 32 columns: each has half as many roundings, of half the size
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
-        for (int j = 0; j < GROUPS; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+        for (int j = 0; j < GROUPS; ++j) acc[i][j] = odd[i][j] = f32x4{0, 0, 0, 0};
     int place[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) place[k] = l * 128 + (((4 * k + q) ^ swizzle<64>(l)) << 4);  // rows 16 on: 2048 bytes
@@ -245,10 +245,17 @@ __global__ __launch_bounds__(WAVES * 64) void loss_few_kernel(LossArgs a)
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i)
 #pragma unroll
-                for (int j = 0; j < GROUPS; ++j) acc[i][j] = mfma16<DT>(x[i], y[j], acc[i][j]);
+                for (int j = 0; j < GROUPS; ++j) {
+                    f32x4 &sum = k ? odd[i][j] : acc[i][j];
+                    sum = mfma16<DT>(x[i], y[j], sum);
+                }
         }
         stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+        for (int j = 0; j < GROUPS; ++j) acc[i][j] += odd[i][j];
     // a lane's results: row 16 j + l, entries 16 i + 4 q .. + 3 from the wave's first
     const int64_t mine = v0 + wave * (16 * BLOCKS) + 4 * q;
     if constexpr (GRADIENT) {
@@ -424,17 +431,17 @@ __device__ __forceinline__ void join_gradients(const LossArgs &a, int id)
     const int i = (wave & 1) * 2 + k / 4, c = k % 4, column = tile % widths * LOSS_TILE + wave * 64 + k * 8 + 4 * (lane >> 5);
     const float *p = (WEIGHT ? a.w_part : a.d_part) + (int64_t)tile * (LOSS_TILE * LOSS_TILE) + ((wave >> 1) * 4 + block / 2) * 8192 + (((block & 1) * 4 + i) * 4 + c) * 256 + lane * 4;
     f32x4 v = {0, 0, 0, 0};
+    i32x2 w = {0, 0};  // the target's, and what its entry of G left out
+    float rest = 0.0f;
+    if (!WEIGHT && there && column < a.width) w = *(const i32x2 *)(a.weight + a.row[row].target * a.weight_stride + column * 2), rest = a.rest[row];
 #pragma unroll 4
     for (int s = 0; s < splits; ++s) v += *(const f32x4 *)(p + s * part);
-    if (!WEIGHT && there && column < a.width) {
-        const float rest = a.rest[row];
-        const char *w = a.weight + a.row[row].target * a.weight_stride + column * 2;
+    if (!WEIGHT)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float more = rest * load16<DT>(w + 2 * j);
+            const float more = rest * unpack<DT>(w[j / 2], j & 1);
             if (fabsf(more) < INFINITY) v[j] += more;
         }
-    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = ldexpf(v[j] * factor, e == NO_EXPONENT ? 0 : e);
     char *out = WEIGHT ? a.d_weight : a.d_hidden;

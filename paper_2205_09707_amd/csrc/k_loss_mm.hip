@@ -11,7 +11,7 @@
 // have 128 x 64 of a tile each.  The axis that is to lie together in memory is the one of the result's registers (M): four neighbours a lane.
 //
 // Measured, 7296 rows of 2048, 5107 of them with a target, on 128000 entries in bf16 (2.7 TFLOP a product): statistics of the scores 2160 us = 1.24 PFLOP/s,
-// G 2260 = 1.18, both gradients 4370 = 1.23 (another card: 2220, 2350 and 4520).  A step of 64 takes 1.6 us (1.34 PFLOP/s), a tile's first loads and its way out 5 (statistics) to 7 (G).
+// G 2260 = 1.18, both gradients 4370 = 1.23 (4540 with what G left out; another card: 2220, 2350).  A step of 64 takes 1.6 us (1.34 PFLOP/s), a tile's first loads and its way out 5 (statistics) to 7 (G).
 // The matrix units are busy for 63 % of the time at 1.73 GHz, and for 52 % at 1.9 GHz before the reads of operands lay among the products: what is
 // left is power and the loads (statistics without loads 1855 in place of 2276, without reads of LDS 2064, without waiting for loads 2243).
 // Kept out: lines of later steps touched in advance (2515), a wave's priority raised for its products (no change), four waves with 128 x 128 each, which
@@ -200,6 +200,19 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
         else if constexpr (KIND == KIND_D_HIDDEN) B.step(((begin + s) & 3) == 3 ? G_TILE - 6 * BK : 2 * BK);
         else B.step(((begin + s) & 3) == 3 ? pieces * G_TILE - 3 * TILE_BYTES : TILE_BYTES);
     };
+    // d_weight: which of a wave's next 1024 rows have a target in the tile; a lane's rows are 64 apart, a bit each
+    const int end = min(live, (begin + steps) * BK), first_entry = (int)a.first + t.n * LOSS_TILE;
+    const auto look = [&](int r0) {
+        int bits = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = r0 + wave * 1024 + i * 64 + lane;
+            bits |= (int)(row < end && (unsigned)(a.row[min(row, end - 1)].target - first_entry) < LOSS_TILE) << i;
+        }
+        return bits;
+    };
+    int bits = 0;
+    if (KIND == KIND_D_WEIGHT && begin * BK + wave * 1024 < end) bits = look(begin * BK);
     i32x4 p[2][4], q[2][2];
     const auto read = [&](int s, int place, int k) {
         const char *x = SCORES ? lds.far[place] : lds.near[s & 1], *y = SCORES ? lds.near[s & 1] : lds.far[place];
@@ -279,21 +292,19 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
 
     if constexpr (KIND == KIND_D_WEIGHT) {
         // What the targets' entries left out: the rows whose target is one of the tile's are multiplied again, 64 of them at a time, with a tile that has a
-        // single entry in each.  They are looked for among all of the axis, up to 8192 at a time, in order.  (7296 rows, 5107 with a target, of 2048 on
-        // 128000 entries: FIGURE.)
-        const int end = min(live, (begin + steps) * BK), first_entry = (int)a.first + t.n * LOSS_TILE;
+        // single entry in each.  They are looked for among all of the axis, up to 8192 at a time, in order.
+        // (Both gradients of 7296 rows of 2048, 5107 with a target, on 128000 entries 4540 us in place of 4370, of 509 rows of 768 on 32128 75 in place
+        // of 70; the errors of both, bf16 0.0024 and fp16 0.0003 of the gradients' norm, are 0.0017 and 0.00021, as of one rounding.)
         int *const list = (int *)lds.far[2], *const counts = (int *)lds.far[1];
         for (int r0 = begin * BK; r0 < end; r0 += TILE_BYTES / 4) {
-            const int mine0 = r0 + wave * 1024 + lane;  // the lane's rows are 64 apart, a bit each
-            int bits = 0, mine = 0;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                bits |= (int)(mine0 + i * 64 < end && (unsigned)(a.row[min(mine0 + i * 64, end - 1)].target - first_entry) < LOSS_TILE) << i;
+            if (r0 > begin * BK) bits = look(r0);
+            const int mine0 = r0 + wave * 1024 + lane;
+            int mine = 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) mine += __popcll(__ballot(bits >> i & 1));
-            __syncthreads();  // the tiles have been read
+            lds_barrier();  // the tiles have been read
             if (lane == 0) counts[wave] = mine;
-            __syncthreads();
+            lds_barrier();
             int at = 0, all = 0;
 #pragma unroll
             for (int w = 0; w < 8; ++w) {
@@ -306,25 +317,31 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
                 at += __popcll(votes);
             }
             for (int b = 0; b < all; b += BK) {
-                __syncthreads();  // the list is there; the tiles have been read
+                lds_barrier();  // the list is there; the tiles have been read
+                const int here = min(all - b, BK), quarters = (here + 15) / 16;
+                const int single = (int)threadIdx.x < here ? list[b + threadIdx.x] : -1;
+                const int entry = single < 0 ? 0 : a.row[single].target - first_entry;
+                const float rest = single < 0 ? 0.0f : a.rest[single];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                    if (((wave * 4 + i) & 15) >= quarters * 4) continue;
                     const int load = wave * 4 + i, k = (load & 15) * 4 + (lane >> 4), column = (load >> 4) * 128 + (((lane & 15) ^ swizzle<128>(k)) * 8);
-                    const int row = b + k < all ? list[b + k] : -1;
+                    const int row = k < here ? list[b + k] : -1;
                     const char *p = a.scaled + ((int64_t)(row / BK) * widths + t.m) * TILE_BYTES + row % BK * (2 * LOSS_TILE) + column * 2;
                     load_to_lds(row < 0 ? (const char *)zero_row : p, near_mine + i * 1024);
-                    *(i32x4 *)(lds.far[0] + (i * 512 + threadIdx.x) * 16) = i32x4{0, 0, 0, 0};
                 }
-                __syncthreads();
-                const int k = threadIdx.x;
-                if (k < BK && b + k < all) {
-                    const int row = list[b + k], v = a.row[row].target - first_entry;
-                    store16<DT>(lds.far[0] + (v >> 7) * (TILE_BYTES / 2) + k * 256 + ((((v & 127) >> 3) ^ swizzle<128>(k)) << 4) + (v & 7) * 2, a.rest[row]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *(i32x4 *)(lds.far[0] + (i * 512 + threadIdx.x) * 16) = i32x4{0, 0, 0, 0};
+                lds_barrier();
+                if (single >= 0) {
+                    const int k = threadIdx.x;
+                    store16<DT>(lds.far[0] + (entry >> 7) * (TILE_BYTES / 2) + k * 256 + ((((entry & 127) >> 3) ^ swizzle<128>(k)) << 4) + (entry & 7) * 2, rest);
                 }
                 wait_loads<0>();
                 lds_barrier();
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
+                    if (s >= quarters) break;
                     read(0, 0, s);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) multiply(s, i >> 1, i & 1);

@@ -327,3 +327,30 @@ def test_gradients_of_gradients_are_refused(pl):
         with torch.no_grad():
             pl.plaid_cross_entropy_backward(d, h, w, t, lse)
         x.requires_grad_(False)
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("rows,vocabulary,width,targets", [
+    (20_000, 300, 64, [5]),  # all rows have one target: as many as are looked at together, and more
+    (20_000, 300, 64, [299, 0, 255, 256]),
+    (9000, 5000, 264, [4999, 17]),
+    (70, 5000, 264, [4999, 17]),
+    (64, 20, 8, [3]),
+    (65, 20, 8, [3]),
+    (1, 2000, 512, [1999]),
+])
+def test_the_targets_entries_lose_nothing(pl, rows, vocabulary, width, targets, dtype):
+    """The bounds allow a target's entry of G the square of a rounding."""
+    h, w, _, d = _inputs(rows, vocabulary, width, dtype, seed=rows + width)
+    t = torch.tensor(targets, device=DEV)[torch.arange(rows, device=DEV) * 7 // 3 % len(targets)]
+    _check(pl, h, w, t, d, width ** -0.5)
+
+
+def test_a_target_whose_entry_is_infinite(pl):
+    """Its score is minus infinity: it has no probability left, a loss that is infinite, and one column of a gradient that is no number."""
+    h, w, t = torch.ones(1, 16, device=DEV, dtype=BF), torch.zeros(70, 16, device=DEV, dtype=BF), torch.tensor([3], device=DEV)
+    w[3, 0] = -INF
+    loss, lse = pl.plaid_cross_entropy(h, w, t, return_lse=True)
+    assert loss.tolist() == [INF]
+    dh, dw = pl.plaid_cross_entropy_backward(torch.full((1,), 0.3, device=DEV), h, w, t, lse)
+    assert not torch.isfinite(dh[0, 0]) and torch.isfinite(dh[0, 1:]).all() and torch.isfinite(dw).all()

@@ -18,7 +18,7 @@ KERNELS = {
     "loss_gradients_kernelILi0E": ("k_loss_mm", 256, 160 << 10),
     "loss_few_kernelILi0ELi4ELi1ELi1ELb0E": ("k_loss", 64, 32 << 10),   # five workgroups per CU
     "loss_few_kernelILi0ELi4ELi1ELi3ELb0E": ("k_loss", 64, 53 << 10),   # three
-    "loss_few_kernelILi0ELi4ELi1ELi8ELb0E": ("k_loss", 128, 80 << 10),  # two
+    "loss_few_kernelILi0ELi4ELi1ELi8ELb0E": ("k_loss", 256, 80 << 10),  # two, a wave of each per SIMD
     "loss_few_kernelILi0ELi8ELi2ELi8ELb0E": ("k_loss", 256, 160 << 10),
     "norm_kernelILi0ELi64ELi4E": ("k_norm", 128, 1 << 10),
     "norm_grad_kernelILi0ELi256ELi1E": ("k_norm", 102, 1 << 10),        # five waves per SIMD
