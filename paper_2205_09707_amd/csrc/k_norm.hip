@@ -6,7 +6,7 @@
 // A row's threads keep it in registers, so that the variance is that of x - m (no difference of large numbers) and the row is read once.
 // LANES threads have a row, each up to C pieces of eight neighbouring elements, LANES * 8 elements apart.  Rows may start at any element.
 //
-// Memory bounds them: 100000 rows of 2048 in bf16 take 157 us forward (819 MB, 5.2 TB/s) and 241 backward (1.23 GB, 5.1 TB/s), and 8 to add up the
+// Memory bounds them: 100000 rows of 2048 in bf16 take 157 us forward (819 MB, 5.2 TB/s) and 241 backward (1.23 GB, 5.1 TB/s), and 6 to add up the
 // workers' sums.  4001 rows of 765 out of rows of 784, in the caches, 8, 12 and 5 us: a chain of loads, sums across lanes and stores.
 // How many threads have a row: as few as hold it in registers, so that no barrier is needed and narrow rows leave no lanes idle (200000 x 64,
 // forward and backward: 38 us with eight lanes, 147 with 64).  Forward, us with a wave and with 256 threads: 100000 x 2048 146 and 171, 100000 x 1500
@@ -153,26 +153,29 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_grad_kernel(No
         }
 }
 
-// A workgroup has 64 columns of dw or of db; its sixteen waves take the workers in turn.
+// A workgroup has NORM_JOIN columns of dw or of db; its shares take the workers in turn.  (us with 64, 32 and 16 columns: 1024 workers of 2048 columns 7.4,
+// 5.5, 8.4; 501 of 765 5.5, 4.8, 5.4; 750 of 4096 4.4, 4.6, 6.7; 1024 of 64 5.1, 3.9, 3.8.)
+#define NORM_JOIN 32
 template <int DT>
 __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a)
 {
-    __shared__ float lds[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, column = blockIdx.x * 64 + lane, k = blockIdx.y;
+    constexpr int SHARES = 1024 / NORM_JOIN;
+    __shared__ float lds[SHARES][NORM_JOIN];
+    const int mine = threadIdx.x % NORM_JOIN, share = threadIdx.x / NORM_JOIN, column = blockIdx.x * NORM_JOIN + mine, k = blockIdx.y;
     char *out = k ? a.dbias : a.dweight;
     if (!out) return;
     float sum = 0.0f;
     if (column < a.width) {
         const float *p = a.part + k * a.width + column;
 #pragma unroll 8
-        for (int i = wave; i < a.workers; i += 16) sum += p[(int64_t)i * 2 * a.width];
+        for (int i = share; i < a.workers; i += SHARES) sum += p[(int64_t)i * 2 * a.width];
     }
-    lds[wave][lane] = sum;
+    lds[share][mine] = sum;
     __syncthreads();
-    if (wave == 0 && column < a.width) {
+    if (share == 0 && column < a.width) {
         sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum += lds[i][lane];
+        for (int i = 0; i < SHARES; ++i) sum += lds[i][mine];
         store16<DT>(out + 2 * column, sum);
     }
 }
@@ -215,7 +218,7 @@ static void launch_norm_backward(hipStream_t st, const NormArgs &a)
     else if (pieces <= 1024) GO(256, 4);
     else GO(1024, 2);
 #undef GO
-    if (a.part) norm_join_kernel<DT><<<dim3((a.width + 63) / 64, 2), 1024, 0, st>>>(a);
+    if (a.part) norm_join_kernel<DT><<<dim3((a.width + NORM_JOIN - 1) / NORM_JOIN, 2), 1024, 0, st>>>(a);
 }
 void plaid_launch_layer_norm(hipStream_t st, const NormArgs &a, int dtype) { dtype == PLAID_BF16 ? launch_norm<PLAID_BF16>(st, a) : launch_norm<PLAID_FP16>(st, a); }
 void plaid_launch_layer_norm_backward(hipStream_t st, const NormArgs &a, int dtype)
