@@ -93,7 +93,10 @@ __global__ __launch_bounds__(128) void loss_prepare_kernel(LossArgs a)
     const bool mine = t < rows && has_target(a, t, target);
     if (mine) {
         const LossRow r = loss_row(a, t, target, BACKWARD);
-        if (threadIdx.x == 0) a.list[before] = t, a.row[before] = r;
+        if (threadIdx.x == 0) {
+            a.list[before] = t, a.row[before] = r;
+            if (BACKWARD) a.target[before] = target;
+        }
         pack_row<DT, BACKWARD>(a, before, t, r.exponent == NO_EXPONENT ? 0 : r.exponent - top);
         return;
     }
@@ -127,6 +130,7 @@ __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a, int backwar
             top = max(top, backward ? r.exponent : 0);
             a.list[at] = (int)t;
             a.row[at] = r;
+            if (backward) a.target[at] = target;
         }
         __syncthreads();
     }

@@ -11,7 +11,8 @@
 // have 128 x 64 of a tile each.  The axis that is to lie together in memory is the one of the result's registers (M): four neighbours a lane.
 //
 // Measured, 7296 rows of 2048, 5107 of them with a target, on 128000 entries in bf16 (2.7 TFLOP a product): statistics of the scores 2160 us = 1.24 PFLOP/s,
-// G 2260 = 1.18, both gradients 4370 = 1.23 (4540 with what G left out; another card: 2220, 2350).  A step of 64 takes 1.6 us (1.34 PFLOP/s), a tile's first loads and its way out 5 (statistics) to 7 (G).
+// G 2260 = 1.18, both gradients 4370 = 1.23; on other cards 2200 to 2250, 2330 to 2370, 4480; with what G left out 4560.  A step
+// of 64 takes 1.6 us (1.34 PFLOP/s), a tile's first loads and its way out 5 (statistics) to 7 (G).
 // The matrix units are busy for 63 % of the time at 1.73 GHz, and for 52 % at 1.9 GHz before the reads of operands lay among the products: what is
 // left is power and the loads (statistics without loads 1855 in place of 2276, without reads of LDS 2064, without waiting for loads 2243).
 // Kept out: lines of later steps touched in advance (2515), a wave's priority raised for its products (no change), four waves with 128 x 128 each, which
@@ -202,17 +203,19 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
     };
     // d_weight: which of a wave's next 1024 rows have a target in the tile; a lane's rows are 64 apart, a bit each
     const int end = min(live, (begin + steps) * BK), first_entry = (int)a.first + t.n * LOSS_TILE;
+    int looked[16];
     const auto look = [&](int r0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) looked[i] = a.target[min(r0 + wave * 1024 + i * 64 + lane, end - 1)];
+    };
+    const auto found = [&](int r0) {
         int bits = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int row = r0 + wave * 1024 + i * 64 + lane;
-            bits |= (int)(row < end && (unsigned)(a.row[min(row, end - 1)].target - first_entry) < LOSS_TILE) << i;
-        }
+        for (int i = 0; i < 16; ++i) bits |= (int)(r0 + wave * 1024 + i * 64 + lane < end && (unsigned)(looked[i] - first_entry) < LOSS_TILE) << i;
         return bits;
     };
     int bits = 0;
-    if (KIND == KIND_D_WEIGHT && begin * BK + wave * 1024 < end) bits = look(begin * BK);
+    if (KIND == KIND_D_WEIGHT && end > 0) look(begin * BK);
     i32x4 p[2][4], q[2][2];
     const auto read = [&](int s, int place, int k) {
         const char *x = SCORES ? lds.far[place] : lds.near[s & 1], *y = SCORES ? lds.near[s & 1] : lds.far[place];
@@ -278,6 +281,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
         first(0, true);
         first(1, true);
         first(2, false);
+        if (KIND == KIND_D_WEIGHT) bits = found(begin * BK);
         if (steps == 1) wait_loads<0>();
         else if (steps == 2) wait_loads<8>();
         else wait_loads<12>();
@@ -293,11 +297,12 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
     if constexpr (KIND == KIND_D_WEIGHT) {
         // What the targets' entries left out: the rows whose target is one of the tile's are multiplied again, 64 of them at a time, with a tile that has a
         // single entry in each.  They are looked for among all of the axis, up to 8192 at a time, in order.
-        // (Both gradients of 7296 rows of 2048, 5107 with a target, on 128000 entries 4540 us in place of 4370, of 509 rows of 768 on 32128 75 in place
-        // of 70; the errors of both, bf16 0.0024 and fp16 0.0003 of the gradients' norm, are 0.0017 and 0.00021, as of one rounding.)
+        // (Both gradients of 7296 rows of 2048, 5107 with a target, on 128000 entries 4560 us in place of 4480, of 509 rows of 768 on 32128 76 in place
+        // of 70; looked for after the other products, and in LossRow: 4710 and 77.  The errors of both, bf16 0.0024 and fp16 0.0003 of the
+        // gradients' norm, are 0.0017 and 0.00021, as of one rounding.)
         int *const list = (int *)lds.far[2], *const counts = (int *)lds.far[1];
         for (int r0 = begin * BK; r0 < end; r0 += TILE_BYTES / 4) {
-            if (r0 > begin * BK) bits = look(r0);
+            if (r0 > begin * BK) look(r0), bits = found(r0);
             const int mine0 = r0 + wave * 1024 + lane;
             int mine = 0;
 #pragma unroll
@@ -320,7 +325,7 @@ __device__ __forceinline__ void product(const LossArgs &a, TileLds &lds, int id)
                 lds_barrier();  // the list is there; the tiles have been read
                 const int here = min(all - b, BK), quarters = (here + 15) / 16;
                 const int single = (int)threadIdx.x < here ? list[b + threadIdx.x] : -1;
-                const int entry = single < 0 ? 0 : a.row[single].target - first_entry;
+                const int entry = single < 0 ? 0 : a.target[single] - first_entry;
                 const float rest = single < 0 ? 0.0f : a.rest[single];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {

@@ -71,6 +71,7 @@ struct LossArgs {
     float *d_part;                     // [parts][tiles of rows that have a target][columns / 256][256 x 256] sums of d_hidden, in the
                                        // order of the products' registers
     float *w_part;                     // [parts][piece / 256][columns / 256][256 x 256] the same of d_weight, null where its axis is never cut
+    int32_t *target;                   // [padded_rows] LossRow::target alone
     float *rest;                       // [padded_rows] what the rounding of the target's entry of `gradient` left out
     int32_t columns;                   // width rounded up to LOSS_TILE
     int32_t hidden_steps;              // steps of a whole piece along d_hidden's axis

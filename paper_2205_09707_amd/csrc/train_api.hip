@@ -117,7 +117,7 @@ LossPlan plan_loss(const plaid_token_loss &a, bool backward)
     if (backward) {
         p.gradient_bytes = p.padded_rows * p.piece * 2;
         p.scaled_bytes = p.padded_rows * p.columns * 2;
-        p.rest_bytes = p.padded_rows * 4;
+        p.rest_bytes = p.padded_rows * 8;
         p.d_part_bytes = loss_hidden_parts(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
         p.w_part_bytes = loss_weight_parts(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
         p.bytes = p.list_bytes + p.row_bytes + p.packed_bytes + p.scaled_bytes + p.gradient_bytes + p.rest_bytes + p.d_part_bytes + p.w_part_bytes;
@@ -173,7 +173,7 @@ LossArgs loss_args(const plaid_token_loss &a, const LossPlan &p, void *workspace
         if (backward) {
             x.scaled = w, w += p.scaled_bytes;
             x.gradient = w, w += p.gradient_bytes;
-            x.rest = (float *)w, w += p.rest_bytes;
+            x.target = (int32_t *)w, x.rest = (float *)w + p.padded_rows, w += p.rest_bytes;
             x.d_part = (float *)w, w += p.d_part_bytes;
             x.w_part = p.w_part_bytes ? (float *)w : nullptr;
         }
