@@ -147,7 +147,9 @@ __device__ __forceinline__ float score_factor(const LossArgs &a) { return fabsf(
 __device__ __forceinline__ float exponent_factor(const LossArgs &a) { return fmaxf(fabsf(a.scale), 1e-30f) * LOG2E; }
 
 // G of a row, in units of its d_loss's power of two, times 2^15 in fp16: of a product, by the score it is.  The target's is the probability less
-// one, formed so that it keeps its digits where the probability is almost one.
+// one, formed so that it keeps its digits where the probability is almost one: its score is then `top`, rounded as the forward pass rounded it, so that
+// the difference is exactly nothing and what is left is the logarithm beside it.  (Fused into the subtraction the product would keep what `top` lost, 2^-24 of
+// the score, which is more than all the others' probabilities.)
 struct ScoreGradient {
     float scale, k, top, log_total, shift, factor;
     __device__ __forceinline__ ScoreGradient(const LossRow &x, const LossArgs &a, int dtype)
@@ -157,7 +159,12 @@ struct ScoreGradient {
     }
     // (the shift's rounding, 2^-24 of a score, costs a probability less than its own rounding to the type while scores stay below 2^12)
     __device__ __forceinline__ float other(float product) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(product, k, -shift)) * factor; }
-    __device__ __forceinline__ float target(float product) const { return expm1f(product * scale - top - log_total) * factor; }
+    __device__ __forceinline__ float target(float product) const
+    {
+#pragma clang fp contract(off)
+        const float score = product * scale;
+        return expm1f((score - top) - log_total) * factor;
+    }
 };
 // The target's entry of G rounds like the others, but a row has nothing larger, so that its rounding alone would be as much of a gradient's error as the
 // result's own: what it left out is kept in 32 bits, and both gradients add its product.  (Where it is no number, they need no digits.)
