@@ -12,8 +12,11 @@
 // --- rows that have a target ----------------------------------------------------------------------------------------------------
 // They are numbered in the caller's order, and their states packed in the order in which the products' tiles take them, with zeros up to a whole
 // tile of rows and a whole step of columns; a row without a target has a loss of zero and no gradient.  Backward, d_loss = fraction 2^exponent:
-// the fraction goes into G, which rounds to the type before it is multiplied, the power of two into what G is multiplied with, where it is
-// exact, so that G in fp16 stays in its range however small the gradient of a mean is.
+// the fraction goes into G, which rounds to the type before it is multiplied, the power of two into what G is multiplied with, so that G in fp16
+// stays in its range however small the gradient of a mean is.  d_hidden takes it from the sums, in 32 bits, d_weight, whose sums go over the rows, in the
+// states, relative to state[1].  In bf16 that is the largest exponent.  fp16 would lose the digits of rows with a small d_loss below its normal range while the range
+// above is empty, so there the largest state of all rows, with its row's power, takes the type's last binade: the states of a row 2^-r of that one are exact down to
+// 2^(r - 29) of the row's own largest, and what rounds there rounds by 2^-40 of the largest of all.  (Finding it is a launch of its own, 2 to 3 us.)
 __device__ __forceinline__ bool has_target(const LossArgs &a, int64_t t, int &target)
 {
     const int64_t v = a.targets[t];
@@ -31,6 +34,36 @@ __device__ __forceinline__ LossRow loss_row(const LossArgs &a, int64_t t, int ta
         r.top = a.lse[2 * t], r.log_total = a.lse[2 * t + 1];
     }
     return r;
+}
+// A row's exponent beside state[1]; above 40 only where all states are zero or not finite.
+__device__ __forceinline__ int state_shift(int exponent, int top) { return exponent == NO_EXPONENT ? 0 : min(exponent - top, 40); }
+
+// fp16: what state[1] has to be for a row's largest finite state to take the last binade, a wave a row.
+__global__ __launch_bounds__(256) void loss_reach_kernel(LossArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    int target = 0, reach = NO_EXPONENT;
+    if (t >= a.rows) return;
+    if (has_target(a, t, target)) {
+        const char *row = a.hidden + t * a.hidden_stride;
+        int most = 0;  // bits of a magnitude; they ascend as it does
+        for (int at = lane * 8; at < a.width; at += 512) {
+            const i32x4 w = *(const i32x4 *)(row + 2 * at);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int bits = (w[i / 2] >> (16 * (i & 1))) & 0x7fff;
+                most = max(most, bits < 0x7c00 ? bits : 0);
+            }
+        }
+#pragma unroll
+        for (int o = 32; o; o >>= 1) most = max(most, __shfl_xor(most, o));
+        const int exponent = loss_row(a, t, target, true).exponent;
+        int e;
+        (void)frexpf(unpack<PLAID_FP16>(most, 0), &e);
+        if (most > 0 && exponent != NO_EXPONENT) reach = exponent + e - 16;
+    }
+    if (lane == 0) a.reach[t] = reach;
 }
 // 128 threads; t < 0: zeros.
 template <int DT, bool BACKWARD>
@@ -79,7 +112,7 @@ __global__ __launch_bounds__(128) void loss_prepare_kernel(LossArgs a)
         int target = 0;
         const bool mine = i < rows && has_target(a, i, target);
         live += __popcll(__ballot(mine)), before += __popcll(__ballot(mine && i < t));
-        if (BACKWARD && mine) top = max(top, loss_row(a, i, target, true).exponent);
+        if (BACKWARD && mine) top = max(top, a.reach ? a.reach[i] : loss_row(a, i, target, true).exponent);
     }
     if (BACKWARD)
 #pragma unroll
@@ -97,7 +130,7 @@ __global__ __launch_bounds__(128) void loss_prepare_kernel(LossArgs a)
             a.list[before] = t, a.row[before] = r;
             if (BACKWARD) a.target[before] = target;
         }
-        pack_row<DT, BACKWARD>(a, before, t, r.exponent == NO_EXPONENT ? 0 : r.exponent - top);
+        pack_row<DT, BACKWARD>(a, before, t, state_shift(r.exponent, top));
         return;
     }
     // the others, and those past the end, are as many as there are places up to the last tile's end
@@ -127,7 +160,7 @@ __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a, int backwar
         before += all;
         if (live) {
             const LossRow r = loss_row(a, t, target, backward);
-            top = max(top, backward ? r.exponent : 0);
+            if (backward) top = max(top, a.reach ? a.reach[t] : r.exponent);
             a.list[at] = (int)t;
             a.row[at] = r;
             if (backward) a.target[at] = target;
@@ -152,12 +185,13 @@ __global__ __launch_bounds__(128) void loss_pack_kernel(LossArgs a)
     if (i < a.rows && !has_target(a, i, target)) no_target<BACKWARD>(a, i);
     if (i >= (live + LOSS_TILE - 1) / LOSS_TILE * LOSS_TILE) return;
     const int e = BACKWARD && i < live ? uniform_load(&a.row[i].exponent) : NO_EXPONENT;
-    pack_row<DT, BACKWARD>(a, i, i < live ? uniform_load(a.list + i) : -1, e == NO_EXPONENT ? 0 : e - top);
+    pack_row<DT, BACKWARD>(a, i, i < live ? uniform_load(a.list + i) : -1, state_shift(e, top));
 }
 
 void plaid_launch_loss_pack(hipStream_t st, const LossArgs &a, int dtype, bool backward)
 {
     const unsigned grid = (unsigned)a.padded_rows;
+    if (a.reach && a.rows > 0) loss_reach_kernel<<<(unsigned)((a.rows + 3) / 4), 256, 0, st>>>(a);
     if (a.rows <= LOSS_PREPARE_ONE) {
         if (!backward) loss_prepare_kernel<PLAID_BF16, false><<<grid, 128, 0, st>>>(a);
         else if (dtype == PLAID_BF16) loss_prepare_kernel<PLAID_BF16, true><<<grid, 128, 0, st>>>(a);

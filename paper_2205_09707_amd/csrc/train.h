@@ -58,11 +58,12 @@ struct LossArgs {
     float scale;
     // workspace
     int32_t padded_rows, pitch;        // rows rounded up to LOSS_TILE, width to LOSS_STEP
-    int32_t *state;                    // [0] rows that have a target, [1] the largest exponent among them
+    int32_t *state;                    // [0] rows that have a target, [1] the exponent that `scaled` is relative to
+    int32_t *reach;                    // [rows] what each of them wants there, null where that is its exponent (bf16) or nothing is scaled
     int32_t *list;                     // [rows] which these are
     LossRow *row;                      // [padded_rows]
     char *packed;                      // [rows / 256][pitch / 64][256][64] states, with the sign of the scale
-    char *scaled;                      // [rows / 64][columns / 256][64][256] the same times 2^(exponent - largest)
+    char *scaled;                      // [rows / 64][columns / 256][64][256] the same times 2^(exponent - state[1])
     float2 *part;                      // [parts][padded_rows] largest product and sum of exponentials beside it over parts of the
                                        // vocabulary, without the target
     float2 *running;                   // [padded_rows] over all parts before

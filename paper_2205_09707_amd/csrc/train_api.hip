@@ -81,7 +81,7 @@ struct LossPlan {
     bool few;
     int entries;
     int64_t padded_rows, pitch, columns, piece;
-    int64_t list_bytes, row_bytes, packed_bytes, scaled_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, rest_bytes, d_part_bytes, w_part_bytes, bytes;
+    int64_t list_bytes, row_bytes, packed_bytes, scaled_bytes, part_bytes, running_bytes, own_bytes, gradient_bytes, rest_bytes, reach_bytes, d_part_bytes, w_part_bytes, bytes;
 };
 LossPlan plan_loss(const plaid_token_loss &a, bool backward)
 {
@@ -118,9 +118,10 @@ LossPlan plan_loss(const plaid_token_loss &a, bool backward)
         p.gradient_bytes = p.padded_rows * p.piece * 2;
         p.scaled_bytes = p.padded_rows * p.columns * 2;
         p.rest_bytes = p.padded_rows * 8;
+        p.reach_bytes = a.dtype == PLAID_FP16 ? p.padded_rows * 4 : 0;
         p.d_part_bytes = loss_hidden_parts(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
         p.w_part_bytes = loss_weight_parts(p.padded_rows, p.columns, ceil_div(p.piece, LOSS_STEP)) * (LOSS_TILE * LOSS_TILE * 4);
-        p.bytes = p.list_bytes + p.row_bytes + p.packed_bytes + p.scaled_bytes + p.gradient_bytes + p.rest_bytes + p.d_part_bytes + p.w_part_bytes;
+        p.bytes = p.list_bytes + p.row_bytes + p.packed_bytes + p.scaled_bytes + p.gradient_bytes + p.rest_bytes + p.reach_bytes + p.d_part_bytes + p.w_part_bytes;
     } else {
         p.part_bytes = p.piece / LOSS_PART * p.padded_rows * 8;
         p.running_bytes = p.padded_rows * 8;
@@ -174,6 +175,7 @@ LossArgs loss_args(const plaid_token_loss &a, const LossPlan &p, void *workspace
             x.scaled = w, w += p.scaled_bytes;
             x.gradient = w, w += p.gradient_bytes;
             x.target = (int32_t *)w, x.rest = (float *)w + p.padded_rows, w += p.rest_bytes;
+            x.reach = p.reach_bytes ? (int32_t *)w : nullptr, w += p.reach_bytes;
             x.d_part = (float *)w, w += p.d_part_bytes;
             x.w_part = p.w_part_bytes ? (float *)w : nullptr;
         }
@@ -360,6 +362,7 @@ extern "C" int plaid_cross_entropy_backward(const plaid_token_loss *args, const 
     LossArgs x = loss_args(*args, p, workspace, true);
     x.d_loss = d_loss, x.d_loss_stride = 4 * d_loss_stride;
     x.d_hidden = args->rows > 0 ? (char *)d_hidden : nullptr, x.d_weight = (char *)d_weight;
+    if (!d_weight) x.reach = nullptr;
     plaid_launch_loss_pack(st, x, args->dtype, true);
     for (x.first = 0; x.first < x.vocabulary; x.first += p.piece) {
         x.piece = (int32_t)(x.vocabulary - x.first < p.piece ? x.vocabulary - x.first : p.piece);

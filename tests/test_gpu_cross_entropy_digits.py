@@ -1,10 +1,10 @@
 """Cross entropy's gradients where the digits are at stake: targets whose probability is almost one, by scales that are no power of two and scores that are
-not exact."""
+not exact; in fp16, rows whose gradients of the loss are far apart."""
 import pytest
 import torch
 
 from loss_bounds import relative
-from training_util import close
+from training_util import close, half_step
 
 pytestmark = pytest.mark.gpu
 DEV, BF, HALF = torch.device("cuda", 0), torch.bfloat16, torch.float16
@@ -45,3 +45,73 @@ def test_targets_near_one(pl, rows, vocabulary, width, scale, dtype):
     score = 18 + 14 * torch.rand(rows, 1, generator=g, device=DEV)
     h = (score / (scale * width) * w[t].float()).to(dtype)
     _check(pl, h, w, t, torch.full((rows,), 2.0 ** 20, device=DEV), scale)
+
+
+def _pointed(rows, vocabulary, width, dtype, seed):
+    """States that point at another entry than their target, with a score of about 40, so that a target's row of d_weight is its own rows' alone."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    w = torch.randn(vocabulary, width, generator=g, device=DEV).to(dtype)
+    h = 40 * width ** -0.5 * w[:1].float() + torch.randn(rows, width, generator=g, device=DEV)
+    return h.to(dtype), w, torch.arange(rows, device=DEV) % (vocabulary - 1) + 1
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("rows,vocabulary,width", [(29, 900, 264), (300, 3000, 136), (700, 15_000, 136), (2050, 3000, 72)])
+def test_rows_whose_gradients_are_far_apart(pl, rows, vocabulary, width, dtype):
+    """2^-28 between the largest and the smallest: each target's row of d_weight has the digits that its own row's states have."""
+    h, w, t = _pointed(rows, vocabulary, width, dtype, rows)
+    d = torch.exp2(13 - torch.arange(rows, device=DEV) % 29.0) * (1 if rows < 100 else 29 / rows)
+    want, (_, _, dw) = _check(pl, h, w, t, d, width ** -0.5)
+    mine = want["d_weight"][t]
+    normal = mine.abs() > 2.0 ** -14
+    # the result's rounding, the states' (2^-25 of what is 2^-28 + 11 or more: less than another), and r
+    assert ((dw[t].double() - mine).abs() <= 2.5 * half_step(dtype) * mine.abs())[normal].all()
+    assert normal.any(1).sum() > 0.6 * rows
+
+
+@pytest.mark.parametrize("rows,vocabulary,width", [(30, 900, 72), (700, 15_000, 72)])
+def test_a_row_of_zeros_and_rows_without_a_target_scale_nothing(pl, rows, vocabulary, width):
+    """Neither a row whose states are zero nor one that takes no part says by what power of two the others' states are scaled."""
+    h, w, t = _pointed(rows, vocabulary, width, HALF, rows)
+    d = torch.ones(rows, device=DEV)
+    h[3] = 0.0
+    d[3] = 0.0
+    t[5] = -1
+    want = _gradients(pl, h, w, t, d, width ** -0.5)
+    d[3], d[5] = 1e30, 1e30
+    h[5] = 65504.0
+    got = _gradients(pl, h, w, t, d, width ** -0.5)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+    keep = torch.arange(rows, device=DEV) != 3
+    assert torch.equal(got[1][keep], want[1][keep])
+
+
+@pytest.mark.parametrize("rows,vocabulary,width", [(30, 900, 72), (700, 15_000, 72)])
+@pytest.mark.parametrize("size", [2.0 ** -20, 3e4])
+def test_states_at_the_ends_of_fp16(pl, rows, vocabulary, width, size):
+    """Subnormal states, and states next to the largest number of fp16."""
+    h, w, t = _pointed(rows, vocabulary, width, HALF, rows)
+    h = (h.float() / h.float().abs().amax() * size * 2).to(HALF)
+    d = torch.exp2(-(torch.arange(rows, device=DEV) % 5.0))
+    scale = 1e-4 if size > 1 else 1.0
+    _check(pl, h, w, t, d * (2.0 ** 12 if size < 1 else 2.0 ** -4), scale)
+
+
+@pytest.mark.parametrize("rows,vocabulary,width", [(30, 900, 72), (2050, 3000, 72)])
+def test_captured_and_replayed(pl, rows, vocabulary, width):
+    h, w, t = _pointed(rows, vocabulary, width, HALF, 0)
+    scale, d = width ** -0.5, torch.ones(rows, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _gradients(pl, h, w, t, d, scale)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = _gradients(pl, h, w, t, d, scale)
+    for seed in (1, 2, 3):
+        h.copy_(_pointed(rows, vocabulary, width, HALF, seed)[0] * seed)
+        d.copy_(torch.exp2(-(torch.arange(rows, device=DEV) * seed % 20.0)))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, _gradients(pl, h, w, t, d, scale)))
