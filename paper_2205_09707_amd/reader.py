@@ -11,6 +11,7 @@ import struct
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad as _forward
 
 from . import plaid as _p
 
@@ -257,8 +258,17 @@ def _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias):
     return _rows(q), _rows(k), _rows(v), q_offsets, k_offsets, key_bias
 
 
+def _no_tangents(**tensors) -> None:
+    """Called where a level of forward differentiation is open (not in a torch.autograd.Function, which sees no tangents)."""
+    for name, t in tensors.items():
+        if t is not None and _forward.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{name} has a forward-mode tangent, which this call does not carry on")
+
+
 def _no_autograd(**tensors) -> None:
     """The calls are not recorded: where one would be differentiated through, its result would be cut off without a word."""
+    if _forward._current_level >= 0:
+        _no_tangents(**tensors)
     if torch.is_grad_enabled():
         for name, t in tensors.items():
             if t is not None and t.requires_grad:

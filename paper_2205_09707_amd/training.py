@@ -3,7 +3,7 @@ over a vocabulary, with their gradients.
 
 Like `reader.py` this only marshals, and keeps nothing from one call for the next.  Autograd records none of the calls: each gradient
 is a call of its own, and inputs that require a gradient are refused where it is enabled, those of the gradients' calls too (examples/reader.py
-has the Functions).
+has the Functions).  Nor do they carry a forward-mode tangent on: inputs that have one are refused.
 """
 from __future__ import annotations
 
@@ -12,9 +12,10 @@ import struct
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad as _forward
 
 from . import plaid as _p
-from .reader import _DTYPES, _workspace
+from .reader import _DTYPES, _no_tangents, _workspace
 
 
 class plaid_token_loss(ct.Structure):
@@ -115,6 +116,8 @@ def _stream(device: int) -> int:
 def plaid_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
     """scale * table[ids] for a table [vocabulary, width] and ids [n] int64; zeros for an id outside the vocabulary."""
     dev = _states(table, "table")
+    if _forward._current_level >= 0:
+        _no_tangents(table=table)
     if _recording() and table.requires_grad:
         _not_recorded("plaid_embedding_backward", table=table)
     ids = _numbers(ids, "ids", dev)
@@ -132,6 +135,8 @@ def plaid_embedding_backward(d_out: torch.Tensor, ids: torch.Tensor, vocabulary:
     """The gradient [vocabulary, width] of plaid_embedding's table from that of its result, d_out [n, width]: dense, or added in place to
     `add_to`, which it then returns (a contiguous gradient of the same table from another use)."""
     dev = _states(d_out, "d_out")
+    if _forward._current_level >= 0:
+        _no_tangents(d_out=d_out, add_to=add_to)
     if _recording() and (d_out.requires_grad or add_to is not None):
         _not_recorded(None, d_out=d_out, add_to=add_to)
     ids = _numbers(ids, "ids", dev, d_out.shape[0])
@@ -157,6 +162,8 @@ def plaid_dropout(x: torch.Tensor, p: float, rng: torch.Tensor, residual: Option
     on x's device: a seed, and a number that no other call of the program has.  The gradient of x is the same call on the result's
     gradient, without a residual; the residual's is the result's."""
     dev = _states(x, "x", None)
+    if _forward._current_level >= 0:
+        _no_tangents(x=x, residual=residual)
     if _recording() and (x.requires_grad or residual is not None):
         _not_recorded("plaid_dropout", x=x, residual=residual)
     rng = _numbers(rng, "rng", dev, 2)
@@ -176,6 +183,8 @@ def plaid_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bia
     """Layer norm of the rows of x [rows, width], times weight [width], plus bias [width].  With return_statistics also what
     plaid_layer_norm_backward wants, each row's mean and 1 / sqrt(variance + eps), [rows, 2] float32."""
     dev = _states(x, "x")
+    if _forward._current_level >= 0:
+        _no_tangents(x=x, weight=weight, bias=bias)
     if _recording() and (x.requires_grad or weight is not None or bias is not None):
         _not_recorded("plaid_layer_norm_backward", x=x, weight=weight, bias=bias)
     x, stride = _rows(x)
@@ -194,6 +203,8 @@ def plaid_layer_norm_backward(d_out: torch.Tensor, x: torch.Tensor, weight: Opti
     """(dx, dweight, dbias) of plaid_layer_norm from its statistics and the gradient d_out; None for a weight or bias that there is not."""
     dev = _states(x, "x")
     _same(d_out, "d_out", x.dtype, x.shape, dev)
+    if _forward._current_level >= 0:
+        _no_tangents(d_out=d_out, x=x, weight=weight, bias=bias, statistics=statistics)
     if _recording():
         _not_recorded(None, d_out=d_out, x=x, weight=weight, bias=bias)
     rows, width = x.shape
@@ -239,6 +250,8 @@ def plaid_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: tor
     [vocabulary, width], targets [rows] int64 -> [rows] float32, zero for a target outside the vocabulary.  With return_lse also what
     plaid_cross_entropy_backward wants, the logarithm of the softmax's sum as two numbers to be added, [rows, 2] float32."""
     rows, table, targets = _loss_inputs(hidden, weight, targets)
+    if _forward._current_level >= 0:
+        _no_tangents(hidden=hidden, weight=weight)
     if _recording() and (hidden.requires_grad or weight.requires_grad):
         _not_recorded("plaid_cross_entropy_backward", hidden=hidden, weight=weight)
     dev = hidden.get_device()
@@ -260,6 +273,8 @@ def plaid_cross_entropy_backward(d_loss: torch.Tensor, hidden: torch.Tensor, wei
     number is taken as it is)."""
     rows, table, targets = _loss_inputs(hidden, weight, targets)
     dev, n = hidden.get_device(), hidden.shape[0]
+    if _forward._current_level >= 0:
+        _no_tangents(d_loss=d_loss, hidden=hidden, weight=weight, lse=lse)
     if _recording():
         _not_recorded(None, d_loss=d_loss, hidden=hidden, weight=weight)
     if _same(d_loss, "d_loss", torch.float32, (n,), dev).stride(0) not in (0, 1):
