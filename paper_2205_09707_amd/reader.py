@@ -261,7 +261,7 @@ def _cross_inputs(q, k, v, q_offsets, k_offsets, key_bias):
 def _no_tangents(**tensors) -> None:
     """Called where a level of forward differentiation is open (not in a torch.autograd.Function, which sees no tangents)."""
     for name, t in tensors.items():
-        if t is not None and _forward.unpack_dual(t).tangent is not None:
+        if isinstance(t, torch.Tensor) and _forward.unpack_dual(t).tangent is not None:
             raise ValueError(f"{name} has a forward-mode tangent, which this call does not carry on")
 
 

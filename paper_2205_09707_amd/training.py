@@ -57,7 +57,7 @@ def _same(t: torch.Tensor, name: str, dtype: torch.dtype, shape, device: int) ->
 def _not_recorded(backward: Optional[str], **tensors) -> None:
     """Called where autograd is enabled and one of the tensors may require a gradient; backward: the call that forms it, if there is one."""
     for name, t in tensors.items():
-        if t is not None and t.requires_grad:
+        if isinstance(t, torch.Tensor) and t.requires_grad:
             raise ValueError(f"{name} requires a gradient, which this call does not record: call it in torch.no_grad()" +
                              (f", or in a torch.autograd.Function whose backward calls {backward}" if backward else " (gradients of gradients are not formed)"))
 
@@ -206,7 +206,7 @@ def plaid_layer_norm_backward(d_out: torch.Tensor, x: torch.Tensor, weight: Opti
     if _forward._current_level >= 0:
         _no_tangents(d_out=d_out, x=x, weight=weight, bias=bias, statistics=statistics)
     if _recording():
-        _not_recorded(None, d_out=d_out, x=x, weight=weight, bias=bias)
+        _not_recorded(None, d_out=d_out, x=x, weight=weight, bias=bias, statistics=statistics)
     rows, width = x.shape
     weight, w = _parameter(weight, "weight", x, width, dev)
     bias, _ = _parameter(bias, "bias", x, width, dev)
@@ -276,7 +276,7 @@ def plaid_cross_entropy_backward(d_loss: torch.Tensor, hidden: torch.Tensor, wei
     if _forward._current_level >= 0:
         _no_tangents(d_loss=d_loss, hidden=hidden, weight=weight, lse=lse)
     if _recording():
-        _not_recorded(None, d_loss=d_loss, hidden=hidden, weight=weight)
+        _not_recorded(None, d_loss=d_loss, hidden=hidden, weight=weight, lse=lse)
     if _same(d_loss, "d_loss", torch.float32, (n,), dev).stride(0) not in (0, 1):
         d_loss = d_loss.contiguous()
     lse = _same(lse, "lse", torch.float32, (n, 2), dev).contiguous()

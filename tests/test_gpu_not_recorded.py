@@ -1,4 +1,5 @@
-"""What autograd would lose without a word is refused: the calls carry no forward-mode tangents."""
+"""What autograd would lose without a word is refused: the calls carry no forward-mode tangents, and the gradients' calls record nothing of what the
+forward ones gave either."""
 import pytest
 import torch
 from torch.autograd import forward_ad
@@ -53,3 +54,13 @@ def test_forward_mode_tangents_are_refused(pl, name):
                 with torch.set_grad_enabled(grad), pytest.raises(ValueError, match=f"{which} has a forward-mode tangent"):
                     call(dual)
     call(tensors)
+
+
+@pytest.mark.parametrize("name,which", [("layer_norm_backward", "statistics"), ("cross_entropy_backward", "lse")])
+def test_gradients_of_what_the_forward_call_gave_are_refused(pl, name, which):
+    call, tensors = _calls(pl)[name]
+    tensors = dict(tensors, **{which: tensors[which].clone().requires_grad_()})
+    with pytest.raises(ValueError, match=f"{which} requires a gradient"):
+        call(tensors)
+    with torch.no_grad():
+        call(tensors)
