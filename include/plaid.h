@@ -473,7 +473,8 @@ int plaid_cross_entropy(const plaid_token_loss *args, void *workspace, int64_t w
  * args->lse is what the forward call gave, args->loss is not looked at.  d_loss [rows] fp32, d_loss_stride 1, or 0: one number for all rows.
  * G rounds to the type before it is multiplied (what its targets' entries lose by that is multiplied too); the power of two of d_loss is kept
  * apart from it.  For d_weight the states carry that power and round to the type: what is lost of a row's is 2^-126 of the largest d_loss in
- * bf16, 2^-40 of the largest product of a state and its row's d_loss in fp16. */
+ * bf16, 2^-40 of the largest product of a state and its row's d_loss in fp16.  lse keeps a row's largest score in 32 bits: where scores are far from zero,
+ * probabilities are off by 2^-24 of it, relative. */
 int plaid_cross_entropy_backward(const plaid_token_loss *args, const float *d_loss, int64_t d_loss_stride, void *d_hidden, void *d_weight,
                                  void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
 int plaid_cross_entropy_workspace(const plaid_token_loss *args, int32_t backward, int64_t *bytes);

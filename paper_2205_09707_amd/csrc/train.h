@@ -145,21 +145,28 @@ __device__ __forceinline__ LossParts loss_parts(const LossArgs &a, int live)
 __device__ __forceinline__ float score_factor(const LossArgs &a) { return fabsf(a.scale); }
 // The same for exponentials of base two.  A factor of zero would meet the infinities of entries that are left out; beside this one every
 // product that is not huge is nothing as well.
-__device__ __forceinline__ float exponent_factor(const LossArgs &a) { return fmaxf(fabsf(a.scale), 1e-30f) * LOG2E; }
+#define LEAST_FACTOR 1e-30f
+__device__ __forceinline__ float exponent_factor(const LossArgs &a) { return fmaxf(fabsf(a.scale), LEAST_FACTOR) * LOG2E; }
 
 // G of a row, in units of its d_loss's power of two, times 2^15 in fp16: of a product, by the score it is.  The target's is the probability less
 // one, formed so that it keeps its digits where the probability is almost one: its score is then `top`, rounded as the forward pass rounded it, so that
 // the difference is exactly nothing and what is left is the logarithm beside it.  (Fused into the subtraction the product would keep what `top` lost, 2^-24 of
 // the score, which is more than all the others' probabilities.)
+//
+// The others' differences from `top` are formed first, in one fused operation: the rounding of `top`, 2^-24 of the largest score, is what a probability is
+// off by beside the products' own.  (Exponent and shift each scaled to base two before, for one operation less, cost 2^-22: scores of 2^20 that differ by a
+// few units had probabilities off by a tenth.  Both directions of 7296 rows of 2048 on 128000 entries: 9280 to 9310 us in place of 9280.)
 struct ScoreGradient {
-    float scale, k, top, log_total, shift, factor;
+    float scale, top, log_total, shift, factor;
     __device__ __forceinline__ ScoreGradient(const LossRow &x, const LossArgs &a, int dtype)
-        : scale(score_factor(a)), k(exponent_factor(a)), top(x.top), log_total(x.log_total), shift((x.top + x.log_total) * LOG2E),
+        : scale(fmaxf(score_factor(a), LEAST_FACTOR)), top(x.top), log_total(x.log_total), shift(x.log_total * LOG2E),
           factor(x.fraction * (dtype == PLAID_FP16 ? 0x1p15f : 1.0f))
     {
     }
-    // (the shift's rounding, 2^-24 of a score, costs a probability less than its own rounding to the type while scores stay below 2^12)
-    __device__ __forceinline__ float other(float product) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(product, k, -shift)) * factor; }
+    __device__ __forceinline__ float other(float product) const
+    {
+        return __builtin_amdgcn_exp2f(__builtin_fmaf(__builtin_fmaf(product, scale, -top), LOG2E, -shift)) * factor;
+    }
     __device__ __forceinline__ float target(float product) const
     {
 #pragma clang fp contract(off)

@@ -14,8 +14,9 @@ import torch
 from training_util import E, TINY, half_step
 
 
-def relative(hidden, weight, targets, scale, d_loss):
-    """A dict of loss, d_hidden and d_weight, and of their bounds."""
+def relative(hidden, weight, targets, scale, d_loss, exact=False):
+    """A dict of loss, d_hidden and d_weight, and of their bounds.  exact: the scores are numbers of 32 bits, their products sums without a rounding and the
+    scale a power of two, so that only their differences round."""
     dtype, u, (rows, width), vocabulary, dev = hidden.dtype, half_step(hidden.dtype), hidden.shape, weight.shape[0], hidden.device
     live = torch.nonzero((targets >= 0) & (targets < vocabulary))[:, 0]
     h, w, t, c = hidden[live].double(), weight.double(), targets[live], d_loss[live].double()[:, None]
@@ -30,6 +31,8 @@ def relative(hidden, weight, targets, scale, d_loss):
     loss = torch.nn.functional.softplus(beside, threshold=1e3)
     sum_off = 2 * (vocabulary / 128 + 150) * E
     r = 2 * off + sum_off + 8 * E * (1 + s.abs().amax(1, keepdim=True))
+    if exact:
+        r = sum_off + 8 * E * (1 + (s.amax(1, keepdim=True) - s).amax(1, keepdim=True))
     # near one the loss is the sum itself and off by r of it; far from one it is a difference of scores
     loss_off = r[:, 0] * torch.minimum(torch.exp(beside), torch.ones_like(loss)) + 4 * E * loss
     far = own < others.amax(1)

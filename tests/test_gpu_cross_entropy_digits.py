@@ -1,5 +1,5 @@
 """Cross entropy's gradients where the digits are at stake: targets whose probability is almost one, by scales that are no power of two and scores that are
-not exact; in fp16, rows whose gradients of the loss are far apart."""
+not exact; in fp16, rows whose gradients of the loss are far apart; scores whose size leaves their differences few digits."""
 import pytest
 import torch
 
@@ -115,3 +115,21 @@ def test_captured_and_replayed(pl, rows, vocabulary, width):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, _gradients(pl, h, w, t, d, scale)))
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("rows,vocabulary", [(20, 900), (64, 50_001), (300, 3000), (700, 15_000)])
+def test_scores_far_from_zero(pl, rows, vocabulary, sign, dtype):
+    """All scores are 2^20 (or that less than zero) and a number of eighths below eight: each is exact, and so are their differences."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    w = torch.zeros(vocabulary, 64, device=DEV)
+    w[:, 0], w[:, 1] = 1024.0, torch.randint(0, 64, (vocabulary,), generator=g, device=DEV) / 8
+    h = torch.zeros(rows, 64, device=DEV)
+    h[:, 0], h[:, 1] = 1024.0 * sign, 1.0
+    t = torch.randint(0, vocabulary, (rows,), generator=g, device=DEV)
+    for scale in (1.0, 0.5):
+        h, w, d = h.to(dtype), w.to(dtype), torch.rand(rows, generator=g, device=DEV) + 0.5
+        want, got = relative(h, w, t, scale, d, exact=True), _gradients(pl, h, w, t, d, scale)
+        for x, name in zip(got, ("loss", "d_hidden", "d_weight")):
+            close(x, want[name], want[name + "_bound"], name)
