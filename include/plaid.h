@@ -471,10 +471,10 @@ int plaid_cross_entropy(const plaid_token_loss *args, void *workspace, int64_t w
 /* Its gradients, the scores formed again over a piece of the vocabulary at a time: with G_tv = d_loss[t] (exp(s_tv - lse[t]) - [v = target]),
  *   d_hidden[t] = scale sum_v G_tv weight[v],   d_weight[v] = scale sum_t G_tv hidden[t]   (contiguous, either may be NULL).
  * args->lse is what the forward call gave, args->loss is not looked at.  d_loss [rows] fp32, d_loss_stride 1, or 0: one number for all rows.
- * G rounds to the type before it is multiplied (what its targets' entries lose by that is multiplied too); the power of two of d_loss is kept
- * apart from it.  For d_weight the states carry that power and round to the type: what is lost of a row's is 2^-126 of the largest d_loss in
- * bf16, 2^-40 of the largest product of a state and its row's d_loss in fp16.  lse keeps a row's largest score in 32 bits: where scores are far from zero,
- * probabilities are off by 2^-24 of it, relative. */
+ * G rounds to the type before it is multiplied, in fp16 in steps of 2^-39 of the power of two above d_loss or more (what its targets' entries
+ * lose by that is multiplied too); that power is kept apart from it.  For d_weight the states carry it and round to the type: what is lost of
+ * a row's is 2^-126 of the largest d_loss in bf16, 2^-40 of the largest product of a state and its row's d_loss in fp16.  lse keeps a row's
+ * largest score in 32 bits: where scores are far from zero, probabilities are off by 2^-24 of it, relative. */
 int plaid_cross_entropy_backward(const plaid_token_loss *args, const float *d_loss, int64_t d_loss_stride, void *d_hidden, void *d_weight,
                                  void *workspace, int64_t workspace_bytes, int device, void *hip_stream);
 int plaid_cross_entropy_workspace(const plaid_token_loss *args, int32_t backward, int64_t *bytes);

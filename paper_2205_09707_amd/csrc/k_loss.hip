@@ -16,7 +16,7 @@
 // stays in its range however small the gradient of a mean is.  d_hidden takes it from the sums, in 32 bits, d_weight, whose sums go over the rows, in the
 // states, relative to state[1].  In bf16 that is the largest exponent.  fp16 would lose the digits of rows with a small d_loss below its normal range while the range
 // above is empty, so there the largest state of all rows, with its row's power, takes the type's last binade: the states of a row 2^-r of that one are exact down to
-// 2^(r - 29) of the row's own largest, and what rounds there rounds by 2^-40 of the largest of all.  (Finding it is a launch of its own, 2 to 3 us.)
+// 2^(r - 29) of the row's own largest, and what rounds there rounds by 2^-40 of the largest of all.  (Finding it is a launch of its own, 2.5 to 5 us.)
 __device__ __forceinline__ bool has_target(const LossArgs &a, int64_t t, int &target)
 {
     const int64_t v = a.targets[t];
